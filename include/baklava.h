@@ -136,6 +136,12 @@ typedef struct baklava_cache {
     const float*   kv_scale;           /* FP8 only: [L, Hkv, 4] = K scale, 1 / K scale, V scale, 1 / V scale */
 } baklava_cache;
 
+/* Where the rows of a [B, heads, T, D] tensor lie, for the calls that take any layout: element (b, h, t, d) is
+ * base[b * seq + h * head + t * token + d].  In elements, multiples of 8 (16 bytes). */
+typedef struct baklava_strides {
+    int64_t seq, head, token;
+} baklava_strides;
+
 /* Parameters of Algorithm 2 (threshold t, reduction r) and the bounds the paper leaves open. */
 typedef struct baklava_alloc_params {
     double        t;                 /* caches with importance < t are reduced                       */
@@ -202,6 +208,60 @@ int baklava_importance(const baklava_shape* shape, const float* head_cos, int32_
 int baklava_allocate(const baklava_shape* shape, const double* kv_importance,
                      const baklava_alloc_params* params, int64_t total_tokens,
                      int32_t* cap_out, int64_t* slab_off_out, int64_t* seq_stride_out);
+
+/* ------------------------------------------------------------------ queries and keys before attention
+ * What the model does between its QKV projection and Eq. 1, in one pass over the queries and keys of ONE layer:
+ * RMS norm of every head, y = x / sqrt(mean(x^2) + eps) * weight, then the rotary position embedding on the first
+ * rotary_dim elements, (a, b) -> (a cos - b sin, b cos + a sin) with the angle position * inv_freq[i] of pair i.
+ * Pair i is elements (i, i + rotary_dim / 2), or (2 i, 2 i + 1) with BAKLAVA_ROPE_INTERLEAVED.  Everything is held
+ * in fp32 (angles in fp64 up to their remainder) and rounded once.  Token (b, t) is at positions[b * T + t]; a
+ * negative position marks a token that sits out: it is not written.  A single decode step is T = 1 (or B = 1 and one
+ * token per sequence), with outputs laid out as baklava_decode_attn takes q and k_new.
+ *   q, k         device bf16, [B, Hq, T, D] and [B, Hkv, T, D] under their strides (e.g. slices of the projection)
+ *   positions    device int32 [B, T]
+ *   inv_freq     device fp32 [rotary_dim / 2]
+ *   rotary_dim   multiple of 16, at most D; the elements behind it are normed but not rotated
+ *   q_weight, k_weight   device bf16 [D], or NULL: that operand is rotated only (eps is then not used)
+ *   q_out, k_out device bf16 under their own strides; the same buffer and strides as the input is allowed (in place),
+ *                any other overlap is not */
+#define BAKLAVA_ROPE_INTERLEAVED   1u
+int baklava_qk_norm_rope(const baklava_shape* shape, const void* q, const baklava_strides* q_strides,
+                         const void* k, const baklava_strides* k_strides, const int32_t* positions,
+                         int32_t B, int32_t T, const float* inv_freq, int32_t rotary_dim,
+                         const void* q_weight, const void* k_weight, float eps, uint32_t flags,
+                         void* q_out, const baklava_strides* q_out_strides,
+                         void* k_out, const baklava_strides* k_out_strides, void* stream);
+
+/* ------------------------------------------------------------------ attention of a whole prompt (Eq. 1)
+ * out[b, h, i] = sum_{j <= i} softmax_j(q_i . k_j / sqrt(D)) v_j for every token i of every prompt and every query
+ * head of ONE layer (head h reads KV head h / g), with the rows' natural-log normalisers: the `lse` that
+ * baklava_prefill_scores takes.  The accumulators are fp32; the probabilities are rounded to bf16 for the product
+ * with V.  A row depends on the tokens up to its own only, whatever later tokens, padding or other prompts hold (NaN and
+ * infinities among them); rows at or past a prompt's end are not written.
+ *   q, out       device bf16 [B, Hq, T, D] under their strides (not overlapping)
+ *   k, v         device bf16 [B, Hkv, T, D] under their strides
+ *   prompt_len   device int32 [B] (clamped to 0 .. T) or NULL for len = T
+ *   lse          device fp32 [B, Hq, T], contiguous, or NULL
+ *   status       device word, OR of BAKLAVA_STATUS_* bits (the call never clears it).  TIMEOUT: a wait gave up and
+ *                some rows were not written */
+int baklava_prefill_attn(const baklava_shape* shape, const void* q, const baklava_strides* q_strides,
+                         const void* k, const baklava_strides* k_strides,
+                         const void* v, const baklava_strides* v_strides, const int32_t* prompt_len,
+                         int32_t B, int32_t T, void* out, const baklava_strides* out_strides, float* lse,
+                         uint32_t* status, void* stream);
+
+/* The same for prompts packed one after the other: tensors of `total` token rows ([Hq, total, D] under their
+ * strides; the sequence stride is not used), prompt b being rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1.
+ *   cu_seqlens   device int32 [B + 1], ascending, at most `total`; empty prompts are allowed
+ *   T            at least the longest prompt
+ *   lse          device fp32 [Hq, total], contiguous, or NULL
+ * A prompt whose bounds are not as described (or longer than T) is skipped with BAKLAVA_STATUS_BAD_STATE; rows that
+ * belong to no prompt are not written. */
+int baklava_prefill_attn_packed(const baklava_shape* shape, const void* q, const baklava_strides* q_strides,
+                                const void* k, const baklava_strides* k_strides,
+                                const void* v, const baklava_strides* v_strides, const int32_t* cu_seqlens,
+                                int32_t B, int32_t T, int64_t total, void* out, const baklava_strides* out_strides,
+                                float* lse, uint32_t* status, void* stream);
 
 /* ------------------------------------------------------------------ decode step (Eq. 4 - 7)
  * baklava_decode_plan (host): cut the heads of layers [layer_begin, layer_end) of B

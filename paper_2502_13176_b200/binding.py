@@ -19,6 +19,7 @@ FLAG_TEST_STALL = 256
 SCOPE_LAYER, SCOPE_MODEL = 0, 1
 STATUS_OVERFLOW, STATUS_BAD_STATE, STATUS_TIMEOUT = 1, 2, 4
 KV_BF16, KV_FP8_E4M3 = 0, 1
+ROPE_INTERLEAVED = 1
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libbaklava.so")
 _lib = None
@@ -43,6 +44,10 @@ class CacheStruct(ctypes.Structure):
                 ("len", c_void_p), ("free_slot", c_void_p), ("cap", c_void_p), ("slab_off", c_void_p),
                 ("seq_stride_tokens", c_int64), ("B", c_int32), ("status", c_void_p), ("kv_dtype", c_int32),
                 ("kv_scale", c_void_p)]
+
+
+class Strides(ctypes.Structure):
+    _fields_ = [("seq", c_int64), ("head", c_int64), ("token", c_int64)]
 
 
 class AllocParams(ctypes.Structure):
@@ -92,6 +97,12 @@ def lib():
                                              c_void_p, c_void_p, c_size_t, c_void_p]
         L.baklava_prefill_workspace_size.restype = c_size_t
         L.baklava_prefill_workspace_size.argtypes = [POINTER(Shape), c_int32, c_int32]
+        L.baklava_qk_norm_rope.argtypes = [POINTER(Shape), c_void_p, POINTER(Strides), c_void_p, POINTER(Strides), c_void_p,
+                                           c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_float, c_uint32,
+                                           c_void_p, POINTER(Strides), c_void_p, POINTER(Strides), c_void_p]
+        prompt = [POINTER(Shape)] + [c_void_p, POINTER(Strides)] * 3 + [c_void_p, c_int32, c_int32]
+        L.baklava_prefill_attn.argtypes = prompt + [c_void_p, POINTER(Strides), c_void_p, c_void_p, c_void_p]
+        L.baklava_prefill_attn_packed.argtypes = prompt + [c_int64, c_void_p, POINTER(Strides), c_void_p, c_void_p, c_void_p]
         L.baklava_output_error.argtypes = [c_void_p, c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
         L.baklava_output_error_workspace_size.restype = c_size_t
         L.baklava_output_error_workspace_size.argtypes = [c_int64]
@@ -309,6 +320,70 @@ def baklava_prefill_scores(shape, q, k, prompt_len, B, T, score, ws, stream=None
     _check(lib().baklava_prefill_scores(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(prompt_len), _ptr(lse), B, T, _ptr(score),
                                         _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)),
            "baklava_prefill_scores")
+
+
+def _here(t, what):
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, the current device is cuda:%d" % (what, t.device, torch.cuda.current_device()))
+
+
+def _rows(t, what, seqs, heads, tokens, D):
+    """Pointer and strides of a bf16 tensor [seqs, heads, tokens, D] (any view whose last dimension is contiguous)."""
+    st = t.stride()
+    if t.dtype != torch.bfloat16 or t.shape != (seqs, heads, tokens, D) or st[3] != 1:
+        raise ValueError("%s: expected bf16 [%d, %d, %d, %d] with contiguous rows, got %s %s with strides %s"
+                         % (what, seqs, heads, tokens, D, t.dtype, tuple(t.shape), st))
+    _here(t, what)
+    return c_void_p(t.data_ptr()), ctypes.byref(Strides(st[0], st[1], st[2]))
+
+
+def _dense(t, what, dtype, shape):
+    """Pointer of a contiguous tensor, NULL for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous %s tensor %s, got %s %s" % (what, dtype, shape, t.dtype, tuple(t.shape)))
+    _here(t, what)
+    return c_void_p(t.data_ptr())
+
+
+def baklava_qk_norm_rope(shape, q, k, positions, inv_freq, q_weight, k_weight, eps, q_out, k_out, flags=0, stream=None):
+    """q, q_out: bf16 [B, Hq, T, D], k, k_out: bf16 [B, Hkv, T, D], each any view with contiguous rows; positions: int32
+    [B, T]; inv_freq: float32 [rotary_dim / 2]; weights: bf16 [D] or None."""
+    B, _, T, D = q.shape
+    _check(lib().baklava_qk_norm_rope(ctypes.byref(shape), *_rows(q, "q", B, shape.Hq, T, shape.D),
+                                      *_rows(k, "k", B, shape.Hkv, T, shape.D), _dense(positions, "positions", torch.int32, (B, T)),
+                                      B, T, _dense(inv_freq, "inv_freq", torch.float32, (inv_freq.numel(),)),
+                                      2 * inv_freq.numel(), _dense(q_weight, "q_weight", torch.bfloat16, (D,)),
+                                      _dense(k_weight, "k_weight", torch.bfloat16, (D,)),
+                                      float(eps), int(flags), *_rows(q_out, "q_out", B, shape.Hq, T, shape.D),
+                                      *_rows(k_out, "k_out", B, shape.Hkv, T, shape.D), _stream(stream)), "baklava_qk_norm_rope")
+
+
+def baklava_prefill_attn(shape, q, k, v, prompt_len, out, lse, status, stream=None):
+    """q, out: bf16 [B, Hq, T, D], k, v: bf16 [B, Hkv, T, D], any views with contiguous rows; prompt_len: int32 [B] or None;
+    lse: float32 [B, Hq, T] or None; status: int32 [1]."""
+    B, _, T, D = q.shape
+    _check(lib().baklava_prefill_attn(ctypes.byref(shape), *_rows(q, "q", B, shape.Hq, T, shape.D),
+                                      *_rows(k, "k", B, shape.Hkv, T, shape.D), *_rows(v, "v", B, shape.Hkv, T, shape.D),
+                                      _dense(prompt_len, "prompt_len", torch.int32, (B,)), B, T,
+                                      *_rows(out, "out", B, shape.Hq, T, shape.D), _dense(lse, "lse", torch.float32, (B, shape.Hq, T)),
+                                      _dense(status, "status", torch.int32, (1,)), _stream(stream)), "baklava_prefill_attn")
+
+
+def baklava_prefill_attn_packed(shape, q, k, v, cu_seqlens, max_len, out, lse, status, stream=None):
+    """q, out: bf16 [Hq, total, D], k, v: bf16 [Hkv, total, D], any views with contiguous rows; cu_seqlens: int32 [B + 1];
+    lse: float32 [Hq, total] or None; status: int32 [1]."""
+    total, D = q.shape[1], shape.D
+    _check(lib().baklava_prefill_attn_packed(ctypes.byref(shape), *_rows(q.unsqueeze(0), "q", 1, shape.Hq, total, D),
+                                             *_rows(k.unsqueeze(0), "k", 1, shape.Hkv, total, D),
+                                             *_rows(v.unsqueeze(0), "v", 1, shape.Hkv, total, D),
+                                             _dense(cu_seqlens, "cu_seqlens", torch.int32, (cu_seqlens.numel(),)),
+                                             cu_seqlens.numel() - 1, int(max_len), total,
+                                             *_rows(out.unsqueeze(0), "out", 1, shape.Hq, total, D),
+                                             _dense(lse, "lse", torch.float32, (shape.Hq, total)),
+                                             _dense(status, "status", torch.int32, (1,)), _stream(stream)),
+           "baklava_prefill_attn_packed")
 
 
 def baklava_output_error(out, ref, loss, ws, stream=None):

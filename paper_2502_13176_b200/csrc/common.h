@@ -41,6 +41,17 @@ size_t baklava_decode_ws_bytes(const baklava_shape* s, int64_t n_items, int64_t 
 
 inline bool baklava_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Strides that can address [seqs, heads, tokens, D] without two elements in one place: multiples of 16 bytes and at least
+// a row apart where the extent is above 1 (those of extents of 1 are not used).  Byte strides stay below the 2^40 of
+// a tensor map.
+inline bool baklava_strides_ok(const baklava_strides* s, int64_t seqs, int64_t heads, int64_t tokens, int D) {
+    if (!s) return false;
+    const int64_t extent[3] = {seqs, heads, tokens}, stride[3] = {s->seq, s->head, s->token};
+    for (int i = 0; i < 3; ++i)
+        if (extent[i] > 1 && ((stride[i] & 7) != 0 || stride[i] < D || stride[i] > ((int64_t)1 << 38))) return false;
+    return true;
+}
+
 // prefill.cu: log2-domain largest logit of every causal query row (+inf past the prompt) into lse2 [B, Hq, T],
 // for the 128-row blocks listed in `list` (flat index ((b * Hq + h) * n_blk + blk), *list_count entries, both on
 // the device); `grid` CTAs share the list

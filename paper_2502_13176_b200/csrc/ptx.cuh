@@ -60,6 +60,11 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
+}
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
@@ -82,18 +87,42 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// Tensor map over bf16 [heads, T, D]: boxes of `box_rows` tokens x 64 elements of one head, 128-byte swizzle, zero
-// fill past T.  Host side; returns false if the driver entry point is missing or the encode fails.
-inline bool make_head_map(CUtensorMap* map, const void* base, int64_t heads, int T, int D, int box_rows = 64) {
+inline EncodeTiledFn encode_tiled() {
     static EncodeTiledFn enc = nullptr;
     if (!enc) {
         void* sym = nullptr;
         cudaDriverEntryPointQueryResult res;
         if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &res) != cudaSuccess ||
             res != cudaDriverEntryPointSuccess)
-            return false;
+            return nullptr;
         enc = reinterpret_cast<EncodeTiledFn>(sym);
     }
+    return enc;
+}
+
+// Tensor map over bf16 rows of D elements addressed as (token, head, sequence) with any strides (in elements,
+// multiples of 8; those of extents of 1 are not looked at): boxes of `box_rows` tokens x 64 elements, 128-byte
+// swizzle, zero fill past the last token.  Host side; false if the driver entry point is missing or the encode fails.
+inline bool make_tokens_map(CUtensorMap* map, const void* base, int D, int64_t tokens, int64_t heads, int64_t seqs,
+                            int64_t stride_token, int64_t stride_head, int64_t stride_seq, int box_rows) {
+    EncodeTiledFn enc = encode_tiled();
+    if (!enc) return false;
+    const cuuint64_t row = (cuuint64_t)D * 2;
+    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)tokens, (cuuint64_t)heads, (cuuint64_t)seqs};
+    const cuuint64_t strides[3] = {tokens > 1 ? (cuuint64_t)stride_token * 2 : row, heads > 1 ? (cuuint64_t)stride_head * 2 : row,
+                                   seqs > 1 ? (cuuint64_t)stride_seq * 2 : row};
+    const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Tensor map over bf16 [heads, T, D]: boxes of `box_rows` tokens x 64 elements of one head, 128-byte swizzle, zero
+// fill past T.  Host side; returns false if the driver entry point is missing or the encode fails.
+inline bool make_head_map(CUtensorMap* map, const void* base, int64_t heads, int T, int D, int box_rows = 64) {
+    EncodeTiledFn enc = encode_tiled();
+    if (!enc) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)T, (cuuint64_t)heads};
     const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)T * D * 2};
     const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};

@@ -1,0 +1,90 @@
+"""CPU tests of the argument checks of the prompt-side attention calls: refused before anything touches a device (the
+pointers are never dereferenced)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2502_13176_b200 import binding as bk
+from paper_2502_13176_b200 import build as bkbuild
+
+INVALID, SHAPE, UNSUPPORTED = -1, -2, -7
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    bkbuild.build()
+
+
+P = ctypes.c_void_p(1 << 20)
+
+
+def strides(seq, head, token):
+    return ctypes.byref(bk.Strides(seq, head, token))
+
+
+def rope(**kw):
+    B, T, Hq, Hkv, D = (kw.get(k, d) for k, d in (("B", 2), ("T", 8), ("Hq", 4), ("Hkv", 2), ("D", 64)))
+    sh = bk.make_shape(1, Hq, Hkv, D)
+    s = strides(Hq * T * D, T * D, D)
+    a = dict(shape=ctypes.byref(sh), q=P, qs=s, k=P, ks=s, pos=P, B=B, T=T, freq=P, rot=D, qw=None, kw=None, eps=1e-6, flags=0,
+             qo=P, qos=s, ko=P, kos=s, stream=None)
+    a.update({k: v for k, v in kw.items() if k in a})
+    return bk.lib().baklava_qk_norm_rope(*a.values())
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(q=None), INVALID), (dict(k=None), INVALID), (dict(pos=None), INVALID), (dict(freq=None), INVALID),
+    (dict(qo=None), INVALID), (dict(ko=None), INVALID), (dict(shape=None), INVALID),
+    (dict(q=ctypes.c_void_p((1 << 20) + 8)), INVALID), (dict(qw=ctypes.c_void_p((1 << 20) + 2)), INVALID),
+    (dict(pos=ctypes.c_void_p((1 << 20) + 2)), INVALID),
+    (dict(B=0), INVALID), (dict(T=0), INVALID), (dict(flags=2), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID),
+    (dict(rot=0), SHAPE), (dict(rot=8), SHAPE), (dict(rot=128), SHAPE), (dict(rot=40), SHAPE), (dict(D=80), SHAPE), (dict(Hq=5), SHAPE),
+    (dict(qs=None), INVALID), (dict(qos=strides(1024, 512, 0)), INVALID), (dict(kos=strides(1024, 32, 64)), INVALID),
+    (dict(ks=strides(1024, 512, 68)), INVALID), (dict(qs=strides(-2048, 512, 64)), INVALID),
+    (dict(B=1 << 17, T=1 << 15), UNSUPPORTED)])
+def test_norm_rope_refuses(kw, code):
+    assert rope(**kw) == code
+
+
+def attn(packed=False, **kw):
+    B, T, Hq, Hkv, D = (kw.get(k, d) for k, d in (("B", 2), ("T", 8), ("Hq", 4), ("Hkv", 2), ("D", 64)))
+    sh = bk.make_shape(1, Hq, Hkv, D)
+    s = strides(Hq * T * D, T * D, D)
+    a = dict(shape=ctypes.byref(sh), q=P, qs=s, k=P, ks=s, v=P, vs=s, len=P if packed else None, B=B, T=T)
+    if packed:
+        a["total"] = 16
+    a.update(out=P, os=s, lse=None, status=P, stream=None)
+    a.update({k: v for k, v in kw.items() if k in a})
+    return (bk.lib().baklava_prefill_attn_packed if packed else bk.lib().baklava_prefill_attn)(*a.values())
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("kw,code", [
+    (dict(q=None), INVALID), (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(out=None), INVALID), (dict(status=None), INVALID),
+    (dict(shape=None), INVALID), (dict(v=ctypes.c_void_p((1 << 20) + 4)), INVALID), (dict(lse=ctypes.c_void_p((1 << 20) + 2)), INVALID),
+    (dict(status=ctypes.c_void_p((1 << 20) + 1)), INVALID), (dict(len=ctypes.c_void_p((1 << 20) + 2)), INVALID),
+    (dict(B=0), INVALID), (dict(T=0), INVALID), (dict(T=-1), INVALID), (dict(B=65536), UNSUPPORTED), (dict(D=96), SHAPE), (dict(Hq=3), SHAPE),
+    (dict(Hq=18), SHAPE), (dict(qs=None), INVALID), (dict(os=strides(2048, 512, 32)), INVALID), (dict(ks=strides(2048, 516, 64)), INVALID),
+    (dict(vs=strides(2048, 0, 64)), INVALID)])
+def test_prompt_attention_refuses(packed, kw, code):
+    assert attn(packed, **kw) == code
+
+
+def test_packed_wants_bounds_and_rows():
+    assert attn(True, len=None) == INVALID
+    assert attn(True, total=0) == INVALID
+    assert attn(True, total=1 << 31) == UNSUPPORTED
+
+
+def test_binding_refuses_other_types_shapes_and_devices():
+    sh = bk.make_shape(1, 4, 2, 64)
+    good = torch.zeros((1, 4, 8, 64), dtype=torch.bfloat16)
+    kv = torch.zeros((1, 2, 8, 64), dtype=torch.bfloat16)
+    status = torch.zeros(1, dtype=torch.int32)
+    for q in (good.float(), good[:, :3], good[..., :32], good.transpose(2, 3)):
+        with pytest.raises(ValueError):
+            bk.baklava_prefill_attn(sh, q, kv, kv, None, good, None, status)
+    if not torch.cuda.is_available():
+        with pytest.raises((ValueError, RuntimeError, AssertionError)):      # host tensors
+            bk.baklava_prefill_attn(sh, good, kv, kv, None, good, None, status)
