@@ -86,6 +86,7 @@ extern "C" {
 
 #define BAKLAVA_KV_BF16            0
 #define BAKLAVA_KV_FP8_E4M3        1
+#define BAKLAVA_KV_INT4            2
 
 /* Model attention shape and retention policy. */
 typedef struct baklava_shape {
@@ -119,10 +120,18 @@ typedef struct baklava_shape {
  * baklava_decode_attn(_varlen) and baklava_evict(_varlen) quantise the rows they write (k_new / v_new,
  * the dense prompt) and read the slabs accordingly; queries stay bf16 (they must be finite in fp16:
  * |q| < 65504).  Only D = 128.  Everything else (positions, scores, policy) is unchanged.
+ *
+ * With kv_dtype = BAKLAVA_KV_INT4 a row is D / 2 bytes of 4-bit codes (an even channel in the low half of its byte)
+ * and one fp32 scale of its own for K and one for V, beside caller-chosen fp32 scales per channel of each (l, h) (keys
+ * and values have channels that stick out, and these take them out of the row's range).  With y = fl32(x * (1 /
+ * channel scale)) the row's scale is s = max |y| / 7 and an element's code is rint(y / s), ties to even, clamped to
+ * +-7, plus 8; it stands for (code - 8) * s * channel scale.  A row of zeros has s = 0 and codes 8.  Rows must be
+ * finite; a row with a NaN becomes NaN.  Queries may have any finite value.  Only D = 128.  baklava_evict in place moves
+ * the scales with their rows.
  */
 typedef struct baklava_cache {
-    void*          k_slab;             /* bf16 [B * seq_stride_tokens, D]        */
-    void*          v_slab;             /* bf16 [B * seq_stride_tokens, D]        */
+    void*          k_slab;             /* bf16 [B * seq_stride_tokens, D], or D bytes (FP8), D / 2 bytes (INT4) a row */
+    void*          v_slab;             /* the same                               */
     int32_t*       pos;                /* token position of each row             */
     float*         score;              /* accumulated attention of each row      */
     int32_t*       len;                /* [B, L, Hkv]                            */
@@ -132,8 +141,11 @@ typedef struct baklava_cache {
     int64_t        seq_stride_tokens;  /* rows per sequence                      */
     int32_t        B;
     uint32_t*      status;             /* one word, OR of BAKLAVA_STATUS_* bits  */
-    int32_t        kv_dtype;           /* BAKLAVA_KV_BF16 or BAKLAVA_KV_FP8_E4M3 */
-    const float*   kv_scale;           /* FP8 only: [L, Hkv, 4] = K scale, 1 / K scale, V scale, 1 / V scale */
+    int32_t        kv_dtype;           /* BAKLAVA_KV_*                           */
+    const float*   kv_scale;           /* FP8: [L, Hkv, 4] = K scale, 1 / K scale, V scale, 1 / V scale; INT4:      */
+                                       /*   [L, Hkv, 4, D], the same per channel; else not used                    */
+    float*         row_scale;          /* INT4 only (read for no other kv_dtype): [B * seq_stride_tokens, 2] = the  */
+                                       /*   rows' K and V scales, >= 0, written along with the rows                 */
 } baklava_cache;
 
 /* Where the rows of a [B, heads, T, D] tensor lie, for the calls that take any layout: element (b, h, t, d) is

@@ -18,7 +18,7 @@ FLAG_OVERLAP_PREV = 8
 FLAG_TEST_STALL = 256
 SCOPE_LAYER, SCOPE_MODEL = 0, 1
 STATUS_OVERFLOW, STATUS_BAD_STATE, STATUS_TIMEOUT = 1, 2, 4
-KV_BF16, KV_FP8_E4M3 = 0, 1
+KV_BF16, KV_FP8_E4M3, KV_INT4 = 0, 1, 2
 ROPE_INTERLEAVED = 1
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libbaklava.so")
@@ -43,7 +43,7 @@ class CacheStruct(ctypes.Structure):
     _fields_ = [("k_slab", c_void_p), ("v_slab", c_void_p), ("pos", c_void_p), ("score", c_void_p),
                 ("len", c_void_p), ("free_slot", c_void_p), ("cap", c_void_p), ("slab_off", c_void_p),
                 ("seq_stride_tokens", c_int64), ("B", c_int32), ("status", c_void_p), ("kv_dtype", c_int32),
-                ("kv_scale", c_void_p)]
+                ("kv_scale", c_void_p), ("row_scale", c_void_p)]
 
 
 class Strides(ctypes.Structure):
@@ -190,24 +190,33 @@ def baklava_decode_plan(shape, cap, B, layer_begin, layer_end, seq_stride_tokens
 
 
 # ------------------------------------------------------------------ device state
+def kv_row_bytes(D, kv_dtype):
+    """Bytes of one cached token's K and V (4-bit rows with their two scales)."""
+    return {KV_BF16: 4 * D, KV_FP8_E4M3: 2 * D, KV_INT4: D + 8}[kv_dtype]
+
+
 class Cache:
     """Device buffers of a budgeted cache plus the struct the library reads.  Memory only."""
 
     def __init__(self, shape, cap, slab_off, seq_stride, B, device="cuda", kv_dtype=KV_BF16, kv_scale=None):
         """kv_scale: float32 array [L, Hkv, 4] = (K scale, 1 / K scale, V scale, 1 / V scale) per head, for FP8
-        slabs; passed to the library as given."""
+        slabs; [L, Hkv, 4, D], the same per channel, for 4-bit slabs; passed to the library as given."""
         self.shape, self.B, self.seq_stride = shape, int(B), int(seq_stride)
         self.kv_dtype = int(kv_dtype)
         self.cap_host = np.ascontiguousarray(cap, dtype=np.int32).reshape(shape.L, shape.Hkv)
         self.off_host = np.ascontiguousarray(slab_off, dtype=np.int64).reshape(shape.L, shape.Hkv)
         rows = self.B * self.seq_stride
-        slab_type = torch.uint8 if self.kv_dtype == KV_FP8_E4M3 else torch.bfloat16
-        self.k_slab = torch.empty((rows, shape.D), dtype=slab_type, device=device)
-        self.v_slab = torch.empty((rows, shape.D), dtype=slab_type, device=device)
-        self.kv_scale = None
-        if self.kv_dtype == KV_FP8_E4M3:
-            self.kv_scale_host = np.ascontiguousarray(kv_scale, dtype=np.float32).reshape(shape.L, shape.Hkv, 4).copy()
+        slab_type = torch.bfloat16 if self.kv_dtype == KV_BF16 else torch.uint8
+        width = shape.D // 2 if self.kv_dtype == KV_INT4 else shape.D
+        self.k_slab = torch.empty((rows, width), dtype=slab_type, device=device)
+        self.v_slab = torch.empty((rows, width), dtype=slab_type, device=device)
+        self.kv_scale = self.row_scale = None
+        if self.kv_dtype != KV_BF16:
+            per_head = (4, shape.D) if self.kv_dtype == KV_INT4 else (4,)
+            self.kv_scale_host = np.ascontiguousarray(kv_scale, dtype=np.float32).reshape((shape.L, shape.Hkv) + per_head).copy()
             self.kv_scale = torch.from_numpy(self.kv_scale_host).to(device)
+        if self.kv_dtype == KV_INT4:
+            self.row_scale = torch.zeros((rows, 2), dtype=torch.float32, device=device)
         self.pos = torch.full((rows,), -1, dtype=torch.int32, device=device)
         self.score = torch.zeros((rows,), dtype=torch.float32, device=device)
         self.len = torch.zeros((self.B, shape.L, shape.Hkv), dtype=torch.int32, device=device)
@@ -219,7 +228,8 @@ class Cache:
                                   self.score.data_ptr(), self.len.data_ptr(), self.free_slot.data_ptr(),
                                   self.cap.data_ptr(), self.slab_off.data_ptr(), self.seq_stride, self.B,
                                   self.status.data_ptr(), self.kv_dtype,
-                                  None if self.kv_scale is None else self.kv_scale.data_ptr())
+                                  None if self.kv_scale is None else self.kv_scale.data_ptr(),
+                                  None if self.row_scale is None else self.row_scale.data_ptr())
 
     def reset(self):
         self.len.zero_()
@@ -233,7 +243,7 @@ class Cache:
 
     def kv_bytes_retained(self):
         """Bytes of K and V rows currently valid (the metric's numerator for one step)."""
-        return int(self.len.sum().item()) * self.shape.D * 2 * (1 if self.kv_dtype == KV_FP8_E4M3 else 2)
+        return int(self.len.sum().item()) * kv_row_bytes(self.shape.D, self.kv_dtype)
 
 
 def decode_workspace(plan, device="cuda"):

@@ -2,6 +2,7 @@
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -31,18 +32,20 @@ def build(force=False, verbose=False):
     """Build libbaklava.so if it is missing or older than its sources.  Returns its path."""
     if not force and not _stale():
         return LIB
-    objs = []
-    log = []
-    for src in SOURCES:
+    os.makedirs(os.path.join(HERE, "_build"), exist_ok=True)
+
+    def compile_one(src):
         obj = os.path.join(HERE, "_build", src + ".o")
-        os.makedirs(os.path.dirname(obj), exist_ok=True)
         cmd = [_nvcc(), *NVCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-x", "cu",
                "-c", os.path.join(CSRC, src), "-o", obj]
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        log.append(r.stderr)
+        return obj, subprocess.run(cmd, capture_output=True, text=True)
+
+    with ThreadPoolExecutor(len(SOURCES)) as pool:
+        done = list(pool.map(compile_one, SOURCES))
+    for src, (_, r) in zip(SOURCES, done):
         if r.returncode != 0:
             raise RuntimeError("nvcc failed for %s:\n%s\n%s" % (src, r.stdout, r.stderr))
-        objs.append(obj)
+    objs, log = [obj for obj, _ in done], [r.stderr for _, r in done]
     cmd = [_nvcc(), "-shared", "-o", LIB, *objs, "-cudart", "static"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

@@ -36,6 +36,7 @@ __host__ __device__
 constexpr int partial_floats(int g, int D) { return (g * D + 2 * g + 2 + 3) / 4 * 4; }
 
 int baklava_check_shape(const baklava_shape* s);
+int baklava_check_kv_format(const baklava_shape* s, const baklava_cache* cache);   // kv_dtype, what it needs, the head sizes it has
 size_t baklava_decode_ws_bytes(const baklava_shape* s, int64_t n_items, int64_t n_score_items, int64_t n_units, int32_t B,
                                int64_t seq_stride_tokens, DecodeWorkspace* layout);
 

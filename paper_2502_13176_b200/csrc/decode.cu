@@ -27,6 +27,7 @@
 #include "baklava.h"
 #include "common.h"
 #include "fp8.cuh"
+#include "int4.cuh"
 #include "ptx.cuh"
 
 namespace {
@@ -49,6 +50,10 @@ constexpr int kStages = 2;                              // bf16 slabs: two 32 KB
 constexpr int kFp8StageTokens = 128;
 constexpr int kFp8Stages = 2;
 constexpr int kFp8CtasPerSm = 3;
+// 4-bit slabs: a row is 64 bytes of codes and a pair of scales, so that 256-token stages are the same 32 KB (+ 2 KB)
+constexpr int kInt4StageTokens = 256;
+constexpr int kInt4Stages = 2;
+constexpr int kInt4CtasPerSm = 3;
 constexpr int kMaxStages = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -88,7 +93,9 @@ struct DecodeParams {
     unsigned long long* best_key;  // [n_score_items]: each piece's eviction candidate (split tail only)
     int32_t* best_slot;            // [n_score_items]
     float scale_log2;   // log2(e) / sqrt(D)
-    const float* kv_scale;   // FP8 slabs: [L, Hkv, 4] (K scale, its reciprocal, V scale, its reciprocal)
+    const float* kv_scale;   // FP8 slabs: [L, Hkv, 4] (K scale, its reciprocal, V scale, its reciprocal);
+                             // 4-bit slabs: [L, Hkv, 4, D], the same per channel
+    float* row_scale;        // 4-bit slabs: [rows, 2] (K, V)
     long long wait_cycles;   // SM clock cycles after which a wait on a tile gives up
 };
 
@@ -638,19 +645,34 @@ __device__ __noinline__ void finish_head(const DecodeParams* pp, float* scratch,
 // ldmatrix (16-bit granules) serve one-byte data: four consecutive bytes of a K row land in one register
 // and become two fp16 pairs; V comes through ldmatrix.trans as two tokens x two adjacent channels per
 // register, which a byte permute splits into an even-channel and an odd-channel operand.
-template <int D, bool kByPosition, bool kFp8>
-__global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) decode_chunk_kernel(const __grid_constant__ DecodeParams p,
-                                                                const __grid_constant__ CUtensorMap k_map,
-                                                                const __grid_constant__ CUtensorMap v_map) {
+//
+// 4-bit slabs (kKv = BAKLAVA_KV_INT4): a code is u = 1 .. 15 and stands for (u - 8) * row scale * channel scale.
+// Everything but the codes is linear in something that is applied once, so that widening them costs little more than
+// one AND per MMA register:
+//   - four bits in the low or second nibble of a 16-bit word ARE the fp16 number u * 2^-24 or u * 2^-20 (a subnormal,
+//     which the MMA takes exactly), and a 32-bit word of eight codes gives the four register pairs of two MMAs by
+//     masking, with one shift; the factor 16 between the two kinds is taken off the other operand (K) or the result (V);
+//   - the offset: sum_d (u - 8) q_d = sum_d u q_d - 8 sum_d q_d, the accumulator's initial value; for V the same with
+//     8 sum_t p_t, which one more MMA against a constant operand sums from the very probabilities that were used;
+//   - the K channel scales are multiplied into the query, the V channel scales into the partial output, the K row
+//     scales into the logits, the V row scales into the probabilities (relative to the largest one met so far, which
+//     is handled like the running maximum: fp16 holds what is at most 1).
+// The scaled query is brought to 2^12 and split into two fp16 terms (22 significant bits): one term (11 bits) would
+// shift every logit of a head by a common error of 1e-4.
+template <int D, bool kByPosition, int kKv>
+__global__ void __launch_bounds__(kThreads, kKv == BAKLAVA_KV_INT4 ? kInt4CtasPerSm : kKv == BAKLAVA_KV_FP8_E4M3 ? kFp8CtasPerSm : kCtasPerSm)
+decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constant__ CUtensorMap k_map,
+                    const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap s_map) {
+    constexpr bool kFp8 = kKv == BAKLAVA_KV_FP8_E4M3, kInt4 = kKv == BAKLAVA_KV_INT4;
     constexpr int kKSteps = D / 16;                    // MMA k-steps over the head dimension
-    constexpr int kNTiles = D / 8;                     // 8-wide output column blocks
-    constexpr int kTT = kFp8 ? kFp8StageTokens : kTileTokens;       // tokens per stage
-    constexpr int kNS = kFp8 ? kFp8Stages : kStages;            // stages of the ring
+    constexpr int kTT = kInt4 ? kInt4StageTokens : kFp8 ? kFp8StageTokens : kTileTokens;       // tokens per stage
+    constexpr int kNS = kInt4 ? kInt4Stages : kFp8 ? kFp8Stages : kStages;            // stages of the ring
     constexpr int kBlocks = kTT / (kConsumerWarps * kWarpTokens);    // 16-token blocks per warp and stage
     static_assert(kBlocks >= 1 && kNS <= kMaxStages, "a stage holds at least one 16-token block per warp");
-    constexpr int kRowBytes = kFp8 ? D : 2 * D;
+    constexpr int kRowBytes = kInt4 ? D / 2 : kFp8 ? D : 2 * D;
     constexpr int kTileBytes = kTT * kRowBytes;        // one K (or V) tile
-    constexpr int kStageBytes = 2 * kTileBytes;
+    constexpr int kScaleBytes = kInt4 ? kTT * 8 : 0;   // the rows' pairs of scales
+    constexpr int kStageBytes = 2 * kTileBytes + kScaleBytes;
     constexpr int kG = BAKLAVA_MAX_GROUP;
 
     extern __shared__ uint8_t smem_raw[];
@@ -683,6 +705,7 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
         ptx::fence_mbar_init();
         prefetch_tensormap(&k_map);
         prefetch_tensormap(&v_map);
+        if (kInt4) prefetch_tensormap(&s_map);
     }
     if (!overlap) grid_dependency_wait();                 // len / free_slot / slab rows / items come from earlier kernels
     else launch_dependents();
@@ -743,6 +766,8 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
     float o[D / 16][4];
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) { o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.0f; }
+    float o8[4] = {0.0f, 0.0f, 0.0f, 0.0f};               // 4-bit slabs: eight times the sums of the probabilities used
+    float v_ref = 0.0f;                                   // 4-bit slabs: largest V row scale met, what they are relative to
 
     if (warp == kConsumerWarps) {
         // ---------------- producer: one lane issues the TMA loads
@@ -765,7 +790,11 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
                 const uint32_t dst = ring + s * kStageBytes;
                 const int y = (int)(row0 + begin + it * kTT);
                 mbar_arrive_expect_tx(full, kStageBytes);
-                if (kFp8) {                                  // one 128-byte-wide box holds the whole row
+                if (kInt4) {                                 // 64-byte rows; sixteen rows' scales are one row of their map
+                    tma_load_2d(dst, &k_map, 0, y, full, stream_policy);
+                    tma_load_2d(dst + kTileBytes, &v_map, 0, y, full, stream_policy);
+                    tma_load_2d(dst + 2 * kTileBytes, &s_map, 0, y >> 4, full, stream_policy);
+                } else if (kFp8) {                           // one 128-byte-wide box holds the whole row
                     tma_load_2d(dst, &k_map, 0, y, full, stream_policy);
                     tma_load_2d(dst + kTileBytes, &v_map, 0, y, full, stream_policy);
                 } else {
@@ -784,8 +813,56 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
         // channels 2 t, 2 t + 1 (q0) and 8 + 2 t, 9 + 2 t (q1); for FP8 slabs the channels 4 t .. 4 t + 3, the order
         // in which the four bytes of a K register arrive (the contraction index may be permuted at will)
         uint32_t qq[2 * kKSteps];                          // (q0, q1) of step ks side by side, as the MMA takes them
-        {
-            const __nv_bfloat16* q_ptr = p.q + ((int64_t)(u.li * p.B + u.b) * p.Hq + u.h * G + g8) * D;
+        uint32_t ql[kInt4 ? 2 * kKSteps : 1];              // 4-bit slabs: the second fp16 term of the same
+        float q_off[2] = {0.0f, 0.0f}, q_fac[2] = {1.0f, 1.0f};   // 4-bit slabs, this lane's two heads: offset, factor
+        const __nv_bfloat16* q_ptr = p.q + ((int64_t)(u.li * p.B + u.b) * p.Hq + u.h * G + g8) * D;
+        if (kInt4) {
+            // lane t holds, of each group of 32 channels, the eight of word t of a K row's 16 bytes
+            float x[D / 4];
+            float big = 0.0f;
+            const float* chan = p.kv_scale + (int64_t)u.head * 4 * D;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                const uint4 raw = g8 < G ? *reinterpret_cast<const uint4*>(q_ptr + 32 * c + 8 * t4) : make_uint4(0u, 0u, 0u, 0u);
+                const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
+                    const float2 cs = *reinterpret_cast<const float2*>(chan + 32 * c + 8 * t4 + 2 * i);
+                    x[8 * c + 2 * i] = f.x * cs.x;
+                    x[8 * c + 2 * i + 1] = f.y * cs.y;
+                    big = fmaxf(big, fmaxf(fabsf(x[8 * c + 2 * i]), fabsf(x[8 * c + 2 * i + 1])));
+                }
+            }
+            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+            // to [2^12, 2^13): a power of two, which the logits are multiplied by again (with the codes' 2^24)
+            const int ex = min(max((int)(__float_as_uint(big) >> 23), 32), 222);     // biased exponent
+            const float up = __uint_as_float((uint32_t)(127 + 12 + 127 - ex) << 23);
+            const float back = __uint_as_float((uint32_t)(ex - 12 + 24) << 23);
+            float sum = 0.0f;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {              // nibbles (j, j + 4) of the word
+                    const float k = (j & 1) ? 0.0625f : 1.0f;      // odd nibbles stand 16 times higher
+                    const float a = x[8 * c + j] * up * k, b = x[8 * c + j + 4] * up * k;
+                    const uint32_t hi = pack_f16(a, b);
+                    const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+                    const uint32_t lo = pack_f16(a - h.x, b - h.y);
+                    const float2 l = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+                    qq[4 * c + j] = hi;
+                    ql[4 * c + j] = lo;
+                    sum = fmaf((h.x + l.x) + (h.y + l.y), (j & 1) ? 16.0f : 1.0f, sum);
+                }
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                q_off[e] = -8.0f * 0x1p-24f * __shfl_sync(0xffffffffu, sum, 4 * (2 * t4 + e));
+                q_fac[e] = __shfl_sync(0xffffffffu, back, 4 * (2 * t4 + e)) * p.scale_log2;
+            }
+        } else {
 #pragma unroll
             for (int ks = 0; ks < kKSteps; ++ks) {
                 if (kFp8) {
@@ -812,6 +889,9 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
         // V load (rows of the MMA = channels) it is the other way round.
         const uint32_t k_lane = kFp8 ? (uint32_t)(((lm >> 1) * 8 + li8) * 128 + ((li8 ^ (lm & 1)) << 4))    // rows (lm / 2) * 8 + .., b = lm % 2
                                      : (uint32_t)(((lm & 1) * 8 + li8) * 128 + ((li8 ^ (lm >> 1)) << 4));   // rows (lm % 2) * 8 + .., b = lm / 2
+        // 4-bit rows are 64 bytes, written with the 64-byte swizzle (piece c of row r at position c ^ (r / 2 % 4)); the
+        // same addresses serve K and the transposed V: matrices (token half) x (16-byte piece)
+        const uint32_t n_lane = (uint32_t)(((lm & 1) * 8 + li8) * 64 + (((lm >> 1) ^ (li8 >> 1)) << 4));
         const uint32_t v_lane = kFp8 ? (uint32_t)(((lm & 1) * 8 + li8) * 128 + ((li8 ^ (lm >> 1)) << 4))
                                      : (uint32_t)(((lm >> 1) * 8 + li8) * 128 + ((li8 ^ (lm & 1)) << 4));
         // where this lane leaves the probabilities of head g8 (tokens 2 t4, 2 t4 + 1 of a block) for the score pass
@@ -846,7 +926,29 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
                             const int64_t src = ((int64_t)(u.li * p.B + u.b) * p.Hkv + u.h) * D;
                             const int64_t row = row0 + hs.f;
                             uint8_t* k_ptr = ring_ptr + s * kStageBytes;
-                            if (kFp8) {                      // quantise the row: eight elements per lane and operand
+                            if (kInt4) {                     // quantise the row: four elements per lane, both operands
+                                const float* chan = p.kv_scale + (int64_t)u.head * 4 * D;
+                                const int r = r0 + (hs.f - tok0);
+#pragma unroll
+                                for (int is_v = 0; is_v < 2; ++is_v) {
+                                    const uint2 raw = *(reinterpret_cast<const uint2*>((is_v ? p.v_new : p.k_new) + src) + lane);
+                                    const float4 inv = *(reinterpret_cast<const float4*>(chan + (2 * is_v + 1) * D) + lane);
+                                    float y[4];
+                                    int4q::scaled4(raw, inv, y);
+                                    uint32_t top = int4q::largest_bits(y);
+                                    top = __reduce_max_sync(0xffffffffu, top);
+                                    const float rs = int4q::row_scale(top);
+                                    const uint16_t val = (uint16_t)int4q::codes4(y, rs);
+                                    *reinterpret_cast<uint16_t*>(k_ptr + is_v * kTileBytes + r * 64 +
+                                                                 (((lane >> 3) ^ ((r >> 1) & 3)) << 4) + (lane & 7) * 2) = val;
+                                    uint8_t* slab = reinterpret_cast<uint8_t*>(is_v ? p.v_slab : p.k_slab);
+                                    *(reinterpret_cast<uint16_t*>(slab + row * kRowBytes) + lane) = val;
+                                    if (lane == 0) {
+                                        reinterpret_cast<float*>(k_ptr + 2 * kTileBytes)[2 * r + is_v] = rs;
+                                        p.row_scale[2 * row + is_v] = rs;
+                                    }
+                                }
+                            } else if (kFp8) {               // quantise the row: eight elements per lane and operand
                                 for (int i = lane; i < 2 * kVec; i += 32) {
                                     const bool is_v = i >= kVec;
                                     const int c = is_v ? i - kVec : i;
@@ -870,7 +972,8 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
                             __syncwarp();
                         }
                         // rows past the end of the head (or the freed slot) may hold anything: keep them out of P.V
-                        if (valid < kWarpTokens || (hole >= tok0 && hole < tok0 + kWarpTokens)) {
+                        // (4-bit codes are finite whatever they are; the rows' scales are left out below)
+                        if (!kInt4) if (valid < kWarpTokens || (hole >= tok0 && hole < tok0 + kWarpTokens)) {
                             uint8_t* v_ptr = ring_ptr + s * kStageBytes + kTileBytes;
                             constexpr int kPieces = kRowBytes / 16;     // 16-byte pieces of a row
                             for (int i = lane; i < kWarpTokens * kPieces; i += 32) {
@@ -888,7 +991,30 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
                 for (int blk = 0; blk < kBlocks; ++blk) {
                     st[blk][0] = st[blk][1] = st[blk][2] = st[blk][3] = 0.0f;
                     const uint32_t k_row = k_tile + (uint32_t)((w0 + blk * kWarpTokens) * 128) + k_lane;
-                    if (kFp8) {
+                    if (kInt4) {
+                        st[blk][0] = st[blk][2] = q_off[0];
+                        st[blk][1] = st[blk][3] = q_off[1];
+                        const uint32_t n_row = k_tile + (uint32_t)((w0 + blk * kWarpTokens) * 64);
+#pragma unroll
+                        for (int cc = 0; cc < D / 64; ++cc) {     // 64 channels per load: (tokens 0-7 | 8-15) x two pieces
+                            uint32_t kb[4];
+                            ldmatrix_x4(n_row + (n_lane ^ (uint32_t)(cc << 5)), kb);
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                const int c = 2 * cc + x;
+                                uint32_t lo = kb[2 * x], hi = kb[2 * x + 1];
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {     // nibbles (0, 4 | 1, 5), then (2, 6 | 3, 7)
+                                    const uint32_t a0 = lo & 0x000f000fu, a1 = hi & 0x000f000fu;
+                                    const uint32_t a2 = lo & 0x00f000f0u, a3 = hi & 0x00f000f0u;
+                                    mma_f16_full(st[blk], a0, a1, a2, a3, qq[4 * c + 2 * j], qq[4 * c + 2 * j + 1]);
+                                    mma_f16_full(st[blk], a0, a1, a2, a3, ql[4 * c + 2 * j], ql[4 * c + 2 * j + 1]);
+                                    lo >>= 8;
+                                    hi >>= 8;
+                                }
+                            }
+                        }
+                    } else if (kFp8) {
 #pragma unroll
                         for (int kk = 0; kk < D / 32; ++kk) {     // 32 channels per load: two steps of 16
                             uint32_t kb[4];      // (tokens 0-7 | 8-15) x (channels 0-15 | 16-31), four bytes per lane
@@ -913,15 +1039,25 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
                 // online softmax for the two heads of this lane over the warp's tokens of the stage
                 float mx[2] = {-INFINITY, -INFINITY};
                 bool ok[kBlocks][2];
+                float sv[kInt4 ? kBlocks : 1][2];             // 4-bit slabs: V scales of this lane's rows
+                float sv_max = 0.0f;
 #pragma unroll
                 for (int blk = 0; blk < kBlocks; ++blk)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
                         const int tok = wtok0 + blk * kWarpTokens + g8 + 8 * r;
                         ok[blk][r] = !kCareful || (tok < end && tok != hole);
+                        float sk = scale_k;
+                        if (kInt4) {
+                            const float2 rs = reinterpret_cast<const float2*>(ring_ptr + s * kStageBytes + 2 * kTileBytes)
+                                                  [w0 + blk * kWarpTokens + g8 + 8 * r];
+                            sk = rs.x;
+                            sv[blk][r] = ok[blk][r] ? rs.y : 0.0f;
+                            sv_max = fmaxf(sv_max, fabsf(sv[blk][r]));
+                        }
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            st[blk][2 * r + e] *= scale_k;
+                            st[blk][2 * r + e] *= kInt4 ? sk * q_fac[e] : sk;
                             if (ok[blk][r]) mx[e] = fmaxf(mx[e], st[blk][2 * r + e]);
                         }
                     }
@@ -948,9 +1084,21 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
                         }
                 l_run[0] = l_run[0] * corr[0] + psum[0];
                 l_run[1] = l_run[1] * corr[1] + psum[1];
+                float v_inv = 0.0f;
+                if (kInt4) {                                  // the V scales' reference follows their maximum
+                    const float seen = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv_max)));
+                    if (seen > v_ref) {
+                        const float ratio = v_ref / seen;
+                        corr[0] *= ratio;
+                        corr[1] *= ratio;
+                        v_ref = seen;
+                    }
+                    v_inv = v_ref > 0.0f ? 1.0f / v_ref : 0.0f;
+                }
                 if (__any_sync(0xffffffffu, corr[0] != 1.0f || corr[1] != 1.0f)) {
 #pragma unroll
                     for (int j = 0; j < D / 16; ++j) { o[j][0] *= corr[0]; o[j][1] *= corr[1]; o[j][2] *= corr[0]; o[j][3] *= corr[1]; }
+                    if (kInt4) { o8[0] *= corr[0]; o8[1] *= corr[1]; o8[2] *= corr[0]; o8[3] *= corr[1]; }
                 }
                 // P^T as the B operand of O^T += V^T P^T: the 8 x 8 blocks (tokens x heads) this warp holds one
                 // row per quad are transposed, so that lane (g, t) gets head g, tokens 2 t, 2 t + 1 (and + 8)
@@ -960,7 +1108,11 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
                     const int tok0 = wtok0 + blk * kWarpTokens;
                     const uint32_t h0 = movmatrix_trans(pack_f16(st[blk][0], st[blk][1]));
                     const uint32_t h1 = movmatrix_trans(pack_f16(st[blk][2], st[blk][3]));
-                    if (kFp8) {
+                    if (kInt4) {
+                        const float s0 = sv[blk][0] * v_inv, s1 = sv[blk][1] * v_inv;
+                        pb[blk][0] = movmatrix_trans(pack_f16(st[blk][0] * s0, st[blk][1] * s0));
+                        pb[blk][1] = movmatrix_trans(pack_f16(st[blk][2] * s1, st[blk][3] * s1));
+                    } else if (kFp8) {
                         pb[blk][0] = h0; pb[blk][1] = h1;
                     } else {
                         pb[blk][0] = movmatrix_trans(pack_bf16(st[blk][0], st[blk][1]));
@@ -990,7 +1142,28 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
 #pragma unroll
                 for (int blk = 0; blk < kBlocks; ++blk) {
                     const uint32_t v_row = v_tile + (uint32_t)((w0 + blk * kWarpTokens) * 128) + v_lane;
-                    if (kFp8) {
+                    if (kInt4) {
+                        // a register of the transposed load = two tokens x four adjacent channels; row g of MMA j is
+                        // channel 4 g + 2 j of the 32-channel group, row g + 8 channel 4 g + 2 j + 1 (16 times too large)
+                        const uint32_t n_row = v_tile + (uint32_t)((w0 + blk * kWarpTokens) * 64);
+                        mma_f16_full(o8, 0x00080008u, 0x00800080u, 0x00080008u, 0x00800080u, pb[blk][0], pb[blk][1]);
+#pragma unroll
+                        for (int cc = 0; cc < D / 64; ++cc) {
+                            uint32_t vb[4];
+                            ldmatrix_x4_trans(n_row + (n_lane ^ (uint32_t)(cc << 5)), vb);
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                uint32_t lo = vb[2 * x], hi = vb[2 * x + 1];     // tokens 0-7 and 8-15 of the block
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    mma_f16_full(o[4 * cc + 2 * x + j], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu,
+                                                 hi & 0x00f000f0u, pb[blk][0], pb[blk][1]);
+                                    lo >>= 8;
+                                    hi >>= 8;
+                                }
+                            }
+                        }
+                    } else if (kFp8) {
                         // a register of the transposed load = two tokens x two adjacent channels; the permute puts the
                         // even channel's token pair in the low half and the odd channel's in the high half.  Row g of
                         // the MMA is channel 2 g of the 16-channel group, row g + 8 channel 2 g + 1.
@@ -1069,7 +1242,8 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
             l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 8);
             l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 16);
         }
-        const float sv_ = kFp8 ? p.kv_scale[u.head * 4 + 2] : 1.0f;
+        const float sv_ = kInt4 ? v_ref * 0x1p24f : kFp8 ? p.kv_scale[u.head * 4 + 2] : 1.0f;
+        const float* v_chan = kInt4 ? p.kv_scale + ((int64_t)u.head * 4 + 2) * D : nullptr;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int head = 2 * t4 + e;
@@ -1077,7 +1251,12 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
                 float* dst = sm_o + (warp * G + head) * D;
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
-                    if (kFp8) {                             // rows g and g + 8 of the MMA are channels 2 g and 2 g + 1
+                    if (kInt4) {                            // rows g and g + 8: channels 4 g + 2 j, 4 g + 2 j + 1 of 32
+                        const int ch = 32 * (c >> 1) + 4 * g8 + 2 * (c & 1);
+                        const float2 cs = *reinterpret_cast<const float2*>(v_chan + ch);
+                        *reinterpret_cast<float2*>(dst + ch) = make_float2((o[c][e] - o8[e]) * sv_ * cs.x,
+                                                                           (o[c][2 + e] - o8[2 + e]) * (sv_ * 0.0625f) * cs.y);
+                    } else if (kFp8) {                      // rows g and g + 8 of the MMA are channels 2 g and 2 g + 1
                         *reinterpret_cast<float2*>(dst + 16 * c + 2 * g8) = make_float2(o[c][e] * sv_, o[c][2 + e] * sv_);
                     } else {
                         dst[16 * c + g8] = o[c][e];
@@ -1324,16 +1503,46 @@ bool make_slab_map_fp8(CUtensorMap* map, void* base, int64_t rows, int D) {
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool kByPosition, bool kFp8 = false>
-cudaError_t launch_chunks(const DecodeParams& p, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t s) {
-    constexpr int kSmem = (kFp8 ? kFp8Stages * 2 * kFp8StageTokens * D : kStages * 2 * kTileTokens * D * 2) + 1024;
+// 4-bit slabs: D / 2 bytes per row, boxes of one stage's rows x 64 bytes (the whole row), 64-byte swizzle
+bool make_slab_map_int4(CUtensorMap* map, void* base, int64_t rows, int D) {
+    EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)D / 2, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)D / 2};
+    const cuuint32_t box[2] = {(cuuint32_t)D / 2, (cuuint32_t)kInt4StageTokens};
+    const cuuint32_t estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The rows' pairs of scales, sixteen rows (128 bytes) to a row of the map (rows come in multiples of 16): the second
+// coordinate stays in 32 bits however long the cache, and a stage is one box.
+bool make_scale_map_int4(CUtensorMap* map, void* base, int64_t rows) {
+    EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {32, (cuuint64_t)rows / 16};
+    const cuuint64_t strides[1] = {128};
+    const cuuint32_t box[2] = {32, (cuuint32_t)kInt4StageTokens / 16};
+    const cuuint32_t estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool kByPosition, int kKv = BAKLAVA_KV_BF16>
+cudaError_t launch_chunks(const DecodeParams& p, const CUtensorMap& km, const CUtensorMap& vm, const CUtensorMap& sm,
+                          cudaStream_t s) {
+    constexpr int kRing = kKv == BAKLAVA_KV_INT4 ? kInt4Stages * kInt4StageTokens * (D + 8)
+                          : kKv == BAKLAVA_KV_FP8_E4M3 ? kFp8Stages * 2 * kFp8StageTokens * D : kStages * 2 * kTileTokens * D * 2;
+    constexpr int kSmem = kRing + 1024;
     // the attribute belongs to the function on the current device: set once per device and instantiation
     static std::atomic<uint64_t> configured{0};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !(configured.load(std::memory_order_acquire) >> dev & 1)) {
-        e = cudaFuncSetAttribute(decode_chunk_kernel<D, kByPosition, kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        e = cudaFuncSetAttribute(decode_chunk_kernel<D, kByPosition, kKv>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (e != cudaSuccess) return e;
         if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
     }
@@ -1347,7 +1556,7 @@ cudaError_t launch_chunks(const DecodeParams& p, const CUtensorMap& km, const CU
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, decode_chunk_kernel<D, kByPosition, kFp8>, p, km, vm);
+    return cudaLaunchKernelEx(&cfg, decode_chunk_kernel<D, kByPosition, kKv>, p, km, vm, sm);
 }
 
 }  // namespace
@@ -1387,12 +1596,15 @@ int decode_attn_impl(
                                                 cache->seq_stride_tokens, &lay);
     if (ws_bytes < need) return BAKLAVA_ERR_WORKSPACE;
 
-    const bool quantised = cache->kv_dtype == BAKLAVA_KV_FP8_E4M3;
-    if (cache->kv_dtype != BAKLAVA_KV_BF16 && !quantised) return BAKLAVA_ERR_INVALID_ARG;
-    if (quantised && !cache->kv_scale) return BAKLAVA_ERR_INVALID_ARG;
-    if (quantised && shape->D != 128) return BAKLAVA_ERR_UNSUPPORTED;
-    CUtensorMap k_map, v_map;
-    if (quantised) {
+    rc = baklava_check_kv_format(shape, cache);
+    if (rc) return rc;
+    const bool fp8 = cache->kv_dtype == BAKLAVA_KV_FP8_E4M3, four_bit = cache->kv_dtype == BAKLAVA_KV_INT4;
+    CUtensorMap k_map, v_map, s_map = {};
+    if (four_bit) {
+        if (!make_slab_map_int4(&k_map, cache->k_slab, rows, shape->D) || !make_slab_map_int4(&v_map, cache->v_slab, rows, shape->D) ||
+            !make_scale_map_int4(&s_map, cache->row_scale, rows))
+            return BAKLAVA_ERR_CUDA;
+    } else if (fp8) {
         if (!make_slab_map_fp8(&k_map, cache->k_slab, rows, shape->D) || !make_slab_map_fp8(&v_map, cache->v_slab, rows, shape->D))
             return BAKLAVA_ERR_CUDA;
     } else if (!make_slab_map(&k_map, cache->k_slab, rows, shape->D) || !make_slab_map(&v_map, cache->v_slab, rows, shape->D)) {
@@ -1441,13 +1653,15 @@ int decode_attn_impl(
     p.split_tail = info->n_score_items > 0 && !(p.flags & (BAKLAVA_FLAG_NO_SCORE | BAKLAVA_FLAG_OVERLAP_PREV));
     p.scale_log2 = kLog2e / sqrtf((float)shape->D);
     p.kv_scale = cache->kv_scale;
+    p.row_scale = four_bit ? cache->row_scale : nullptr;
     p.wait_cycles = g_wait_cycles.load(std::memory_order_relaxed);
 
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t err = cudaSuccess;
-    if (quantised) err = p.window_evict ? launch_chunks<128, true, true>(p, k_map, v_map, s) : launch_chunks<128, false, true>(p, k_map, v_map, s);
-    else if (p.window_evict) err = shape->D == 128 ? launch_chunks<128, true>(p, k_map, v_map, s) : launch_chunks<64, true>(p, k_map, v_map, s);
-    else err = shape->D == 128 ? launch_chunks<128, false>(p, k_map, v_map, s) : launch_chunks<64, false>(p, k_map, v_map, s);
+    if (four_bit) err = p.window_evict ? launch_chunks<128, true, BAKLAVA_KV_INT4>(p, k_map, v_map, s_map, s) : launch_chunks<128, false, BAKLAVA_KV_INT4>(p, k_map, v_map, s_map, s);
+    else if (fp8) err = p.window_evict ? launch_chunks<128, true, BAKLAVA_KV_FP8_E4M3>(p, k_map, v_map, s_map, s) : launch_chunks<128, false, BAKLAVA_KV_FP8_E4M3>(p, k_map, v_map, s_map, s);
+    else if (p.window_evict) err = shape->D == 128 ? launch_chunks<128, true>(p, k_map, v_map, s_map, s) : launch_chunks<64, true>(p, k_map, v_map, s_map, s);
+    else err = shape->D == 128 ? launch_chunks<128, false>(p, k_map, v_map, s_map, s) : launch_chunks<64, false>(p, k_map, v_map, s_map, s);
     if (err != cudaSuccess) return BAKLAVA_ERR_CUDA;
     if (p.split_tail) {
         cudaLaunchAttribute attr[1];

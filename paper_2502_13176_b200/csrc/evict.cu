@@ -15,6 +15,7 @@
 #include "baklava.h"
 #include "common.h"
 #include "fp8.cuh"
+#include "int4.cuh"
 
 namespace {
 
@@ -42,7 +43,9 @@ struct EvictParams {
     const int32_t* seq_len;   // [B] tokens of each sequence's prompt (clamped to 0 .. T) or NULL: T for all
     int64_t stride_layer, stride_seq, stride_head;
     int32_t* kept;   // [n_units][T]
-    const float* kv_scale;   // FP8 slabs: [L, Hkv, 4] (K scale, its reciprocal, V scale, its reciprocal)
+    const float* kv_scale;   // FP8 slabs: [L, Hkv, 4] (K scale, its reciprocal, V scale, its reciprocal);
+                             // 4-bit slabs: [L, Hkv, 4, D], the same per channel
+    float2* row_scale;       // 4-bit slabs: [rows] (K, V), else null
 };
 
 struct Where {
@@ -179,8 +182,9 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const EvictPa
     if (tid == 0) { p.len[w.st] = R; p.free_slot[w.st] = R; }
 }
 
-template <int D, bool kFp8>
+template <int D, int kKv>
 __global__ void __launch_bounds__(kCopyThreads) evict_copy_kernel(const EvictParams p) {
+    constexpr bool kFp8 = kKv == BAKLAVA_KV_FP8_E4M3, kInt4 = kKv == BAKLAVA_KV_INT4;
     const int unit = blockIdx.x;
     const Where w = locate(p, unit);
     const int n = p.len[w.st];
@@ -196,7 +200,21 @@ __global__ void __launch_bounds__(kCopyThreads) evict_copy_kernel(const EvictPar
         const bool is_v = piece >= kVec;
         const int c = is_v ? piece - kVec : piece;
         const uint4* from = reinterpret_cast<const uint4*>((is_v ? p.v_dense : p.k_dense) + (w.dense0 + src) * D) + c;
-        if (kFp8) {          // the row is quantised on its way into the slab: D bytes per row
+        if (kInt4) {         // sixteen lanes per row and operand find its scale (a warp holds one row: D = 128)
+            static_assert(!kInt4 || kPerRow == 32, "one warp per row");
+            const float4* inv = reinterpret_cast<const float4*>(p.kv_scale + ((int64_t)w.head * 4 + (is_v ? 3 : 1)) * D) + 2 * c;
+            const uint4 raw = __ldg(from);
+            float y0[4], y1[4];
+            int4q::scaled4(make_uint2(raw.x, raw.y), __ldg(inv), y0);
+            int4q::scaled4(make_uint2(raw.z, raw.w), __ldg(inv + 1), y1);
+            uint32_t top = max(int4q::largest_bits(y0), int4q::largest_bits(y1));
+#pragma unroll
+            for (int off = 8; off > 0; off >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+            const float rs = int4q::row_scale(top);
+            uint32_t* slab = reinterpret_cast<uint32_t*>(is_v ? p.v_slab : p.k_slab);
+            slab[(w.slab0 + r) * kVec + c] = int4q::codes4(y0, rs) | (int4q::codes4(y1, rs) << 16);
+            if (c == 0) reinterpret_cast<float*>(p.row_scale + w.slab0 + r)[is_v] = rs;
+        } else if (kFp8) {   // the row is quantised on its way into the slab: D bytes per row
             const float inv_scale = p.kv_scale[w.head * 4 + (is_v ? 3 : 1)];
             uint8_t* slab = reinterpret_cast<uint8_t*>(is_v ? p.v_slab : p.k_slab);
             *(reinterpret_cast<uint2*>(slab + (w.slab0 + r) * D) + c) = fp8::quantise8(__ldg(from), inv_scale);
@@ -356,20 +374,29 @@ __global__ void __launch_bounds__(kSelThreads) evict_inplace_kernel(const EvictP
         const bool on = r < n_keep;
         int src = 0, ps = 0;
         float sc = 0.0f;
+        float2 rs = make_float2(0.0f, 0.0f);
         uint4 kv = make_uint4(0, 0, 0, 0), vv = kv;
         if (on) {
             src = __ldcg(order + r);
             if (src != r) {
                 kv = *(reinterpret_cast<const uint4*>(ks + (int64_t)src * kRowBytes) + c);
                 vv = *(reinterpret_cast<const uint4*>(vs + (int64_t)src * kRowBytes) + c);
-                if (c == 0) { ps = pos_w[src]; sc = score[src]; }
+                if (c == 0) {
+                    ps = pos_w[src];
+                    sc = score[src];
+                    if (p.row_scale) rs = p.row_scale[w.slab0 + src];
+                }
             }
         }
         __syncthreads();
         if (on && src != r) {
             *(reinterpret_cast<uint4*>(ks + (int64_t)r * kRowBytes) + c) = kv;
             *(reinterpret_cast<uint4*>(vs + (int64_t)r * kRowBytes) + c) = vv;
-            if (c == 0) { pos_w[r] = ps; score[r] = sc; }
+            if (c == 0) {
+                pos_w[r] = ps;
+                score[r] = sc;
+                if (p.row_scale) p.row_scale[w.slab0 + r] = rs;
+            }
         }
         __syncthreads();
     }
@@ -419,14 +446,15 @@ int evict_impl(const baklava_shape* shape, const baklava_cache* cache, int32_t l
     p.stride_layer = stride_layer; p.stride_seq = stride_seq; p.stride_head = stride_head;
     p.kept = kept;
     p.kv_scale = cache->kv_scale;
-    const bool quantised = cache->kv_dtype == BAKLAVA_KV_FP8_E4M3;
-    if (cache->kv_dtype != BAKLAVA_KV_BF16 && !quantised) return BAKLAVA_ERR_INVALID_ARG;
-    if (quantised && !cache->kv_scale) return BAKLAVA_ERR_INVALID_ARG;
-    if (quantised && shape->D != 128) return BAKLAVA_ERR_UNSUPPORTED;
+    const int rc = baklava_check_kv_format(shape, cache);
+    if (rc) return rc;
+    const bool fp8 = cache->kv_dtype == BAKLAVA_KV_FP8_E4M3, four_bit = cache->kv_dtype == BAKLAVA_KV_INT4;
+    p.row_scale = four_bit ? reinterpret_cast<float2*>(cache->row_scale) : nullptr;
 
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (in_place) {
-        if (quantised) evict_inplace_kernel<128><<<(unsigned)units, kSelThreads, 0, s>>>(p);
+        if (four_bit) evict_inplace_kernel<64><<<(unsigned)units, kSelThreads, 0, s>>>(p);
+        else if (fp8) evict_inplace_kernel<128><<<(unsigned)units, kSelThreads, 0, s>>>(p);
         else if (shape->D == 128) evict_inplace_kernel<256><<<(unsigned)units, kSelThreads, 0, s>>>(p);
         else evict_inplace_kernel<128><<<(unsigned)units, kSelThreads, 0, s>>>(p);
         return cudaGetLastError() == cudaSuccess ? BAKLAVA_OK : BAKLAVA_ERR_CUDA;
@@ -434,9 +462,10 @@ int evict_impl(const baklava_shape* shape, const baklava_cache* cache, int32_t l
     evict_select_kernel<<<(unsigned)units, kSelThreads, 0, s>>>(p);
     if (cudaGetLastError() != cudaSuccess) return BAKLAVA_ERR_CUDA;
     const dim3 grid((unsigned)units, (unsigned)row_blocks);
-    if (quantised) evict_copy_kernel<128, true><<<grid, kCopyThreads, 0, s>>>(p);
-    else if (shape->D == 128) evict_copy_kernel<128, false><<<grid, kCopyThreads, 0, s>>>(p);
-    else evict_copy_kernel<64, false><<<grid, kCopyThreads, 0, s>>>(p);
+    if (four_bit) evict_copy_kernel<128, BAKLAVA_KV_INT4><<<grid, kCopyThreads, 0, s>>>(p);
+    else if (fp8) evict_copy_kernel<128, BAKLAVA_KV_FP8_E4M3><<<grid, kCopyThreads, 0, s>>>(p);
+    else if (shape->D == 128) evict_copy_kernel<128, BAKLAVA_KV_BF16><<<grid, kCopyThreads, 0, s>>>(p);
+    else evict_copy_kernel<64, BAKLAVA_KV_BF16><<<grid, kCopyThreads, 0, s>>>(p);
     return cudaGetLastError() == cudaSuccess ? BAKLAVA_OK : BAKLAVA_ERR_CUDA;
 }
 

@@ -34,6 +34,18 @@ int baklava_check_shape(const baklava_shape* s) {
     return BAKLAVA_OK;
 }
 
+int baklava_check_kv_format(const baklava_shape* s, const baklava_cache* cache) {
+    if (cache->kv_dtype == BAKLAVA_KV_BF16) return BAKLAVA_OK;
+    if (cache->kv_dtype != BAKLAVA_KV_FP8_E4M3 && cache->kv_dtype != BAKLAVA_KV_INT4) return BAKLAVA_ERR_INVALID_ARG;
+    if (!cache->kv_scale) return BAKLAVA_ERR_INVALID_ARG;
+    if (cache->kv_dtype == BAKLAVA_KV_INT4) {
+        // read in 16-byte vectors and through a tensor map whose rows are sixteen rows' scales
+        if (!cache->row_scale || !baklava_aligned16(cache->row_scale) || !baklava_aligned16(cache->kv_scale)) return BAKLAVA_ERR_INVALID_ARG;
+        if (cache->seq_stride_tokens % 16 != 0) return BAKLAVA_ERR_INVALID_ARG;
+    }
+    return s->D == 128 ? BAKLAVA_OK : BAKLAVA_ERR_UNSUPPORTED;
+}
+
 // ---------------------------------------------------------------- Algorithm 1, step 2
 extern "C" __attribute__((visibility("default"))) int baklava_importance(const baklava_shape* shape, const float* head_cos, int32_t P,
                                   double* kv_importance) {
@@ -186,7 +198,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_decode_plan(const 
     if (!cap || !info || B <= 0 || seq_stride_tokens <= 0) return BAKLAVA_ERR_INVALID_ARG;
     if (layer_begin < 0 || layer_end > shape->L || layer_begin >= layer_end) return BAKLAVA_ERR_INVALID_ARG;
     if (chunk_tokens < 0 || (chunk_tokens == 0 && n_sm <= 0)) return BAKLAVA_ERR_INVALID_ARG;
-    if (kv_dtype != BAKLAVA_KV_BF16 && kv_dtype != BAKLAVA_KV_FP8_E4M3) return BAKLAVA_ERR_INVALID_ARG;
+    if (kv_dtype != BAKLAVA_KV_BF16 && kv_dtype != BAKLAVA_KV_FP8_E4M3 && kv_dtype != BAKLAVA_KV_INT4) return BAKLAVA_ERR_INVALID_ARG;
     const int Hkv = shape->Hkv, layers = layer_end - layer_begin;
 
     std::vector<int> heads((size_t)layers * Hkv);       // index (li * Hkv + h) inside the range
@@ -211,7 +223,8 @@ extern "C" __attribute__((visibility("default"))) int baklava_decode_plan(const 
         const int64_t slots = (int64_t)n_sm * kCtasPerSm;
         // what a chunk costs besides its rows (start-up, partial, arrival) is paid per chunk, not per byte: with
         // one-byte rows the same balance between that and the tail of the launch is struck at twice the length
-        const int64_t wide = kv_dtype == BAKLAVA_KV_FP8_E4M3 ? 2 : 1;
+        // (4-bit rows: the same length as with one-byte rows)
+        const int64_t wide = kv_dtype != BAKLAVA_KV_BF16 ? 2 : 1;
         min_chunk = wide * kMinChunk;
         target = (wide * tokens / (2 * slots) + kTile - 1) / kTile * kTile;
         target = std::max<int64_t>(kMinChunk, std::min<int64_t>(target, wide * 4096));

@@ -27,9 +27,9 @@ class DecodeSession:
             self.shape, self.importance, t, 0 if uniform else r_num, r_den, total,
             w.min_pages * w.page, w.max_pages * w.page)
         self.kv_dtype = kv_dtype
-        fp8_scales = wl.kv_fp8_scales(w, self.scales) if kv_dtype == bk.KV_FP8_E4M3 else None
+        kv_scale = {bk.KV_FP8_E4M3: wl.kv_fp8_scales, bk.KV_INT4: wl.kv_int4_scales}.get(kv_dtype)
         self.cache = bk.Cache(self.shape, self.cap, self.off, self.stride, w.B, self.device, kv_dtype=kv_dtype,
-                              kv_scale=fp8_scales)
+                              kv_scale=kv_scale and kv_scale(w, self.scales))
         self.lb, self.le = (0, w.L) if layers is None else layers
         n_sm = torch.cuda.get_device_properties(self.device).multi_processor_count
         self.plan = bk.baklava_decode_plan(self.shape, self.cap, w.B, self.lb, self.le, self.stride,
@@ -99,7 +99,7 @@ class DecodeSession:
     def retained_kv_bytes(self):
         """Bytes of K and V in valid rows of the session's layers: what one step must read."""
         n = int(self.cache.len[:, self.lb:self.le].sum().item())
-        return n * self.w.D * 2 * (1 if self.kv_dtype == bk.KV_FP8_E4M3 else 2)
+        return n * bk.kv_row_bytes(self.w.D, self.kv_dtype)
 
     def check_status(self):
         code = int(self.cache.status.item())

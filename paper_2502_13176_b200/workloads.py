@@ -121,6 +121,13 @@ def kv_fp8_scales(w, scales):
     return four.numpy()
 
 
+def kv_int4_scales(w, scales):
+    """Per-channel scales of 4-bit slabs as float32 [L, Hkv, 4, D] = (K scale, 1 / K scale, V scale, 1 / V scale): the
+    channels' own magnitudes, so that no channel sets the range of its rows; the reciprocals are inputs like the scales."""
+    one = torch.ones((), dtype=torch.float32)
+    return torch.stack([scales[0], one / scales[0], scales[1], one / scales[1]], dim=2).numpy()
+
+
 def dense_kv(w, l, b, h, scales, device="cpu", T=None):
     """Prefilled K and V of one (layer, sequence, KV head): two bf16 [T, D] tensors."""
     T = w.T if T is None else T
