@@ -128,8 +128,10 @@ def _ptr(t):
 
 
 def _stream(stream):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return c_void_p(s.cuda_stream)
+    if stream is not None:
+        return c_void_p(stream.cuda_stream)
+    # the current stream's handle without building a Stream object for it (3 us of a call that launches in 4)
+    return c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
 
 
 def make_shape(L, Hq, Hkv, D, page=16, n_sink=4, recent_num=1, recent_den=2):
@@ -332,67 +334,74 @@ def baklava_prefill_scores(shape, q, k, prompt_len, B, T, score, ws, stream=None
            "baklava_prefill_scores")
 
 
-def _here(t, what):
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError("%s is on %s, the current device is cuda:%d" % (what, t.device, torch.cuda.current_device()))
+def _device():
+    return torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else -2   # -2: none
 
 
-def _rows(t, what, seqs, heads, tokens, D):
+def _elsewhere(t, what, dev):
+    raise ValueError("%s is on %s; the current device is cuda:%d" % (what, t.device, dev))
+
+
+def _rows(t, what, dev, seqs, heads, tokens, D):
     """Pointer and strides of a bf16 tensor [seqs, heads, tokens, D] (any view whose last dimension is contiguous)."""
     st = t.stride()
     if t.dtype != torch.bfloat16 or t.shape != (seqs, heads, tokens, D) or st[3] != 1:
         raise ValueError("%s: expected bf16 [%d, %d, %d, %d] with contiguous rows, got %s %s with strides %s"
                          % (what, seqs, heads, tokens, D, t.dtype, tuple(t.shape), st))
-    _here(t, what)
-    return c_void_p(t.data_ptr()), ctypes.byref(Strides(st[0], st[1], st[2]))
+    if t.get_device() != dev:
+        _elsewhere(t, what, dev)
+    return t.data_ptr(), Strides(st[0], st[1], st[2])
 
 
-def _dense(t, what, dtype, shape):
+def _dense(t, what, dev, dtype, shape):
     """Pointer of a contiguous tensor, NULL for None."""
     if t is None:
         return None
     if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: expected a contiguous %s tensor %s, got %s %s" % (what, dtype, shape, t.dtype, tuple(t.shape)))
-    _here(t, what)
-    return c_void_p(t.data_ptr())
+    if t.get_device() != dev:
+        _elsewhere(t, what, dev)
+    return t.data_ptr()
 
 
 def baklava_qk_norm_rope(shape, q, k, positions, inv_freq, q_weight, k_weight, eps, q_out, k_out, flags=0, stream=None):
     """q, q_out: bf16 [B, Hq, T, D], k, k_out: bf16 [B, Hkv, T, D], each any view with contiguous rows; positions: int32
     [B, T]; inv_freq: float32 [rotary_dim / 2]; weights: bf16 [D] or None."""
     B, _, T, D = q.shape
-    _check(lib().baklava_qk_norm_rope(ctypes.byref(shape), *_rows(q, "q", B, shape.Hq, T, shape.D),
-                                      *_rows(k, "k", B, shape.Hkv, T, shape.D), _dense(positions, "positions", torch.int32, (B, T)),
-                                      B, T, _dense(inv_freq, "inv_freq", torch.float32, (inv_freq.numel(),)),
-                                      2 * inv_freq.numel(), _dense(q_weight, "q_weight", torch.bfloat16, (D,)),
-                                      _dense(k_weight, "k_weight", torch.bfloat16, (D,)),
-                                      float(eps), int(flags), *_rows(q_out, "q_out", B, shape.Hq, T, shape.D),
-                                      *_rows(k_out, "k_out", B, shape.Hkv, T, shape.D), _stream(stream)), "baklava_qk_norm_rope")
+    Hq, Hkv, dev, n = shape.Hq, shape.Hkv, _device(), inv_freq.numel()
+    _check(lib().baklava_qk_norm_rope(shape, *_rows(q, "q", dev, B, Hq, T, D), *_rows(k, "k", dev, B, Hkv, T, D),
+                                      _dense(positions, "positions", dev, torch.int32, (B, T)), B, T,
+                                      _dense(inv_freq, "inv_freq", dev, torch.float32, (n,)), 2 * n,
+                                      _dense(q_weight, "q_weight", dev, torch.bfloat16, (D,)),
+                                      _dense(k_weight, "k_weight", dev, torch.bfloat16, (D,)), eps, flags,
+                                      *_rows(q_out, "q_out", dev, B, Hq, T, D), *_rows(k_out, "k_out", dev, B, Hkv, T, D),
+                                      _stream(stream)), "baklava_qk_norm_rope")
 
 
 def baklava_prefill_attn(shape, q, k, v, prompt_len, out, lse, status, stream=None):
     """q, out: bf16 [B, Hq, T, D], k, v: bf16 [B, Hkv, T, D], any views with contiguous rows; prompt_len: int32 [B] or None;
     lse: float32 [B, Hq, T] or None; status: int32 [1]."""
     B, _, T, D = q.shape
-    _check(lib().baklava_prefill_attn(ctypes.byref(shape), *_rows(q, "q", B, shape.Hq, T, shape.D),
-                                      *_rows(k, "k", B, shape.Hkv, T, shape.D), *_rows(v, "v", B, shape.Hkv, T, shape.D),
-                                      _dense(prompt_len, "prompt_len", torch.int32, (B,)), B, T,
-                                      *_rows(out, "out", B, shape.Hq, T, shape.D), _dense(lse, "lse", torch.float32, (B, shape.Hq, T)),
-                                      _dense(status, "status", torch.int32, (1,)), _stream(stream)), "baklava_prefill_attn")
+    Hq, Hkv, dev = shape.Hq, shape.Hkv, _device()
+    _check(lib().baklava_prefill_attn(shape, *_rows(q, "q", dev, B, Hq, T, D), *_rows(k, "k", dev, B, Hkv, T, D),
+                                      *_rows(v, "v", dev, B, Hkv, T, D), _dense(prompt_len, "prompt_len", dev, torch.int32, (B,)),
+                                      B, T, *_rows(out, "out", dev, B, Hq, T, D),
+                                      _dense(lse, "lse", dev, torch.float32, (B, Hq, T)),
+                                      _dense(status, "status", dev, torch.int32, (1,)), _stream(stream)), "baklava_prefill_attn")
 
 
 def baklava_prefill_attn_packed(shape, q, k, v, cu_seqlens, max_len, out, lse, status, stream=None):
     """q, out: bf16 [Hq, total, D], k, v: bf16 [Hkv, total, D], any views with contiguous rows; cu_seqlens: int32 [B + 1];
     lse: float32 [Hq, total] or None; status: int32 [1]."""
     total, D = q.shape[1], shape.D
-    _check(lib().baklava_prefill_attn_packed(ctypes.byref(shape), *_rows(q.unsqueeze(0), "q", 1, shape.Hq, total, D),
-                                             *_rows(k.unsqueeze(0), "k", 1, shape.Hkv, total, D),
-                                             *_rows(v.unsqueeze(0), "v", 1, shape.Hkv, total, D),
-                                             _dense(cu_seqlens, "cu_seqlens", torch.int32, (cu_seqlens.numel(),)),
-                                             cu_seqlens.numel() - 1, int(max_len), total,
-                                             *_rows(out.unsqueeze(0), "out", 1, shape.Hq, total, D),
-                                             _dense(lse, "lse", torch.float32, (shape.Hq, total)),
-                                             _dense(status, "status", torch.int32, (1,)), _stream(stream)),
+    Hq, Hkv, dev, n = shape.Hq, shape.Hkv, _device(), cu_seqlens.numel()
+    _check(lib().baklava_prefill_attn_packed(shape, *_rows(q.unsqueeze(0), "q", dev, 1, Hq, total, D),
+                                             *_rows(k.unsqueeze(0), "k", dev, 1, Hkv, total, D),
+                                             *_rows(v.unsqueeze(0), "v", dev, 1, Hkv, total, D),
+                                             _dense(cu_seqlens, "cu_seqlens", dev, torch.int32, (n,)), n - 1, max_len, total,
+                                             *_rows(out.unsqueeze(0), "out", dev, 1, Hq, total, D),
+                                             _dense(lse, "lse", dev, torch.float32, (Hq, total)),
+                                             _dense(status, "status", dev, torch.int32, (1,)), _stream(stream)),
            "baklava_prefill_attn_packed")
 
 

@@ -19,6 +19,7 @@
 // probabilities of zero, which is not enough when they hold infinities or NaN (0 * inf): value rows past the prompt's
 // end are cleared in shared memory before the product, and in the repeated form non-finite values of the diagonal
 // tile are taken out too and added afterwards to the rows that do see them.
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 
@@ -427,8 +428,16 @@ cudaError_t launch(const AttnParams& p, const CUtensorMap& qm, const CUtensorMap
     // the Q, K and V tiles; at least 80 KB, so that never more than two CTAs (2 x 256 TMEM columns) share an SM
     constexpr int kTiles = 3 * kTileRows * D * 2 + 1024;
     constexpr int kSmem = kTiles > 80 * 1024 ? kTiles : 80 * 1024;
-    cudaError_t e = cudaFuncSetAttribute(prompt_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    // the attribute belongs to the function on the current device: set once per device and instantiation
+    static std::atomic<uint64_t> configured{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    if (dev >= 64 || !(configured.load(std::memory_order_acquire) >> dev & 1)) {
+        e = cudaFuncSetAttribute(prompt_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
+    }
     prompt_attn_kernel<D><<<dim3(p.n_blk, p.Hq, B), kThreads, kSmem, s>>>(p, qm, km, vm);
     return cudaGetLastError();
 }

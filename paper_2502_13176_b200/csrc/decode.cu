@@ -255,6 +255,14 @@ __device__ __forceinline__ void mma_f16_full(float (&d)[4], uint32_t a0, uint32_
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// the same without `volatile`: the compiler may move it between other work (nothing but its registers is touched)
+__device__ __forceinline__ void mma_f16_free(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                             uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 // transpose of an 8 x 8 matrix of 16-bit elements held one row per quad of lanes (lane / 4 = row, two
 // consecutive elements per lane): afterwards lane (g, t) holds elements (2 t, g) and (2 t + 1, g)
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a) {
@@ -659,11 +667,15 @@ __device__ __noinline__ void finish_head(const DecodeParams* pp, float* scratch,
 //     is handled like the running maximum: fp16 holds what is at most 1).
 // The scaled query is brought to 2^12 and split into two fp16 terms (22 significant bits): one term (11 bits) would
 // shift every logit of a head by a common error of 1e-4.
-template <int D, bool kByPosition, int kKv>
+// With at most four heads in the group (kTwice) the two terms of a head are two columns of ONE MMA, h and h + 4, whose
+// results are added by one exchange between lanes: half the MMAs.  Columns 4 .. 7 then carry the heads 0 .. 3 a second
+// time through the softmax and the product with V, where they would be zero.
+template <int D, bool kByPosition, int kKv, bool kTwice>
 __global__ void __launch_bounds__(kThreads, kKv == BAKLAVA_KV_INT4 ? kInt4CtasPerSm : kKv == BAKLAVA_KV_FP8_E4M3 ? kFp8CtasPerSm : kCtasPerSm)
 decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constant__ CUtensorMap k_map,
                     const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap s_map) {
     constexpr bool kFp8 = kKv == BAKLAVA_KV_FP8_E4M3, kInt4 = kKv == BAKLAVA_KV_INT4;
+    static_assert(kInt4 || !kTwice, "two columns per head: 4-bit slabs only");
     constexpr int kKSteps = D / 16;                    // MMA k-steps over the head dimension
     constexpr int kTT = kInt4 ? kInt4StageTokens : kFp8 ? kFp8StageTokens : kTileTokens;       // tokens per stage
     constexpr int kNS = kInt4 ? kInt4Stages : kFp8 ? kFp8Stages : kStages;            // stages of the ring
@@ -813,9 +825,10 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
         // channels 2 t, 2 t + 1 (q0) and 8 + 2 t, 9 + 2 t (q1); for FP8 slabs the channels 4 t .. 4 t + 3, the order
         // in which the four bytes of a K register arrive (the contraction index may be permuted at will)
         uint32_t qq[2 * kKSteps];                          // (q0, q1) of step ks side by side, as the MMA takes them
-        uint32_t ql[kInt4 ? 2 * kKSteps : 1];              // 4-bit slabs: the second fp16 term of the same
+        uint32_t ql[kInt4 && !kTwice ? 2 * kKSteps : 1];   // 4-bit slabs: the second fp16 term of the same
         float q_off[2] = {0.0f, 0.0f}, q_fac[2] = {1.0f, 1.0f};   // 4-bit slabs, this lane's two heads: offset, factor
-        const __nv_bfloat16* q_ptr = p.q + ((int64_t)(u.li * p.B + u.b) * p.Hq + u.h * G + g8) * D;
+        const int q_head = kTwice ? g8 & 3 : g8;
+        const __nv_bfloat16* q_ptr = p.q + ((int64_t)(u.li * p.B + u.b) * p.Hq + u.h * G + q_head) * D;
         if (kInt4) {
             // lane t holds, of each group of 32 channels, the eight of word t of a K row's 16 bytes
             float x[D / 4];
@@ -823,7 +836,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
             const float* chan = p.kv_scale + (int64_t)u.head * 4 * D;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
-                const uint4 raw = g8 < G ? *reinterpret_cast<const uint4*>(q_ptr + 32 * c + 8 * t4) : make_uint4(0u, 0u, 0u, 0u);
+                const uint4 raw = q_head < G ? *reinterpret_cast<const uint4*>(q_ptr + 32 * c + 8 * t4) : make_uint4(0u, 0u, 0u, 0u);
                 const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -851,8 +864,12 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                     const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
                     const uint32_t lo = pack_f16(a - h.x, b - h.y);
                     const float2 l = __half22float2(*reinterpret_cast<const __half2*>(&lo));
-                    qq[4 * c + j] = hi;
-                    ql[4 * c + j] = lo;
+                    if (kTwice) {
+                        qq[4 * c + j] = g8 < 4 ? hi : lo;
+                    } else {
+                        qq[4 * c + j] = hi;
+                        ql[4 * c + j] = lo;
+                    }
                     sum = fmaf((h.x + l.x) + (h.y + l.y), (j & 1) ? 16.0f : 1.0f, sum);
                 }
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
@@ -860,6 +877,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 q_off[e] = -8.0f * 0x1p-24f * __shfl_sync(0xffffffffu, sum, 4 * (2 * t4 + e));
+                if (kTwice && t4 >= 2) q_off[e] = 0.0f;    // (once per head)
                 q_fac[e] = __shfl_sync(0xffffffffu, back, 4 * (2 * t4 + e)) * p.scale_log2;
             }
         } else {
@@ -987,34 +1005,47 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                 }
                 // S^T = K Q^T for the warp's tokens: st[blk] = (token g: heads 2 t, 2 t + 1; token g + 8: the same)
                 float st[kBlocks][4];
+                if (kInt4) {
 #pragma unroll
-                for (int blk = 0; blk < kBlocks; ++blk) {
-                    st[blk][0] = st[blk][1] = st[blk][2] = st[blk][3] = 0.0f;
-                    const uint32_t k_row = k_tile + (uint32_t)((w0 + blk * kWarpTokens) * 128) + k_lane;
-                    if (kInt4) {
+                    for (int blk = 0; blk < kBlocks; ++blk) {
                         st[blk][0] = st[blk][2] = q_off[0];
                         st[blk][1] = st[blk][3] = q_off[1];
-                        const uint32_t n_row = k_tile + (uint32_t)((w0 + blk * kWarpTokens) * 64);
+                    }
+                    // the blocks' chains of MMAs side by side: an accumulator is added to every kBlocks-th MMA only
 #pragma unroll
-                        for (int cc = 0; cc < D / 64; ++cc) {     // 64 channels per load: (tokens 0-7 | 8-15) x two pieces
-                            uint32_t kb[4];
-                            ldmatrix_x4(n_row + (n_lane ^ (uint32_t)(cc << 5)), kb);
+                    for (int cc = 0; cc < D / 64; ++cc) {         // 64 channels per load: (tokens 0-7 | 8-15) x two pieces
+                        uint32_t kb[kBlocks][4];
 #pragma unroll
-                            for (int x = 0; x < 2; ++x) {
-                                const int c = 2 * cc + x;
-                                uint32_t lo = kb[2 * x], hi = kb[2 * x + 1];
+                        for (int blk = 0; blk < kBlocks; ++blk)
+                            ldmatrix_x4(k_tile + (uint32_t)((w0 + blk * kWarpTokens) * 64) + (n_lane ^ (uint32_t)(cc << 5)), kb[blk]);
 #pragma unroll
-                                for (int j = 0; j < 2; ++j) {     // nibbles (0, 4 | 1, 5), then (2, 6 | 3, 7)
-                                    const uint32_t a0 = lo & 0x000f000fu, a1 = hi & 0x000f000fu;
-                                    const uint32_t a2 = lo & 0x00f000f0u, a3 = hi & 0x00f000f0u;
-                                    mma_f16_full(st[blk], a0, a1, a2, a3, qq[4 * c + 2 * j], qq[4 * c + 2 * j + 1]);
-                                    mma_f16_full(st[blk], a0, a1, a2, a3, ql[4 * c + 2 * j], ql[4 * c + 2 * j + 1]);
-                                    lo >>= 8;
-                                    hi >>= 8;
-                                }
+                        for (int x = 0; x < 2; ++x)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {         // nibbles (0, 4 | 1, 5), then (2, 6 | 3, 7)
+                                const int at = 4 * (2 * cc + x) + 2 * j;
+#pragma unroll
+                                for (int term = 0; term < (kTwice ? 1 : 2); ++term)
+#pragma unroll
+                                    for (int blk = 0; blk < kBlocks; ++blk) {
+                                        const uint32_t lo = kb[blk][2 * x] >> (8 * j), hi = kb[blk][2 * x + 1] >> (8 * j);
+                                        const uint32_t* b = term ? ql : qq;
+                                        mma_f16_free(st[blk], lo & 0x000f000fu, hi & 0x000f000fu, lo & 0x00f000f0u, hi & 0x00f000f0u,
+                                                     b[at], b[at + 1]);
+                                    }
                             }
-                        }
-                    } else if (kFp8) {
+                    }
+                    if (kTwice) {
+#pragma unroll
+                        for (int blk = 0; blk < kBlocks; ++blk)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) st[blk][i] += __shfl_xor_sync(0xffffffffu, st[blk][i], 2);
+                    }
+                }
+#pragma unroll
+                for (int blk = 0; blk < kBlocks && !kInt4; ++blk) {
+                    st[blk][0] = st[blk][1] = st[blk][2] = st[blk][3] = 0.0f;
+                    const uint32_t k_row = k_tile + (uint32_t)((w0 + blk * kWarpTokens) * 128) + k_lane;
+                    if (kFp8) {
 #pragma unroll
                         for (int kk = 0; kk < D / 32; ++kk) {     // 32 channels per load: two steps of 16
                             uint32_t kb[4];      // (tokens 0-7 | 8-15) x (channels 0-15 | 16-31), four bytes per lane
@@ -1057,7 +1088,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                         }
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            st[blk][2 * r + e] *= kInt4 ? sk * q_fac[e] : sk;
+                            st[blk][2 * r + e] *= sk;          // (4-bit slabs: q_fac follows, with the maximum)
                             if (ok[blk][r]) mx[e] = fmaxf(mx[e], st[blk][2 * r + e]);
                         }
                     }
@@ -1067,6 +1098,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                     mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 4));
                     mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 8));
                     mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 16));
+                    if (kInt4) mx[e] *= q_fac[e];             // (positive)
                     const float m_new = fmaxf(m_run[e], mx[e]);
                     corr[e] = (m_new == -INFINITY) ? 1.0f : fast_exp2(m_run[e] - m_new);
                     m_run[e] = m_new;
@@ -1078,7 +1110,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                     for (int r = 0; r < 2; ++r)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float pv = ok[blk][r] ? fast_exp2(st[blk][2 * r + e] - m_run[e]) : 0.0f;
+                            const float pv = ok[blk][r] ? fast_exp2(kInt4 ? fmaf(st[blk][2 * r + e], q_fac[e], -m_run[e]) : st[blk][2 * r + e] - m_run[e]) : 0.0f;
                             st[blk][2 * r + e] = pv;
                             psum[e] += pv;
                         }
@@ -1146,7 +1178,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                         // a register of the transposed load = two tokens x four adjacent channels; row g of MMA j is
                         // channel 4 g + 2 j of the 32-channel group, row g + 8 channel 4 g + 2 j + 1 (16 times too large)
                         const uint32_t n_row = v_tile + (uint32_t)((w0 + blk * kWarpTokens) * 64);
-                        mma_f16_full(o8, 0x00080008u, 0x00800080u, 0x00080008u, 0x00800080u, pb[blk][0], pb[blk][1]);
+                        mma_f16_free(o8, 0x00080008u, 0x00800080u, 0x00080008u, 0x00800080u, pb[blk][0], pb[blk][1]);
 #pragma unroll
                         for (int cc = 0; cc < D / 64; ++cc) {
                             uint32_t vb[4];
@@ -1156,7 +1188,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                                 uint32_t lo = vb[2 * x], hi = vb[2 * x + 1];     // tokens 0-7 and 8-15 of the block
 #pragma unroll
                                 for (int j = 0; j < 2; ++j) {
-                                    mma_f16_full(o[4 * cc + 2 * x + j], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu,
+                                    mma_f16_free(o[4 * cc + 2 * x + j], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu,
                                                  hi & 0x00f000f0u, pb[blk][0], pb[blk][1]);
                                     lo >>= 8;
                                     hi >>= 8;
@@ -1530,7 +1562,7 @@ bool make_scale_map_int4(CUtensorMap* map, void* base, int64_t rows) {
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool kByPosition, int kKv = BAKLAVA_KV_BF16>
+template <int D, bool kByPosition, int kKv = BAKLAVA_KV_BF16, bool kTwice = false>
 cudaError_t launch_chunks(const DecodeParams& p, const CUtensorMap& km, const CUtensorMap& vm, const CUtensorMap& sm,
                           cudaStream_t s) {
     constexpr int kRing = kKv == BAKLAVA_KV_INT4 ? kInt4Stages * kInt4StageTokens * (D + 8)
@@ -1542,7 +1574,7 @@ cudaError_t launch_chunks(const DecodeParams& p, const CUtensorMap& km, const CU
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !(configured.load(std::memory_order_acquire) >> dev & 1)) {
-        e = cudaFuncSetAttribute(decode_chunk_kernel<D, kByPosition, kKv>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        e = cudaFuncSetAttribute(decode_chunk_kernel<D, kByPosition, kKv, kTwice>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (e != cudaSuccess) return e;
         if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
     }
@@ -1556,7 +1588,7 @@ cudaError_t launch_chunks(const DecodeParams& p, const CUtensorMap& km, const CU
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, decode_chunk_kernel<D, kByPosition, kKv>, p, km, vm, sm);
+    return cudaLaunchKernelEx(&cfg, decode_chunk_kernel<D, kByPosition, kKv, kTwice>, p, km, vm, sm);
 }
 
 }  // namespace
@@ -1658,7 +1690,8 @@ int decode_attn_impl(
 
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t err = cudaSuccess;
-    if (four_bit) err = p.window_evict ? launch_chunks<128, true, BAKLAVA_KV_INT4>(p, k_map, v_map, s_map, s) : launch_chunks<128, false, BAKLAVA_KV_INT4>(p, k_map, v_map, s_map, s);
+    if (four_bit && p.G <= 4) err = p.window_evict ? launch_chunks<128, true, BAKLAVA_KV_INT4, true>(p, k_map, v_map, s_map, s) : launch_chunks<128, false, BAKLAVA_KV_INT4, true>(p, k_map, v_map, s_map, s);
+    else if (four_bit) err = p.window_evict ? launch_chunks<128, true, BAKLAVA_KV_INT4>(p, k_map, v_map, s_map, s) : launch_chunks<128, false, BAKLAVA_KV_INT4>(p, k_map, v_map, s_map, s);
     else if (fp8) err = p.window_evict ? launch_chunks<128, true, BAKLAVA_KV_FP8_E4M3>(p, k_map, v_map, s_map, s) : launch_chunks<128, false, BAKLAVA_KV_FP8_E4M3>(p, k_map, v_map, s_map, s);
     else if (p.window_evict) err = shape->D == 128 ? launch_chunks<128, true>(p, k_map, v_map, s_map, s) : launch_chunks<64, true>(p, k_map, v_map, s_map, s);
     else err = shape->D == 128 ? launch_chunks<128, false>(p, k_map, v_map, s_map, s) : launch_chunks<64, false>(p, k_map, v_map, s_map, s);
