@@ -668,8 +668,8 @@ __device__ __noinline__ void finish_head(const DecodeParams* pp, float* scratch,
 // The scaled query is brought to 2^12 and split into two fp16 terms (22 significant bits): one term (11 bits) would
 // shift every logit of a head by a common error of 1e-4.
 // With at most four heads in the group (kTwice) the two terms of a head are two columns of ONE MMA, h and h + 4, whose
-// results are added by one exchange between lanes: half the MMAs.  Columns 4 .. 7 then carry the heads 0 .. 3 a second
-// time through the softmax and the product with V, where they would be zero.
+// results are added by one exchange between lanes: half the MMAs.  The exchange leaves a lane one token row instead of
+// two, so that the softmax runs on all 32 lanes where half of them would have had the group's missing heads.
 template <int D, bool kByPosition, int kKv, bool kTwice>
 __global__ void __launch_bounds__(kThreads, kKv == BAKLAVA_KV_INT4 ? kInt4CtasPerSm : kKv == BAKLAVA_KV_FP8_E4M3 ? kFp8CtasPerSm : kCtasPerSm)
 decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constant__ CUtensorMap k_map,
@@ -779,7 +779,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) { o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.0f; }
     float o8[4] = {0.0f, 0.0f, 0.0f, 0.0f};               // 4-bit slabs: eight times the sums of the probabilities used
-    float v_ref = 0.0f;                                   // 4-bit slabs: largest V row scale met, what they are relative to
+    float v_ref = 0.0f, v_inv = 0.0f;                     // 4-bit slabs: largest V row scale met, what they are relative to
 
     if (warp == kConsumerWarps) {
         // ---------------- producer: one lane issues the TMA loads
@@ -1003,9 +1003,10 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                         }
                     }
                 }
-                // S^T = K Q^T for the warp's tokens: st[blk] = (token g: heads 2 t, 2 t + 1; token g + 8: the same)
-                float st[kBlocks][4];
-                if (kInt4) {
+                if constexpr (kInt4) {
+                    constexpr int kR = kTwice ? 1 : 2;            // token rows per lane and block
+                    const bool upper = kTwice && t4 >= 2;
+                    float st[kBlocks][4];
 #pragma unroll
                     for (int blk = 0; blk < kBlocks; ++blk) {
                         st[blk][0] = st[blk][2] = q_off[0];
@@ -1034,15 +1035,121 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                                     }
                             }
                     }
-                    if (kTwice) {
+                    // kTwice: lane t has the first terms of heads 2 t, 2 t + 1 for tokens g and g + 8, lane t + 2 the
+                    // second terms: they swap a token, after which the lower lanes hold token g, the upper token g + 8
+                    float lg[kBlocks][kR][2];
+                    float sv[kBlocks][kR];                        // V scales of this lane's rows
+                    float mx[2] = {-INFINITY, -INFINITY}, sv_max = 0.0f;
+                    bool ok[kBlocks][kR];
+                    const float2* const scales = reinterpret_cast<const float2*>(ring_ptr + s * kStageBytes + 2 * kTileBytes) + w0;
+#pragma unroll
+                    for (int blk = 0; blk < kBlocks; ++blk)
+#pragma unroll
+                        for (int r = 0; r < kR; ++r) {
+                            const int at = blk * kWarpTokens + g8 + (kTwice ? (upper ? 8 : 0) : 8 * r);
+                            const int tok = wtok0 + at;
+                            ok[blk][r] = !kCareful || (tok < end && tok != hole);
+                            const float2 rs = scales[at];
+                            sv[blk][r] = ok[blk][r] ? rs.y : 0.0f;
+                            sv_max = fmaxf(sv_max, fabsf(sv[blk][r]));
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                float x = st[blk][2 * r + e];
+                                if (kTwice) {
+                                    const float give = upper ? st[blk][e] : st[blk][2 + e];
+                                    x = (upper ? st[blk][2 + e] : st[blk][e]) + __shfl_xor_sync(0xffffffffu, give, 2);
+                                }
+                                lg[blk][r][e] = x * rs.x;         // (the head's factor follows, with the maximum)
+                                if (ok[blk][r]) mx[e] = fmaxf(mx[e], lg[blk][r][e]);
+                            }
+                        }
+                    float corr[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if (kTwice) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
+                        mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 4));
+                        mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 8));
+                        mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 16));
+                        const float m_new = fmaxf(m_run[e], mx[e] * q_fac[e]);      // (positive)
+                        corr[e] = (m_new == -INFINITY) ? 1.0f : fast_exp2(m_run[e] - m_new);
+                        m_run[e] = m_new;
+                        float psum = 0.0f;
 #pragma unroll
                         for (int blk = 0; blk < kBlocks; ++blk)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) st[blk][i] += __shfl_xor_sync(0xffffffffu, st[blk][i], 2);
+                            for (int r = 0; r < kR; ++r) {
+                                lg[blk][r][e] = ok[blk][r] ? fast_exp2(fmaf(lg[blk][r][e], q_fac[e], -m_new)) : 0.0f;
+                                psum += lg[blk][r][e];
+                            }
+                        l_run[e] = l_run[e] * corr[e] + psum;
                     }
-                }
+                    // the V scales' reference follows their maximum
+                    const float seen = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv_max)));
+                    if (seen > v_ref) {
+                        const float ratio = v_ref / seen;
+                        corr[0] *= ratio;
+                        corr[1] *= ratio;
+                        v_ref = seen;
+                        v_inv = 1.0f / seen;
+                    }
+                    if (__any_sync(0xffffffffu, corr[0] != 1.0f || corr[1] != 1.0f)) {
 #pragma unroll
-                for (int blk = 0; blk < kBlocks && !kInt4; ++blk) {
+                        for (int j = 0; j < D / 16; ++j) { o[j][0] *= corr[0]; o[j][1] *= corr[1]; o[j][2] *= corr[0]; o[j][3] *= corr[1]; }
+                        o8[0] *= corr[0]; o8[1] *= corr[1]; o8[2] *= corr[0]; o8[3] *= corr[1];
+                    }
+#pragma unroll
+                    for (int blk = 0; blk < kBlocks; ++blk) {
+                        const int tok0 = wtok0 + blk * kWarpTokens;
+                        // P^T as the B operand: the transposed 8 x 8 block gives lane (g, t) head g, tokens 2 t, 2 t + 1;
+                        // kTwice: the lanes g >= 4 get head g - 4, tokens 8 + 2 t, 9 + 2 t, which the lane 16 below needs
+                        uint32_t pb[2], pr[2];
+#pragma unroll
+                        for (int r = 0; r < kR; ++r) {
+                            const float f = sv[blk][r] * v_inv;
+                            pb[r] = movmatrix_trans(pack_f16(lg[blk][r][0] * f, lg[blk][r][1] * f));
+                            if (keep_logits) pr[r] = movmatrix_trans(pack_f16(lg[blk][r][0], lg[blk][r][1]));
+                        }
+                        if (kTwice) pb[1] = __shfl_xor_sync(0xffffffffu, pb[0], 16);
+                        if (keep_logits) {
+                            // the unnormalised probabilities, in fp16, and the maximum they were taken under
+                            __half* dst = kTwice ? prob_h + (int64_t)(g8 & 3) * C + 2 * t4 + 8 * (g8 >> 2) + tok0 : prob_lane + tok0;
+#pragma unroll
+                            for (int r = 0; r < kR; ++r) {
+                                const int left = end - (tok0 + 2 * t4 + (kTwice ? 8 * (g8 >> 2) : 8 * r));
+                                if (q_head < G) {
+                                    if (!kCareful || left >= 2) *reinterpret_cast<uint32_t*>(dst + 8 * r) = pr[r];
+                                    else if (left == 1) dst[8 * r] = __ushort_as_half((unsigned short)(pr[r] & 0xffffu));
+                                }
+                            }
+                            if (g8 == 0 && (!kCareful || tok0 < end)) {
+                                if (2 * t4 < G) mref_h[(2 * t4) * (C >> 4) + (tok0 >> 4)] = m_run[0];
+                                if (2 * t4 + 1 < G) mref_h[(2 * t4 + 1) * (C >> 4) + (tok0 >> 4)] = m_run[1];
+                            }
+                        }
+                        // a register of the transposed load = two tokens x four adjacent channels; row g of MMA j is
+                        // channel 4 g + 2 j of the 32-channel group, row g + 8 channel 4 g + 2 j + 1 (16 times too large)
+                        const uint32_t n_row = v_tile + (uint32_t)((w0 + blk * kWarpTokens) * 64);
+                        mma_f16_free(o8, 0x00080008u, 0x00800080u, 0x00080008u, 0x00800080u, pb[0], pb[1]);
+#pragma unroll
+                        for (int cc = 0; cc < D / 64; ++cc) {
+                            uint32_t vb[4];
+                            ldmatrix_x4_trans(n_row + (n_lane ^ (uint32_t)(cc << 5)), vb);
+#pragma unroll
+                            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    const uint32_t lo = vb[2 * x] >> (8 * j), hi = vb[2 * x + 1] >> (8 * j);   // tokens 0-7, 8-15
+                                    mma_f16_free(o[4 * cc + 2 * x + j], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu,
+                                                 hi & 0x00f000f0u, pb[0], pb[1]);
+                                }
+                        }
+                    }
+                    return;
+                }
+                // S^T = K Q^T for the warp's tokens: st[blk] = (token g: heads 2 t, 2 t + 1; token g + 8: the same)
+                float st[kBlocks][4];
+#pragma unroll
+                for (int blk = 0; blk < kBlocks; ++blk) {
                     st[blk][0] = st[blk][1] = st[blk][2] = st[blk][3] = 0.0f;
                     const uint32_t k_row = k_tile + (uint32_t)((w0 + blk * kWarpTokens) * 128) + k_lane;
                     if (kFp8) {
@@ -1070,25 +1177,15 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                 // online softmax for the two heads of this lane over the warp's tokens of the stage
                 float mx[2] = {-INFINITY, -INFINITY};
                 bool ok[kBlocks][2];
-                float sv[kInt4 ? kBlocks : 1][2];             // 4-bit slabs: V scales of this lane's rows
-                float sv_max = 0.0f;
 #pragma unroll
                 for (int blk = 0; blk < kBlocks; ++blk)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
                         const int tok = wtok0 + blk * kWarpTokens + g8 + 8 * r;
                         ok[blk][r] = !kCareful || (tok < end && tok != hole);
-                        float sk = scale_k;
-                        if (kInt4) {
-                            const float2 rs = reinterpret_cast<const float2*>(ring_ptr + s * kStageBytes + 2 * kTileBytes)
-                                                  [w0 + blk * kWarpTokens + g8 + 8 * r];
-                            sk = rs.x;
-                            sv[blk][r] = ok[blk][r] ? rs.y : 0.0f;
-                            sv_max = fmaxf(sv_max, fabsf(sv[blk][r]));
-                        }
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            st[blk][2 * r + e] *= sk;          // (4-bit slabs: q_fac follows, with the maximum)
+                            st[blk][2 * r + e] *= scale_k;
                             if (ok[blk][r]) mx[e] = fmaxf(mx[e], st[blk][2 * r + e]);
                         }
                     }
@@ -1098,7 +1195,6 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                     mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 4));
                     mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 8));
                     mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 16));
-                    if (kInt4) mx[e] *= q_fac[e];             // (positive)
                     const float m_new = fmaxf(m_run[e], mx[e]);
                     corr[e] = (m_new == -INFINITY) ? 1.0f : fast_exp2(m_run[e] - m_new);
                     m_run[e] = m_new;
@@ -1110,27 +1206,15 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                     for (int r = 0; r < 2; ++r)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float pv = ok[blk][r] ? fast_exp2(kInt4 ? fmaf(st[blk][2 * r + e], q_fac[e], -m_run[e]) : st[blk][2 * r + e] - m_run[e]) : 0.0f;
+                            const float pv = ok[blk][r] ? fast_exp2(st[blk][2 * r + e] - m_run[e]) : 0.0f;
                             st[blk][2 * r + e] = pv;
                             psum[e] += pv;
                         }
                 l_run[0] = l_run[0] * corr[0] + psum[0];
                 l_run[1] = l_run[1] * corr[1] + psum[1];
-                float v_inv = 0.0f;
-                if (kInt4) {                                  // the V scales' reference follows their maximum
-                    const float seen = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv_max)));
-                    if (seen > v_ref) {
-                        const float ratio = v_ref / seen;
-                        corr[0] *= ratio;
-                        corr[1] *= ratio;
-                        v_ref = seen;
-                    }
-                    v_inv = v_ref > 0.0f ? 1.0f / v_ref : 0.0f;
-                }
                 if (__any_sync(0xffffffffu, corr[0] != 1.0f || corr[1] != 1.0f)) {
 #pragma unroll
                     for (int j = 0; j < D / 16; ++j) { o[j][0] *= corr[0]; o[j][1] *= corr[1]; o[j][2] *= corr[0]; o[j][3] *= corr[1]; }
-                    if (kInt4) { o8[0] *= corr[0]; o8[1] *= corr[1]; o8[2] *= corr[0]; o8[3] *= corr[1]; }
                 }
                 // P^T as the B operand of O^T += V^T P^T: the 8 x 8 blocks (tokens x heads) this warp holds one
                 // row per quad are transposed, so that lane (g, t) gets head g, tokens 2 t, 2 t + 1 (and + 8)
@@ -1140,11 +1224,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                     const int tok0 = wtok0 + blk * kWarpTokens;
                     const uint32_t h0 = movmatrix_trans(pack_f16(st[blk][0], st[blk][1]));
                     const uint32_t h1 = movmatrix_trans(pack_f16(st[blk][2], st[blk][3]));
-                    if (kInt4) {
-                        const float s0 = sv[blk][0] * v_inv, s1 = sv[blk][1] * v_inv;
-                        pb[blk][0] = movmatrix_trans(pack_f16(st[blk][0] * s0, st[blk][1] * s0));
-                        pb[blk][1] = movmatrix_trans(pack_f16(st[blk][2] * s1, st[blk][3] * s1));
-                    } else if (kFp8) {
+                    if (kFp8) {
                         pb[blk][0] = h0; pb[blk][1] = h1;
                     } else {
                         pb[blk][0] = movmatrix_trans(pack_bf16(st[blk][0], st[blk][1]));
@@ -1174,28 +1254,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
 #pragma unroll
                 for (int blk = 0; blk < kBlocks; ++blk) {
                     const uint32_t v_row = v_tile + (uint32_t)((w0 + blk * kWarpTokens) * 128) + v_lane;
-                    if (kInt4) {
-                        // a register of the transposed load = two tokens x four adjacent channels; row g of MMA j is
-                        // channel 4 g + 2 j of the 32-channel group, row g + 8 channel 4 g + 2 j + 1 (16 times too large)
-                        const uint32_t n_row = v_tile + (uint32_t)((w0 + blk * kWarpTokens) * 64);
-                        mma_f16_free(o8, 0x00080008u, 0x00800080u, 0x00080008u, 0x00800080u, pb[blk][0], pb[blk][1]);
-#pragma unroll
-                        for (int cc = 0; cc < D / 64; ++cc) {
-                            uint32_t vb[4];
-                            ldmatrix_x4_trans(n_row + (n_lane ^ (uint32_t)(cc << 5)), vb);
-#pragma unroll
-                            for (int x = 0; x < 2; ++x) {
-                                uint32_t lo = vb[2 * x], hi = vb[2 * x + 1];     // tokens 0-7 and 8-15 of the block
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) {
-                                    mma_f16_free(o[4 * cc + 2 * x + j], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu,
-                                                 hi & 0x00f000f0u, pb[blk][0], pb[blk][1]);
-                                    lo >>= 8;
-                                    hi >>= 8;
-                                }
-                            }
-                        }
-                    } else if (kFp8) {
+                    if (kFp8) {
                         // a register of the transposed load = two tokens x two adjacent channels; the permute puts the
                         // even channel's token pair in the low half and the odd channel's in the high half.  Row g of
                         // the MMA is channel 2 g of the 16-channel group, row g + 8 channel 2 g + 1.
@@ -1254,6 +1313,9 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                 mbar_wait(smem_u32(&bar_full[t % kNS]), (t / kNS) & 1, p.wait_cycles);
         if (tid < G) part[G * D + tid] = __int_as_float(0x7fc00000);
     }
+    // A head of one chunk whose scores are not kept needs no partial and no arrival: its output is written from here
+    // (the same numbers: a single partial has weight 1).  The batch of 16 short caches has a CTA per head.
+    const bool direct = active == 1 && !keep_logits && !pos_evict;
     if (!aborted) {
     // ---- the four warps' states -> one partial for the chunk (the ring is idle now: reuse it)
     float* sm_o = reinterpret_cast<float*>(ring_ptr);       // [kConsumerWarps][G][D]
@@ -1270,6 +1332,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
         // the sums were kept per lane (its own token rows): add them up over the eight row groups
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
+            if (kTwice) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 2);
             l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 4);
             l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 8);
             l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 16);
@@ -1312,8 +1375,18 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
             acc = fmaf(sm_o[(w * G + a) * D + d], c, acc);
             lsum = fmaf(sm_l[w][a], c, lsum);
         }
+        if (direct) {
+            const int64_t at = (int64_t)(u.li * p.B + u.b) * p.Hq + u.h * G + a;
+            p.out[at * D + d] = __float2bfloat16_rn(acc * (lsum > 0.0f ? 1.0f / lsum : 0.0f));
+            if (d == 0 && p.lse) p.lse[at] = lsum > 0.0f ? (mm + log2f(lsum)) * kLn2 : -INFINITY;
+            continue;
+        }
         part[i] = acc;
         if (d == 0) { part[G * D + a] = mm; part[G * D + G + a] = lsum; }
+    }
+    if (direct && tid == 0 && hs.do_append) {
+        p.len[u.st] = n + 1;
+        p.free_slot[u.st] = n + 1;
     }
     if (kByPosition && pos_evict && tid == 0) {
         int bp = INT32_MAX, bs = -1;
@@ -1322,6 +1395,10 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
         part[G * D + 2 * G] = __int_as_float(bp);
         part[G * D + 2 * G + 1] = __int_as_float(bs);
     }
+    }
+    if (direct) {
+        if (overlap && tid == 0) grid_dependency_wait();
+        return;
     }
     __syncthreads();                                        // the whole partial is written ...
     if (tid == 0) sm_last = (arrive_acq_rel(p.arrive + unit) == active - 1);   // ... and published with the arrival
