@@ -50,10 +50,6 @@ constexpr int kStages = 2;                              // bf16 slabs: two 32 KB
 constexpr int kFp8StageTokens = 128;
 constexpr int kFp8Stages = 2;
 constexpr int kFp8CtasPerSm = 3;
-// 4-bit slabs: a row is 64 bytes of codes and a pair of scales, so that 256-token stages are the same 32 KB (+ 2 KB)
-constexpr int kInt4StageTokens = 256;
-constexpr int kInt4Stages = 2;
-constexpr int kInt4CtasPerSm = 3;
 constexpr int kMaxStages = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -251,14 +247,6 @@ __device__ __forceinline__ void mma_f16_full(float (&d)[4], uint32_t a0, uint32_
                                              uint32_t b1) {
     asm volatile(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-        "{%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// the same without `volatile`: the compiler may move it between other work (nothing but its registers is touched)
-__device__ __forceinline__ void mma_f16_free(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                             uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
         "{%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -653,38 +641,19 @@ __device__ __noinline__ void finish_head(const DecodeParams* pp, float* scratch,
 // ldmatrix (16-bit granules) serve one-byte data: four consecutive bytes of a K row land in one register
 // and become two fp16 pairs; V comes through ldmatrix.trans as two tokens x two adjacent channels per
 // register, which a byte permute splits into an even-channel and an odd-channel operand.
-//
-// 4-bit slabs (kKv = BAKLAVA_KV_INT4): a code is u = 1 .. 15 and stands for (u - 8) * row scale * channel scale.
-// Everything but the codes is linear in something that is applied once, so that widening them costs little more than
-// one AND per MMA register:
-//   - four bits in the low or second nibble of a 16-bit word ARE the fp16 number u * 2^-24 or u * 2^-20 (a subnormal,
-//     which the MMA takes exactly), and a 32-bit word of eight codes gives the four register pairs of two MMAs by
-//     masking, with one shift; the factor 16 between the two kinds is taken off the other operand (K) or the result (V);
-//   - the offset: sum_d (u - 8) q_d = sum_d u q_d - 8 sum_d q_d, the accumulator's initial value; for V the same with
-//     8 sum_t p_t, which one more MMA against a constant operand sums from the very probabilities that were used;
-//   - the K channel scales are multiplied into the query, the V channel scales into the partial output, the K row
-//     scales into the logits, the V row scales into the probabilities (relative to the largest one met so far, which
-//     is handled like the running maximum: fp16 holds what is at most 1).
-// The scaled query is brought to 2^12 and split into two fp16 terms (22 significant bits): one term (11 bits) would
-// shift every logit of a head by a common error of 1e-4.
-// With at most four heads in the group (kTwice) the two terms of a head are two columns of ONE MMA, h and h + 4, whose
-// results are added by one exchange between lanes: half the MMAs.  The exchange leaves a lane one token row instead of
-// two, so that the softmax runs on all 32 lanes where half of them would have had the group's missing heads.
-template <int D, bool kByPosition, int kKv, bool kTwice>
-__global__ void __launch_bounds__(kThreads, kKv == BAKLAVA_KV_INT4 ? kInt4CtasPerSm : kKv == BAKLAVA_KV_FP8_E4M3 ? kFp8CtasPerSm : kCtasPerSm)
-decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constant__ CUtensorMap k_map,
-                    const __grid_constant__ CUtensorMap v_map, const __grid_constant__ CUtensorMap s_map) {
-    constexpr bool kFp8 = kKv == BAKLAVA_KV_FP8_E4M3, kInt4 = kKv == BAKLAVA_KV_INT4;
-    static_assert(kInt4 || !kTwice, "two columns per head: 4-bit slabs only");
+template <int D, bool kByPosition, bool kFp8>
+__global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) decode_chunk_kernel(const __grid_constant__ DecodeParams p,
+                                                                const __grid_constant__ CUtensorMap k_map,
+                                                                const __grid_constant__ CUtensorMap v_map) {
     constexpr int kKSteps = D / 16;                    // MMA k-steps over the head dimension
-    constexpr int kTT = kInt4 ? kInt4StageTokens : kFp8 ? kFp8StageTokens : kTileTokens;       // tokens per stage
-    constexpr int kNS = kInt4 ? kInt4Stages : kFp8 ? kFp8Stages : kStages;            // stages of the ring
+    constexpr int kNTiles = D / 8;                     // 8-wide output column blocks
+    constexpr int kTT = kFp8 ? kFp8StageTokens : kTileTokens;       // tokens per stage
+    constexpr int kNS = kFp8 ? kFp8Stages : kStages;            // stages of the ring
     constexpr int kBlocks = kTT / (kConsumerWarps * kWarpTokens);    // 16-token blocks per warp and stage
     static_assert(kBlocks >= 1 && kNS <= kMaxStages, "a stage holds at least one 16-token block per warp");
-    constexpr int kRowBytes = kInt4 ? D / 2 : kFp8 ? D : 2 * D;
+    constexpr int kRowBytes = kFp8 ? D : 2 * D;
     constexpr int kTileBytes = kTT * kRowBytes;        // one K (or V) tile
-    constexpr int kScaleBytes = kInt4 ? kTT * 8 : 0;   // the rows' pairs of scales
-    constexpr int kStageBytes = 2 * kTileBytes + kScaleBytes;
+    constexpr int kStageBytes = 2 * kTileBytes;
     constexpr int kG = BAKLAVA_MAX_GROUP;
 
     extern __shared__ uint8_t smem_raw[];
@@ -717,7 +686,6 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
         ptx::fence_mbar_init();
         prefetch_tensormap(&k_map);
         prefetch_tensormap(&v_map);
-        if (kInt4) prefetch_tensormap(&s_map);
     }
     if (!overlap) grid_dependency_wait();                 // len / free_slot / slab rows / items come from earlier kernels
     else launch_dependents();
@@ -778,8 +746,6 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
     float o[D / 16][4];
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) { o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.0f; }
-    float o8[4] = {0.0f, 0.0f, 0.0f, 0.0f};               // 4-bit slabs: eight times the sums of the probabilities used
-    float v_ref = 0.0f, v_inv = 0.0f;                     // 4-bit slabs: largest V row scale met, what they are relative to
 
     if (warp == kConsumerWarps) {
         // ---------------- producer: one lane issues the TMA loads
@@ -802,11 +768,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                 const uint32_t dst = ring + s * kStageBytes;
                 const int y = (int)(row0 + begin + it * kTT);
                 mbar_arrive_expect_tx(full, kStageBytes);
-                if (kInt4) {                                 // 64-byte rows; sixteen rows' scales are one row of their map
-                    tma_load_2d(dst, &k_map, 0, y, full, stream_policy);
-                    tma_load_2d(dst + kTileBytes, &v_map, 0, y, full, stream_policy);
-                    tma_load_2d(dst + 2 * kTileBytes, &s_map, 0, y >> 4, full, stream_policy);
-                } else if (kFp8) {                           // one 128-byte-wide box holds the whole row
+                if (kFp8) {                                  // one 128-byte-wide box holds the whole row
                     tma_load_2d(dst, &k_map, 0, y, full, stream_policy);
                     tma_load_2d(dst + kTileBytes, &v_map, 0, y, full, stream_policy);
                 } else {
@@ -825,62 +787,8 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
         // channels 2 t, 2 t + 1 (q0) and 8 + 2 t, 9 + 2 t (q1); for FP8 slabs the channels 4 t .. 4 t + 3, the order
         // in which the four bytes of a K register arrive (the contraction index may be permuted at will)
         uint32_t qq[2 * kKSteps];                          // (q0, q1) of step ks side by side, as the MMA takes them
-        uint32_t ql[kInt4 && !kTwice ? 2 * kKSteps : 1];   // 4-bit slabs: the second fp16 term of the same
-        float q_off[2] = {0.0f, 0.0f}, q_fac[2] = {1.0f, 1.0f};   // 4-bit slabs, this lane's two heads: offset, factor
-        const int q_head = kTwice ? g8 & 3 : g8;
-        const __nv_bfloat16* q_ptr = p.q + ((int64_t)(u.li * p.B + u.b) * p.Hq + u.h * G + q_head) * D;
-        if (kInt4) {
-            // lane t holds, of each group of 32 channels, the eight of word t of a K row's 16 bytes
-            float x[D / 4];
-            float big = 0.0f;
-            const float* chan = p.kv_scale + (int64_t)u.head * 4 * D;
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-                const uint4 raw = q_head < G ? *reinterpret_cast<const uint4*>(q_ptr + 32 * c + 8 * t4) : make_uint4(0u, 0u, 0u, 0u);
-                const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
-                    const float2 cs = *reinterpret_cast<const float2*>(chan + 32 * c + 8 * t4 + 2 * i);
-                    x[8 * c + 2 * i] = f.x * cs.x;
-                    x[8 * c + 2 * i + 1] = f.y * cs.y;
-                    big = fmaxf(big, fmaxf(fabsf(x[8 * c + 2 * i]), fabsf(x[8 * c + 2 * i + 1])));
-                }
-            }
-            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-            // to [2^12, 2^13): a power of two, which the logits are multiplied by again (with the codes' 2^24)
-            const int ex = min(max((int)(__float_as_uint(big) >> 23), 32), 222);     // biased exponent
-            const float up = __uint_as_float((uint32_t)(127 + 12 + 127 - ex) << 23);
-            const float back = __uint_as_float((uint32_t)(ex - 12 + 24) << 23);
-            float sum = 0.0f;
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {              // nibbles (j, j + 4) of the word
-                    const float k = (j & 1) ? 0.0625f : 1.0f;      // odd nibbles stand 16 times higher
-                    const float a = x[8 * c + j] * up * k, b = x[8 * c + j + 4] * up * k;
-                    const uint32_t hi = pack_f16(a, b);
-                    const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-                    const uint32_t lo = pack_f16(a - h.x, b - h.y);
-                    const float2 l = __half22float2(*reinterpret_cast<const __half2*>(&lo));
-                    if (kTwice) {
-                        qq[4 * c + j] = g8 < 4 ? hi : lo;
-                    } else {
-                        qq[4 * c + j] = hi;
-                        ql[4 * c + j] = lo;
-                    }
-                    sum = fmaf((h.x + l.x) + (h.y + l.y), (j & 1) ? 16.0f : 1.0f, sum);
-                }
-            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                q_off[e] = -8.0f * 0x1p-24f * __shfl_sync(0xffffffffu, sum, 4 * (2 * t4 + e));
-                if (kTwice && t4 >= 2) q_off[e] = 0.0f;    // (once per head)
-                q_fac[e] = __shfl_sync(0xffffffffu, back, 4 * (2 * t4 + e)) * p.scale_log2;
-            }
-        } else {
+        {
+            const __nv_bfloat16* q_ptr = p.q + ((int64_t)(u.li * p.B + u.b) * p.Hq + u.h * G + g8) * D;
 #pragma unroll
             for (int ks = 0; ks < kKSteps; ++ks) {
                 if (kFp8) {
@@ -907,9 +815,6 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
         // V load (rows of the MMA = channels) it is the other way round.
         const uint32_t k_lane = kFp8 ? (uint32_t)(((lm >> 1) * 8 + li8) * 128 + ((li8 ^ (lm & 1)) << 4))    // rows (lm / 2) * 8 + .., b = lm % 2
                                      : (uint32_t)(((lm & 1) * 8 + li8) * 128 + ((li8 ^ (lm >> 1)) << 4));   // rows (lm % 2) * 8 + .., b = lm / 2
-        // 4-bit rows are 64 bytes, written with the 64-byte swizzle (piece c of row r at position c ^ (r / 2 % 4)); the
-        // same addresses serve K and the transposed V: matrices (token half) x (16-byte piece)
-        const uint32_t n_lane = (uint32_t)(((lm & 1) * 8 + li8) * 64 + (((lm >> 1) ^ (li8 >> 1)) << 4));
         const uint32_t v_lane = kFp8 ? (uint32_t)(((lm & 1) * 8 + li8) * 128 + ((li8 ^ (lm >> 1)) << 4))
                                      : (uint32_t)(((lm >> 1) * 8 + li8) * 128 + ((li8 ^ (lm & 1)) << 4));
         // where this lane leaves the probabilities of head g8 (tokens 2 t4, 2 t4 + 1 of a block) for the score pass
@@ -944,29 +849,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                             const int64_t src = ((int64_t)(u.li * p.B + u.b) * p.Hkv + u.h) * D;
                             const int64_t row = row0 + hs.f;
                             uint8_t* k_ptr = ring_ptr + s * kStageBytes;
-                            if (kInt4) {                     // quantise the row: four elements per lane, both operands
-                                const float* chan = p.kv_scale + (int64_t)u.head * 4 * D;
-                                const int r = r0 + (hs.f - tok0);
-#pragma unroll
-                                for (int is_v = 0; is_v < 2; ++is_v) {
-                                    const uint2 raw = *(reinterpret_cast<const uint2*>((is_v ? p.v_new : p.k_new) + src) + lane);
-                                    const float4 inv = *(reinterpret_cast<const float4*>(chan + (2 * is_v + 1) * D) + lane);
-                                    float y[4];
-                                    int4q::scaled4(raw, inv, y);
-                                    uint32_t top = int4q::largest_bits(y);
-                                    top = __reduce_max_sync(0xffffffffu, top);
-                                    const float rs = int4q::row_scale(top);
-                                    const uint16_t val = (uint16_t)int4q::codes4(y, rs);
-                                    *reinterpret_cast<uint16_t*>(k_ptr + is_v * kTileBytes + r * 64 +
-                                                                 (((lane >> 3) ^ ((r >> 1) & 3)) << 4) + (lane & 7) * 2) = val;
-                                    uint8_t* slab = reinterpret_cast<uint8_t*>(is_v ? p.v_slab : p.k_slab);
-                                    *(reinterpret_cast<uint16_t*>(slab + row * kRowBytes) + lane) = val;
-                                    if (lane == 0) {
-                                        reinterpret_cast<float*>(k_ptr + 2 * kTileBytes)[2 * r + is_v] = rs;
-                                        p.row_scale[2 * row + is_v] = rs;
-                                    }
-                                }
-                            } else if (kFp8) {               // quantise the row: eight elements per lane and operand
+                            if (kFp8) {                      // quantise the row: eight elements per lane and operand
                                 for (int i = lane; i < 2 * kVec; i += 32) {
                                     const bool is_v = i >= kVec;
                                     const int c = is_v ? i - kVec : i;
@@ -990,8 +873,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                             __syncwarp();
                         }
                         // rows past the end of the head (or the freed slot) may hold anything: keep them out of P.V
-                        // (4-bit codes are finite whatever they are; the rows' scales are left out below)
-                        if (!kInt4) if (valid < kWarpTokens || (hole >= tok0 && hole < tok0 + kWarpTokens)) {
+                        if (valid < kWarpTokens || (hole >= tok0 && hole < tok0 + kWarpTokens)) {
                             uint8_t* v_ptr = ring_ptr + s * kStageBytes + kTileBytes;
                             constexpr int kPieces = kRowBytes / 16;     // 16-byte pieces of a row
                             for (int i = lane; i < kWarpTokens * kPieces; i += 32) {
@@ -1002,149 +884,6 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                             __syncwarp();
                         }
                     }
-                }
-                if constexpr (kInt4) {
-                    constexpr int kR = kTwice ? 1 : 2;            // token rows per lane and block
-                    const bool upper = kTwice && t4 >= 2;
-                    float st[kBlocks][4];
-#pragma unroll
-                    for (int blk = 0; blk < kBlocks; ++blk) {
-                        st[blk][0] = st[blk][2] = q_off[0];
-                        st[blk][1] = st[blk][3] = q_off[1];
-                    }
-                    // the blocks' chains of MMAs side by side: an accumulator is added to every kBlocks-th MMA only
-#pragma unroll
-                    for (int cc = 0; cc < D / 64; ++cc) {         // 64 channels per load: (tokens 0-7 | 8-15) x two pieces
-                        uint32_t kb[kBlocks][4];
-#pragma unroll
-                        for (int blk = 0; blk < kBlocks; ++blk)
-                            ldmatrix_x4(k_tile + (uint32_t)((w0 + blk * kWarpTokens) * 64) + (n_lane ^ (uint32_t)(cc << 5)), kb[blk]);
-#pragma unroll
-                        for (int x = 0; x < 2; ++x)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) {         // nibbles (0, 4 | 1, 5), then (2, 6 | 3, 7)
-                                const int at = 4 * (2 * cc + x) + 2 * j;
-#pragma unroll
-                                for (int term = 0; term < (kTwice ? 1 : 2); ++term)
-#pragma unroll
-                                    for (int blk = 0; blk < kBlocks; ++blk) {
-                                        const uint32_t lo = kb[blk][2 * x] >> (8 * j), hi = kb[blk][2 * x + 1] >> (8 * j);
-                                        const uint32_t* b = term ? ql : qq;
-                                        mma_f16_free(st[blk], lo & 0x000f000fu, hi & 0x000f000fu, lo & 0x00f000f0u, hi & 0x00f000f0u,
-                                                     b[at], b[at + 1]);
-                                    }
-                            }
-                    }
-                    // kTwice: lane t has the first terms of heads 2 t, 2 t + 1 for tokens g and g + 8, lane t + 2 the
-                    // second terms: they swap a token, after which the lower lanes hold token g, the upper token g + 8
-                    float lg[kBlocks][kR][2];
-                    float sv[kBlocks][kR];                        // V scales of this lane's rows
-                    float mx[2] = {-INFINITY, -INFINITY}, sv_max = 0.0f;
-                    bool ok[kBlocks][kR];
-                    const float2* const scales = reinterpret_cast<const float2*>(ring_ptr + s * kStageBytes + 2 * kTileBytes) + w0;
-#pragma unroll
-                    for (int blk = 0; blk < kBlocks; ++blk)
-#pragma unroll
-                        for (int r = 0; r < kR; ++r) {
-                            const int at = blk * kWarpTokens + g8 + (kTwice ? (upper ? 8 : 0) : 8 * r);
-                            const int tok = wtok0 + at;
-                            ok[blk][r] = !kCareful || (tok < end && tok != hole);
-                            const float2 rs = scales[at];
-                            sv[blk][r] = ok[blk][r] ? rs.y : 0.0f;
-                            sv_max = fmaxf(sv_max, fabsf(sv[blk][r]));
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                float x = st[blk][2 * r + e];
-                                if (kTwice) {
-                                    const float give = upper ? st[blk][e] : st[blk][2 + e];
-                                    x = (upper ? st[blk][2 + e] : st[blk][e]) + __shfl_xor_sync(0xffffffffu, give, 2);
-                                }
-                                lg[blk][r][e] = x * rs.x;         // (the head's factor follows, with the maximum)
-                                if (ok[blk][r]) mx[e] = fmaxf(mx[e], lg[blk][r][e]);
-                            }
-                        }
-                    float corr[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        if (kTwice) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
-                        mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 4));
-                        mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 8));
-                        mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 16));
-                        const float m_new = fmaxf(m_run[e], mx[e] * q_fac[e]);      // (positive)
-                        corr[e] = (m_new == -INFINITY) ? 1.0f : fast_exp2(m_run[e] - m_new);
-                        m_run[e] = m_new;
-                        float psum = 0.0f;
-#pragma unroll
-                        for (int blk = 0; blk < kBlocks; ++blk)
-#pragma unroll
-                            for (int r = 0; r < kR; ++r) {
-                                lg[blk][r][e] = ok[blk][r] ? fast_exp2(fmaf(lg[blk][r][e], q_fac[e], -m_new)) : 0.0f;
-                                psum += lg[blk][r][e];
-                            }
-                        l_run[e] = l_run[e] * corr[e] + psum;
-                    }
-                    // the V scales' reference follows their maximum
-                    const float seen = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv_max)));
-                    if (seen > v_ref) {
-                        const float ratio = v_ref / seen;
-                        corr[0] *= ratio;
-                        corr[1] *= ratio;
-                        v_ref = seen;
-                        v_inv = 1.0f / seen;
-                    }
-                    if (__any_sync(0xffffffffu, corr[0] != 1.0f || corr[1] != 1.0f)) {
-#pragma unroll
-                        for (int j = 0; j < D / 16; ++j) { o[j][0] *= corr[0]; o[j][1] *= corr[1]; o[j][2] *= corr[0]; o[j][3] *= corr[1]; }
-                        o8[0] *= corr[0]; o8[1] *= corr[1]; o8[2] *= corr[0]; o8[3] *= corr[1];
-                    }
-#pragma unroll
-                    for (int blk = 0; blk < kBlocks; ++blk) {
-                        const int tok0 = wtok0 + blk * kWarpTokens;
-                        // P^T as the B operand: the transposed 8 x 8 block gives lane (g, t) head g, tokens 2 t, 2 t + 1;
-                        // kTwice: the lanes g >= 4 get head g - 4, tokens 8 + 2 t, 9 + 2 t, which the lane 16 below needs
-                        uint32_t pb[2], pr[2];
-#pragma unroll
-                        for (int r = 0; r < kR; ++r) {
-                            const float f = sv[blk][r] * v_inv;
-                            pb[r] = movmatrix_trans(pack_f16(lg[blk][r][0] * f, lg[blk][r][1] * f));
-                            if (keep_logits) pr[r] = movmatrix_trans(pack_f16(lg[blk][r][0], lg[blk][r][1]));
-                        }
-                        if (kTwice) pb[1] = __shfl_xor_sync(0xffffffffu, pb[0], 16);
-                        if (keep_logits) {
-                            // the unnormalised probabilities, in fp16, and the maximum they were taken under
-                            __half* dst = kTwice ? prob_h + (int64_t)(g8 & 3) * C + 2 * t4 + 8 * (g8 >> 2) + tok0 : prob_lane + tok0;
-#pragma unroll
-                            for (int r = 0; r < kR; ++r) {
-                                const int left = end - (tok0 + 2 * t4 + (kTwice ? 8 * (g8 >> 2) : 8 * r));
-                                if (q_head < G) {
-                                    if (!kCareful || left >= 2) *reinterpret_cast<uint32_t*>(dst + 8 * r) = pr[r];
-                                    else if (left == 1) dst[8 * r] = __ushort_as_half((unsigned short)(pr[r] & 0xffffu));
-                                }
-                            }
-                            if (g8 == 0 && (!kCareful || tok0 < end)) {
-                                if (2 * t4 < G) mref_h[(2 * t4) * (C >> 4) + (tok0 >> 4)] = m_run[0];
-                                if (2 * t4 + 1 < G) mref_h[(2 * t4 + 1) * (C >> 4) + (tok0 >> 4)] = m_run[1];
-                            }
-                        }
-                        // a register of the transposed load = two tokens x four adjacent channels; row g of MMA j is
-                        // channel 4 g + 2 j of the 32-channel group, row g + 8 channel 4 g + 2 j + 1 (16 times too large)
-                        const uint32_t n_row = v_tile + (uint32_t)((w0 + blk * kWarpTokens) * 64);
-                        mma_f16_free(o8, 0x00080008u, 0x00800080u, 0x00080008u, 0x00800080u, pb[0], pb[1]);
-#pragma unroll
-                        for (int cc = 0; cc < D / 64; ++cc) {
-                            uint32_t vb[4];
-                            ldmatrix_x4_trans(n_row + (n_lane ^ (uint32_t)(cc << 5)), vb);
-#pragma unroll
-                            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) {
-                                    const uint32_t lo = vb[2 * x] >> (8 * j), hi = vb[2 * x + 1] >> (8 * j);   // tokens 0-7, 8-15
-                                    mma_f16_free(o[4 * cc + 2 * x + j], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu,
-                                                 hi & 0x00f000f0u, pb[0], pb[1]);
-                                }
-                        }
-                    }
-                    return;
                 }
                 // S^T = K Q^T for the warp's tokens: st[blk] = (token g: heads 2 t, 2 t + 1; token g + 8: the same)
                 float st[kBlocks][4];
@@ -1314,7 +1053,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
         if (tid < G) part[G * D + tid] = __int_as_float(0x7fc00000);
     }
     // A head of one chunk whose scores are not kept needs no partial and no arrival: its output is written from here
-    // (the same numbers: a single partial has weight 1).  The batch of 16 short caches has a CTA per head.
+    // (the same numbers: a single partial has weight 1).
     const bool direct = active == 1 && !keep_logits && !pos_evict;
     if (!aborted) {
     // ---- the four warps' states -> one partial for the chunk (the ring is idle now: reuse it)
@@ -1332,13 +1071,11 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
         // the sums were kept per lane (its own token rows): add them up over the eight row groups
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            if (kTwice) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 2);
             l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 4);
             l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 8);
             l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 16);
         }
-        const float sv_ = kInt4 ? v_ref * 0x1p24f : kFp8 ? p.kv_scale[u.head * 4 + 2] : 1.0f;
-        const float* v_chan = kInt4 ? p.kv_scale + ((int64_t)u.head * 4 + 2) * D : nullptr;
+        const float sv_ = kFp8 ? p.kv_scale[u.head * 4 + 2] : 1.0f;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int head = 2 * t4 + e;
@@ -1346,12 +1083,7 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
                 float* dst = sm_o + (warp * G + head) * D;
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
-                    if (kInt4) {                            // rows g and g + 8: channels 4 g + 2 j, 4 g + 2 j + 1 of 32
-                        const int ch = 32 * (c >> 1) + 4 * g8 + 2 * (c & 1);
-                        const float2 cs = *reinterpret_cast<const float2*>(v_chan + ch);
-                        *reinterpret_cast<float2*>(dst + ch) = make_float2((o[c][e] - o8[e]) * sv_ * cs.x,
-                                                                           (o[c][2 + e] - o8[2 + e]) * (sv_ * 0.0625f) * cs.y);
-                    } else if (kFp8) {                      // rows g and g + 8 of the MMA are channels 2 g and 2 g + 1
+                    if (kFp8) {                             // rows g and g + 8 of the MMA are channels 2 g and 2 g + 1
                         *reinterpret_cast<float2*>(dst + 16 * c + 2 * g8) = make_float2(o[c][e] * sv_, o[c][2 + e] * sv_);
                     } else {
                         dst[16 * c + g8] = o[c][e];
@@ -1408,6 +1140,8 @@ decode_chunk_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
     // ---- this CTA delivered the head's last partial and finishes the head
     finish_head<D, kByPosition>(&p, reinterpret_cast<float*>(ring_ptr), unit, piece, active);   // the ring is idle now
 }
+
+#include "decode_int4.cuh"
 
 // ---------------------------------------------------------------- steps 3-4 as a kernel of their own
 // A short launch (one layer of one sequence) ends with a few long heads, and one CTA sweeping a long head would
@@ -1612,46 +1346,44 @@ bool make_slab_map_fp8(CUtensorMap* map, void* base, int64_t rows, int D) {
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// 4-bit slabs: D / 2 bytes per row, boxes of one stage's rows x 64 bytes (the whole row), 64-byte swizzle
+// 4-bit slabs: two rows of D / 2 bytes to a row of the map (rows come in multiples of 16), boxes of one tile's rows,
+// 128-byte swizzle
 bool make_slab_map_int4(CUtensorMap* map, void* base, int64_t rows, int D) {
     EncodeTiledFn enc = encode_tiled_fn();
     if (!enc) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)D / 2, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)D / 2};
-    const cuuint32_t box[2] = {(cuuint32_t)D / 2, (cuuint32_t)kInt4StageTokens};
+    const cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows / 2};
+    const cuuint64_t strides[1] = {(cuuint64_t)D};
+    const cuuint32_t box[2] = {(cuuint32_t)D, (cuuint32_t)kInt4Tokens / 2};
     const cuuint32_t estr[2] = {1, 1};
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The rows' pairs of scales, sixteen rows (128 bytes) to a row of the map (rows come in multiples of 16): the second
-// coordinate stays in 32 bits however long the cache, and a stage is one box.
+// The rows' pairs of scales, sixteen rows (128 bytes) to a row of the map: the second coordinate stays in 32 bits
+// however long the cache, and a tile is one box.
 bool make_scale_map_int4(CUtensorMap* map, void* base, int64_t rows) {
     EncodeTiledFn enc = encode_tiled_fn();
     if (!enc) return false;
     const cuuint64_t dims[2] = {32, (cuuint64_t)rows / 16};
     const cuuint64_t strides[1] = {128};
-    const cuuint32_t box[2] = {32, (cuuint32_t)kInt4StageTokens / 16};
+    const cuuint32_t box[2] = {32, (cuuint32_t)kInt4Tokens / 16};
     const cuuint32_t estr[2] = {1, 1};
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool kByPosition, int kKv = BAKLAVA_KV_BF16, bool kTwice = false>
-cudaError_t launch_chunks(const DecodeParams& p, const CUtensorMap& km, const CUtensorMap& vm, const CUtensorMap& sm,
-                          cudaStream_t s) {
-    constexpr int kRing = kKv == BAKLAVA_KV_INT4 ? kInt4Stages * kInt4StageTokens * (D + 8)
-                          : kKv == BAKLAVA_KV_FP8_E4M3 ? kFp8Stages * 2 * kFp8StageTokens * D : kStages * 2 * kTileTokens * D * 2;
-    constexpr int kSmem = kRing + 1024;
+// one CTA per work item, `threads` wide, with programmatic stream serialisation
+template <typename... Args>
+cudaError_t launch_items(void (*kernel)(Args...), std::atomic<uint64_t>& configured, int threads, int smem, int n_items,
+                         cudaStream_t s, const Args&... args) {
     // the attribute belongs to the function on the current device: set once per device and instantiation
-    static std::atomic<uint64_t> configured{0};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !(configured.load(std::memory_order_acquire) >> dev & 1)) {
-        e = cudaFuncSetAttribute(decode_chunk_kernel<D, kByPosition, kKv, kTwice>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
         if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
     }
@@ -1659,13 +1391,26 @@ cudaError_t launch_chunks(const DecodeParams& p, const CUtensorMap& km, const CU
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)p.n_items);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kSmem;
+    cfg.gridDim = dim3((unsigned)n_items);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, decode_chunk_kernel<D, kByPosition, kKv, kTwice>, p, km, vm, sm);
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int D, bool kByPosition, bool kFp8 = false>
+cudaError_t launch_chunks(const DecodeParams& p, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t s) {
+    constexpr int kSmem = (kFp8 ? kFp8Stages * 2 * kFp8StageTokens * D : kStages * 2 * kTileTokens * D * 2) + 1024;
+    static std::atomic<uint64_t> configured{0};
+    return launch_items(decode_chunk_kernel<D, kByPosition, kFp8>, configured, kThreads, kSmem, p.n_items, s, p, km, vm);
+}
+
+template <bool kByPosition, bool kTwice>
+cudaError_t launch_int4(const DecodeParams& p, const CUtensorMap& km, const CUtensorMap& vm, const CUtensorMap& sm, cudaStream_t s) {
+    static std::atomic<uint64_t> configured{0};
+    return launch_items(decode_int4_kernel<kByPosition, kTwice>, configured, kInt4Threads, kInt4Smem, p.n_items, s, p, km, vm, sm);
 }
 
 }  // namespace
@@ -1767,11 +1512,11 @@ int decode_attn_impl(
 
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t err = cudaSuccess;
-    if (four_bit && p.G <= 4) err = p.window_evict ? launch_chunks<128, true, BAKLAVA_KV_INT4, true>(p, k_map, v_map, s_map, s) : launch_chunks<128, false, BAKLAVA_KV_INT4, true>(p, k_map, v_map, s_map, s);
-    else if (four_bit) err = p.window_evict ? launch_chunks<128, true, BAKLAVA_KV_INT4>(p, k_map, v_map, s_map, s) : launch_chunks<128, false, BAKLAVA_KV_INT4>(p, k_map, v_map, s_map, s);
-    else if (fp8) err = p.window_evict ? launch_chunks<128, true, BAKLAVA_KV_FP8_E4M3>(p, k_map, v_map, s_map, s) : launch_chunks<128, false, BAKLAVA_KV_FP8_E4M3>(p, k_map, v_map, s_map, s);
-    else if (p.window_evict) err = shape->D == 128 ? launch_chunks<128, true>(p, k_map, v_map, s_map, s) : launch_chunks<64, true>(p, k_map, v_map, s_map, s);
-    else err = shape->D == 128 ? launch_chunks<128, false>(p, k_map, v_map, s_map, s) : launch_chunks<64, false>(p, k_map, v_map, s_map, s);
+    if (four_bit && p.G <= 4) err = p.window_evict ? launch_int4<true, true>(p, k_map, v_map, s_map, s) : launch_int4<false, true>(p, k_map, v_map, s_map, s);
+    else if (four_bit) err = p.window_evict ? launch_int4<true, false>(p, k_map, v_map, s_map, s) : launch_int4<false, false>(p, k_map, v_map, s_map, s);
+    else if (fp8) err = p.window_evict ? launch_chunks<128, true, true>(p, k_map, v_map, s) : launch_chunks<128, false, true>(p, k_map, v_map, s);
+    else if (p.window_evict) err = shape->D == 128 ? launch_chunks<128, true>(p, k_map, v_map, s) : launch_chunks<64, true>(p, k_map, v_map, s);
+    else err = shape->D == 128 ? launch_chunks<128, false>(p, k_map, v_map, s) : launch_chunks<64, false>(p, k_map, v_map, s);
     if (err != cudaSuccess) return BAKLAVA_ERR_CUDA;
     if (p.split_tail) {
         cudaLaunchAttribute attr[1];
