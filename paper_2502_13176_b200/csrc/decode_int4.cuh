@@ -86,6 +86,24 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     const int unit = item.x, begin = item.y, chunk_len = item.z, piece = item.w & 0xffff;
     const Unit u = decode_unit(p, unit);
     if (!overlap) launch_dependents();
+    // what depends on the head alone is asked for together with its state: the query, its K channel scales (lane t of a
+    // quad: of each group of 32 channels the eight of word t of a K row's 16 bytes), a V channel scale per thread
+    const int g8 = lane >> 2, t4 = lane & 3;
+    const int q_head = kTwice ? g8 & 3 : g8;
+    uint4 q_raw[D / 32];
+    float4 k_chan[D / 32][2];
+    {
+        const __nv_bfloat16* q_ptr = p.q + ((int64_t)(u.li * p.B + u.b) * p.Hq + u.h * G + q_head) * D + 8 * t4;
+        const float* chan = p.kv_scale + (int64_t)u.head * 4 * D + 8 * t4;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+            q_raw[c] = q_head < G ? *reinterpret_cast<const uint4*>(q_ptr + 32 * c) : make_uint4(0u, 0u, 0u, 0u);
+            k_chan[c][0] = *reinterpret_cast<const float4*>(chan + 32 * c);
+            k_chan[c][1] = *reinterpret_cast<const float4*>(chan + 32 * c + 4);
+        }
+    }
+    static_assert(kInt4Threads == D, "a thread owns one channel of the merged output");
+    const float v_chan = p.kv_scale[((int64_t)u.head * 4 + 2) * D + tid];
     const int t_pos = p.t_pos_seq ? p.t_pos_seq[u.b] : p.t_pos;
     const HeadState hs = head_state(p, u);
     const int C = hs.C, n = hs.n, hole = hs.hole, n_hi = hs.n_att;
@@ -141,7 +159,6 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     if (lane == 0)
         for (int j = 0; j < min(fed, kInt4Slots); ++j) { load_k(j); load_v(j); }
 
-    const int g8 = lane >> 2, t4 = lane & 3;
     float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
     float o[D / 16][4];
 #pragma unroll
@@ -149,22 +166,17 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     float o8[4] = {0.0f, 0.0f, 0.0f, 0.0f};               // eight times the sums of the probabilities used
     float v_ref = 0.0f, v_inv = 0.0f;                     // largest V row scale met, what the probabilities are relative to
 
-    // ---- query fragments (B operand): head g (kTwice: first terms for g < 4, second terms for g >= 4), of each group of 32
-    // channels the eight of word t of a K row's 16 bytes; registers j = 0 .. 3 are the nibbles (j, j + 4)
+    // ---- query fragments (B operand): head g (kTwice: first terms for g < 4, second terms for g >= 4); registers
+    // j = 0 .. 3 of a group of 32 channels are the nibbles (j, j + 4)
     uint32_t qq[D / 8], ql[kTwice ? 1 : D / 8];
     float q_off[2], q_fac[2];                             // this lane's two heads: offset, factor of the logits
-    const int q_head = kTwice ? g8 & 3 : g8;
     {
-        const __nv_bfloat16* q_ptr = p.q + ((int64_t)(u.li * p.B + u.b) * p.Hq + u.h * G + q_head) * D;
-        const float* chan = p.kv_scale + (int64_t)u.head * 4 * D;
         float x[D / 4];
         float big = 0.0f;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
-            const uint4 raw = q_head < G ? *reinterpret_cast<const uint4*>(q_ptr + 32 * c + 8 * t4) : make_uint4(0u, 0u, 0u, 0u);
-            const float4 ca = *reinterpret_cast<const float4*>(chan + 32 * c + 8 * t4);
-            const float4 cb = *reinterpret_cast<const float4*>(chan + 32 * c + 8 * t4 + 4);
-            const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+            const float4 ca = k_chan[c][0], cb = k_chan[c][1];
+            const uint32_t w[4] = {q_raw[c].x, q_raw[c].y, q_raw[c].z, q_raw[c].w};
             const float cs[8] = {ca.x, ca.y, ca.z, ca.w, cb.x, cb.y, cb.z, cb.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -464,7 +476,6 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
             }
             if (lane == 0) { sm_old_pos[warp] = old_pos; sm_old_slot[warp] = old_slot; }
         }
-        const float* v_chan = p.kv_scale + ((int64_t)u.head * 4 + 2) * D;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {                      // the sums were kept per lane (its own token rows)
             if (kTwice) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], 2);
@@ -477,16 +488,15 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
                     const int ch = 32 * (c >> 1) + 4 * g8 + 2 * (c & 1);
-                    const float2 cs = *reinterpret_cast<const float2*>(v_chan + ch);
-                    *reinterpret_cast<float2*>(dst + ch) = make_float2((o[c][e] - o8[e]) * (v_ref * 0x1p24f) * cs.x,
-                                                                       (o[c][2 + e] - o8[2 + e]) * (v_ref * 0x1p20f) * cs.y);
+                    *reinterpret_cast<float2*>(dst + ch) = make_float2((o[c][e] - o8[e]) * (v_ref * 0x1p24f),
+                                                                       (o[c][2 + e] - o8[2 + e]) * (v_ref * 0x1p20f));
                 }
                 if (g8 == 0) { sm_m[warp][head] = m_run[e]; sm_l[warp][head] = l_run[e]; }
             }
         }
         __syncthreads();
-        for (int i = tid; i < G * D; i += kInt4Threads) {
-            const int a = i / D, d = i - a * D;
+        for (int a = 0; a < G; ++a) {
+            const int d = tid, i = a * D + d;
             float mm = -INFINITY;
 #pragma unroll
             for (int w = 0; w < kInt4Warps; ++w) mm = fmaxf(mm, sm_m[w][a]);
@@ -497,6 +507,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
                 acc = fmaf(sm_o[(w * G + a) * D + d], c, acc);
                 lsum = fmaf(sm_l[w][a], c, lsum);
             }
+            acc *= v_chan;
             if (direct) {
                 const int64_t at = (int64_t)(u.li * p.B + u.b) * p.Hq + u.h * G + a;
                 p.out[at * D + d] = __float2bfloat16_rn(acc * (lsum > 0.0f ? 1.0f / lsum : 0.0f));
