@@ -18,7 +18,7 @@
 // would have had the group's missing heads.
 //
 // Four warps, each with its own tiles of 64 tokens (tiles w, w + 4, ... of the chunk) in two slots of its own, which it
-// refills itself: K and the scales as soon as the logits are formed, V after the product.  No warp waits for another
+// refills itself.  No warp waits for another
 // before the end of the chunk (with one ring for all of them and a producer warp, a fifth of the time went into
 // waiting for the slowest), and the tiles in flight are the same 64 KB per CTA.
 
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     constexpr int kBlocks = kInt4Blocks;
     constexpr int kG = BAKLAVA_MAX_GROUP;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bar_k[kInt4Warps][kInt4Slots], bar_v[kInt4Warps][kInt4Slots];
+    __shared__ __align__(8) uint64_t bar[kInt4Warps][kInt4Slots];
     __shared__ float sm_m[kInt4Warps][kG];
     __shared__ float sm_l[kInt4Warps][kG];
     __shared__ int sm_last, sm_abort;
@@ -71,8 +71,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     if (tid == 0) {
         for (int w = 0; w < kInt4Warps; ++w)
             for (int s = 0; s < kInt4Slots; ++s) {
-                mbar_init(smem_u32(&bar_k[w][s]), 1);
-                mbar_init(smem_u32(&bar_v[w][s]), 1);
+                mbar_init(smem_u32(&bar[w][s]), 1);
             }
         sm_abort = 0;
         ptx::fence_mbar_init();
@@ -143,21 +142,16 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     // test aid (BAKLAVA_FLAG_TEST_STALL): the first chunk of a head is fed its first tile only
     const int fed = (p.flags & BAKLAVA_FLAG_TEST_STALL) && piece == 0 ? (warp == 0 ? min(mine, 1) : 0) : mine;
     const uint64_t stream_policy = l2_evict_first_policy();
-    auto load_k = [&](int j) {                             // one lane
+    auto load = [&](int j) {                               // one lane
         const int y = (int)(row0 + begin + (kInt4Warps * j + warp) * kInt4Tokens), s = j % kInt4Slots;
-        const uint32_t bar = smem_u32(&bar_k[warp][s]);
-        mbar_arrive_expect_tx(bar, kInt4TileBytes + kInt4ScaleBytes);
-        tma_load_2d(ring + my_tiles + 2 * s * kInt4TileBytes, &k_map, 0, y >> 1, bar, stream_policy);
-        tma_load_2d(ring + my_scales + s * kInt4ScaleBytes, &s_map, 0, y >> 4, bar, stream_policy);
-    };
-    auto load_v = [&](int j) {
-        const int y = (int)(row0 + begin + (kInt4Warps * j + warp) * kInt4Tokens), s = j % kInt4Slots;
-        const uint32_t bar = smem_u32(&bar_v[warp][s]);
-        mbar_arrive_expect_tx(bar, kInt4TileBytes);
-        tma_load_2d(ring + my_tiles + (2 * s + 1) * kInt4TileBytes, &v_map, 0, y >> 1, bar, stream_policy);
+        const uint32_t full = smem_u32(&bar[warp][s]), dst = ring + my_tiles + 2 * s * kInt4TileBytes;
+        mbar_arrive_expect_tx(full, 2 * kInt4TileBytes + kInt4ScaleBytes);
+        tma_load_2d(dst, &k_map, 0, y >> 1, full, stream_policy);
+        tma_load_2d(ring + my_scales + s * kInt4ScaleBytes, &s_map, 0, y >> 4, full, stream_policy);
+        tma_load_2d(dst + kInt4TileBytes, &v_map, 0, y >> 1, full, stream_policy);
     };
     if (lane == 0)
-        for (int j = 0; j < min(fed, kInt4Slots); ++j) { load_k(j); load_v(j); }
+        for (int j = 0; j < min(fed, kInt4Slots); ++j) load(j);
 
     float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
     float o[D / 16][4];
@@ -225,7 +219,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     const uint32_t n_lane = int4_offset((lm & 1) * 8 + li8, lm >> 1);
     __half* const prob_lane = prob_h + (int64_t)q_head * C + 2 * t4 + (kTwice ? 8 * (g8 >> 2) : 0);
 
-    int used_k = 0, used_v = 0;                            // tiles of this warp whose loads have been waited for
+    int used = 0;                                          // tiles of this warp whose loads have been waited for
     bool alive = true;
     for (int j = 0; j < mine && alive; ++j) {
         const int s = j % kInt4Slots;
@@ -238,11 +232,9 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
         // append to nor a freed slot (nearly always), and the careful form that patches the tile and masks rows.
         auto tile_body = [&](auto careful_tag) -> bool {
             constexpr bool kCareful = decltype(careful_tag)::value;
-            if (!mbar_wait(smem_u32(&bar_k[warp][s]), par, p.wait_cycles)) return false;
-            ++used_k;
+            if (!mbar_wait(smem_u32(&bar[warp][s]), par, p.wait_cycles)) return false;
+            ++used;
             if (kCareful) {
-                if (!mbar_wait(smem_u32(&bar_v[warp][s]), par, p.wait_cycles)) return false;
-                ++used_v;
                 const int r = hs.f - tok_t;
                 if (hs.do_append && r >= 0 && r < kInt4Tokens && hs.f < end) {
                     // step 1 (Eq. 4): the new token's row, quantised (four elements per lane), replaces whatever the
@@ -340,8 +332,6 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
                 mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 8));
                 mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 16));
             }
-            __syncwarp();                                  // the maxima are there: K and the scales have been read
-            if (lane == 0 && j + kInt4Slots < fed) load_k(j + kInt4Slots);
             float corr[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -370,10 +360,6 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) { o[i][0] *= corr[0]; o[i][1] *= corr[1]; o[i][2] *= corr[0]; o[i][3] *= corr[1]; }
                 o8[0] *= corr[0]; o8[1] *= corr[1]; o8[2] *= corr[0]; o8[3] *= corr[1];
-            }
-            if (!kCareful) {
-                if (!mbar_wait(smem_u32(&bar_v[warp][s]), par, p.wait_cycles)) return false;
-                ++used_v;
             }
             // ---- P^T as the B operand: the transposed 8 x 8 block gives lane (g, t) head g, tokens 2 t, 2 t + 1; kTwice: the
             // lanes g >= 4 get head g - 4, tokens 8 + 2 t, 9 + 2 t, which the lane 16 below needs
@@ -433,8 +419,8 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
                                      pb[blk][0], pb[blk][1]);
                     }
             }
-            __syncwarp();                                  // V has been read (the volatile MMAs above have their operands)
-            if (lane == 0 && j + kInt4Slots < fed) load_v(j + kInt4Slots);
+            __syncwarp();                                  // the tile has been read (the volatile MMAs above have their operands)
+            if (lane == 0 && j + kInt4Slots < fed) load(j + kInt4Slots);
             return true;
         };
         if (kByPosition && pos_evict) {
@@ -453,9 +439,8 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
         // a bounded wait gave up: the status word says so, and what this warp has requested is left time to land
         atomicOr(p.status, BAKLAVA_STATUS_TIMEOUT);
         sm_abort = 1;
-        const int asked_k = min(fed, used_k + kInt4Slots), asked_v = min(fed, used_v + kInt4Slots);
-        for (int j = used_k; j < asked_k; ++j) mbar_wait(smem_u32(&bar_k[warp][j % kInt4Slots]), (j / kInt4Slots) & 1, p.wait_cycles);
-        for (int j = used_v; j < asked_v; ++j) mbar_wait(smem_u32(&bar_v[warp][j % kInt4Slots]), (j / kInt4Slots) & 1, p.wait_cycles);
+        for (int j = used; j < min(fed, used + kInt4Slots); ++j)
+            mbar_wait(smem_u32(&bar[warp][j % kInt4Slots]), (j / kInt4Slots) & 1, p.wait_cycles);
     }
     __syncthreads();
     const int psz = partial_floats(G, D);
@@ -488,8 +473,8 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
                     const int ch = 32 * (c >> 1) + 4 * g8 + 2 * (c & 1);
-                    *reinterpret_cast<float2*>(dst + ch) = make_float2((o[c][e] - o8[e]) * (v_ref * 0x1p24f),
-                                                                       (o[c][2 + e] - o8[2 + e]) * (v_ref * 0x1p20f));
+                    *reinterpret_cast<float2*>(dst + ch) = make_float2((o[c][e] - o8[e]) * 0x1p24f * v_ref,
+                                                                       (o[c][2 + e] - o8[2 + e]) * 0x1p20f * v_ref);
                 }
                 if (g8 == 0) { sm_m[warp][head] = m_run[e]; sm_l[warp][head] = l_run[e]; }
             }

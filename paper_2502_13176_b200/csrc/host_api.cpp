@@ -217,18 +217,32 @@ extern "C" __attribute__((visibility("default"))) int baklava_decode_plan(const 
     // Chunk length.  A fixed request is used as given.  Otherwise the launch is self-balancing: CTAs are
     // dispatched in item order, so the list starts with long chunks (about half of a CTA slot's share of
     // the tokens: little per-chunk overhead) and ends with short ones (a short tail).
+    auto pieces_of = [](int64_t c, int64_t want) {           // equal pieces of about `want` tokens, whole tiles
+        const int64_t pieces = (c + want - 1) / want;
+        const int64_t len = ((c + pieces - 1) / pieces + kTile - 1) / kTile * kTile;
+        return (c + len - 1) / len;
+    };
     bool guided = chunk_tokens == 0;
     int64_t target = chunk_tokens, min_chunk = kMinChunk;
     if (guided) {
         const int64_t slots = (int64_t)n_sm * kCtasPerSm;
         // what a chunk costs besides its rows (start-up, partial, arrival) is paid per chunk, not per byte: with
         // one-byte rows the same balance between that and the tail of the launch is struck at twice the length
-        // (4-bit rows: the same length as with one-byte rows)
         const int64_t wide = kv_dtype != BAKLAVA_KV_BF16 ? 2 : 1;
         min_chunk = wide * kMinChunk;
         target = (wide * tokens / (2 * slots) + kTile - 1) / kTile * kTile;
         target = std::max<int64_t>(kMinChunk, std::min<int64_t>(target, wide * 4096));
-        if (target == kMinChunk) {
+        if (kv_dtype == BAKLAVA_KV_INT4 && target > kMinChunk) {
+            // 4-bit rows: what a chunk costs besides its rows (start, merge: 10 us, as long as 2500 rows take) outweighs
+            // what a graded list gains at the launch's end.  Equal chunks, the shortest with which the launch is two full
+            // waves (Llama-shaped step 66 us, graded list 70 us; one wave of 8192-token chunks 75 us).
+            guided = false;
+            for (target = 2 * kMinChunk; target < 8192; target += kTile) {
+                int64_t count = 0;
+                for (int i : heads) count += pieces_of(cap[(size_t)layer_begin * Hkv + i], target) * B;
+                if (count <= 2 * slots) break;
+            }
+        } else if (target == kMinChunk) {
             // A short launch (one layer of a model): nothing balances a second, partly filled wave, so all chunks
             // get the same length, the shortest (from the minimum up) with which every chunk is resident at once.
             // (4-bit rows: from twice the minimum; what a chunk costs besides its rows is most of it then, 16.4 us
@@ -237,12 +251,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_decode_plan(const 
             if (kv_dtype == BAKLAVA_KV_INT4) target = 2 * kMinChunk;
             for (; target < 4096; target += kTile) {
                 int64_t count = 0;
-                for (int i : heads) {
-                    const int64_t c = cap[(size_t)layer_begin * Hkv + i];
-                    const int64_t pieces = (c + target - 1) / target;
-                    const int64_t len = ((c + pieces - 1) / pieces + kTile - 1) / kTile * kTile;
-                    count += (c + len - 1) / len * B;
-                }
+                for (int i : heads) count += pieces_of(cap[(size_t)layer_begin * Hkv + i], target) * B;
                 if (count <= slots) break;
             }
         }
