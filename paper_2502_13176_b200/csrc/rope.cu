@@ -16,10 +16,12 @@
 
 #include "baklava.h"
 #include "common.h"
+#include "ptx.cuh"
 
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kAhead = 3;            // rows a thread has asked for while it works on one
 
 struct RopeParams {
     const __nv_bfloat16* in[2];      // queries, keys
@@ -29,127 +31,194 @@ struct RopeParams {
     int32_t heads[2];
     const int32_t* pos;              // [B, T]
     const float* inv_freq;           // [rot / 2]
-    int64_t tokens;                  // B * T
+    uint32_t tokens;                 // B * T
     int32_t T, rot;
     float eps;
 };
 
-__device__ __forceinline__ void widen(const uint4 raw, float* f) {
+// 16 bytes into shared memory without waiting for them; zeros (and no read) where `on` is false
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+// pairs of fp32 values in one 64-bit register: one instruction for both
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float lo, float hi) {
+    f32x2 v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+    return v;
+}
+__device__ __forceinline__ float2 unpack2(f32x2 v) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+    return f;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ f32x2 neg2(f32x2 v) { return v ^ 0x8000000080000000ull; }
+__device__ __forceinline__ f32x2 swap2(f32x2 v) {
+    const float2 f = unpack2(v);
+    return pack2(f.y, f.x);
+}
+__device__ __forceinline__ void widen(const uint4 raw, f32x2 (&f)[4]) {
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 v = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
-        f[2 * i] = v.x;
-        f[2 * i + 1] = v.y;
-    }
+    for (int i = 0; i < 4; ++i) f[i] = pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-__device__ __forceinline__ uint4 narrow(const float* f) {       // the only rounding: once, to the output's type
+__device__ __forceinline__ uint4 narrow(const f32x2 (&f)[4]) {  // the only rounding: once, to the output's type
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        const float2 x = unpack2(f[i]);
+        const __nv_bfloat162 v = __floats2bfloat162_rn(x.x, x.y);
         w[i] = *reinterpret_cast<const uint32_t*>(&v);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// four pairs from shared memory (32 bytes)
+__device__ __forceinline__ void load4(const float* from, f32x2 (&f)[4]) {
+    const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(from), y = *reinterpret_cast<const ulonglong2*>(from + 4);
+    f[0] = x.x; f[1] = x.y; f[2] = y.x; f[3] = y.y;
 }
 
 // kTok tokens per CTA, a power of two.  Thread = (row group, lane of the group); a group keeps its token and walks
 // over the heads.
 template <int D, bool kInterleaved, int kTok>
-__global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const RopeParams p) {
+__global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_kernel(const RopeParams p) {
     constexpr int kLanes = D / 16;                   // lanes per row, two 8-element pieces each
     constexpr int kGroups = kThreads / kLanes;
     constexpr int kHeadStep = kGroups / kTok;        // heads worked on at the same time
-    __shared__ float2 turn[kTok][D / 2 + 1];         // (cos, sin)
+    // cosine and sine as the lanes read them: piece by piece, each the multiplier of the element itself and of its
+    // partner (half-split: cos / sin of the eight pairs; side by side: cos twice, -sin and sin)
+    __shared__ __align__(16) float t_cos[kTok][D], t_sin[kTok][D];
+    __shared__ __align__(16) float wt[2][D];         // the norms' weights
+    __shared__ uint4 ring[kAhead + 1][2][kThreads];  // every thread's two pieces of the rows ahead
     const int tid = threadIdx.x;
-    const int64_t n0 = (int64_t)blockIdx.x * kTok;
-    const int half = p.rot >> 1;
-    for (int i = tid; i < kTok * half; i += kThreads) {
-        const int tk = i / half, f = i - tk * half;
-        if (n0 + tk < p.tokens) {
-            const double turns = (double)p.pos[n0 + tk] * (double)p.inv_freq[f] * 0.15915494309189535;   // 1 / (2 pi)
-            float s, c;
-            sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-            turn[tk][f] = make_float2(c, s);
-        }
-    }
-    __syncthreads();
-
+    const uint32_t n0 = blockIdx.x * kTok;           // (tokens are counted in 31 bits)
     const int lane = tid % kLanes, grp = tid / kLanes;
     const int tk = grp % kTok;
-    const int64_t n = n0 + tk;
-    const bool on = n < p.tokens && p.pos[n] >= 0;   // a negative position: the token sits out
-    const int64_t b = n / p.T, t = n - b * p.T;
+    const uint32_t n = n0 + tk;
+    const bool exists = n < p.tokens;
+    const uint32_t b = n / (uint32_t)p.T, t = n - b * (uint32_t)p.T;
     // this lane's two pieces (of 8 elements): one from each half of the rotated part, or two adjacent unrotated ones
     const int pairs = p.rot >> 4;                    // lanes that hold rotated pieces
     const bool rotates = lane < pairs;
     const int pa = rotates ? lane : 2 * lane, pb = rotates ? lane + pairs : 2 * lane + 1;
-    float cs[8], sn[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        // half-split: pair i of the lane is (element i of piece a, element i of piece b), frequency 8 a + i;
-        // side by side: pairs 0-3 lie in piece a, pairs 4-7 in piece b
-        const int f = kInterleaved ? (i < 4 ? 4 * pa + i : 4 * pb + i - 4) : 8 * pa + i;
-        const float2 v = rotates && on ? turn[tk][f] : make_float2(1.0f, 0.0f);
-        cs[i] = v.x;
-        sn[i] = v.y;
-    }
+    const __nv_bfloat16* src[2];
+    __nv_bfloat16* dst[2];
 #pragma unroll
     for (int op = 0; op < 2; ++op) {
-        const bool norm = p.w[op] != nullptr;
-        float wa[8], wb[8];
-        if (norm) {
-            widen(*(reinterpret_cast<const uint4*>(p.w[op]) + pa), wa);
-            widen(*(reinterpret_cast<const uint4*>(p.w[op]) + pb), wb);
+        src[op] = p.in[op] + b * p.si[op].seq + t * p.si[op].token;
+        dst[op] = p.out[op] + b * p.so[op].seq + t * p.so[op].token;
+    }
+    const int n_heads = p.heads[0] + p.heads[1];     // query heads, then key heads
+    const int n_rows = (n_heads + kHeadStep - 1) / kHeadStep;       // rows of this thread's group, some past the last head
+    auto fetch = [&](int i) {                        // into this thread's own slots: nobody else reads them
+        const int h = i * kHeadStep + grp / kTok;
+        const bool row = exists && h < n_heads;
+        const __nv_bfloat16* from = !row ? p.in[0] : h < p.heads[0] ? src[0] + h * p.si[0].head : src[1] + (h - p.heads[0]) * p.si[1].head;
+        const int s = i % (kAhead + 1);
+        copy16(ptx::smem_u32(&ring[s][0][tid]), reinterpret_cast<const uint4*>(from) + pa, row);
+        copy16(ptx::smem_u32(&ring[s][1][tid]), reinterpret_cast<const uint4*>(from) + pb, row);
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        if (i < n_rows) fetch(i);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // the first rows are on their way: now the angles of the CTA's tokens
+    const int half = p.rot >> 1;
+    for (int i = tid; i < kTok * half; i += kThreads) {
+        const int tq = i / half, f = i - tq * half;
+        if (n0 + tq < p.tokens) {
+            const double turns = (double)p.pos[n0 + tq] * (double)p.inv_freq[f] * 0.15915494309189535;   // 1 / (2 pi)
+            float s, c;
+            sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+            if (kInterleaved) {
+                t_cos[tq][2 * f] = t_cos[tq][2 * f + 1] = c;
+                t_sin[tq][2 * f] = -s;
+                t_sin[tq][2 * f + 1] = s;
+            } else {
+                t_cos[tq][f] = c;
+                t_sin[tq][f] = s;
+            }
         }
-        const __nv_bfloat16* src = p.in[op] + b * p.si[op].seq + t * p.si[op].token;
-        __nv_bfloat16* dst = p.out[op] + b * p.so[op].seq + t * p.so[op].token;
-#pragma unroll 2
-        for (int h0 = 0; h0 < p.heads[op]; h0 += kHeadStep) {      // (the same trip count for the whole warp)
-            const int h = h0 + grp / kTok;
-            const bool row = on && h < p.heads[op];
-            uint4 ra = make_uint4(0, 0, 0, 0), rb = ra;
-            if (row) {
-                const uint4* from = reinterpret_cast<const uint4*>(src + h * p.si[op].head);
-                ra = from[pa];
-                rb = from[pb];
-            }
-            float a[8], c[8];
-            widen(ra, a);
-            widen(rb, c);
-            if (norm) {
-                float ss = 0.0f;
+    }
+    for (int i = tid; i < 2 * D; i += kThreads) {
+        const __nv_bfloat16* w = p.w[i / D];
+        if (w) wt[i / D][i % D] = __bfloat162float(w[i % D]);
+    }
+    __syncthreads();
+    const bool on = exists && p.pos[n] >= 0;         // a negative position: the token sits out
+    // the lane's multipliers, the same for all its rows (side by side: of piece a, then of piece b)
+    f32x2 cs[kInterleaved ? 8 : 4], sn[kInterleaved ? 8 : 4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ss = fmaf(a[i], a[i], fmaf(c[i], c[i], ss));
+    for (int i = 0; i < (kInterleaved ? 2 : 1); ++i) {
+        f32x2 v[4];
+        load4(&t_cos[tk][8 * (i ? pb : pa)], v);
 #pragma unroll
-                for (int off = 1; off < kLanes; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-                const float r = 1.0f / sqrtf(ss * (1.0f / D) + p.eps);
+        for (int e = 0; e < 4; ++e) cs[4 * i + e] = v[e];
+        load4(&t_sin[tk][8 * (i ? pb : pa)], v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    a[i] = a[i] * r * wa[i];
-                    c[i] = c[i] * r * wb[i];
+        for (int e = 0; e < 4; ++e) sn[4 * i + e] = v[e];
+    }
+#pragma unroll 1
+    for (int i = 0; i < n_rows; ++i) {
+        if (i + kAhead < n_rows) fetch(i + kAhead);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+        const int h = i * kHeadStep + grp / kTok;
+        const bool key = h >= p.heads[0];
+        f32x2 a[4], c[4];
+        widen(ring[i % (kAhead + 1)][0][tid], a);
+        widen(ring[i % (kAhead + 1)][1][tid], c);
+        f32x2 s2 = mul2(a[0], a[0]);
+#pragma unroll
+        for (int e = 1; e < 4; ++e) s2 = fma2(a[e], a[e], s2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s2 = fma2(c[e], c[e], s2);
+        const float2 s1 = unpack2(s2);
+        float ss = s1.x + s1.y;
+#pragma unroll
+        for (int off = 1; off < kLanes; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+        if (key ? p.w[1] != nullptr : p.w[0] != nullptr) {
+            const float r = 1.0f / sqrtf(ss * (1.0f / D) + p.eps);
+            const f32x2 r2 = pack2(r, r);
+            f32x2 w[4];
+            load4(&wt[key][8 * pa], w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[e] = mul2(mul2(a[e], r2), w[e]);
+            load4(&wt[key][8 * pb], w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[e] = mul2(mul2(c[e], r2), w[e]);
+        }
+        if (rotates) {
+            if (kInterleaved) {                      // partner = the other element of the pair
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    a[e] = fma2(a[e], cs[e], mul2(swap2(a[e]), sn[e]));
+                    c[e] = fma2(c[e], cs[kInterleaved ? 4 + e : e], mul2(swap2(c[e]), sn[kInterleaved ? 4 + e : e]));
+                }
+            } else {                                 // partner = the same element of the other piece
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x2 u = a[e], v = c[e];
+                    a[e] = fma2(u, cs[e], mul2(v, neg2(sn[e])));
+                    c[e] = fma2(v, cs[e], mul2(u, sn[e]));
                 }
             }
-            if (rotates) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (kInterleaved) {
-                        float* x = i < 4 ? a + 2 * i : c + 2 * (i - 4);
-                        const float u = x[0], v = x[1];
-                        x[0] = fmaf(u, cs[i], -v * sn[i]);
-                        x[1] = fmaf(v, cs[i], u * sn[i]);
-                    } else {
-                        const float u = a[i], v = c[i];
-                        a[i] = fmaf(u, cs[i], -v * sn[i]);
-                        c[i] = fmaf(v, cs[i], u * sn[i]);
-                    }
-                }
-            }
-            if (row) {
-                uint4* to = reinterpret_cast<uint4*>(dst + h * p.so[op].head);
-                to[pa] = narrow(a);
-                to[pb] = narrow(c);
-            }
+        }
+        if (on && h < n_heads) {
+            uint4* to = reinterpret_cast<uint4*>(key ? dst[1] + (h - p.heads[0]) * p.so[1].head : dst[0] + h * p.so[0].head);
+            to[pa] = narrow(a);
+            to[pb] = narrow(c);
         }
     }
 }
@@ -159,9 +228,9 @@ cudaError_t launch(const RopeParams& p, cudaStream_t s) {
     // Eight tokens per CTA share the angles' work and write 8 rows of a head side by side; with few tokens one per
     // CTA spreads the heads over more of the GPU.
     if (p.tokens >= 8 * 148 * 4)
-        qk_norm_rope_kernel<D, kInterleaved, 8><<<(unsigned)((p.tokens + 7) / 8), kThreads, 0, s>>>(p);
+        qk_norm_rope_kernel<D, kInterleaved, 8><<<(p.tokens + 7) / 8, kThreads, 0, s>>>(p);
     else
-        qk_norm_rope_kernel<D, kInterleaved, 1><<<(unsigned)p.tokens, kThreads, 0, s>>>(p);
+        qk_norm_rope_kernel<D, kInterleaved, 1><<<p.tokens, kThreads, 0, s>>>(p);
     return cudaGetLastError();
 }
 
@@ -199,7 +268,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_qk_norm_rope(
     p.heads[0] = shape->Hq; p.heads[1] = shape->Hkv;
     p.pos = positions;
     p.inv_freq = inv_freq;
-    p.tokens = (int64_t)B * T;
+    p.tokens = (uint32_t)B * (uint32_t)T;
     p.T = T; p.rot = rotary_dim;
     p.eps = eps;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
