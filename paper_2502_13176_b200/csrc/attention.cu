@@ -219,7 +219,8 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Block& blk, Sh
         const int t = blk.row0 + row;
         float ref = kMode == kExact ? sm.ref[row] : 0.0f;      // log2 domain
         float m_run = -INFINITY;
-        float l4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        f32x2 sum[2] = {0ull, 0ull};                           // the row's sum (this thread's keys), four accumulators
+        const f32x2 scale2 = pack2(p.scale_log2, p.scale_log2);
         bool ok = true;
         for (int it = 0; it < n_it; ++it) {
             if (!group_wait(it)) { ok = false; break; }        // S(it) is ready
@@ -273,12 +274,12 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Block& blk, Sh
                     for (int c = 0; c < 32; ++c) m_run = fmaxf(m_run, __uint_as_float(v[c]));
                 } else {
                     uint32_t w[16];
+                    const f32x2 minus = pack2(-ref, -ref);
 #pragma unroll
                     for (int c = 0; c < 16; ++c) {
-                        const float p0 = fast_exp2(fmaf(__uint_as_float(v[2 * c]), p.scale_log2, -ref));
-                        const float p1 = fast_exp2(fmaf(__uint_as_float(v[2 * c + 1]), p.scale_log2, -ref));
-                        l4[2 * (c & 1)] += p0;
-                        l4[2 * (c & 1) + 1] += p1;
+                        const float2 x = unpack2(fma2(pack2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1])), scale2, minus));
+                        const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
+                        sum[c & 1] = add2(sum[c & 1], pack2(p0, p1));
                         w[c] = pack_bf16(p0, p1);
                     }
                     tc::tmem_st_32x32_x16(lane_addr + col_base + hh * 32, w);
@@ -292,7 +293,8 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Block& blk, Sh
         if (ok) ok = group_wait(n_it);                        // the last group: O is complete
         if (!ok) sm.abort = 1;
         // the two threads of a row join their halves through shared memory, the second's first
-        const float mine = kMode == kRowMax ? m_run : (l4[0] + l4[1]) + (l4[2] + l4[3]);
+        const float2 total = unpack2(add2(sum[0], sum[1]));
+        const float mine = kMode == kRowMax ? m_run : total.x + total.y;
         if (part == 1) sm.part[row] = mine;
         softmax_barrier();
         if (kMode == kRowMax) {

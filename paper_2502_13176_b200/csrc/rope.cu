@@ -20,6 +20,8 @@
 
 namespace {
 
+using namespace ptx;
+
 constexpr int kThreads = 256;
 constexpr int kAhead = 3;            // rows a thread has asked for while it works on one
 
@@ -39,28 +41,6 @@ struct RopeParams {
 // 16 bytes into shared memory without waiting for them; zeros (and no read) where `on` is false
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
-}
-// pairs of fp32 values in one 64-bit register: one instruction for both
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pack2(float lo, float hi) {
-    f32x2 v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
-    return v;
-}
-__device__ __forceinline__ float2 unpack2(f32x2 v) {
-    float2 f;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
-    return f;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-    f32x2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-    f32x2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
 }
 __device__ __forceinline__ f32x2 neg2(f32x2 v) { return v ^ 0x8000000080000000ull; }
 __device__ __forceinline__ f32x2 swap2(f32x2 v) {
@@ -125,8 +105,8 @@ __global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_kernel(const RopePar
         const bool row = exists && h < n_heads;
         const __nv_bfloat16* from = !row ? p.in[0] : h < p.heads[0] ? src[0] + h * p.si[0].head : src[1] + (h - p.heads[0]) * p.si[1].head;
         const int s = i % (kAhead + 1);
-        copy16(ptx::smem_u32(&ring[s][0][tid]), reinterpret_cast<const uint4*>(from) + pa, row);
-        copy16(ptx::smem_u32(&ring[s][1][tid]), reinterpret_cast<const uint4*>(from) + pb, row);
+        copy16(smem_u32(&ring[s][0][tid]), reinterpret_cast<const uint4*>(from) + pa, row);
+        copy16(smem_u32(&ring[s][1][tid]), reinterpret_cast<const uint4*>(from) + pb, row);
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
