@@ -9,16 +9,23 @@
 // next P V), and keep the row's sum in fp32.  Inside a CTA these steps follow one another; the SM's second CTA, at
 // another point of its own chain, uses the tensor pipe and the special-function unit meanwhile.
 //
+// A CTA goes on to further row blocks without starting anew (barriers, tensor memory, the first tiles' latency): it
+// asks the hardware for a block of the grid that has not been launched yet (clusterlaunchcontrol.try_cancel), so that
+// blocks of very unequal lengths balance themselves, and the producer and the MMA thread are already at the next block's
+// first tile while the softmax warps write this one's rows.
+//
 // The softmax needs a stabiliser per row, not the row's maximum: the largest logit among the row's first eight
 // keys serves (every row sees key 0).  p = exp2(s - reference) may then exceed 1, which bf16 and the fp32
 // accumulators hold up to 2^127: no running maximum, no exchange between the threads of a row, no rescaling of O.
 // A row whose sum or output leaves the fp32 range that way (or is not finite for any other reason) shows in the
-// epilogue, and the CTA then does its row block again: once for the rows' true maxima, once with them as reference.
+// epilogue; the CTA notes the row block and does it again at its end: once for the rows' true maxima, once with them
+// as reference.
 //
 // Nothing a row must not see may reach it.  Keys above the query are masked in S.  Their value rows meet
 // probabilities of zero, which is not enough when they hold infinities or NaN (0 * inf): value rows past the prompt's
 // end are cleared in shared memory before the product, and in the repeated form non-finite values of the diagonal
 // tile are taken out too and added afterwards to the rows that do see them.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstdint>
@@ -32,21 +39,19 @@ namespace {
 using namespace ptx;
 
 constexpr int kTileRows = 128;        // query rows per CTA = keys per streamed tile
+constexpr int kBoxBytes = kTileRows * 128;   // one TMA box: 128 rows x 64 elements
 constexpr int kSoftmaxWarps = 8;
-constexpr int kSoftmaxThreads = kSoftmaxWarps * 32;
 constexpr int kThreads = (2 + kSoftmaxWarps) * 32;
 constexpr int kGroupRing = 4;         // mbarriers that track the MMA groups in flight
+constexpr int kItemRing = 4;          // row blocks the roles of a CTA may be apart, and more
+constexpr int kMaxRedo = 32;          // row blocks a CTA can note; it asks for no further ones when they run short
 constexpr uint32_t kTmemColumns = 256;
+constexpr uint32_t kOColumn = kTileRows;     // O sits after S in tensor memory
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFinite = 3.0e38f;
 constexpr float kMaxSum = 0x1p120f;   // a row sum above this is redone: its reciprocal would be subnormal
-constexpr long long kGraceCycles = 2000000;   // about a millisecond, see the end of a pass
-
-// the three forms of a pass over a row block
-constexpr int kFast = 0;     // reference = largest logit of the first eight keys
-constexpr int kRowMax = 1;   // the rows' largest logits only
-constexpr int kExact = 2;    // reference = the row's largest logit; non-finite values of the diagonal tile apart
+constexpr long long kGraceCycles = 2000000;   // about a millisecond, see let_copies_land
 
 struct AttnParams {
     const int32_t* prompt_len;     // [B] or null (padded batches)
@@ -59,24 +64,31 @@ struct AttnParams {
     int64_t lse_seq, lse_head;
     uint32_t* status;
     int64_t total;
-    int32_t T, Hq, Hkv, n_blk;
+    int32_t B, T, Hq, Hkv, n_blk;
     float scale_log2;
 };
 
-// The row block a CTA works on.
+// A row block: what a CTA works on.  The grid counts row blocks in one dimension, prompt by prompt, head by head, the long
+// blocks of the causal triangle first; prompts take as many numbers as they have blocks, so that the numbers without
+// a block are the last ones.
 struct Block {
-    int row0;          // first row of the block inside the prompt
+    int row0;          // first row of the block inside the prompt; negative: no more blocks
     int len;           // tokens of the prompt
     int base;          // the prompt's first row along the token axis of the tensors (packed), else 0
-    int seq, h, kvh;   // index along the sequence axis (0 when packed), heads
+    int seq, h;        // index along the sequence axis (0 when packed), query head
 };
 
 struct Shared {
+    uint4 answer;                  // the hardware's answer to a request for a further block
     uint64_t bar_q, bar_k0, bar_v, bar_pa[kGroupRing], bar_pb[kGroupRing], bar_group[kGroupRing];
+    uint64_t bar_item[kItemRing], bar_answer, bar_ref[4], bar_sum[4];
+    Block item[kItemRing];         // row blocks handed from the producer to the other warps
+    Block redo[kMaxRedo];
+    int redo_count, redo_mark[kItemRing];
     uint32_t tmem_slot;
-    int abort, redo, bad_values;
+    int abort, bad_values;
     float ref[kTileRows];          // the rows' references for the exact form, log2 domain
-    float part[kTileRows];         // exchange between the two threads of a row
+    float part[2][kTileRows];      // exchange between the two threads of a row
 };
 
 __device__ __forceinline__ float fast_exp2(float x) {
@@ -88,7 +100,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ void softmax_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 // bf16 pair with its infinities and NaNs replaced by zero; `any` is set if there were any
 __device__ __forceinline__ uint32_t finite_pair(uint32_t w, bool& any) {
     if ((w & 0x7f80u) == 0x7f80u) { w &= 0xffff0000u; any = true; }
@@ -96,137 +107,322 @@ __device__ __forceinline__ uint32_t finite_pair(uint32_t w, bool& any) {
     return w;
 }
 
-// One pass over the key tiles of a row block.  `tiles` = Q, K and V tile in shared memory, tmem = 256 columns.
-template <int D, int kMode>
-__device__ __forceinline__ void attend(const AttnParams& p, const Block& blk, Shared& sm, const uint32_t tiles,
-                                       uint8_t* const tiles_ptr, const uint32_t tmem, const CUtensorMap& q_map,
-                                       const CUtensorMap& k_map, const CUtensorMap& v_map) {
-    constexpr int kKSteps = D / 16;                          // MMA steps over the head dimension (S = Q K^T)
-    constexpr int kPvSteps = kTileRows / 16;                 // MMA steps over the keys (O += P V)
-    constexpr int kBoxBytes = kTileRows * 128;               // one TMA box: 128 rows x 64 elements
-    constexpr int kTileBytes = kTileRows * D * 2;
-    constexpr uint32_t kOColumn = kTileRows;                 // O sits after S in tensor memory
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int qb = blk.row0 / kTileRows;
-    const int n_it = qb + 1;                                 // key tiles 0 .. qb
-    const uint32_t q_tile = tiles, k_tile = tiles + kTileBytes, v_tile = tiles + 2 * kTileBytes;
-    // value rows of the diagonal tile are looked through by the softmax warps before they are used
-    const bool clean = kMode == kExact || (kMode == kFast && blk.row0 + kTileRows > blk.len);
-
-    if (tid == 0) {
-        mbar_init(smem_u32(&sm.bar_q), 1);
-        mbar_init(smem_u32(&sm.bar_k0), 1);
-        mbar_init(smem_u32(&sm.bar_v), 1);
-        for (int s = 0; s < kGroupRing; ++s) {
-            mbar_init(smem_u32(&sm.bar_pa[s]), kSoftmaxWarps + 1);   // first half of P(it) written, V(it) landed
-            mbar_init(smem_u32(&sm.bar_pb[s]), kSoftmaxWarps + 1);   // second half of P(it) written, K(it + 1) landed
-            mbar_init(smem_u32(&sm.bar_group[s]), 1);
-        }
-        sm.bad_values = 0;
-        fence_mbar_init();
-    }
-    tc::fence_before_sync();
-    __syncthreads();
-    tc::fence_after_sync();
-    // completion of MMA group g: group 0 = S(0), group it + 1 = { O += P(it) V(it), S(it + 1) }
-    auto group_wait = [&](int g) { return mbar_wait(smem_u32(&sm.bar_group[g % kGroupRing]), (g / kGroupRing) & 1); };
-
-    if (warp == 0) {
-        // ---------------- TMA producer
-        if (lane == 0) {
-            auto load = [&](const CUtensorMap* map, uint32_t bar, uint32_t dst, int row0, int head) {
-                mbar_arrive_expect_tx(bar, kTileBytes);
+// ---------------------------------------------------------------- which block
+// Asks for a block of the grid that has not been launched; the answer (16 bytes) arrives on `bar`.  One thread.
+__device__ __forceinline__ void request_block(uint32_t answer, uint32_t bar) {
+    tc::fence_proxy_async_smem();                            // the answer before this one has been read
+    mbar_arrive_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+                 ::"r"(answer), "r"(bar) : "memory");
+}
+// true: block number `x` is this CTA's now; false: there is none left (and no more may be asked for)
+__device__ __forceinline__ bool granted_block(uint32_t answer, uint32_t& x) {
+    uint32_t got;
+    asm volatile(
+        "{\n\t.reg .b128 r;\n\t.reg .b64 lo, hi;\n\t.reg .pred p;\n\t"
+        "ld.shared.v2.b64 {lo, hi}, [%2];\n\t"
+        "mov.b128 r, {lo, hi};\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t"
+        "mov.u32 %1, 0;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t}"
+        : "=r"(got), "=r"(x) : "r"(answer) : "memory");
+    return got != 0;
+}
+// Where a search for a block number stands: the prompts before b0 have `before` blocks, and their bounds reach `reached`.
+struct Cursor {
+    int b0;
+    uint32_t before;
+    int reached;
+};
+// Row block number x; false if there is no such block (then there is none behind it either).  A whole warp: 32 prompts'
+// lengths at a time.  Prompts whose bounds cannot be are reported and have no blocks.
+__device__ __forceinline__ bool locate(const AttnParams& p, uint32_t x, Cursor& c, Block& blk, const int lane) {
+    blk.seq = 0;
+    blk.base = 0;
+    uint32_t in, n_blk;                                      // number inside the prompt, the prompt's row blocks
+    if (!p.cu_seqlens && !p.prompt_len) {
+        const uint32_t per = (uint32_t)p.n_blk * p.Hq;
+        blk.seq = x / per;
+        blk.len = p.T;
+        in = x - blk.seq * per;
+        n_blk = p.n_blk;
+        if (blk.seq >= p.B) return false;
+    } else {
+        if (x < c.before) c = Cursor{0, 0u, 0};
+        for (;; c.b0 += 32) {
+            if (c.b0 >= p.B) return false;
+            const int b = c.b0 + lane;
+            int first = 0, len = 0, top = c.reached;
+            if (b < p.B) {
+                if (p.cu_seqlens) {
+                    first = p.cu_seqlens[b];
+                    const int last = p.cu_seqlens[b + 1];
+                    len = last - first;
+                    top = max(first, last);
+                } else {
+                    len = min(max(p.prompt_len[b], 0), p.T);
+                }
+            }
+            if (p.cu_seqlens) {
+                // prompts start at or behind everything before them: they never overlap, so that the grid has room for all
 #pragma unroll
-                for (int bx = 0; bx < D / 64; ++bx) tma_load_4d(dst + bx * kBoxBytes, map, bx * 64, blk.base + row0, head, blk.seq, bar);
-            };
-            load(&q_map, smem_u32(&sm.bar_q), q_tile, blk.row0, blk.h);
-            load(&k_map, smem_u32(&sm.bar_k0), k_tile, 0, blk.kvh);
-            // bar_pa[it] collects the eight softmax warps and the load V(it), bar_pb[it] the same warps and K(it + 1):
-            // K(j + 1) takes the place of K(j) once S(j) is complete, V(j) that of V(j - 1) once P V of tile
-            // j - 1 is, and both are in MMA group j.
-            bool ok = true;
-            for (int j = 0; j < n_it && ok; ++j) {
-                if (j >= 1) ok = group_wait(j);
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, top, o);
+                    if (lane >= o) top = max(top, y);
+                }
+                int low = __shfl_up_sync(0xffffffffu, top, 1);
+                if (lane == 0) low = c.reached;
+                if (b < p.B && (first < low || len < 0 || first + (int64_t)len > p.total || len > p.T)) {
+                    atomicOr(p.status, BAKLAVA_STATUS_BAD_STATE);
+                    len = 0;
+                }
+            }
+            const uint32_t blocks = ((uint32_t)len + kTileRows - 1) / kTileRows;
+            uint32_t upto = blocks * p.Hq;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += y;
+            }
+            const uint32_t here = __ballot_sync(0xffffffffu, c.before + upto > x);
+            if (here) {
+                const int src = __ffs(here) - 1;
+                n_blk = __shfl_sync(0xffffffffu, blocks, src);
+                in = x - c.before - (__shfl_sync(0xffffffffu, upto, src) - n_blk * p.Hq);
+                blk.len = __shfl_sync(0xffffffffu, len, src);
+                if (p.cu_seqlens) blk.base = __shfl_sync(0xffffffffu, first, src);
+                else blk.seq = c.b0 + src;
+                break;
+            }
+            c.before += __shfl_sync(0xffffffffu, upto, 31);
+            c.reached = __shfl_sync(0xffffffffu, top, 31);
+        }
+    }
+    blk.h = in / n_blk;
+    blk.row0 = (int)(n_blk - 1 - (in - blk.h * n_blk)) * kTileRows;
+    return true;
+}
+
+// ---------------------------------------------------------------- the steps on a tile
+// 32 keys of this thread's 64: probabilities in bf16 over the first columns of the 32 logits they came from; `sum` += the
+// probabilities before their rounding.
+__device__ __forceinline__ void softmax_half(uint32_t column, bool diagonal, int first_key, int row, f32x2 scale2, float ref,
+                                             f32x2 (&sum)[2]) {
+    uint32_t v[32], w[16];
+    tc::tmem_ld_32x32(column, v);
+    tc::tmem_ld_wait();
+    if (diagonal) {                                           // keys above the query do not exist
+#pragma unroll
+        for (int c = 0; c < 32; ++c)
+            if (first_key + c > row) v[c] = 0xff800000u;
+    }
+    const f32x2 minus = pack2(-ref, -ref);
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+        const float2 x = unpack2(fma2(pack2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1])), scale2, minus));
+        const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
+        sum[c & 1] = add2(sum[c & 1], pack2(p0, p1));
+        w[c] = pack_bf16(p0, p1);
+    }
+    tc::tmem_st_32x32_x16(column, w);
+    tc::tmem_st_wait();
+}
+// This thread's share (part 0 or 1) of row `row` of a value tile: zeros where the row is no token of the prompt; with
+// kFiniteOnly infinities and NaNs become zeros too.  Returns whether there were any.
+template <int D, bool kFiniteOnly>
+__device__ __forceinline__ bool clean_value_row(uint8_t* tile, int row, int part, bool token) {
+    uint8_t* const v_row = tile + row * 128 + (D == 128 ? part * kBoxBytes : 0);
+    bool any = false;
+#pragma unroll 1
+    for (int c = 0; c < D / 16; ++c) {
+        const int piece = D == 128 ? c : part * 4 + c;
+        uint4* const at = reinterpret_cast<uint4*>(v_row + ((piece ^ (row & 7)) << 4));
+        if (!token) {
+            *at = make_uint4(0, 0, 0, 0);
+        } else if (kFiniteOnly) {
+            uint4 w = *at;
+            bool here = false;
+            w.x = finite_pair(w.x, here); w.y = finite_pair(w.y, here);
+            w.z = finite_pair(w.z, here); w.w = finite_pair(w.w, here);
+            if (here) { *at = w; any = true; }
+        }
+    }
+    tc::fence_proxy_async_smem();                             // the MMA reads what was written here
+    return any;
+}
+// S[128 q x 128 keys] = Q K^T
+template <int D>
+__device__ __forceinline__ void issue_s(uint32_t tmem, uint64_t dq, uint64_t dk) {
+    constexpr uint32_t idesc = tc::idesc_bf16_f32(kTileRows, kTileRows);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        const uint32_t off = ((ks >> 2) * kBoxBytes + (ks & 3) * 32) >> 4;
+        tc::umma_bf16(tmem, dq + off, dk + off, idesc, ks > 0);
+    }
+}
+// half hh of O[128 q x D] += P V: 16 keys per step = 8 columns of probabilities; a softmax thread's halves are keys 0..31
+// and 32..63 of its 64
+template <int D>
+__device__ __forceinline__ void issue_pv(uint32_t tmem, uint64_t dv, int hh, bool accumulate) {
+    constexpr uint32_t idesc = tc::idesc_bf16_f32_b_mn(kTileRows, D);
+#pragma unroll
+    for (int k4 = 0; k4 < kTileRows / 32; ++k4) {
+        const int ks = (k4 >> 1) * 4 + hh * 2 + (k4 & 1);
+        tc::umma_bf16_ts(tmem + kOColumn, tmem + (ks >> 2) * 64 + hh * 32 + (ks & 1) * 8, dv + (ks * 2048 >> 4), idesc,
+                         accumulate || hh > 0 || k4 > 0);
+    }
+}
+// A wait gave up long after the last copy was requested.  The copies share their barriers with the warps that have left,
+// so what may still be in flight is given time to land, not waited for by count.
+__device__ __forceinline__ void let_copies_land() {
+    const long long t0 = clock64();
+    while (clock64() - t0 < kGraceCycles) { }
+}
+__device__ __forceinline__ __nv_bfloat16* out_row(const AttnParams& p, const Block& blk, int t) {
+    return p.out + blk.seq * p.so.seq + (int64_t)(blk.base + t) * p.so.token + blk.h * p.so.head;
+}
+
+// What a role needs to know of the CTA.
+struct Cta {
+    uint32_t q_tile, k_tile, v_tile, tmem;
+    uint8_t* v_ptr;
+    int kv_group;                 // query heads per KV head
+};
+
+// ---------------------------------------------------------------- the stream of row blocks
+// All counters run on over the blocks: `tile0` tiles and `group0` MMA groups have gone before the block at hand (a block
+// of n tiles has n + 1 groups: S(0), then { P V(it), S(it + 1) } for it = 0 .. n - 1).
+template <int D>
+__device__ __forceinline__ void produce(const AttnParams& p, Shared& sm, const Cta& cta, Block blk, Cursor cursor,
+                                        const CUtensorMap& q_map, const CUtensorMap& k_map, const CUtensorMap& v_map,
+                                        const int lane) {
+    constexpr int kTileBytes = kTileRows * D * 2;
+    auto load = [&](const CUtensorMap* map, uint32_t bar, uint32_t dst, int row0, int head) {
+        mbar_arrive_expect_tx(bar, kTileBytes);
+#pragma unroll
+        for (int bx = 0; bx < D / 64; ++bx) tma_load_4d(dst + bx * kBoxBytes, map, bx * 64, blk.base + row0, head, blk.seq, bar);
+    };
+    auto group_wait = [&](int g) { return mbar_wait(smem_u32(&sm.bar_group[g % kGroupRing]), (g / kGroupRing) & 1); };
+    const uint32_t answer = smem_u32(&sm.answer), bar_answer = smem_u32(&sm.bar_answer);
+    int tile0 = 0, group0 = 0;
+    bool more = true;
+    for (int k = 0;; ++k) {
+        const int n_it = blk.row0 / kTileRows + 1;
+        bool ok = true, asked = false, got = false;
+        uint32_t x = 0;
+        if (lane == 0) {
+            // a block in the list of those to redo may come from this block, the one before it and the one after
+            asked = more && *(volatile int*)&sm.redo_count + 4 <= kMaxRedo;
+            if (asked) request_block(answer, bar_answer);
+            const int kvh = blk.h / cta.kv_group;
+            const bool clean = blk.row0 + kTileRows > blk.len;   // the last tile holds value rows that are no tokens
+            // Q and K are free: S of the block before has been formed (its last S was waited for below)
+            load(&q_map, smem_u32(&sm.bar_q), cta.q_tile, blk.row0, blk.h);
+            load(&k_map, smem_u32(&sm.bar_k0), cta.k_tile, 0, kvh);
+            // bar_pa collects the eight softmax warps and the load V(it), bar_pb the same warps and K(it + 1): K(j + 1)
+            // takes the place of K(j) once S(j) is complete, V(j) that of the tile before it once P V of that tile is.
+            for (int j = 0; j < n_it; ++j) {
+                if (group0 + j >= 1) ok = group_wait(group0 + j - (j == 0));
                 if (!ok) break;
-                const uint32_t pa = smem_u32(&sm.bar_pa[j % kGroupRing]);
-                if (kMode == kRowMax) {
-                    tc::mbar_arrive(pa);
-                } else if (clean && j == qb) {              // through the softmax warps, which arrive on bar_pa as ever
-                    load(&v_map, smem_u32(&sm.bar_v), v_tile, j * kTileRows, blk.kvh);
+                const uint32_t pa = smem_u32(&sm.bar_pa[(tile0 + j) % kGroupRing]);
+                if (clean && j == n_it - 1) {                // through the softmax warps, which arrive on bar_pa as ever
+                    load(&v_map, smem_u32(&sm.bar_v), cta.v_tile, j * kTileRows, kvh);
                     tc::mbar_arrive(pa);
                 } else {
-                    load(&v_map, pa, v_tile, j * kTileRows, blk.kvh);
+                    load(&v_map, pa, cta.v_tile, j * kTileRows, kvh);
                 }
-                if (j == 0) ok = group_wait(0);
+                if (j == 0) ok = group_wait(group0);
                 if (!ok) break;
-                const uint32_t pb = smem_u32(&sm.bar_pb[j % kGroupRing]);
-                if (j + 1 < n_it) load(&k_map, pb, k_tile, (j + 1) * kTileRows, blk.kvh);
+                const uint32_t pb = smem_u32(&sm.bar_pb[(tile0 + j) % kGroupRing]);
+                if (j + 1 < n_it) load(&k_map, pb, cta.k_tile, (j + 1) * kTileRows, kvh);
                 else tc::mbar_arrive(pb);
             }
+            if (ok && asked) {
+                ok = mbar_wait(bar_answer, k & 1);
+                if (ok) got = granted_block(answer, x);
+            }
             if (!ok) sm.abort = 1;
         }
-    } else if (warp == 1) {
-        // ---------------- MMA issuer
+        if (!__shfl_sync(0xffffffffu, ok, 0)) return;
+        tile0 += n_it;
+        group0 += n_it + 1;
+        // the next block, if there is one; once there is none nothing more is asked for
+        x = __shfl_sync(0xffffffffu, x, 0);
+        more = __shfl_sync(0xffffffffu, got, 0);
+        more = more && locate(p, x, cursor, blk, lane);
+        if (!more) blk.row0 = -1;
         if (lane == 0) {
-            constexpr uint32_t idesc_s = tc::idesc_bf16_f32(kTileRows, kTileRows);      // S[128 q x 128 keys]
-            constexpr uint32_t idesc_o = tc::idesc_bf16_f32_b_mn(kTileRows, D);         // O[128 q x D]
-            const uint64_t dq = tc::desc_k_major_sw128(q_tile), dk = tc::desc_k_major_sw128(k_tile);
-            const uint64_t dv = tc::desc_mn_major_sw128(v_tile, kBoxBytes);
-            auto issue_s = [&]() {
-#pragma unroll
-                for (int ks = 0; ks < kKSteps; ++ks) {
-                    const uint32_t off = ((ks >> 2) * kBoxBytes + (ks & 3) * 32) >> 4;
-                    tc::umma_bf16(tmem, dq + off, dk + off, idesc_s, ks > 0);
-                }
-            };
-            bool ok = mbar_wait(smem_u32(&sm.bar_q), 0);
-            if (ok) ok = mbar_wait(smem_u32(&sm.bar_k0), 0);
-            if (ok) {
-                tc::fence_after_sync();
-                issue_s();
-                tc::umma_commit(smem_u32(&sm.bar_group[0]));
-            }
-            for (int it = 0; it < n_it && ok; ++it) {
-                // 16 keys per step = 8 columns of probabilities; a thread's halves are keys 0..31 and 32..63 of its 64
-                auto issue_pv = [&](int hh) {
-#pragma unroll
-                    for (int k4 = 0; k4 < kPvSteps / 2; ++k4) {
-                        const int ks = (k4 >> 1) * 4 + hh * 2 + (k4 & 1);
-                        tc::umma_bf16_ts(tmem + kOColumn, tmem + (ks >> 2) * 64 + hh * 32 + (ks & 1) * 8,
-                                         dv + (ks * 2048 >> 4), idesc_o, (it > 0) || (hh > 0) || (k4 > 0));
-                    }
-                };
-                ok = mbar_wait(smem_u32(&sm.bar_pa[it % kGroupRing]), (it / kGroupRing) & 1);
-                if (!ok) break;
-                tc::fence_after_sync();
-                if (kMode != kRowMax) issue_pv(0);
-                ok = mbar_wait(smem_u32(&sm.bar_pb[it % kGroupRing]), (it / kGroupRing) & 1);
-                if (!ok) break;
-                tc::fence_after_sync();
-                if (kMode != kRowMax) issue_pv(1);
-                if (it + 1 < n_it) issue_s();
-                tc::umma_commit(smem_u32(&sm.bar_group[(it + 1) % kGroupRing]));
-            }
-            if (!ok) sm.abort = 1;
+            sm.item[k % kItemRing] = blk;
+            tc::mbar_arrive(smem_u32(&sm.bar_item[k % kItemRing]));
         }
-    } else {
-        // ---------------- softmax warps: a warp reads its quarter of the TMEM lanes (thread = query row); the
-        // first four of them take keys 0..63 of every tile, the others keys 64..127
-        const int row = 32 * (warp & 3) + lane;
-        const int part = (warp - 2) >> 2;
-        const int col_base = part * 64;
-        const uint32_t lane_addr = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-        const int t = blk.row0 + row;
-        float ref = kMode == kExact ? sm.ref[row] : 0.0f;      // log2 domain
-        float m_run = -INFINITY;
-        f32x2 sum[2] = {0ull, 0ull};                           // the row's sum (this thread's keys), four accumulators
-        const f32x2 scale2 = pack2(p.scale_log2, p.scale_log2);
-        bool ok = true;
-        for (int it = 0; it < n_it; ++it) {
-            if (!group_wait(it)) { ok = false; break; }        // S(it) is ready
+        if (!more) return;
+    }
+}
+
+// The block after block k of this CTA; false (and blk untouched) if the wait gave up.
+__device__ __forceinline__ bool next_block(Shared& sm, int k, Block& blk) {
+    const int s = k % kItemRing;
+    if (!mbar_wait(smem_u32(&sm.bar_item[s]), (k / kItemRing) & 1)) return false;
+    blk = sm.item[s];
+    return true;
+}
+
+template <int D>
+__device__ __forceinline__ void issue(Shared& sm, const Cta& cta, Block blk) {
+    const uint64_t dq = tc::desc_k_major_sw128(cta.q_tile), dk = tc::desc_k_major_sw128(cta.k_tile);
+    const uint64_t dv = tc::desc_mn_major_sw128(cta.v_tile, kBoxBytes);
+    int tile = 0, group = 0;
+    bool ok = true;
+    for (int k = 0; ok && blk.row0 >= 0; ++k) {
+        const int n_it = blk.row0 / kTileRows + 1;
+        ok = mbar_wait(smem_u32(&sm.bar_q), k & 1);
+        if (ok) ok = mbar_wait(smem_u32(&sm.bar_k0), k & 1);
+        if (!ok) break;
+        tc::fence_after_sync();
+        issue_s<D>(cta.tmem, dq, dk);                        // (the pipe runs in order: behind the last block's P V)
+        tc::umma_commit(smem_u32(&sm.bar_group[group++ % kGroupRing]));
+        for (int it = 0; it < n_it; ++it, ++tile) {
+            // the first half of P is written and V has landed (for it = 0: and the rows before it have been read from O)
+            ok = mbar_wait(smem_u32(&sm.bar_pa[tile % kGroupRing]), (tile / kGroupRing) & 1);
+            if (!ok) break;
             tc::fence_after_sync();
-            if (kMode == kFast && it == 0) {
-                // every thread of the row reads the same eight columns, so the two agree without talking
+            issue_pv<D>(cta.tmem, dv, 0, it > 0);
+            // the second half is written (so all of S has been read) and the next K has landed
+            ok = mbar_wait(smem_u32(&sm.bar_pb[tile % kGroupRing]), (tile / kGroupRing) & 1);
+            if (!ok) break;
+            tc::fence_after_sync();
+            issue_pv<D>(cta.tmem, dv, 1, true);
+            if (it + 1 < n_it) issue_s<D>(cta.tmem, dq, dk);
+            tc::umma_commit(smem_u32(&sm.bar_group[group++ % kGroupRing]));
+        }
+        if (ok) ok = next_block(sm, k, blk);
+    }
+    if (!ok) sm.abort = 1;
+}
+
+// Thread = (query row, half of the keys): a warp reads its quarter of the TMEM lanes; the first four softmax warps take
+// keys 0..63 of every tile, the others keys 64..127.
+template <int D>
+__device__ __forceinline__ void soften(const AttnParams& p, Shared& sm, const Cta& cta, Block blk, const int warp, const int lane) {
+    const int quarter = warp & 3, row = 32 * quarter + lane, part = (warp - 2) >> 2, col_base = part * 64;
+    const uint32_t lane_addr = cta.tmem + ((uint32_t)(32 * quarter) << 16);
+    const f32x2 scale2 = pack2(p.scale_log2, p.scale_log2);
+    auto group_wait = [&](int g) { return mbar_wait(smem_u32(&sm.bar_group[g % kGroupRing]), (g / kGroupRing) & 1); };
+    int tile = 0, group = 0, cleaned = 0;
+    bool ok = true;
+    for (int k = 0; ok && blk.row0 >= 0; ++k) {
+        const int qb = blk.row0 / kTileRows, t = blk.row0 + row;
+        const bool clean = blk.row0 + kTileRows > blk.len;
+        float ref = 0.0f;                                     // log2 domain
+        f32x2 sum[2] = {0ull, 0ull};                          // the row's sum (this thread's keys), four accumulators
+        for (int it = 0; it <= qb; ++it, ++tile) {
+            ok = group_wait(group++);                         // S(it) is ready
+            if (!ok) break;
+            tc::fence_after_sync();
+            if (it == 0) {
+                // every thread of the row reads the same eight columns, so the two agree without talking; part 0 puts
+                // its probabilities over them only when part 1 has read them
                 uint32_t first[8];
                 tc::tmem_ld_32x32_x8(lane_addr, first);
                 tc::tmem_ld_wait();
@@ -235,90 +431,200 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Block& blk, Sh
                 for (int c = 1; c < 8; ++c)
                     if (qb > 0 || c <= row) mx = fmaxf(mx, __uint_as_float(first[c]));
                 ref = mx * p.scale_log2;
-                softmax_barrier();                             // probabilities go over these columns only now
+                if (part == 1) {
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(smem_u32(&sm.bar_ref[quarter]));
+                } else {
+                    ok = mbar_wait(smem_u32(&sm.bar_ref[quarter]), k & 1);
+                    if (!ok) break;
+                }
             }
             if (clean && it == qb) {
-                if (!mbar_wait(smem_u32(&sm.bar_v), 0)) { ok = false; break; }
-                // this thread's share of value row `row` (the key at blk.row0 + row)
-                uint8_t* const v_row = tiles_ptr + 2 * kTileBytes + row * 128 + (D == 128 ? part * kBoxBytes : 0);
-                bool any = false;
-#pragma unroll 1
-                for (int c = 0; c < D / 16; ++c) {
-                    const int piece = D == 128 ? c : part * 4 + c;
-                    uint4* const at = reinterpret_cast<uint4*>(v_row + ((piece ^ (row & 7)) << 4));
-                    if (t >= blk.len) {
-                        *at = make_uint4(0, 0, 0, 0);
-                    } else if (kMode == kExact) {
-                        uint4 w = *at;
-                        bool here = false;
-                        w.x = finite_pair(w.x, here); w.y = finite_pair(w.y, here);
-                        w.z = finite_pair(w.z, here); w.w = finite_pair(w.w, here);
-                        if (here) { *at = w; any = true; }
-                    }
-                }
-                if (any) sm.bad_values = 1;
-                tc::fence_proxy_async_smem();                  // the MMA reads what was written here
+                ok = mbar_wait(smem_u32(&sm.bar_v), cleaned++ & 1);
+                if (!ok) break;
+                clean_value_row<D, false>(cta.v_ptr, row, part, t < blk.len);
             }
 #pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
-                uint32_t v[32];
-                tc::tmem_ld_32x32(lane_addr + col_base + hh * 32, v);
-                tc::tmem_ld_wait();
-                if (it == qb) {                               // diagonal tile: keys above the query do not exist
+                softmax_half(lane_addr + col_base + hh * 32, it == qb, col_base + hh * 32, row, scale2, ref, sum);
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(smem_u32(hh == 0 ? &sm.bar_pa[tile % kGroupRing] : &sm.bar_pb[tile % kGroupRing]));
+            }
+        }
+        if (!ok) break;
+        // the two threads of a row join their sums (each writes its own, both add them in the same order)
+        const float2 total = unpack2(add2(sum[0], sum[1]));
+        sm.part[part][row] = total.x + total.y;
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(smem_u32(&sm.bar_sum[quarter]));
+        ok = mbar_wait(smem_u32(&sm.bar_sum[quarter]), k & 1);
+        if (ok) ok = group_wait(group++);                     // the block's last group: O is complete
+        if (!ok) break;
+        const float l = sm.part[0][row] + sm.part[1][row], inv = 1.0f / l;
+        bool again = !(l <= kMaxSum);
+        tc::fence_after_sync();
+        __nv_bfloat16* const dst = out_row(p, blk, t) + part * (D / 2);
+#pragma unroll
+        for (int ch = 0; ch < D / 64; ++ch) {                 // 32 columns of the head dimension at a time
+            uint32_t o[32];
+            tc::tmem_ld_32x32(lane_addr + kOColumn + part * (D / 2) + ch * 32, o);
+            tc::tmem_ld_wait();
+            float worst = 0.0f;                               // NaN propagates through the sum, infinities too
+#pragma unroll
+            for (int c = 0; c < 32; ++c) worst = fmaf(fabsf(__uint_as_float(o[c])), 0x1p-20f, worst);
+            again = again || !(worst <= kFinite);
+            if (t < blk.len) {
+#pragma unroll
+                for (int c8 = 0; c8 < 4; ++c8) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        w[c] = pack_bf16(__uint_as_float(o[8 * c8 + 2 * c]) * inv, __uint_as_float(o[8 * c8 + 2 * c + 1]) * inv);
+                    *reinterpret_cast<uint4*>(dst + ch * 32 + 8 * c8) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+        }
+        tc::fence_before_sync();                              // (O may be written again behind this block's next arrival)
+        if (p.lse && part == 0 && t < blk.len)
+            p.lse[blk.seq * p.lse_seq + blk.h * p.lse_head + blk.base + t] = (ref + log2f(l)) * kLn2;
+        if (again && t < blk.len) {
+            // the first thread that finds such a row notes the block
+            const int s = k % kItemRing;
+            if (atomicExch(&sm.redo_mark[s], k + 1) != k + 1) sm.redo[atomicAdd(&sm.redo_count, 1)] = blk;
+        }
+        ok = next_block(sm, k, blk);
+    }
+    if (!ok) sm.abort = 1;
+}
+
+// ---------------------------------------------------------------- a row block done again
+// kExact = false: the rows' largest logits into sm.ref; kExact = true: with them as reference, the non-finite values of the
+// diagonal tile taken out and added to the rows that see them.  The whole CTA; the barriers are set up anew.
+template <int D, bool kExact>
+__device__ __noinline__ void redo_pass(const AttnParams& p, const Block blk, Shared& sm, const Cta cta, const CUtensorMap& q_map,
+                                       const CUtensorMap& k_map, const CUtensorMap& v_map) {
+    constexpr int kTileBytes = kTileRows * D * 2;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int qb = blk.row0 / kTileRows, n_it = qb + 1, kvh = blk.h / cta.kv_group;
+    __syncthreads();
+    if (tid == 0) {
+        mbar_init(smem_u32(&sm.bar_q), 1);
+        mbar_init(smem_u32(&sm.bar_k0), 1);
+        mbar_init(smem_u32(&sm.bar_v), 1);
+        for (int s = 0; s < kGroupRing; ++s) {
+            mbar_init(smem_u32(&sm.bar_pa[s]), kSoftmaxWarps + 1);
+            mbar_init(smem_u32(&sm.bar_pb[s]), kSoftmaxWarps + 1);
+            mbar_init(smem_u32(&sm.bar_group[s]), 1);
+        }
+        sm.bad_values = 0;
+        fence_mbar_init();
+    }
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    auto group_wait = [&](int g) { return mbar_wait(smem_u32(&sm.bar_group[g % kGroupRing]), (g / kGroupRing) & 1); };
+    bool ok = true;
+    if (warp == 0 && lane == 0) {
+        auto load = [&](const CUtensorMap* map, uint32_t bar, uint32_t dst, int row0, int head) {
+            mbar_arrive_expect_tx(bar, kTileBytes);
+#pragma unroll
+            for (int bx = 0; bx < D / 64; ++bx) tma_load_4d(dst + bx * kBoxBytes, map, bx * 64, blk.base + row0, head, blk.seq, bar);
+        };
+        load(&q_map, smem_u32(&sm.bar_q), cta.q_tile, blk.row0, blk.h);
+        load(&k_map, smem_u32(&sm.bar_k0), cta.k_tile, 0, kvh);
+        for (int j = 0; j < n_it && ok; ++j) {
+            if (j >= 1) ok = group_wait(j);
+            if (!ok) break;
+            const uint32_t pa = smem_u32(&sm.bar_pa[j % kGroupRing]), pb = smem_u32(&sm.bar_pb[j % kGroupRing]);
+            if (kExact && j < qb) load(&v_map, pa, cta.v_tile, j * kTileRows, kvh);
+            else tc::mbar_arrive(pa);
+            if (kExact && j == qb) load(&v_map, smem_u32(&sm.bar_v), cta.v_tile, j * kTileRows, kvh);
+            if (j == 0) ok = group_wait(0);
+            if (!ok) break;
+            if (j + 1 < n_it) load(&k_map, pb, cta.k_tile, (j + 1) * kTileRows, kvh);
+            else tc::mbar_arrive(pb);
+        }
+    } else if (warp == 1 && lane == 0) {
+        const uint64_t dq = tc::desc_k_major_sw128(cta.q_tile), dk = tc::desc_k_major_sw128(cta.k_tile);
+        const uint64_t dv = tc::desc_mn_major_sw128(cta.v_tile, kBoxBytes);
+        ok = mbar_wait(smem_u32(&sm.bar_q), 0);
+        if (ok) ok = mbar_wait(smem_u32(&sm.bar_k0), 0);
+        if (ok) {
+            tc::fence_after_sync();
+            issue_s<D>(cta.tmem, dq, dk);
+            tc::umma_commit(smem_u32(&sm.bar_group[0]));
+        }
+        for (int it = 0; it < n_it && ok; ++it) {
+            ok = mbar_wait(smem_u32(&sm.bar_pa[it % kGroupRing]), (it / kGroupRing) & 1);
+            if (!ok) break;
+            tc::fence_after_sync();
+            if (kExact) issue_pv<D>(cta.tmem, dv, 0, it > 0);
+            ok = mbar_wait(smem_u32(&sm.bar_pb[it % kGroupRing]), (it / kGroupRing) & 1);
+            if (!ok) break;
+            tc::fence_after_sync();
+            if (kExact) issue_pv<D>(cta.tmem, dv, 1, true);
+            if (it + 1 < n_it) issue_s<D>(cta.tmem, dq, dk);
+            tc::umma_commit(smem_u32(&sm.bar_group[(it + 1) % kGroupRing]));
+        }
+    } else if (warp >= 2) {
+        const int quarter = warp & 3, row = 32 * quarter + lane, part = (warp - 2) >> 2, col_base = part * 64;
+        const uint32_t lane_addr = cta.tmem + ((uint32_t)(32 * quarter) << 16);
+        const int t = blk.row0 + row;
+        const f32x2 scale2 = pack2(p.scale_log2, p.scale_log2);
+        const float ref = kExact ? sm.ref[row] : 0.0f;
+        float m_run = -INFINITY;
+        f32x2 sum[2] = {0ull, 0ull};
+        for (int it = 0; it < n_it; ++it) {
+            ok = group_wait(it);
+            if (!ok) break;
+            tc::fence_after_sync();
+            if (kExact && it == qb) {
+                ok = mbar_wait(smem_u32(&sm.bar_v), 0);
+                if (!ok) break;
+                if (clean_value_row<D, true>(cta.v_ptr, row, part, t < blk.len)) sm.bad_values = 1;
+            }
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                const int first_key = col_base + hh * 32;
+                if (kExact) {
+                    softmax_half(lane_addr + first_key, it == qb, first_key, row, scale2, ref, sum);
+                } else {
+                    uint32_t v[32];
+                    tc::tmem_ld_32x32(lane_addr + first_key, v);
+                    tc::tmem_ld_wait();
 #pragma unroll
                     for (int c = 0; c < 32; ++c)
-                        if (col_base + hh * 32 + c > row) v[c] = 0xff800000u;
-                }
-                if (kMode == kRowMax) {
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) m_run = fmaxf(m_run, __uint_as_float(v[c]));
-                } else {
-                    uint32_t w[16];
-                    const f32x2 minus = pack2(-ref, -ref);
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        const float2 x = unpack2(fma2(pack2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1])), scale2, minus));
-                        const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
-                        sum[c & 1] = add2(sum[c & 1], pack2(p0, p1));
-                        w[c] = pack_bf16(p0, p1);
-                    }
-                    tc::tmem_st_32x32_x16(lane_addr + col_base + hh * 32, w);
-                    tc::tmem_st_wait();
+                        if (it < qb || first_key + c <= row) m_run = fmaxf(m_run, __uint_as_float(v[c]));
                 }
                 tc::fence_before_sync();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(smem_u32(hh == 0 ? &sm.bar_pa[it % kGroupRing] : &sm.bar_pb[it % kGroupRing]));
             }
         }
-        if (ok) ok = group_wait(n_it);                        // the last group: O is complete
-        if (!ok) sm.abort = 1;
-        // the two threads of a row join their halves through shared memory, the second's first
+        if (ok) ok = group_wait(n_it);
         const float2 total = unpack2(add2(sum[0], sum[1]));
-        const float mine = kMode == kRowMax ? m_run : total.x + total.y;
-        if (part == 1) sm.part[row] = mine;
-        softmax_barrier();
-        if (kMode == kRowMax) {
-            if (part == 0) sm.ref[row] = fmaxf(mine, sm.part[row]) * p.scale_log2;
+        sm.part[part][row] = kExact ? total.x + total.y : m_run;
+    }
+    if (!ok) sm.abort = 1;
+    __syncthreads();                                          // sums / maxima, and whether values were taken out
+    if (warp >= 2 && !sm.abort) {
+        const int quarter = warp & 3, row = 32 * quarter + lane, part = (warp - 2) >> 2;
+        const int t = blk.row0 + row;
+        if (!kExact) {
+            if (part == 0) sm.ref[row] = fmaxf(sm.part[0][row], sm.part[1][row]) * p.scale_log2;
         } else {
-            if (part == 0) sm.part[row] += mine;
-            softmax_barrier();
-            const float l = sm.part[row];
-            if (ok && kMode == kFast && t < blk.len && !(l <= kMaxSum)) sm.redo = 1;
-            const float inv = 1.0f / l;
+            const float l = sm.part[0][row] + sm.part[1][row], inv = 1.0f / l;
             tc::fence_after_sync();
-            __nv_bfloat16* const dst = p.out + blk.seq * p.so.seq + (int64_t)(blk.base + t) * p.so.token + blk.h * p.so.head;
-            bool leave = false;
-#pragma unroll
-            for (int ch = 0; ch < D / 64; ++ch) {             // 32 columns of the head dimension at a time
-                const int col0 = part * (D / 2) + ch * 32;
+            __nv_bfloat16* const dst = out_row(p, blk, t) + part * (D / 2);
+            for (int ch = 0; ch < D / 64; ++ch) {
                 uint32_t o[32];
-                tc::tmem_ld_32x32(lane_addr + kOColumn + col0, o);
+                tc::tmem_ld_32x32(cta.tmem + ((uint32_t)(32 * quarter) << 16) + kOColumn + part * (D / 2) + ch * 32, o);
                 tc::tmem_ld_wait();
-                if (kMode == kExact && sm.bad_values) {
-                    // infinities and NaNs that were taken out of the diagonal tile, for the rows that see them
-                    for (int j = 0; j <= row && blk.row0 + j < blk.len; ++j) {
+                if (sm.bad_values && t < blk.len) {
+                    for (int j = 0; j <= row; ++j) {          // (rows up to this one are tokens)
                         const __nv_bfloat16* vj = p.v + blk.seq * p.sv.seq + (int64_t)(blk.base + blk.row0 + j) * p.sv.token +
-                                                  blk.kvh * p.sv.head + col0;
+                                                  kvh * p.sv.head + part * (D / 2) + ch * 32;
 #pragma unroll
                         for (int c = 0; c < 32; ++c) {
                             const float x = __bfloat162float(vj[c]);
@@ -326,38 +632,26 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Block& blk, Sh
                         }
                     }
                 }
-                if (kMode == kFast) {
-                    float worst = 0.0f;                        // NaN propagates through the sum, infinities too
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) worst += fabsf(__uint_as_float(o[c])) * 0x1p-20f;
-                    if (!(worst <= kFinite)) leave = true;
-                }
-                if (ok && t < blk.len) {
+                if (t < blk.len) {
 #pragma unroll
                     for (int c8 = 0; c8 < 4; ++c8) {
                         uint32_t w[4];
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
                             w[c] = pack_bf16(__uint_as_float(o[8 * c8 + 2 * c]) * inv, __uint_as_float(o[8 * c8 + 2 * c + 1]) * inv);
-                        *reinterpret_cast<uint4*>(dst + col0 + 8 * c8) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(dst + ch * 32 + 8 * c8) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 }
             }
-            if (leave && t < blk.len) sm.redo = 1;
-            if (p.lse && ok && part == 0 && t < blk.len)
-                p.lse[blk.seq * p.lse_seq + blk.h * p.lse_head + blk.base + t] = (ref + log2f(l)) * kLn2;
+            if (p.lse && part == 0 && t < blk.len)
+                p.lse[blk.seq * p.lse_seq + blk.h * p.lse_head + blk.base + t] = (sm.ref[row] + log2f(l)) * kLn2;
         }
     }
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
-    if (tid == 0) {                                           // the barriers may be set up again by the next pass
-        if (sm.abort) {
-            // a wait gave up long after the last copy was requested; the copies share their barriers with the warps
-            // that have left, so what may still be in flight is given time to land, not waited for by count
-            const long long t0 = clock64();
-            while (clock64() - t0 < kGraceCycles) { }
-        }
+    if (tid == 0) {
+        if (sm.abort) let_copies_land();
         mbar_inval(smem_u32(&sm.bar_q));
         mbar_inval(smem_u32(&sm.bar_k0));
         mbar_inval(smem_u32(&sm.bar_v));
@@ -370,43 +664,54 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Block& blk, Sh
     __syncthreads();
 }
 
-// Grid (row blocks, query heads, prompts), long blocks of the causal triangle first.
 template <int D>
 __global__ void __launch_bounds__(kThreads, 2) prompt_attn_kernel(const __grid_constant__ AttnParams p,
                                                                   const __grid_constant__ CUtensorMap q_map,
                                                                   const __grid_constant__ CUtensorMap k_map,
                                                                   const __grid_constant__ CUtensorMap v_map) {
     constexpr int kTileBytes = kTileRows * D * 2;
+    static_assert(kTileBytes % 1024 == 0, "operand tiles start on swizzle-pattern boundaries");
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(16) Shared sm;
-    const int tid = threadIdx.x, warp = tid >> 5;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     Block blk;
-    blk.row0 = (p.n_blk - 1 - (int)blockIdx.x) * kTileRows;
-    blk.h = blockIdx.y;
-    blk.kvh = blk.h / (p.Hq / p.Hkv);
-    const int b = blockIdx.z;
-    if (p.cu_seqlens) {
-        const int first = p.cu_seqlens[b], last = p.cu_seqlens[b + 1];
-        if (first < 0 || last < first || last > p.total || last - first > p.T) {
-            if (tid == 0 && blockIdx.x == 0 && blockIdx.y == 0) atomicOr(p.status, BAKLAVA_STATUS_BAD_STATE);
-            return;
-        }
-        blk.base = first;
-        blk.len = last - first;
-        blk.seq = 0;
-    } else {
-        blk.base = 0;
-        blk.len = p.prompt_len ? min(max(p.prompt_len[b], 0), p.T) : p.T;
-        blk.seq = b;
+    Cursor cursor = {0, 0u, 0};
+    if (warp == 0) {
+        if (!locate(p, blockIdx.x, cursor, blk, lane)) blk.row0 = -1;
+        if (lane == 0) sm.item[kItemRing - 1] = blk;          // (not used for a further block before this one is under way)
     }
-    if (blk.row0 >= blk.len) return;
+    Cta cta;
     const uint32_t tiles = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    uint8_t* const tiles_ptr = smem_raw + (tiles - smem_u32(smem_raw));
-    static_assert(kTileBytes % 1024 == 0, "operand tiles start on swizzle-pattern boundaries");
+    cta.q_tile = tiles;
+    cta.k_tile = tiles + kTileBytes;
+    cta.v_tile = tiles + 2 * kTileBytes;
+    cta.v_ptr = smem_raw + (tiles - smem_u32(smem_raw)) + 2 * kTileBytes;
+    cta.kv_group = p.Hq / p.Hkv;
     if (tid == 0) {
+        mbar_init(smem_u32(&sm.bar_q), 1);
+        mbar_init(smem_u32(&sm.bar_k0), 1);
+        mbar_init(smem_u32(&sm.bar_v), 1);
+        mbar_init(smem_u32(&sm.bar_answer), 1);
+        for (int s = 0; s < kGroupRing; ++s) {
+            mbar_init(smem_u32(&sm.bar_pa[s]), kSoftmaxWarps + 1);   // first half of P(it) written, V(it) landed
+            mbar_init(smem_u32(&sm.bar_pb[s]), kSoftmaxWarps + 1);   // second half of P(it) written, K(it + 1) landed
+            mbar_init(smem_u32(&sm.bar_group[s]), 1);
+        }
+        for (int s = 0; s < kItemRing; ++s) {
+            mbar_init(smem_u32(&sm.bar_item[s]), 1);
+            sm.redo_mark[s] = 0;
+        }
+        for (int s = 0; s < 4; ++s) {
+            mbar_init(smem_u32(&sm.bar_ref[s]), 1);
+            mbar_init(smem_u32(&sm.bar_sum[s]), 2);
+        }
         sm.abort = 0;
-        sm.redo = 0;
+        sm.redo_count = 0;
+        fence_mbar_init();
     }
+    __syncthreads();
+    blk = sm.item[kItemRing - 1];
+    if (blk.row0 < 0) return;
     if (warp == 1) {
         tc::tmem_alloc(smem_u32(&sm.tmem_slot), kTmemColumns);
         tc::tmem_relinquish();
@@ -414,19 +719,46 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attn_kernel(const __grid_c
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
-    const uint32_t tmem = sm.tmem_slot;
-    attend<D, kFast>(p, blk, sm, tiles, tiles_ptr, tmem, q_map, k_map, v_map);
-    if (sm.redo && !sm.abort) {
-        attend<D, kRowMax>(p, blk, sm, tiles, tiles_ptr, tmem, q_map, k_map, v_map);
-        if (!sm.abort) attend<D, kExact>(p, blk, sm, tiles, tiles_ptr, tmem, q_map, k_map, v_map);
+    cta.tmem = sm.tmem_slot;
+    if (warp == 0) {
+        produce<D>(p, sm, cta, blk, cursor, q_map, k_map, v_map, lane);
+    } else if (warp == 1) {
+        if (lane == 0) issue<D>(sm, cta, blk);
+    } else {
+        soften<D>(p, sm, cta, blk, warp, lane);
     }
-    if (warp == 1) tc::tmem_dealloc(tmem, kTmemColumns);
-    if (tid == 0 && sm.abort) atomicOr(p.status, BAKLAVA_STATUS_TIMEOUT);
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    if (sm.abort) {
+        if (tid == 0) {
+            atomicOr(p.status, BAKLAVA_STATUS_TIMEOUT);
+            let_copies_land();
+        }
+    } else if (sm.redo_count > 0) {
+        if (tid == 0) {
+            mbar_inval(smem_u32(&sm.bar_q));
+            mbar_inval(smem_u32(&sm.bar_k0));
+            mbar_inval(smem_u32(&sm.bar_v));
+            for (int s = 0; s < kGroupRing; ++s) {
+                mbar_inval(smem_u32(&sm.bar_pa[s]));
+                mbar_inval(smem_u32(&sm.bar_pb[s]));
+                mbar_inval(smem_u32(&sm.bar_group[s]));
+            }
+        }
+        for (int i = 0; i < sm.redo_count && !sm.abort; ++i) {
+            redo_pass<D, false>(p, sm.redo[i], sm, cta, q_map, k_map, v_map);
+            if (!sm.abort) redo_pass<D, true>(p, sm.redo[i], sm, cta, q_map, k_map, v_map);
+        }
+        if (sm.abort && tid == 0) atomicOr(p.status, BAKLAVA_STATUS_TIMEOUT);
+    }
+    __syncthreads();
+    if (warp == 1) tc::tmem_dealloc(cta.tmem, kTmemColumns);
 }
 
 template <int D>
-cudaError_t launch(const AttnParams& p, const CUtensorMap& qm, const CUtensorMap& km, const CUtensorMap& vm, int B,
-                   cudaStream_t s) {
+cudaError_t launch(const AttnParams& p, const CUtensorMap& qm, const CUtensorMap& km, const CUtensorMap& vm,
+                   uint32_t n_blocks, cudaStream_t s) {
     // the Q, K and V tiles; at least 80 KB, so that never more than two CTAs (2 x 256 TMEM columns) share an SM
     constexpr int kTiles = 3 * kTileRows * D * 2 + 1024;
     constexpr int kSmem = kTiles > 80 * 1024 ? kTiles : 80 * 1024;
@@ -440,7 +772,7 @@ cudaError_t launch(const AttnParams& p, const CUtensorMap& qm, const CUtensorMap
         if (e != cudaSuccess) return e;
         if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
     }
-    prompt_attn_kernel<D><<<dim3(p.n_blk, p.Hq, B), kThreads, kSmem, s>>>(p, qm, km, vm);
+    prompt_attn_kernel<D><<<n_blocks, kThreads, kSmem, s>>>(p, qm, km, vm);
     return cudaGetLastError();
 }
 
@@ -465,6 +797,10 @@ int prompt_attn(const baklava_shape* shape, const void* q, const baklava_strides
         !baklava_strides_ok(o_str, seqs, shape->Hq, tokens, shape->D))
         return BAKLAVA_ERR_INVALID_ARG;
     if (B > 65535 || shape->Hq > 65535 || tokens > INT32_MAX - kTileRows) return BAKLAVA_ERR_UNSUPPORTED;
+    const int64_t n_blk = ((int64_t)T + kTileRows - 1) / kTileRows;
+    // room for every row block: packed prompts have at most total / 128 full ones and one begun each
+    int64_t n_blocks = (packed ? std::min<int64_t>(total / kTileRows + B, n_blk * B) : n_blk * B) * shape->Hq;
+    if (n_blocks > INT32_MAX) return BAKLAVA_ERR_UNSUPPORTED;
 
     AttnParams p;
     p.prompt_len = prompt_len;
@@ -478,8 +814,8 @@ int prompt_attn(const baklava_shape* shape, const void* q, const baklava_strides
     p.lse_head = packed ? total : T;
     p.status = status;
     p.total = total;
-    p.T = T; p.Hq = shape->Hq; p.Hkv = shape->Hkv;
-    p.n_blk = (int)(((int64_t)T + kTileRows - 1) / kTileRows);
+    p.B = B; p.T = T; p.Hq = shape->Hq; p.Hkv = shape->Hkv;
+    p.n_blk = (int)n_blk;
     p.scale_log2 = kLog2e / sqrtf((float)shape->D);
 
     CUtensorMap qm, km, vm;
@@ -488,7 +824,8 @@ int prompt_attn(const baklava_shape* shape, const void* q, const baklava_strides
         !make_tokens_map(&vm, v, shape->D, tokens, shape->Hkv, seqs, v_str->token, v_str->head, v_str->seq, kTileRows))
         return BAKLAVA_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = shape->D == 128 ? launch<128>(p, qm, km, vm, B, s) : launch<64>(p, qm, km, vm, B, s);
+    const cudaError_t e = shape->D == 128 ? launch<128>(p, qm, km, vm, (uint32_t)n_blocks, s)
+                                            : launch<64>(p, qm, km, vm, (uint32_t)n_blocks, s);
     return e == cudaSuccess ? BAKLAVA_OK : BAKLAVA_ERR_CUDA;
 }
 
