@@ -308,55 +308,66 @@ __device__ __forceinline__ void produce(const AttnParams& p, Shared& sm, const C
     int tile0 = 0, group0 = 0;
     bool more = true;
     for (int k = 0;; ++k) {
-        const int n_it = blk.row0 / kTileRows + 1;
-        bool ok = true, asked = false, got = false;
+        const int n_it = blk.row0 / kTileRows + 1, kvh = blk.h / cta.kv_group;
+        const bool clean = blk.row0 + kTileRows > blk.len;   // the last tile holds value rows that are no tokens
+        bool ok = true, got = false;
         uint32_t x = 0;
+        // bar_pa collects the eight softmax warps and the load V(it), bar_pb the same warps and K(it + 1): K(j + 1)
+        // takes the place of K(j) once S(j) is complete, V(j) that of the tile before it once P V of that tile is.
+        auto load_value_tile = [&](int j) {
+            const uint32_t pa = smem_u32(&sm.bar_pa[(tile0 + j) % kGroupRing]);
+            if (clean && j == n_it - 1) {                    // through the softmax warps, which arrive on bar_pa as ever
+                load(&v_map, smem_u32(&sm.bar_v), cta.v_tile, j * kTileRows, kvh);
+                tc::mbar_arrive(pa);
+            } else {
+                load(&v_map, pa, cta.v_tile, j * kTileRows, kvh);
+            }
+        };
+        auto load_next_key_tile = [&](int j) {
+            const uint32_t pb = smem_u32(&sm.bar_pb[(tile0 + j) % kGroupRing]);
+            if (j + 1 < n_it) load(&k_map, pb, cta.k_tile, (j + 1) * kTileRows, kvh);
+            else tc::mbar_arrive(pb);
+        };
         if (lane == 0) {
             // a block in the list of those to redo may come from this block, the one before it and the one after
-            asked = more && *(volatile int*)&sm.redo_count + 4 <= kMaxRedo;
-            if (asked) request_block(answer, bar_answer);
-            const int kvh = blk.h / cta.kv_group;
-            const bool clean = blk.row0 + kTileRows > blk.len;   // the last tile holds value rows that are no tokens
+            const bool ask = more && *(volatile int*)&sm.redo_count + 4 <= kMaxRedo;
+            if (ask) request_block(answer, bar_answer);
             // Q and K are free: S of the block before has been formed (its last S was waited for below)
             load(&q_map, smem_u32(&sm.bar_q), cta.q_tile, blk.row0, blk.h);
             load(&k_map, smem_u32(&sm.bar_k0), cta.k_tile, 0, kvh);
-            // bar_pa collects the eight softmax warps and the load V(it), bar_pb the same warps and K(it + 1): K(j + 1)
-            // takes the place of K(j) once S(j) is complete, V(j) that of the tile before it once P V of that tile is.
-            for (int j = 0; j < n_it; ++j) {
-                if (group0 + j >= 1) ok = group_wait(group0 + j - (j == 0));
-                if (!ok) break;
-                const uint32_t pa = smem_u32(&sm.bar_pa[(tile0 + j) % kGroupRing]);
-                if (clean && j == n_it - 1) {                // through the softmax warps, which arrive on bar_pa as ever
-                    load(&v_map, smem_u32(&sm.bar_v), cta.v_tile, j * kTileRows, kvh);
-                    tc::mbar_arrive(pa);
-                } else {
-                    load(&v_map, pa, cta.v_tile, j * kTileRows, kvh);
-                }
-                if (j == 0) ok = group_wait(group0);
-                if (!ok) break;
-                const uint32_t pb = smem_u32(&sm.bar_pb[(tile0 + j) % kGroupRing]);
-                if (j + 1 < n_it) load(&k_map, pb, cta.k_tile, (j + 1) * kTileRows, kvh);
-                else tc::mbar_arrive(pb);
-            }
-            if (ok && asked) {
+            if (group0 > 0) ok = group_wait(group0 - 1);     // the block before is through with V
+            if (ok) load_value_tile(0);
+            if (ok && n_it == 1) load_next_key_tile(0);
+            if (ok && ask) {
                 ok = mbar_wait(bar_answer, k & 1);
                 if (ok) got = granted_block(answer, x);
             }
             if (!ok) sm.abort = 1;
         }
         if (!__shfl_sync(0xffffffffu, ok, 0)) return;
-        tile0 += n_it;
-        group0 += n_it + 1;
-        // the next block, if there is one; once there is none nothing more is asked for
+        // the next block, if there is one (once there is none nothing more is asked for): known before it is needed
         x = __shfl_sync(0xffffffffu, x, 0);
         more = __shfl_sync(0xffffffffu, got, 0);
-        more = more && locate(p, x, cursor, blk, lane);
-        if (!more) blk.row0 = -1;
+        Block next = blk;
+        more = more && locate(p, x, cursor, next, lane);
+        if (!more) next.row0 = -1;
         if (lane == 0) {
-            sm.item[k % kItemRing] = blk;
+            sm.item[k % kItemRing] = next;
             tc::mbar_arrive(smem_u32(&sm.bar_item[k % kItemRing]));
+            ok = group_wait(group0);
+            if (ok && n_it > 1) load_next_key_tile(0);
+            for (int j = 1; j < n_it && ok; ++j) {
+                ok = group_wait(group0 + j);
+                if (!ok) break;
+                load_value_tile(j);
+                load_next_key_tile(j);
+            }
+            if (!ok) sm.abort = 1;
         }
-        if (!more) return;
+        if (!__shfl_sync(0xffffffffu, ok, 0) || !more) return;
+        tile0 += n_it;
+        group0 += n_it + 1;
+        blk = next;
     }
 }
 
