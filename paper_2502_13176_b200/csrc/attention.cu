@@ -207,12 +207,13 @@ __device__ __forceinline__ bool locate(const AttnParams& p, uint32_t x, Cursor& 
 // ---------------------------------------------------------------- the steps on a tile
 // 32 keys of this thread's 64: probabilities in bf16 over the first columns of the 32 logits they came from; `sum` += the
 // probabilities before their rounding.
-__device__ __forceinline__ void softmax_half(uint32_t column, bool diagonal, int first_key, int row, f32x2 scale2, float ref,
+template <bool kDiagonal>
+__device__ __forceinline__ void softmax_half(uint32_t column, int first_key, int row, f32x2 scale2, float ref,
                                              f32x2 (&sum)[2]) {
     uint32_t v[32], w[16];
     tc::tmem_ld_32x32(column, v);
     tc::tmem_ld_wait();
-    if (diagonal) {                                           // keys above the query do not exist
+    if (kDiagonal) {                                          // keys above the query do not exist
 #pragma unroll
         for (int c = 0; c < 32; ++c)
             if (first_key + c > row) v[c] = 0xff800000u;
@@ -225,6 +226,12 @@ __device__ __forceinline__ void softmax_half(uint32_t column, bool diagonal, int
         sum[c & 1] = add2(sum[c & 1], pack2(p0, p1));
         w[c] = pack_bf16(p0, p1);
     }
+    tc::tmem_st_32x32_x16(column, w);
+    tc::tmem_st_wait();
+}
+// the same where none of the keys is seen
+__device__ __forceinline__ void no_probabilities(uint32_t column) {
+    const uint32_t w[16] = {};
     tc::tmem_st_32x32_x16(column, w);
     tc::tmem_st_wait();
 }
@@ -427,43 +434,57 @@ __device__ __forceinline__ void soften(const AttnParams& p, Shared& sm, const Ct
         const bool clean = blk.row0 + kTileRows > blk.len;
         float ref = 0.0f;                                     // log2 domain
         f32x2 sum[2] = {0ull, 0ull};                          // the row's sum (this thread's keys), four accumulators
-        for (int it = 0; it <= qb; ++it, ++tile) {
-            ok = group_wait(group++);                         // S(it) is ready
-            if (!ok) break;
-            tc::fence_after_sync();
-            if (it == 0) {
-                // every thread of the row reads the same eight columns, so the two agree without talking; part 0 puts
-                // its probabilities over them only when part 1 has read them
-                uint32_t first[8];
-                tc::tmem_ld_32x32_x8(lane_addr, first);
-                tc::tmem_ld_wait();
-                float mx = __uint_as_float(first[0]);
+        ok = group_wait(group++);                             // S(0) is ready
+        if (!ok) break;
+        tc::fence_after_sync();
+        {
+            // every thread of the row reads the same eight columns, so the two agree without talking; part 0 puts its
+            // probabilities over them only when part 1 has read them
+            uint32_t first[8];
+            tc::tmem_ld_32x32_x8(lane_addr, first);
+            tc::tmem_ld_wait();
+            float mx = __uint_as_float(first[0]);
 #pragma unroll
-                for (int c = 1; c < 8; ++c)
-                    if (qb > 0 || c <= row) mx = fmaxf(mx, __uint_as_float(first[c]));
-                ref = mx * p.scale_log2;
-                if (part == 1) {
-                    __syncwarp();
-                    if (lane == 0) tc::mbar_arrive(smem_u32(&sm.bar_ref[quarter]));
-                } else {
-                    ok = mbar_wait(smem_u32(&sm.bar_ref[quarter]), k & 1);
-                    if (!ok) break;
-                }
-            }
-            if (clean && it == qb) {
-                ok = mbar_wait(smem_u32(&sm.bar_v), cleaned++ & 1);
-                if (!ok) break;
-                clean_value_row<D, false>(cta.v_ptr, row, part, t < blk.len);
-            }
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-                softmax_half(lane_addr + col_base + hh * 32, it == qb, col_base + hh * 32, row, scale2, ref, sum);
-                tc::fence_before_sync();
+            for (int c = 1; c < 8; ++c)
+                if (qb > 0 || c <= row) mx = fmaxf(mx, __uint_as_float(first[c]));
+            ref = mx * p.scale_log2;
+            if (part == 1) {
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(smem_u32(hh == 0 ? &sm.bar_pa[tile % kGroupRing] : &sm.bar_pb[tile % kGroupRing]));
+                if (lane == 0) tc::mbar_arrive(smem_u32(&sm.bar_ref[quarter]));
+            } else {
+                ok = mbar_wait(smem_u32(&sm.bar_ref[quarter]), k & 1);
+                if (!ok) break;
             }
         }
+        auto hand_over = [&](uint64_t* bars) {
+            tc::fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(smem_u32(&bars[tile % kGroupRing]));
+        };
+        for (int it = 0; it < qb; ++it, ++tile) {
+            softmax_half<false>(lane_addr + col_base, col_base, row, scale2, ref, sum);
+            hand_over(sm.bar_pa);
+            softmax_half<false>(lane_addr + col_base + 32, col_base + 32, row, scale2, ref, sum);
+            hand_over(sm.bar_pb);
+            ok = group_wait(group++);                         // S(it + 1)
+            if (!ok) break;
+            tc::fence_after_sync();
+        }
         if (!ok) break;
+        // the diagonal tile; in the prompt's last block its value rows may not all be tokens
+        // (32 keys that none of the warp's rows sees need no exponentials)
+        if (col_base <= 32 * quarter + 31) softmax_half<true>(lane_addr + col_base, col_base, row, scale2, ref, sum);
+        else no_probabilities(lane_addr + col_base);
+        if (clean) {
+            ok = mbar_wait(smem_u32(&sm.bar_v), cleaned++ & 1);
+            if (!ok) break;
+            clean_value_row<D, false>(cta.v_ptr, row, part, t < blk.len);
+        }
+        hand_over(sm.bar_pa);
+        if (col_base <= 32 * quarter - 1) softmax_half<true>(lane_addr + col_base + 32, col_base + 32, row, scale2, ref, sum);
+        else no_probabilities(lane_addr + col_base + 32);
+        hand_over(sm.bar_pb);
+        ++tile;
         // the two threads of a row join their sums (each writes its own, both add them in the same order)
         const float2 total = unpack2(add2(sum[0], sum[1]));
         sm.part[part][row] = total.x + total.y;
@@ -599,7 +620,8 @@ __device__ __noinline__ void redo_pass(const AttnParams& p, const Block blk, Sha
             for (int hh = 0; hh < 2; ++hh) {
                 const int first_key = col_base + hh * 32;
                 if (kExact) {
-                    softmax_half(lane_addr + first_key, it == qb, first_key, row, scale2, ref, sum);
+                    if (it == qb) softmax_half<true>(lane_addr + first_key, first_key, row, scale2, ref, sum);
+                    else softmax_half<false>(lane_addr + first_key, first_key, row, scale2, ref, sum);
                 } else {
                     uint32_t v[32];
                     tc::tmem_ld_32x32(lane_addr + first_key, v);
