@@ -29,6 +29,7 @@ METRIC = "decode-step retained-KV GB/s"
 WORKLOADS = {"llama": wl.LLAMA3_8B_32K, "qwen": wl.QWEN25_7B_8K_B16, "tiny": wl.TINY}
 TRAFFIC_TABLE = os.path.join(ROOT, "profiles", "dram_traffic.txt")
 KERNEL_SOURCES = {"decode_chunk_kernel": ["decode.cu", "ptx.cuh", "common.h", "fp8.cuh"],
+                  "decode_int4_kernel": ["decode_int4.cuh", "decode.cu", "ptx.cuh", "common.h", "int4.cuh"],
                   "profile_pv_kernel": ["profile.cu", "ptx.cuh", "common.h"],
                   "qk_pass_kernel": ["prefill.cu", "ptx.cuh", "common.h"]}
 
@@ -394,8 +395,9 @@ def main():
     ap.add_argument("--policy", default="heavy", choices=["heavy", "window"],
                     help="heavy: sinks + window + accumulated-attention heavy hitters (default); "
                          "window: the paper's evaluated sinks + window policy, run without scores")
-    ap.add_argument("--kv", default="bf16", choices=["bf16", "fp8"],
-                    help="slab format: bf16 (the headline) or FP8 E4M3 with per-head scales (half the bytes per row)")
+    ap.add_argument("--kv", default="bf16", choices=["bf16", "fp8", "int4"],
+                    help="slab format: bf16 (the headline), FP8 E4M3 with per-head scales (half the bytes per row) or 4-bit "
+                         "codes with a scale per row and per channel (27 %% of the bytes)")
     ap.add_argument("--mixed-lengths", action="store_true",
                     help="prompts of different lengths (seeded, uniform in [T/8, T]) decoded at per-sequence "
                          "positions through baklava_decode_attn_varlen")
@@ -438,9 +440,9 @@ def main():
     bk.lib()                                             # fail now if the library is missing
     step_flags = bk.FLAG_NO_SCORE if args.policy == "window" else 0
     sess = DecodeSession(w, dev, chunk_tokens=args.chunk,
-                         kv_dtype=bk.KV_FP8_E4M3 if args.kv == "fp8" else bk.KV_BF16)
-    if args.kv == "fp8":
-        w = wl.scaled(w, name=w.name + "-fp8")
+                         kv_dtype={"bf16": bk.KV_BF16, "fp8": bk.KV_FP8_E4M3, "int4": bk.KV_INT4}[args.kv])
+    if args.kv != "bf16":
+        w = wl.scaled(w, name=w.name + "-" + args.kv)
     total = args.warmup + args.steps
     if args.mixed_lengths:
         from paper_2502_13176_b200 import synth
@@ -577,7 +579,8 @@ def main():
     elapsed_ms, e2e_ms = max_over_ranks([elapsed_ms, e2e_ms], dev)
 
     if rank == 0:
-        bytes_per_step = rows_per_step * w.D * 2 * (1 if args.kv == "fp8" else 2)   # K and V rows, bf16 or one byte
+        bytes_per_step = rows_per_step * bk.kv_row_bytes(w.D, sess.kv_dtype)   # K and V rows as they are stored
+        kernel = "decode_int4_kernel" if args.kv == "int4" else "decode_chunk_kernel"
         gbs = whole_job_rate(world, bytes_per_step, args.steps, elapsed_ms) / 1e9
         e2e_gbs = whole_job_rate(world, bytes_per_step, args.steps, e2e_ms) / 1e9
         peak, peak_kind = measured_peaks()
@@ -586,7 +589,7 @@ def main():
         line = {
             "metric": METRIC, "value": gbs, "unit": "GB/s", "n_gpus": world, "steps": args.steps,
             "warmup": args.warmup, "ms_per_step": elapsed_ms / args.steps, "higher_is_better": True,
-            "scaling": "weak", "vs_baseline": None, "dtype": "bf16" if args.kv == "bf16" else "fp8-e4m3 slabs, fp16 MMA",
+            "scaling": "weak", "vs_baseline": None, "dtype": {"bf16": "bf16", "fp8": "fp8-e4m3 slabs, fp16 MMA", "int4": "4-bit slabs, fp16 MMA"}[args.kv],
             "data": "synthetic",
             "config": {"workload": w.name, "layers": w.L, "batch": w.B, "context": w.T, "budget": w.budget,
                        "kv_bytes_per_step": bytes_per_step, "l2": "inputs larger than L2 (no flush)",
@@ -603,8 +606,8 @@ def main():
             "step_us_with_event_per_step": {"p10": pct(0.1), "median": pct(0.5), "p90": pct(0.9)},
             "pct_of_hbm_peak": 100.0 * gbs / world / peak,
             "roofline": {"bound": "hbm", "achieved": achieved, "peak": peak, "unit": "GB/s",
-                         "frac": achieved / peak, "traffic": ncu_traffic(w.name, "decode_chunk_kernel"),
-                         "peak_kind": peak_kind, "kernel": "decode_chunk_kernel",
+                         "frac": achieved / peak, "traffic": ncu_traffic(w.name, kernel),
+                         "peak_kind": peak_kind, "kernel": kernel,
                          "note": "events bracket one call = one kernel (attention, score update and eviction)"},
             "e2e": {"value": e2e_gbs, "unit": "GB/s", "h2d_bytes_per_step": h2d, "d2h_bytes_per_step": d2h},
             "gpu_launches": args.steps * (w.L if args.per_layer != "off" else 1),

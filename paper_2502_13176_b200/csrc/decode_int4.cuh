@@ -423,17 +423,24 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
             if (lane == 0 && j + kInt4Slots < fed) load(j + kInt4Slots);
             return true;
         };
+        // sinks + window: the rows' positions are asked for before the tile and looked at after it
+        int ps[kInt4Tokens / 32];
         if (kByPosition && pos_evict) {
-            for (int tok = tok_t + lane; tok < min(end, tok_t + kInt4Tokens); tok += 32) {
-                if (tok == hs.f) continue;
-                const int ps = p.pos[row0 + tok];
-                if (ps >= p.n_sink && ps <= window_from && ps < old_pos) { old_pos = ps; old_slot = tok; }
+#pragma unroll
+            for (int i = 0; i < kInt4Tokens / 32; ++i) {
+                const int tok = tok_t + lane + 32 * i;
+                ps[i] = tok < end && tok != hs.f ? p.pos[row0 + tok] : -1;
             }
         }
         const bool inside = tok_t + kInt4Tokens <= end;
         const bool has_hole = hole >= tok_t && hole < tok_t + kInt4Tokens;
         const bool has_slot = hs.do_append && hs.f >= tok_t && hs.f < tok_t + kInt4Tokens;
         alive = inside && !has_hole && !has_slot ? tile_body(std::false_type{}) : tile_body(std::true_type{});
+        if (kByPosition && pos_evict) {
+#pragma unroll
+            for (int i = 0; i < kInt4Tokens / 32; ++i)
+                if (ps[i] >= p.n_sink && ps[i] <= window_from && ps[i] < old_pos) { old_pos = ps[i]; old_slot = tok_t + lane + 32 * i; }
+        }
     }
     if (!alive && lane == 0) {
         // a bounded wait gave up: the status word says so, and what this warp has requested is left time to land
