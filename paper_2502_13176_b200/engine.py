@@ -1,6 +1,6 @@
 """Convenience layer over the binding: owns the device buffers of one budgeted cache and drives
-allocate -> bulk evict -> decode steps.  Memory management and call sequencing only; every
-computation happens inside libbaklava.so."""
+allocate -> prompt (attention, scores, bulk evict) -> decode steps.  Memory management and call
+sequencing only; every computation happens inside libbaklava.so."""
 import numpy as np
 import torch
 
@@ -10,6 +10,16 @@ from . import workloads as wl
 
 def shape_of(w):
     return bk.make_shape(w.L, w.Hq, w.Hkv, w.D, w.page, w.n_sink, w.recent_num, w.recent_den)
+
+
+def norm_rope(shape, q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6, flags=0):
+    """Queries [B, Hq, T, D] and keys [B, Hkv, T, D] (any views with contiguous rows, e.g. of the projection's output)
+    as attention takes them: normed per head where a weight is given, rotated to their positions (int32 [B, T]); new
+    contiguous tensors.  For a decode step T = 1: `.squeeze(2)` is the [B, H, D] of `DecodeSession.step`."""
+    qo = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+    ko = torch.zeros(k.shape, dtype=k.dtype, device=k.device)
+    bk.baklava_qk_norm_rope(shape, q, k, positions, inv_freq, q_weight, k_weight, eps, qo, ko, flags)
+    return qo, ko
 
 
 class DecodeSession:
@@ -39,6 +49,7 @@ class DecodeSession:
         self.out = torch.zeros((nl, w.B, w.Hq, w.D), dtype=torch.bfloat16, device=self.device)
         self.lse = torch.zeros((nl, w.B, w.Hq), dtype=torch.float32, device=self.device)
         self.t = 0
+        self.prompt_error = None
 
     def prefill_synthetic(self, prompt_len=None, data=None):
         """Fill every head from the workload's dense synthetic prompt through baklava_evict, a layer at a time.
@@ -55,6 +66,25 @@ class DecodeSession:
             torch.cuda.synchronize(self.device)
         self.t = w.T
         self.t_seq = plen
+
+    def prefill_layer(self, l, q, k, v, prompt_len=None):
+        """One layer of a real prompt: causal attention (its output [B, Hq, T, D] is returned), the attention every token
+        received as its score (from the same rows' log-sum-exp), and the bulk eviction into the layer's slabs.
+        q: bf16 [B, Hq, T, D], k, v: bf16 [B, Hkv, T, D], contiguous; prompt_len: device int32 [B] or None."""
+        B, T = q.shape[0], q.shape[2]
+        w = self.w
+        out = torch.zeros(q.shape, dtype=q.dtype, device=self.device)
+        lse = torch.empty((B, w.Hq, T), dtype=torch.float32, device=self.device)
+        bk.baklava_prefill_attn(self.shape, q, k, v, prompt_len, out, lse, self.cache.status)
+        score = torch.empty((B, w.Hkv, T), dtype=torch.float32, device=self.device)
+        ws = torch.empty((max(bk.baklava_prefill_workspace_size(self.shape, B, T),
+                              bk.baklava_evict_workspace_size(self.shape, B, 1, T)),), dtype=torch.uint8, device=self.device)
+        bk.baklava_prefill_scores(self.shape, q, k, prompt_len, B, T, score, ws, lse=lse)
+        self.prompt_error = ws[:4].view(torch.int32).clone()          # (the eviction uses the workspace next)
+        bk.baklava_evict_varlen(self.shape, self.cache, l, l + 1, k, v, score, T, prompt_len, 0, w.Hkv * T, T, 1, ws)
+        self.t = T
+        self.t_seq = prompt_len
+        return out
 
     def step(self, q, k_new, v_new, flags=0):
         """One decode step for the session's layer range; returns the output tensor (device, bf16)."""
@@ -105,3 +135,5 @@ class DecodeSession:
         code = int(self.cache.status.item())
         if code:
             raise RuntimeError("device status word = %d" % code)
+        if self.prompt_error is not None and int(self.prompt_error.item()):
+            raise RuntimeError("the prompt scores gave up a wait")
