@@ -11,8 +11,10 @@
 //   - the K channel scales are multiplied into the query, the V channel scales into the partial output, the K row
 //     scales into the logits, the V row scales into the probabilities (relative to the largest one met so far, which
 //     is handled like the running maximum: fp16 holds what is at most 1).
-// The scaled query is brought to 2^12 and split into two fp16 terms (22 significant bits): one term (11 bits) would
-// shift every logit of a head by a common error of 1e-4.  With at most four heads in the group (kTwice) the two terms of
+// The scaled query is brought to below 2^10 and split into two fixed-point terms, an integer and a multiple of 2^-11: one
+// term would shift every logit of a head by a common error of 1e-4, and sums of small integers times small integers
+// stay below 2^22 units, so that the accumulators hold them exactly (the tensor cores cut off what an fp32 accumulator
+// cannot hold, which with floating-point terms shifted a head's logits by up to 5e-5).  With at most four heads in the group (kTwice) the two terms of
 // a head are two columns of ONE MMA, h and h + 4, whose results are added by one exchange between lanes: half the MMAs.
 // The exchange leaves a lane one token row instead of two, so that the softmax runs on all 32 lanes where half of them
 // would have had the group's missing heads.
@@ -163,7 +165,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     // ---- query fragments (B operand): head g (kTwice: first terms for g < 4, second terms for g >= 4); registers
     // j = 0 .. 3 of a group of 32 channels are the nibbles (j, j + 4)
     uint32_t qq[D / 8], ql[kTwice ? 1 : D / 8];
-    float q_off[2], q_fac[2];                             // this lane's two heads: offset, factor of the logits
+    float q_off[2], q_off2[2], q_fac[2];                  // this lane's two columns: offsets of the terms, factor of the logits
     {
         float x[D / 4];
         float big = 0.0f;
@@ -182,35 +184,38 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
         }
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-        // to [2^12, 2^13): a power of two, which the logits are multiplied by again (with the codes' 2^24)
+        // to [2^9, 2^10): a power of two, which the logits are multiplied by again (with the codes' 2^24)
         const int ex = min(max((int)(__float_as_uint(big) >> 23), 32), 222);     // biased exponent
-        const float up = __uint_as_float((uint32_t)(127 + 12 + 127 - ex) << 23);
-        const float back = __uint_as_float((uint32_t)(ex - 12 + 24) << 23);
-        float sum = 0.0f;
+        const float up = __uint_as_float((uint32_t)(127 + 9 + 127 - ex) << 23);
+        const float back = __uint_as_float((uint32_t)(ex - 9 + 24) << 23);
+        float sum = 0.0f, sum2 = 0.0f;                     // of the terms: integers, and multiples of 2^-11
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float k = (j & 1) ? 0.0625f : 1.0f;      // odd nibbles stand 16 times higher
-                const float a = x[8 * c + j] * up * k, b = x[8 * c + j + 4] * up * k;
-                const uint32_t hi = pack_f16(a, b);
-                const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-                const uint32_t lo = pack_f16(a - h.x, b - h.y);
-                const float2 l = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+                const float a = x[8 * c + j] * up, b = x[8 * c + j + 4] * up;
+                const float a1 = rintf(a), b1 = rintf(b);
+                const float a2 = rintf((a - a1) * 2048.0f) * 0x1p-11f, b2 = rintf((b - b1) * 2048.0f) * 0x1p-11f;
+                const uint32_t hi = pack_f16(a1 * k, b1 * k), lo = pack_f16(a2 * k, b2 * k);     // (exact)
                 if (kTwice) {
                     qq[4 * c + j] = g8 < 4 ? hi : lo;
                 } else {
                     qq[4 * c + j] = hi;
                     ql[4 * c + j] = lo;
                 }
-                sum = fmaf((h.x + l.x) + (h.y + l.y), (j & 1) ? 16.0f : 1.0f, sum);
+                sum += a1 + b1;
+                sum2 += a2 + b2;
             }
+        if (kTwice && g8 >= 4) sum = sum2;                 // this lane's column
+        sum2 += __shfl_xor_sync(0xffffffffu, sum2, 1);
+        sum2 += __shfl_xor_sync(0xffffffffu, sum2, 2);
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             q_off[e] = -8.0f * 0x1p-24f * __shfl_sync(0xffffffffu, sum, 4 * (2 * t4 + e));
-            if (kTwice && t4 >= 2) q_off[e] = 0.0f;        // (once per head)
+            q_off2[e] = -8.0f * 0x1p-24f * __shfl_sync(0xffffffffu, sum2, 4 * (2 * t4 + e));
             q_fac[e] = __shfl_sync(0xffffffffu, back, 4 * (2 * t4 + e)) * p.scale_log2;
         }
     }
@@ -278,11 +283,15 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
             for (int blk = 0; blk < kBlocks; ++blk)
 #pragma unroll
                 for (int r = 0; r < kR; ++r) rs[blk][r] = scales[blk * 16 + g8 + (kTwice ? (upper ? 8 : 0) : 8 * r)];
-            float st[kBlocks][4];
+            float st[kBlocks][4], st2[kTwice ? 1 : kBlocks][4];      // (the second terms' sums apart: see above)
 #pragma unroll
             for (int blk = 0; blk < kBlocks; ++blk) {
                 st[blk][0] = st[blk][2] = q_off[0];
                 st[blk][1] = st[blk][3] = q_off[1];
+                if (!kTwice) {
+                    st2[blk][0] = st2[blk][2] = q_off2[0];
+                    st2[blk][1] = st2[blk][3] = q_off2[1];
+                }
             }
 #pragma unroll
             for (int c = 0; c < D / 32; ++c)
@@ -295,7 +304,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
                         for (int blk = 0; blk < kBlocks; ++blk) {
                             const uint32_t lo = kb[blk][c >> 1][2 * (c & 1)] >> (8 * jj), hi = kb[blk][c >> 1][2 * (c & 1) + 1] >> (8 * jj);
                             const uint32_t* b = term ? ql : qq;
-                            mma_f16_free(st[blk], lo & 0x000f000fu, hi & 0x000f000fu, lo & 0x00f000f0u, hi & 0x00f000f0u,
+                            mma_f16_free(term ? st2[kTwice ? 0 : blk] : st[blk], lo & 0x000f000fu, hi & 0x000f000fu, lo & 0x00f000f0u, hi & 0x00f000f0u,
                                          b[at], b[at + 1]);
                         }
                 }
@@ -315,7 +324,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
                     sv_max = fmaxf(sv_max, fabsf(sv[blk][r]));
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float x = st[blk][2 * r + e];
+                        float x = st[blk][2 * r + e] + (kTwice ? 0.0f : st2[kTwice ? 0 : blk][2 * r + e]);
                         if (kTwice) {
                             const float give = upper ? st[blk][e] : st[blk][2 + e];
                             x = (upper ? st[blk][2 + e] : st[blk][e]) + __shfl_xor_sync(0xffffffffu, give, 2);
