@@ -75,9 +75,8 @@ __global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_kernel(const RopePar
     constexpr int kLanes = D / 16;                   // lanes per row, two 8-element pieces each
     constexpr int kGroups = kThreads / kLanes;
     constexpr int kHeadStep = kGroups / kTok;        // heads worked on at the same time
-    // cosine and sine as the lanes read them: piece by piece, each the multiplier of the element itself and of its
-    // partner (half-split: cos / sin of the eight pairs; side by side: cos twice, -sin and sin)
-    __shared__ __align__(16) float t_cos[kTok][D], t_sin[kTok][D];
+    // cosine and sine of the pairs
+    __shared__ __align__(16) float t_cos[kTok][D / 2], t_sin[kTok][D / 2];
     __shared__ __align__(16) float wt[2][D];         // the norms' weights
     __shared__ uint4 ring[kAhead + 1][2][kThreads];  // every thread's two pieces of the rows ahead
     const int tid = threadIdx.x;
@@ -121,14 +120,8 @@ __global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_kernel(const RopePar
             const double turns = (double)p.pos[n0 + tq] * (double)p.inv_freq[f] * 0.15915494309189535;   // 1 / (2 pi)
             float s, c;
             sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-            if (kInterleaved) {
-                t_cos[tq][2 * f] = t_cos[tq][2 * f + 1] = c;
-                t_sin[tq][2 * f] = -s;
-                t_sin[tq][2 * f + 1] = s;
-            } else {
-                t_cos[tq][f] = c;
-                t_sin[tq][f] = s;
-            }
+            t_cos[tq][f] = c;
+            t_sin[tq][f] = s;
         }
     }
     for (int i = tid; i < 2 * D; i += kThreads) {
@@ -137,17 +130,24 @@ __global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_kernel(const RopePar
     }
     __syncthreads();
     const bool on = exists && p.pos[n] >= 0;         // a negative position: the token sits out
-    // the lane's multipliers, the same for all its rows (side by side: of piece a, then of piece b)
+    // the lane's multipliers of an element and of its partner, the same for all its rows.  Half-split: cos and sin of
+    // the lane's eight pairs; side by side: cos twice, -sin and sin for the four pairs of piece a, then of piece b.
     f32x2 cs[kInterleaved ? 8 : 4], sn[kInterleaved ? 8 : 4];
+    if (rotates) {
 #pragma unroll
-    for (int i = 0; i < (kInterleaved ? 2 : 1); ++i) {
-        f32x2 v[4];
-        load4(&t_cos[tk][8 * (i ? pb : pa)], v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) cs[4 * i + e] = v[e];
-        load4(&t_sin[tk][8 * (i ? pb : pa)], v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sn[4 * i + e] = v[e];
+        for (int i = 0; i < 4; ++i) {
+            if (kInterleaved) {
+                const float ca = t_cos[tk][4 * pa + i], sa = t_sin[tk][4 * pa + i];
+                const float cb = t_cos[tk][4 * pb + i], sb = t_sin[tk][4 * pb + i];
+                cs[i] = pack2(ca, ca);
+                sn[i] = pack2(-sa, sa);
+                cs[kInterleaved ? 4 + i : i] = pack2(cb, cb);
+                sn[kInterleaved ? 4 + i : i] = pack2(-sb, sb);
+            } else {
+                cs[i] = pack2(t_cos[tk][8 * pa + 2 * i], t_cos[tk][8 * pa + 2 * i + 1]);
+                sn[i] = pack2(t_sin[tk][8 * pa + 2 * i], t_sin[tk][8 * pa + 2 * i + 1]);
+            }
+        }
     }
 #pragma unroll 1
     for (int i = 0; i < n_rows; ++i) {
