@@ -286,14 +286,48 @@ __device__ __forceinline__ void let_copies_land() {
     const long long t0 = clock64();
     while (clock64() - t0 < kGraceCycles) { }
 }
-__device__ __forceinline__ __nv_bfloat16* out_row(const AttnParams& p, const Block& blk, int t) {
-    return p.out + blk.seq * p.so.seq + (int64_t)(blk.base + t) * p.so.token + blk.h * p.so.head;
+// 32 rows x 32 columns of a warp (thread = row) times the rows' factors, rounded, into the output.  Rows lie far apart, so
+// they go through the warp's patch of shared memory, from which neighbouring lanes write a row's neighbouring 16-byte
+// pieces: 64 bytes of a row at a time (D = 64), 32 where shared memory is short (D = 128).  A store of one piece per row
+// costs the store unit one pass per row: the epilogue took 3 500 cycles of a row block that way (D = 128).
+template <int D>
+constexpr int kPatchPieces = D == 64 ? 4 : 2;
+template <int D>
+constexpr int kPatchBytes = 32 * 16 * kPatchPieces<D>;
+template <int D>
+__device__ __forceinline__ void store_rows(const AttnParams& p, const Block& blk, uint8_t* patch, int first_row, int col0, int lane,
+                                           const uint32_t (&o)[32], float factor) {
+    constexpr int kPieces = kPatchPieces<D>;
+    __nv_bfloat16* const base = p.out + blk.seq * p.so.seq + (int64_t)(blk.base + first_row) * p.so.token + blk.h * p.so.head + col0;
+    auto place = [&](int row, int piece) {                    // (the exclusive-or keeps eight lanes on different banks)
+        return reinterpret_cast<uint4*>(patch + row * (16 * kPieces) + ((piece ^ (row >> (kPieces == 4 ? 1 : 2) & (kPieces - 1))) << 4));
+    };
+#pragma unroll
+    for (int c = 0; c < 4; c += kPieces) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[e] = pack_bf16(__uint_as_float(o[8 * (c + i) + 2 * e]) * factor, __uint_as_float(o[8 * (c + i) + 2 * e + 1]) * factor);
+            *place(lane, i) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            const int row = 32 / kPieces * k + lane / kPieces, piece = lane % kPieces;
+            const uint4 v = *place(row, piece);
+            if (first_row + row < blk.len) *reinterpret_cast<uint4*>(base + row * p.so.token + 8 * (c + piece)) = v;
+        }
+        __syncwarp();
+    }
 }
 
 // What a role needs to know of the CTA.
 struct Cta {
     uint32_t q_tile, k_tile, v_tile, tmem;
     uint8_t* v_ptr;
+    uint8_t* patch;               // this warp's patch for the output
     int kv_group;                 // query heads per KV head
 };
 
@@ -496,7 +530,6 @@ __device__ __forceinline__ void soften(const AttnParams& p, Shared& sm, const Ct
         const float l = sm.part[0][row] + sm.part[1][row], inv = 1.0f / l;
         bool again = !(l <= kMaxSum);
         tc::fence_after_sync();
-        __nv_bfloat16* const dst = out_row(p, blk, t) + part * (D / 2);
 #pragma unroll
         for (int ch = 0; ch < D / 64; ++ch) {                 // 32 columns of the head dimension at a time
             uint32_t o[32];
@@ -506,16 +539,7 @@ __device__ __forceinline__ void soften(const AttnParams& p, Shared& sm, const Ct
 #pragma unroll
             for (int c = 0; c < 32; ++c) worst = fmaf(fabsf(__uint_as_float(o[c])), 0x1p-20f, worst);
             again = again || !(worst <= kFinite);
-            if (t < blk.len) {
-#pragma unroll
-                for (int c8 = 0; c8 < 4; ++c8) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        w[c] = pack_bf16(__uint_as_float(o[8 * c8 + 2 * c]) * inv, __uint_as_float(o[8 * c8 + 2 * c + 1]) * inv);
-                    *reinterpret_cast<uint4*>(dst + ch * 32 + 8 * c8) = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            }
+            store_rows<D>(p, blk, cta.patch, blk.row0 + 32 * quarter, part * (D / 2) + ch * 32, lane, o, inv);
         }
         tc::fence_before_sync();                              // (O may be written again behind this block's next arrival)
         if (p.lse && part == 0 && t < blk.len)
@@ -649,7 +673,6 @@ __device__ __noinline__ void redo_pass(const AttnParams& p, const Block blk, Sha
         } else {
             const float l = sm.part[0][row] + sm.part[1][row], inv = 1.0f / l;
             tc::fence_after_sync();
-            __nv_bfloat16* const dst = out_row(p, blk, t) + part * (D / 2);
             for (int ch = 0; ch < D / 64; ++ch) {
                 uint32_t o[32];
                 tc::tmem_ld_32x32(cta.tmem + ((uint32_t)(32 * quarter) << 16) + kOColumn + part * (D / 2) + ch * 32, o);
@@ -665,16 +688,7 @@ __device__ __noinline__ void redo_pass(const AttnParams& p, const Block blk, Sha
                         }
                     }
                 }
-                if (t < blk.len) {
-#pragma unroll
-                    for (int c8 = 0; c8 < 4; ++c8) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            w[c] = pack_bf16(__uint_as_float(o[8 * c8 + 2 * c]) * inv, __uint_as_float(o[8 * c8 + 2 * c + 1]) * inv);
-                        *reinterpret_cast<uint4*>(dst + ch * 32 + 8 * c8) = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                }
+                store_rows<D>(p, blk, cta.patch, blk.row0 + 32 * quarter, part * (D / 2) + ch * 32, lane, o, inv);
             }
             if (p.lse && part == 0 && t < blk.len)
                 p.lse[blk.seq * p.lse_seq + blk.h * p.lse_head + blk.base + t] = (sm.ref[row] + log2f(l)) * kLn2;
@@ -719,6 +733,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attn_kernel(const __grid_c
     cta.k_tile = tiles + kTileBytes;
     cta.v_tile = tiles + 2 * kTileBytes;
     cta.v_ptr = smem_raw + (tiles - smem_u32(smem_raw)) + 2 * kTileBytes;
+    cta.patch = smem_raw + (tiles - smem_u32(smem_raw)) + 3 * kTileBytes + (warp & 7) * kPatchBytes<D>;   // (softmax warps: 2 .. 9)
     cta.kv_group = p.Hq / p.Hkv;
     if (tid == 0) {
         mbar_init(smem_u32(&sm.bar_q), 1);
@@ -792,8 +807,10 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attn_kernel(const __grid_c
 template <int D>
 cudaError_t launch(const AttnParams& p, const CUtensorMap& qm, const CUtensorMap& km, const CUtensorMap& vm,
                    uint32_t n_blocks, cudaStream_t s) {
-    // the Q, K and V tiles; at least 80 KB, so that never more than two CTAs (2 x 256 TMEM columns) share an SM
-    constexpr int kTiles = 3 * kTileRows * D * 2 + 1024;
+    // the Q, K and V tiles and the patches; at least 80 KB, so that never more than two CTAs (2 x 256 TMEM columns)
+    // share an SM, and at most 110 KB, so that two do
+    constexpr int kTiles = 3 * kTileRows * D * 2 + kSoftmaxWarps * kPatchBytes<D> + 1024;
+    static_assert(kTiles <= 110 * 1024, "two CTAs per SM");
     constexpr int kSmem = kTiles > 80 * 1024 ? kTiles : 80 * 1024;
     // the attribute belongs to the function on the current device: set once per device and instantiation
     static std::atomic<uint64_t> configured{0};
