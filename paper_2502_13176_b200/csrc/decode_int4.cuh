@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
         // to [2^9, 2^10): a power of two, which the logits are multiplied by again (with the codes' 2^24)
-        const int ex = min(max((int)(__float_as_uint(big) >> 23), 32), 222);     // biased exponent
+        const int ex = min(max((int)(__float_as_uint(big) >> 23), 9), 239);      // biased exponent
         const float up = __uint_as_float((uint32_t)(127 + 9 + 127 - ex) << 23);
         const float back = __uint_as_float((uint32_t)(ex - 9 + 24) << 23);
         float sum = 0.0f, sum2 = 0.0f;                     // of the terms: integers, and multiples of 2^-11
@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
                 l_run[e] = l_run[e] * corr[e] + psum;
             }
             const float seen = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv_max)));
-            if (seen > v_ref) {                            // the V scales' reference follows their maximum
+            if (seen > fmaxf(v_ref, 0x1p-126f)) {          // the V scales' reference follows their maximum
                 const float ratio = v_ref / seen;
                 corr[0] *= ratio;
                 corr[1] *= ratio;

@@ -238,9 +238,13 @@ extern "C" __attribute__((visibility("default"))) int baklava_decode_plan(const 
             // waves (Llama-shaped step 66 us, graded list 70 us; one wave of 8192-token chunks 75 us).
             guided = false;
             for (target = 2 * kMinChunk; target < 8192; target += kTile) {
-                int64_t count = 0;
-                for (int i : heads) count += pieces_of(cap[(size_t)layer_begin * Hkv + i], target) * B;
-                if (count <= 2 * slots) break;
+                int64_t count = 0, most = 0;
+                for (int i : heads) {
+                    const int64_t pieces = pieces_of(cap[(size_t)layer_begin * Hkv + i], target);
+                    count += pieces * B;
+                    most = std::max(most, pieces);
+                }
+                if (count <= 2 * slots && most * (shape->Hq / Hkv) <= max_merge_entries(shape->D)) break;
             }
         } else if (target == kMinChunk) {
             // A short launch (one layer of a model): nothing balances a second, partly filled wave, so all chunks

@@ -260,6 +260,49 @@ def test_queries_of_any_size(q_scale):
     check_direct(lens, 4, setup, out, lse)
 
 
+def test_scales_at_the_ends_of_the_range():
+    lens = [130, 130]
+    chan = plain_chan(2, np.random.default_rng(21))
+    chan[0, 0] *= 1e30                                     # the scaled query is huge, the rows are tiny
+
+    def scales(r, shape):
+        s = 0.2 + 0.3 * r.random(shape)
+        s[:144, 0] *= 1e-30
+        s[144:, 1] = 1e-42                                 # V rows below the normal range: their sum is 0 to 1e-38
+        return s
+
+    setup = direct(lens, 4, chan, 22, row_scale=scales)
+    out, lse = attend(*setup[:3], setup[4], setup[8])
+    check_direct(lens[:1], 4, (setup[0], setup[1], setup[2], setup[3][:, :1], setup[4], setup[5], setup[6], setup[7][:1],
+                               setup[8], setup[9][:, :1]), out, lse)
+    assert float(out[:, :, 4:].float().abs().max()) <= 1e-37 and bool(torch.isfinite(lse).all())
+
+
+@pytest.mark.parametrize("flags", [0, bk.FLAG_OVERLAP_PREV, bk.FLAG_NO_SCORE], ids=["two kernels", "one kernel", "no scores"])
+def test_a_wait_that_runs_out_loses_the_step_and_nothing_else(flags):
+    w = wl.scaled(wl.LLAMA3_8B_32K, L=2, T=3000, steps=4)
+    chunk = 256 if flags != bk.FLAG_NO_SCORE else 8192     # (heads of one chunk write their own output)
+    s = Session4(w, chunk_tokens=chunk)
+    s.step(0)
+    state = [t.clone() for t in (s.cache.len, s.cache.free_slot, s.cache.score)]
+    q, kn, vn = wl.decode_inputs(w, 1, s.scales, "cuda")
+    bk.baklava_set_wait_limit(2_000_000)                             # about a millisecond
+    try:
+        s.out.fill_(7.0)
+        bk.baklava_decode_attn(s.shape, s.cache, q, kn, vn, s.t, s.out, s.lse, bk.FLAG_TEST_STALL | flags, s.plan, s.ws)
+        torch.cuda.synchronize()
+    finally:
+        bk.baklava_set_wait_limit(100_000_000)
+    assert int(s.cache.status.item()) == bk.STATUS_TIMEOUT
+    assert torch.equal(state[0], s.cache.len) and torch.equal(state[1], s.cache.free_slot)
+    valid = s.cache.pos.ne(-1) & (s.cache.pos < s.t)
+    assert torch.equal(state[2][valid], s.cache.score[valid])
+    assert torch.all(s.out == 7.0)
+    s.cache.status.zero_()
+    for i in range(1, 4):                                            # the same workspace, no re-zeroing
+        s.step(i)
+
+
 def test_empty_cache_and_infinite_stale_rows():
     setup = direct([0, 40], 2, plain_chan(2, np.random.default_rng(4)), 11, stale=float("inf"))
     out, lse = attend(*setup[:3], setup[4], setup[8])

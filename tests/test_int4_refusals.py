@@ -53,3 +53,14 @@ def test_plan_knows_the_format():
     assert plan.info.n_items > 0
     with pytest.raises(bk.BaklavaError):
         bk.baklava_decode_plan(sh, cap, 4, 0, 1, int(cap.sum()), kv_dtype=3)
+
+
+def test_plan_of_one_very_long_head_stays_mergeable():
+    for Hq in (1, 8):
+        sh = bk.make_shape(1, Hq, 1, 128)
+        cap = np.array([[2 << 20]], dtype=np.int32)
+        plan = bk.baklava_decode_plan(sh, cap, 1, 0, 1, 2 << 20, kv_dtype=bk.KV_INT4)
+        items = plan.items[:plan.info.n_items]
+        assert plan.info.n_items * Hq <= 48 * 128
+        assert (np.sort(items[:, 1]) == np.cumsum(np.concatenate([[0], items[np.argsort(items[:, 1]), 2]]))[:-1]).all()
+        assert items[:, 2].sum() >= 2 << 20 and (items[:, 2] % 64 == 0).all()
