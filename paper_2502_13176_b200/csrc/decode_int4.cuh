@@ -3,17 +3,19 @@
 //
 // A code is u = 1 .. 15 and stands for (u - 8) * row scale * channel scale.  Everything but the codes is linear in
 // something that is applied once, so that widening them costs little more than one AND per MMA register:
-//   - four bits in the low or second nibble of a 16-bit word ARE the fp16 number u * 2^-24 or u * 2^-20 (a subnormal,
-//     which the MMA takes exactly), and a 32-bit word of eight codes gives the four register pairs of two MMAs by
-//     masking, with one shift; the factor 16 between the two kinds is taken off the other operand (K) or the result (V);
+//   - four or eight bits at the bottom of a 16-bit word ARE an fp16 number, u * 2^-24 (a subnormal, which the MMA takes
+//     exactly): of two neighbouring codes u0, u1 the operands u0 and u0 + 16 u1 serve as well as u0 and u1, since
+//     q0 u0 + q1 u1 = (q0 - q1 / 16) u0 + (q1 / 16) (u0 + 16 u1), and likewise the two products with V give both
+//     channels.  A 32-bit word of eight codes becomes the four register pairs of two MMAs by three ANDs and a byte
+//     permute (four ANDs and a shift for the codes themselves; the ALU pipe is the busiest one);
 //   - the offset: sum_d (u - 8) q_d = sum_d u q_d - 8 sum_d q_d, the accumulator's initial value; for V the same with
 //     8 sum_t p_t, which one more MMA against a constant operand sums from the very probabilities that were used;
 //   - the K channel scales are multiplied into the query, the V channel scales into the partial output, the K row
 //     scales into the logits, the V row scales into the probabilities (relative to the largest one met so far, which
 //     is handled like the running maximum: fp16 holds what is at most 1).
-// The scaled query is brought to below 2^10 and split into two fixed-point terms, an integer and a multiple of 2^-11: one
-// term would shift every logit of a head by a common error of 1e-4, and sums of small integers times small integers
-// stay below 2^22 units, so that the accumulators hold them exactly (the tensor cores cut off what an fp32 accumulator
+// The scaled query is brought to below 2^9 and split into two fixed-point terms, an integer (or sixteenths of one) and a
+// multiple of 2^-11 of it: one term would shift every logit of a head by a common error of 1e-4, and sums of small
+// integers times small integers stay below 2^24 units, so that the accumulators hold them exactly (the tensor cores cut off what an fp32 accumulator
 // cannot hold, which with floating-point terms shifted a head's logits by up to 5e-5).  With at most four heads in the group (kTwice) the two terms of
 // a head are two columns of ONE MMA, h and h + 4, whose results are added by one exchange between lanes: half the MMAs.
 // The exchange leaves a lane one token row instead of two, so that the softmax runs on all 32 lanes where half of them
@@ -44,6 +46,9 @@ __device__ __forceinline__ void mma_f16_free(float (&d)[4], uint32_t a0, uint32_
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+
+// of each half of a word the codes 0 and 1 (jj = 0) or 2 and 3 (jj = 1): one byte, u0 + 16 u1
+__device__ __forceinline__ uint32_t two_codes(uint32_t w, int jj) { return jj == 0 ? w & 0x00ff00ffu : __byte_perm(w, 0u, 0x4341); }
 
 // 16-byte piece `piece` (0 .. 3) of 4-bit row `row` of a tile: two rows of 64 bytes to a 128-byte row, 128-byte swizzle
 __device__ __forceinline__ uint32_t int4_offset(int row, int piece) {
@@ -163,7 +168,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     float v_ref = 0.0f, v_inv = 0.0f;                     // largest V row scale met, what the probabilities are relative to
 
     // ---- query fragments (B operand): head g (kTwice: first terms for g < 4, second terms for g >= 4); registers
-    // j = 0 .. 3 of a group of 32 channels are the nibbles (j, j + 4)
+    // 2 j and 2 j + 1 of a group of 32 channels belong to the operands of codes (2 j, 2 j + 1 | 2 j + 4, 2 j + 5)
     uint32_t qq[D / 8], ql[kTwice ? 1 : D / 8];
     float q_off[2], q_off2[2], q_fac[2];                  // this lane's two columns: offsets of the terms, factor of the logits
     {
@@ -184,28 +189,38 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
         }
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-        // to [2^9, 2^10): a power of two, which the logits are multiplied by again (with the codes' 2^24)
-        const int ex = min(max((int)(__float_as_uint(big) >> 23), 9), 239);      // biased exponent
-        const float up = __uint_as_float((uint32_t)(127 + 9 + 127 - ex) << 23);
-        const float back = __uint_as_float((uint32_t)(ex - 9 + 24) << 23);
-        float sum = 0.0f, sum2 = 0.0f;                     // of the terms: integers, and multiples of 2^-11
+        // to [2^8, 2^9): a power of two, which the logits are multiplied by again (with the codes' 2^24)
+        const int ex = min(max((int)(__float_as_uint(big) >> 23), 9), 238);      // biased exponent
+        const float up = __uint_as_float((uint32_t)(127 + 8 + 127 - ex) << 23);
+        const float back = __uint_as_float((uint32_t)(ex - 8 + 24) << 23);
+        float sum = 0.0f, sum2 = 0.0f;                     // what a code of 1 everywhere gives, of either term (exact)
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float k = (j & 1) ? 0.0625f : 1.0f;      // odd nibbles stand 16 times higher
-                const float a = x[8 * c + j] * up, b = x[8 * c + j + 4] * up;
-                const float a1 = rintf(a), b1 = rintf(b);
-                const float a2 = rintf((a - a1) * 2048.0f) * 0x1p-11f, b2 = rintf((b - b1) * 2048.0f) * 0x1p-11f;
-                const uint32_t hi = pack_f16(a1 * k, b1 * k), lo = pack_f16(a2 * k, b2 * k);     // (exact)
-                if (kTwice) {
-                    qq[4 * c + j] = g8 < 4 ? hi : lo;
-                } else {
-                    qq[4 * c + j] = hi;
-                    ql[4 * c + j] = lo;
+            for (int j = 0; j < 2; ++j) {                  // codes (2 j, 2 j + 1) and (2 j + 4, 2 j + 5) of the word
+                float f1[2][2], f2[2][2];                  // the terms, [low or high half][operand u0 or u0 + 16 u1]
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float q0 = x[8 * c + 2 * j + 4 * h] * up, q1 = x[8 * c + 2 * j + 4 * h + 1] * up;
+                    const float b1 = rintf(q1), b2 = rintf((q1 - b1) * 2048.0f) * 0x1p-11f;
+                    f1[h][1] = b1 * 0.0625f;
+                    f2[h][1] = b2 * 0.0625f;
+                    const float q = q0 - (f1[h][1] + f2[h][1]);
+                    f1[h][0] = rintf(q);
+                    f2[h][0] = rintf((q - f1[h][0]) * 2048.0f) * 0x1p-11f;
+                    sum += fmaf(17.0f, f1[h][1], f1[h][0]);
+                    sum2 += fmaf(17.0f, f2[h][1], f2[h][0]);
                 }
-                sum += a1 + b1;
-                sum2 += a2 + b2;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t hi = pack_f16(f1[0][i], f1[1][i]), lo = pack_f16(f2[0][i], f2[1][i]);     // (exact)
+                    if (kTwice) {
+                        qq[4 * c + 2 * j + i] = g8 < 4 ? hi : lo;
+                    } else {
+                        qq[4 * c + 2 * j + i] = hi;
+                        ql[4 * c + 2 * j + i] = lo;
+                    }
+                }
             }
         if (kTwice && g8 >= 4) sum = sum2;                 // this lane's column
         sum2 += __shfl_xor_sync(0xffffffffu, sum2, 1);
@@ -296,15 +311,15 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
 #pragma unroll
             for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-                for (int jj = 0; jj < 2; ++jj) {           // nibbles (0, 4 | 1, 5), then (2, 6 | 3, 7)
+                for (int jj = 0; jj < 2; ++jj) {           // codes (0, 1 | 4, 5) of the words, then (2, 3 | 6, 7)
                     const int at = 4 * c + 2 * jj;
 #pragma unroll
                     for (int term = 0; term < (kTwice ? 1 : 2); ++term)
 #pragma unroll
                         for (int blk = 0; blk < kBlocks; ++blk) {
-                            const uint32_t lo = kb[blk][c >> 1][2 * (c & 1)] >> (8 * jj), hi = kb[blk][c >> 1][2 * (c & 1) + 1] >> (8 * jj);
+                            const uint32_t lo = two_codes(kb[blk][c >> 1][2 * (c & 1)], jj), hi = two_codes(kb[blk][c >> 1][2 * (c & 1) + 1], jj);
                             const uint32_t* b = term ? ql : qq;
-                            mma_f16_free(term ? st2[kTwice ? 0 : blk] : st[blk], lo & 0x000f000fu, hi & 0x000f000fu, lo & 0x00f000f0u, hi & 0x00f000f0u,
+                            mma_f16_free(term ? st2[kTwice ? 0 : blk] : st[blk], lo & 0x000f000fu, hi & 0x000f000fu, lo, hi,
                                          b[at], b[at + 1]);
                         }
                 }
@@ -413,19 +428,18 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
                 }
             }
             // ---- O^T += V^T P^T: a register of the transposed load = two tokens x four adjacent channels; row g of MMA jj
-            // is channel 4 g + 2 jj of the 32-channel group, row g + 8 channel 4 g + 2 jj + 1 (16 times too large)
+            // is channel 4 g + 2 jj of the 32-channel group, row g + 8 that plus 16 times channel 4 g + 2 jj + 1
 #pragma unroll
             for (int blk = 0; blk < kBlocks; ++blk) {
                 if (blk + 1 < kBlocks) load_vb(blk + 1);
-                mma_f16_free(o8, 0x00080008u, 0x00800080u, 0x00080008u, 0x00800080u, pb[blk][0], pb[blk][1]);
+                mma_f16_free(o8, 0x00080008u, 0x00880088u, 0x00080008u, 0x00880088u, pb[blk][0], pb[blk][1]);
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c)
 #pragma unroll
                     for (int jj = 0; jj < 2; ++jj) {
-                        const uint32_t lo = vb[blk & 1][c >> 1][2 * (c & 1)] >> (8 * jj);            // tokens 0-7 of the block
-                        const uint32_t hi = vb[blk & 1][c >> 1][2 * (c & 1) + 1] >> (8 * jj);        // tokens 8-15
-                        mma_f16_full(o[2 * c + jj], lo & 0x000f000fu, lo & 0x00f000f0u, hi & 0x000f000fu, hi & 0x00f000f0u,
-                                     pb[blk][0], pb[blk][1]);
+                        const uint32_t lo = two_codes(vb[blk & 1][c >> 1][2 * (c & 1)], jj);         // tokens 0-7 of the block
+                        const uint32_t hi = two_codes(vb[blk & 1][c >> 1][2 * (c & 1) + 1], jj);     // tokens 8-15
+                        mma_f16_full(o[2 * c + jj], lo & 0x000f000fu, lo, hi & 0x000f000fu, hi, pb[blk][0], pb[blk][1]);
                     }
             }
             __syncwarp();                                  // the tile has been read (the volatile MMAs above have their operands)
@@ -489,8 +503,8 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
                     const int ch = 32 * (c >> 1) + 4 * g8 + 2 * (c & 1);
-                    *reinterpret_cast<float2*>(dst + ch) = make_float2((o[c][e] - o8[e]) * 0x1p24f * v_ref,
-                                                                       (o[c][2 + e] - o8[2 + e]) * 0x1p20f * v_ref);
+                    const float even = o[c][e] - o8[e], both = o[c][2 + e] - o8[2 + e];
+                    *reinterpret_cast<float2*>(dst + ch) = make_float2(even * 0x1p24f * v_ref, (both - even) * 0x1p20f * v_ref);
                 }
                 if (g8 == 0) { sm_m[warp][head] = m_run[e]; sm_l[warp][head] = l_run[e]; }
             }

@@ -186,7 +186,7 @@ def attend(sh, cache, cap, stride, q, chunk=0):
 
 def check_direct(lens, G, setup, out, lse):
     """Bound of an output: the probability times V scale is rounded to fp16 (2^-12 of itself, 2^-11 with the products
-    around it; below the normal range 2^-25 of the largest V scale per row).  The scaled query is held to 2^-21 of its
+    around it; below the normal range 2^-25 of the largest V scale per row).  The scaled query is held to 2^-20 of its
     largest element per channel, which a code of up to 7 multiplies (sums of the terms are exact), and a logit has a
     few fp32 factors: 2^-19 of sum 15 |q c| s / sqrt(D) covers them.  The sums over the rows of 16 p s c go in steps of
     16 rows (2^-23 each); the result is rounded once to bf16 (2^-8)."""
@@ -204,7 +204,7 @@ def check_direct(lens, G, setup, out, lse):
             l = p.sum()
             ref, ref_lse = p @ V / l, m + np.log(l)
             qc = np.abs(qv * four[0, h, 0])
-            e = (2.0 ** -19 * 15 * qc.sum() + 2.0 ** -21 * D * 7 * qc.max()) * np.abs(scale[rows, 0]).max() / np.sqrt(D) + 2.0 ** -21
+            e = (2.0 ** -19 * 15 * qc.sum() + 2.0 ** -20 * D * 7 * qc.max()) * np.abs(scale[rows, 0]).max() / np.sqrt(D) + 2.0 ** -21
             span = np.abs(scale[rows, 1]).astype(np.float64)
             bound = ((2.0 ** -11 + 2 * e) * (p @ np.abs(V)) / l
                      + (n / 16 + 40) * 2.0 ** -23 * 16 * (p @ span) / l * four[0, h, 2]
