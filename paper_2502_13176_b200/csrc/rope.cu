@@ -42,7 +42,6 @@ struct RopeParams {
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ f32x2 neg2(f32x2 v) { return v ^ 0x8000000080000000ull; }
 __device__ __forceinline__ f32x2 swap2(f32x2 v) {
     const float2 f = unpack2(v);
     return pack2(f.y, f.x);
@@ -62,12 +61,6 @@ __device__ __forceinline__ uint4 narrow(const f32x2 (&f)[4]) {  // the only roun
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// four pairs from shared memory (32 bytes)
-__device__ __forceinline__ void load4(const float* from, f32x2 (&f)[4]) {
-    const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(from), y = *reinterpret_cast<const ulonglong2*>(from + 4);
-    f[0] = x.x; f[1] = x.y; f[2] = y.x; f[3] = y.y;
-}
-
 // kTok tokens per CTA, a power of two.  Thread = (row group, lane of the group); a group keeps its token and walks
 // over the heads.
 template <int D, bool kInterleaved, int kTok>
@@ -77,7 +70,8 @@ __global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_kernel(const RopePar
     constexpr int kHeadStep = kGroups / kTok;        // heads worked on at the same time
     // cosine and sine of the pairs
     __shared__ __align__(16) float t_cos[kTok][D / 2], t_sin[kTok][D / 2];
-    __shared__ __align__(16) float wt[2][D];         // the norms' weights
+    // the norms' weights, first and second half of every piece apart (lanes side by side read banks side by side)
+    __shared__ __align__(16) float wt[2][2][D / 8][4];
     __shared__ uint4 ring[kAhead + 1][2][kThreads];  // every thread's two pieces of the rows ahead
     const int tid = threadIdx.x;
     const uint32_t n0 = blockIdx.x * kTok;           // (tokens are counted in 31 bits)
@@ -90,22 +84,22 @@ __global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_kernel(const RopePar
     const int pairs = p.rot >> 4;                    // lanes that hold rotated pieces
     const bool rotates = lane < pairs;
     const int pa = rotates ? lane : 2 * lane, pb = rotates ? lane + pairs : 2 * lane + 1;
-    const __nv_bfloat16* src[2];
-    __nv_bfloat16* dst[2];
-#pragma unroll
-    for (int op = 0; op < 2; ++op) {
-        src[op] = p.in[op] + b * p.si[op].seq + t * p.si[op].token;
-        dst[op] = p.out[op] + b * p.so[op].seq + t * p.so[op].token;
-    }
-    const int n_heads = p.heads[0] + p.heads[1];     // query heads, then key heads
-    const int n_rows = (n_heads + kHeadStep - 1) / kHeadStep;       // rows of this thread's group, some past the last head
-    auto fetch = [&](int i) {                        // into this thread's own slots: nobody else reads them
-        const int h = i * kHeadStep + grp / kTok;
-        const bool row = exists && h < n_heads;
-        const __nv_bfloat16* from = !row ? p.in[0] : h < p.heads[0] ? src[0] + h * p.si[0].head : src[1] + (h - p.heads[0]) * p.si[1].head;
-        const int s = i % (kAhead + 1);
-        copy16(smem_u32(&ring[s][0][tid]), reinterpret_cast<const uint4*>(from) + pa, row);
-        copy16(smem_u32(&ring[s][1][tid]), reinterpret_cast<const uint4*>(from) + pb, row);
+    // this group's rows: n_q query heads, then n_k key heads, kHeadStep apart (the last of either may lie past the heads)
+    const int sub = grp / kTok;
+    const int n_q = (p.heads[0] + kHeadStep - 1) / kHeadStep, n_rows = n_q + (p.heads[1] + kHeadStep - 1) / kHeadStep;
+    const __nv_bfloat16* from = p.in[0] + b * p.si[0].seq + t * p.si[0].token + sub * p.si[0].head;
+    int64_t from_step = kHeadStep * p.si[0].head;
+    auto fetch = [&](int i) {                        // rows in order, into this thread's own slots: nobody else reads them
+        if (i == n_q) {
+            from = p.in[1] + b * p.si[1].seq + t * p.si[1].token + sub * p.si[1].head;
+            from_step = kHeadStep * p.si[1].head;
+        }
+        const bool row = exists && (i < n_q ? i * kHeadStep + sub < p.heads[0] : (i - n_q) * kHeadStep + sub < p.heads[1]);
+        const uint4* at = reinterpret_cast<const uint4*>(row ? from : p.in[0]);
+        const uint32_t slot = smem_u32(&ring[i % (kAhead + 1)][0][tid]);
+        copy16(slot, at + pa, row);
+        copy16(slot + sizeof(uint4) * kThreads, at + pb, row);
+        from += from_step;
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
@@ -126,7 +120,7 @@ __global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_kernel(const RopePar
     }
     for (int i = tid; i < 2 * D; i += kThreads) {
         const __nv_bfloat16* w = p.w[i / D];
-        if (w) wt[i / D][i % D] = __bfloat162float(w[i % D]);
+        if (w) wt[i / D][i % 8 / 4][i % D / 8][i % 4] = __bfloat162float(w[i % D]);
     }
     __syncthreads();
     const bool on = exists && p.pos[n] >= 0;         // a negative position: the token sits out
@@ -149,35 +143,47 @@ __global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_kernel(const RopePar
             }
         }
     }
+    const f32x2 minus = pack2(-1.0f, -1.0f);
+    __nv_bfloat16* to = p.out[0] + b * p.so[0].seq + t * p.so[0].token + sub * p.so[0].head;
+    int64_t to_step = kHeadStep * p.so[0].head;
+    bool norm = p.w[0] != nullptr;
+    int op = 0, h = sub;
 #pragma unroll 1
     for (int i = 0; i < n_rows; ++i) {
         if (i + kAhead < n_rows) fetch(i + kAhead);
         asm volatile("cp.async.commit_group;" ::: "memory");
         asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
-        const int h = i * kHeadStep + grp / kTok;
-        const bool key = h >= p.heads[0];
+        if (i == n_q) {
+            to = p.out[1] + b * p.so[1].seq + t * p.so[1].token + sub * p.so[1].head;
+            to_step = kHeadStep * p.so[1].head;
+            norm = p.w[1] != nullptr;
+            op = 1;
+            h = sub;
+        }
         f32x2 a[4], c[4];
         widen(ring[i % (kAhead + 1)][0][tid], a);
         widen(ring[i % (kAhead + 1)][1][tid], c);
-        f32x2 s2 = mul2(a[0], a[0]);
+        if (norm) {
+            f32x2 s2 = mul2(a[0], a[0]);
 #pragma unroll
-        for (int e = 1; e < 4; ++e) s2 = fma2(a[e], a[e], s2);
+            for (int e = 1; e < 4; ++e) s2 = fma2(a[e], a[e], s2);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s2 = fma2(c[e], c[e], s2);
-        const float2 s1 = unpack2(s2);
-        float ss = s1.x + s1.y;
+            for (int e = 0; e < 4; ++e) s2 = fma2(c[e], c[e], s2);
+            const float2 s1 = unpack2(s2);
+            float ss = s1.x + s1.y;
 #pragma unroll
-        for (int off = 1; off < kLanes; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-        if (key ? p.w[1] != nullptr : p.w[0] != nullptr) {
-            const float r = 1.0f / sqrtf(ss * (1.0f / D) + p.eps);
+            for (int off = 1; off < kLanes; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+            const float r = rsqrtf(fmaf(ss, 1.0f / D, p.eps));       // (2 units in the last place)
             const f32x2 r2 = pack2(r, r);
-            f32x2 w[4];
-            load4(&wt[key][8 * pa], w);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) a[e] = mul2(mul2(a[e], r2), w[e]);
-            load4(&wt[key][8 * pb], w);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) c[e] = mul2(mul2(c[e], r2), w[e]);
+            for (int half2 = 0; half2 < 2; ++half2) {
+                const ulonglong2 wa = *reinterpret_cast<const ulonglong2*>(wt[op][half2][pa]);
+                const ulonglong2 wb = *reinterpret_cast<const ulonglong2*>(wt[op][half2][pb]);
+                a[2 * half2] = mul2(mul2(a[2 * half2], r2), wa.x);
+                a[2 * half2 + 1] = mul2(mul2(a[2 * half2 + 1], r2), wa.y);
+                c[2 * half2] = mul2(mul2(c[2 * half2], r2), wb.x);
+                c[2 * half2 + 1] = mul2(mul2(c[2 * half2 + 1], r2), wb.y);
+            }
         }
         if (rotates) {
             if (kInterleaved) {                      // partner = the other element of the pair
@@ -190,16 +196,18 @@ __global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_kernel(const RopePar
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const f32x2 u = a[e], v = c[e];
-                    a[e] = fma2(u, cs[e], mul2(v, neg2(sn[e])));
+                    a[e] = fma2(mul2(v, sn[e]), minus, mul2(u, cs[e]));
                     c[e] = fma2(v, cs[e], mul2(u, sn[e]));
                 }
             }
         }
-        if (on && h < n_heads) {
-            uint4* to = reinterpret_cast<uint4*>(key ? dst[1] + (h - p.heads[0]) * p.so[1].head : dst[0] + h * p.so[0].head);
-            to[pa] = narrow(a);
-            to[pb] = narrow(c);
+        if (on && h < p.heads[op]) {
+            uint4* at = reinterpret_cast<uint4*>(to);
+            at[pa] = narrow(a);
+            at[pb] = narrow(c);
         }
+        to += to_step;
+        h += kHeadStep;
     }
 }
 
