@@ -6,6 +6,7 @@ step of the method runs inside the library.  If the library is missing the
 first call raises: there is no other path.
 """
 import ctypes
+import functools
 import os
 from ctypes import POINTER, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 
@@ -127,11 +128,11 @@ def _ptr(t):
     return None if t is None else c_void_p(t.data_ptr())
 
 
-def _stream(stream):
+def _stream(stream, dev=None):
     if stream is not None:
-        return c_void_p(stream.cuda_stream)
+        return stream.cuda_stream
     # the current stream's handle without building a Stream object for it (3 us of a call that launches in 4)
-    return c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if dev is None else dev)
 
 
 def make_shape(L, Hq, Hkv, D, page=16, n_sink=4, recent_num=1, recent_den=2):
@@ -342,22 +343,30 @@ def _elsewhere(t, what, dev):
     raise ValueError("%s is on %s; the current device is cuda:%d" % (what, t.device, dev))
 
 
-def _rows(t, what, dev, seqs, heads, tokens, D):
+@functools.lru_cache(maxsize=256)
+def _strides(st):
+    return Strides(st[0], st[1], st[2])              # (the library only reads it)
+
+
+_BF16 = torch.bfloat16
+
+
+def _rows(t, what, dev, shape):
     """Pointer and strides of a bf16 tensor [seqs, heads, tokens, D] (any view whose last dimension is contiguous)."""
     st = t.stride()
-    if t.dtype != torch.bfloat16 or t.shape != (seqs, heads, tokens, D) or st[3] != 1:
+    if t.dtype is not _BF16 or t.shape != shape or st[3] != 1:
         raise ValueError("%s: expected bf16 [%d, %d, %d, %d] with contiguous rows, got %s %s with strides %s"
-                         % (what, seqs, heads, tokens, D, t.dtype, tuple(t.shape), st))
+                         % ((what,) + shape + (t.dtype, tuple(t.shape), st)))
     if t.get_device() != dev:
         _elsewhere(t, what, dev)
-    return t.data_ptr(), Strides(st[0], st[1], st[2])
+    return t.data_ptr(), _strides(st)
 
 
 def _dense(t, what, dev, dtype, shape):
     """Pointer of a contiguous tensor, NULL for None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: expected a contiguous %s tensor %s, got %s %s" % (what, dtype, shape, t.dtype, tuple(t.shape)))
     if t.get_device() != dev:
         _elsewhere(t, what, dev)
@@ -368,40 +377,44 @@ def baklava_qk_norm_rope(shape, q, k, positions, inv_freq, q_weight, k_weight, e
     """q, q_out: bf16 [B, Hq, T, D], k, k_out: bf16 [B, Hkv, T, D], each any view with contiguous rows; positions: int32
     [B, T]; inv_freq: float32 [rotary_dim / 2]; weights: bf16 [D] or None."""
     B, _, T, D = q.shape
-    Hq, Hkv, dev, n = shape.Hq, shape.Hkv, _device(), inv_freq.numel()
-    _check(lib().baklava_qk_norm_rope(shape, *_rows(q, "q", dev, B, Hq, T, D), *_rows(k, "k", dev, B, Hkv, T, D),
+    dev, n = _device(), inv_freq.numel()
+    queries, keys = (B, shape.Hq, T, D), (B, shape.Hkv, T, D)
+    _check(lib().baklava_qk_norm_rope(shape, *_rows(q, "q", dev, queries), *_rows(k, "k", dev, keys),
                                       _dense(positions, "positions", dev, torch.int32, (B, T)), B, T,
                                       _dense(inv_freq, "inv_freq", dev, torch.float32, (n,)), 2 * n,
-                                      _dense(q_weight, "q_weight", dev, torch.bfloat16, (D,)),
-                                      _dense(k_weight, "k_weight", dev, torch.bfloat16, (D,)), eps, flags,
-                                      *_rows(q_out, "q_out", dev, B, Hq, T, D), *_rows(k_out, "k_out", dev, B, Hkv, T, D),
-                                      _stream(stream)), "baklava_qk_norm_rope")
+                                      _dense(q_weight, "q_weight", dev, _BF16, (D,)),
+                                      _dense(k_weight, "k_weight", dev, _BF16, (D,)), eps, flags,
+                                      *_rows(q_out, "q_out", dev, queries), *_rows(k_out, "k_out", dev, keys),
+                                      _stream(stream, dev)), "baklava_qk_norm_rope")
 
 
 def baklava_prefill_attn(shape, q, k, v, prompt_len, out, lse, status, stream=None):
     """q, out: bf16 [B, Hq, T, D], k, v: bf16 [B, Hkv, T, D], any views with contiguous rows; prompt_len: int32 [B] or None;
     lse: float32 [B, Hq, T] or None; status: int32 [1]."""
     B, _, T, D = q.shape
-    Hq, Hkv, dev = shape.Hq, shape.Hkv, _device()
-    _check(lib().baklava_prefill_attn(shape, *_rows(q, "q", dev, B, Hq, T, D), *_rows(k, "k", dev, B, Hkv, T, D),
-                                      *_rows(v, "v", dev, B, Hkv, T, D), _dense(prompt_len, "prompt_len", dev, torch.int32, (B,)),
-                                      B, T, *_rows(out, "out", dev, B, Hq, T, D),
-                                      _dense(lse, "lse", dev, torch.float32, (B, Hq, T)),
-                                      _dense(status, "status", dev, torch.int32, (1,)), _stream(stream)), "baklava_prefill_attn")
+    dev = _device()
+    queries, keys = (B, shape.Hq, T, D), (B, shape.Hkv, T, D)
+    _check(lib().baklava_prefill_attn(shape, *_rows(q, "q", dev, queries), *_rows(k, "k", dev, keys),
+                                      *_rows(v, "v", dev, keys), _dense(prompt_len, "prompt_len", dev, torch.int32, (B,)),
+                                      B, T, *_rows(out, "out", dev, queries),
+                                      _dense(lse, "lse", dev, torch.float32, queries[:3]),
+                                      _dense(status, "status", dev, torch.int32, (1,)), _stream(stream, dev)),
+           "baklava_prefill_attn")
 
 
 def baklava_prefill_attn_packed(shape, q, k, v, cu_seqlens, max_len, out, lse, status, stream=None):
     """q, out: bf16 [Hq, total, D], k, v: bf16 [Hkv, total, D], any views with contiguous rows; cu_seqlens: int32 [B + 1];
     lse: float32 [Hq, total] or None; status: int32 [1]."""
-    total, D = q.shape[1], shape.D
-    Hq, Hkv, dev, n = shape.Hq, shape.Hkv, _device(), cu_seqlens.numel()
-    _check(lib().baklava_prefill_attn_packed(shape, *_rows(q.unsqueeze(0), "q", dev, 1, Hq, total, D),
-                                             *_rows(k.unsqueeze(0), "k", dev, 1, Hkv, total, D),
-                                             *_rows(v.unsqueeze(0), "v", dev, 1, Hkv, total, D),
+    total, D, Hq = q.shape[1], shape.D, shape.Hq
+    dev, n = _device(), cu_seqlens.numel()
+    queries, keys = (1, Hq, total, D), (1, shape.Hkv, total, D)
+    _check(lib().baklava_prefill_attn_packed(shape, *_rows(q.unsqueeze(0), "q", dev, queries),
+                                             *_rows(k.unsqueeze(0), "k", dev, keys),
+                                             *_rows(v.unsqueeze(0), "v", dev, keys),
                                              _dense(cu_seqlens, "cu_seqlens", dev, torch.int32, (n,)), n - 1, max_len, total,
-                                             *_rows(out.unsqueeze(0), "out", dev, 1, Hq, total, D),
+                                             *_rows(out.unsqueeze(0), "out", dev, queries),
                                              _dense(lse, "lse", dev, torch.float32, (Hq, total)),
-                                             _dense(status, "status", dev, torch.int32, (1,)), _stream(stream)),
+                                             _dense(status, "status", dev, torch.int32, (1,)), _stream(stream, dev)),
            "baklava_prefill_attn_packed")
 
 
