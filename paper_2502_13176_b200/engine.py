@@ -71,8 +71,15 @@ class DecodeSession:
         """One layer of a real prompt: causal attention (its output [B, Hq, T, D] is returned), the attention every token
         received as its score (from the same rows' log-sum-exp), and the bulk eviction into the layer's slabs.
         q: bf16 [B, Hq, T, D], k, v: bf16 [B, Hkv, T, D], contiguous; prompt_len: device int32 [B] or None."""
-        B, T = q.shape[0], q.shape[2]
         w = self.w
+        B, T = w.B, q.shape[2]
+        if not 0 <= l < w.L:
+            raise ValueError("layer %d of %d" % (l, w.L))
+        for what, x, heads in (("q", q, w.Hq), ("k", k, w.Hkv), ("v", v, w.Hkv)):
+            # (attention takes any strides; the scores and the eviction read the same tensors densely)
+            if x.shape != (B, heads, T, w.D) or not x.is_contiguous():
+                raise ValueError("%s: expected a contiguous [%d, %d, %d, %d], got %s with strides %s"
+                                 % (what, B, heads, T, w.D, tuple(x.shape), x.stride()))
         out = torch.zeros(q.shape, dtype=q.dtype, device=self.device)
         lse = torch.empty((B, w.Hq, T), dtype=torch.float32, device=self.device)
         bk.baklava_prefill_attn(self.shape, q, k, v, prompt_len, out, lse, self.cache.status)
@@ -80,7 +87,8 @@ class DecodeSession:
         ws = torch.empty((max(bk.baklava_prefill_workspace_size(self.shape, B, T),
                               bk.baklava_evict_workspace_size(self.shape, B, 1, T)),), dtype=torch.uint8, device=self.device)
         bk.baklava_prefill_scores(self.shape, q, k, prompt_len, B, T, score, ws, lse=lse)
-        self.prompt_error = ws[:4].view(torch.int32).clone()          # (the eviction uses the workspace next)
+        err = ws[:4].view(torch.int32).clone()                        # (the eviction uses the workspace next)
+        self.prompt_error = err if self.prompt_error is None else self.prompt_error | err
         bk.baklava_evict_varlen(self.shape, self.cache, l, l + 1, k, v, score, T, prompt_len, 0, w.Hkv * T, T, 1, ws)
         self.t = T
         self.t_seq = prompt_len

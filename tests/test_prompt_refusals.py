@@ -1,12 +1,14 @@
 """CPU tests of the argument checks of the prompt-side attention calls: refused before anything touches a device (the
 pointers are never dereferenced)."""
 import ctypes
+from types import SimpleNamespace
 
 import pytest
 import torch
 
 from paper_2502_13176_b200 import binding as bk
 from paper_2502_13176_b200 import build as bkbuild
+from paper_2502_13176_b200 import engine
 
 INVALID, SHAPE, UNSUPPORTED = -1, -2, -7
 
@@ -88,3 +90,46 @@ def test_binding_refuses_other_types_shapes_and_devices():
     if not torch.cuda.is_available():
         with pytest.raises((ValueError, RuntimeError, AssertionError)):      # host tensors
             bk.baklava_prefill_attn(sh, good, kv, kv, None, good, None, status)
+
+
+def session(monkeypatch, scores=lambda ws: None):
+    """A session of two sequences whose calls into the library do nothing but what `scores` does to the workspace."""
+    sess = engine.DecodeSession.__new__(engine.DecodeSession)
+    sess.w = SimpleNamespace(B=2, L=2, Hq=4, Hkv=2, D=64)
+    sess.shape, sess.device, sess.prompt_error = None, "cpu", None
+    sess.cache = SimpleNamespace(status=torch.zeros(1, dtype=torch.int32))
+    calls = []
+    for name in ("baklava_prefill_attn", "baklava_evict_varlen"):
+        monkeypatch.setattr(bk, name, lambda *a, **kw: calls.append(a))
+    for name in ("baklava_prefill_workspace_size", "baklava_evict_workspace_size"):
+        monkeypatch.setattr(bk, name, lambda *a: 256)
+    monkeypatch.setattr(bk, "baklava_prefill_scores", lambda *a, **kw: scores(a[7]))
+    return sess, calls
+
+
+def prompt(B=2, T=8):
+    return [torch.zeros((B, h, T, 64), dtype=torch.bfloat16) for h in (4, 2, 2)]
+
+
+def test_session_prompt_refuses_other_batches_and_layouts(monkeypatch):
+    # the scores and the eviction read the prompt's tensors densely, for as many sequences as the cache has
+    sess, calls = session(monkeypatch)
+    q, k, v = prompt()
+    sess.prefill_layer(1, q, k, v)
+    assert len(calls) == 2
+    wide = torch.zeros((2, 8, 8, 64), dtype=torch.bfloat16).transpose(1, 2)
+    for bad in ((0, *prompt(B=1)), (0, *prompt(B=3)), (0, q, k, prompt(T=9)[2]), (0, q, k[:, :1], v), (0, wide[:, :4], k, v),
+                (0, q, wide[:, :2], v), (0, q, k, wide[:, :2]), (2, q, k, v), (-1, q, k, v)):
+        with pytest.raises(ValueError):
+            sess.prefill_layer(*bad)
+    assert len(calls) == 2
+
+
+@pytest.mark.parametrize("bad_layer", [0, 1])
+def test_session_keeps_the_error_of_every_layer(monkeypatch, bad_layer):
+    layer = [0]
+    sess, _ = session(monkeypatch, lambda ws: ws[:4].view(torch.int32).fill_(int(layer[0] == bad_layer)))
+    for layer[0] in range(2):
+        sess.prefill_layer(layer[0], *prompt())
+    with pytest.raises(RuntimeError, match="prompt scores"):
+        sess.check_status()
