@@ -5,10 +5,14 @@
 //
 // Bound: HBM (4 bytes per element moved, about ten fp32 operations), or the launch when there are few tokens.  A
 // head row belongs to D / 16 lanes, each with two 16-byte pieces chosen so that both members of every rotated pair
-// sit in one lane: no shuffle but the norm's sum.  A CTA takes `tok` consecutive tokens and all their heads, and
+// sit in one lane: no shuffle but the norm's sum.  A CTA takes some consecutive tokens and all their heads, and
 // the angles of its tokens are computed once, into shared memory: the product and the reduction to one turn in
 // fp64 (a position of 2^30 times a frequency near 1 keeps 1e-7 of a turn; fp32 would keep none), the sine and
-// cosine of the remainder in fp32.
+// cosine of the remainder in fp32.  Every thread has the pieces of its next three rows on their way into shared memory
+// (rows in registers, four at a time, took 212 us where this takes 109).
+//
+// Measured: 32 768 tokens of 32 + 8 heads of 128, 671 MB: 108.8 us = 6.17 TB/s = 94 % of the copy bandwidth; 5 001 tokens
+// of 12 + 4 heads of 64, 20.5 MB: 7.7 us; one token: 3.6 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -211,14 +215,30 @@ __global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_kernel(const RopePar
     }
 }
 
+template <int D, bool kInterleaved, int kTok>
+void launch_tokens(const RopeParams& p, cudaStream_t s) {
+    qk_norm_rope_kernel<D, kInterleaved, kTok><<<(p.tokens + kTok - 1) / kTok, kThreads, 0, s>>>(p);
+}
+
 template <int D, bool kInterleaved>
 cudaError_t launch(const RopeParams& p, cudaStream_t s) {
-    // Eight tokens per CTA share the angles' work and write 8 rows of a head side by side; with few tokens one per
-    // CTA spreads the heads over more of the GPU.
-    if (p.tokens >= 8 * 148 * 4)
-        qk_norm_rope_kernel<D, kInterleaved, 8><<<(p.tokens + 7) / 8, kThreads, 0, s>>>(p);
-    else
-        qk_norm_rope_kernel<D, kInterleaved, 1><<<p.tokens, kThreads, 0, s>>>(p);
+    // Tokens per CTA: the fewest with which two CTAs per SM take all of them, so that few tokens spread over the GPU (a
+    // CTA's rows follow one another: 32 + 8 heads of 128, 16 tokens: 4.0 us with one token per CTA, 8.1 with eight), up to
+    // eight, which share a CTA's start and angles and write eight rows of a head side by side (2 368 tokens: 19.1 us with
+    // one, 12.3 with eight; 18 944: 117, 65 and, with sixteen, 72 us).  Sixteen where eight leave a thread six rows or
+    // fewer, too little beside a CTA's start (12 + 4 heads of 64, 18 944 tokens: 24.9 us with eight, 18.6 with sixteen).
+    constexpr int kStep8 = kThreads / (D / 16) / 8;
+    const int rows8 = (p.heads[0] + kStep8 - 1) / kStep8 + (p.heads[1] + kStep8 - 1) / kStep8;
+    const uint32_t most = rows8 <= 6 ? 16 : 8;
+    uint32_t tok = 1;
+    while (tok < most && (p.tokens + tok - 1) / tok > 2 * 148) tok *= 2;
+    switch (tok) {
+        case 1: launch_tokens<D, kInterleaved, 1>(p, s); break;
+        case 2: launch_tokens<D, kInterleaved, 2>(p, s); break;
+        case 4: launch_tokens<D, kInterleaved, 4>(p, s); break;
+        case 8: launch_tokens<D, kInterleaved, 8>(p, s); break;
+        default: launch_tokens<D, kInterleaved, 16>(p, s); break;
+    }
     return cudaGetLastError();
 }
 

@@ -68,14 +68,27 @@ CASES = [
     dict(B=2, T=37, Hq=6, Hkv=2, D=64, rot=32, norm=False, il=True),
     dict(B=2, T=37, Hq=6, Hkv=3, D=128, rot=96, norm=True, il=False, far=1000),
     dict(B=1, T=200, Hq=5, Hkv=5, D=64, rot=16, norm=True, il=False, far=2 ** 31 - 1 - 300),
-    dict(B=3, T=1701, Hq=3, Hkv=1, D=128, rot=128, norm=False, il=False),     # the form with eight tokens per CTA,
-    dict(B=3, T=1701, Hq=9, Hkv=3, D=64, rot=48, norm=True, il=True),         #   the last of them ragged
+    dict(B=3, T=1701, Hq=3, Hkv=1, D=128, rot=128, norm=False, il=False),     # many tokens per CTA,
+    dict(B=3, T=1701, Hq=9, Hkv=3, D=64, rot=48, norm=True, il=True),         #   the last CTA's not all there
 ]
 
 
 @pytest.mark.parametrize("c", CASES)
 def test_matches_the_oracle_from_projection_slices_to_head_major(c):
     q, k, pos, freq, qw, kw = inputs(c["B"], c["T"], c["Hq"], c["Hkv"], c["D"], c["rot"], c["norm"], c.get("far", 0))
+    qo, ko = (torch.zeros(x.shape, dtype=torch.bfloat16, device="cuda") for x in (q, k))
+    call(c, q, k, pos, freq, qw, kw, qo, ko)
+    check(qo, q, pos, freq, qw, c["il"], "q")
+    check(ko, k, pos, freq, kw, c["il"], "k")
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 2, 1), (128, 18, 6)])
+@pytest.mark.parametrize("B,T", [(1, 296), (1, 297), (2, 296), (1, 593), (2, 592), (5, 237), (1, 2367), (3, 791)])
+def test_every_number_of_tokens_per_cta(B, T, D, Hq, Hkv):
+    # the numbers change behind 296, 592, 1 184 and 2 368 tokens (few heads go on to sixteen); ragged ends, sequences that
+    # end inside a CTA's tokens
+    c = dict(il=T % 2 == 0)
+    q, k, pos, freq, qw, kw = inputs(B, T, Hq, Hkv, D, D, True, seed=T)
     qo, ko = (torch.zeros(x.shape, dtype=torch.bfloat16, device="cuda") for x in (q, k))
     call(c, q, k, pos, freq, qw, kw, qo, ko)
     check(qo, q, pos, freq, qw, c["il"], "q")
