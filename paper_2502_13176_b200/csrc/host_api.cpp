@@ -1,6 +1,7 @@
 // Host-side entry points: error names, Algorithm 1 step 2, Algorithm 2, and the decode work plan.
 // Nothing here touches the device.
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <cstring>
 #include <numeric>
@@ -232,27 +233,40 @@ extern "C" __attribute__((visibility("default"))) int baklava_decode_plan(const 
         min_chunk = wide * kMinChunk;
         target = (wide * tokens / (2 * slots) + kTile - 1) / kTile * kTile;
         target = std::max<int64_t>(kMinChunk, std::min<int64_t>(target, wide * 4096));
-        if (kv_dtype == BAKLAVA_KV_INT4 && target > kMinChunk) {
+        if (kv_dtype == BAKLAVA_KV_INT4) {
             // 4-bit rows: what a chunk costs besides its rows (start, merge: 10 us, as long as 2500 rows take) outweighs
-            // what a graded list gains at the launch's end.  Equal chunks, the shortest with which the launch is two full
-            // waves (Llama-shaped step 66 us, graded list 70 us; one wave of 8192-token chunks 75 us).
+            // what a graded list gains at the launch's end (Llama-shaped step 66 us, graded list 70 us).  Equal chunks,
+            // the shortest with which they are one full wave of CTAs or two.
             guided = false;
-            for (target = 2 * kMinChunk; target < 8192; target += kTile) {
-                int64_t count = 0, most = 0;
-                for (int i : heads) {
-                    const int64_t pieces = pieces_of(cap[(size_t)layer_begin * Hkv + i], target);
-                    count += pieces * B;
-                    most = std::max(most, pieces);
+            const int64_t g = shape->Hq / shape->Hkv, longest = cap[(size_t)layer_begin * Hkv + heads[0]];
+            // one CTA merges a head's chunks, 16 ns for each chunk and query head, while a row costs 4 ns of a chunk: of n
+            // rows in chunks of c the sum of 16 g n / c and 4 c is least here (23 000 rows a head, g = 8: 28 us with
+            // chunks of 512, 22 us)
+            const int64_t shortest = std::max<int64_t>(2 * kMinChunk, (int64_t)(2.0 * std::sqrt((double)(longest * g))) / kTile * kTile);
+            auto chunks_for = [&](int64_t waves) {
+                int64_t len = shortest;
+                for (; len < 8192; len += kTile) {
+                    int64_t count = 0, most = 0;
+                    for (int i : heads) {
+                        const int64_t pieces = pieces_of(cap[(size_t)layer_begin * Hkv + i], len);
+                        count += pieces * B;
+                        most = std::max(most, pieces);
+                    }
+                    if (count <= waves * slots && most * g <= max_merge_entries(shape->D)) break;
                 }
-                if (count <= 2 * slots && most * (shape->Hq / Hkv) <= max_merge_entries(shape->D)) break;
-            }
+                return len;
+            };
+            // One wave pays a chunk's start and end once (Llama-shaped layers, chunks of 1792: 26 us, two waves of 832:
+            // 33 us; 6080 and 2944: 65 and 69 us) unless heads of few pieces leave it far from full (step: 71 us with 8320,
+            // 66 us with 3328).  In ragged batches, whose sequences hold less than their capacities, chunks that turn out
+            // empty leave a single wave's places idle, which costs most with the larger groups' slower rows
+            // (g = 7: 30 us with 1728, 26 us with 832; 46 and 33 us with 3456 and 1728; g = 4: 48 and 49 us with 4608, 2176).
+            const int64_t one = chunks_for(1), two = chunks_for(2);
+            target = one <= 2 * two + 512 && one <= (g <= 4 ? 5120 : 2048) ? one : two;
         } else if (target == kMinChunk) {
             // A short launch (one layer of a model): nothing balances a second, partly filled wave, so all chunks
             // get the same length, the shortest (from the minimum up) with which every chunk is resident at once.
-            // (4-bit rows: from twice the minimum; what a chunk costs besides its rows is most of it then, 16.4 us
-            // against 19 us for a layer of 78 000 rows)
             guided = false;
-            if (kv_dtype == BAKLAVA_KV_INT4) target = 2 * kMinChunk;
             for (; target < 4096; target += kTile) {
                 int64_t count = 0;
                 for (int i : heads) count += pieces_of(cap[(size_t)layer_begin * Hkv + i], target) * B;
@@ -303,9 +317,20 @@ extern "C" __attribute__((visibility("default"))) int baklava_decode_plan(const 
     if (n_items > INT32_MAX) return BAKLAVA_ERR_UNSUPPORTED;
     // A launch whose chunks are all resident at once ends with its few longest heads; the plan then also lists
     // pieces of the heads for a score / eviction pass that runs as a kernel of its own (about two per SM).
-    const bool short_launch = n_sm > 0 && n_items <= (int64_t)n_sm * kCtasPerSm;
-    if (short_launch) {
-        const int64_t len = std::min<int64_t>(kScoreChunk, std::max<int64_t>(kMinChunk, (tokens / (2 * (int64_t)n_sm) + kTile - 1) / kTile * kTile));
+    const int64_t longest = cap[(size_t)layer_begin * Hkv + heads[0]], g = shape->Hq / shape->Hkv;
+    bool pieces_follow = n_sm > 0 && n_items <= (int64_t)n_sm * kCtasPerSm;
+    if (n_sm > 0 && kv_dtype == BAKLAVA_KV_INT4) {
+        // With 4-bit rows the pass decides more.  One CTA takes 0.21 ns for each row and query head of the longest head,
+        // which in a single wave follows the attention and in longer launches half of it; the pass takes 8 us and 13 ns
+        // for every thousand rows of the launch.  (One wave, 621 000 rows, g = 4: longest head 34 080 rows 44 us with the
+        // pass and 58 us without; 12 752 rows 44 and 39 us.  Two waves: the Llama-shaped step 114 and 94 us; g = 4, heads up
+        // to 180 768 of 3 552 000 rows 148 and 248 us.)
+        pieces_follow = longest * g > (pieces_follow ? 24000 + tokens / 16 : 38000 + tokens / 8);
+    }
+    if (pieces_follow) {
+        int64_t len = std::min<int64_t>(kScoreChunk, std::max<int64_t>(kMinChunk, (tokens / (2 * (int64_t)n_sm) + kTile - 1) / kTile * kTile));
+        const int64_t most = max_merge_entries(shape->D) / g;
+        len = std::max(len, (longest + most - 1) / most);  // (no more pieces of a head than its merge has room for)
         rc = emit(len, false, &n_score);
         if (rc) return rc;
     }

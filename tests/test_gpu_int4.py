@@ -76,6 +76,24 @@ def test_filling_from_empty_then_evicting():
         s.step(i)
 
 
+LONG = wl.scaled(W4, L=1, Hq=16, Hkv=2, T=8192, budget=0.6)
+
+
+@pytest.mark.parametrize("w,chunk,waves", [(LONG, 0, 1), (LONG, 64, 1), (wl.scaled(W4, L=1, Hq=8, Hkv=1, T=36000, budget=0.9), 64, 2)],
+                         ids=["one wave", "short chunks", "two waves"])
+def test_long_heads_end_in_a_kernel_of_their_own(w, chunk, waves):
+    s = Session4(w, chunk_tokens=chunk)
+    assert s.plan.info.n_score_items > 0 and (s.plan.info.n_items > 444) == (waves == 2)
+    for i in range(3):
+        s.step(i)
+
+
+def test_a_lost_wait_before_the_kernel_of_its_own():
+    s = Session4(LONG, chunk_tokens=512)
+    assert s.plan.info.n_score_items > 0
+    lost_step(s, LONG, 0)
+
+
 @pytest.mark.parametrize("Hq,Hkv", [(2, 2), (10, 2), (14, 2), (16, 2)])
 def test_groups_and_batch(Hq, Hkv):
     w = wl.scaled(W4, Hq=Hq, Hkv=Hkv, B=3, T=256)
@@ -283,6 +301,10 @@ def test_a_wait_that_runs_out_loses_the_step_and_nothing_else(flags):
     w = wl.scaled(wl.LLAMA3_8B_32K, L=2, T=3000, steps=4)
     chunk = 256 if flags != bk.FLAG_NO_SCORE else 8192     # (heads of one chunk write their own output)
     s = Session4(w, chunk_tokens=chunk)
+    lost_step(s, w, flags)
+
+
+def lost_step(s, w, flags):
     s.step(0)
     state = [t.clone() for t in (s.cache.len, s.cache.free_slot, s.cache.score)]
     q, kn, vn = wl.decode_inputs(w, 1, s.scales, "cuda")
