@@ -518,16 +518,16 @@ def main():
     if args.sustain_seconds > 0:
         est = max(elapsed_ms / args.steps, 1e-3)
         n_sus = int(args.sustain_seconds * 1e3 / est) + 1
-        sv = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        ends = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
         with ClockSampler(local) as sus_clocks:
             s_open = time.perf_counter()
-            sv[0].record()
+            ends[0].record()
             for i in range(n_sus):
                 sess.step(*feeds[i % total], flags=step_flags)
-            sv[1].record()
+            ends[1].record()
             torch.cuda.synchronize(dev)
             s_close = time.perf_counter()
-        sus_ms = sv[0].elapsed_time(sv[1])
+        sus_ms = ends[0].elapsed_time(ends[1])
         sustained = {"steps": n_sus, "seconds": sus_ms * 1e-3, "ms_per_step": sus_ms / n_sus,
                      "clocks": sus_clocks.summary(s_open, s_close)}
         sess.check_status()
