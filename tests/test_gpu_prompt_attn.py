@@ -267,3 +267,61 @@ def test_two_streams_and_a_captured_graph():
         torch.cuda.synchronize()
         assert torch.equal(o, out) and torch.equal(l, lse)
     assert int(status.item()) == 0
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv", [(2, 1), (6, 2), (14, 2), (8, 1), (20, 4)])
+@pytest.mark.parametrize("T", [1, 2, 8, 9, 16, 17, 32, 33, 63, 64])
+def test_short_prompts_share_a_tile_among_the_heads_of_a_group(D, Hq, Hkv, T):
+    lens = [T, 0, (T + 1) // 2, T]
+    q, k, v = make(4, T, Hq, Hkv, D, seed=T + Hq)
+    for b, n in enumerate(lens):
+        for x in (q, k, v):
+            x[b, :, n:] = float("nan")
+    out, lse = run(q, k, v, lens)
+    check_padded(q, k, v, out, lse, lens)
+
+
+@pytest.mark.parametrize("D,T", [(64, 20), (128, 7), (128, 50)])
+def test_many_short_packed_prompts(D, T):
+    # more row blocks than places for CTAs: they go on from one to another
+    rng = np.random.default_rng(T)
+    lens = rng.integers(0, T + 1, 200)
+    Hq, Hkv, total = 15, 5, int(lens.sum()) + 3
+    g = torch.Generator(device="cuda").manual_seed(T)
+    heads = torch.randn((total, Hq + 2 * Hkv, D), generator=g, device="cuda").bfloat16().transpose(0, 1)
+    q, k, v = heads[:Hq], heads[Hq:Hq + Hkv], heads[Hq + Hkv:]
+    out = torch.full((total, Hq, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((Hq, total), 7.0, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    cu = torch.from_numpy(np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)).cuda()
+    bk.baklava_prefill_attn_packed(bk.make_shape(1, Hq, Hkv, D), q, k, v, cu, T, out.transpose(0, 1), lse, status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    at = 0
+    for n in lens:
+        for h in range(Hq if n else 0):
+            check_head(q[h, at:at + n], k[h // 3, at:at + n], v[h // 3, at:at + n], out[at:at + n, h], lse[h, at:at + n],
+                       "rows %d.. head %d" % (at, h))
+        at += int(n)
+    assert bool((out[at:] == 7.0).all()) and bool((lse[:, at:] == 7.0).all())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_short_prompts_done_again(D):
+    # infinite and NaN tokens, in a head of its own and in the keys of all, and logits of several hundred
+    T, at = 48, 30
+    q, k, v = make(2, T, 6, 2, D, seed=31)
+    k[0, 0, 20] = (q[0, 1, 25].float() * 40).bfloat16()
+    out, lse = run(q, k, v)
+    assert float(lse.max()) > 200
+    check_padded(q, k, v, out, lse)
+    bad = [x.clone() for x in (q, k, v)]
+    bad[0][0, 2, 5] = float("nan")                                # one row of one head
+    bad[1][1, :, at:], bad[2][1, :, at:] = float("inf"), float("nan")
+    out2, lse2 = run(*bad)
+    assert bool(out2[0, 2, 5].isnan().all())
+    out2[0, 2, 5], lse2[0, 2, 5] = out[0, 2, 5], lse[0, 2, 5]
+    check_padded(q[:1], k[:1], v[:1], out2[:1], lse2[:1])
+    check_padded(q[1:, :, :at], k[1:, :, :at], v[1:, :, :at], out2[1:, :, :at], lse2[1:, :, :at])
+    assert bool(out2[1, :, at:].isnan().all())
