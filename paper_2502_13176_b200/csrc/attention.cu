@@ -254,6 +254,41 @@ __device__ __forceinline__ void softmax_half(uint32_t column, int first_key, int
     tc::tmem_st_32x32_x16(column, w);
     tc::tmem_st_wait();
 }
+// 16 logits -> 8 columns of probabilities
+__device__ __forceinline__ void softmax_16(const uint32_t (&v)[16], uint32_t column, f32x2 scale2, f32x2 minus, f32x2 (&sum)[2]) {
+    uint32_t w[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        const float2 x = unpack2(fma2(pack2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1])), scale2, minus));
+        const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
+        sum[c & 1] = add2(sum[c & 1], pack2(p0, p1));
+        w[c] = pack_bf16(p0, p1);
+    }
+    tc::tmem_st_32x32_x8(column, w);
+}
+// A thread's 64 keys of a tile that is seen whole: sixteen logits are asked for while the sixteen before them are worked on
+// (32K prompt 7.6 ms; halves of 32, each asked for, worked on and written before the next, 7.9 ms).
+template <typename F0, typename F1>
+__device__ __forceinline__ void softmax_tile(uint32_t column, f32x2 scale2, float ref, f32x2 (&sum)[2], F0 first_done, F1 second_done) {
+    const f32x2 minus = pack2(-ref, -ref);
+    uint32_t a[16], b[16];
+    tc::tmem_ld_32x32_x16(column, a);
+    tc::tmem_ld_wait();
+    tc::tmem_ld_32x32_x16(column + 16, b);
+    softmax_16(a, column, scale2, minus, sum);
+    tc::tmem_ld_wait();
+    tc::tmem_ld_32x32_x16(column + 32, a);
+    softmax_16(b, column + 8, scale2, minus, sum);
+    tc::tmem_st_wait();
+    first_done();
+    tc::tmem_ld_wait();
+    tc::tmem_ld_32x32_x16(column + 48, b);
+    softmax_16(a, column + 32, scale2, minus, sum);
+    tc::tmem_ld_wait();
+    softmax_16(b, column + 40, scale2, minus, sum);
+    tc::tmem_st_wait();
+    second_done();
+}
 // the same where none of the keys is seen
 __device__ __forceinline__ void no_probabilities(uint32_t column) {
     const uint32_t w[16] = {};
@@ -536,10 +571,7 @@ __device__ __forceinline__ void soften(const AttnParams& p, Shared& sm, const Ct
             if (lane == 0) tc::mbar_arrive(smem_u32(&bars[tile % kGroupRing]));
         };
         for (int it = 0; it < qb; ++it, ++tile) {
-            softmax_half<false>(lane_addr + col_base, col_base, row, scale2, ref, sum);
-            hand_over(sm.bar_pa);
-            softmax_half<false>(lane_addr + col_base + 32, col_base + 32, row, scale2, ref, sum);
-            hand_over(sm.bar_pb);
+            softmax_tile(lane_addr + col_base, scale2, ref, sum, [&] { hand_over(sm.bar_pa); }, [&] { hand_over(sm.bar_pb); });
             ok = group_wait(group++);                         // S(it + 1)
             if (!ok) break;
             tc::fence_after_sync();
