@@ -18,6 +18,12 @@
 // put side by side in one tile (the short form: 8, 16, 32 or 64 rows to a head), against the same keys: 64 prompts of up
 // to 16 tokens with 32 heads in groups of four are 512 blocks instead of 2 048.
 //
+// Measured: one 32K prompt of 32 heads of 128 (8.80 TFLOP) 7.4 to 7.9 ms = 1 115 to 1 190 TFLOP/s at the 1.55 GHz that the
+// power cap leaves (cuBLAS sustains 1 349 there), 16 packed prompts of up to 8K 2.67 ms, 2 048 tokens 59 us, 64 packed prompts
+// of up to 500 with heads of 64 93 us, 200 tokens 7.4 us.  Per tile the tensor pipe and the special-function unit are each
+// busy 60 % of the time; at D = 64 it is the softmax warps alone that set the pace (forming S of the next tile beside the
+// softmax, from two key and value tiles per CTA, took 350 us where this takes 332: eight prompts of 4 096, 12 heads).
+//
 // The softmax needs a stabiliser per row, not the row's maximum: the largest logit among the row's first eight
 // keys serves (every row sees key 0).  p = exp2(s - reference) may then exceed 1, which bf16 and the fp32
 // accumulators hold up to 2^127: no running maximum, no exchange between the threads of a row, no rescaling of O.
@@ -254,6 +260,18 @@ __device__ __forceinline__ void softmax_half(uint32_t column, int first_key, int
     tc::tmem_st_32x32_x16(column, w);
     tc::tmem_st_wait();
 }
+// 32 lanes x 16 columns of tensor memory into registers, 8 columns back
+__device__ __forceinline__ void load_16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void store_8(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
 // 16 logits -> 8 columns of probabilities
 __device__ __forceinline__ void softmax_16(const uint32_t (&v)[16], uint32_t column, f32x2 scale2, f32x2 minus, f32x2 (&sum)[2]) {
     uint32_t w[8];
@@ -264,7 +282,7 @@ __device__ __forceinline__ void softmax_16(const uint32_t (&v)[16], uint32_t col
         sum[c & 1] = add2(sum[c & 1], pack2(p0, p1));
         w[c] = pack_bf16(p0, p1);
     }
-    tc::tmem_st_32x32_x8(column, w);
+    store_8(column, w);
 }
 // A thread's 64 keys of a tile that is seen whole: sixteen logits are asked for while the sixteen before them are worked on
 // (32K prompt 7.6 ms; halves of 32, each asked for, worked on and written before the next, 7.9 ms).
@@ -272,17 +290,17 @@ template <typename F0, typename F1>
 __device__ __forceinline__ void softmax_tile(uint32_t column, f32x2 scale2, float ref, f32x2 (&sum)[2], F0 first_done, F1 second_done) {
     const f32x2 minus = pack2(-ref, -ref);
     uint32_t a[16], b[16];
-    tc::tmem_ld_32x32_x16(column, a);
+    load_16(column, a);
     tc::tmem_ld_wait();
-    tc::tmem_ld_32x32_x16(column + 16, b);
+    load_16(column + 16, b);
     softmax_16(a, column, scale2, minus, sum);
     tc::tmem_ld_wait();
-    tc::tmem_ld_32x32_x16(column + 32, a);
+    load_16(column + 32, a);
     softmax_16(b, column + 8, scale2, minus, sum);
     tc::tmem_st_wait();
     first_done();
     tc::tmem_ld_wait();
-    tc::tmem_ld_32x32_x16(column + 48, b);
+    load_16(column + 48, b);
     softmax_16(a, column + 32, scale2, minus, sum);
     tc::tmem_ld_wait();
     softmax_16(b, column + 40, scale2, minus, sum);

@@ -15,16 +15,21 @@
 //     is handled like the running maximum: fp16 holds what is at most 1).
 // The scaled query is brought to below 2^9 and split into two fixed-point terms, an integer (or sixteenths of one) and a
 // multiple of 2^-11 of it: one term would shift every logit of a head by a common error of 1e-4, and sums of small
-// integers times small integers stay below 2^24 units, so that the accumulators hold them exactly (the tensor cores cut off what an fp32 accumulator
-// cannot hold, which with floating-point terms shifted a head's logits by up to 5e-5).  With at most four heads in the group (kTwice) the two terms of
-// a head are two columns of ONE MMA, h and h + 4, whose results are added by one exchange between lanes: half the MMAs.
+// integers times small integers stay below 2^24 units, so that the accumulators hold them exactly (the tensor cores cut off
+// what an fp32 accumulator cannot hold, which with floating-point terms shifted a head's logits by up to 5e-5).  With at
+// most four heads in the group (kTwice) the two terms of a head are two columns of ONE MMA, h and h + 4, whose results are
+// added by one exchange between lanes: half the MMAs.
 // The exchange leaves a lane one token row instead of two, so that the softmax runs on all 32 lanes where half of them
 // would have had the group's missing heads.
 //
 // Four warps, each with its own tiles of 64 tokens (tiles w, w + 4, ... of the chunk) in two slots of its own, which it
-// refills itself.  No warp waits for another
-// before the end of the chunk (with one ring for all of them and a producer warp, a fifth of the time went into
-// waiting for the slowest), and the tiles in flight are the same 64 KB per CTA.
+// refills itself.  No warp waits for another before the end of the chunk (with one ring for all of them and a producer
+// warp, a fifth of the time went into waiting for the slowest), and the tiles in flight are the same 64 KB per CTA.
+//
+// Measured, attention alone: 2.51 million rows of 32 Llama-shaped layers (342.6 MB) 65.5 us = 5.23 TB/s, 80 % of the copy
+// bandwidth; 16 ragged sequences (272 MB in 1 792 short heads) 78.8 us; one layer of 78 000 rows 15 us.  Bound by latency:
+// three warps a scheduler (registers and the 64 KB of tiles), ALU 48 %, issue 48 %, tensor pipe 32 % busy.  Four CTAs with
+// tiles of 48 tokens 79 us (where this took 72), two with tiles of 96 72 to 80 us (66), six of two warps each 68.5 us.
 
 constexpr int kInt4Warps = 4;
 constexpr int kInt4Threads = kInt4Warps * 32;
