@@ -18,7 +18,7 @@ constexpr int max_merge_entries(int D) { return 48 * D; }
 // Byte offsets of the regions of the decode workspace.
 struct DecodeWorkspace {
     size_t control_off;    // 64 int32: launch-wide counters
-    size_t arrive_off;     // int32 [n_units]: chunks of a head that have delivered their partial result
+    size_t arrive_off;     // int32 [n_units]: pieces of a head that have arrived
     size_t stats_off;      // fp32 [n_units][2 * 8 + 4]: final (max, 1 / sum) of each query head, log2 domain, and where the
                            //   head's partials are (split tail)
     size_t best_off;       // uint64 [n_score_items] + int32 [n_score_items]: each score piece's eviction candidate

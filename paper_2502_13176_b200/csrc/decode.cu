@@ -3,8 +3,8 @@
 //
 // One launch covers every (layer, sequence, KV head) of a layer range.  A head is cut into
 // chunks (the host plan); one CTA reduces one chunk to a partial (o, m, l) and leaves the
-// chunk's unnormalised probabilities in the workspace.  The CTA that delivers the last partial of a
-// head finishes the head: it merges the partials in chunk order, writes the output, brings the
+// chunk's unnormalised probabilities in the workspace.  The CTA that arrives last of a head's
+// finishes the head: it merges the partials in chunk order, writes the output, brings the
 // probabilities to the final normaliser, adds them to the scores and picks the row to evict.
 //
 // Inside a chunk: a producer warp streams 64-token K and V tiles with TMA (128-byte swizzle)
@@ -81,7 +81,7 @@ struct DecodeParams {
     const int4* items;             // the plan's work items
     int32_t n_items;
     int32_t split_tail;            // 1: the score update and the eviction run as a second kernel (short launches)
-    int32_t* arrive;               // [n_units]: chunks of a head that have delivered their partial
+    int32_t* arrive;               // [n_units]: pieces of a head that have arrived (with their partial, if they hold rows)
     float* partial;
     float* logit;
     float* stats;                  // [n_units][kStatsStride]: final (max, 1 / sum) of every query head, the head's first
@@ -120,6 +120,14 @@ struct HeadState {
     bool overflow;      // a row was offered but the cache has no free slot
     bool do_append;     // this step writes the new row at slot f (Eq. 4)
 };
+
+// How many of a head's pieces arrive before one of them finishes it.  The finisher may change len / free_slot, from
+// which every CTA of the head tells what it has to do, and a CTA of a later wave may read them only then: with a row
+// that fills a chunk, the next piece would take itself for a piece with rows and append the row again.  So where the
+// state is going to change, all pieces of the plan's item arrive, those without rows too, each with the state read.
+__device__ __forceinline__ int arrivals_of(const HeadState& hs, int item_w, int active, bool changes_state) {
+    return hs.do_append && changes_state ? item_w >> 16 : active;
+}
 
 __device__ __forceinline__ HeadState head_state(const DecodeParams& p, const Unit& u) {
     HeadState h;
@@ -411,7 +419,7 @@ __device__ __forceinline__ void sweep_head(const float* logit_h, float* score, c
 }
 
 // ---------------------------------------------------------------- the end of a head
-// Run by the CTA that delivered a head's last partial: final (max, 1 / sum) of every query head, the merged
+// Run by the CTA that arrived last of a head's: final (max, 1 / sum) of every query head, the merged
 // output (chunks in order: the result does not depend on which CTA comes last), then the score update over the
 // whole head, the row to evict and the bookkeeping.  Other heads' CTAs keep streaming meanwhile; the plan puts
 // the largest heads first, so the long tails fall into the middle of a launch.  Not inlined: its registers are
@@ -631,6 +639,17 @@ __device__ __noinline__ void finish_head(const DecodeParams* pp, float* scratch,
     }
 }
 
+// A CTA whose piece holds no rows: it arrives all the same (see arrivals_of), and finishes the head if it is the last.
+template <int D, bool kByPosition, int NT>
+__device__ __noinline__ void arrive_without_rows(const DecodeParams& p, int& sm_last, uint8_t* smem, int unit, int piece,
+                                                 int active, int arrivals, bool overlap) {
+    __syncthreads();                                        // every thread has read the head's state
+    if (threadIdx.x == 0) sm_last = (arrive_acq_rel(p.arrive + unit) == arrivals - 1);
+    __syncthreads();
+    if (sm_last) finish_head<D, kByPosition, NT>(&p, reinterpret_cast<float*>(smem), unit, piece, active);
+    else if (overlap && threadIdx.x == 0) grid_dependency_wait();
+}
+
 // ---------------------------------------------------------------- steps 2-4
 // kByPosition: the score-free sinks + window policy (a second instantiation, so that the default
 // path carries none of its registers or branches).
@@ -700,10 +719,16 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
     const HeadState hs = head_state(p, u);                // (its loads go out together with the one above)
     const int C = hs.C, n = hs.n, hole = hs.hole, n_hi = hs.n_att;
     const int active = n_hi > 0 ? (n_hi + chunk_len - 1) / chunk_len : 1;
+    // (the second kernel of a short launch changes the state itself)
+    const int arrivals = arrivals_of(hs, item.w, active, !p.split_tail);
     // idle sequence (none of its rows, outputs or bookkeeping is touched), inconsistent head, chunk past the rows
-    if (t_pos < 0 || hs.bad || piece >= active) {
+    if (t_pos < 0 || hs.bad || piece >= arrivals) {
         if (t_pos >= 0 && hs.bad && tid == 0 && piece == 0) atomicOr(p.status, BAKLAVA_STATUS_BAD_STATE);
         if (overlap && tid == 0) grid_dependency_wait();
+        return;
+    }
+    if (piece >= active) {                                // no rows, but the head waits for this CTA to have read its state
+        arrive_without_rows<D, kByPosition, kThreads>(p, sm_last, smem_raw, unit, piece, active, arrivals, overlap);
         return;
     }
     if (hs.overflow && tid == 0 && piece == 0) atomicOr(p.status, BAKLAVA_STATUS_OVERFLOW);
@@ -1052,9 +1077,9 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
                 mbar_wait(smem_u32(&bar_full[t % kNS]), (t / kNS) & 1, p.wait_cycles);
         if (tid < G) part[G * D + tid] = __int_as_float(0x7fc00000);
     }
-    // A head of one chunk whose scores are not kept needs no partial and no arrival: its output is written from here
-    // (the same numbers: a single partial has weight 1).
-    const bool direct = active == 1 && !keep_logits && !pos_evict;
+    // A head for which no other CTA arrives and whose scores are not kept needs no partial and no arrival: its output is
+    // written from here (the same numbers: a single partial has weight 1).
+    const bool direct = arrivals == 1 && !keep_logits && !pos_evict;
     if (!aborted) {
     // ---- the four warps' states -> one partial for the chunk (the ring is idle now: reuse it)
     float* sm_o = reinterpret_cast<float*>(ring_ptr);       // [kConsumerWarps][G][D]
@@ -1133,11 +1158,11 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
         return;
     }
     __syncthreads();                                        // the whole partial is written ...
-    if (tid == 0) sm_last = (arrive_acq_rel(p.arrive + unit) == active - 1);   // ... and published with the arrival
+    if (tid == 0) sm_last = (arrive_acq_rel(p.arrive + unit) == arrivals - 1);   // ... and published with the arrival
     __syncthreads();
     if (!sm_last) return;
 
-    // ---- this CTA delivered the head's last partial and finishes the head
+    // ---- this CTA is the head's last and finishes it
     finish_head<D, kByPosition>(&p, reinterpret_cast<float*>(ring_ptr), unit, piece, active);   // the ring is idle now
 }
 
@@ -1169,12 +1194,13 @@ __global__ void __launch_bounds__(kThreads) sweep_kernel(const DecodeParams p) {
     const HeadState hs = head_state(p, u);
     const int C = hs.C, n = hs.n, n_hi = hs.n_att;
     const int active = n_hi > 0 ? (n_hi + chunk_len - 1) / chunk_len : 1;
+    const int arrivals = arrivals_of(hs, item.w, active, true);
     const int end = min(begin + chunk_len, n_hi);
     const int64_t row0 = (int64_t)u.b * p.seq_stride + p.slab_off[u.head];
-    if (tid == 0 || !(hs.bad || t_pos < 0 || piece >= active))
+    if (tid == 0 || !(hs.bad || t_pos < 0 || piece >= arrivals))
         grid_dependency_wait();                           // the attention kernel: statistics, scratch, partials, appended rows
     if (hs.bad || t_pos < 0) return;                      // reported by the attention kernel / idle sequence
-    if (piece >= active) return;
+    if (piece >= arrivals) return;
     const float* stats = p.stats + (int64_t)unit * kStatsStride;
     if (tid < G) {
         sm_M[tid] = stats[tid];
@@ -1210,7 +1236,7 @@ __global__ void __launch_bounds__(kThreads) sweep_kernel(const DecodeParams p) {
     // ---- this piece's share of the output: column groups [lo, hi) of the g * D / 4 four-element groups, summed
     // over the chunks.  Up to kMergeSplit threads share a group (each takes every P-th chunk, in ascending
     // order) and the group's first thread adds their sums in thread order: the result does not depend on timing.
-    if (!lost) {
+    if (!lost && piece < active) {
         constexpr int kMergeSplit = 16;
         __shared__ float4 sm_acc[kThreads];
         const int n_grp = G * D / 4;
@@ -1267,7 +1293,7 @@ __global__ void __launch_bounds__(kThreads) sweep_kernel(const DecodeParams p) {
             if (sm_key[w] < bk) { bk = sm_key[w]; bs = sm_slot[w]; }
         p.best_key[blockIdx.x] = bk;
         p.best_slot[blockIdx.x] = bs;
-        sm_last = (arrive_acq_rel(p.arrive + unit) == active - 1);
+        sm_last = (arrive_acq_rel(p.arrive + unit) == arrivals - 1);
     }
     __syncthreads();
     if (!sm_last || warp != 0) return;

@@ -119,9 +119,14 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     const HeadState hs = head_state(p, u);
     const int C = hs.C, n = hs.n, hole = hs.hole, n_hi = hs.n_att;
     const int active = n_hi > 0 ? (n_hi + chunk_len - 1) / chunk_len : 1;
-    if (t_pos < 0 || hs.bad || piece >= active) {
+    const int arrivals = arrivals_of(hs, item.w, active, !p.split_tail);
+    if (t_pos < 0 || hs.bad || piece >= arrivals) {
         if (t_pos >= 0 && hs.bad && tid == 0 && piece == 0) atomicOr(p.status, BAKLAVA_STATUS_BAD_STATE);
         if (overlap && tid == 0) grid_dependency_wait();
+        return;
+    }
+    if (piece >= active) {                                // no rows, but the head waits for this CTA to have read its state
+        arrive_without_rows<D, kByPosition, kInt4Threads>(p, sm_last, smem_raw, unit, piece, active, arrivals, overlap);
         return;
     }
     if (hs.overflow && tid == 0 && piece == 0) atomicOr(p.status, BAKLAVA_STATUS_OVERFLOW);
@@ -482,8 +487,8 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     float* part = p.partial + (int64_t)blockIdx.x * psz;
     const bool aborted = sm_abort != 0;                    // the chunk still arrives, with a mark
     if (aborted && tid < G) part[G * D + tid] = __int_as_float(0x7fc00000);
-    // a head of one chunk whose scores are not kept writes its output from here (see decode_chunk_kernel)
-    const bool direct = active == 1 && !keep_logits && !pos_evict;
+    // a head for which no other CTA arrives and whose scores are not kept is written from here (see decode_chunk_kernel)
+    const bool direct = arrivals == 1 && !keep_logits && !pos_evict;
     if (!aborted) {
         // ---- the four warps' states -> one partial for the chunk (the tiles are spent: their memory is reused)
         float* sm_o = reinterpret_cast<float*>(ring_ptr);   // [kInt4Warps][G][D]
@@ -554,7 +559,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
         return;
     }
     __syncthreads();                                        // the whole partial is written ...
-    if (tid == 0) sm_last = (arrive_acq_rel(p.arrive + unit) == active - 1);   // ... and published with the arrival
+    if (tid == 0) sm_last = (arrive_acq_rel(p.arrive + unit) == arrivals - 1);   // ... and published with the arrival
     __syncthreads();
     if (!sm_last) return;
     finish_head<D, kByPosition, kInt4Threads>(&p, reinterpret_cast<float*>(ring_ptr), unit, piece, active);
