@@ -100,7 +100,10 @@ struct Shared {
     uint32_t tmem_slot;
     int abort, bad_values;
     float ref[kTileRows];          // the rows' references for the exact form, log2 domain
-    float part[2][kTileRows];      // exchange between the two threads of a row
+    // exchange between the two threads of a row, two buffers in turn: the upper thread may be through with the next block's
+    // sum, which waits for nothing of the lower one's where that block has one tile, before the lower one has read this
+    // block's; the block after the next waits for its probabilities
+    float part[2][2][kTileRows];
 };
 
 __device__ __forceinline__ float fast_exp2(float x) {
@@ -611,13 +614,14 @@ __device__ __forceinline__ void soften(const AttnParams& p, Shared& sm, const Ct
         ++tile;
         // the two threads of a row join their sums (each writes its own, both add them in the same order)
         const float2 total = unpack2(add2(sum[0], sum[1]));
-        sm.part[part][row] = total.x + total.y;
+        float (&sums)[2][kTileRows] = sm.part[k & 1];
+        sums[part][row] = total.x + total.y;
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(smem_u32(&sm.bar_sum[quarter]));
         ok = mbar_wait(smem_u32(&sm.bar_sum[quarter]), k & 1);
         if (ok) ok = group_wait(group++);                     // the block's last group: O is complete
         if (!ok) break;
-        const float l = sm.part[0][row] + sm.part[1][row], inv = 1.0f / l;
+        const float l = sums[0][row] + sums[1][row], inv = 1.0f / l;
         bool again = !(l <= kMaxSum);
         tc::fence_after_sync();
 #pragma unroll
@@ -751,7 +755,7 @@ __device__ __noinline__ void redo_pass(const AttnParams& p, const Block blk, Sha
         }
         if (ok) ok = group_wait(n_it);
         const float2 total = unpack2(add2(sum[0], sum[1]));
-        sm.part[part][row] = kExact ? total.x + total.y : m_run;
+        sm.part[0][part][row] = kExact ? total.x + total.y : m_run;
     }
     if (!ok) sm.abort = 1;
     __syncthreads();                                          // sums / maxima, and whether values were taken out
@@ -759,9 +763,9 @@ __device__ __noinline__ void redo_pass(const AttnParams& p, const Block blk, Sha
         const int quarter = warp & 3, row = 32 * quarter + lane, part = (warp - 2) >> 2;
         const Row<kShort> r(p, blk, row);
         if (!kExact) {
-            if (part == 0) sm.ref[row] = fmaxf(sm.part[0][row], sm.part[1][row]) * p.scale_log2;
+            if (part == 0) sm.ref[row] = fmaxf(sm.part[0][0][row], sm.part[0][1][row]) * p.scale_log2;
         } else {
-            const float l = sm.part[0][row] + sm.part[1][row], inv = 1.0f / l;
+            const float l = sm.part[0][0][row] + sm.part[0][1][row], inv = 1.0f / l;
             tc::fence_after_sync();
             for (int ch = 0; ch < D / 64; ++ch) {
                 uint32_t o[32];

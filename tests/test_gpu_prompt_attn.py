@@ -325,3 +325,17 @@ def test_short_prompts_done_again(D):
     check_padded(q[:1], k[:1], v[:1], out2[:1], lse2[:1])
     check_padded(q[1:, :, :at], k[1:, :, :at], v[1:, :, :at], out2[1:, :, :at], lse2[1:, :, :at])
     assert bool(out2[1, :, at:].isnan().all())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T,Hq,Hkv", [(128, 4, 4), (100, 6, 1), (40, 16, 2)])
+def test_runs_of_one_tile_blocks(D, T, Hq, Hkv):
+    # a block of one tile asks nothing of the lower thread of a row before the upper one writes its sum: thousands of them
+    # in a row, which every CTA goes through one after the other, give the same bits every time
+    q, k, v = make(500, T, Hq, Hkv, D, seed=T)
+    lens = [T - b % 7 if b % 5 else T // 2 for b in range(500)]
+    out, lse = run(q, k, v, lens)
+    for _ in range(10):
+        again = run(q, k, v, lens)
+        assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+    check_padded(q[::25], k[::25], v[::25], out[::25], lse[::25], lens[::25])
