@@ -12,7 +12,8 @@
 //     8 sum_t p_t, which one more MMA against a constant operand sums from the very probabilities that were used;
 //   - the K channel scales are multiplied into the query, the V channel scales into the partial output, the K row
 //     scales into the logits, the V row scales into the probabilities (relative to the largest one met so far, which
-//     is handled like the running maximum: fp16 holds what is at most 1).
+//     is handled like the running maximum, and times 2^15: of fp16's range what is below that is left, and a product
+//     keeps its 11 bits down to 2^-29 of the largest).
 // The scaled query is brought to below 2^9 and split into two fixed-point terms, an integer (or sixteenths of one) and a
 // multiple of 2^-11 of it: one term would shift every logit of a head by a common error of 1e-4, and sums of small
 // integers times small integers stay below 2^24 units, so that the accumulators hold them exactly (the tensor cores cut off
@@ -27,7 +28,7 @@
 // warp, a fifth of the time went into waiting for the slowest), and the tiles in flight are the same 64 KB per CTA.
 //
 // Measured, attention alone: 2.51 million rows of 32 Llama-shaped layers (342.6 MB) 65.5 us = 5.23 TB/s, 80 % of the copy
-// bandwidth; 16 ragged sequences (272 MB in 1 792 short heads) 78.8 us; one layer of 78 000 rows 15 us.  Bound by latency:
+// bandwidth; 16 ragged sequences (272 MB in 1 792 short heads) 80.2 us; one layer of 78 000 rows 15 us.  Bound by latency:
 // three warps a scheduler (registers and the 64 KB of tiles), ALU 48 %, issue 48 %, tensor pipe 32 % busy.  Four CTAs with
 // tiles of 48 tokens 79 us (where this took 72), two with tiles of 96 72 to 80 us (66), six of two warps each 68.5 us.
 
@@ -174,8 +175,10 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     float o[D / 16][4];
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) { o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.0f; }
-    float o8[4] = {0.0f, 0.0f, 0.0f, 0.0f};               // eight times the sums of the probabilities used
-    float v_ref = 0.0f, v_inv = 0.0f;                     // largest V row scale met, what the probabilities are relative to
+    float o8[4] = {0.0f, 0.0f, 0.0f, 0.0f};               // eight times the sums of the operand used
+    // largest V row scale met (from the smallest on whose reciprocal times 2^15 is finite; scales below it need no more),
+    // and the factor of a row's scale in the probabilities' operand
+    float v_ref = 0x1p-110f, v_inv = 0x1p125f;
 
     // ---- query fragments (B operand): head g (kTwice: first terms for g < 4, second terms for g >= 4); registers
     // 2 j and 2 j + 1 of a group of 32 channels belong to the operands of codes (2 j, 2 j + 1 | 2 j + 4, 2 j + 5)
@@ -383,12 +386,12 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
                 l_run[e] = l_run[e] * corr[e] + psum;
             }
             const float seen = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv_max)));
-            if (seen > fmaxf(v_ref, 0x1p-126f)) {          // the V scales' reference follows their maximum
+            if (seen > v_ref) {                            // the V scales' reference follows their maximum
                 const float ratio = v_ref / seen;
                 corr[0] *= ratio;
                 corr[1] *= ratio;
                 v_ref = seen;
-                v_inv = 1.0f / seen;
+                v_inv = 0x1p15f / seen;
             }
             if (__any_sync(0xffffffffu, corr[0] != 1.0f || corr[1] != 1.0f)) {
 #pragma unroll
@@ -514,7 +517,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
                 for (int c = 0; c < D / 16; ++c) {
                     const int ch = 32 * (c >> 1) + 4 * g8 + 2 * (c & 1);
                     const float even = o[c][e] - o8[e], both = o[c][2 + e] - o8[2 + e];
-                    *reinterpret_cast<float2*>(dst + ch) = make_float2(even * 0x1p24f * v_ref, (both - even) * 0x1p20f * v_ref);
+                    *reinterpret_cast<float2*>(dst + ch) = make_float2(even * 0x1p9f * v_ref, (both - even) * 0x1p5f * v_ref);
                 }
                 if (g8 == 0) { sm_m[warp][head] = m_run[e]; sm_l[warp][head] = l_run[e]; }
             }
