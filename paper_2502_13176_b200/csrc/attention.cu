@@ -29,7 +29,8 @@
 // accumulators hold up to 2^127: no running maximum, no exchange between the threads of a row, no rescaling of O.
 // A row whose sum or output leaves the fp32 range that way (or is not finite for any other reason) shows in the
 // epilogue; the CTA notes the row block and does it again at its end: once for the rows' true maxima, once with them
-// as reference.
+// as reference, raised by as many powers of two as keep the row's sum below 1, so that the accumulators hold every
+// average of values that bf16 holds.
 //
 // Nothing a row must not see may reach it.  Keys above the query are masked in S.  Their value rows meet
 // probabilities of zero, which is not enough when they hold infinities or NaN (0 * inf): value rows past the prompt's
@@ -763,7 +764,8 @@ __device__ __noinline__ void redo_pass(const AttnParams& p, const Block blk, Sha
         const int quarter = warp & 3, row = 32 * quarter + lane, part = (warp - 2) >> 2;
         const Row<kShort> r(p, blk, row);
         if (!kExact) {
-            if (part == 0) sm.ref[row] = fmaxf(sm.part[0][0][row], sm.part[0][1][row]) * p.scale_log2;
+            // (2^k is more than the keys that the row sees)
+            if (part == 0) sm.ref[row] = fmaxf(sm.part[0][0][row], sm.part[0][1][row]) * p.scale_log2 + (float)(32 - __clz(blk.row0 + r.key + 1));
         } else {
             const float l = sm.part[0][0][row] + sm.part[0][1][row], inv = 1.0f / l;
             tc::fence_after_sync();
@@ -777,8 +779,8 @@ __device__ __noinline__ void redo_pass(const AttnParams& p, const Block blk, Sha
                                                   kvh * p.sv.head + part * (D / 2) + ch * 32;
 #pragma unroll
                         for (int c = 0; c < 32; ++c) {
-                            const float x = __bfloat162float(vj[c]);
-                            if (!(fabsf(x) <= kFinite)) o[c] = __float_as_uint(__uint_as_float(o[c]) + x);
+                            const float x = __bfloat162float(vj[c]);   // (what finite_pair took out)
+                            if ((__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) o[c] = __float_as_uint(__uint_as_float(o[c]) + x);
                         }
                     }
                 }

@@ -339,3 +339,28 @@ def test_runs_of_one_tile_blocks(D, T, Hq, Hkv):
         again = run(q, k, v, lens)
         assert torch.equal(again[0], out) and torch.equal(again[1], lse)
     check_padded(q[::25], k[::25], v[::25], out[::25], lse[::25], lens[::25])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T", [50, 300])
+def test_values_up_to_the_end_of_the_range(D, T):
+    # averages of values between 1e37 and 3.3e38: the terms' sum is far outside fp32, the average is not
+    q, k, v = make(1, T, 4, 2, D, seed=33, scale=0.3)
+    g = torch.Generator(device="cuda").manual_seed(T)
+    v.copy_((1e37 + 3.2e38 * torch.rand(v.shape, generator=g, device="cuda", dtype=torch.float64)).bfloat16())
+    v[:, :, :, ::3] *= -1
+    out, lse = run(q, k, v)
+    check_padded(q, k, v, out, lse)
+    # and beside infinities, which are looked for among them
+    at = T // 2
+    v2 = v.clone()
+    v2[0, 0, at, 1] = float("inf")
+    out2, lse2 = run(q, k, v2)
+    assert bool((out2[0, :2, at:, 1] == float("inf")).all())
+    v2[0, 0, at, 1] = 0.0
+    for h in range(2):
+        ref, bound, rl, bl = reference(q[0, h], k[0, 0], v2[0, 0])
+        cols = [c for c in range(D) if c != 1]
+        assert bool(((out2[0, h].double() - ref).abs() <= bound)[:, cols].all())
+        assert bool(((out2[0, h].double() - ref).abs() <= bound)[:at, 1].all())
+        assert bool(((lse2[0, h].double() - rl).abs() <= bl).all())
