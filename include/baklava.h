@@ -149,7 +149,9 @@ typedef struct baklava_cache {
 } baklava_cache;
 
 /* Where the rows of a [B, heads, T, D] tensor lie, for the calls that take any layout: element (b, h, t, d) is
- * base[b * seq + h * head + t * token + d].  In elements, multiples of 8 (16 bytes). */
+ * base[b * seq + h * head + t * token + d].  In elements, multiples of 8 (16 bytes), at least D; those of extents of 1 are
+ * not looked at.  No two elements of an output may lie in one place (INVALID_ARG): taken from the smallest up, each
+ * stride steps over all that the ones before it span, as in every permutation and slice of a dense tensor. */
 typedef struct baklava_strides {
     int64_t seq, head, token;
 } baklava_strides;

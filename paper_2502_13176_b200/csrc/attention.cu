@@ -943,6 +943,7 @@ int prompt_attn(const baklava_shape* shape, const void* q, const baklava_strides
         !baklava_strides_ok(o_str, seqs, shape->Hq, tokens, shape->D))
         return BAKLAVA_ERR_INVALID_ARG;
     if (B > 65535 || shape->Hq > 65535 || tokens > INT32_MAX - kTileRows) return BAKLAVA_ERR_UNSUPPORTED;
+    if (!baklava_output_strides_ok(o_str, seqs, shape->Hq, tokens, shape->D)) return BAKLAVA_ERR_INVALID_ARG;
     const int64_t n_blk = ((int64_t)T + kTileRows - 1) / kTileRows;
     // The short form where it makes fewer blocks: 64 prompts of up to 16 tokens, 32 heads in groups of four: 16.9 us,
     // a block per head 33.9 us.

@@ -42,14 +42,35 @@ size_t baklava_decode_ws_bytes(const baklava_shape* s, int64_t n_items, int64_t 
 
 inline bool baklava_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Strides that can address [seqs, heads, tokens, D] without two elements in one place: multiples of 16 bytes and at least
-// a row apart where the extent is above 1 (those of extents of 1 are not used).  Byte strides stay below the 2^40 of
-// a tensor map.
+// Strides that can address [seqs, heads, tokens, D]: multiples of 16 bytes and at least a row apart where the extent is
+// above 1 (those of extents of 1 are not used).  Byte strides stay below the 2^40 of a tensor map.
 inline bool baklava_strides_ok(const baklava_strides* s, int64_t seqs, int64_t heads, int64_t tokens, int D) {
     if (!s) return false;
     const int64_t extent[3] = {seqs, heads, tokens}, stride[3] = {s->seq, s->head, s->token};
     for (int i = 0; i < 3; ++i)
         if (extent[i] > 1 && ((stride[i] & 7) != 0 || stride[i] < D || stride[i] > ((int64_t)1 << 38))) return false;
+    return true;
+}
+
+// The same for what is written: besides, no two elements may lie in one place.  Taken from the smallest stride up, each
+// steps over all that the ones before it span (so it is for every permutation and slice of a dense tensor).
+inline bool baklava_output_strides_ok(const baklava_strides* s, int64_t seqs, int64_t heads, int64_t tokens, int D) {
+    if (!baklava_strides_ok(s, seqs, heads, tokens, D)) return false;
+    int64_t extent[3] = {seqs, heads, tokens}, stride[3] = {s->seq, s->head, s->token};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2; ++j)
+            if (stride[j] > stride[j + 1]) {
+                const int64_t e = extent[j], t = stride[j];
+                extent[j] = extent[j + 1]; stride[j] = stride[j + 1];
+                extent[j + 1] = e; stride[j + 1] = t;
+            }
+    int64_t span = D;
+    for (int i = 0; i < 3; ++i) {
+        if (extent[i] <= 1) continue;
+        if (stride[i] < span) return false;
+        if (stride[i] > (INT64_MAX - span) / (extent[i] - 1)) return false;
+        span += (extent[i] - 1) * stride[i];
+    }
     return true;
 }
 

@@ -256,7 +256,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_qk_norm_rope(
     if (flags & ~BAKLAVA_ROPE_INTERLEAVED) return BAKLAVA_ERR_INVALID_ARG;
     if (!(eps >= 0.0f)) return BAKLAVA_ERR_INVALID_ARG;
     if (!baklava_strides_ok(q_str, B, shape->Hq, T, shape->D) || !baklava_strides_ok(k_str, B, shape->Hkv, T, shape->D) ||
-        !baklava_strides_ok(qo_str, B, shape->Hq, T, shape->D) || !baklava_strides_ok(ko_str, B, shape->Hkv, T, shape->D))
+        !baklava_output_strides_ok(qo_str, B, shape->Hq, T, shape->D) || !baklava_output_strides_ok(ko_str, B, shape->Hkv, T, shape->D))
         return BAKLAVA_ERR_INVALID_ARG;
     const void* ptrs[] = {q, k, q_out, k_out, q_weight, k_weight};
     for (const void* ptr : ptrs)

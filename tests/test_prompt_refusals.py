@@ -133,3 +133,29 @@ def test_session_keeps_the_error_of_every_layer(monkeypatch, bad_layer):
         sess.prefill_layer(layer[0], *prompt())
     with pytest.raises(RuntimeError, match="prompt scores"):
         sess.check_status()
+
+
+@pytest.mark.parametrize("seq,head,token,code", [
+    (64, 64, 64, INVALID), (2048, 64, 64, INVALID), (64, 512, 64, INVALID), (512, 512, 64, INVALID),
+    (2048, 448, 64, INVALID), (2048, 512, 72, INVALID), (2040, 512, 64, INVALID), (2048, 64, 248, INVALID),
+    (1 << 38, 1 << 38, 1 << 38, INVALID)])
+def test_outputs_that_overlap_themselves_are_refused(seq, head, token, code):
+    # [2, 4, 8, 64] in less room than it takes, or with rows across others
+    assert rope(qos=strides(seq, head, token)) == code
+    assert attn(os=strides(seq, head, token)) == code
+
+
+def test_output_layouts_that_are_no_overlap():
+    # every order of the axes, dense and as slices of something wider; inputs whose rows lie across each other too.  The
+    # rotary dimension, which is looked at later, is out of range, so that nothing is enqueued where the strides pass
+    import itertools
+    for pad in (0, 64, 192):
+        for order in itertools.permutations(range(3)):
+            step, st = 64 + pad, [0, 0, 0]
+            for axis in order:
+                st[axis] = step
+                step = step * (2, 4, 8)[axis] + pad
+            assert rope(qos=strides(*st), rot=8) == SHAPE
+    assert rope(qs=strides(64, 64, 64), ks=strides(64, 128, 64), rot=8) == SHAPE
+    assert rope(qos=strides(0, 512, 64), kos=strides(-8, 512, 64), B=1, rot=8) == SHAPE
+    assert rope(qos=strides(512, 64, 3), kos=strides(512, 64, 0), T=1, rot=8) == SHAPE
