@@ -376,7 +376,8 @@ def _dense(t, what, dev, dtype, shape):
 def baklava_qk_norm_rope(shape, q, k, positions, inv_freq, q_weight, k_weight, eps, q_out, k_out, flags=0, stream=None):
     """q, q_out: bf16 [B, Hq, T, D], k, k_out: bf16 [B, Hkv, T, D], each any view with contiguous rows; positions: int32
     [B, T]; inv_freq: float32 [rotary_dim / 2]; weights: bf16 [D] or None."""
-    B, _, T, D = q.shape
+    B, _, T, _ = q.shape
+    D = shape.D
     dev, n = _device(), inv_freq.numel()
     queries, keys = (B, shape.Hq, T, D), (B, shape.Hkv, T, D)
     _check(lib().baklava_qk_norm_rope(shape, *_rows(q, "q", dev, queries), *_rows(k, "k", dev, keys),
@@ -391,7 +392,8 @@ def baklava_qk_norm_rope(shape, q, k, positions, inv_freq, q_weight, k_weight, e
 def baklava_prefill_attn(shape, q, k, v, prompt_len, out, lse, status, stream=None):
     """q, out: bf16 [B, Hq, T, D], k, v: bf16 [B, Hkv, T, D], any views with contiguous rows; prompt_len: int32 [B] or None;
     lse: float32 [B, Hq, T] or None; status: int32 [1]."""
-    B, _, T, D = q.shape
+    B, _, T, _ = q.shape
+    D = shape.D
     dev = _device()
     queries, keys = (B, shape.Hq, T, D), (B, shape.Hkv, T, D)
     _check(lib().baklava_prefill_attn(shape, *_rows(q, "q", dev, queries), *_rows(k, "k", dev, keys),

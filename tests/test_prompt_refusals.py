@@ -159,3 +159,18 @@ def test_output_layouts_that_are_no_overlap():
     assert rope(qs=strides(64, 64, 64), ks=strides(64, 128, 64), rot=8) == SHAPE
     assert rope(qos=strides(0, 512, 64), kos=strides(-8, 512, 64), B=1, rot=8) == SHAPE
     assert rope(qos=strides(512, 64, 3), kos=strides(512, 64, 0), T=1, rot=8) == SHAPE
+
+
+@pytest.mark.parametrize("wrong", [64, 32])
+def test_head_dimension_of_the_tensors_and_of_the_shape(wrong):
+    # rows of 64 elements are not read as rows of 128, however far apart they lie
+    sh, st = bk.make_shape(1, 4, 2, 128), torch.zeros(1, dtype=torch.int32)
+    q, k = (torch.zeros((1, h, 8, 256), dtype=torch.bfloat16)[..., :wrong] for h in (4, 2))
+    pos = torch.zeros((1, 8), dtype=torch.int32)
+    freq = torch.ones(wrong // 2)
+    with pytest.raises(ValueError, match=r"\[1, 4, 8, 128\]"):
+        bk.baklava_prefill_attn(sh, q, k, k, None, q, None, st)
+    with pytest.raises(ValueError, match=r"\[1, 4, 8, 128\]"):
+        bk.baklava_qk_norm_rope(sh, q, k, pos, freq, None, None, 1e-6, q, k)
+    with pytest.raises(ValueError, match=r"\[1, 4, 8, 128\]"):
+        bk.baklava_prefill_attn_packed(sh, q[0], k[0], k[0], pos[0, :2], 8, q[0], None, st)
