@@ -126,8 +126,9 @@ typedef struct baklava_shape {
  * and values have channels that stick out, and these take them out of the row's range).  With y = fl32(x * (1 /
  * channel scale)) the row's scale is s = max |y| / 7 and an element's code is rint(y / s), ties to even, clamped to
  * +-7, plus 8; it stands for (code - 8) * s * channel scale.  A row of zeros has s = 0 and codes 8.  Rows must be
- * finite; a row with a NaN becomes NaN.  Queries may have any finite value.  Only D = 128.  baklava_evict in place moves
- * the scales with their rows.
+ * finite; a row with a NaN becomes NaN.  Queries must be finite and, times the K channel scales, below 2^112 in
+ * magnitude (they are held to 2^-20 of the head's largest, at least to 2^-138).  Only D = 128.  baklava_evict in place
+ * moves the scales with their rows.
  */
 typedef struct baklava_cache {
     void*          k_slab;             /* bf16 [B * seq_stride_tokens, D], or D bytes (FP8), D / 2 bytes (INT4) a row */

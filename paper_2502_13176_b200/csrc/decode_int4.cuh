@@ -202,7 +202,8 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
         }
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-        // to [2^8, 2^9): a power of two, which the logits are multiplied by again (with the codes' 2^24)
+        // to [2^8, 2^9): a power of two, which the logits are multiplied by again (with the codes' 2^24, which is why the
+        // query ends at 2^112: the factor has to be finite)
         const int ex = min(max((int)(__float_as_uint(big) >> 23), 9), 238);      // biased exponent
         const float up = __uint_as_float((uint32_t)(127 + 8 + 127 - ex) << 23);
         const float back = __uint_as_float((uint32_t)(ex - 8 + 24) << 23);

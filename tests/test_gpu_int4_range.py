@@ -78,3 +78,19 @@ def test_many_small_shares_beside_a_dominant_key_and_a_large_value_row(G, outlie
     for chunk in (0, 2048):
         out, lse = attend(sh, cache, cap, stride, q, chunk)
         check(lens, G, setup, out, lse)
+
+
+@pytest.mark.parametrize("G", [4, 7])
+@pytest.mark.parametrize("power", [-100, 109])
+def test_scaled_queries_at_the_ends_of_their_range(G, power):
+    # up to 2^112 and down to where 2^-20 of the largest element is still held; the rows' scales make up for it
+    lens = [700, 90]
+    rng = np.random.default_rng(G + 200 + power)
+    chan = plain_chan(2, rng)
+    chan = (chan / np.abs(chan).max() * 1.9).astype(np.float32)
+    chan[0] *= np.float32(2.0 ** power)
+    setup = direct(lens, G, chan, 60 + G, row_scale=lambda r, shape: (0.2 + 0.3 * r.random(shape)) * np.array([2.0 ** -power, 1.0]))
+    q = setup[8]
+    q.copy_(q.clamp(-4, 4))
+    out, lse = attend(*setup[:3], setup[4], q)
+    check(lens, G, setup, out, lse)
