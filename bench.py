@@ -514,8 +514,10 @@ def main():
     elapsed_ms = ev[0].elapsed_time(ev[1])
 
     # ---- sustained: a second or more of continuous stepping, the clock the GPU settles at under it
+    # (not on a batch of mixed lengths: thousands of steps would fill its caches up, and the positions of its steps are laid
+    # out ahead)
     sustained = None
-    if args.sustain_seconds > 0:
+    if args.sustain_seconds > 0 and not args.mixed_lengths:
         est = max(elapsed_ms / args.steps, 1e-3)
         n_sus = int(args.sustain_seconds * 1e3 / est) + 1
         ends = [torch.cuda.Event(enable_timing=True) for _ in range(2)]

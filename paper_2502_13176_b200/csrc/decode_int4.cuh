@@ -35,6 +35,7 @@
 constexpr int kInt4Warps = 4;
 constexpr int kInt4Threads = kInt4Warps * 32;
 constexpr int kInt4CtasPerSm = 3;
+static_assert(kInt4CtasPerSm == kCtasPerSm && kFp8CtasPerSm == kCtasPerSm, "the plan counts a launch's places by kCtasPerSm");
 constexpr int kInt4Blocks = 4;                              // 16-token blocks of a tile
 constexpr int kInt4Tokens = 16 * kInt4Blocks;               // tokens of a tile
 constexpr int kInt4Slots = 2;

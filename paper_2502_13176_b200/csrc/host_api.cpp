@@ -261,6 +261,8 @@ extern "C" __attribute__((visibility("default"))) int baklava_decode_plan(const 
             // 66 us with 3328).  In ragged batches, whose sequences hold less than their capacities, chunks that turn out
             // empty leave a single wave's places idle, which costs most with the larger groups' slower rows
             // (g = 7: 30 us with 1728, 26 us with 832; 46 and 33 us with 3456 and 1728; g = 4: 48 and 49 us with 4608, 2176).
+            // The limits stand a little above the longest single wave that was measured to be no worse (4608) and below the
+            // shortest that was (8320; g > 4: 3456, with 1728 already behind); nothing was measured between.
             const int64_t one = chunks_for(1), two = chunks_for(2);
             target = one <= 2 * two + 512 && one <= (g <= 4 ? 5120 : 2048) ? one : two;
         } else if (target == kMinChunk) {

@@ -28,6 +28,7 @@ using namespace ptx;
 
 constexpr int kThreads = 256;
 constexpr int kAhead = 3;            // rows a thread has asked for while it works on one
+constexpr uint32_t kSms = 148;       // of the GPU this library is built for: a rule for spreading work, nothing depends on it
 
 struct RopeParams {
     const __nv_bfloat16* in[2];      // queries, keys
@@ -231,7 +232,7 @@ cudaError_t launch(const RopeParams& p, cudaStream_t s) {
     const int rows8 = (p.heads[0] + kStep8 - 1) / kStep8 + (p.heads[1] + kStep8 - 1) / kStep8;
     const uint32_t most = rows8 <= 6 ? 16 : 8;
     uint32_t tok = 1;
-    while (tok < most && (p.tokens + tok - 1) / tok > 2 * 148) tok *= 2;
+    while (tok < most && (p.tokens + tok - 1) / tok > 2 * kSms) tok *= 2;
     switch (tok) {
         case 1: launch_tokens<D, kInterleaved, 1>(p, s); break;
         case 2: launch_tokens<D, kInterleaved, 2>(p, s); break;
