@@ -639,17 +639,6 @@ __device__ __noinline__ void finish_head(const DecodeParams* pp, float* scratch,
     }
 }
 
-// A CTA whose piece holds no rows: it arrives all the same (see arrivals_of), and finishes the head if it is the last.
-template <int D, bool kByPosition, int NT>
-__device__ __noinline__ void arrive_without_rows(const DecodeParams& p, int& sm_last, uint8_t* smem, int unit, int piece,
-                                                 int active, int arrivals, bool overlap) {
-    __syncthreads();                                        // every thread has read the head's state
-    if (threadIdx.x == 0) sm_last = (arrive_acq_rel(p.arrive + unit) == arrivals - 1);
-    __syncthreads();
-    if (sm_last) finish_head<D, kByPosition, NT>(&p, reinterpret_cast<float*>(smem), unit, piece, active);
-    else if (overlap && threadIdx.x == 0) grid_dependency_wait();
-}
-
 // ---------------------------------------------------------------- steps 2-4
 // kByPosition: the score-free sinks + window policy (a second instantiation, so that the default
 // path carries none of its registers or branches).
@@ -727,10 +716,10 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
         if (overlap && tid == 0) grid_dependency_wait();
         return;
     }
-    if (piece >= active) {                                // no rows, but the head waits for this CTA to have read its state
-        arrive_without_rows<D, kByPosition, kThreads>(p, sm_last, smem_raw, unit, piece, active, arrivals, overlap);
-        return;
-    }
+    // 1024-byte aligned stage ring inside the dynamic shared memory
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
+    if (piece < active) {                                 // (a piece without rows only arrives)
     if (hs.overflow && tid == 0 && piece == 0) atomicOr(p.status, BAKLAVA_STATUS_OVERFLOW);
     const int end = min(begin + chunk_len, n_hi);
     const int n_tiles = end > begin ? (end - begin + kTT - 1) / kTT : 0;
@@ -746,10 +735,6 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
     // running maximum its 16-token block was computed under, and those maxima [G][C / 16] in fp32
     __half* prob_h = reinterpret_cast<__half*>(p.logit + row0 * G);
     float* mref_h = reinterpret_cast<float*>(prob_h + (int64_t)G * C);
-
-    // 1024-byte aligned stage ring inside the dynamic shared memory
-    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    uint8_t* ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
 
     // The head's tail reads and rewrites the score (and reads the position) of every row; those lines were last
     // touched a whole step ago.  Each chunk asks for its own share now, so that the tail finds them in L2.
@@ -1157,10 +1142,14 @@ __global__ void __launch_bounds__(kThreads, kFp8 ? kFp8CtasPerSm : kCtasPerSm) d
         if (overlap && tid == 0) grid_dependency_wait();
         return;
     }
-    __syncthreads();                                        // the whole partial is written ...
+    }
+    __syncthreads();                                        // the whole partial is written, the head's state read ...
     if (tid == 0) sm_last = (arrive_acq_rel(p.arrive + unit) == arrivals - 1);   // ... and published with the arrival
     __syncthreads();
-    if (!sm_last) return;
+    if (!sm_last) {
+        if (overlap && piece >= active && tid == 0) grid_dependency_wait();      // (as every CTA with nothing to do)
+        return;
+    }
 
     // ---- this CTA is the head's last and finishes it
     finish_head<D, kByPosition>(&p, reinterpret_cast<float*>(ring_ptr), unit, piece, active);   // the ring is idle now

@@ -127,10 +127,9 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
         if (overlap && tid == 0) grid_dependency_wait();
         return;
     }
-    if (piece >= active) {                                // no rows, but the head waits for this CTA to have read its state
-        arrive_without_rows<D, kByPosition, kInt4Threads>(p, sm_last, smem_raw, unit, piece, active, arrivals, overlap);
-        return;
-    }
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* const ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
+    if (piece < active) {                                 // (a piece without rows only arrives)
     if (hs.overflow && tid == 0 && piece == 0) atomicOr(p.status, BAKLAVA_STATUS_OVERFLOW);
     const int end = min(begin + chunk_len, n_hi);
     const int n_tiles = end > begin ? (end - begin + kInt4Tokens - 1) / kInt4Tokens : 0;
@@ -142,8 +141,6 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
     __half* prob_h = reinterpret_cast<__half*>(p.logit + row0 * G);        // the scratch of decode_chunk_kernel
     float* mref_h = reinterpret_cast<float*>(prob_h + (int64_t)G * C);
 
-    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    uint8_t* const ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
     // this warp's slots: K tile and V tile side by side, the scales of all slots behind the tiles
     const uint32_t my_tiles = warp * kInt4Slots * 2 * kInt4TileBytes;
     const uint32_t my_scales = kInt4Warps * kInt4Slots * 2 * kInt4TileBytes + warp * kInt4Slots * kInt4ScaleBytes;
@@ -563,9 +560,13 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
         if (overlap && tid == 0) grid_dependency_wait();
         return;
     }
-    __syncthreads();                                        // the whole partial is written ...
+    }
+    __syncthreads();                                        // the whole partial is written, the head's state read ...
     if (tid == 0) sm_last = (arrive_acq_rel(p.arrive + unit) == arrivals - 1);   // ... and published with the arrival
     __syncthreads();
-    if (!sm_last) return;
+    if (!sm_last) {
+        if (overlap && piece >= active && tid == 0) grid_dependency_wait();      // (as every CTA with nothing to do)
+        return;
+    }
     finish_head<D, kByPosition, kInt4Threads>(&p, reinterpret_cast<float*>(ring_ptr), unit, piece, active);
 }
