@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(kInt4Threads, kInt4CtasPerSm) decode_int4_kern
                 corr[0] *= ratio;
                 corr[1] *= ratio;
                 v_ref = seen;
-                v_inv = 0x1p15f / seen;
+                v_inv = 0x1p15f * (1.0f / seen);
             }
             if (__any_sync(0xffffffffu, corr[0] != 1.0f || corr[1] != 1.0f)) {
 #pragma unroll
