@@ -110,3 +110,50 @@ def test_score_pass_of_long_4bit_heads():
 @pytest.mark.parametrize("kv", ["bf16", "int4"])
 def test_overlapping_calls_layer_by_layer(kv):
     grow(FORMATS[kv], 4, 128, L=4, Hkv=8, B=32, cap=256, chunk=64, steps=100, flags=0, per_layer=True)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "int4"])
+@pytest.mark.parametrize("flags,n_sm", [(0, 148), (0, 1), (bk.FLAG_NO_SCORE, 148)], ids=["two kernels", "one kernel", "no scores"])
+def test_a_lost_step_of_a_growing_head(kv, flags, n_sm):
+    # the first piece gives up its wait, the pieces without rows arrive: nothing of the step counts, the counters are zero
+    # again, and the head grows on over the end of the piece
+    L, Hkv, g, D, cap = 1, 3, 4, 128, 512
+    sh = bk.make_shape(L, g * Hkv, Hkv, D)
+    caps = np.full((L, Hkv), cap, dtype=np.int32)
+    off = (np.arange(L * Hkv, dtype=np.int64) * cap).reshape(L, Hkv)
+    kind = FORMATS[kv]
+    one = {bk.KV_FP8_E4M3: np.ones((L, Hkv, 4), np.float32), bk.KV_INT4: np.ones((L, Hkv, 4, D), np.float32)}.get(kind)
+    cache = bk.Cache(sh, caps, off, Hkv * cap, 1, kv_dtype=kind, kv_scale=one)
+    plan = bk.baklava_decode_plan(sh, caps, 1, 0, 1, Hkv * cap, chunk_tokens=128 if kind != bk.KV_FP8_E4M3 else 256, n_sm=n_sm, kv_dtype=kind).to("cuda")
+    ws = bk.decode_workspace(plan)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    # (256-row pieces are fed 128 rows, 128-row pieces 64)
+    at = 100 if kind != bk.KV_FP8_E4M3 else 200
+    steps = at + 70
+    hist = torch.zeros((2, Hkv, steps, D), dtype=torch.float64, device="cuda")
+    out, lse = torch.zeros((L, 1, g * Hkv, D), dtype=torch.bfloat16, device="cuda"), torch.zeros((L, 1, g * Hkv), device="cuda")
+    for t in range(steps):
+        q = (torch.randn((L, 1, g * Hkv, D), generator=gen, device="cuda") * 0.7).bfloat16()
+        kn, vn = exact_rows((L, 1, Hkv, D), gen), exact_rows((L, 1, Hkv, D), gen)
+        if t == at:
+            score = cache.score.clone()
+            out.fill_(7.0)
+            bk.baklava_set_wait_limit(2_000_000)                     # about a millisecond
+            try:
+                bk.baklava_decode_attn(sh, cache, q, kn, vn, t, out, lse, flags | bk.FLAG_TEST_STALL, plan, ws)
+                torch.cuda.synchronize()
+            finally:
+                bk.baklava_set_wait_limit(100_000_000)
+            assert int(cache.status.item()) == bk.STATUS_TIMEOUT
+            cache.status.zero_()
+            assert bool((cache.len == t).all()) and bool((cache.free_slot == t).all()) and bool((out == 7.0).all())
+            held = (torch.arange(cap, device="cuda") < t).repeat(Hkv)
+            assert torch.equal(cache.score[held], score[held]) and not bool(counters(plan, ws).any())
+        bk.baklava_decode_attn(sh, cache, q, kn, vn, t, out, lse, flags, plan, ws)
+        torch.cuda.synchronize()
+        hist[0, :, t], hist[1, :, t] = kn[0, 0].double(), vn[0, 0].double()
+        s = torch.einsum("hgd,htd->hgt", q.double().view(Hkv, g, D), hist[0, :, :t + 1]) / D ** 0.5
+        ref = torch.einsum("hgt,htd->hgd", torch.softmax(s, -1), hist[1, :, :t + 1])
+        assert_close(out.view(Hkv, g, D).double().cpu(), ref.cpu(), "step %d out" % t)
+        assert int(cache.status.item()) == 0 and bool((cache.len == t + 1).all()) and bool((cache.free_slot == t + 1).all())
+        assert not bool(counters(plan, ws).any())
