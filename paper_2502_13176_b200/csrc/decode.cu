@@ -282,7 +282,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 
 // ---------------------------------------------------------------- steps 3-4: scores and the row to evict
-// Run over the whole head by the CTA that delivered its last partial, or over a piece of it by a CTA of the
+// Run over the whole head by the CTA that arrived last of it, or over a piece of it by a CTA of the
 // second kernel of a short launch.  Every row's stored probabilities
 // are brought to the head's final normaliser and added to its score; rows that may be evicted compete on the
 // 64-bit key (score bits, inverted position): the smallest key is the lowest score and, among equal scores,
