@@ -27,10 +27,11 @@
 // refills itself.  No warp waits for another before the end of the chunk (with one ring for all of them and a producer
 // warp, a fifth of the time went into waiting for the slowest), and the tiles in flight are the same 64 KB per CTA.
 //
-// Measured, attention alone: 2.51 million rows of 32 Llama-shaped layers (342.6 MB) 65.5 to 71.5 us by GPU = 4.8 to 5.2 TB/s,
-// 73 to 80 % of the copy bandwidth; 16 ragged sequences (272 MB in 1 792 short heads) 79.3 us; one layer of 78 000 rows 15 us.  Bound by latency:
-// three warps a scheduler (registers and the 64 KB of tiles), ALU 48 %, issue 48 %, tensor pipe 32 % busy.  Four CTAs with
-// tiles of 48 tokens 79 us (where this took 72), two with tiles of 96 72 to 80 us (66), six of two warps each 68.5 us.
+// Measured, attention alone: 2.51 million rows of 32 Llama-shaped layers (342.6 MB) 65.5 to 71.5 us by GPU = 4.8 to 5.2
+// TB/s, 73 to 80 % of the copy bandwidth; 16 ragged sequences (272 MB in 1 792 short heads) 79.3 us; one layer of 78 000
+// rows 15 us.  Bound by latency: three warps a scheduler (registers and the 64 KB of tiles), ALU 48 %, issue 48 %, tensor
+// pipe 32 % busy.  Four CTAs with tiles of 48 tokens 79 us (where this took 72), two with tiles of 96 72 to 80 us (66), six
+// of two warps each 68.5 us.
 
 constexpr int kInt4Warps = 4;
 constexpr int kInt4Threads = kInt4Warps * 32;

@@ -89,3 +89,18 @@ def test_bulk_eviction_without_a_workspace(scored):
         assert n == y["len"] == int(a.cap[key[1], key[2]]) - 1 and x["free"] == y["free"]
         for name in ("K", "V", "pos", "score"):
             np.testing.assert_array_equal(x[name][:n], y[name][:n])
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_random_shapes_and_batches(seed):
+    rng = np.random.default_rng(900 + seed)
+    B, g, Hkv = int(rng.integers(1, 6)), int(rng.integers(1, 9)), int(rng.integers(1, 4))
+    window = rng.random() < 0.3
+    w = wl.scaled(W4, B=B, L=int(rng.integers(1, 3)), Hq=g * Hkv, Hkv=Hkv, T=int(rng.choice([64, 200, 512, 900])),
+                  budget=float(rng.choice([0.125, 0.25, 0.5, 0.9])), seed=wl.MASTER_SEED + 300 + seed,
+                  **(dict(recent_num=1, recent_den=1) if window else {}))
+    lens = [int(x) for x in rng.integers(0, w.T + 1, size=B)]
+    s = Varlen4(w, lens, chunk_tokens=int(rng.choice([0, 64, 128, 192])), per_layer=bool(rng.random() < 0.3))
+    for i in range(8):
+        idle = tuple(int(b) for b in range(B) if rng.random() < 0.25)
+        s.step_varlen(i, idle=idle, flags=bk.FLAG_NO_SCORE if window else 0)
