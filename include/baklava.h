@@ -55,7 +55,7 @@ extern "C" {
 #define BAKLAVA_ERR_INVALID_ARG   (-1)  /* NULL / misaligned pointer, bad range, bad flag            */
 #define BAKLAVA_ERR_SHAPE         (-2)  /* unsupported D, g, page ...                                 */
 #define BAKLAVA_ERR_CAPACITY      (-3)  /* budget cannot be met inside [min, max]                     */
-#define BAKLAVA_ERR_WORKSPACE     (-4)  /* workspace / output buffer too small                        */
+#define BAKLAVA_ERR_WORKSPACE     (-4)  /* workspace / output buffer too small, or no host memory left for a host call's lists */
 #define BAKLAVA_ERR_CUDA          (-5)  /* a CUDA runtime call failed (launch error, no device)       */
 #define BAKLAVA_ERR_TIMEOUT       (-6)  /* reserved for bounded device waits                          */
 #define BAKLAVA_ERR_UNSUPPORTED   (-7)  /* valid request that this build does not implement           */

@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <new>
 #include <numeric>
 #include <vector>
 
@@ -125,7 +126,7 @@ int reallocate_group(const double* imp, int m, double t, int64_t r_num, int64_t 
 
 extern "C" __attribute__((visibility("default"))) int baklava_allocate(const baklava_shape* shape, const double* kv_importance,
                                 const baklava_alloc_params* p, int64_t total_tokens,
-                                int32_t* cap_out, int64_t* slab_off_out, int64_t* seq_stride_out) {
+                                int32_t* cap_out, int64_t* slab_off_out, int64_t* seq_stride_out) try {
     int rc = baklava_check_shape(shape);
     if (rc) return rc;
     if (!kv_importance || !p || !cap_out || !slab_off_out || !seq_stride_out) return BAKLAVA_ERR_INVALID_ARG;
@@ -170,6 +171,8 @@ extern "C" __attribute__((visibility("default"))) int baklava_allocate(const bak
     }
     *seq_stride_out = run;
     return BAKLAVA_OK;
+} catch (const std::bad_alloc&) {                         // (nothing is thrown across the C boundary)
+    return BAKLAVA_ERR_WORKSPACE;
 }
 
 // ---------------------------------------------------------------- decode work plan
@@ -193,7 +196,7 @@ size_t baklava_decode_ws_bytes(const baklava_shape* s, int64_t n_items, int64_t 
 extern "C" __attribute__((visibility("default"))) int baklava_decode_plan(const baklava_shape* shape, const int32_t* cap, int32_t B,
                                    int32_t layer_begin, int32_t layer_end, int32_t chunk_tokens, int32_t n_sm,
                                    int32_t kv_dtype, int64_t seq_stride_tokens, int32_t* items_out, int64_t items_capacity,
-                                   baklava_plan_info* info) {
+                                   baklava_plan_info* info) try {
     int rc = baklava_check_shape(shape);
     if (rc) return rc;
     if (!cap || !info || B <= 0 || seq_stride_tokens <= 0) return BAKLAVA_ERR_INVALID_ARG;
@@ -345,6 +348,8 @@ extern "C" __attribute__((visibility("default"))) int baklava_decode_plan(const 
     info->B = B;
     info->ws_bytes = (int64_t)baklava_decode_ws_bytes(shape, n_items, n_score, info->n_units, B, seq_stride_tokens, nullptr);
     return BAKLAVA_OK;
+} catch (const std::bad_alloc&) {
+    return BAKLAVA_ERR_WORKSPACE;
 }
 
 // ---------------------------------------------------------------- Algorithm 3: which configuration wins
