@@ -398,6 +398,98 @@ int baklava_evict_varlen(const baklava_shape* shape, const baklava_cache* cache,
                          int64_t stride_layer, int64_t stride_seq, int64_t stride_head, int32_t reserve,
                          void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------ drafted tokens
+ * A draft model puts forward several tokens per step, as a tree: node i of sequence b hangs on node parent[b * T + i] < i,
+ * or on the cache itself (-1).  A chain is parent[i] = i - 1.  Three calls take a tree through a step: attention of all
+ * its nodes at once over each layer's slabs (which are read once instead of once per token), the verification of the
+ * drafted tokens by the target's probabilities, and the commit of the accepted path to the slabs.  The paper decodes one
+ * token at a time; what is kept of it here is Eq. 7 per node and the retention policy.
+ * n_nodes[b] (clamped to 0 .. T) nodes of sequence b exist; what the arrays hold behind them is read for nothing and left
+ * as it is.  A sequence with a parent that is not in -1 .. i - 1 is skipped with BAKLAVA_STATUS_BAD_STATE. */
+#define BAKLAVA_MAX_TREE           64
+
+/* Attention of the nodes of ONE layer, for every node i < n_nodes[b] and query head h (KV head h / g):
+ *   out[b, h, i] = sum_j softmax_j(q_i . k_j / sqrt(D)) v_j  over the valid rows j of the slab (Eq. 7) and over node i
+ * and its ancestors in the tree, whose keys and values are k and v; lse is the natural-log normaliser.  The cache is not
+ * changed.  A node's result depends on nothing else: not on other branches, freed slots or rows behind the last one,
+ * whatever they hold (NaN and infinities among them).  Sums are held in fp32; probabilities are rounded to 16 bits for the
+ * product with V.  Quantised slabs as described above; k and v of the nodes are taken as they are.
+ *   q, out       device bf16 [B, Hq, T, D] under their strides (not overlapping)
+ *   k, v         device bf16 [B, Hkv, T, D] under their strides
+ *   parent       device int32 [B, T], T <= BAKLAVA_MAX_TREE
+ *   n_nodes      device int32 [B] or NULL for T everywhere
+ *   lse          device fp32 [B, Hq, T], contiguous, or NULL
+ *   items, info  baklava_tree_plan's (the layer is info->layer_begin)
+ *   ws           device workspace >= info->ws_bytes; need not be cleared; not shared by calls that overlap in time
+ * Errors as for baklava_decode_attn: BAD_STATE heads (and trees) are skipped, a lost wait sets TIMEOUT and leaves the
+ * head's rows unwritten. */
+int baklava_tree_attn(const baklava_shape* shape, const baklava_cache* cache,
+                      const void* q, const baklava_strides* q_strides, const void* k, const baklava_strides* k_strides,
+                      const void* v, const baklava_strides* v_strides, const int32_t* parent, const int32_t* n_nodes,
+                      int32_t T, void* out, const baklava_strides* out_strides, float* lse,
+                      const int32_t* items, const baklava_plan_info* info, void* ws, size_t ws_bytes, void* stream);
+
+/* The work list of baklava_tree_attn for one layer (host; arguments and use as baklava_decode_plan's; a plan serves
+ * trees of up to T nodes). */
+int baklava_tree_plan(const baklava_shape* shape, const int32_t* cap, int32_t B, int32_t layer, int32_t T,
+                      int32_t chunk_tokens, int32_t n_sm, int32_t kv_dtype, int32_t* items_out, int64_t items_capacity,
+                      baklava_plan_info* info);
+
+/* Which drafted tokens stand.  Node 0 is the token that is certain already; the others are drafts.  The walk starts at
+ * node 0 with r = target[b, 0]; at node n the children c of n are tried in ascending order:
+ *   c is accepted if u_accept[b, c] * q(x) < r(x), x = tokens[b, c], and the walk goes on at c with r = target[b, c];
+ *   otherwise r <- max(r - q, 0) / (its sum), and the next child is tried (if the sum is 0, r = target[b, n]).
+ * When no child is left the next token is drawn from r: the lowest v with r(0) + .. + r(v) > u_sample[b] * (sum of r).
+ * q is the distribution that n's children were drawn from: draft[b, n]; with BAKLAVA_VERIFY_DISTINCT (siblings drawn without
+ * replacement) a refused token leaves it, q(v) <- 0 and q <- q / (1 - what has left); with draft = NULL (children chosen, not
+ * drawn) q is 1 at x and 0 elsewhere.  Everything is computed in fp64 from the given values; the accepted tokens and the
+ * next one are then distributed as the target's own (speculative sampling).
+ *   target, draft     device, [B, T] rows of V probabilities >= 0, rows target_stride (draft_stride) >= V elements apart,
+ *                     fp32 or bf16 (prob_dtype); what is not above 0 (NaN) counts as 0
+ *   tokens, parent    device int32 [B, T]; n_nodes device int32 [B] or NULL
+ *   u_accept          device fp32 [B, T], u_sample device fp32 [B]: uniform in [0, 1)
+ *   path              device int32 [B, T]: the accepted nodes from node 0 on, then -1
+ *   n_path            device int32 [B]: their number
+ *   next_token        device int32 [B]
+ * A sequence without nodes, or skipped with BAD_STATE (a token outside 0 .. V - 1, a parent that cannot be), gets n_path = 0
+ * and next_token = -1; so does next_token, with BAD_STATE, where the last target row has nothing above 0. */
+#define BAKLAVA_PROB_F32           0
+#define BAKLAVA_PROB_BF16          1
+#define BAKLAVA_VERIFY_DISTINCT    1u
+int baklava_tree_verify(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int32_t prob_dtype,
+                        const int32_t* tokens, const int32_t* parent, const int32_t* n_nodes, int32_t B, int32_t T, int32_t V,
+                        const float* u_accept, const float* u_sample, uint32_t flags,
+                        int32_t* path, int32_t* n_path, int32_t* next_token, uint32_t* status, void* stream);
+
+/* The accepted path into the slabs of layers [info->layer_begin, info->layer_end), per (sequence, layer, KV head), with
+ * a = n_path[b] nodes at positions t_pos[b] .. t_pos[b] + a - 1:
+ *   1. score_j += sum over the path's nodes i and the group's queries of exp(q_i . k_j / sqrt(D) - lse_i) for every valid
+ *      row j, and the same over the nodes from j on for the path's own rows: what their attention gave each row
+ *   2. the a rows join the cache                                                                          (Eq. 4)
+ *   3. if it then holds more than cap - 1 rows, it is cut to cap - 1 by the retention policy as baklava_evict does it (sinks
+ *      and the last W positions stay, of the rest the lowest scores go, among equal ones the latest; W as for the decode
+ *      step, positions counted from t_pos[b] + a - 1)                                                     (Eq. 5-6)
+ * Rows that stay keep their slots.  The joining rows that stay take the free slots in ascending order; the next free
+ * slot becomes free_slot.  Freed slots keep what they held.  Flags as for the decode step: NO_SCORE leaves scores as they are
+ * (joining rows have 0) and implies NO_EVICT except under sinks + window, where the oldest rows go; NO_EVICT: a path that does
+ * not fit into the slab as a whole does not join (OVERFLOW; its scores are still counted).
+ *   q            device bf16 [layers, B, Hq, T, D], contiguous (not read with NO_SCORE: may be NULL)
+ *   k, v         device bf16 [layers, B, Hkv, T, D], contiguous
+ *   lse          device fp32 [layers, B, Hq, T] as baklava_tree_attn left it (not read with NO_SCORE: may be NULL)
+ *   path, n_path as baklava_tree_verify left them; n_path[b] = 0 or t_pos[b] < 0: the sequence sits out
+ *   max_path     at least every n_path[b], at most T; sizes the workspace (a longer path, or a node that is not in
+ *                0 .. T - 1: the sequence is skipped with BAD_STATE)
+ *   t_pos        device int32 [B], above every position in the cache
+ *   t_next       device int32 [B] or NULL: t_pos + n_path, the next step's t_pos (not the same array); a sequence that sits
+ *                out or is skipped keeps its t_pos
+ *   items, info  a plan of baklava_decode_plan for the layer range (the one that the session's decode step has)
+ *   ws           device workspace >= baklava_tree_commit_workspace_size(); need not be cleared */
+int baklava_tree_commit(const baklava_shape* shape, const baklava_cache* cache, const void* q, const void* k, const void* v,
+                        const float* lse, int32_t T, const int32_t* path, const int32_t* n_path, int32_t max_path,
+                        const int32_t* t_pos, int32_t* t_next, uint32_t flags, const int32_t* items,
+                        const baklava_plan_info* info, void* ws, size_t ws_bytes, void* stream);
+size_t baklava_tree_commit_workspace_size(const baklava_shape* shape, const baklava_plan_info* info, int32_t max_path);
+
 /* ------------------------------------------------------------------ prompt scores (seed of step 3)
  * The accumulated attention a prompt leaves on its own tokens, for ONE layer: with the causal
  * attention matrix A_h = softmax(Q_h K^T / sqrt(D)) of Eq. 1,

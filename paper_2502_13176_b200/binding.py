@@ -21,6 +21,9 @@ SCOPE_LAYER, SCOPE_MODEL = 0, 1
 STATUS_OVERFLOW, STATUS_BAD_STATE, STATUS_TIMEOUT = 1, 2, 4
 KV_BF16, KV_FP8_E4M3, KV_INT4 = 0, 1, 2
 ROPE_INTERLEAVED = 1
+MAX_TREE = 64
+PROB_F32, PROB_BF16 = 0, 1
+VERIFY_DISTINCT = 1
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libbaklava.so")
 _lib = None
@@ -104,6 +107,15 @@ def lib():
         prompt = [POINTER(Shape)] + [c_void_p, POINTER(Strides)] * 3 + [c_void_p, c_int32, c_int32]
         L.baklava_prefill_attn.argtypes = prompt + [c_void_p, POINTER(Strides), c_void_p, c_void_p, c_void_p]
         L.baklava_prefill_attn_packed.argtypes = prompt + [c_int64, c_void_p, POINTER(Strides), c_void_p, c_void_p, c_void_p]
+        L.baklava_tree_plan.argtypes = [POINTER(Shape), POINTER(c_int32)] + [c_int32] * 6 + [POINTER(c_int32), c_int64, POINTER(PlanInfo)]
+        L.baklava_tree_attn.argtypes = [POINTER(Shape), POINTER(CacheStruct)] + [c_void_p, POINTER(Strides)] * 3 + [
+            c_void_p, c_void_p, c_int32, c_void_p, POINTER(Strides), c_void_p, c_void_p, POINTER(PlanInfo), c_void_p, c_size_t, c_void_p]
+        L.baklava_tree_verify.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_int32] + [c_void_p] * 3 + [c_int32] * 3 + [
+            c_void_p, c_void_p, c_uint32] + [c_void_p] * 5
+        L.baklava_tree_commit.argtypes = [POINTER(Shape), POINTER(CacheStruct)] + [c_void_p] * 4 + [
+            c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_uint32, c_void_p, POINTER(PlanInfo), c_void_p, c_size_t, c_void_p]
+        L.baklava_tree_commit_workspace_size.restype = c_size_t
+        L.baklava_tree_commit_workspace_size.argtypes = [POINTER(Shape), POINTER(PlanInfo), c_int32]
         L.baklava_output_error.argtypes = [c_void_p, c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
         L.baklava_output_error_workspace_size.restype = c_size_t
         L.baklava_output_error_workspace_size.argtypes = [c_int64]
@@ -418,6 +430,111 @@ def baklava_prefill_attn_packed(shape, q, k, v, cu_seqlens, max_len, out, lse, s
                                              _dense(lse, "lse", dev, torch.float32, (Hq, total)),
                                              _dense(status, "status", dev, torch.int32, (1,)), _stream(stream, dev)),
            "baklava_prefill_attn_packed")
+
+
+# ------------------------------------------------------------------ drafted tokens
+def baklava_tree_plan(shape, cap, B, layer, T, chunk_tokens=0, n_sm=148, kv_dtype=KV_BF16):
+    """cap: int32 array [L, Hkv].  The plan of baklava_tree_attn for one layer; `decode_workspace(plan)` is its workspace."""
+    cap = np.ascontiguousarray(cap, dtype=np.int32).reshape(shape.L, shape.Hkv)
+    info = PlanInfo()
+    args = (ctypes.byref(shape), cap.ctypes.data_as(POINTER(c_int32)), B, layer, T, chunk_tokens, n_sm, kv_dtype)
+    _check(lib().baklava_tree_plan(*args, None, 0, ctypes.byref(info)), "baklava_tree_plan")
+    items = np.empty((info.n_items, 4), dtype=np.int32)
+    _check(lib().baklava_tree_plan(*args, items.ctypes.data_as(POINTER(c_int32)), info.n_items, ctypes.byref(info)),
+           "baklava_tree_plan")
+    return Plan(items, info)
+
+
+def _planned(plan, dev):
+    if plan.items_dev is None or plan.items_dev.get_device() != dev:
+        raise ValueError("the plan's items are not on the current device (Plan.to)")
+    return plan.items_dev.data_ptr()
+
+
+def _workspace(ws, dev):
+    if not ws.is_contiguous():
+        raise ValueError("ws: expected a contiguous tensor")
+    if ws.get_device() != dev:
+        _elsewhere(ws, "ws", dev)
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _cache_here(cache, B, dev):
+    if cache.B != B:
+        raise ValueError("the cache holds %d sequences, the tensors %d" % (cache.B, B))
+    if cache.k_slab.get_device() != dev:
+        _elsewhere(cache.k_slab, "the cache", dev)
+
+
+def baklava_tree_attn(shape, cache, q, k, v, parent, n_nodes, out, lse, plan, ws, stream=None):
+    """q, out: bf16 [B, Hq, T, D], k, v: bf16 [B, Hkv, T, D], any views with contiguous rows; parent: int32 [B, T]; n_nodes:
+    int32 [B] or None; lse: float32 [B, Hq, T] or None; plan: baklava_tree_plan's for the layer."""
+    B, _, T, _ = q.shape
+    D = shape.D
+    dev = _device()
+    queries, keys = (B, shape.Hq, T, D), (B, shape.Hkv, T, D)
+    _cache_here(cache, B, dev)
+    _check(lib().baklava_tree_attn(shape, ctypes.byref(cache.struct), *_rows(q, "q", dev, queries), *_rows(k, "k", dev, keys),
+                                   *_rows(v, "v", dev, keys), _dense(parent, "parent", dev, torch.int32, (B, T)),
+                                   _dense(n_nodes, "n_nodes", dev, torch.int32, (B,)), T, *_rows(out, "out", dev, queries),
+                                   _dense(lse, "lse", dev, torch.float32, queries[:3]), _planned(plan, dev),
+                                   ctypes.byref(plan.info), *_workspace(ws, dev), _stream(stream, dev)), "baklava_tree_attn")
+
+
+def _probabilities(t, what, dev, shape, dtype):
+    """Pointer and row stride of probabilities [B, T, V]: rows contiguous, all the same distance apart."""
+    B, T, _ = shape
+    st = t.stride()
+    row = st[1] if T > 1 else st[0]
+    if t.dtype is not dtype or t.shape != shape or st[2] != 1 and shape[2] > 1 or B > 1 and T > 1 and st[0] != T * st[1]:
+        raise ValueError("%s: expected %s [%d, %d, %d] with contiguous rows at one distance, got %s %s with strides %s"
+                         % ((what, dtype) + tuple(shape) + (t.dtype, tuple(t.shape), st)))
+    if t.get_device() != dev:
+        _elsewhere(t, what, dev)
+    return t.data_ptr(), max(row, shape[2])
+
+
+def baklava_tree_verify(target, draft, tokens, parent, n_nodes, u_accept, u_sample, path, n_path, next_token, status, flags=0,
+                        stream=None):
+    """target: float32 or bf16 [B, T, V]; draft: the same or None; tokens, parent, path: int32 [B, T]; n_nodes, n_path,
+    next_token: int32 [B] (n_nodes may be None); u_accept: float32 [B, T]; u_sample: float32 [B]; status: int32 [1]."""
+    B, T, V = target.shape
+    dev = _device()
+    if target.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("target: expected float32 or bfloat16, got %s" % target.dtype)
+    i32, f32 = torch.int32, torch.float32
+    _check(lib().baklava_tree_verify(*_probabilities(target, "target", dev, target.shape, target.dtype),
+                                     *((None, 0) if draft is None else _probabilities(draft, "draft", dev, target.shape, target.dtype)),
+                                     PROB_F32 if target.dtype is f32 else PROB_BF16, _dense(tokens, "tokens", dev, i32, (B, T)),
+                                     _dense(parent, "parent", dev, i32, (B, T)), _dense(n_nodes, "n_nodes", dev, i32, (B,)), B, T, V,
+                                     _dense(u_accept, "u_accept", dev, f32, (B, T)), _dense(u_sample, "u_sample", dev, f32, (B,)),
+                                     flags, _dense(path, "path", dev, i32, (B, T)), _dense(n_path, "n_path", dev, i32, (B,)),
+                                     _dense(next_token, "next_token", dev, i32, (B,)), _dense(status, "status", dev, i32, (1,)),
+                                     _stream(stream, dev)), "baklava_tree_verify")
+
+
+def tree_commit_workspace(shape, plan, max_path, device="cuda"):
+    n = int(lib().baklava_tree_commit_workspace_size(ctypes.byref(shape), ctypes.byref(plan.info), max_path))
+    return torch.empty((n,), dtype=torch.uint8, device=device)
+
+
+def baklava_tree_commit(shape, cache, q, k, v, lse, path, n_path, max_path, t_pos, t_next, flags, plan, ws, stream=None):
+    """q: bf16 [layers, B, Hq, T, D], k, v: bf16 [layers, B, Hkv, T, D], lse: float32 [layers, B, Hq, T], contiguous (q and lse
+    may be None with FLAG_NO_SCORE); path: int32 [B, T]; n_path, t_pos, t_next: int32 [B] (t_next may be None); plan: one of
+    baklava_decode_plan for the layers; ws: tree_commit_workspace."""
+    n, B, _, T, _ = k.shape
+    dev, i32 = _device(), torch.int32
+    if n != plan.info.layer_end - plan.info.layer_begin:
+        raise ValueError("k has %d layers, the plan %d" % (n, plan.info.layer_end - plan.info.layer_begin))
+    _cache_here(cache, B, dev)
+    keys = (n, B, shape.Hkv, T, shape.D)
+    _check(lib().baklava_tree_commit(shape, ctypes.byref(cache.struct), _dense(q, "q", dev, _BF16, (n, B, shape.Hq, T, shape.D)),
+                                     _dense(k, "k", dev, _BF16, keys), _dense(v, "v", dev, _BF16, keys),
+                                     _dense(lse, "lse", dev, torch.float32, (n, B, shape.Hq, T)), T,
+                                     _dense(path, "path", dev, i32, (B, T)), _dense(n_path, "n_path", dev, i32, (B,)), max_path,
+                                     _dense(t_pos, "t_pos", dev, i32, (B,)), _dense(t_next, "t_next", dev, i32, (B,)), flags,
+                                     _planned(plan, dev), ctypes.byref(plan.info), *_workspace(ws, dev), _stream(stream, dev)),
+           "baklava_tree_commit")
 
 
 def baklava_output_error(out, ref, loss, ws, stream=None):

@@ -40,6 +40,9 @@ int baklava_check_kv_format(const baklava_shape* s, const baklava_cache* cache);
 size_t baklava_decode_ws_bytes(const baklava_shape* s, int64_t n_items, int64_t n_score_items, int64_t n_units, int32_t B,
                                int64_t seq_stride_tokens, DecodeWorkspace* layout);
 
+// tree_attn.cu: workspace of attention over drafted tokens (partials, then their references and sums)
+size_t baklava_tree_ws_bytes(const baklava_shape* s, int64_t n_items, int32_t T, size_t* stats_off);
+
 inline bool baklava_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Strides that can address [seqs, heads, tokens, D]: multiples of 16 bytes and at least a row apart where the extent is

@@ -352,6 +352,63 @@ extern "C" __attribute__((visibility("default"))) int baklava_decode_plan(const 
     return BAKLAVA_ERR_WORKSPACE;
 }
 
+// ---------------------------------------------------------------- work plan of attention over drafted tokens
+extern "C" __attribute__((visibility("default"))) int baklava_tree_plan(const baklava_shape* shape, const int32_t* cap, int32_t B,
+                                 int32_t layer, int32_t T, int32_t chunk_tokens, int32_t n_sm, int32_t kv_dtype,
+                                 int32_t* items_out, int64_t items_capacity, baklava_plan_info* info) try {
+    int rc = baklava_check_shape(shape);
+    if (rc) return rc;
+    if (!cap || !info || B <= 0 || T <= 0 || layer < 0 || layer >= shape->L) return BAKLAVA_ERR_INVALID_ARG;
+    if (chunk_tokens < 0 || (chunk_tokens == 0 && n_sm <= 0)) return BAKLAVA_ERR_INVALID_ARG;
+    if (kv_dtype != BAKLAVA_KV_BF16 && kv_dtype != BAKLAVA_KV_FP8_E4M3 && kv_dtype != BAKLAVA_KV_INT4) return BAKLAVA_ERR_INVALID_ARG;
+    if (T > BAKLAVA_MAX_TREE) return BAKLAVA_ERR_UNSUPPORTED;
+    const int Hkv = shape->Hkv;
+    const int32_t* const c = cap + (size_t)layer * Hkv;
+    std::vector<int> heads(Hkv);
+    std::iota(heads.begin(), heads.end(), 0);
+    int64_t tokens = 0;
+    for (int h : heads) {
+        if (c[h] <= 0 || c[h] % shape->page != 0) return BAKLAVA_ERR_INVALID_ARG;
+        if (c[h] > INT32_MAX - 256) return BAKLAVA_ERR_UNSUPPORTED;
+        tokens += c[h];
+    }
+    tokens *= B;
+    std::stable_sort(heads.begin(), heads.end(), [&](int a, int b) { return c[a] > c[b]; });
+    constexpr int kKeys = 128;                               // keys to a tile
+    int64_t want = chunk_tokens;
+    if (want == 0) want = std::max<int64_t>(4 * kKeys, std::min<int64_t>(8192, tokens / n_sm));
+    want = std::max<int64_t>(kKeys, (want + kKeys - 1) / kKeys * kKeys);
+    int64_t n_items = 0;
+    for (int h : heads) {
+        int64_t pieces = (c[h] + want - 1) / want;
+        const int64_t len = ((c[h] + pieces - 1) / pieces + kKeys - 1) / kKeys * kKeys;
+        pieces = (c[h] + len - 1) / len;
+        if (pieces > 32767) return BAKLAVA_ERR_UNSUPPORTED;
+        for (int b = 0; b < B; ++b)
+            for (int64_t pc = 0; pc < pieces; ++pc, ++n_items) {
+                if (!items_out) continue;
+                if (n_items >= items_capacity) return BAKLAVA_ERR_WORKSPACE;
+                int32_t* it = items_out + 4 * n_items;
+                it[0] = b * Hkv + h;
+                it[1] = (int32_t)(pc * len);
+                it[2] = (int32_t)len;
+                it[3] = (int32_t)(pc | (pieces << 16));
+            }
+    }
+    if (n_items > INT32_MAX) return BAKLAVA_ERR_UNSUPPORTED;
+    info->n_items = (int32_t)n_items;
+    info->n_score_items = 0;
+    info->n_units = B * Hkv;
+    info->chunk_tokens = (int32_t)want;
+    info->layer_begin = layer;
+    info->layer_end = layer + 1;
+    info->B = B;
+    info->ws_bytes = (int64_t)baklava_tree_ws_bytes(shape, n_items, T, nullptr);
+    return BAKLAVA_OK;
+} catch (const std::bad_alloc&) {
+    return BAKLAVA_ERR_WORKSPACE;
+}
+
 // ---------------------------------------------------------------- Algorithm 3: which configuration wins
 extern "C" __attribute__((visibility("default"))) int baklava_search_pick(const double* avg_loss, int32_t n,
                                                                           int32_t* best) {

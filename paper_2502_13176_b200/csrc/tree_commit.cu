@@ -1,0 +1,615 @@
+// The accepted path of a drafted tree into the budgeted slabs: what its attention gave every row, the joining rows, and
+// the cut back to capacity - 1 rows (Eq. 4 - 6).
+//
+// Attention over the tree has left every node's log-sum-exp, so that a row's share is exp2(s - lse) straight away: one
+// pass over K, no maximum, no V.  Rows go from global memory into the registers of the A operand (a lane's 16 bytes of a
+// row supply two MMA steps or more; the contraction's order is free, the queries are laid out to match), 16 rows to a
+// warp, against the queries of the path's nodes only: the drafts that were refused cost nothing here.
+//
+// A block then holds the new scores of its rows and lists those that would leave first, as many as the head has to give
+// up.  The second kernel joins the lists of a head, picks the rows that leave, and writes the joining ones.
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+#include <cstdint>
+
+#include "baklava.h"
+#include "common.h"
+#include "fp8.cuh"
+#include "int4.cuh"
+#include "tree.cuh"
+
+namespace {
+
+using namespace tree;
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kBlockRows = 1024;              // rows of a head to a block
+constexpr int kRowsPerThread = kBlockRows / kThreads;
+constexpr int kMaxTree = BAKLAVA_MAX_TREE;
+
+struct CommitParams {
+    Slabs c;
+    const __nv_bfloat16* q;
+    const __nv_bfloat16* k;
+    const __nv_bfloat16* v;
+    const float* lse;
+    const int32_t* path;
+    const int32_t* n_path;
+    const int32_t* t_pos;
+    int32_t* t_next;                // or null
+    const int4* items;
+    unsigned long long* best_key;   // [n_items][subs][max_path + 1], ascending; ~0: none
+    int32_t* best_slot;
+    float* fresh;                   // [n_items][max_path]: the joining rows' scores (in the place of a head's first item)
+    int32_t T, g, D, Hq, layer_begin, max_path, subs, n_sink, recent_num, recent_den;
+    int32_t scored, evict;          // scores are kept; rows may leave
+    float scale_log2;
+};
+
+// What is to be done with a head, the same for every block that touches it.
+struct Job {
+    int a, t0;                      // joining rows, position of the first
+    int leave;                      // rows that leave
+    int newest;                     // rows at positions up to this may leave
+    bool idle, bad, overflow;
+    __device__ __forceinline__ Job(const CommitParams& p, const Unit& u, const Head& hd) {
+        a = p.n_path[u.b];
+        t0 = p.t_pos[u.b];
+        idle = t0 < 0 || a == 0;
+        bad = !idle && (hd.bad || a < 0 || a > p.max_path || t0 > INT32_MAX - kMaxTree);
+        if (!idle && !bad) {
+            const int32_t* const path = p.path + (int64_t)u.b * p.T;
+            for (int i = 0; i < a; ++i) bad = bad || path[i] < 0 || path[i] >= p.T;
+        }
+        leave = p.evict ? max(0, hd.n + a - (hd.C - 1)) : 0;
+        overflow = !p.evict && hd.n + a > hd.C;
+        const long long window = max(0ll, (long long)(hd.C - 1 - p.n_sink) * p.recent_num / p.recent_den);
+        newest = (int)max(-1ll, (long long)t0 + a - 1 - window);
+    }
+};
+// Order in which rows leave: lowest score first, among equal ones the latest; without scores the oldest first.
+__device__ __forceinline__ unsigned long long leave_key(bool scored, float score, int pos) {
+    return scored ? ((unsigned long long)__float_as_uint(score) << 32) | (uint32_t)~(uint32_t)pos : (unsigned long long)(uint32_t)pos;
+}
+__device__ __forceinline__ unsigned long long warp_min(unsigned long long x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const unsigned long long y = __shfl_xor_sync(0xffffffffu, x, o);
+        x = y < x ? y : x;
+    }
+    return x;
+}
+
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// How a format's rows go into A registers.  A lane (c = lane % 4) takes kPieces pieces of 16 bytes of a row; the operand has
+// D / 32 pairs of MMA steps, and element e of lane c in pair t is dimension dim(t, c, e).
+template <int D, int KV>
+struct Format {
+    static constexpr int kRowBytes = KV == BAKLAVA_KV_BF16 ? 2 * D : KV == BAKLAVA_KV_FP8_E4M3 ? D : D / 2;
+    static constexpr int kPieces = kRowBytes / 64;
+    static constexpr int kTerms = KV == BAKLAVA_KV_INT4 ? 2 : 1;     // 16-bit terms of a query element
+    static __device__ __forceinline__ int dim(int t, int c, int e) {
+        if (KV == BAKLAVA_KV_BF16) return t * 32 + c * 8 + e;
+        if (KV == BAKLAVA_KV_FP8_E4M3) return (t >> 1) * 64 + c * 16 + (t & 1) * 8 + e;
+        return c * 32 + t * 8 + (e >> 1) + 4 * (e & 1);              // nibbles 0 and 4 of a word make a pair, 1 and 5, ...
+    }
+    // the four 16-bit pairs of pair of steps t
+    static __device__ __forceinline__ void operand(const uint4 (&raw)[kPieces], int t, uint32_t (&a)[4]) {
+        if (KV == BAKLAVA_KV_BF16) {
+            a[0] = raw[t].x; a[1] = raw[t].y; a[2] = raw[t].z; a[3] = raw[t].w;
+        } else if (KV == BAKLAVA_KV_FP8_E4M3) {
+            const uint4 w = raw[t >> 1];
+            fp8::f16x4_from_e4m3x4(t & 1 ? w.z : w.x, a[0], a[1]);
+            fp8::f16x4_from_e4m3x4(t & 1 ? w.w : w.y, a[2], a[3]);
+        } else {
+            const uint4 four = raw[0];
+            const uint32_t w = t == 0 ? four.x : t == 1 ? four.y : t == 2 ? four.z : four.w;
+            const __half2 eight = __half2half2(__ushort_as_half(0x6408));                    // 1024 + 8
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t n = ((w >> (4 * i)) & 0x000f000fu) | 0x64006400u;             // 1024 + code
+                const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&n), eight);
+                a[i] = *reinterpret_cast<const uint32_t*>(&x);
+            }
+        }
+    }
+};
+
+// One element of a query's row as the operand holds it: bf16 as it is; else fp16, scaled by a power of two that brings the
+// row's largest to 2^14 .. 2^15 (4 bits: times the channels' scales, in two terms, 22 bits of it).
+constexpr int kColumnPad = 64;                // bytes between the columns' rows in shared memory: no bank conflicts
+constexpr int kMaxColumns = 256;              // columns in shared memory at a time (long paths of large groups take several rounds)
+
+template <int D, int KV>
+__global__ void __launch_bounds__(kThreads, 2) path_scores_kernel(const __grid_constant__ CommitParams p) {
+    using F = Format<D, KV>;
+    constexpr int kColumnBytes = 2 * D + kColumnPad;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ float sums[kBlockRows];
+    __shared__ unsigned long long lists[kWarps][kMaxTree + 1];
+    __shared__ int list_slots[kWarps][kMaxTree + 1];
+    const int4 item = p.items[blockIdx.x];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, sub = blockIdx.y;
+    const Unit u(p.c, p.layer_begin, item.x);
+    const Head hd(p.c, u);
+    const Job job(p, u, hd);
+    const int lo = item.y + sub * kBlockRows, hi = min(min(item.y + item.z, lo + kBlockRows), hd.slots);
+    const int top = p.max_path + 1;
+    const int64_t list_at = ((int64_t)blockIdx.x * p.subs + sub) * top;
+    if (job.idle || job.bad) return;                          // (the second kernel reports what is bad)
+    if (sub == p.subs) {
+        // the joining rows' own scores: one warp per row, its node and those behind it on the path
+        if ((item.w & 0xffff) != 0 || !p.scored) return;
+        const int32_t* const path = p.path + (int64_t)u.b * p.T;
+        constexpr int kE = D / 32;
+        const int64_t head0 = (int64_t)u.li * p.c.B + u.b;
+        for (int j = warp; j < job.a; j += kWarps) {
+            const __nv_bfloat16* const kj = p.k + ((head0 * p.c.Hkv + u.h) * p.T + path[j]) * D + kE * lane;
+            float x[kE], total = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kE; ++e) x[e] = __bfloat162float(kj[e]);
+            for (int i = j; i < job.a; ++i)
+                for (int a = 0; a < p.g; ++a) {
+                    const int64_t row = (head0 * p.Hq + u.h * p.g + a) * p.T + path[i];
+                    const __nv_bfloat16* const qi = p.q + row * D + kE * lane;
+                    float s = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < kE; ++e) s = fmaf(__bfloat162float(qi[e]), x[e], s);
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                    total += exp2f(fmaf(s, p.scale_log2, -p.lse[row] * kLog2e));
+                }
+            if (lane == 0) p.fresh[(int64_t)blockIdx.x * p.max_path + j] = total;
+        }
+        return;
+    }
+    if (lo >= hi) {                                           // no rows: an empty list
+        for (int i = tid; i < job.leave; i += kThreads) p.best_key[list_at + i] = ~0ull;
+        return;
+    }
+    // what the end needs of the rows, asked for now
+    int pos[kRowsPerThread];
+    float score[kRowsPerThread];
+#pragma unroll
+    for (int i = 0; i < kRowsPerThread; ++i) {
+        const int j = lo + tid + i * kThreads;
+        const bool there = j < hi && j != hd.hole;
+        pos[i] = there ? p.c.pos[hd.first + j] : -1;
+        score[i] = there && p.scored ? p.c.score[hd.first + j] : 0.0f;
+    }
+    if (p.scored) {
+        const int all = job.a * p.g;
+        float2* const of_column = reinterpret_cast<float2*>(smem + min((p.max_path * p.g + 7) / 8 * 8, kMaxColumns) * kColumnBytes * F::kTerms);
+        const int32_t* const path = p.path + (int64_t)u.b * p.T;
+        for (int col0 = 0; col0 < all; col0 += kMaxColumns) {
+            const int columns = min(all - col0, kMaxColumns), blocks = (columns + 7) / 8;
+            if (col0 > 0) __syncthreads();
+            for (int n = warp; n < blocks * 8; n += kWarps) {     // the queries, column = node column / g, head column % g
+                constexpr int kE = D / 32;
+                float x[kE];                                      // dimensions lane + 32 e
+                float lse2 = INFINITY, factor = 0.0f;             // a column that is none adds exp2(-inf)
+                int64_t row = 0;
+                if (n < columns) {
+                    row = (((int64_t)u.li * p.c.B + u.b) * p.Hq + u.h * p.g + (col0 + n) % p.g) * p.T + path[(col0 + n) / p.g];
+                    lse2 = p.lse[row] * kLog2e;
+                    factor = p.scale_log2;
+                }
+#pragma unroll
+                for (int e = 0; e < kE; ++e) {
+                    x[e] = n < columns ? __bfloat162float(p.q[row * D + lane + 32 * e]) : 0.0f;
+                    if (KV == BAKLAVA_KV_INT4) x[e] *= p.c.kv_scale[(int64_t)u.head * 4 * D + lane + 32 * e];
+                }
+                if (KV != BAKLAVA_KV_BF16) {
+                    float big = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < kE; ++e) big = fmaxf(big, fabsf(x[e]));
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+                    int power;
+                    frexpf(big, &power);                          // big = f 2^power, f in 0.5 .. 1
+                    power = big > 0.0f && big < INFINITY ? power - 15 : 0;
+#pragma unroll
+                    for (int e = 0; e < kE; ++e) x[e] = ldexpf(x[e], -power);
+                    factor = ldexpf(factor, power);
+                    if (KV == BAKLAVA_KV_FP8_E4M3) factor *= p.c.kv_scale[(int64_t)u.head * 4];
+                }
+                // dimension d goes to pair t, lane c, element e of the column: the inverse of Format::dim
+#pragma unroll
+                for (int e = 0; e < kE; ++e) {
+                    const int d = lane + 32 * e;
+                    int t, c, i;
+                    if (KV == BAKLAVA_KV_BF16) { t = d >> 5; c = (d >> 3) & 3; i = d & 7; }
+                    else if (KV == BAKLAVA_KV_FP8_E4M3) { t = (d >> 6) * 2 + ((d >> 3) & 1); c = (d >> 4) & 3; i = d & 7; }
+                    else { t = (d >> 3) & 3; c = d >> 5; i = (d & 3) * 2 + ((d >> 2) & 1); }
+                    uint8_t* const at = smem + (size_t)n * F::kTerms * kColumnBytes + t * 64 + c * 16 + i * 2;
+                    if (KV == BAKLAVA_KV_BF16) {
+                        *reinterpret_cast<__nv_bfloat16*>(at) = __float2bfloat16(x[e]);
+                    } else {
+                        const __half high = __float2half_rn(x[e]);
+                        *reinterpret_cast<__half*>(at) = high;
+                        if (F::kTerms == 2) *reinterpret_cast<__half*>(at + kColumnBytes) = __float2half_rn(x[e] - __half2float(high));
+                    }
+                }
+                if (lane == 0) of_column[n] = make_float2(factor, lse2);
+            }
+            __syncthreads();
+            const uint8_t* const slab = static_cast<const uint8_t*>(p.c.k) + hd.first * F::kRowBytes;
+            const int r = lane >> 2, c = lane & 3;
+            for (int j0 = lo + warp * 16; j0 < hi; j0 += kWarps * 16) {
+                const int row0 = min(j0 + r, hi - 1), row1 = min(j0 + r + 8, hi - 1);            // (behind the end: not used)
+                uint4 raw0[F::kPieces], raw1[F::kPieces];
+#pragma unroll
+                for (int i = 0; i < F::kPieces; ++i) {
+                    raw0[i] = __ldg(reinterpret_cast<const uint4*>(slab + (int64_t)row0 * F::kRowBytes + i * 64 + c * 16));
+                    raw1[i] = __ldg(reinterpret_cast<const uint4*>(slab + (int64_t)row1 * F::kRowBytes + i * 64 + c * 16));
+                }
+                float rs0 = 1.0f, rs1 = 1.0f;
+                if (KV == BAKLAVA_KV_INT4) {
+                    rs0 = p.c.row_scale[2 * (hd.first + row0)];
+                    rs1 = p.c.row_scale[2 * (hd.first + row1)];
+                }
+                float sum0 = 0.0f, sum1 = 0.0f;
+                for (int nb = 0; nb < blocks; ++nb) {
+                    float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    const uint8_t* const column = smem + (size_t)(nb * 8 + r) * F::kTerms * kColumnBytes + c * 16;
+#pragma unroll
+                    for (int t = 0; t < D / 32; ++t) {
+                        uint32_t a0[4], a1[4];
+                        F::operand(raw0, t, a0);
+                        F::operand(raw1, t, a1);
+#pragma unroll
+                        for (int term = 0; term < F::kTerms; ++term) {
+                            const uint4 b = *reinterpret_cast<const uint4*>(column + term * kColumnBytes + t * 64);
+                            if (KV == BAKLAVA_KV_BF16) {
+                                mma_bf16(d, a0[0], a1[0], a0[1], a1[1], b.x, b.y);
+                                mma_bf16(d, a0[2], a1[2], a0[3], a1[3], b.z, b.w);
+                            } else {
+                                mma_f16(d, a0[0], a1[0], a0[1], a1[1], b.x, b.y);
+                                mma_f16(d, a0[2], a1[2], a0[3], a1[3], b.z, b.w);
+                            }
+                        }
+                    }
+                    const float4 two = *reinterpret_cast<const float4*>(of_column + nb * 8 + 2 * c);   // (factor, lse) of two columns
+                    sum0 += fast_exp2(fmaf(d[0] * rs0, two.x, -two.y)) + fast_exp2(fmaf(d[1] * rs0, two.z, -two.w));
+                    sum1 += fast_exp2(fmaf(d[2] * rs1, two.x, -two.y)) + fast_exp2(fmaf(d[3] * rs1, two.z, -two.w));
+                }
+                sum0 += __shfl_xor_sync(0xffffffffu, sum0, 1);
+                sum0 += __shfl_xor_sync(0xffffffffu, sum0, 2);
+                sum1 += __shfl_xor_sync(0xffffffffu, sum1, 1);
+                sum1 += __shfl_xor_sync(0xffffffffu, sum1, 2);
+                if (c == 0) {
+                    float* const to = sums + j0 + r - lo;          // (always the same lane's)
+                    to[0] = col0 > 0 ? to[0] + sum0 : sum0;
+                    to[8] = col0 > 0 ? to[8] + sum1 : sum1;
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kRowsPerThread; ++i) {
+            const int j = lo + tid + i * kThreads;
+            if (j < hi && j != hd.hole) {
+                score[i] += sums[j - lo];
+                p.c.score[hd.first + j] = score[i];
+            }
+        }
+    }
+    if (job.leave == 0) return;
+    // each warp's first `leave` rows in the order, then the warps' lists joined
+    unsigned long long key[kRowsPerThread];
+#pragma unroll
+    for (int i = 0; i < kRowsPerThread; ++i)
+        key[i] = pos[i] >= p.n_sink && pos[i] <= job.newest ? leave_key(p.scored, score[i], pos[i]) : ~0ull;
+    for (int n = 0; n < job.leave; ++n) {
+        unsigned long long best = key[0];
+#pragma unroll
+        for (int i = 1; i < kRowsPerThread; ++i) best = key[i] < best ? key[i] : best;
+        const unsigned long long first = warp_min(best);
+        const uint32_t who = __ballot_sync(0xffffffffu, best == first);
+        if (lane == __ffs(who) - 1) {
+            int at = -1;
+#pragma unroll
+            for (int i = kRowsPerThread - 1; i >= 0; --i)
+                if (key[i] == first) at = i;
+            lists[warp][n] = first;
+            list_slots[warp][n] = lo + tid + at * kThreads;
+#pragma unroll
+            for (int i = 0; i < kRowsPerThread; ++i)
+                if (i == at) key[i] = ~0ull;
+        }
+        if (first == ~0ull) {
+            for (int i = n + lane; i < job.leave; i += 32) lists[warp][i] = ~0ull;
+            break;
+        }
+    }
+    __syncthreads();
+    if (warp == 0) {
+        int cursor = 0;                                       // lane = warp whose list it reads
+        for (int n = 0; n < job.leave; ++n) {
+            const unsigned long long head = lane < kWarps && cursor < job.leave ? lists[lane][cursor] : ~0ull;
+            const unsigned long long first = warp_min(head);
+            const uint32_t who = __ballot_sync(0xffffffffu, head == first);
+            if (lane == __ffs(who) - 1) {
+                p.best_key[list_at + n] = first;
+                if (first != ~0ull) p.best_slot[list_at + n] = list_slots[lane][cursor];
+                ++cursor;
+            }
+        }
+    }
+}
+
+// A head's lists joined, the rows that leave, the rows that join.  Blocks of items that are not a head's first have
+// nothing to do.
+template <int D>
+__global__ void __launch_bounds__(kThreads) join_rows_kernel(const __grid_constant__ CommitParams p) {
+    const int4 item = p.items[blockIdx.x];
+    if ((item.w & 0xffff) != 0) return;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const Unit u(p.c, p.layer_begin, item.x);
+    grid_dependency_wait();
+    const Head hd(p.c, u);
+    const Job job(p, u, hd);
+    if (p.t_next && u.li == 0 && u.h == 0 && tid == 0) p.t_next[u.b] = job.idle || job.bad ? p.t_pos[u.b] : job.t0 + job.a;
+    if (job.idle) return;
+    if (job.bad || job.overflow) {
+        if (tid == 0) atomicOr(p.c.status, job.bad ? BAKLAVA_STATUS_BAD_STATE : BAKLAVA_STATUS_OVERFLOW);
+        return;
+    }
+    __shared__ unsigned long long warp_best[2][kWarps], gone_key[2][kMaxTree + 1];
+    __shared__ int gone[2][kMaxTree + 1];                     // slots that leave, two lists in turn; joining row j: -1 - j
+    __shared__ int open[3 * kMaxTree], sorted[3 * kMaxTree];
+    __shared__ int to[kMaxTree];                              // slot of each joining row, or -1
+    __shared__ float fresh[kMaxTree];
+    int last = 0;
+    const int pieces = item.w >> 16, top = p.max_path + 1, a = job.a;
+    if (tid < a) {
+        to[tid] = 0;
+        fresh[tid] = p.scored ? p.fresh[(int64_t)blockIdx.x * p.max_path + tid] : 0.0f;
+    }
+    __syncthreads();
+    if (job.leave > 0) {
+        // The blocks' lists, eight to a thread at a time (a head of over two million rows has more: what the batch before
+        // left is then one more list); the joining rows are candidates of their own, one to a thread.
+        constexpr int kHeld = 8;
+        const int lists = pieces * p.subs;
+        unsigned long long mine = ~0ull;
+        if (tid < a) {
+            const int ps = job.t0 + tid;
+            if (ps >= p.n_sink && ps <= job.newest) mine = leave_key(p.scored, fresh[tid], ps);
+        }
+        int kept = 0;                                         // entries of the list of the batch before
+        for (int list0 = 0; list0 < lists; list0 += kHeld * kThreads) {
+            const int from = (list0 / (kHeld * kThreads)) & 1, into = from ^ 1;
+            auto head_of = [&](int list, int cursor) {
+                return cursor < job.leave ? __ldcg(p.best_key + ((int64_t)blockIdx.x * p.subs + list) * top + cursor) : ~0ull;
+            };
+            unsigned long long head[kHeld];
+            int at[kHeld], carried = 0, n = 0;
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k) {
+                const int list = list0 + tid + k * kThreads;
+                at[k] = 0;
+                head[k] = list < lists ? head_of(list, 0) : ~0ull;
+            }
+            for (; n < job.leave; ++n) {
+                unsigned long long best = mine;
+#pragma unroll
+                for (int k = 0; k < kHeld; ++k) best = head[k] < best ? head[k] : best;
+                const unsigned long long of_warp = warp_min(best);
+                if (lane == 0) warp_best[n & 1][warp] = of_warp;
+                __syncthreads();
+                unsigned long long first = carried < kept ? gone_key[from][carried] : ~0ull;
+                int winner = -1;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w)
+                    if (warp_best[n & 1][w] < first) { first = warp_best[n & 1][w]; winner = w; }
+                if (first == ~0ull) break;
+                if (winner < 0) {
+                    if (tid == 0) { gone_key[into][n] = first; gone[into][n] = gone[from][carried]; }
+                    ++carried;
+                    continue;
+                }
+                const uint32_t who = __ballot_sync(0xffffffffu, best == first);
+                if (warp == winner && lane == __ffs(who) - 1) {
+                    gone_key[into][n] = first;
+                    if (mine == first) {
+                        gone[into][n] = -1 - tid;
+                        mine = ~0ull;
+                    } else {
+                        bool done = false;
+#pragma unroll
+                        for (int k = 0; k < kHeld; ++k)
+                            if (!done && head[k] == first) {
+                                const int list = list0 + tid + k * kThreads;
+                                gone[into][n] = __ldcg(p.best_slot + ((int64_t)blockIdx.x * p.subs + list) * top + at[k]);
+                                head[k] = head_of(list, ++at[k]);
+                                done = true;
+                            }
+                    }
+                }
+            }
+            __syncthreads();
+            kept = n;
+            last = into;
+            // a joining row that did not make this batch's list stays a candidate of none: the lists only get better, and
+            // what made it is carried by the list
+            mine = ~0ull;
+        }
+        if (kept < job.leave) {                               // fewer rows may leave than have to
+            if (tid == 0) atomicOr(p.c.status, BAKLAVA_STATUS_BAD_STATE);
+            return;
+        }
+        for (int i = tid; i < job.leave; i += kThreads)
+            if (gone[last][i] < 0) to[-1 - gone[last][i]] = -1;
+        __syncthreads();
+    }
+    // free slots: the hole, the slots that become free, the next ones that were never taken
+    const int was_hole = hd.hole >= 0 ? 1 : 0, unused = min(hd.C - hd.slots, a + 1), count = was_hole + job.leave + unused;
+    for (int i = tid; i < count; i += kThreads)
+        open[i] = i < was_hole ? hd.hole : i < was_hole + job.leave ? (gone[last][i - was_hole] < 0 ? INT32_MAX : gone[last][i - was_hole])
+                                                                    : hd.slots + i - was_hole - job.leave;
+    __syncthreads();
+    for (int i = tid; i < count; i += kThreads) {
+        int rank = 0;
+        for (int k = 0; k < count; ++k) rank += open[k] < open[i] || (open[k] == open[i] && k < i);
+        sorted[rank] = open[i];
+    }
+    __syncthreads();
+    if (tid == 0) {
+        int next = 0;
+        for (int j = 0; j < a; ++j)
+            if (to[j] >= 0) to[j] = sorted[next++];
+        p.c.len[u.st] = hd.n + a - job.leave;
+        p.c.free_slot[u.st] = next < count && sorted[next] < INT32_MAX ? sorted[next] : hd.C;
+    }
+    __syncthreads();
+    constexpr int kE = D / 32;
+    const int32_t* const path = p.path + (int64_t)u.b * p.T;
+    for (int j = warp; j < 2 * a; j += kWarps) {              // K and V of each row, a warp each
+        const int i = j >> 1, which = j & 1, slot = to[i];
+        if (slot < 0) continue;
+        const int64_t row = hd.first + slot;
+        const __nv_bfloat16* const from =
+            (which ? p.v : p.k) + ((((int64_t)u.li * p.c.B + u.b) * p.c.Hkv + u.h) * p.T + path[i]) * D + kE * lane;
+        uint8_t* const slab = static_cast<uint8_t*>(which ? p.c.v : p.c.k);
+        if (p.c.kv_dtype == BAKLAVA_KV_BF16) {
+            if (D == 128) *reinterpret_cast<uint2*>(slab + row * 256 + 8 * lane) = *reinterpret_cast<const uint2*>(from);
+            else *reinterpret_cast<uint32_t*>(slab + row * 128 + 4 * lane) = *reinterpret_cast<const uint32_t*>(from);
+        } else if (D == 128) {
+            const uint2 raw = *reinterpret_cast<const uint2*>(from);
+            if (p.c.kv_dtype == BAKLAVA_KV_FP8_E4M3) {
+                const float inv = p.c.kv_scale[(int64_t)u.head * 4 + 2 * which + 1];
+                const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw.x));
+                const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw.y));
+                *reinterpret_cast<uint32_t*>(slab + row * 128 + 4 * lane) =
+                    fp8::e4m3x2_from_f32(x.x * inv, x.y * inv) | (fp8::e4m3x2_from_f32(y.x * inv, y.y * inv) << 16);
+            } else {
+                float y[4];
+                int4q::scaled4(raw, *reinterpret_cast<const float4*>(p.c.kv_scale + ((int64_t)u.head * 4 + 2 * which + 1) * 128 + 4 * lane), y);
+                const float s = int4q::row_scale(__reduce_max_sync(0xffffffffu, int4q::largest_bits(y)));
+                *reinterpret_cast<uint16_t*>(slab + row * 64 + 2 * lane) = (uint16_t)int4q::codes4(y, s);
+                if (lane == 0) p.c.row_scale[2 * row + which] = s;
+            }
+        }
+        if (which == 0 && lane == 0) {
+            p.c.pos[row] = job.t0 + i;
+            p.c.score[row] = fresh[i];
+        }
+    }
+}
+
+struct CommitWorkspace {
+    size_t slot_off, fresh_off, total;
+    int subs;
+};
+CommitWorkspace layout(const baklava_plan_info* info, int32_t max_path) {
+    CommitWorkspace w;
+    w.subs = (std::max(info->chunk_tokens, 1) + kBlockRows - 1) / kBlockRows;
+    const size_t entries = (size_t)info->n_items * w.subs * (max_path + 1);
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    w.slot_off = up(entries * 8);
+    w.fresh_off = w.slot_off + up(entries * 4);
+    w.total = w.fresh_off + up((size_t)info->n_items * max_path * 4);
+    return w;
+}
+
+template <int D, int KV>
+cudaError_t launch_scores(const CommitParams& p, int n_items, cudaStream_t s) {
+    using F = Format<D, KV>;
+    const int columns = std::min((p.max_path * p.g + 7) / 8 * 8, kMaxColumns);
+    const int smem = p.scored ? columns * ((2 * D + kColumnPad) * F::kTerms + 8) : 0;
+    static std::atomic<uint64_t> configured{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !(configured.load(std::memory_order_acquire) >> dev & 1)) {
+        e = cudaFuncSetAttribute(path_scores_kernel<D, KV>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
+    }
+    path_scores_kernel<D, KV><<<dim3((unsigned)n_items, (unsigned)p.subs + 1), kThreads, smem, s>>>(p);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+extern "C" __attribute__((visibility("default"))) size_t baklava_tree_commit_workspace_size(
+        const baklava_shape* shape, const baklava_plan_info* info, int32_t max_path) {
+    if (baklava_check_shape(shape) || !info || info->n_items <= 0 || max_path <= 0 || max_path > BAKLAVA_MAX_TREE) return 0;
+    return layout(info, max_path).total;
+}
+
+extern "C" __attribute__((visibility("default"))) int baklava_tree_commit(
+        const baklava_shape* shape, const baklava_cache* cache, const void* q, const void* k, const void* v, const float* lse,
+        int32_t T, const int32_t* path, const int32_t* n_path, int32_t max_path, const int32_t* t_pos, int32_t* t_next,
+        uint32_t flags, const int32_t* items, const baklava_plan_info* info, void* ws, size_t ws_bytes, void* stream) {
+    int rc = baklava_check_shape(shape);
+    if (rc) return rc;
+    if (!cache || !k || !v || !path || !n_path || !t_pos || !items || !info || !ws || T <= 0 || max_path <= 0 || max_path > T)
+        return BAKLAVA_ERR_INVALID_ARG;
+    if (flags & ~(BAKLAVA_FLAG_NO_SCORE | BAKLAVA_FLAG_NO_EVICT)) return BAKLAVA_ERR_INVALID_ARG;
+    const bool scored = !(flags & BAKLAVA_FLAG_NO_SCORE);
+    if (scored && (!q || !lse)) return BAKLAVA_ERR_INVALID_ARG;
+    if (t_next == t_pos) return BAKLAVA_ERR_INVALID_ARG;
+    if (T > BAKLAVA_MAX_TREE) return BAKLAVA_ERR_UNSUPPORTED;
+    const void* ptrs[] = {q, k, v, items, ws};
+    for (const void* ptr : ptrs)
+        if (!baklava_aligned16(ptr)) return BAKLAVA_ERR_INVALID_ARG;
+    const void* words[] = {lse, path, n_path, t_pos, t_next};
+    for (const void* ptr : words)
+        if (reinterpret_cast<uintptr_t>(ptr) & 3u) return BAKLAVA_ERR_INVALID_ARG;
+    rc = tree_check_cache(shape, cache);
+    if (rc) return rc;
+    if (info->layer_begin < 0 || info->layer_end > shape->L || info->layer_begin >= info->layer_end || info->B != cache->B ||
+        info->n_items <= 0 || info->chunk_tokens <= 0 || info->n_units != (info->layer_end - info->layer_begin) * cache->B * shape->Hkv)
+        return BAKLAVA_ERR_INVALID_ARG;
+    const CommitWorkspace w = layout(info, max_path);
+    if (ws_bytes < w.total) return BAKLAVA_ERR_WORKSPACE;
+    // (grid.y counts 1 024-row parts of a chunk; a thread of the second kernel joins up to eight lists)
+    if (w.subs >= 65535) return BAKLAVA_ERR_UNSUPPORTED;
+
+    CommitParams p;
+    p.c = tree_slabs(shape, cache);
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.k = static_cast<const __nv_bfloat16*>(k);
+    p.v = static_cast<const __nv_bfloat16*>(v);
+    p.lse = lse;
+    p.path = path; p.n_path = n_path; p.t_pos = t_pos; p.t_next = t_next;
+    p.items = reinterpret_cast<const int4*>(items);
+    char* const base = static_cast<char*>(ws);
+    p.best_key = reinterpret_cast<unsigned long long*>(base);
+    p.best_slot = reinterpret_cast<int32_t*>(base + w.slot_off);
+    p.fresh = reinterpret_cast<float*>(base + w.fresh_off);
+    p.T = T; p.g = shape->Hq / shape->Hkv; p.D = shape->D; p.Hq = shape->Hq;
+    p.layer_begin = info->layer_begin;
+    p.max_path = max_path;
+    p.subs = w.subs;
+    p.n_sink = shape->n_sink; p.recent_num = shape->recent_num; p.recent_den = shape->recent_den;
+    p.scored = scored;
+    p.evict = !(flags & BAKLAVA_FLAG_NO_EVICT) && (scored || shape->recent_num == shape->recent_den);
+    p.scale_log2 = kLog2e / sqrtf((float)shape->D);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t e = cudaSuccess;
+    if (p.scored || p.evict) {
+        if (cache->kv_dtype == BAKLAVA_KV_FP8_E4M3) e = launch_scores<128, BAKLAVA_KV_FP8_E4M3>(p, info->n_items, s);
+        else if (cache->kv_dtype == BAKLAVA_KV_INT4) e = launch_scores<128, BAKLAVA_KV_INT4>(p, info->n_items, s);
+        else if (shape->D == 128) e = launch_scores<128, BAKLAVA_KV_BF16>(p, info->n_items, s);
+        else e = launch_scores<64, BAKLAVA_KV_BF16>(p, info->n_items, s);
+        if (e != cudaSuccess) return BAKLAVA_ERR_CUDA;
+    }
+    if (shape->D == 128) join_rows_kernel<128><<<info->n_items, kThreads, 0, s>>>(p);
+    else join_rows_kernel<64><<<info->n_items, kThreads, 0, s>>>(p);
+    return cudaGetLastError() == cudaSuccess ? BAKLAVA_OK : BAKLAVA_ERR_CUDA;
+}
