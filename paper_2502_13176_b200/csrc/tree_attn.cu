@@ -3,6 +3,8 @@
 // Two kernels.  The first reduces the chunks of the plan to partials (o, m, l) of every node and query head; the second
 // adds each node's ancestors, whose keys and values it reads itself (a path has few of them), joins the partials and
 // writes the rows.
+#include <cuda_fp16.h>
+
 #include <atomic>
 #include <cmath>
 #include <cstdint>
@@ -54,88 +56,17 @@ __device__ __forceinline__ float warp_sum(float x) {
     for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
-// the values a slab row stands for
-template <int kE>
-__device__ __forceinline__ void load_slab(const Slabs& c, int which, int64_t row, int head, int lane, float (&x)[kE]) {
-    const void* slab = which ? c.v : c.k;
-    if (c.kv_dtype == BAKLAVA_KV_BF16) {
-        load_bf16<kE>(static_cast<const __nv_bfloat16*>(slab) + row * (32 * kE), lane, x);
-    } else if (c.kv_dtype == BAKLAVA_KV_FP8_E4M3) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(slab) + row * 128 + 4 * lane);
-        uint32_t lo, hi;
-        fp8::f16x4_from_e4m3x4(w, lo, hi);
-        const float s = c.kv_scale[head * 4 + 2 * which];
-        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-        x[0] = a.x * s; x[1] = a.y * s;
-        if (kE == 4) { x[2] = b.x * s; x[3] = b.y * s; }
-    } else {
-        const uint32_t w = *reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(slab) + row * 64 + 2 * lane);
-        const float s = c.row_scale[2 * row + which];
-        const float* ch = c.kv_scale + ((int64_t)head * 4 + 2 * which) * 128 + 4 * lane;
-#pragma unroll
-        for (int e = 0; e < kE; ++e) x[e] = ((float)((w >> (4 * e)) & 15u) - 8.0f) * s * ch[e];
-    }
-}
-
-// one warp per node and query head of the group, over one chunk
-template <int D>
-__global__ void __launch_bounds__(256) tree_chunk_kernel(const __grid_constant__ TreeParams p) {
-    constexpr int kE = D / 32;
-    const int4 item = p.items[blockIdx.x];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y * 8 + warp;
-    if (row >= p.g * p.T) return;
-    const Unit u(p.c, p.layer, item.x);
-    const Head hd(p.c, u);
-    const int a = row / p.T, i = row - a * p.T;
-    const int n = nodes_of(p.n_nodes, u.b, p.T);
-    if (i >= n) return;
-    float2* const stat = p.stats + (int64_t)blockIdx.x * p.g * p.T + row;
-    if (hd.bad) {
-        if (lane == 0) {
-            atomicOr(p.c.status, BAKLAVA_STATUS_BAD_STATE);
-            *stat = make_float2(0.0f, -1.0f);
-        }
-        return;
-    }
-    float q[kE], o[kE], x[kE];
-    load_bf16<kE>(p.q + u.b * p.sq.seq + (int64_t)(u.h * p.g + a) * p.sq.head + i * p.sq.token, lane, q);
-#pragma unroll
-    for (int e = 0; e < kE; ++e) o[e] = 0.0f;
-    float m = -INFINITY, l = 0.0f;
-    const int end = min(item.y + item.z, hd.slots);
-    for (int j = item.y; j < end; ++j) {
-        if (j == hd.hole) continue;
-        load_slab<kE>(p.c, 0, hd.first + j, u.head, lane, x);
-        float s = 0.0f;
-#pragma unroll
-        for (int e = 0; e < kE; ++e) s = fmaf(q[e], x[e], s);
-        s = warp_sum(s) * p.scale_log2;
-        // (the reference stands 24 powers of two above the largest logit: sums of up to 2^24 values stay in range)
-        s -= 24.0f;
-        const float top = fmaxf(m, s + 24.0f), was = m == -INFINITY ? 0.0f : exp2f(m - top), now = s == -INFINITY ? 0.0f : exp2f(s - top);
-        load_slab<kE>(p.c, 1, hd.first + j, u.head, lane, x);
-#pragma unroll
-        for (int e = 0; e < kE; ++e) o[e] = fmaf(now, x[e], o[e] * was);
-        l = l * was + now;
-        m = top;
-    }
-    if (lane == 0) *stat = make_float2(m + 24.0f, l);
-    float* const out = p.partial + ((int64_t)blockIdx.x * p.g * p.T + row) * D + kE * lane;
-#pragma unroll
-    for (int e = 0; e < kE; ++e) out[e] = o[e];
-}
-
-
 // ---------------------------------------------------------------- slab rows on the tensor cores
 constexpr int kKeys = 128;                    // slab rows to a tile
 constexpr int kRows = 128;                    // query rows to an accumulator
 constexpr int kSoftmaxWarps = 8;              // two streams of four
-constexpr int kThreads = (2 + kSoftmaxWarps) * 32;
+constexpr int kConvertWarps = 4;
 constexpr int kItemRing = 4;
 constexpr int kMaxRedo = 8;
-constexpr int kMaxSlots = 12;
+constexpr int kMaxSlots = 13;
 constexpr uint32_t kTmemColumns = 512;
-constexpr uint32_t kOColumn = 256;            // S of the streams at columns 0 and 128, O at 256 and 384
+constexpr uint32_t kOColumn = 256;            // S of the streams at columns 0 and 128, O at 256 (R = 2: and 384)
+constexpr uint32_t kQColumn = 384;            // R = 1: the queries
 constexpr float kFinite = 3.0e38f;
 constexpr float kMaxSum = 0x1p120f;
 constexpr long long kGraceCycles = 2000000;
@@ -153,28 +84,43 @@ struct Item {
 
 struct Shared {
     uint4 answer;
-    uint64_t full[kMaxSlots], empty[kMaxSlots];
-    uint64_t s_full[2], p_ready[2], q_full, q_free, o_full, both, bar_answer, bar_item[kItemRing];
+    uint64_t full[kMaxSlots], empty[kMaxSlots], raw_full[kMaxSlots], raw_empty[kMaxSlots];
+    uint64_t s_full[2], p_ready[2], o_full[2], q_full, q_free, ref_ready, both, bar_answer, bar_item[kItemRing];
     Item item[kItemRing], redo[kMaxRedo];
     int redo_count, redo_mark[kItemRing];
     uint32_t tmem_slot;
     int abort;
-    float2 of_stream[2][kRows];               // the streams' references and sums (one accumulator's rows in two streams)
+    float ref[kRows], part[2][kRows];         // R = 1: the rows' references, the streams' sums (or maxima)
 };
 constexpr int kSharedBytes = 3072;
 static_assert(sizeof(Shared) <= kSharedBytes, "the tiles take the rest");
 
-// How an instance lies in shared memory: the query rows, then the ring of tiles, then Shared.
-template <int D, int R>
+// How an instance lies in shared memory: the query rows (R = 2), the ring of operand tiles, for quantised slabs the ring of
+// tiles as they are in the slab and the rows' scales (4 bits: beside each operand tile), then Shared.
+template <int D, int R, int KV>
 struct Layout {
+    static constexpr bool kQuantised = KV != BAKLAVA_KV_BF16;
     static constexpr int kTileBytes = kKeys * D * 2;
     static constexpr int kBoxBytes = kKeys * 128;                      // 64 elements of a tile's rows
-    static constexpr int kQBytes = R * kRows * D * 2;
+    static constexpr int kRowBytes = KV == BAKLAVA_KV_BF16 ? 2 * D : KV == BAKLAVA_KV_FP8_E4M3 ? D : D / 2;   // of the slab
+    static constexpr int kRawBytes = kKeys * kRowBytes;
+    static constexpr int kQBytes = R == 2 ? R * kRows * D * 2 : 0;
     static constexpr int kQBox = R * kRows * 128;
-    static constexpr int kSlots = D == 128 ? 7 - R : kMaxSlots;
-    static constexpr int kShared = kQBytes + kSlots * kTileBytes;
+    static constexpr int kScaleBytes = KV == BAKLAVA_KV_INT4 ? kKeys * 8 : 0;
+    static constexpr int kSlots = kQuantised ? (R == 2 ? 3 : 4) : D == 128 ? (R == 2 ? 5 : 7) : R == 2 ? 12 : 13;
+    static constexpr int kRawSlots = !kQuantised ? 0 : KV == BAKLAVA_KV_INT4 ? 10 : R == 2 ? 4 : 6;
+    static constexpr int kRing = kQBytes, kScales = kRing + kSlots * kTileBytes, kRaw = kScales + kSlots * kScaleBytes;
+    static constexpr int kShared = kRaw + kRawSlots * kRawBytes;
     static constexpr int kTotal = kShared + kSharedBytes;
+    static constexpr int kThreads = (2 + kSoftmaxWarps + (kQuantised ? kConvertWarps : 0)) * 32;
+    static constexpr bool kLoadsQ = R == 2 && !kQuantised;             // the queries come by TMA
+    static constexpr int kTerms = KV == BAKLAVA_KV_INT4 ? 2 : 1;       // 16-bit terms of a query element
     static_assert(kTotal <= 232448, "one CTA's shared memory");
+    static_assert(R == 1 || KV != BAKLAVA_KV_INT4, "queries in two terms lie in tensor memory");
+    // fp16 operands: keys of quantised slabs (codes are exact in fp16, and so are queries or their two terms), FP8 values
+    static constexpr uint32_t kBf16 = (1u << 7) | (1u << 10);
+    static constexpr uint32_t kIdescS = tc::idesc_bf16_f32(kRows, kKeys) & ~(kQuantised ? kBf16 : 0u);
+    static constexpr uint32_t kIdescPv = tc::idesc_bf16_f32_b_mn(kRows, D) & ~(KV == BAKLAVA_KV_FP8_E4M3 ? kBf16 : 0u);
 };
 
 __device__ __forceinline__ void request_block(uint32_t answer, uint32_t bar) {
@@ -196,8 +142,17 @@ __device__ __forceinline__ bool granted_block(uint32_t answer, uint32_t& x) {
         : "=r"(got), "=r"(x) : "r"(answer) : "memory");
     return got != 0;
 }
+// untiled copy of `bytes` (a multiple of 16) to shared memory
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 __device__ __forceinline__ void load_16(uint32_t taddr, uint32_t (&r)[16]) {
@@ -223,24 +178,36 @@ __device__ __forceinline__ void let_copies_land() {
 
 // What the roles know of the CTA.
 struct Cta {
-    uint32_t q_tile, ring, tmem;
-    uint8_t* ring_ptr;
+    uint32_t base, tmem;          // shared memory, tensor memory
+    uint8_t* ptr;
 };
-// Counters that run on over the items: tiles through the ring, steps of the streams, items that had work.
+// Counters that run on over the items: tiles through the rings, steps of the streams, items that had work.
 struct Count {
     uint32_t entry = 0, step[2] = {0, 0}, work = 0, both = 0;
 };
 enum Mode { kFast, kMaxima, kExact };
 
-// Tiles pass through the ring in the order in which the tensor core takes them.  A step is one S = Q K^T and one O += P V of
-// one stream; step n belongs to stream n & 1.  With two accumulators (R = 2) a stream is an accumulator, and both take every
-// tile; with one, the streams take the tiles in turn, each with its own O.  S(n + 2) follows P V (n).
+// Tiles pass through the rings in the order in which the tensor core takes them.  A step is one S = Q K^T and one O += P V of
+// one stream of four softmax warps; step n belongs to stream n & 1, and S(n + 2) follows P V (n).  With two accumulators of
+// query rows (R = 2) a stream is an accumulator, and both take every tile; with one, the streams take the tiles in turn.
 template <int R>
 __device__ __forceinline__ int tile_of(int step) { return R == 2 ? step >> 1 : step; }
 template <int R, int kMode>
 __device__ __forceinline__ uint32_t key_entry(int t) { return kMode == kMaxima ? t : R == 2 ? 2 * t : t == 0 ? 0 : 2 * t - 1; }
 template <int R>
 __device__ __forceinline__ uint32_t value_entry(int t, int tiles) { return R == 2 || t == tiles - 1 ? 2 * t + 1 : 2 * t + 2; }
+// the other way round: entry e of an item is the key or value tile t
+template <int R, int kMode>
+__device__ __forceinline__ bool entry_is_value(int e, int tiles, int& t) {
+    if (kMode == kMaxima) { t = e; return false; }
+    if (R == 2) { t = e >> 1; return e & 1; }
+    if (e == 2 * tiles - 1) { t = tiles - 1; return true; }
+    if (e == 0 || (e & 1)) { t = (e + 1) >> 1; return false; }
+    t = (e - 2) >> 1;
+    return true;
+}
+template <int kMode>
+__device__ __forceinline__ int entries_of(const Item& it) { return kMode == kMaxima ? it.tiles : 2 * it.tiles; }
 
 // The plan's item (and part of the group) that block number x stands for.  One thread; notes what is to be said of it if
 // nothing else will be: skipped, or empty.
@@ -271,65 +238,73 @@ __device__ __forceinline__ Item find_item(const TreeParams& p, uint32_t x) {
 // An item that was lost: its rows are not written.  The whole CTA.
 __device__ __forceinline__ void note_lost(const TreeParams& p, const Item& it) {
     if (it.index < 0 || it.tiles == 0) return;
-    for (int i = threadIdx.x; i < it.heads * p.T; i += kThreads) p.stats[((int64_t)it.index * p.g + it.a0) * p.T + i] = make_float2(0.0f, -1.0f);
+    for (int i = threadIdx.x; i < it.heads * p.T; i += blockDim.x) p.stats[((int64_t)it.index * p.g + it.a0) * p.T + i] = make_float2(0.0f, -1.0f);
 }
 
 // ---------------------------------------------------------------- the producer
-template <int D, int R, int kMode>
-__device__ __forceinline__ bool load_entry(const TreeParams&, Shared& sm, const Cta& cta, const Item& it, uint32_t base, int e,
+template <int D, int R, int KV, int kMode>
+__device__ __forceinline__ bool load_entry(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, uint32_t base, int e,
                                            const CUtensorMap& k_map, const CUtensorMap& v_map) {
-    using L = Layout<D, R>;
-    const uint32_t n = base + e, slot = n % L::kSlots;
-    if (!ptx::mbar_wait(ptx::smem_u32(&sm.empty[slot]), (n / L::kSlots & 1) ^ 1)) return false;
-    bool value;
+    using L = Layout<D, R, KV>;
     int t;
-    if (kMode == kMaxima) { value = false; t = e; }
-    else if (R == 2) { value = e & 1; t = e >> 1; }
-    else if (e == 2 * it.tiles - 1) { value = true; t = it.tiles - 1; }
-    else if (e == 0 || (e & 1)) { value = false; t = (e + 1) >> 1; }
-    else { value = true; t = (e - 2) >> 1; }
-    const uint32_t bar = ptx::smem_u32(&sm.full[slot]), dst = cta.ring + slot * L::kTileBytes;
-    ptx::mbar_arrive_expect_tx(bar, L::kTileBytes);
+    const bool value = entry_is_value<R, kMode>(e, it.tiles, t);
+    const uint32_t n = base + e;
+    if (L::kQuantised) {
+        const uint32_t slot = n % L::kRawSlots, bar = ptx::smem_u32(&sm.raw_full[slot]);
+        if (!ptx::mbar_wait(ptx::smem_u32(&sm.raw_empty[slot]), (n / L::kRawSlots & 1) ^ 1)) return false;
+        const uint32_t bytes = min(kKeys, it.keys - t * kKeys) * L::kRowBytes;
+        ptx::mbar_arrive_expect_tx(bar, bytes);
+        bulk_load(cta.base + L::kRaw + slot * L::kRawBytes,
+                  static_cast<const uint8_t*>(value ? p.c.v : p.c.k) + ((int64_t)it.first + t * kKeys) * L::kRowBytes, bytes, bar);
+    } else {
+        const uint32_t slot = n % L::kSlots, bar = ptx::smem_u32(&sm.full[slot]), dst = cta.base + L::kRing + slot * L::kTileBytes;
+        if (!ptx::mbar_wait(ptx::smem_u32(&sm.empty[slot]), (n / L::kSlots & 1) ^ 1)) return false;
+        ptx::mbar_arrive_expect_tx(bar, L::kTileBytes);
 #pragma unroll
-    for (int bx = 0; bx < D / 64; ++bx)
-        ptx::tma_load_4d(dst + bx * L::kBoxBytes, value ? &v_map : &k_map, bx * 64, it.first + t * kKeys, 0, 0, bar);
+        for (int bx = 0; bx < D / 64; ++bx)
+            ptx::tma_load_4d(dst + bx * L::kBoxBytes, value ? &v_map : &k_map, bx * 64, it.first + t * kKeys, 0, 0, bar);
+    }
     return true;
 }
-template <int D, int R>
+template <int D, int R, int KV>
 __device__ __forceinline__ void load_queries(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, const CUtensorMap& q_map) {
-    using L = Layout<D, R>;
+    using L = Layout<D, R, KV>;
     const uint32_t bar = ptx::smem_u32(&sm.q_full);
     ptx::mbar_arrive_expect_tx(bar, (uint32_t)(it.heads * p.rows_per_head * D * 2));
     for (int a = 0; a < it.heads; ++a)
 #pragma unroll
         for (int bx = 0; bx < D / 64; ++bx)
-            ptx::tma_load_4d(cta.q_tile + bx * L::kQBox + a * p.rows_per_head * 128, &q_map, bx * 64, 0, it.h * p.g + it.a0 + a, it.b, bar);
+            ptx::tma_load_4d(cta.base + bx * L::kQBox + a * p.rows_per_head * 128, &q_map, bx * 64, 0, it.h * p.g + it.a0 + a, it.b, bar);
 }
-template <int D, int R>
+template <int D, int R, int KV>
 __device__ __forceinline__ void produce(const TreeParams& p, Shared& sm, const Cta& cta, Item it, const CUtensorMap& q_map,
                                         const CUtensorMap& k_map, const CUtensorMap& v_map) {
-    using L = Layout<D, R>;
+    using L = Layout<D, R, KV>;
     const uint32_t answer = ptx::smem_u32(&sm.answer), bar_answer = ptx::smem_u32(&sm.bar_answer);
+    constexpr int kAhead = L::kQuantised ? L::kRawSlots : L::kSlots;
     Count c;
     bool ok = true, more = true;
     uint32_t asked = 0;
     for (int k = 0; ok; ++k) {
+        // a block in the list of those to redo may come from the two items before this one, from it and from the next
         const bool ask = more && *(volatile int*)&sm.redo_count + 4 <= kMaxRedo;
         if (ask) request_block(answer, bar_answer);
         const int total = 2 * it.tiles;
         int e = 0;
         if (total > 0) {
-            // the queries' place is free once the last S of the item before has been formed
-            if (c.work > 0) ok = ptx::mbar_wait(ptx::smem_u32(&sm.q_free), (c.work - 1) & 1);
-            if (!ok) break;
-            load_queries<D, R>(p, sm, cta, it, q_map);
-            for (; e < min(total, L::kSlots) && ok; ++e) ok = load_entry<D, R, kFast>(p, sm, cta, it, c.entry, e, k_map, v_map);
+            // never more than two items ahead of the tensor core
+            if (c.work > 1) ok = ptx::mbar_wait(ptx::smem_u32(&sm.o_full[c.work & 1]), ((c.work - 2) >> 1) & 1);
+            if (L::kLoadsQ) {
+                // the queries' place is free once the last S of the item before has been formed
+                if (ok && c.work > 0) ok = ptx::mbar_wait(ptx::smem_u32(&sm.q_free), (c.work - 1) & 1);
+                if (ok) load_queries<D, R, KV>(p, sm, cta, it, q_map);
+            }
+            for (; e < min(total, kAhead) && ok; ++e) ok = load_entry<D, R, KV, kFast>(p, sm, cta, it, c.entry, e, k_map, v_map);
             if (!ok) break;
         }
-        // the next item, while these are under way
+        // the next item, while these are under way (those without work are done with here)
         Item next = it;
         next.index = -1;
-        // (those without work are done with here: the items handed on are never more than a few ahead of the other roles)
         for (bool waiting = ask; waiting && ok;) {
             uint32_t x = 0;
             ok = ptx::mbar_wait(bar_answer, asked++ & 1);
@@ -344,7 +319,7 @@ __device__ __forceinline__ void produce(const TreeParams& p, Shared& sm, const C
         more = next.index >= 0;
         sm.item[k % kItemRing] = next;
         tc::mbar_arrive(ptx::smem_u32(&sm.bar_item[k % kItemRing]));
-        for (; e < total && ok; ++e) ok = load_entry<D, R, kFast>(p, sm, cta, it, c.entry, e, k_map, v_map);
+        for (; e < total && ok; ++e) ok = load_entry<D, R, KV, kFast>(p, sm, cta, it, c.entry, e, k_map, v_map);
         if (!more) break;
         c.entry += total;
         c.work += total > 0;
@@ -353,41 +328,130 @@ __device__ __forceinline__ void produce(const TreeParams& p, Shared& sm, const C
     if (!ok) sm.abort = 1;
 }
 
-// ---------------------------------------------------------------- the tensor core's thread
-template <int D, int R>
-__device__ __forceinline__ void issue_s(const Cta& cta, int stream, uint32_t slot) {
-    using L = Layout<D, R>;
-    constexpr uint32_t idesc = tc::idesc_bf16_f32(kRows, kKeys);
-    const uint64_t dq = tc::desc_k_major_sw128(cta.q_tile + (R == 2 ? stream * kRows * 128 : 0));
-    const uint64_t dk = tc::desc_k_major_sw128(cta.ring + slot * L::kTileBytes);
+// ---------------------------------------------------------------- quantised rows into operand tiles
+// A lane takes 16 bytes of a row.  FP8: 16 codes, 32 bytes of fp16.  4 bits: 32 codes, 64 bytes; a word's nibbles i and i + 4
+// make a pair, so that an operand's eight elements are dimensions 0, 4, 1, 5, 2, 6, 3, 7 of eight (queries and output rows are
+// ordered to match).  The pieces go to their places under the 128-byte swizzle, in an order that keeps eight lanes on
+// different banks.
+template <int D, int R, int KV, int kMode>
+__device__ __forceinline__ bool convert_item(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, Count& c, int warp, int lane) {
+    using L = Layout<D, R, KV>;
+    constexpr int kLanes = L::kRowBytes / 16, kStep = 32 / kLanes;     // lanes to a row, rows to a warp's step
+    const int w = warp - 2 - kSoftmaxWarps, piece = lane % kLanes;
+    const int entries = entries_of<kMode>(it);
+    for (int e = 0; e < entries; ++e) {
+        int t;
+        const bool value = entry_is_value<R, kMode>(e, it.tiles, t);
+        const uint32_t n = c.entry + e, slot = n % L::kSlots, raw = n % L::kRawSlots;
+        const int keys = it.keys - t * kKeys, no_row = it.hole >= 0 ? it.hole - t * kKeys : -1;
+        float2 scale = make_float2(0.0f, 0.0f);
+        const int scale_row = w * 32 + lane;
+        if (KV == BAKLAVA_KV_INT4 && value && scale_row < keys && scale_row != no_row)
+            scale = *reinterpret_cast<const float2*>(p.c.row_scale + 2 * ((int64_t)it.first + t * kKeys + scale_row));
+        if (!ptx::mbar_wait(ptx::smem_u32(&sm.raw_full[raw]), n / L::kRawSlots & 1)) return false;
+        if (!ptx::mbar_wait(ptx::smem_u32(&sm.empty[slot]), (n / L::kSlots & 1) ^ 1)) return false;
+        __syncwarp();
+        const uint8_t* const from = cta.ptr + L::kRaw + raw * L::kRawBytes;
+        uint8_t* const to = cta.ptr + L::kRing + slot * L::kTileBytes;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-        tc::umma_bf16(cta.tmem + stream * kKeys, dq + (((ks >> 2) * L::kQBox + (ks & 3) * 32) >> 4),
-                      dk + (((ks >> 2) * L::kBoxBytes + (ks & 3) * 32) >> 4), idesc, ks > 0);
+        for (int i = 0; i < 32 / kStep; ++i) {                // a warp has 32 of the tile's rows
+            const int row = w * 32 + i * kStep + lane / kLanes;
+            const bool here = row < keys && row != no_row;
+            uint4 x = *reinterpret_cast<const uint4*>(from + row * L::kRowBytes + piece * 16);
+            uint8_t* const at = to + row * 128;
+            auto place = [&](int chunk) { return reinterpret_cast<uint4*>(at + (chunk >> 3) * L::kBoxBytes + (((chunk & 7) ^ (row & 7)) << 4)); };
+            if (KV == BAKLAVA_KV_FP8_E4M3) {
+                if (!here) x = make_uint4(0, 0, 0, 0);
+                uint4 y[2];
+                fp8::f16x4_from_e4m3x4(x.x, y[0].x, y[0].y);
+                fp8::f16x4_from_e4m3x4(x.y, y[0].z, y[0].w);
+                fp8::f16x4_from_e4m3x4(x.z, y[1].x, y[1].y);
+                fp8::f16x4_from_e4m3x4(x.w, y[1].z, y[1].w);
+                const int swap = piece >> 2;
+                *place(2 * piece + swap) = swap ? y[1] : y[0];
+                *place(2 * piece + 1 - swap) = swap ? y[0] : y[1];
+            } else {
+                if (!here) x = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
+                const uint32_t word[4] = {x.x, x.y, x.z, x.w};
+                uint4 y[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t z[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t nib = (word[k] >> (4 * q)) & 0x000f000fu;
+                        if (value) {                          // bf16: 128 + code, less 136
+                            const uint32_t m = nib | 0x43004300u;
+                            const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&m), __float2bfloat162_rn(136.0f));
+                            z[q] = *reinterpret_cast<const uint32_t*>(&v);
+                        } else {                              // fp16: 1024 + code, less 1032
+                            const uint32_t m = nib | 0x64006400u;
+                            const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&m), __half2half2(__ushort_as_half(0x6408)));
+                            z[q] = *reinterpret_cast<const uint32_t*>(&v);
+                        }
+                    }
+                    y[k] = make_uint4(z[0], z[1], z[2], z[3]);
+                }
+                const int swap = piece & 2;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) *place(4 * piece + (k ^ swap)) = swap ? y[k ^ 2] : y[k];
+            }
+        }
+        if (KV == BAKLAVA_KV_INT4 && value)
+            *reinterpret_cast<float2*>(cta.ptr + L::kScales + slot * L::kScaleBytes + scale_row * 8) = scale;
+        tc::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            tc::mbar_arrive(ptx::smem_u32(&sm.full[slot]));
+            tc::mbar_arrive(ptx::smem_u32(&sm.raw_empty[raw]));
+        }
+    }
+    c.entry += entries;
+    return true;
 }
-template <int D, int R>
+
+// ---------------------------------------------------------------- the tensor core's thread
+template <int D, int R, int KV>
+__device__ __forceinline__ void issue_s(const Cta& cta, int stream, uint32_t slot) {
+    using L = Layout<D, R, KV>;
+    const uint64_t dk = tc::desc_k_major_sw128(cta.base + L::kRing + slot * L::kTileBytes);
+    if (R == 1) {
+#pragma unroll
+        for (int term = 0; term < L::kTerms; ++term)
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks)
+                tc::umma_bf16_ts(cta.tmem + stream * kKeys, cta.tmem + kQColumn + term * (D / 2) + ks * 8,
+                                 dk + (((ks >> 2) * L::kBoxBytes + (ks & 3) * 32) >> 4), L::kIdescS, term + ks > 0);
+    } else {
+        const uint64_t dq = tc::desc_k_major_sw128(cta.base + stream * kRows * 128);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+            tc::umma_bf16(cta.tmem + stream * kKeys, dq + (((ks >> 2) * L::kQBox + (ks & 3) * 32) >> 4),
+                          dk + (((ks >> 2) * L::kBoxBytes + (ks & 3) * 32) >> 4), L::kIdescS, ks > 0);
+    }
+}
+template <int D, int R, int KV>
 __device__ __forceinline__ void issue_pv(const Cta& cta, int stream, uint32_t slot, bool accumulate) {
-    using L = Layout<D, R>;
-    constexpr uint32_t idesc = tc::idesc_bf16_f32_b_mn(kRows, D);
-    const uint64_t dv = tc::desc_mn_major_sw128(cta.ring + slot * L::kTileBytes, L::kBoxBytes);
+    using L = Layout<D, R, KV>;
+    const uint64_t dv = tc::desc_mn_major_sw128(cta.base + L::kRing + slot * L::kTileBytes, L::kBoxBytes);
 #pragma unroll
     for (int ks = 0; ks < kKeys / 16; ++ks)
-        tc::umma_bf16_ts(cta.tmem + kOColumn + stream * 128, cta.tmem + stream * kKeys + ks * 8, dv + (ks * 2048 >> 4), idesc,
-                         accumulate || ks > 0);
+        tc::umma_bf16_ts(cta.tmem + kOColumn + (R == 2 ? stream * 128 : 0), cta.tmem + stream * kKeys + ks * 8, dv + (ks * 2048 >> 4),
+                         L::kIdescPv, accumulate || ks > 0);
 }
-template <int D, int R, int kMode>
+template <int D, int R, int KV, int kMode>
 __device__ __forceinline__ bool issue_item(Shared& sm, const Cta& cta, const Item& it, Count& c) {
-    using L = Layout<D, R>;
+    using L = Layout<D, R, KV>;
     const int steps = it.tiles * R;
     auto full = [&](uint32_t n) { return ptx::mbar_wait(ptx::smem_u32(&sm.full[n % L::kSlots]), n / L::kSlots & 1); };
     auto form_s = [&](int n) {
         const uint32_t entry = c.entry + key_entry<R, kMode>(tile_of<R>(n)), slot = entry % L::kSlots;
         if (!full(entry)) return false;
         tc::fence_after_sync();
-        issue_s<D, R>(cta, n & 1, slot);
+        issue_s<D, R, KV>(cta, n & 1, slot);
         tc::umma_commit(ptx::smem_u32(&sm.s_full[n & 1]));
         if (R == 1 || (n & 1)) tc::umma_commit(ptx::smem_u32(&sm.empty[slot]));
-        if (n == steps - 1) tc::umma_commit(ptx::smem_u32(&sm.q_free));
+        if (L::kLoadsQ && n == steps - 1) tc::umma_commit(ptx::smem_u32(&sm.q_free));
         return true;
     };
     if (!ptx::mbar_wait(ptx::smem_u32(&sm.q_full), c.work & 1)) return false;
@@ -400,25 +464,130 @@ __device__ __forceinline__ bool issue_item(Shared& sm, const Cta& cta, const Ite
             const uint32_t entry = c.entry + value_entry<R>(tile_of<R>(n), it.tiles), slot = entry % L::kSlots;
             if (!full(entry)) return false;
             tc::fence_after_sync();
-            issue_pv<D, R>(cta, stream, slot, n >= 2);
+            issue_pv<D, R, KV>(cta, stream, slot, n >= R);
             if (R == 1 || stream == 1) tc::umma_commit(ptx::smem_u32(&sm.empty[slot]));
-            if (n == steps - 1) tc::umma_commit(ptx::smem_u32(&sm.o_full));
+            if (n == steps - 1) tc::umma_commit(ptx::smem_u32(&sm.o_full[c.work & 1]));
         } else {
             tc::fence_after_sync();
         }
         if (n + 2 < steps && !form_s(n + 2)) return false;
     }
-    c.entry += kMode == kMaxima ? it.tiles : 2 * it.tiles;
+    c.entry += entries_of<kMode>(it);
     ++c.work;
     return true;
 }
 
 // ---------------------------------------------------------------- the softmax warps
+// A thread's query row: its stream's (R = 2), or the one that it shares with the other stream's thread (R = 1).
+struct Row {
+    int a, node;
+    bool there;
+    __device__ __forceinline__ Row(const TreeParams& p, const Item& it, int full_row) {
+        a = full_row / p.rows_per_head;
+        node = full_row - a * p.rows_per_head;
+        there = a < it.heads && node < it.nodes;
+    }
+};
+template <int D, int R, int KV>
+__device__ __forceinline__ float query_factor(const TreeParams& p, const Item& it) {
+    return KV == BAKLAVA_KV_FP8_E4M3 ? p.scale_log2 * p.c.kv_scale[((int64_t)p.layer * p.c.Hkv + it.h) * 4] : p.scale_log2;
+}
+// What of its row a thread puts into the operand: with R = 1 half of it (the streams share the row), else all.
+template <int D, int R>
+constexpr int kHeldPieces = D / 8 / (R == 1 ? 2 : 1);
+template <int D, int R>
+__device__ __forceinline__ void fetch_queries(const TreeParams& p, const Item& it, const Row& r, int stream, uint4 (&held)[kHeldPieces<D, R>]) {
+    const __nv_bfloat16* const row = p.q + it.b * p.sq.seq + (int64_t)(it.h * p.g + it.a0 + r.a) * p.sq.head + r.node * p.sq.token;
+#pragma unroll
+    for (int i = 0; i < kHeldPieces<D, R>; ++i)
+        held[i] = r.there ? *reinterpret_cast<const uint4*>(row + 8 * (i + (R == 1 ? stream * kHeldPieces<D, R> : 0))) : make_uint4(0, 0, 0, 0);
+}
+// The queries as operand: R = 1 into tensor memory, R = 2 (FP8) into shared memory.  `factor`: what an S has to be multiplied
+// with besides its key's scale, for base-2 logits.
+template <int D, int R, int KV>
+__device__ __forceinline__ void place_queries(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, const Row& r, int stream, int full_row,
+                                              uint32_t lane_addr, int lane, const uint4 (&held)[kHeldPieces<D, R>], float& factor) {
+    using L = Layout<D, R, KV>;
+    factor = query_factor<D, R, KV>(p, it);
+    float back = 1.0f;
+    const float* const chan = p.c.kv_scale + ((int64_t)p.layer * p.c.Hkv + it.h) * 4 * D;      // 4 bits: the K channels' scales
+    if (KV == BAKLAVA_KV_INT4) {
+        // times the channels' scales, brought to 2^14 .. 2^15 by a power of two, in two fp16 terms: 22 bits of the largest
+        float big = 0.0f;
+        if (r.there) {
+            const __nv_bfloat16* const row = p.q + it.b * p.sq.seq + (int64_t)(it.h * p.g + it.a0 + r.a) * p.sq.head + r.node * p.sq.token;
+#pragma unroll 4
+            for (int i = 0; i < D / 2; ++i) {
+                const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(row + 2 * i));
+                const float2 s = *reinterpret_cast<const float2*>(chan + 2 * i);
+                big = fmaxf(big, fmaxf(fabsf(x.x * s.x), fabsf(x.y * s.y)));
+            }
+        }
+        int power;
+        frexpf(big, &power);
+        power = big > 0.0f && big < INFINITY ? max(power - 15, -100) : 0;                   // (rows below 2^-86 are held less exactly)
+        factor = ldexpf(factor, power);
+        back = ldexpf(1.0f, -power);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kHeldPieces<D, R>; i += 2) {
+        uint32_t w[8], low[8];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t raw[4] = {held[i + k].x, held[i + k].y, held[i + k].z, held[i + k].w};
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw[j]));
+                x[2 * j] = f.x; x[2 * j + 1] = f.y;
+            }
+            if (KV == BAKLAVA_KV_INT4) {
+                const int d0 = 8 * (i + k + stream * kHeldPieces<D, R>);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] *= chan[d0 + j] * back;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {                 // nibbles j and j + 4 of a word are a pair
+                    w[4 * k + j] = pack_f16(x[j], x[j + 4]);
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[4 * k + j]));
+                    low[4 * k + j] = pack_f16(x[j] - f.x, x[j + 4] - f.y);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[4 * k + j] = KV == BAKLAVA_KV_BF16 ? raw[j] : pack_f16(x[2 * j], x[2 * j + 1]);
+            }
+        }
+        if (R == 1) {
+            const uint32_t column = lane_addr + kQColumn + stream * (D / 4) + i * 4;
+            store_8(column, w);
+            if (L::kTerms == 2) store_8(column + D / 2, low);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                *reinterpret_cast<uint4*>(cta.ptr + ((i + k) >> 3) * L::kQBox + full_row * 128 + ((((i + k) & 7) ^ (full_row & 7)) << 4)) =
+                    make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+        }
+    }
+    if (R == 1) tc::tmem_st_wait();
+    else tc::fence_proxy_async_smem();
+    tc::fence_before_sync();
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.q_full));
+}
+
 // Sixteen logits -> eight columns of probabilities.  kMasked: keys first .. first + 15 of the tile, of which those at or
-// behind `keys` and `hole` are no rows.
-template <bool kMasked>
-__device__ __forceinline__ void softmax_16(uint32_t (&v)[16], uint32_t column, int first, int keys, int hole, ptx::f32x2 scale2,
-                                           ptx::f32x2 minus, ptx::f32x2 (&sum)[2]) {
+// behind `keys` and `hole` are no rows.  4 bits: `scales` are the rows' (K, V) pairs; a probability takes its value row's scale.
+template <int KV, bool kMasked>
+__device__ __forceinline__ void softmax_16(uint32_t (&v)[16], uint32_t column, int first, int keys, int hole, const float4* scales,
+                                           ptx::f32x2 scale2, ptx::f32x2 minus, ptx::f32x2 (&sum)[2]) {
+    if (KV == BAKLAVA_KV_INT4) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const float4 s = scales[(first >> 1) + c];
+            v[2 * c] = __float_as_uint(__uint_as_float(v[2 * c]) * s.x);
+            v[2 * c + 1] = __float_as_uint(__uint_as_float(v[2 * c + 1]) * s.z);
+        }
+    }
     if (kMasked) {
 #pragma unroll
         for (int c = 0; c < 16; ++c)
@@ -428,16 +597,21 @@ __device__ __forceinline__ void softmax_16(uint32_t (&v)[16], uint32_t column, i
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
         const float2 x = ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1])), scale2, minus));
-        const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
+        float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
         sum[c & 1] = ptx::add2(sum[c & 1], ptx::pack2(p0, p1));
-        w[c] = pack_bf16(p0, p1);
+        if (KV == BAKLAVA_KV_INT4) {
+            const float4 s = scales[(first >> 1) + c];
+            p0 *= s.y;
+            p1 *= s.w;
+        }
+        w[c] = KV == BAKLAVA_KV_FP8_E4M3 ? pack_f16(p0, p1) : pack_bf16(p0, p1);
     }
     store_8(column, w);
 }
 // A row's 128 logits of a tile: sixteen are asked for while the sixteen before are worked on.  Probabilities take the place
 // of logits that have been read.
-template <bool kMasked>
-__device__ __forceinline__ void softmax_row(uint32_t column, int keys, int hole, float scale, float ref, ptx::f32x2 (&sum)[2]) {
+template <int KV, bool kMasked>
+__device__ __forceinline__ void softmax_row(uint32_t column, int keys, int hole, const float4* scales, float scale, float ref, ptx::f32x2 (&sum)[2]) {
     const ptx::f32x2 scale2 = ptx::pack2(scale, scale), minus = ptx::pack2(-ref, -ref);
     uint32_t a[16], b[16];
     load_16(column, a);
@@ -445,34 +619,33 @@ __device__ __forceinline__ void softmax_row(uint32_t column, int keys, int hole,
     for (int c = 0; c < kKeys; c += 32) {
         tc::tmem_ld_wait();
         load_16(column + c + 16, b);
-        softmax_16<kMasked>(a, column + c / 2, c, keys, hole, scale2, minus, sum);
+        softmax_16<KV, kMasked>(a, column + c / 2, c, keys, hole, scales, scale2, minus, sum);
         tc::tmem_ld_wait();
         if (c + 32 < kKeys) load_16(column + c + 32, a);
-        softmax_16<kMasked>(b, column + c / 2 + 8, c + 16, keys, hole, scale2, minus, sum);
+        softmax_16<KV, kMasked>(b, column + c / 2 + 8, c + 16, keys, hole, scales, scale2, minus, sum);
     }
     tc::tmem_st_wait();
 }
 // What holds no row becomes zeros in the value tile (its probability is zero, but 0 times NaN is not).
-template <int D, int R>
+template <int D, int R, int KV>
 __device__ __forceinline__ void clear_value_row(uint8_t* tile, int row) {
 #pragma unroll 1
     for (int c = 0; c < D / 8; ++c)
-        *reinterpret_cast<uint4*>(tile + (c >> 3) * Layout<D, R>::kBoxBytes + row * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(tile + (c >> 3) * Layout<D, R, KV>::kBoxBytes + row * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
     tc::fence_proxy_async_smem();
 }
 
-// One item's rows: this thread's row of its stream.  kMaxima: `ref` becomes the row's largest logit, raised so that sums of
-// that many probabilities stay below one.
-template <int D, int R, int kMode>
+// One item's rows.  kMaxima: `ref` becomes the row's largest logit, raised so that the sum of that many probabilities stays
+// below one.  `before_end` is called when the last tile has been worked on.
+template <int D, int R, int KV, int kMode, typename F>
 __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, Count& c, int warp, int lane,
-                                            float& ref, bool& again) {
-    using L = Layout<D, R>;
+                                            float factor, float& ref, bool& again, F before_end) {
+    using L = Layout<D, R, KV>;
     const int stream = (warp - 2) >> 2, quarter = warp & 3, row = 32 * quarter + lane;
-    const int full_row = R == 2 ? stream * kRows + row : row;          // among the CTA's query rows
-    const int a = full_row / p.rows_per_head, node = full_row - a * p.rows_per_head;
-    const int64_t at = ((int64_t)it.index * p.g + it.a0 + a) * p.T + node;
+    const Row r(p, it, R == 2 ? stream * kRows + row : row);
+    const int64_t at = ((int64_t)it.index * p.g + it.a0 + r.a) * p.T + r.node;
     // (done again, a row is written only if it was marked: the others stay what they are whatever happened to this one)
-    const bool there = a < it.heads && node < it.nodes && (kMode == kFast || p.stats[at].y == INFINITY);
+    const bool there = r.there && (kMode == kFast || p.stats[at].y == INFINITY);
     const bool busy = __any_sync(0xffffffffu, there);                  // (a warp without rows leaves its part of P as it is)
     const uint32_t lane_addr = cta.tmem + ((uint32_t)(32 * quarter) << 16), column = lane_addr + stream * kKeys;
     const int steps = it.tiles * R;
@@ -482,7 +655,11 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
         const int t = tile_of<R>(n), keys = it.keys - t * kKeys, hole = it.hole - t * kKeys;
         const bool masked = keys < kKeys || (it.hole >= 0 && hole >= 0 && hole < kKeys);
         const int no_row = it.hole >= 0 ? hole : -1;
+        const uint32_t entry = c.entry + value_entry<R>(t, it.tiles), slot = entry % L::kSlots;
+        const float4* const scales = reinterpret_cast<const float4*>(cta.ptr + L::kScales + slot * L::kScaleBytes);
         if (!ptx::mbar_wait(ptx::smem_u32(&sm.s_full[stream]), c.step[stream]++ & 1)) return false;
+        if (kMode != kMaxima && (KV == BAKLAVA_KV_INT4 || (!L::kQuantised && masked && (R == 1 || stream == 0))))
+            if (!ptx::mbar_wait(ptx::smem_u32(&sm.full[slot]), entry / L::kSlots & 1)) return false;
         __syncwarp();
         tc::fence_after_sync();
         if (kMode == kMaxima) {
@@ -494,18 +671,20 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
                     tc::tmem_ld_wait();
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        if (k + e < keys && k + e != no_row) largest = fmaxf(largest, __uint_as_float(v[e]));
+                        if (k + e < keys && k + e != no_row) {
+                            float s = __uint_as_float(v[e]);
+                            if (KV == BAKLAVA_KV_INT4) s *= p.c.row_scale[2 * ((int64_t)it.first + t * kKeys + k + e)];
+                            largest = fmaxf(largest, s * factor);
+                        }
                 }
             }
         } else {
-            if (masked && (R == 1 || stream == 0)) {
-                const uint32_t entry = c.entry + value_entry<R>(t, it.tiles), slot = entry % L::kSlots;
-                if (!ptx::mbar_wait(ptx::smem_u32(&sm.full[slot]), entry / L::kSlots & 1)) return false;
-                if (row >= keys || row == no_row) clear_value_row<D, R>(cta.ring_ptr + slot * L::kTileBytes, row);
+            if (!L::kQuantised && masked && (R == 1 || stream == 0)) {
+                if (row >= keys || row == no_row) clear_value_row<D, R, KV>(cta.ptr + L::kRing + slot * L::kTileBytes, row);
                 __syncwarp();
             }
             if (busy) {
-                if (kMode == kFast && n == stream) {
+                if (kMode == kFast && n == stream && (R == 2 || stream == 0)) {
                     // the stabiliser need not be the maximum: the largest of the first eight rows will do
                     uint32_t v[8];
                     tc::tmem_ld_32x32_x8(column, v);
@@ -513,80 +692,97 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
                     float top = -INFINITY;
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (e < keys && e != no_row) top = fmaxf(top, __uint_as_float(v[e]));
-                    ref = top == -INFINITY ? 0.0f : top * p.scale_log2;
+                        if (e < keys && e != no_row) {
+                            float s = __uint_as_float(v[e]);
+                            if (KV == BAKLAVA_KV_INT4) s *= reinterpret_cast<const float*>(scales)[2 * e];
+                            top = fmaxf(top, s * factor);
+                        }
+                    ref = top == -INFINITY ? 0.0f : top;
                 }
-                if (masked) softmax_row<true>(column, keys, no_row, p.scale_log2, ref, sum);
-                else softmax_row<false>(column, keys, no_row, p.scale_log2, ref, sum);
+                if (kMode == kFast && R == 1 && n == stream) {          // stream 1 takes stream 0's
+                    if (stream == 0) {
+                        sm.ref[row] = ref;
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.ref_ready));
+                    } else {
+                        if (!ptx::mbar_wait(ptx::smem_u32(&sm.ref_ready), c.work & 1)) return false;
+                        __syncwarp();
+                        ref = sm.ref[row];
+                    }
+                }
+                if (masked) softmax_row<KV, true>(column, keys, no_row, scales, factor, ref, sum);
+                else softmax_row<KV, false>(column, keys, no_row, scales, factor, ref, sum);
+            } else if (kMode == kFast && R == 1 && n == 0) {
+                if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.ref_ready));
             }
         }
         tc::fence_before_sync();
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.p_ready[stream]));
     }
-    c.entry += kMode == kMaxima ? it.tiles : 2 * it.tiles;
+    c.entry += entries_of<kMode>(it);
     ++c.work;
-    if (kMode == kMaxima) {
-        ref = largest == -INFINITY ? 0.0f : largest * p.scale_log2 + (float)(32 - __clz(it.keys));
-        return true;
-    }
-    const float2 halves = ptx::unpack2(ptx::add2(sum[0], sum[1]));
-    float l = halves.x + halves.y;
-    float* const out = p.partial + at * D;
-    float mine = 1.0f, other = 0.0f, top = l == 0.0f ? -INFINITY : ref;      // (no row of weight: the reference means nothing)
     // the softmax warps wait for one another
     auto together = [&] {
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.both));
         return ptx::mbar_wait(ptx::smem_u32(&sm.both), c.both++ & 1);
     };
-    if (R == 1) {
-        // both streams hold a part of every row: they share the columns
-        sm.of_stream[stream][row] = make_float2(top, l);
-        if (!together()) return false;
-        const float2 s0 = sm.of_stream[0][row], s1 = sm.of_stream[1][row];
-        again = !(s0.y <= kMaxSum) || !(s1.y <= kMaxSum);
-        top = fmaxf(s0.x, s1.x);
-        mine = s0.x == -INFINITY ? 0.0f : exp2f(s0.x - top);
-        other = s1.x == -INFINITY ? 0.0f : exp2f(s1.x - top);
-        l = s0.y * mine + s1.y * other;
-    } else {
-        again = !(l <= kMaxSum);
+    if (kMode == kMaxima) {
+        if (R == 1) {
+            sm.part[stream][row] = largest;
+            if (!together()) return false;
+            largest = fmaxf(sm.part[0][row], sm.part[1][row]);
+        }
+        ref = largest == -INFINITY ? 0.0f : largest + (float)(32 - __clz(it.keys));
+        return true;
     }
-    if (!ptx::mbar_wait(ptx::smem_u32(&sm.o_full), (c.work - 1) & 1)) return false;
+    before_end();
+    const float2 halves = ptx::unpack2(ptx::add2(sum[0], sum[1]));
+    float l = halves.x + halves.y;
+    if (R == 1) {                                                       // the streams hold a part of every row's sum each
+        sm.part[stream][row] = l;
+        if (!together()) return false;
+        l = sm.part[0][row] + sm.part[1][row];
+    }
+    again = !(l <= kMaxSum);
+    if (!ptx::mbar_wait(ptx::smem_u32(&sm.o_full[(c.work - 1) & 1]), ((c.work - 1) >> 1) & 1)) return false;
     __syncwarp();
     tc::fence_after_sync();
     if (busy) {
-        constexpr int kColumns = R == 1 ? D / 2 : D;
-        const uint32_t o0 = lane_addr + kOColumn + (R == 1 ? stream * kColumns : stream * 128);
+        constexpr int kColumns = R == 1 ? D / 2 : D;                    // R = 1: the streams share a row's columns
+        const int col0 = R == 1 ? stream * kColumns : 0;
+        const uint32_t o = lane_addr + kOColumn + (R == 2 ? stream * 128 : col0);
+        float* const out = p.partial + at * D + col0;
+        const float* const four = p.c.kv_scale + ((int64_t)p.layer * p.c.Hkv + it.h) * 4 * (KV == BAKLAVA_KV_INT4 ? D : 1);
+        const float v_scale = KV == BAKLAVA_KV_FP8_E4M3 ? four[2] : 1.0f;
 #pragma unroll 1
         for (int col = 0; col < kColumns; col += 16) {
-            uint32_t v[16], w[16];
-            load_16(o0 + col, v);
-            if (R == 1 && steps > 1) load_16(o0 + 128 + col, w);
+            uint32_t v[16];
+            load_16(o + col, v);
             tc::tmem_ld_wait();
             float x[2][8], worst = 0.0f;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 float y = __uint_as_float(v[e]);
-                if (R == 1) {
-                    y *= mine;
-                    if (steps > 1) y = fmaf(__uint_as_float(w[e]), other, y);
-                }
-                worst = fmaf(fabsf(y), 0x1p-20f, worst);
-                x[e >> 3][e & 7] = y;
+                worst = fmaf(fabsf(y), 0x1p-20f, worst);                // NaN propagates through the sum, infinities too
+                const int d = KV == BAKLAVA_KV_INT4 ? (e & 8) + ((e & 7) >> 1) + 4 * (e & 1) : e;
+                if (KV == BAKLAVA_KV_FP8_E4M3) y *= v_scale;
+                if (KV == BAKLAVA_KV_INT4) y *= four[2 * D + col0 + col + d];
+                x[d >> 3][d & 7] = y;
             }
             again = again || !(worst <= kFinite);
             if (there) {
-                store_sector(out + (R == 1 ? stream * kColumns : 0) + col, x[0]);
-                store_sector(out + (R == 1 ? stream * kColumns : 0) + col + 8, x[1]);
+                store_sector(out + col, x[0]);
+                store_sector(out + col + 8, x[1]);
             }
         }
-        if (there && (R == 2 || stream == 0)) p.stats[at] = make_float2(top, l);
+        // (a row without any weight: the reference means nothing)
+        if (there && (R == 2 || stream == 0)) p.stats[at] = make_float2(l == 0.0f ? -INFINITY : ref, l);
     }
     again = again && there && kMode == kFast;
     tc::fence_before_sync();
-    if (R == 1 && !together()) return false;                            // (O may be written again when both have read it)
+    if (R == 1 && !together()) return false;                            // (O and the sums may be written again when both have read them)
     if (again) p.stats[at].y = INFINITY;
     return true;
 }
@@ -597,43 +793,36 @@ __device__ __forceinline__ bool next_item(Shared& sm, int k, Item& it) {
     it = sm.item[k % kItemRing];
     return true;
 }
-__device__ __forceinline__ void init_barriers(Shared& sm, int slots) {
-    for (int s = 0; s < slots; ++s) {
-        ptx::mbar_init(ptx::smem_u32(&sm.full[s]), 1);
-        ptx::mbar_init(ptx::smem_u32(&sm.empty[s]), 1);
+template <typename L, typename F>
+__device__ __forceinline__ void each_barrier(Shared& sm, F f) {
+    for (int s = 0; s < L::kSlots; ++s) {
+        f(sm.full[s], L::kQuantised ? kConvertWarps : 1);
+        f(sm.empty[s], 1);
+    }
+    for (int s = 0; s < L::kRawSlots; ++s) {
+        f(sm.raw_full[s], 1);
+        f(sm.raw_empty[s], kConvertWarps);
     }
     for (int s = 0; s < 2; ++s) {
-        ptx::mbar_init(ptx::smem_u32(&sm.s_full[s]), 1);
-        ptx::mbar_init(ptx::smem_u32(&sm.p_ready[s]), kSoftmaxWarps / 2);
+        f(sm.s_full[s], 1);
+        f(sm.p_ready[s], kSoftmaxWarps / 2);
+        f(sm.o_full[s], 1);
     }
-    ptx::mbar_init(ptx::smem_u32(&sm.q_full), 1);
-    ptx::mbar_init(ptx::smem_u32(&sm.q_free), 1);
-    ptx::mbar_init(ptx::smem_u32(&sm.o_full), 1);
-    ptx::mbar_init(ptx::smem_u32(&sm.both), kSoftmaxWarps);
-}
-__device__ __forceinline__ void drop_barriers(Shared& sm, int slots) {
-    for (int s = 0; s < slots; ++s) {
-        ptx::mbar_inval(ptx::smem_u32(&sm.full[s]));
-        ptx::mbar_inval(ptx::smem_u32(&sm.empty[s]));
-    }
-    for (int s = 0; s < 2; ++s) {
-        ptx::mbar_inval(ptx::smem_u32(&sm.s_full[s]));
-        ptx::mbar_inval(ptx::smem_u32(&sm.p_ready[s]));
-    }
-    ptx::mbar_inval(ptx::smem_u32(&sm.q_full));
-    ptx::mbar_inval(ptx::smem_u32(&sm.q_free));
-    ptx::mbar_inval(ptx::smem_u32(&sm.o_full));
-    ptx::mbar_inval(ptx::smem_u32(&sm.both));
+    f(sm.q_full, L::kLoadsQ ? 1 : kSoftmaxWarps);
+    f(sm.q_free, 1);
+    f(sm.ref_ready, kSoftmaxWarps / 2);
+    f(sm.both, kSoftmaxWarps);
 }
 
 // An item again, alone: first for its rows' maxima, then with them as references.  The whole CTA; barriers are set up anew.
-template <int D, int R, int kMode>
+template <int D, int R, int KV, int kMode>
 __device__ __noinline__ void redo_pass(const TreeParams& p, Shared& sm, const Cta cta, const Item it, float& ref, const CUtensorMap& q_map,
                                        const CUtensorMap& k_map, const CUtensorMap& v_map) {
+    using L = Layout<D, R, KV>;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     __syncthreads();
     if (tid == 0) {
-        init_barriers(sm, Layout<D, R>::kSlots);
+        each_barrier<L>(sm, [](uint64_t& bar, int count) { ptx::mbar_init(ptx::smem_u32(&bar), count); });
         ptx::fence_mbar_init();
     }
     tc::fence_before_sync();
@@ -643,45 +832,53 @@ __device__ __noinline__ void redo_pass(const TreeParams& p, Shared& sm, const Ct
     bool ok = true, again = false;
     if (warp == 0) {
         if (lane == 0) {
-            load_queries<D, R>(p, sm, cta, it, q_map);
-            for (int e = 0; e < (kMode == kMaxima ? 1 : 2) * it.tiles && ok; ++e)
-                ok = load_entry<D, R, kMode>(p, sm, cta, it, 0, e, k_map, v_map);
+            if (L::kLoadsQ) load_queries<D, R, KV>(p, sm, cta, it, q_map);
+            for (int e = 0; e < entries_of<kMode>(it) && ok; ++e) ok = load_entry<D, R, KV, kMode>(p, sm, cta, it, 0, e, k_map, v_map);
         }
     } else if (warp == 1) {
-        if (lane == 0) ok = issue_item<D, R, kMode>(sm, cta, it, c);
+        if (lane == 0) ok = issue_item<D, R, KV, kMode>(sm, cta, it, c);
+    } else if (warp < 2 + kSoftmaxWarps) {
+        const int stream = (warp - 2) >> 2, full_row = 32 * (warp & 3) + lane + (R == 2 ? stream * kRows : 0);
+        float factor = query_factor<D, R, KV>(p, it);
+        if (!L::kLoadsQ) {
+            const Row r(p, it, full_row);
+            uint4 held[kHeldPieces<D, R>];
+            fetch_queries<D, R>(p, it, r, stream, held);
+            place_queries<D, R, KV>(p, sm, cta, it, r, stream, full_row, cta.tmem + ((uint32_t)(32 * (warp & 3)) << 16), lane, held, factor);
+        }
+        ok = soften_item<D, R, KV, kMode>(p, sm, cta, it, c, warp, lane, factor, ref, again, [] {});
     } else {
-        ok = soften_item<D, R, kMode>(p, sm, cta, it, c, warp, lane, ref, again);
+        ok = convert_item<D, R, KV, kMode>(p, sm, cta, it, c, warp, lane);
     }
     if (!ok) sm.abort = 1;
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
     if (sm.abort && tid == 0) let_copies_land();
-    if (tid == 0) drop_barriers(sm, Layout<D, R>::kSlots);
+    if (tid == 0) each_barrier<L>(sm, [](uint64_t& bar, int) { ptx::mbar_inval(ptx::smem_u32(&bar)); });
     __syncthreads();
 }
 
-template <int D, int R>
-__global__ void __launch_bounds__(kThreads, 1) tree_tile_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap q_map,
-                                                                const __grid_constant__ CUtensorMap k_map,
-                                                                const __grid_constant__ CUtensorMap v_map) {
-    using L = Layout<D, R>;
+template <int D, int R, int KV>
+__global__ void __launch_bounds__(Layout<D, R, KV>::kThreads, 1) tree_tile_kernel(
+        const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+        const __grid_constant__ CUtensorMap v_map) {
+    using L = Layout<D, R, KV>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     Shared& sm = *reinterpret_cast<Shared*>(smem_raw + L::kShared);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     Cta cta;
-    cta.q_tile = ptx::smem_u32(smem_raw);
-    cta.ring = cta.q_tile + L::kQBytes;
-    cta.ring_ptr = smem_raw + L::kQBytes;
+    cta.base = ptx::smem_u32(smem_raw);
+    cta.ptr = smem_raw;
     if (tid == 0) {
-        init_barriers(sm, L::kSlots);
+        each_barrier<L>(sm, [](uint64_t& bar, int count) { ptx::mbar_init(ptx::smem_u32(&bar), count); });
         ptx::mbar_init(ptx::smem_u32(&sm.bar_answer), 1);
         for (int s = 0; s < kItemRing; ++s) {
             ptx::mbar_init(ptx::smem_u32(&sm.bar_item[s]), 1);
             sm.redo_mark[s] = 0;
             sm.item[s].index = -1;
         }
-        sm.abort = cta.q_tile & 1023u ? 1 : 0;                // (the tiles' swizzle needs it; the base is where it is)
+        sm.abort = cta.base & 1023u ? 1 : 0;                  // (the tiles' swizzle needs it; the base is where it is)
         sm.redo_count = 0;
         sm.item[kItemRing - 1] = find_item(p, blockIdx.x);
         ptx::fence_mbar_init();
@@ -696,30 +893,52 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tile_kernel(const __grid_con
     cta.tmem = sm.tmem_slot;
     Item it = sm.item[kItemRing - 1];
     if (!sm.abort) {
+        bool ok = true;
+        Count c;
         if (warp == 0) {
-            if (lane == 0) produce<D, R>(p, sm, cta, it, q_map, k_map, v_map);
+            if (lane == 0) produce<D, R, KV>(p, sm, cta, it, q_map, k_map, v_map);
         } else if (warp == 1) {
-            if (lane == 0) {
-                Count c;
-                bool ok = true;
+            if (lane == 0)
                 for (int k = 0; ok && it.index >= 0; ++k) {
-                    if (it.tiles > 0) ok = issue_item<D, R, kFast>(sm, cta, it, c);
+                    if (it.tiles > 0) ok = issue_item<D, R, KV, kFast>(sm, cta, it, c);
                     if (ok) ok = next_item(sm, k, it);
                 }
-                if (!ok) sm.abort = 1;
+        } else if (warp < 2 + kSoftmaxWarps) {
+            const int stream = (warp - 2) >> 2, full_row = 32 * (warp & 3) + lane + (R == 2 ? stream * kRows : 0);
+            const uint32_t lane_addr = cta.tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+            float ref = 0.0f, factor = 0.0f;
+            uint4 held[kHeldPieces<D, R>];
+            bool fetched = false;
+            for (int k = 0; ok && it.index >= 0; ++k) {
+                bool again = false, found = false;
+                Item next = it;
+                if (it.tiles > 0) {
+                    if (!L::kLoadsQ) {
+                        const Row r(p, it, full_row);
+                        if (!fetched) fetch_queries<D, R>(p, it, r, stream, held);
+                        place_queries<D, R, KV>(p, sm, cta, it, r, stream, full_row, lane_addr, lane, held, factor);
+                    } else {
+                        factor = query_factor<D, R, KV>(p, it);
+                    }
+                    ok = soften_item<D, R, KV, kFast>(p, sm, cta, it, c, warp, lane, factor, ref, again, [&] {
+                        // the next item's queries are asked for while this one's rows are written
+                        found = next_item(sm, k, next);
+                        __syncwarp();
+                        fetched = found && next.index >= 0;
+                        if (!L::kLoadsQ && fetched) fetch_queries<D, R>(p, next, Row(p, next, full_row), stream, held);
+                    });
+                    if (ok && again && atomicExch(&sm.redo_mark[k % kItemRing], k + 1) != k + 1) sm.redo[atomicAdd(&sm.redo_count, 1)] = it;
+                }
+                if (ok && !found) ok = next_item(sm, k, next);
+                it = next;
             }
         } else {
-            Count c;
-            float ref = 0.0f;
-            bool ok = true;
             for (int k = 0; ok && it.index >= 0; ++k) {
-                bool again = false;
-                if (it.tiles > 0) ok = soften_item<D, R, kFast>(p, sm, cta, it, c, warp, lane, ref, again);
-                if (ok && again && atomicExch(&sm.redo_mark[k % kItemRing], k + 1) != k + 1) sm.redo[atomicAdd(&sm.redo_count, 1)] = it;
+                if (it.tiles > 0) ok = convert_item<D, R, KV, kFast>(p, sm, cta, it, c, warp, lane);
                 if (ok) ok = next_item(sm, k, it);
             }
-            if (!ok) sm.abort = 1;
         }
+        if (!ok) sm.abort = 1;
     }
     tc::fence_before_sync();
     __syncthreads();
@@ -727,11 +946,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tile_kernel(const __grid_con
     if (sm.abort) {
         if (tid == 0) let_copies_land();
     } else if (sm.redo_count > 0) {
-        if (tid == 0) drop_barriers(sm, L::kSlots);
+        if (tid == 0) each_barrier<L>(sm, [](uint64_t& bar, int) { ptx::mbar_inval(ptx::smem_u32(&bar)); });
         for (int i = 0; i < sm.redo_count && !sm.abort; ++i) {
             float ref = 0.0f;
-            redo_pass<D, R, kMaxima>(p, sm, cta, sm.redo[i], ref, q_map, k_map, v_map);
-            if (!sm.abort) redo_pass<D, R, kExact>(p, sm, cta, sm.redo[i], ref, q_map, k_map, v_map);
+            redo_pass<D, R, KV, kMaxima>(p, sm, cta, sm.redo[i], ref, q_map, k_map, v_map);
+            if (!sm.abort) redo_pass<D, R, KV, kExact>(p, sm, cta, sm.redo[i], ref, q_map, k_map, v_map);
         }
     }
     if (sm.abort) {
@@ -744,6 +963,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tile_kernel(const __grid_con
     if (warp == 1) tc::tmem_dealloc(cta.tmem, kTmemColumns);
 }
 
+// x 2^(ref - top).  A reference is not the maximum: it may lie so far below that its sums reach 2^120, and 2^(ref - top) alone
+// would leave the range.
+__device__ __forceinline__ float join_weight(float x, float ref, float top) {
+    const float half = exp2f(0.5f * (ref - top));
+    return x * half * half;
+}
 // One warp per node and query head: the logits of its ancestors, the normaliser of everything, then the sum of the
 // ancestors' values and the partials under their final weights (which add up to one, so that averages of values near the
 // end of the range do not overflow on the way).  Blocks of items that are not a head's first have nothing to do.
@@ -800,14 +1025,14 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const __grid
     for (int c = lane; c < pieces; c += 32) {
         const float2 st = p.stats[first + c * rows];
         skipped = skipped || st.y < 0.0f;
-        top = fmaxf(top, st.x);
+        if (st.x != -INFINITY) top = fmaxf(top, st.x + log2f(st.y));
     }
     if (__any_sync(0xffffffffu, skipped)) return;
 #pragma unroll
     for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
     for (int c = lane; c < pieces; c += 32) {
         const float2 st = p.stats[first + c * rows];
-        if (st.x != -INFINITY) sum += st.y * exp2f(st.x - top);
+        if (st.x != -INFINITY) sum += join_weight(st.y, st.x, top);
     }
     if (lane < depth && s0 != -INFINITY) sum += exp2f(s0 - top);
     if (lane + 32 < depth && s1 != -INFINITY) sum += exp2f(s1 - top);
@@ -851,9 +1076,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const __grid
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (c0 + k >= pieces || st[k].x == -INFINITY) continue;       // (no rows: its partial was not written)
-            const float w = exp2f(st[k].x - top) * inv;
 #pragma unroll
-            for (int e = 0; e < kE; ++e) o[e] = fmaf(w, x[k][e], o[e]);
+            for (int e = 0; e < kE; ++e) o[e] += join_weight(x[k][e], st[k].x, top) * inv;
         }
     }
     __nv_bfloat16* const out = p.out + u.b * p.so.seq + (int64_t)y * p.so.head + i * p.so.token + kE * lane;
@@ -866,19 +1090,20 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const __grid
     if (p.lse && lane == 0) p.lse[((int64_t)u.b * p.Hq + y) * p.T + i] = (top + log2f(sum)) * kLn2;
 }
 
-template <int D, int R>
+template <int D, int R, int KV>
 cudaError_t launch_tiles(const TreeParams& p, int n_items, const CUtensorMap& qm, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t s) {
+    using L = Layout<D, R, KV>;
     // the attribute belongs to the function on the current device: set once per device and instantiation
     static std::atomic<uint64_t> configured{0};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !(configured.load(std::memory_order_acquire) >> dev & 1)) {
-        e = cudaFuncSetAttribute(tree_tile_kernel<D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<D, R>::kTotal);
+        e = cudaFuncSetAttribute(tree_tile_kernel<D, R, KV>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kTotal);
         if (e != cudaSuccess) return e;
         if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
     }
-    tree_tile_kernel<D, R><<<(unsigned)(n_items * p.parts), kThreads, Layout<D, R>::kTotal, s>>>(p, qm, km, vm);
+    tree_tile_kernel<D, R, KV><<<(unsigned)(n_items * p.parts), L::kThreads, L::kTotal, s>>>(p, qm, km, vm);
     return cudaGetLastError();
 }
 
@@ -936,32 +1161,33 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_attn(
     p.g = shape->Hq / shape->Hkv;
     p.Hq = shape->Hq;
     p.layer = info->layer_begin;
+    const int kv = cache->kv_dtype;
     p.rows_per_head = (T + 7) / 8 * 8;
-    const int most = 2 * kRows / p.rows_per_head;             // query heads that two accumulators have room for
+    // query heads that the accumulators have room for (4 bits: one accumulator, the queries' two terms take the other's place)
+    const int most = (kv == BAKLAVA_KV_INT4 ? 1 : 2) * kRows / p.rows_per_head;
     p.parts = (p.g + most - 1) / most;
     p.heads = (p.g + p.parts - 1) / p.parts;
     p.scale_log2 = kLog2e / sqrtf((float)shape->D);
     if ((int64_t)info->n_items * p.parts > INT32_MAX) return BAKLAVA_ERR_UNSUPPORTED;
     const int64_t rows = (int64_t)B * cache->seq_stride_tokens;
-    CUtensorMap qm, km, vm;
-    if (cache->kv_dtype == BAKLAVA_KV_BF16 && (!ptx::make_tokens_map(&qm, q, shape->D, T, shape->Hq, B, q_str->token, q_str->head, q_str->seq, p.rows_per_head) ||
-        !ptx::make_tokens_map(&km, cache->k_slab, shape->D, rows, 1, 1, shape->D, shape->D, shape->D, kKeys) ||
-        !ptx::make_tokens_map(&vm, cache->v_slab, shape->D, rows, 1, 1, shape->D, shape->D, shape->D, kKeys)))
+    CUtensorMap qm = {}, km = {}, vm = {};
+    if (kv == BAKLAVA_KV_BF16 &&
+        (!ptx::make_tokens_map(&qm, q, shape->D, T, shape->Hq, B, q_str->token, q_str->head, q_str->seq, p.rows_per_head) ||
+         !ptx::make_tokens_map(&km, cache->k_slab, shape->D, rows, 1, 1, shape->D, shape->D, shape->D, kKeys) ||
+         !ptx::make_tokens_map(&vm, cache->v_slab, shape->D, rows, 1, 1, shape->D, shape->D, shape->D, kKeys)))
         return BAKLAVA_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool two = p.heads * p.rows_per_head > kRows;
-    const dim3 join((unsigned)info->n_items, (unsigned)((p.g * T + kJoinWarps - 1) / kJoinWarps));
+    const int n = info->n_items;
     cudaError_t e;
-    if (cache->kv_dtype != BAKLAVA_KV_BF16) {
-        tree_chunk_kernel<128><<<dim3((unsigned)info->n_items, (unsigned)((p.g * T + 7) / 8)), 256, 0, s>>>(p);
-        e = cudaGetLastError();
-        if (e == cudaSuccess) tree_join_kernel<128><<<join, kJoinWarps * 32, 0, s>>>(p);
-    } else if (shape->D == 128) {
-        e = two ? launch_tiles<128, 2>(p, info->n_items, qm, km, vm, s) : launch_tiles<128, 1>(p, info->n_items, qm, km, vm, s);
-        if (e == cudaSuccess) tree_join_kernel<128><<<join, kJoinWarps * 32, 0, s>>>(p);
-    } else {
-        e = two ? launch_tiles<64, 2>(p, info->n_items, qm, km, vm, s) : launch_tiles<64, 1>(p, info->n_items, qm, km, vm, s);
-        if (e == cudaSuccess) tree_join_kernel<64><<<join, kJoinWarps * 32, 0, s>>>(p);
+    if (kv == BAKLAVA_KV_INT4) e = launch_tiles<128, 1, BAKLAVA_KV_INT4>(p, n, qm, km, vm, s);
+    else if (kv == BAKLAVA_KV_FP8_E4M3) e = two ? launch_tiles<128, 2, BAKLAVA_KV_FP8_E4M3>(p, n, qm, km, vm, s) : launch_tiles<128, 1, BAKLAVA_KV_FP8_E4M3>(p, n, qm, km, vm, s);
+    else if (shape->D == 128) e = two ? launch_tiles<128, 2, BAKLAVA_KV_BF16>(p, n, qm, km, vm, s) : launch_tiles<128, 1, BAKLAVA_KV_BF16>(p, n, qm, km, vm, s);
+    else e = two ? launch_tiles<64, 2, BAKLAVA_KV_BF16>(p, n, qm, km, vm, s) : launch_tiles<64, 1, BAKLAVA_KV_BF16>(p, n, qm, km, vm, s);
+    const dim3 join((unsigned)n, (unsigned)((p.g * T + kJoinWarps - 1) / kJoinWarps));
+    if (e == cudaSuccess) {
+        if (shape->D == 128) tree_join_kernel<128><<<join, kJoinWarps * 32, 0, s>>>(p);
+        else tree_join_kernel<64><<<join, kJoinWarps * 32, 0, s>>>(p);
     }
     if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? BAKLAVA_OK : BAKLAVA_ERR_CUDA;
