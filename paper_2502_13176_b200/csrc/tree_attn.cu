@@ -249,7 +249,7 @@ __device__ __forceinline__ bool load_entry(const TreeParams& p, Shared& sm, cons
     int t;
     const bool value = entry_is_value<R, kMode>(e, it.tiles, t);
     const uint32_t n = base + e;
-    if (L::kQuantised) {
+    if constexpr (L::kQuantised) {
         const uint32_t slot = n % L::kRawSlots, bar = ptx::smem_u32(&sm.raw_full[slot]);
         if (!ptx::mbar_wait(ptx::smem_u32(&sm.raw_empty[slot]), (n / L::kRawSlots & 1) ^ 1)) return false;
         const uint32_t bytes = min(kKeys, it.keys - t * kKeys) * L::kRowBytes;

@@ -49,41 +49,96 @@ struct Shared {
     int tried_token[kMaxTree];                // tokens with residuals of their own at this node, with their target
     double tried_r[kMaxTree], tried_p[kMaxTree];
     double warp_sum[kWarps];
+    double block_sum[2];                      // this block's share of a mass, two in turn; the cluster's blocks read them
     int bad;
 };
 
-// Residual of token v: list first, then the common form.
-template <typename P, bool kDraft>
-__device__ __forceinline__ double residual(const Shared& sm, const P* target, const P* draft, double K, int tried, int v) {
-    const double p = prob(target + v);
-    double r = p;
-    if (kDraft) r = above_zero(fma(-K, (double)prob(draft + v), p));
-    for (int t = 0; t < tried; ++t)
-        if (sm.tried_token[t] == v) r = sm.tried_r[t];
-    return r;
+// One block of the cluster that works on a sequence, and its part of the vocabulary.
+struct Part {
+    int rank, blocks, lo, hi, share;          // tokens lo .. hi - 1, `share` to a warp
+    __device__ __forceinline__ Part(int V) {
+        asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+        asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(blocks));
+        const int each = (V + blocks - 1) / blocks;
+        lo = min(V, rank * each);
+        hi = min(V, lo + each);
+        share = (each + kWarps - 1) / kWarps;
+    }
+};
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+__device__ __forceinline__ double of_block(const double* mine, int rank) {
+    uint32_t at;
+    double x;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(x) : "r"(at) : "memory");
+    return x;
 }
 
-// Mass of the residual over the vocabulary; each warp's share stays in sm.warp_sum.  The whole block.
+// The residual of a node: of 256 tokens v0 .. v0 + 255, this lane's v0 + lane + 32 j.  Tokens of the list have values of their
+// own; those at or behind `hi` have none.
 template <typename P, bool kDraft>
-__device__ __forceinline__ double mass(Shared& sm, const P* target, const P* draft, double K, int tried, int V) {
+struct Residual {
+    const P* target;
+    const P* draft;
+    double K;
+    int tried;
+    __device__ __forceinline__ void load(const Shared& sm, int v0, int hi, int lane, double (&r)[8]) const {
+        float p[8], q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int v = v0 + lane + 32 * j;
+            p[j] = v < hi ? prob(target + v) : 0.0f;
+            q[j] = kDraft && v < hi ? prob(draft + v) : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[j] = kDraft ? above_zero(fma(-K, (double)q[j], (double)p[j])) : (double)p[j];
+        for (int t = 0; t < tried; ++t) {
+            const int d = sm.tried_token[t] - v0;
+            if (d < 0 || d >= 256 || v0 + d >= hi) continue;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (lane + 32 * j == d) r[j] = sm.tried_r[t];
+        }
+    }
+};
+
+// Mass of the residual over the vocabulary, the same number in every block; each warp's share stays in sm.warp_sum, each block's in
+// sm.block_sum[round & 1].  The whole cluster.
+template <typename R>
+__device__ __forceinline__ double mass(Shared& sm, const R& of, const Part& part, int& round) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int share = (V + kWarps - 1) / kWarps, lo = warp * share, hi = min(V, lo + share);
+    const int lo = part.lo + warp * part.share, hi = min(part.hi, lo + part.share);
     double sum = 0.0;
-    for (int v = lo + lane; v < hi; v += 32) sum += residual<P, kDraft>(sm, target, draft, K, tried, v);
+    for (int v0 = lo; v0 < hi; v0 += 256) {
+        double r[8];
+        of.load(sm, v0, hi, lane, r);
+        sum += ((r[0] + r[1]) + (r[2] + r[3])) + ((r[4] + r[5]) + (r[6] + r[7]));
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     __syncthreads();                                          // (the sums before these have been read)
     if (lane == 0) sm.warp_sum[warp] = sum;
     __syncthreads();
     double total = 0.0;
+#pragma unroll
     for (int w = 0; w < kWarps; ++w) total += sm.warp_sum[w];
+    ++round;
+    if (part.blocks == 1) return total;
+    if (threadIdx.x == 0) sm.block_sum[round & 1] = total;
+    cluster_sync();                                           // (the buffer of the round before last has been read by all)
+    total = 0.0;
+    for (int k = 0; k < part.blocks; ++k) total += of_block(&sm.block_sum[round & 1], k);
     return total;
 }
 
 template <typename P, bool kDraft>
-__global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant__ VerifyParams p) {
+__global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_constant__ VerifyParams p) {
     __shared__ Shared sm;
-    const int b = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, T = p.T, V = p.V;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, T = p.T, V = p.V;
+    const Part part(V);
+    const int b = blockIdx.x / part.blocks;
     const int n = tree::nodes_of(p.n_nodes, b, T);
     const P* const target = static_cast<const P*>(p.target) + (int64_t)b * T * p.target_stride;
     const P* const draft = kDraft ? static_cast<const P*>(p.draft) + (int64_t)b * T * p.draft_stride : nullptr;
@@ -102,18 +157,22 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
         }
     }
     __syncthreads();
-    if (n == 0 || sm.bad) {
-        if (tid < T) p.path[(int64_t)b * T + tid] = -1;
-        if (tid == 0) {
-            p.n_path[b] = 0;
-            p.next_token[b] = -1;
-            if (sm.bad) atomicOr(p.status, BAKLAVA_STATUS_BAD_STATE);
+    if (n == 0 || sm.bad) {                                   // (every block of the cluster sees the same)
+        if (part.rank == 0) {
+            if (tid < T) p.path[(int64_t)b * T + tid] = -1;
+            if (tid == 0) {
+                p.n_path[b] = 0;
+                p.next_token[b] = -1;
+                if (sm.bad) atomicOr(p.status, BAKLAVA_STATUS_BAD_STATE);
+            }
         }
         return;
     }
-    // The walk: every thread takes it, on the same numbers.
-    int cur = 0, count = 1, tried = 0;
-    double K = 0.0, c = 1.0, gone = 0.0, total = -1.0;
+    // The walk: every thread of every block takes it, on the same numbers.
+    int cur = 0, count = 1, tried = 0, round = 0;
+    double K = 0.0, c = 1.0, gone = 0.0, total = -1.0;        // total: the mass of what is left, -1 where it is not known
+    double row_mass = -1.0;                                   // no draft: mass of the node's whole row
+    auto residual = [&] { return Residual<P, kDraft>{target + cur * p.target_stride, kDraft ? draft + cur * p.draft_stride : nullptr, K, tried}; };
     if (tid == 0) sm.path[0] = 0;
     for (int i = 1; i < n; ++i) {
         if (sm.parent[i] != cur) continue;
@@ -122,7 +181,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
         while (at < tried && sm.tried_token[at] != x) ++at;
         const bool again = at < tried;
         const double px = sm.p[i], qx = sm.q[i];
-        double R = again ? sm.tried_r[at] : kDraft ? above_zero(fma(-K, qx, px)) : px;
+        const double R = again ? sm.tried_r[at] : kDraft ? above_zero(fma(-K, qx, px)) : px;
         const double left = 1.0 - gone;
         const double q = !kDraft ? 1.0 : !p.distinct ? qx : again || !(left > 0.0) ? 0.0 : qx / left;
         if ((double)sm.u[i] * q < R / c) {
@@ -130,16 +189,17 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
             ++count;
             cur = i;
             tried = 0;
-            K = 0.0; c = 1.0; gone = 0.0; total = -1.0;
+            K = 0.0; c = 1.0; gone = 0.0; total = -1.0; row_mass = -1.0;
             continue;
         }
         if (kDraft) K += !p.distinct ? c : left > 0.0 ? c / left : 0.0;
+        const double now = !kDraft ? above_zero(R - c) : again ? R : above_zero(fma(-K, qx, px));
         __syncthreads();                                      // (the list has been read)
         if (!kDraft || p.distinct) {
             if (tid == 0) {
                 sm.tried_token[at] = x;
                 sm.tried_p[at] = px;
-                sm.tried_r[at] = !kDraft ? above_zero(R - c) : again ? R : above_zero(fma(-K, qx, px));
+                sm.tried_r[at] = now;
             }
             if (!again) {
                 ++tried;
@@ -147,7 +207,15 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
             }
         }
         __syncthreads();
-        total = mass<P, kDraft>(sm, target + cur * p.target_stride, kDraft ? draft + cur * p.draft_stride : nullptr, K, tried, V);
+        // Point masses take away what they stand on: the row's mass, known from one pass, less that, unless so little is left
+        // that the difference does not tell it.
+        double less = -1.0;
+        if (!kDraft) {
+            if (row_mass < 0.0) row_mass = mass(sm, Residual<P, kDraft>{residual().target, nullptr, 0.0, 0}, part, round);
+            less = row_mass;
+            for (int t = 0; t < tried; ++t) less -= sm.tried_p[t] - sm.tried_r[t];
+        }
+        total = !kDraft && less > 0x1p-20 * row_mass ? less : mass(sm, residual(), part, round);
         c = total;
         if (!(total > 0.0)) {                                 // nothing is left: the target's own row again
             __syncthreads();
@@ -156,50 +224,90 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
             K = 0.0; c = 1.0; total = -1.0;
         }
     }
-    const P* const row = target + cur * p.target_stride;
-    const P* const beside = kDraft ? draft + cur * p.draft_stride : nullptr;
-    if (total < 0.0) {
-        __syncthreads();
-        total = mass<P, kDraft>(sm, row, beside, K, tried, V);
-    }
-    __syncthreads();
-    if (tid < T) p.path[(int64_t)b * T + tid] = tid < count ? sm.path[tid] : -1;
-    if (tid == 0) p.n_path[b] = count;
-    if (!(total > 0.0)) {
+    // the shares have to be those of the residual that is drawn from
+    const auto last = residual();
+    if (!kDraft || total < 0.0) total = mass(sm, last, part, round);
+    if (part.rank == 0) {
+        if (tid < T) p.path[(int64_t)b * T + tid] = tid < count ? sm.path[tid] : -1;
         if (tid == 0) {
-            p.next_token[b] = -1;
-            atomicOr(p.status, BAKLAVA_STATUS_BAD_STATE);
+            p.n_path[b] = count;
+            if (!(total > 0.0)) {
+                p.next_token[b] = -1;
+                atomicOr(p.status, BAKLAVA_STATUS_BAD_STATE);
+            }
         }
-        return;
     }
-    // the first token whose running sum is above u times the mass: first which warp's share it is in
+    // The first token whose running sum is above u times the mass: which block's part it is in, which warp's share, which 256
+    // tokens.  Where rounding leaves no sum above, the last of those that hold any mass.
     const double want = (double)p.u_sample[b] * total;
     int mine = -1;
     double before = 0.0, run = 0.0;
+    for (int k = 0; k < part.blocks; ++k) {
+        const double s = part.blocks == 1 ? total : of_block(&sm.block_sum[round & 1], k);
+        if (s > 0.0) { mine = k; before = run; }
+        run += s;
+        if (run > want) break;
+    }
+    if (part.blocks > 1) cluster_sync();                      // (no block leaves while its sums are read)
+    if (!(total > 0.0) || mine != part.rank) return;
+    run = before;
+    mine = -1;
     for (int w = 0; w < kWarps; ++w) {
         const double s = sm.warp_sum[w];
-        if (s > 0.0) { mine = w; before = run; }              // (the last share with any mass where rounding leaves none above)
+        if (s > 0.0) { mine = w; before = run; }
         run += s;
         if (run > want) break;
     }
     if (warp != mine) return;
-    const int share = (V + kWarps - 1) / kWarps, lo = warp * share, hi = min(V, lo + share);
-    int last = -1;
-    for (int v0 = lo; v0 < hi; v0 += 32) {
-        const double r = v0 + lane < hi ? residual<P, kDraft>(sm, row, beside, K, tried, v0 + lane) : 0.0;
-        double upto = r;
+    const int lo = part.lo + warp * part.share, hi = min(part.hi, lo + part.share);
+    int pick = lo;
+    run = before;
+    for (int v0 = lo; v0 < hi && !(run > want); v0 += 256) {
+        double r[8];
+        last.load(sm, v0, hi, lane, r);
+        double sum = ((r[0] + r[1]) + (r[2] + r[3])) + ((r[4] + r[5]) + (r[6] + r[7]));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (sum > 0.0) { pick = v0; before = run; }
+        run += sum;
+    }
+    double r[8];
+    last.load(sm, pick, hi, lane, r);
+    int found = -1;
+    bool done = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        double scan = r[j];
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const double y = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += y;
+            const double y = __shfl_up_sync(0xffffffffu, scan, o);
+            if (lane >= o) scan += y;
         }
-        const uint32_t some = __ballot_sync(0xffffffffu, r > 0.0);
-        const uint32_t here = __ballot_sync(0xffffffffu, r > 0.0 && before + upto > want);
-        if (some) last = v0 + (here ? __ffs(here) - 1 : 31 - __clz(some));
-        if (here) break;
-        before += __shfl_sync(0xffffffffu, upto, 31);
+        const uint32_t some = __ballot_sync(0xffffffffu, r[j] > 0.0);
+        const uint32_t here = __ballot_sync(0xffffffffu, r[j] > 0.0 && before + scan > want);
+        if (!done && some) found = pick + 32 * j + (here ? __ffs(here) - 1 : 31 - __clz(some));
+        done = done || here != 0;
+        before += __shfl_sync(0xffffffffu, scan, 31);
     }
-    if (lane == 0) p.next_token[b] = last;
+    if (lane == 0) p.next_token[b] = found;
+}
+
+template <typename P, bool kDraft>
+cudaError_t launch(const VerifyParams& p, int B, cudaStream_t s) {
+    // Blocks to a sequence: enough to fill the device, each with at least a few thousand tokens.
+    int blocks = 1;
+    while (blocks < 8 && blocks * B < 2 * 148 && p.V / (2 * blocks) >= 2048) blocks *= 2;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = blocks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)B * blocks);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, verify_kernel<P, kDraft>, p);
 }
 
 }  // namespace
@@ -231,12 +339,10 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_verify(
     p.T = T; p.V = V;
     p.distinct = flags & BAKLAVA_VERIFY_DISTINCT ? 1 : 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (prob_dtype == BAKLAVA_PROB_F32) {
-        if (draft) verify_kernel<float, true><<<B, kThreads, 0, s>>>(p);
-        else verify_kernel<float, false><<<B, kThreads, 0, s>>>(p);
-    } else {
-        if (draft) verify_kernel<__nv_bfloat16, true><<<B, kThreads, 0, s>>>(p);
-        else verify_kernel<__nv_bfloat16, false><<<B, kThreads, 0, s>>>(p);
-    }
+    if (B > (1 << 27)) return BAKLAVA_ERR_UNSUPPORTED;
+    cudaError_t e;
+    if (prob_dtype == BAKLAVA_PROB_F32) e = draft ? launch<float, true>(p, B, s) : launch<float, false>(p, B, s);
+    else e = draft ? launch<__nv_bfloat16, true>(p, B, s) : launch<__nv_bfloat16, false>(p, B, s);
+    if (e != cudaSuccess) return BAKLAVA_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? BAKLAVA_OK : BAKLAVA_ERR_CUDA;
 }
