@@ -20,6 +20,7 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxTree = BAKLAVA_MAX_TREE;
+constexpr int kMaxBlocks = 8;
 
 struct VerifyParams {
     const void* target;
@@ -41,6 +42,18 @@ __device__ __forceinline__ float prob(const float* p) { return fmaxf(*p, 0.0f); 
 __device__ __forceinline__ float prob(const __nv_bfloat16* p) { return fmaxf(__bfloat162float(*p), 0.0f); }
 __device__ __forceinline__ double above_zero(double x) { return x > 0.0 ? x : 0.0; }
 
+// Conversions to 64 bits run at a quarter of the rate of anything else here.  The bits of a float >= 0, moved to where a double
+// has them, are the float times 2^-896, subnormals and zero among them: two shifts.  Sums over the vocabulary are formed at
+// that scale.
+constexpr double kDown = 0x1p-896, kUp = 0x1p896;
+__device__ __forceinline__ double scaled(float x) {
+    const uint32_t bits = __float_as_uint(x);
+    return __hiloint2double((int)(bits >> 3), (int)(bits << 29));
+}
+__device__ __forceinline__ double scaled_above_zero(double x) {                                   // (no NaN comes here)
+    return __double2hiint(x) < 0 ? 0.0 : x;
+}
+
 struct Shared {
     int parent[kMaxTree], token[kMaxTree];
     double p[kMaxTree], q[kMaxTree];          // target and draft of each node's token at its parent
@@ -48,21 +61,17 @@ struct Shared {
     int path[kMaxTree];
     int tried_token[kMaxTree];                // tokens with residuals of their own at this node, with their target
     double tried_r[kMaxTree], tried_p[kMaxTree];
-    double warp_sum[kWarps];
-    double block_sum[2];                      // this block's share of a mass, two in turn; the cluster's blocks read them
+    double warp_sum[kWarps];                  // (times 2^-896)
+    double block_sum[2];                      // (the same) this block's share of a mass, two in turn; the cluster's blocks read them
     int bad;
 };
 
-// One block of the cluster that works on a sequence, and its part of the vocabulary.
+// One block of the cluster that works on a sequence.
 struct Part {
-    int rank, blocks, lo, hi, share;          // tokens lo .. hi - 1, `share` to a warp
-    __device__ __forceinline__ Part(int V) {
+    int rank, blocks;
+    __device__ __forceinline__ Part() {
         asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
         asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(blocks));
-        const int each = (V + blocks - 1) / blocks;
-        lo = min(V, rank * each);
-        hi = min(V, lo + each);
-        share = (each + kWarps - 1) / kWarps;
     }
 };
 __device__ __forceinline__ void cluster_sync() {
@@ -76,46 +85,107 @@ __device__ __forceinline__ double of_block(const double* mine, int rank) {
     return x;
 }
 
-// The residual of a node: of 256 tokens v0 .. v0 + 255, this lane's v0 + lane + 32 j.  Tokens of the list have values of their
-// own; those at or behind `hi` have none.
+// eight values from a 16-byte boundary
+__device__ __forceinline__ void load_8(const float* from, float (&x)[8]) {
+    const float4 a = __ldg(reinterpret_cast<const float4*>(from)), b = __ldg(reinterpret_cast<const float4*>(from) + 1);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load_8(const __nv_bfloat16* from, float (&x)[8]) {
+    const uint4 w = __ldg(reinterpret_cast<const uint4*>(from));
+    const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(word[i] << 16);
+        x[2 * i + 1] = __uint_as_float(word[i] & 0xffff0000u);
+    }
+}
+
+// The residual of a node, times 2^-896.  Rows begin anywhere: places x = token + shift are counted from the last 16-byte
+// boundary before the row, so that eight places from a multiple of eight are one or two vectors.  A lane takes eight, a warp
+// 256 at a time.  Tokens of the list have values of their own.
 template <typename P, bool kDraft>
 struct Residual {
     const P* target;
     const P* draft;
     double K;
-    int tried;
-    __device__ __forceinline__ void load(const Shared& sm, int v0, int hi, int lane, double (&r)[8]) const {
-        float p[8], q[8];
+    int tried, shift, end, lo, hi;            // row in places shift .. end - 1, this warp's among them lo .. hi - 1
+    bool same;                                // the draft's row begins at the same distance from a boundary
+    __device__ __forceinline__ Residual(const P* target_row, const P* draft_row, double K_, int tried_, int V, const Part& part)
+        : target(target_row), draft(draft_row), K(K_), tried(tried_) {
+        shift = (int)(reinterpret_cast<uintptr_t>(target) & 15u) / (int)sizeof(P);
+        same = kDraft && ((reinterpret_cast<uintptr_t>(target) ^ reinterpret_cast<uintptr_t>(draft)) & 15u) == 0;
+        end = V + shift;
+        const int w = part.rank * kWarps + (threadIdx.x >> 5);
+        lo = lo_of(part, w);
+        hi = hi_of(part, w);
+    }
+    // places of the cluster's warp w
+    __device__ __forceinline__ int lo_of(const Part& part, int w) const {
+        const int warps = part.blocks * kWarps, share = ((end + warps - 1) / warps + 7) & ~7;
+        return (int)min((long long)end, (long long)w * share);
+    }
+    __device__ __forceinline__ int hi_of(const Part& part, int w) const { return lo_of(part, w + 1); }
+    __device__ __forceinline__ void fetch(const P* row, int x0, float (&x)[8], bool vector) const {
+        if (vector && x0 >= shift && x0 + 8 <= hi) {
+            load_8(row + (x0 - shift), x);
+        } else if (x0 >= hi) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = 0.0f;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = x0 + j >= shift && x0 + j < hi ? prob(row + (x0 + j - shift)) : 0.0f;
+        }
+    }
+    __device__ __forceinline__ void finish(const Shared& sm, int x0, const float (&p)[8], const float (&q)[8], double (&r)[8]) const {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int v = v0 + lane + 32 * j;
-            p[j] = v < hi ? prob(target + v) : 0.0f;
-            q[j] = kDraft && v < hi ? prob(draft + v) : 0.0f;
+            r[j] = scaled(fmaxf(p[j], 0.0f));                 // (NaN becomes 0)
+            if (kDraft) r[j] = scaled_above_zero(fma(-K, scaled(fmaxf(q[j], 0.0f)), r[j]));
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) r[j] = kDraft ? above_zero(fma(-K, (double)q[j], (double)p[j])) : (double)p[j];
         for (int t = 0; t < tried; ++t) {
-            const int d = sm.tried_token[t] - v0;
-            if (d < 0 || d >= 256 || v0 + d >= hi) continue;
+            const int d = sm.tried_token[t] + shift - x0;
+            if (d < 0 || d >= 8 || x0 + d >= hi) continue;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (lane + 32 * j == d) r[j] = sm.tried_r[t];
+                if (j == d) r[j] = sm.tried_r[t] * kDown;
         }
+    }
+    // this lane's places x0 .. x0 + 7
+    __device__ __forceinline__ void load(const Shared& sm, int x0, double (&r)[8]) const {
+        float p[8], q[8];
+        fetch(target, x0, p, true);
+        if (kDraft) fetch(draft, x0, q, same);
+        finish(sm, x0, p, q, r);
+    }
+    // sum over the warp's places, as every lane's share
+    __device__ __forceinline__ double sum(const Shared& sm, int lane) const {
+        constexpr int kSteps = 64 / (8 * (int)sizeof(P) * (kDraft ? 2 : 1));      // 64 bytes of a lane are in flight together
+        double total = 0.0;
+        for (int x0 = lo + 8 * lane; x0 < hi; x0 += 256 * kSteps) {
+            float p[kSteps][8], q[kSteps][8];
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                fetch(target, x0 + 256 * k, p[k], true);
+                if (kDraft) fetch(draft, x0 + 256 * k, q[k], same);
+            }
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                double r[8];
+                finish(sm, x0 + 256 * k, p[k], q[k], r);
+                total += ((r[0] + r[1]) + (r[2] + r[3])) + ((r[4] + r[5]) + (r[6] + r[7]));
+            }
+        }
+        return total;
     }
 };
 
-// Mass of the residual over the vocabulary, the same number in every block; each warp's share stays in sm.warp_sum, each block's in
-// sm.block_sum[round & 1].  The whole cluster.
+// Mass of the residual over the vocabulary (as it is, not scaled), the same number in every block; each warp's share stays in
+// sm.warp_sum, each block's in sm.block_sum[round & 1].  The whole cluster.
 template <typename R>
 __device__ __forceinline__ double mass(Shared& sm, const R& of, const Part& part, int& round) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int lo = part.lo + warp * part.share, hi = min(part.hi, lo + part.share);
-    double sum = 0.0;
-    for (int v0 = lo; v0 < hi; v0 += 256) {
-        double r[8];
-        of.load(sm, v0, hi, lane, r);
-        sum += ((r[0] + r[1]) + (r[2] + r[3])) + ((r[4] + r[5]) + (r[6] + r[7]));
-    }
+    double sum = of.sum(sm, lane);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     __syncthreads();                                          // (the sums before these have been read)
@@ -125,19 +195,20 @@ __device__ __forceinline__ double mass(Shared& sm, const R& of, const Part& part
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) total += sm.warp_sum[w];
     ++round;
-    if (part.blocks == 1) return total;
+    if (part.blocks == 1) return total * kUp;
     if (threadIdx.x == 0) sm.block_sum[round & 1] = total;
     cluster_sync();                                           // (the buffer of the round before last has been read by all)
+    const double of_lane = lane < part.blocks ? of_block(&sm.block_sum[round & 1], lane) : 0.0;
     total = 0.0;
-    for (int k = 0; k < part.blocks; ++k) total += of_block(&sm.block_sum[round & 1], k);
-    return total;
+    for (int k = 0; k < part.blocks; ++k) total += __shfl_sync(0xffffffffu, of_lane, k);
+    return total * kUp;
 }
 
 template <typename P, bool kDraft>
 __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_constant__ VerifyParams p) {
     __shared__ Shared sm;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, T = p.T, V = p.V;
-    const Part part(V);
+    const Part part;
     const int b = blockIdx.x / part.blocks;
     const int n = tree::nodes_of(p.n_nodes, b, T);
     const P* const target = static_cast<const P*>(p.target) + (int64_t)b * T * p.target_stride;
@@ -170,12 +241,38 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     }
     // The walk: every thread of every block takes it, on the same numbers.
     int cur = 0, count = 1, tried = 0, round = 0;
-    double K = 0.0, c = 1.0, gone = 0.0, total = -1.0;        // total: the mass of what is left, -1 where it is not known
-    double row_mass = -1.0;                                   // no draft: mass of the node's whole row
-    auto residual = [&] { return Residual<P, kDraft>{target + cur * p.target_stride, kDraft ? draft + cur * p.draft_stride : nullptr, K, tried}; };
+    bool open = false;                                        // a child was refused and what it left has not been summed yet
+    double K = 0.0, c = 1.0, gone = 0.0;                      // c: the residual's mass (1 for a row as it is given)
+    double row_mass = -1.0;                                   // no draft: mass of the node's whole row, -1 where it is not known
+    auto residual = [&](int listed) {
+        return Residual<P, kDraft>(target + cur * p.target_stride, kDraft ? draft + cur * p.draft_stride : nullptr, K, listed, V, part);
+    };
+    // the mass that refused children have left; nothing: the target's own row again
+    auto settle = [&](double total) {
+        open = false;
+        c = total;
+        if (total > 0.0) return;
+        __syncthreads();
+        if (tid < tried) sm.tried_r[tid] = sm.tried_p[tid];
+        __syncthreads();
+        K = 0.0;
+        c = 1.0;
+    };
     if (tid == 0) sm.path[0] = 0;
     for (int i = 1; i < n; ++i) {
         if (sm.parent[i] != cur) continue;
+        // what the children before this one have left, if any of them was refused since it was last known
+        if (open) {
+            double less = -1.0;
+            if (!kDraft) {
+                // Point masses take away what they stand on: the row's mass, known from one pass, less that, unless so little
+                // is left that the difference does not tell it.
+                if (row_mass < 0.0) row_mass = mass(sm, residual(0), part, round);
+                less = row_mass;
+                for (int t = 0; t < tried; ++t) less -= sm.tried_p[t] - sm.tried_r[t];
+            }
+            settle(!kDraft && less > 0x1p-20 * row_mass ? less : mass(sm, residual(tried), part, round));
+        }
         const int x = sm.token[i];
         int at = 0;
         while (at < tried && sm.tried_token[at] != x) ++at;
@@ -189,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
             ++count;
             cur = i;
             tried = 0;
-            K = 0.0; c = 1.0; gone = 0.0; total = -1.0; row_mass = -1.0;
+            K = 0.0; c = 1.0; gone = 0.0; row_mass = -1.0;
             continue;
         }
         if (kDraft) K += !p.distinct ? c : left > 0.0 ? c / left : 0.0;
@@ -206,27 +303,16 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
                 if (kDraft) gone += qx;
             }
         }
+        open = true;
         __syncthreads();
-        // Point masses take away what they stand on: the row's mass, known from one pass, less that, unless so little is left
-        // that the difference does not tell it.
-        double less = -1.0;
-        if (!kDraft) {
-            if (row_mass < 0.0) row_mass = mass(sm, Residual<P, kDraft>{residual().target, nullptr, 0.0, 0}, part, round);
-            less = row_mass;
-            for (int t = 0; t < tried; ++t) less -= sm.tried_p[t] - sm.tried_r[t];
-        }
-        total = !kDraft && less > 0x1p-20 * row_mass ? less : mass(sm, residual(), part, round);
-        c = total;
-        if (!(total > 0.0)) {                                 // nothing is left: the target's own row again
-            __syncthreads();
-            if (tid < tried) sm.tried_r[tid] = sm.tried_p[tid];
-            __syncthreads();
-            K = 0.0; c = 1.0; total = -1.0;
-        }
     }
-    // the shares have to be those of the residual that is drawn from
-    const auto last = residual();
-    if (!kDraft || total < 0.0) total = mass(sm, last, part, round);
+    // the shares that the draw looks at have to be those of the residual that is drawn from
+    double total = mass(sm, residual(tried), part, round);
+    if (open && !(total > 0.0)) {
+        settle(total);
+        total = mass(sm, residual(tried), part, round);
+    }
+    auto last = residual(tried);
     if (part.rank == 0) {
         if (tid < T) p.path[(int64_t)b * T + tid] = tid < count ? sm.path[tid] : -1;
         if (tid == 0) {
@@ -239,64 +325,83 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const __grid_consta
     }
     // The first token whose running sum is above u times the mass: which block's part it is in, which warp's share, which 256
     // tokens.  Where rounding leaves no sum above, the last of those that hold any mass.
-    const double want = (double)p.u_sample[b] * total;
+    const double want = (double)p.u_sample[b] * (total * kDown);
     int mine = -1;
     double before = 0.0, run = 0.0;
+    const double of_lane = part.blocks == 1 ? total * kDown : lane < part.blocks ? of_block(&sm.block_sum[round & 1], lane) : 0.0;
     for (int k = 0; k < part.blocks; ++k) {
-        const double s = part.blocks == 1 ? total : of_block(&sm.block_sum[round & 1], k);
+        const double s = __shfl_sync(0xffffffffu, of_lane, k);
         if (s > 0.0) { mine = k; before = run; }
         run += s;
         if (run > want) break;
     }
     if (part.blocks > 1) cluster_sync();                      // (no block leaves while its sums are read)
     if (!(total > 0.0) || mine != part.rank) return;
-    run = before;
-    mine = -1;
-    for (int w = 0; w < kWarps; ++w) {
-        const double s = sm.warp_sum[w];
-        if (s > 0.0) { mine = w; before = run; }
-        run += s;
-        if (run > want) break;
+    auto share_of = [&] {                                     // the warp whose share it is in; `before`: what stands before it
+        run = before;
+        mine = 0;
+        for (int w = 0; w < kWarps; ++w) {
+            const double s = sm.warp_sum[w];
+            if (s > 0.0) { mine = w; before = run; }
+            run += s;
+            if (run > want) break;
+        }
+    };
+    share_of();
+    // that share is divided among the block's warps once more (one warp alone would go through it a step after another)
+    const int share = last.hi_of(part, part.rank * kWarps + mine) - last.lo_of(part, part.rank * kWarps + mine);
+    if (share > 512) {
+        const int piece = ((share + kWarps - 1) / kWarps + 7) & ~7, lo = last.lo_of(part, part.rank * kWarps + mine), hi = lo + share;
+        last.lo = min(hi, lo + warp * piece);
+        last.hi = min(hi, last.lo + piece);
+        double sum = last.sum(sm, lane);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        __syncthreads();
+        if (lane == 0) sm.warp_sum[warp] = sum;
+        __syncthreads();
+        share_of();
     }
     if (warp != mine) return;
-    const int lo = part.lo + warp * part.share, hi = min(part.hi, lo + part.share);
-    int pick = lo;
+    // the 256 places, then the lane, then its token
+    int pick = last.lo;
     run = before;
-    for (int v0 = lo; v0 < hi && !(run > want); v0 += 256) {
+    for (int x0 = last.lo; last.hi - last.lo > 256 && x0 < last.hi && !(run > want); x0 += 256) {
         double r[8];
-        last.load(sm, v0, hi, lane, r);
+        last.load(sm, x0 + 8 * lane, r);
         double sum = ((r[0] + r[1]) + (r[2] + r[3])) + ((r[4] + r[5]) + (r[6] + r[7]));
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (sum > 0.0) { pick = v0; before = run; }
+        if (sum > 0.0) { pick = x0; before = run; }
         run += sum;
     }
     double r[8];
-    last.load(sm, pick, hi, lane, r);
+    last.load(sm, pick + 8 * lane, r);
+    const double mine_sum = ((r[0] + r[1]) + (r[2] + r[3])) + ((r[4] + r[5]) + (r[6] + r[7]));
+    double upto = mine_sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
+    }
+    const uint32_t some = __ballot_sync(0xffffffffu, mine_sum > 0.0);
+    const uint32_t above = __ballot_sync(0xffffffffu, mine_sum > 0.0 && before + upto > want);
+    if (lane != (above ? __ffs(above) - 1 : 31 - __clz(some))) return;
+    double at = before + (upto - mine_sum);
     int found = -1;
-    bool done = false;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        double scan = r[j];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const double y = __shfl_up_sync(0xffffffffu, scan, o);
-            if (lane >= o) scan += y;
-        }
-        const uint32_t some = __ballot_sync(0xffffffffu, r[j] > 0.0);
-        const uint32_t here = __ballot_sync(0xffffffffu, r[j] > 0.0 && before + scan > want);
-        if (!done && some) found = pick + 32 * j + (here ? __ffs(here) - 1 : 31 - __clz(some));
-        done = done || here != 0;
-        before += __shfl_sync(0xffffffffu, scan, 31);
+        if (r[j] > 0.0 && (found < 0 || !(at > want))) found = pick + 8 * lane + j - last.shift;
+        at += r[j];
     }
-    if (lane == 0) p.next_token[b] = found;
+    p.next_token[b] = found;
 }
 
 template <typename P, bool kDraft>
 cudaError_t launch(const VerifyParams& p, int B, cudaStream_t s) {
-    // Blocks to a sequence: enough to fill the device, each with at least a few thousand tokens.
+    // Blocks to a sequence: as many as are resident at once (two to an SM), each with a thousand tokens at least.
     int blocks = 1;
-    while (blocks < 8 && blocks * B < 2 * 148 && p.V / (2 * blocks) >= 2048) blocks *= 2;
+    while (blocks < kMaxBlocks && 2 * blocks * B <= 2 * 148 && p.V / (2 * blocks) >= 1024) blocks *= 2;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = blocks;
@@ -339,7 +444,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_verify(
     p.T = T; p.V = V;
     p.distinct = flags & BAKLAVA_VERIFY_DISTINCT ? 1 : 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (B > (1 << 27)) return BAKLAVA_ERR_UNSUPPORTED;
+    if (B > (1 << 27) || V > (1 << 30)) return BAKLAVA_ERR_UNSUPPORTED;
     cudaError_t e;
     if (prob_dtype == BAKLAVA_PROB_F32) e = draft ? launch<float, true>(p, B, s) : launch<float, false>(p, B, s);
     else e = draft ? launch<__nv_bfloat16, true>(p, B, s) : launch<__nv_bfloat16, false>(p, B, s);
