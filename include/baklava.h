@@ -469,6 +469,7 @@ int baklava_tree_verify(const void* target, int64_t target_stride, const void* d
  *   3. if it then holds more than cap - 1 rows, it is cut to cap - 1 by the retention policy as baklava_evict does it (sinks
  *      and the last W positions stay, of the rest the lowest scores go, among equal ones the latest; W as for the decode
  *      step, positions counted from t_pos[b] + a - 1)                                                     (Eq. 5-6)
+ * 4-bit rows join with the scale max |y| * fl32(1 / 7), which may differ by one rounding from the other calls' quotient.
  * Rows that stay keep their slots.  The joining rows that stay take the free slots in ascending order; the next free
  * slot becomes free_slot.  Freed slots keep what they held.  Flags as for the decode step: NO_SCORE leaves scores as they are
  * (joining rows have 0) and implies NO_EVICT except under sinks + window, where the oldest rows go; NO_EVICT: a path that does

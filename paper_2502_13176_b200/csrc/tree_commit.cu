@@ -6,8 +6,8 @@
 // row supply two MMA steps or more; the contraction's order is free, the queries are laid out to match), 16 rows to a
 // warp, against the queries of the path's nodes only: the drafts that were refused cost nothing here.
 //
-// A block then holds the new scores of its rows and lists those that would leave first, as many as the head has to give
-// up.  The second kernel joins the lists of a head, picks the rows that leave, and writes the joining ones.
+// A warp brings its rows' scores up to date and lists those that would leave first, as many as the head has to give up.  The
+// second kernel joins the lists of a head, picks the rows that leave, and writes the joining ones.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -27,9 +27,8 @@ using namespace tree;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kBlockRows = 1024;              // rows of a head to a block
-constexpr int kRowsPerThread = kBlockRows / kThreads;
 constexpr int kMaxTree = BAKLAVA_MAX_TREE;
+constexpr int kMaxEntries = 512;              // of a head's lists that are ranked in one go
 
 struct CommitParams {
     Slabs c;
@@ -42,10 +41,10 @@ struct CommitParams {
     const int32_t* t_pos;
     int32_t* t_next;                // or null
     const int4* items;
-    unsigned long long* best_key;   // [n_items][subs][max_path + 1], ascending; ~0: none
+    unsigned long long* best_key;   // [n_items][max_path + 1]: the item's rows that would leave first, ascending; ~0: none
     int32_t* best_slot;
-    float* fresh;                   // [n_items][max_path]: the joining rows' scores (in the place of a head's first item)
-    int32_t T, g, D, Hq, layer_begin, max_path, subs, n_sink, recent_num, recent_den;
+    float* fresh;                   // [n_units][max_path]: the joining rows' scores
+    int32_t T, g, D, Hq, layer_begin, max_path, n_sink, recent_num, recent_den;
     int32_t scored, evict;          // scores are kept; rows may leave
     float scale_log2;
 };
@@ -132,222 +131,283 @@ struct Format {
 constexpr int kColumnPad = 64;                // bytes between the columns' rows in shared memory: no bank conflicts
 constexpr int kMaxColumns = 256;              // columns in shared memory at a time (long paths of large groups take several rounds)
 
-template <int D, int KV>
-__global__ void __launch_bounds__(kThreads, 2) path_scores_kernel(const __grid_constant__ CommitParams p) {
-    using F = Format<D, KV>;
-    constexpr int kColumnBytes = 2 * D + kColumnPad;
-    extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ float sums[kBlockRows];
-    __shared__ unsigned long long lists[kWarps][kMaxTree + 1];
-    __shared__ int list_slots[kWarps][kMaxTree + 1];
+// The first `leave` of a warp's rows in the order in which rows leave, ascending, in shared memory.  Few rows get in once the
+// list is full: a key is looked at only if it is below the last one.
+struct LeaveList {
+    unsigned long long keys[96];
+    int slots[96];
+};
+__device__ __forceinline__ void start_list(LeaveList& list, int lane) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) list.keys[lane + 32 * i] = ~0ull;
+    __syncwarp();
+}
+// every lane's key (~0: none); `last`: the list's entry leave - 1
+__device__ __forceinline__ void enlist(LeaveList& list, unsigned long long key, int slot, int leave, unsigned long long& last, int lane) {
+    while (__any_sync(0xffffffffu, key < last)) {
+        const unsigned long long first = warp_min(key);
+        const int who = __ffs(__ballot_sync(0xffffffffu, key == first)) - 1, its = __shfl_sync(0xffffffffu, slot, who);
+        if (lane == who) key = ~0ull;
+        unsigned long long e[3];
+        int f[3], at = 0;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            if (32 * i >= leave) continue;
+            e[i] = list.keys[lane + 32 * i];
+            f[i] = list.slots[lane + 32 * i];
+            at += __popc(__ballot_sync(0xffffffffu, e[i] < first));
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const int k = lane + 32 * i;
+            if (32 * i >= leave || k < at || k + 1 >= leave) continue;
+            list.keys[k + 1] = e[i];
+            list.slots[k + 1] = f[i];
+        }
+        if (lane == 0) { list.keys[at] = first; list.slots[at] = its; }
+        __syncwarp();
+        last = list.keys[leave - 1];
+    }
+}
+// The warps' lists joined into the item's.  The whole block.
+__device__ __forceinline__ void write_list(const CommitParams& p, const LeaveList* lists, int leave, int warp, int lane) {
+    __syncthreads();
+    if (warp != 0) return;
+    const int64_t at = (int64_t)blockIdx.x * (p.max_path + 1);
+    int cursor = 0;                                           // lane = warp whose list it reads
+    for (int n = 0; n < leave; ++n) {
+        const unsigned long long head = lane < kWarps && cursor < leave ? lists[lane].keys[cursor] : ~0ull;
+        const unsigned long long first = warp_min(head);
+        if (lane == __ffs(__ballot_sync(0xffffffffu, head == first)) - 1) {
+            p.best_key[at + n] = first;
+            if (first != ~0ull) p.best_slot[at + n] = lists[lane].slots[cursor];
+            ++cursor;
+        }
+    }
+}
+
+// Positions only: the oldest rows of an item.
+__global__ void __launch_bounds__(kThreads) oldest_rows_kernel(const __grid_constant__ CommitParams p) {
+    __shared__ LeaveList lists[kWarps];
     const int4 item = p.items[blockIdx.x];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, sub = blockIdx.y;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    launch_dependents();
     const Unit u(p.c, p.layer_begin, item.x);
     const Head hd(p.c, u);
     const Job job(p, u, hd);
-    const int lo = item.y + sub * kBlockRows, hi = min(min(item.y + item.z, lo + kBlockRows), hd.slots);
-    const int top = p.max_path + 1;
-    const int64_t list_at = ((int64_t)blockIdx.x * p.subs + sub) * top;
-    if (job.idle || job.bad) return;                          // (the second kernel reports what is bad)
-    if (sub == p.subs) {
-        // the joining rows' own scores: one warp per row, its node and those behind it on the path
-        if ((item.w & 0xffff) != 0 || !p.scored) return;
-        const int32_t* const path = p.path + (int64_t)u.b * p.T;
-        constexpr int kE = D / 32;
-        const int64_t head0 = (int64_t)u.li * p.c.B + u.b;
-        for (int j = warp; j < job.a; j += kWarps) {
-            const __nv_bfloat16* const kj = p.k + ((head0 * p.c.Hkv + u.h) * p.T + path[j]) * D + kE * lane;
-            float x[kE], total = 0.0f;
+    if (job.idle || job.bad || job.leave == 0) return;        // (the second kernel reports what is bad)
+    const int hi = min(item.y + item.z, hd.slots);
+    start_list(lists[warp], lane);
+    unsigned long long last = ~0ull;
+    for (int j0 = item.y + warp * 32; j0 < hi; j0 += 4 * kThreads) {
+        int pos[4];
 #pragma unroll
-            for (int e = 0; e < kE; ++e) x[e] = __bfloat162float(kj[e]);
-            for (int i = j; i < job.a; ++i)
-                for (int a = 0; a < p.g; ++a) {
-                    const int64_t row = (head0 * p.Hq + u.h * p.g + a) * p.T + path[i];
-                    const __nv_bfloat16* const qi = p.q + row * D + kE * lane;
-                    float s = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < kE; ++e) s = fmaf(__bfloat162float(qi[e]), x[e], s);
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                    total += exp2f(fmaf(s, p.scale_log2, -p.lse[row] * kLog2e));
-                }
-            if (lane == 0) p.fresh[(int64_t)blockIdx.x * p.max_path + j] = total;
+        for (int i = 0; i < 4; ++i) {
+            const int j = j0 + i * kThreads + lane;
+            pos[i] = j < hi && j != hd.hole ? p.c.pos[hd.first + j] : -1;
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            enlist(lists[warp], pos[i] >= p.n_sink && pos[i] <= job.newest ? leave_key(false, 0.0f, pos[i]) : ~0ull,
+                   j0 + i * kThreads + lane, job.leave, last, lane);
+    }
+    write_list(p, lists, job.leave, warp, lane);
+}
+
+// The joining rows' own scores: one warp per row, its node and those behind it on the path.
+template <int D>
+__device__ __forceinline__ void fresh_scores(const CommitParams& p, int unit, int warp, int lane) {
+    constexpr int kE = D / 32;
+    const Unit u(p.c, p.layer_begin, unit);
+    const Head hd(p.c, u);
+    const Job job(p, u, hd);
+    if (job.idle || job.bad) return;
+    const int32_t* const path = p.path + (int64_t)u.b * p.T;
+    const int64_t head0 = (int64_t)u.li * p.c.B + u.b;
+    for (int j = warp; j < job.a; j += kWarps) {
+        const __nv_bfloat16* const kj = p.k + ((head0 * p.c.Hkv + u.h) * p.T + path[j]) * D + kE * lane;
+        float x[kE], total = 0.0f;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) x[e] = __bfloat162float(kj[e]);
+        for (int i = j; i < job.a; ++i) {
+            const int64_t row0 = (head0 * p.Hq + u.h * p.g) * p.T + path[i];
+            float s[BAKLAVA_MAX_GROUP];
+#pragma unroll
+            for (int a = 0; a < BAKLAVA_MAX_GROUP; ++a) {
+                s[a] = 0.0f;
+                if (a >= p.g) continue;
+                const __nv_bfloat16* const qi = p.q + (row0 + (int64_t)a * p.T) * D + kE * lane;
+#pragma unroll
+                for (int e = 0; e < kE; ++e) s[a] = fmaf(__bfloat162float(qi[e]), x[e], s[a]);
+            }
+#pragma unroll
+            for (int a = 0; a < BAKLAVA_MAX_GROUP; ++a) {
+                if (a >= p.g) continue;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) s[a] += __shfl_xor_sync(0xffffffffu, s[a], o);
+                total += exp2f(fmaf(s[a], p.scale_log2, -p.lse[row0 + (int64_t)a * p.T] * kLog2e));
+            }
+        }
+        if (lane == 0) p.fresh[(int64_t)unit * p.max_path + j] = total;
+    }
+}
+
+// What a warp has asked for of sixteen rows: a lane's pieces of rows r and r + 8 (r = lane / 4) and, the first sixteen lanes,
+// a row's score and position.
+template <int D, int KV>
+struct Rows {
+    uint4 low[Format<D, KV>::kPieces], high[Format<D, KV>::kPieces];
+    float scale_low, scale_high, score;
+    int pos;
+    __device__ __forceinline__ void fetch(const CommitParams& p, const Head& hd, const uint8_t* slab, int j0, int hi, int lane) {
+        using F = Format<D, KV>;
+        const int r = lane >> 2, c = lane & 3, row0 = min(j0 + r, hi - 1), row1 = min(j0 + r + 8, hi - 1);   // (behind the end: not used)
+#pragma unroll
+        for (int i = 0; i < F::kPieces; ++i) {
+            low[i] = __ldg(reinterpret_cast<const uint4*>(slab + (int64_t)row0 * F::kRowBytes + i * 64 + c * 16));
+            high[i] = __ldg(reinterpret_cast<const uint4*>(slab + (int64_t)row1 * F::kRowBytes + i * 64 + c * 16));
+        }
+        if (KV == BAKLAVA_KV_INT4) {
+            scale_low = p.c.row_scale[2 * (hd.first + row0)];
+            scale_high = p.c.row_scale[2 * (hd.first + row1)];
+        }
+        const int j = j0 + lane;
+        const bool there = lane < 16 && j < hi && j != hd.hole;
+        score = there ? p.c.score[hd.first + j] : 0.0f;
+        pos = there ? p.c.pos[hd.first + j] : -1;
+    }
+};
+
+// One block per item (a chunk of a head), its warps on their own: sixteen rows at a time against all of the path's queries, the
+// next sixteen asked for meanwhile.  Behind the items a block per unit for the joining rows' own scores.
+template <int D, int KV>
+__global__ void __launch_bounds__(kThreads, 2) path_scores_kernel(const __grid_constant__ CommitParams p, const int n_items) {
+    using F = Format<D, KV>;
+    constexpr int kColumnBytes = 2 * D + kColumnPad;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ LeaveList lists[kWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    launch_dependents();
+    if ((int)blockIdx.x >= n_items) {
+        fresh_scores<D>(p, (int)blockIdx.x - n_items, warp, lane);
         return;
     }
-    if (lo >= hi) {                                           // no rows: an empty list
-        for (int i = tid; i < job.leave; i += kThreads) p.best_key[list_at + i] = ~0ull;
-        return;
-    }
-    // what the end needs of the rows, asked for now
-    int pos[kRowsPerThread];
-    float score[kRowsPerThread];
-#pragma unroll
-    for (int i = 0; i < kRowsPerThread; ++i) {
-        const int j = lo + tid + i * kThreads;
-        const bool there = j < hi && j != hd.hole;
-        pos[i] = there ? p.c.pos[hd.first + j] : -1;
-        score[i] = there && p.scored ? p.c.score[hd.first + j] : 0.0f;
-    }
-    if (p.scored) {
-        const int all = job.a * p.g;
-        float2* const of_column = reinterpret_cast<float2*>(smem + min((p.max_path * p.g + 7) / 8 * 8, kMaxColumns) * kColumnBytes * F::kTerms);
-        const int32_t* const path = p.path + (int64_t)u.b * p.T;
-        for (int col0 = 0; col0 < all; col0 += kMaxColumns) {
-            const int columns = min(all - col0, kMaxColumns), blocks = (columns + 7) / 8;
-            if (col0 > 0) __syncthreads();
-            for (int n = warp; n < blocks * 8; n += kWarps) {     // the queries, column = node column / g, head column % g
-                constexpr int kE = D / 32;
-                float x[kE];                                      // dimensions lane + 32 e
-                float lse2 = INFINITY, factor = 0.0f;             // a column that is none adds exp2(-inf)
-                int64_t row = 0;
-                if (n < columns) {
-                    row = (((int64_t)u.li * p.c.B + u.b) * p.Hq + u.h * p.g + (col0 + n) % p.g) * p.T + path[(col0 + n) / p.g];
-                    lse2 = p.lse[row] * kLog2e;
-                    factor = p.scale_log2;
-                }
-#pragma unroll
-                for (int e = 0; e < kE; ++e) {
-                    x[e] = n < columns ? __bfloat162float(p.q[row * D + lane + 32 * e]) : 0.0f;
-                    if (KV == BAKLAVA_KV_INT4) x[e] *= p.c.kv_scale[(int64_t)u.head * 4 * D + lane + 32 * e];
-                }
-                if (KV != BAKLAVA_KV_BF16) {
-                    float big = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < kE; ++e) big = fmaxf(big, fabsf(x[e]));
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-                    int power;
-                    frexpf(big, &power);                          // big = f 2^power, f in 0.5 .. 1
-                    power = big > 0.0f && big < INFINITY ? power - 15 : 0;
-#pragma unroll
-                    for (int e = 0; e < kE; ++e) x[e] = ldexpf(x[e], -power);
-                    factor = ldexpf(factor, power);
-                    if (KV == BAKLAVA_KV_FP8_E4M3) factor *= p.c.kv_scale[(int64_t)u.head * 4];
-                }
-                // dimension d goes to pair t, lane c, element e of the column: the inverse of Format::dim
-#pragma unroll
-                for (int e = 0; e < kE; ++e) {
-                    const int d = lane + 32 * e;
-                    int t, c, i;
-                    if (KV == BAKLAVA_KV_BF16) { t = d >> 5; c = (d >> 3) & 3; i = d & 7; }
-                    else if (KV == BAKLAVA_KV_FP8_E4M3) { t = (d >> 6) * 2 + ((d >> 3) & 1); c = (d >> 4) & 3; i = d & 7; }
-                    else { t = (d >> 3) & 3; c = d >> 5; i = (d & 3) * 2 + ((d >> 2) & 1); }
-                    uint8_t* const at = smem + (size_t)n * F::kTerms * kColumnBytes + t * 64 + c * 16 + i * 2;
-                    if (KV == BAKLAVA_KV_BF16) {
-                        *reinterpret_cast<__nv_bfloat16*>(at) = __float2bfloat16(x[e]);
-                    } else {
-                        const __half high = __float2half_rn(x[e]);
-                        *reinterpret_cast<__half*>(at) = high;
-                        if (F::kTerms == 2) *reinterpret_cast<__half*>(at + kColumnBytes) = __float2half_rn(x[e] - __half2float(high));
-                    }
-                }
-                if (lane == 0) of_column[n] = make_float2(factor, lse2);
+    const int4 item = p.items[blockIdx.x];
+    const Unit u(p.c, p.layer_begin, item.x);
+    const Head hd(p.c, u);
+    const Job job(p, u, hd);
+    if (job.idle || job.bad) return;                          // (the second kernel reports what is bad)
+    const int lo = item.y, hi = min(item.y + item.z, hd.slots);
+    const uint8_t* const slab = static_cast<const uint8_t*>(p.c.k) + hd.first * F::kRowBytes;
+    start_list(lists[warp], lane);
+    unsigned long long last = ~0ull;
+    const int all = job.a * p.g;
+    float2* const of_column = reinterpret_cast<float2*>(smem + min((p.max_path * p.g + 7) / 8 * 8, kMaxColumns) * kColumnBytes * F::kTerms);
+    const int32_t* const path = p.path + (int64_t)u.b * p.T;
+    for (int col0 = 0; col0 < all; col0 += kMaxColumns) {
+        const int columns = min(all - col0, kMaxColumns), blocks = (columns + 7) / 8;
+        Rows<D, KV> rows;
+        int j0 = lo + warp * 16;
+        if (j0 < hi) rows.fetch(p, hd, slab, j0, hi, lane);
+        if (col0 > 0) __syncthreads();
+        for (int n = warp; n < blocks * 8; n += kWarps) {     // the queries, column = node column / g, head column % g
+            constexpr int kE = D / 32;
+            float x[kE];                                      // dimensions lane + 32 e
+            float lse2 = INFINITY, factor = 0.0f;             // a column that is none adds exp2(-inf)
+            int64_t row = 0;
+            if (n < columns) {
+                row = (((int64_t)u.li * p.c.B + u.b) * p.Hq + u.h * p.g + (col0 + n) % p.g) * p.T + path[(col0 + n) / p.g];
+                lse2 = p.lse[row] * kLog2e;
+                factor = p.scale_log2;
             }
-            __syncthreads();
-            const uint8_t* const slab = static_cast<const uint8_t*>(p.c.k) + hd.first * F::kRowBytes;
-            const int r = lane >> 2, c = lane & 3;
-            for (int j0 = lo + warp * 16; j0 < hi; j0 += kWarps * 16) {
-                const int row0 = min(j0 + r, hi - 1), row1 = min(j0 + r + 8, hi - 1);            // (behind the end: not used)
-                uint4 raw0[F::kPieces], raw1[F::kPieces];
 #pragma unroll
-                for (int i = 0; i < F::kPieces; ++i) {
-                    raw0[i] = __ldg(reinterpret_cast<const uint4*>(slab + (int64_t)row0 * F::kRowBytes + i * 64 + c * 16));
-                    raw1[i] = __ldg(reinterpret_cast<const uint4*>(slab + (int64_t)row1 * F::kRowBytes + i * 64 + c * 16));
-                }
-                float rs0 = 1.0f, rs1 = 1.0f;
-                if (KV == BAKLAVA_KV_INT4) {
-                    rs0 = p.c.row_scale[2 * (hd.first + row0)];
-                    rs1 = p.c.row_scale[2 * (hd.first + row1)];
-                }
-                float sum0 = 0.0f, sum1 = 0.0f;
-                for (int nb = 0; nb < blocks; ++nb) {
-                    float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    const uint8_t* const column = smem + (size_t)(nb * 8 + r) * F::kTerms * kColumnBytes + c * 16;
+            for (int e = 0; e < kE; ++e) {
+                x[e] = n < columns ? __bfloat162float(p.q[row * D + lane + 32 * e]) : 0.0f;
+                if (KV == BAKLAVA_KV_INT4) x[e] *= p.c.kv_scale[(int64_t)u.head * 4 * D + lane + 32 * e];
+            }
+            if (KV != BAKLAVA_KV_BF16) {
+                float big = 0.0f;
 #pragma unroll
-                    for (int t = 0; t < D / 32; ++t) {
-                        uint32_t a0[4], a1[4];
-                        F::operand(raw0, t, a0);
-                        F::operand(raw1, t, a1);
+                for (int e = 0; e < kE; ++e) big = fmaxf(big, fabsf(x[e]));
 #pragma unroll
-                        for (int term = 0; term < F::kTerms; ++term) {
-                            const uint4 b = *reinterpret_cast<const uint4*>(column + term * kColumnBytes + t * 64);
-                            if (KV == BAKLAVA_KV_BF16) {
-                                mma_bf16(d, a0[0], a1[0], a0[1], a1[1], b.x, b.y);
-                                mma_bf16(d, a0[2], a1[2], a0[3], a1[3], b.z, b.w);
-                            } else {
-                                mma_f16(d, a0[0], a1[0], a0[1], a1[1], b.x, b.y);
-                                mma_f16(d, a0[2], a1[2], a0[3], a1[3], b.z, b.w);
-                            }
-                        }
-                    }
-                    const float4 two = *reinterpret_cast<const float4*>(of_column + nb * 8 + 2 * c);   // (factor, lse) of two columns
-                    sum0 += fast_exp2(fmaf(d[0] * rs0, two.x, -two.y)) + fast_exp2(fmaf(d[1] * rs0, two.z, -two.w));
-                    sum1 += fast_exp2(fmaf(d[2] * rs1, two.x, -two.y)) + fast_exp2(fmaf(d[3] * rs1, two.z, -two.w));
-                }
-                sum0 += __shfl_xor_sync(0xffffffffu, sum0, 1);
-                sum0 += __shfl_xor_sync(0xffffffffu, sum0, 2);
-                sum1 += __shfl_xor_sync(0xffffffffu, sum1, 1);
-                sum1 += __shfl_xor_sync(0xffffffffu, sum1, 2);
-                if (c == 0) {
-                    float* const to = sums + j0 + r - lo;          // (always the same lane's)
-                    to[0] = col0 > 0 ? to[0] + sum0 : sum0;
-                    to[8] = col0 > 0 ? to[8] + sum1 : sum1;
+                for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+                int power;
+                frexpf(big, &power);                          // big = f 2^power, f in 0.5 .. 1
+                power = big > 0.0f && big < INFINITY ? power - 15 : 0;
+#pragma unroll
+                for (int e = 0; e < kE; ++e) x[e] = ldexpf(x[e], -power);
+                factor = ldexpf(factor, power);
+                if (KV == BAKLAVA_KV_FP8_E4M3) factor *= p.c.kv_scale[(int64_t)u.head * 4];
+            }
+            // dimension d goes to pair t, lane c, element i of the column: the inverse of Format::dim
+#pragma unroll
+            for (int e = 0; e < kE; ++e) {
+                const int d = lane + 32 * e;
+                int t, c, i;
+                if (KV == BAKLAVA_KV_BF16) { t = d >> 5; c = (d >> 3) & 3; i = d & 7; }
+                else if (KV == BAKLAVA_KV_FP8_E4M3) { t = (d >> 6) * 2 + ((d >> 3) & 1); c = (d >> 4) & 3; i = d & 7; }
+                else { t = (d >> 3) & 3; c = d >> 5; i = (d & 3) * 2 + ((d >> 2) & 1); }
+                uint8_t* const at = smem + (size_t)n * F::kTerms * kColumnBytes + t * 64 + c * 16 + i * 2;
+                if (KV == BAKLAVA_KV_BF16) {
+                    *reinterpret_cast<__nv_bfloat16*>(at) = __float2bfloat16(x[e]);
+                } else {
+                    const __half high = __float2half_rn(x[e]);
+                    *reinterpret_cast<__half*>(at) = high;
+                    if (F::kTerms == 2) *reinterpret_cast<__half*>(at + kColumnBytes) = __float2half_rn(x[e] - __half2float(high));
                 }
             }
+            if (lane == 0) of_column[n] = make_float2(factor, lse2);
         }
         __syncthreads();
+        const int r = lane >> 2, c = lane & 3;
+        while (j0 < hi) {
+            uint32_t a0[D / 32][4], a1[D / 32][4];
 #pragma unroll
-        for (int i = 0; i < kRowsPerThread; ++i) {
-            const int j = lo + tid + i * kThreads;
-            if (j < hi && j != hd.hole) {
-                score[i] += sums[j - lo];
-                p.c.score[hd.first + j] = score[i];
+            for (int t = 0; t < D / 32; ++t) {
+                F::operand(rows.low, t, a0[t]);
+                F::operand(rows.high, t, a1[t]);
             }
-        }
-    }
-    if (job.leave == 0) return;
-    // each warp's first `leave` rows in the order, then the warps' lists joined
-    unsigned long long key[kRowsPerThread];
+            const float rs0 = KV == BAKLAVA_KV_INT4 ? rows.scale_low : 1.0f, rs1 = KV == BAKLAVA_KV_INT4 ? rows.scale_high : 1.0f;
+            const float score = rows.score;
+            const int pos = rows.pos, j = j0 + lane;
+            j0 += kWarps * 16;
+            if (j0 < hi) rows.fetch(p, hd, slab, j0, hi, lane);
+            float sum0 = 0.0f, sum1 = 0.0f;
+            for (int nb = 0; nb < blocks; ++nb) {
+                float d[2][4] = {};                           // two chains of products
+                const uint8_t* const column = smem + (size_t)(nb * 8 + r) * F::kTerms * kColumnBytes + c * 16;
 #pragma unroll
-    for (int i = 0; i < kRowsPerThread; ++i)
-        key[i] = pos[i] >= p.n_sink && pos[i] <= job.newest ? leave_key(p.scored, score[i], pos[i]) : ~0ull;
-    for (int n = 0; n < job.leave; ++n) {
-        unsigned long long best = key[0];
+                for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-        for (int i = 1; i < kRowsPerThread; ++i) best = key[i] < best ? key[i] : best;
-        const unsigned long long first = warp_min(best);
-        const uint32_t who = __ballot_sync(0xffffffffu, best == first);
-        if (lane == __ffs(who) - 1) {
-            int at = -1;
-#pragma unroll
-            for (int i = kRowsPerThread - 1; i >= 0; --i)
-                if (key[i] == first) at = i;
-            lists[warp][n] = first;
-            list_slots[warp][n] = lo + tid + at * kThreads;
-#pragma unroll
-            for (int i = 0; i < kRowsPerThread; ++i)
-                if (i == at) key[i] = ~0ull;
-        }
-        if (first == ~0ull) {
-            for (int i = n + lane; i < job.leave; i += 32) lists[warp][i] = ~0ull;
-            break;
-        }
-    }
-    __syncthreads();
-    if (warp == 0) {
-        int cursor = 0;                                       // lane = warp whose list it reads
-        for (int n = 0; n < job.leave; ++n) {
-            const unsigned long long head = lane < kWarps && cursor < job.leave ? lists[lane][cursor] : ~0ull;
-            const unsigned long long first = warp_min(head);
-            const uint32_t who = __ballot_sync(0xffffffffu, head == first);
-            if (lane == __ffs(who) - 1) {
-                p.best_key[list_at + n] = first;
-                if (first != ~0ull) p.best_slot[list_at + n] = list_slots[lane][cursor];
-                ++cursor;
+                    for (int term = 0; term < F::kTerms; ++term) {
+                        const uint4 b = *reinterpret_cast<const uint4*>(column + term * kColumnBytes + t * 64);
+                        if (KV == BAKLAVA_KV_BF16) {
+                            mma_bf16(d[0], a0[t][0], a1[t][0], a0[t][1], a1[t][1], b.x, b.y);
+                            mma_bf16(d[1], a0[t][2], a1[t][2], a0[t][3], a1[t][3], b.z, b.w);
+                        } else {
+                            mma_f16(d[0], a0[t][0], a1[t][0], a0[t][1], a1[t][1], b.x, b.y);
+                            mma_f16(d[1], a0[t][2], a1[t][2], a0[t][3], a1[t][3], b.z, b.w);
+                        }
+                    }
+                const float4 two = *reinterpret_cast<const float4*>(of_column + nb * 8 + 2 * c);   // (factor, lse) of two columns
+                sum0 += fast_exp2(fmaf((d[0][0] + d[1][0]) * rs0, two.x, -two.y)) + fast_exp2(fmaf((d[0][1] + d[1][1]) * rs0, two.z, -two.w));
+                sum1 += fast_exp2(fmaf((d[0][2] + d[1][2]) * rs1, two.x, -two.y)) + fast_exp2(fmaf((d[0][3] + d[1][3]) * rs1, two.z, -two.w));
             }
+            sum0 += __shfl_xor_sync(0xffffffffu, sum0, 1);
+            sum0 += __shfl_xor_sync(0xffffffffu, sum0, 2);
+            sum1 += __shfl_xor_sync(0xffffffffu, sum1, 1);
+            sum1 += __shfl_xor_sync(0xffffffffu, sum1, 2);
+            // lane i < 16 takes row i
+            const float mine0 = __shfl_sync(0xffffffffu, sum0, (lane & 7) * 4), mine1 = __shfl_sync(0xffffffffu, sum1, (lane & 7) * 4);
+            const float now = score + (lane < 8 ? mine0 : mine1);
+            const bool there = lane < 16 && j < hi && j != hd.hole;
+            if (there) p.c.score[hd.first + j] = now;
+            if (job.leave > 0 && col0 + kMaxColumns >= all)
+                enlist(lists[warp], there && pos >= p.n_sink && pos <= job.newest ? leave_key(true, now, pos) : ~0ull, j, job.leave, last, lane);
         }
     }
+    if (job.leave > 0) write_list(p, lists, job.leave, warp, lane);
 }
 
 // A head's lists joined, the rows that leave, the rows that join.  Blocks of items that are not a head's first have
@@ -358,9 +418,9 @@ __global__ void __launch_bounds__(kThreads) join_rows_kernel(const __grid_consta
     if ((item.w & 0xffff) != 0) return;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const Unit u(p.c, p.layer_begin, item.x);
-    grid_dependency_wait();
     const Head hd(p.c, u);
     const Job job(p, u, hd);
+    grid_dependency_wait();                                   // (the first kernel reads a head's state, this one changes it)
     if (p.t_next && u.li == 0 && u.h == 0 && tid == 0) p.t_next[u.b] = job.idle || job.bad ? p.t_pos[u.b] : job.t0 + job.a;
     if (job.idle) return;
     if (job.bad || job.overflow) {
@@ -372,28 +432,58 @@ __global__ void __launch_bounds__(kThreads) join_rows_kernel(const __grid_consta
     __shared__ int open[3 * kMaxTree], sorted[3 * kMaxTree];
     __shared__ int to[kMaxTree];                              // slot of each joining row, or -1
     __shared__ float fresh[kMaxTree];
+    __shared__ unsigned long long entry[kMaxEntries];
+    __shared__ int found;
     int last = 0;
     const int pieces = item.w >> 16, top = p.max_path + 1, a = job.a;
     if (tid < a) {
         to[tid] = 0;
-        fresh[tid] = p.scored ? p.fresh[(int64_t)blockIdx.x * p.max_path + tid] : 0.0f;
+        fresh[tid] = p.scored ? p.fresh[(int64_t)item.x * p.max_path + tid] : 0.0f;
     }
+    if (tid == 0) found = 0;
     __syncthreads();
     if (job.leave > 0) {
-        // The blocks' lists, eight to a thread at a time (a head of over two million rows has more: what the batch before
-        // left is then one more list); the joining rows are candidates of their own, one to a thread.
-        constexpr int kHeld = 8;
-        const int lists = pieces * p.subs;
+        // The items' lists, each from its first entry on; the joining rows are candidates of their own, one to a thread.
+        const int lists = pieces;
         unsigned long long mine = ~0ull;
         if (tid < a) {
             const int ps = job.t0 + tid;
             if (ps >= p.n_sink && ps <= job.newest) mine = leave_key(p.scored, fresh[tid], ps);
         }
-        int kept = 0;                                         // entries of the list of the batch before
+        const int64_t lists_at = (int64_t)blockIdx.x * top;
+        const int entries = lists * job.leave + a;
+        int kept = 0;                                         // rows found that leave
+        if (entries <= kMaxEntries) {
+            // few: all of them in shared memory, each counts those before it (equal keys: by their place)
+            for (int i = tid; i < entries; i += kThreads) {
+                const int list = i / job.leave, n = i - list * job.leave;
+                unsigned long long key = ~0ull;
+                if (i < lists * job.leave) key = __ldcg(p.best_key + lists_at + (int64_t)list * top + n);
+                entry[i] = key;
+            }
+            __syncthreads();
+            if (tid < a) entry[lists * job.leave + tid] = mine;
+            __syncthreads();
+            for (int i = tid; i < entries; i += kThreads) {
+                const unsigned long long key = entry[i];
+                if (key == ~0ull) continue;
+                int rank = 0;
+                for (int k = 0; k < entries; ++k) rank += entry[k] < key || (entry[k] == key && k < i);
+                if (rank >= job.leave) continue;
+                const int list = i / job.leave, n = i - list * job.leave;
+                gone[0][rank] = i < lists * job.leave ? __ldcg(p.best_slot + lists_at + (int64_t)list * top + n) : -1 - (i - lists * job.leave);
+                atomicAdd(&found, 1);
+            }
+            __syncthreads();
+            kept = found;
+        } else {
+        // many: eight lists to a thread at a time (a head of over 2 000 pieces has more: what the batch before left is then
+        // one more list)
+        constexpr int kHeld = 8;
         for (int list0 = 0; list0 < lists; list0 += kHeld * kThreads) {
             const int from = (list0 / (kHeld * kThreads)) & 1, into = from ^ 1;
             auto head_of = [&](int list, int cursor) {
-                return cursor < job.leave ? __ldcg(p.best_key + ((int64_t)blockIdx.x * p.subs + list) * top + cursor) : ~0ull;
+                return cursor < job.leave ? __ldcg(p.best_key + lists_at + (int64_t)list * top + cursor) : ~0ull;
             };
             unsigned long long head[kHeld];
             int at[kHeld], carried = 0, n = 0;
@@ -433,7 +523,7 @@ __global__ void __launch_bounds__(kThreads) join_rows_kernel(const __grid_consta
                         for (int k = 0; k < kHeld; ++k)
                             if (!done && head[k] == first) {
                                 const int list = list0 + tid + k * kThreads;
-                                gone[into][n] = __ldcg(p.best_slot + ((int64_t)blockIdx.x * p.subs + list) * top + at[k]);
+                                gone[into][n] = __ldcg(p.best_slot + lists_at + (int64_t)list * top + at[k]);
                                 head[k] = head_of(list, ++at[k]);
                                 done = true;
                             }
@@ -446,6 +536,7 @@ __global__ void __launch_bounds__(kThreads) join_rows_kernel(const __grid_consta
             // a joining row that did not make this batch's list stays a candidate of none: the lists only get better, and
             // what made it is carried by the list
             mine = ~0ull;
+        }
         }
         if (kept < job.leave) {                               // fewer rows may leave than have to
             if (tid == 0) atomicOr(p.c.status, BAKLAVA_STATUS_BAD_STATE);
@@ -498,7 +589,10 @@ __global__ void __launch_bounds__(kThreads) join_rows_kernel(const __grid_consta
             } else {
                 float y[4];
                 int4q::scaled4(raw, *reinterpret_cast<const float4*>(p.c.kv_scale + ((int64_t)u.head * 4 + 2 * which + 1) * 128 + 4 * lane), y);
-                const float s = int4q::row_scale(__reduce_max_sync(0xffffffffu, int4q::largest_bits(y)));
+                // The scale by the reciprocal of 7, which is what array libraries make of a division by a constant: rows that
+                // were quantised by such code and rows that join here agree bit for bit (from the other calls' quotient it is
+                // one rounding away).
+                const float s = __fmul_rn(__uint_as_float(__reduce_max_sync(0xffffffffu, int4q::largest_bits(y))), 1.0f / 7.0f);
                 *reinterpret_cast<uint16_t*>(slab + row * 64 + 2 * lane) = (uint16_t)int4q::codes4(y, s);
                 if (lane == 0) p.c.row_scale[2 * row + which] = s;
             }
@@ -512,24 +606,22 @@ __global__ void __launch_bounds__(kThreads) join_rows_kernel(const __grid_consta
 
 struct CommitWorkspace {
     size_t slot_off, fresh_off, total;
-    int subs;
 };
 CommitWorkspace layout(const baklava_plan_info* info, int32_t max_path) {
     CommitWorkspace w;
-    w.subs = (std::max(info->chunk_tokens, 1) + kBlockRows - 1) / kBlockRows;
-    const size_t entries = (size_t)info->n_items * w.subs * (max_path + 1);
+    const size_t entries = (size_t)info->n_items * (max_path + 1);
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     w.slot_off = up(entries * 8);
     w.fresh_off = w.slot_off + up(entries * 4);
-    w.total = w.fresh_off + up((size_t)info->n_items * max_path * 4);
+    w.total = w.fresh_off + up((size_t)info->n_units * max_path * 4);
     return w;
 }
 
 template <int D, int KV>
-cudaError_t launch_scores(const CommitParams& p, int n_items, cudaStream_t s) {
+cudaError_t launch_scores(const CommitParams& p, int n_items, int n_units, cudaStream_t s) {
     using F = Format<D, KV>;
     const int columns = std::min((p.max_path * p.g + 7) / 8 * 8, kMaxColumns);
-    const int smem = p.scored ? columns * ((2 * D + kColumnPad) * F::kTerms + 8) : 0;
+    const int smem = columns * ((2 * D + kColumnPad) * F::kTerms + 8);
     static std::atomic<uint64_t> configured{0};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -539,7 +631,7 @@ cudaError_t launch_scores(const CommitParams& p, int n_items, cudaStream_t s) {
         if (e != cudaSuccess) return e;
         if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
     }
-    path_scores_kernel<D, KV><<<dim3((unsigned)n_items, (unsigned)p.subs + 1), kThreads, smem, s>>>(p);
+    path_scores_kernel<D, KV><<<(unsigned)n_items + (unsigned)n_units, kThreads, smem, s>>>(p, n_items);
     return cudaGetLastError();
 }
 
@@ -577,8 +669,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_commit(
         return BAKLAVA_ERR_INVALID_ARG;
     const CommitWorkspace w = layout(info, max_path);
     if (ws_bytes < w.total) return BAKLAVA_ERR_WORKSPACE;
-    // (grid.y counts 1 024-row parts of a chunk; a thread of the second kernel joins up to eight lists)
-    if (w.subs >= 65535) return BAKLAVA_ERR_UNSUPPORTED;
+    if ((int64_t)info->n_items + info->n_units > INT32_MAX) return BAKLAVA_ERR_UNSUPPORTED;
 
     CommitParams p;
     p.c = tree_slabs(shape, cache);
@@ -595,21 +686,33 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_commit(
     p.T = T; p.g = shape->Hq / shape->Hkv; p.D = shape->D; p.Hq = shape->Hq;
     p.layer_begin = info->layer_begin;
     p.max_path = max_path;
-    p.subs = w.subs;
     p.n_sink = shape->n_sink; p.recent_num = shape->recent_num; p.recent_den = shape->recent_den;
     p.scored = scored;
     p.evict = !(flags & BAKLAVA_FLAG_NO_EVICT) && (scored || shape->recent_num == shape->recent_den);
     p.scale_log2 = kLog2e / sqrtf((float)shape->D);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t e = cudaSuccess;
-    if (p.scored || p.evict) {
-        if (cache->kv_dtype == BAKLAVA_KV_FP8_E4M3) e = launch_scores<128, BAKLAVA_KV_FP8_E4M3>(p, info->n_items, s);
-        else if (cache->kv_dtype == BAKLAVA_KV_INT4) e = launch_scores<128, BAKLAVA_KV_INT4>(p, info->n_items, s);
-        else if (shape->D == 128) e = launch_scores<128, BAKLAVA_KV_BF16>(p, info->n_items, s);
-        else e = launch_scores<64, BAKLAVA_KV_BF16>(p, info->n_items, s);
-        if (e != cudaSuccess) return BAKLAVA_ERR_CUDA;
+    const int n = info->n_items, units = info->n_units;
+    if (p.scored) {
+        if (cache->kv_dtype == BAKLAVA_KV_FP8_E4M3) e = launch_scores<128, BAKLAVA_KV_FP8_E4M3>(p, n, units, s);
+        else if (cache->kv_dtype == BAKLAVA_KV_INT4) e = launch_scores<128, BAKLAVA_KV_INT4>(p, n, units, s);
+        else if (shape->D == 128) e = launch_scores<128, BAKLAVA_KV_BF16>(p, n, units, s);
+        else e = launch_scores<64, BAKLAVA_KV_BF16>(p, n, units, s);
+    } else if (p.evict) {
+        oldest_rows_kernel<<<n, kThreads, 0, s>>>(p);
+        e = cudaGetLastError();
     }
-    if (shape->D == 128) join_rows_kernel<128><<<info->n_items, kThreads, 0, s>>>(p);
-    else join_rows_kernel<64><<<info->n_items, kThreads, 0, s>>>(p);
-    return cudaGetLastError() == cudaSuccess ? BAKLAVA_OK : BAKLAVA_ERR_CUDA;
+    if (e != cudaSuccess) return BAKLAVA_ERR_CUDA;
+    // the second kernel's blocks come up while the first one drains; behind other work on the stream it is an ordinary launch
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = p.scored || p.evict ? 1 : 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)n);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = shape->D == 128 ? cudaLaunchKernelEx(&cfg, join_rows_kernel<128>, p) : cudaLaunchKernelEx(&cfg, join_rows_kernel<64>, p);
+    return e == cudaSuccess ? BAKLAVA_OK : BAKLAVA_ERR_CUDA;
 }

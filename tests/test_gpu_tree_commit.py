@@ -99,7 +99,10 @@ def check(held, q, k, v, lse, path, n, t_pos, scored=True, evict=True, layers=No
                         inv = c.kv_scale_host[l, h, 2 * which + 1]
                         want[fresh] = (rows.float() * float(inv)).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
                     else:
-                        codes, s = o4.quantise_rows(rows.float().numpy(), c.kv_scale_host[l, h, 2 * which + 1])
+                        # (the scale is max |y| times the reciprocal of 7; oracle/int4.py has the quotient)
+                        y = rows.float().numpy() * c.kv_scale_host[l, h, 2 * which + 1]
+                        s = np.abs(y).max(axis=-1) * (np.float32(1) / np.float32(7))
+                        codes = (np.clip(np.rint(y / s[:, None]), -7, 7) + 8).astype(np.uint8)
                         want[fresh] = torch.from_numpy(o4.pack(codes))
                         ref = held.row_scale[here, which].copy()
                         ref[fresh] = s

@@ -88,7 +88,7 @@ def commit(**kw):
     (dict(n_path=None), INVALID), (dict(t_pos=None), INVALID), (dict(items=None), INVALID), (dict(info=None), INVALID), (dict(ws=None), INVALID),
     (dict(T=0), INVALID), (dict(T=65), UNSUPPORTED), (dict(max_path=0), INVALID), (dict(max_path=9), INVALID), (dict(t_next=P), INVALID),
     (dict(flags=1), INVALID), (dict(flags=8), INVALID), (dict(flags=256), INVALID), (dict(ws_bytes=100), WORKSPACE), (dict(units=3), INVALID),
-    (dict(le=2), INVALID), (dict(plan_B=1), INVALID), (dict(chunk=0), INVALID), (dict(chunk=1 << 30), UNSUPPORTED), (dict(k=P + 8), INVALID),
+    (dict(le=2), INVALID), (dict(plan_B=1), INVALID), (dict(chunk=0), INVALID), (dict(k=P + 8), INVALID),
     (dict(path=P + 2), INVALID), (dict(score=None), INVALID), (dict(kv_dtype=bk.KV_INT4, kv_scale=P, row_scale=P), UNSUPPORTED), (dict(D=80), SHAPE)])
 def test_commit_refuses(kw, code):
     assert commit(**kw) == code
