@@ -215,41 +215,50 @@ __global__ void __launch_bounds__(kThreads) oldest_rows_kernel(const __grid_cons
     write_list(p, lists, job.leave, warp, lane);
 }
 
-// The joining rows' own scores: one warp per row, its node and those behind it on the path.
+// The joining rows' own scores: a block per unit, a warp per pair of path nodes (j, i >= j), the pairs' sums over the group added
+// up in the path's order.
 template <int D>
-__device__ __forceinline__ void fresh_scores(const CommitParams& p, int unit, int warp, int lane) {
+__global__ void __launch_bounds__(kThreads) fresh_scores_kernel(const __grid_constant__ CommitParams p) {
     constexpr int kE = D / 32;
+    extern __shared__ float pair[];                           // [max_path][max_path]
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, unit = blockIdx.x;
+    launch_dependents();
     const Unit u(p.c, p.layer_begin, unit);
     const Head hd(p.c, u);
     const Job job(p, u, hd);
     if (job.idle || job.bad) return;
     const int32_t* const path = p.path + (int64_t)u.b * p.T;
     const int64_t head0 = (int64_t)u.li * p.c.B + u.b;
-    for (int j = warp; j < job.a; j += kWarps) {
+    for (int n = warp; n < job.a * job.a; n += kWarps) {
+        const int j = n / job.a, i = n - j * job.a;
+        if (i < j) continue;
         const __nv_bfloat16* const kj = p.k + ((head0 * p.c.Hkv + u.h) * p.T + path[j]) * D + kE * lane;
-        float x[kE], total = 0.0f;
+        const int64_t row0 = (head0 * p.Hq + u.h * p.g) * p.T + path[i];
+        float x[kE], s[BAKLAVA_MAX_GROUP], total = 0.0f;
 #pragma unroll
         for (int e = 0; e < kE; ++e) x[e] = __bfloat162float(kj[e]);
-        for (int i = j; i < job.a; ++i) {
-            const int64_t row0 = (head0 * p.Hq + u.h * p.g) * p.T + path[i];
-            float s[BAKLAVA_MAX_GROUP];
 #pragma unroll
-            for (int a = 0; a < BAKLAVA_MAX_GROUP; ++a) {
-                s[a] = 0.0f;
-                if (a >= p.g) continue;
-                const __nv_bfloat16* const qi = p.q + (row0 + (int64_t)a * p.T) * D + kE * lane;
+        for (int a = 0; a < BAKLAVA_MAX_GROUP; ++a) {
+            s[a] = 0.0f;
+            if (a >= p.g) continue;
+            const __nv_bfloat16* const qi = p.q + (row0 + (int64_t)a * p.T) * D + kE * lane;
 #pragma unroll
-                for (int e = 0; e < kE; ++e) s[a] = fmaf(__bfloat162float(qi[e]), x[e], s[a]);
-            }
-#pragma unroll
-            for (int a = 0; a < BAKLAVA_MAX_GROUP; ++a) {
-                if (a >= p.g) continue;
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) s[a] += __shfl_xor_sync(0xffffffffu, s[a], o);
-                total += exp2f(fmaf(s[a], p.scale_log2, -p.lse[row0 + (int64_t)a * p.T] * kLog2e));
-            }
+            for (int e = 0; e < kE; ++e) s[a] = fmaf(__bfloat162float(qi[e]), x[e], s[a]);
         }
-        if (lane == 0) p.fresh[(int64_t)unit * p.max_path + j] = total;
+#pragma unroll
+        for (int a = 0; a < BAKLAVA_MAX_GROUP; ++a) {
+            if (a >= p.g) continue;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) s[a] += __shfl_xor_sync(0xffffffffu, s[a], o);
+            total += exp2f(fmaf(s[a], p.scale_log2, -p.lse[row0 + (int64_t)a * p.T] * kLog2e));
+        }
+        if (lane == 0) pair[j * p.max_path + i] = total;
+    }
+    __syncthreads();
+    for (int j = threadIdx.x; j < job.a; j += kThreads) {
+        float total = 0.0f;
+        for (int i = j; i < job.a; ++i) total += pair[j * p.max_path + i];
+        p.fresh[(int64_t)unit * p.max_path + j] = total;
     }
 }
 
@@ -280,24 +289,23 @@ struct Rows {
 };
 
 // One block per item (a chunk of a head), its warps on their own: sixteen rows at a time against all of the path's queries, the
-// next sixteen asked for meanwhile.  Behind the items a block per unit for the joining rows' own scores.
+// next sixteen asked for meanwhile.
 template <int D, int KV>
-__global__ void __launch_bounds__(kThreads, 2) path_scores_kernel(const __grid_constant__ CommitParams p, const int n_items) {
+__global__ void __launch_bounds__(kThreads, KV == BAKLAVA_KV_INT4 ? 3 : 2) path_scores_kernel(const __grid_constant__ CommitParams p) {
     using F = Format<D, KV>;
     constexpr int kColumnBytes = 2 * D + kColumnPad;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ LeaveList lists[kWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     launch_dependents();
-    if ((int)blockIdx.x >= n_items) {
-        fresh_scores<D>(p, (int)blockIdx.x - n_items, warp, lane);
-        return;
-    }
     const int4 item = p.items[blockIdx.x];
     const Unit u(p.c, p.layer_begin, item.x);
     const Head hd(p.c, u);
     const Job job(p, u, hd);
-    if (job.idle || job.bad) return;                          // (the second kernel reports what is bad)
+    if (job.idle || job.bad) {                                // (the second kernel reports what is bad)
+        grid_dependency_wait();
+        return;
+    }
     const int lo = item.y, hi = min(item.y + item.z, hd.slots);
     const uint8_t* const slab = static_cast<const uint8_t*>(p.c.k) + hd.first * F::kRowBytes;
     start_list(lists[warp], lane);
@@ -311,10 +319,12 @@ __global__ void __launch_bounds__(kThreads, 2) path_scores_kernel(const __grid_c
         int j0 = lo + warp * 16;
         if (j0 < hi) rows.fetch(p, hd, slab, j0, hi, lane);
         if (col0 > 0) __syncthreads();
-        for (int n = warp; n < blocks * 8; n += kWarps) {     // the queries, column = node column / g, head column % g
-            constexpr int kE = D / 32;
-            float x[kE];                                      // dimensions lane + 32 e
-            float lse2 = INFINITY, factor = 0.0f;             // a column that is none adds exp2(-inf)
+        // the queries, column = node column / g, head column % g: eight lanes to a column
+        for (int n = threadIdx.x >> 3; n < blocks * 8; n += kThreads / 8) {
+            constexpr int kParts = D / 64;                    // pieces of eight dimensions to a lane
+            const int part = lane & 7;
+            float lse2 = INFINITY, factor = 0.0f, big = 0.0f; // a column that is none adds exp2(-inf)
+            float x[kParts][8];
             int64_t row = 0;
             if (n < columns) {
                 row = (((int64_t)u.li * p.c.B + u.b) * p.Hq + u.h * p.g + (col0 + n) % p.g) * p.T + path[(col0 + n) / p.g];
@@ -322,42 +332,67 @@ __global__ void __launch_bounds__(kThreads, 2) path_scores_kernel(const __grid_c
                 factor = p.scale_log2;
             }
 #pragma unroll
-            for (int e = 0; e < kE; ++e) {
-                x[e] = n < columns ? __bfloat162float(p.q[row * D + lane + 32 * e]) : 0.0f;
-                if (KV == BAKLAVA_KV_INT4) x[e] *= p.c.kv_scale[(int64_t)u.head * 4 * D + lane + 32 * e];
+            for (int k = 0; k < kParts; ++k) {
+                const int d0 = 8 * (part + 8 * k);
+                const uint4 raw = n < columns ? *reinterpret_cast<const uint4*>(p.q + row * D + d0) : make_uint4(0, 0, 0, 0);
+                const uint32_t word[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&word[i]));
+                    x[k][2 * i] = f.x; x[k][2 * i + 1] = f.y;
+                }
+                if (KV == BAKLAVA_KV_INT4) {
+                    const float4* const chan = reinterpret_cast<const float4*>(p.c.kv_scale + (int64_t)u.head * 4 * D + d0);
+                    const float4 c0 = chan[0], c1 = chan[1];
+                    x[k][0] *= c0.x; x[k][1] *= c0.y; x[k][2] *= c0.z; x[k][3] *= c0.w;
+                    x[k][4] *= c1.x; x[k][5] *= c1.y; x[k][6] *= c1.z; x[k][7] *= c1.w;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(x[k][i]));
             }
             if (KV != BAKLAVA_KV_BF16) {
-                float big = 0.0f;
 #pragma unroll
-                for (int e = 0; e < kE; ++e) big = fmaxf(big, fabsf(x[e]));
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+                for (int o = 4; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
                 int power;
                 frexpf(big, &power);                          // big = f 2^power, f in 0.5 .. 1
-                power = big > 0.0f && big < INFINITY ? power - 15 : 0;
+                power = big > 0.0f && big < INFINITY ? max(power - 15, -100) : 0;
+                const float back = ldexpf(1.0f, -power);
 #pragma unroll
-                for (int e = 0; e < kE; ++e) x[e] = ldexpf(x[e], -power);
+                for (int k = 0; k < kParts; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[k][i] *= back;
                 factor = ldexpf(factor, power);
                 if (KV == BAKLAVA_KV_FP8_E4M3) factor *= p.c.kv_scale[(int64_t)u.head * 4];
             }
-            // dimension d goes to pair t, lane c, element i of the column: the inverse of Format::dim
+            // eight dimensions from d0 on go to pair t, lane c of the column (the inverse of Format::dim); 4 bits: nibbles i and
+            // i + 4 side by side
 #pragma unroll
-            for (int e = 0; e < kE; ++e) {
-                const int d = lane + 32 * e;
-                int t, c, i;
-                if (KV == BAKLAVA_KV_BF16) { t = d >> 5; c = (d >> 3) & 3; i = d & 7; }
-                else if (KV == BAKLAVA_KV_FP8_E4M3) { t = (d >> 6) * 2 + ((d >> 3) & 1); c = (d >> 4) & 3; i = d & 7; }
-                else { t = (d >> 3) & 3; c = d >> 5; i = (d & 3) * 2 + ((d >> 2) & 1); }
-                uint8_t* const at = smem + (size_t)n * F::kTerms * kColumnBytes + t * 64 + c * 16 + i * 2;
-                if (KV == BAKLAVA_KV_BF16) {
-                    *reinterpret_cast<__nv_bfloat16*>(at) = __float2bfloat16(x[e]);
-                } else {
-                    const __half high = __float2half_rn(x[e]);
-                    *reinterpret_cast<__half*>(at) = high;
-                    if (F::kTerms == 2) *reinterpret_cast<__half*>(at + kColumnBytes) = __float2half_rn(x[e] - __half2float(high));
+            for (int k = 0; k < kParts; ++k) {
+                const int d0 = 8 * (part + 8 * k);
+                int t, c;
+                if (KV == BAKLAVA_KV_BF16) { t = d0 >> 5; c = (d0 >> 3) & 3; }
+                else if (KV == BAKLAVA_KV_FP8_E4M3) { t = (d0 >> 6) * 2 + ((d0 >> 3) & 1); c = (d0 >> 4) & 3; }
+                else { t = (d0 >> 3) & 3; c = d0 >> 5; }
+                uint8_t* const at = smem + (size_t)n * F::kTerms * kColumnBytes + t * 64 + c * 16;
+                uint32_t high[4], low[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float lo_x = KV == BAKLAVA_KV_INT4 ? x[k][i] : x[k][2 * i], hi_x = KV == BAKLAVA_KV_INT4 ? x[k][i + 4] : x[k][2 * i + 1];
+                    if (KV == BAKLAVA_KV_BF16) {
+                        const __nv_bfloat162 v = __floats2bfloat162_rn(lo_x, hi_x);
+                        high[i] = *reinterpret_cast<const uint32_t*>(&v);
+                    } else {
+                        const __half2 v = __floats2half2_rn(lo_x, hi_x);
+                        high[i] = *reinterpret_cast<const uint32_t*>(&v);
+                        const float2 f = __half22float2(v);
+                        const __half2 rest = __floats2half2_rn(lo_x - f.x, hi_x - f.y);
+                        low[i] = *reinterpret_cast<const uint32_t*>(&rest);
+                    }
                 }
+                *reinterpret_cast<uint4*>(at) = make_uint4(high[0], high[1], high[2], high[3]);
+                if (F::kTerms == 2) *reinterpret_cast<uint4*>(at + kColumnBytes) = make_uint4(low[0], low[1], low[2], low[3]);
             }
-            if (lane == 0) of_column[n] = make_float2(factor, lse2);
+            if (part == 0) of_column[n] = make_float2(factor, lse2);
         }
         __syncthreads();
         const int r = lane >> 2, c = lane & 3;
@@ -408,6 +443,7 @@ __global__ void __launch_bounds__(kThreads, 2) path_scores_kernel(const __grid_c
         }
     }
     if (job.leave > 0) write_list(p, lists, job.leave, warp, lane);
+    grid_dependency_wait();                                   // (so that this grid does not complete before the one in front of it)
 }
 
 // A head's lists joined, the rows that leave, the rows that join.  Blocks of items that are not a head's first have
@@ -617,6 +653,21 @@ CommitWorkspace layout(const baklava_plan_info* info, int32_t max_path) {
     return w;
 }
 
+// With programmatic stream serialisation where something of this call is in front: the kernel's blocks come up while that drains.
+template <typename... Args>
+cudaError_t launch(void (*kernel)(Args...), unsigned blocks, int smem, bool behind, cudaStream_t s, const Args&... args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = behind ? 1 : 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 template <int D, int KV>
 cudaError_t launch_scores(const CommitParams& p, int n_items, int n_units, cudaStream_t s) {
     using F = Format<D, KV>;
@@ -631,8 +682,9 @@ cudaError_t launch_scores(const CommitParams& p, int n_items, int n_units, cudaS
         if (e != cudaSuccess) return e;
         if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
     }
-    path_scores_kernel<D, KV><<<(unsigned)n_items + (unsigned)n_units, kThreads, smem, s>>>(p, n_items);
-    return cudaGetLastError();
+    e = launch(fresh_scores_kernel<D>, (unsigned)n_units, p.max_path * p.max_path * (int)sizeof(float), false, s, p);
+    if (e != cudaSuccess) return e;
+    return launch(path_scores_kernel<D, KV>, (unsigned)n_items, smem, true, s, p);
 }
 
 }  // namespace
@@ -699,20 +751,10 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_commit(
         else if (shape->D == 128) e = launch_scores<128, BAKLAVA_KV_BF16>(p, n, units, s);
         else e = launch_scores<64, BAKLAVA_KV_BF16>(p, n, units, s);
     } else if (p.evict) {
-        oldest_rows_kernel<<<n, kThreads, 0, s>>>(p);
-        e = cudaGetLastError();
+        e = launch(oldest_rows_kernel, (unsigned)n, 0, false, s, p);
     }
     if (e != cudaSuccess) return BAKLAVA_ERR_CUDA;
-    // the second kernel's blocks come up while the first one drains; behind other work on the stream it is an ordinary launch
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = p.scored || p.evict ? 1 : 0;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)n);
-    cfg.blockDim = dim3(kThreads);
-    cfg.stream = s;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    e = shape->D == 128 ? cudaLaunchKernelEx(&cfg, join_rows_kernel<128>, p) : cudaLaunchKernelEx(&cfg, join_rows_kernel<64>, p);
+    const bool behind = p.scored || p.evict;
+    e = shape->D == 128 ? launch(join_rows_kernel<128>, (unsigned)n, 0, behind, s, p) : launch(join_rows_kernel<64>, (unsigned)n, 0, behind, s, p);
     return e == cudaSuccess ? BAKLAVA_OK : BAKLAVA_ERR_CUDA;
 }
