@@ -107,7 +107,7 @@ struct Layout {
     static constexpr int kQBytes = R == 2 ? R * kRows * D * 2 : 0;
     static constexpr int kQBox = R * kRows * 128;
     static constexpr int kScaleBytes = KV == BAKLAVA_KV_INT4 ? kKeys * 8 : 0;
-    static constexpr int kSlots = kQuantised ? (R == 2 ? 3 : 4) : D == 128 ? (R == 2 ? 5 : 7) : R == 2 ? 12 : 13;
+    static constexpr int kSlots = kQuantised ? (R == 2 ? 3 : 4) : D == 128 ? (R == 2 ? 4 : 6) : R == 2 ? 10 : 12;
     static constexpr int kRawSlots = !kQuantised ? 0 : KV == BAKLAVA_KV_INT4 ? 10 : R == 2 ? 4 : 6;
     static constexpr int kRing = kQBytes, kScales = kRing + kSlots * kTileBytes, kRaw = kScales + kSlots * kScaleBytes;
     static constexpr int kShared = kRaw + kRawSlots * kRawBytes;
@@ -870,6 +870,7 @@ __global__ void __launch_bounds__(Layout<D, R, KV>::kThreads, 1) tree_tile_kerne
     Cta cta;
     cta.base = ptx::smem_u32(smem_raw);
     cta.ptr = smem_raw;
+    launch_dependents();
     if (tid == 0) {
         each_barrier<L>(sm, [](uint64_t& bar, int count) { ptx::mbar_init(ptx::smem_u32(&bar), count); });
         ptx::mbar_init(ptx::smem_u32(&sm.bar_answer), 1);
@@ -969,12 +970,14 @@ __device__ __forceinline__ float join_weight(float x, float ref, float top) {
     const float half = exp2f(0.5f * (ref - top));
     return x * half * half;
 }
-// One warp per node and query head: the logits of its ancestors, the normaliser of everything, then the sum of the
-// ancestors' values and the partials under their final weights (which add up to one, so that averages of values near the
-// end of the range do not overflow on the way).  Blocks of items that are not a head's first have nothing to do.
-constexpr int kJoinWarps = 8;
+// One warp per node and query head.  First the node's ancestors, whose keys and values it reads itself: a partial like the
+// chunks'.  This part waits for nothing of the first kernel and runs beside it (blocks of 128 threads, small enough for the
+// registers that a tile kernel's block leaves).  Then the normaliser of everything, and the partials under their final weights,
+// which add up to one, so that averages of values near the end of the range do not overflow on the way.  Blocks of items that are
+// not a head's first have nothing to do.
+constexpr int kJoinWarps = 4;
 template <int D>
-__global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const __grid_constant__ TreeParams p) {
+__global__ void __launch_bounds__(kJoinWarps * 32, 5) tree_join_kernel(const __grid_constant__ TreeParams p) {
     constexpr int kE = D / 32;
     const int4 item = p.items[blockIdx.x];
     const int pieces = item.w >> 16;
@@ -983,47 +986,64 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const __grid
     if (row >= p.g * p.T) return;
     const Unit u(p.c, p.layer, item.x);
     const int a = row / p.T, i = row - a * p.T, y = u.h * p.g + a;
+    const int32_t* const parent = p.parent + (int64_t)u.b * p.T;
+    const int up0 = lane < p.T ? parent[lane] : -1, up1 = lane + 32 < p.T ? parent[lane + 32] : -1;
+    float q[kE], o[kE];
+    load_bf16<kE>(p.q + u.b * p.sq.seq + (int64_t)y * p.sq.head + i * p.sq.token, lane, q);
     const int n = nodes_of(p.n_nodes, u.b, p.T);
     if (i >= n) return;
-    const int32_t* const parent = p.parent + (int64_t)u.b * p.T;
-    const int up0 = lane < n ? parent[lane] : -1, up1 = lane + 32 < n ? parent[lane + 32] : -1;
-    if (!__all_sync(0xffffffffu, up0 >= -1 && up1 >= -1 && (up0 < lane) && (up1 < lane + 32))) {
+    if (!__all_sync(0xffffffffu, (lane >= n || (up0 >= -1 && up0 < lane)) && (lane + 32 >= n || (up1 >= -1 && up1 < lane + 32)))) {
         if (lane == 0) atomicOr(p.c.status, BAKLAVA_STATUS_BAD_STATE);
         return;
     }
-    // lane d holds the d-th node of the way up and the one 32 further
-    int way0 = 0, way1 = 0, depth = 0;
-    for (int j = i; j >= 0; ++depth) {
-        if (lane == (depth & 31)) (depth < 32 ? way0 : way1) = j;
-        j = __shfl_sync(0xffffffffu, j < 32 ? up0 : up1, j & 31);
-    }
-    float q[kE], o[kE];
-    load_bf16<kE>(p.q + u.b * p.sq.seq + (int64_t)y * p.sq.head + i * p.sq.token, lane, q);
     const __nv_bfloat16* const keys = p.k + u.b * p.sk.seq + (int64_t)u.h * p.sk.head;
     const __nv_bfloat16* const vals = p.v + u.b * p.sv.seq + (int64_t)u.h * p.sv.head;
-    float s0 = -INFINITY, s1 = -INFINITY;                     // the logits, log2 domain
-    for (int d = 0; d < depth; d += 4) {
-        float x[4][kE];
+    // the way up, four nodes at a time: reference six powers of two above the largest logit (64 values of any size stay in range)
+    float ref = -INFINITY, l = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int j = __shfl_sync(0xffffffffu, d + k < 32 ? way0 : way1, (d + k) & 31);
-            load_bf16<kE>(keys + (d + k < depth ? j : i) * p.sk.token, lane, x[k]);
+    for (int e = 0; e < kE; ++e) o[e] = 0.0f;
+    for (int j = i; j >= 0;) {
+        float k[4][kE], v[4][kE], s[4];
+        bool there[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            there[c] = j >= 0;
+            const int at = there[c] ? j : i;                  // (behind the root: the node itself, not counted)
+            load_bf16<kE>(keys + at * p.sk.token, lane, k[c]);
+            load_bf16<kE>(vals + at * p.sv.token, lane, v[c]);
+            const int up = __shfl_sync(0xffffffffu, at < 32 ? up0 : up1, at & 31);
+            j = there[c] ? up : -1;
         }
+        float top = ref;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float s = 0.0f;
+        for (int c = 0; c < 4; ++c) {
+            s[c] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < kE; ++e) s = fmaf(q[e], x[k][e], s);
-            s = warp_sum(s) * p.scale_log2;
-            if (d + k < depth && lane == ((d + k) & 31)) (d + k < 32 ? s0 : s1) = s;
+            for (int e = 0; e < kE; ++e) s[c] = fmaf(q[e], k[c][e], s[c]);
+            s[c] = warp_sum(s[c]) * p.scale_log2;
+            if (there[c]) top = fmaxf(top, s[c] + 6.0f);
         }
+        const float was = ref == -INFINITY ? 0.0f : exp2f(ref - top);
+        l *= was;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) o[e] *= was;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (!there[c]) continue;
+            const float w = s[c] == -INFINITY ? 0.0f : exp2f(s[c] - top);
+            l += w;
+#pragma unroll
+            for (int e = 0; e < kE; ++e) o[e] = fmaf(w, v[c][e], o[e]);
+        }
+        ref = top;
     }
     grid_dependency_wait();
     const int64_t rows = (int64_t)p.g * p.T, first = (int64_t)blockIdx.x * rows + row;
     bool skipped = false;
-    float top = fmaxf(s0, s1), sum = 0.0f;
+    float top = l > 0.0f ? ref + log2f(l) : l == 0.0f ? -INFINITY : l, sum = 0.0f;
+    const float2 mine = lane < pieces ? p.stats[first + lane * rows] : make_float2(-INFINITY, 0.0f);
     for (int c = lane; c < pieces; c += 32) {
-        const float2 st = p.stats[first + c * rows];
+        const float2 st = c < 32 ? mine : p.stats[first + c * rows];
         skipped = skipped || st.y < 0.0f;
         if (st.x != -INFINITY) top = fmaxf(top, st.x + log2f(st.y));
     }
@@ -1031,40 +1051,25 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const __grid
 #pragma unroll
     for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
     for (int c = lane; c < pieces; c += 32) {
-        const float2 st = p.stats[first + c * rows];
+        const float2 st = c < 32 ? mine : p.stats[first + c * rows];
         if (st.x != -INFINITY) sum += join_weight(st.y, st.x, top);
     }
-    if (lane < depth && s0 != -INFINITY) sum += exp2f(s0 - top);
-    if (lane + 32 < depth && s1 != -INFINITY) sum += exp2f(s1 - top);
-    sum = warp_sum(sum);
+    sum = warp_sum(sum) + (l == 0.0f ? 0.0f : join_weight(l, ref, top));
     const float inv = 1.0f / sum;
-    s0 = s0 == -INFINITY ? 0.0f : exp2f(s0 - top) * inv;      // weights from here on
-    s1 = s1 == -INFINITY ? 0.0f : exp2f(s1 - top) * inv;
 #pragma unroll
-    for (int e = 0; e < kE; ++e) o[e] = 0.0f;
-    for (int d = 0; d < depth; d += 4) {
-        float x[4][kE];
+    for (int e = 0; e < kE; ++e) o[e] = l == 0.0f ? 0.0f : join_weight(o[e], ref, top) * inv;
+    for (int c0 = 0; c0 < pieces; c0 += 8) {
+        float x[8][kE], of[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int j = __shfl_sync(0xffffffffu, d + k < 32 ? way0 : way1, (d + k) & 31);
-            load_bf16<kE>(vals + (d + k < depth ? j : i) * p.sv.token, lane, x[k]);
-        }
+        for (int k = 0; k < 8; ++k) {
+            const int c = c0 + k;
+            of[k] = __shfl_sync(0xffffffffu, mine.x, c & 31);
+            if (c >= 32 && c < pieces) of[k] = p.stats[first + c * rows].x;
+            if (c >= pieces) of[k] = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float w = __shfl_sync(0xffffffffu, d + k < 32 ? s0 : s1, (d + k) & 31);
-            if (d + k < depth)
-#pragma unroll
-                for (int e = 0; e < kE; ++e) o[e] = fmaf(w, x[k][e], o[e]);
-        }
-    }
-    for (int c0 = 0; c0 < pieces; c0 += 4) {
-        float2 st[4];
-        float x[4][kE];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int64_t at = first + min(c0 + k, pieces - 1) * rows;
-            st[k] = p.stats[at];
-            const float* const part = p.partial + at * D + kE * lane;
+            for (int e = 0; e < kE; ++e) x[k][e] = 0.0f;
+            if (of[k] == -INFINITY) continue;                 // (no rows: its partial was not written)
+            const float* const part = p.partial + (first + c * rows) * D + kE * lane;
             if (kE == 4) {
                 const float4 w = *reinterpret_cast<const float4*>(part);
                 x[k][0] = w.x; x[k][1] = w.y; x[k][kE - 2] = w.z; x[k][kE - 1] = w.w;
@@ -1074,10 +1079,10 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const __grid
             }
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (c0 + k >= pieces || st[k].x == -INFINITY) continue;       // (no rows: its partial was not written)
+        for (int k = 0; k < 8; ++k) {
+            if (of[k] == -INFINITY) continue;
 #pragma unroll
-            for (int e = 0; e < kE; ++e) o[e] += join_weight(x[k][e], st[k].x, top) * inv;
+            for (int e = 0; e < kE; ++e) o[e] += join_weight(x[k][e], of[k], top) * inv;
         }
     }
     __nv_bfloat16* const out = p.out + u.b * p.so.seq + (int64_t)y * p.so.head + i * p.so.token + kE * lane;
@@ -1186,9 +1191,16 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_attn(
     else e = two ? launch_tiles<64, 2, BAKLAVA_KV_BF16>(p, n, qm, km, vm, s) : launch_tiles<64, 1, BAKLAVA_KV_BF16>(p, n, qm, km, vm, s);
     const dim3 join((unsigned)n, (unsigned)((p.g * T + kJoinWarps - 1) / kJoinWarps));
     if (e == cudaSuccess) {
-        if (shape->D == 128) tree_join_kernel<128><<<join, kJoinWarps * 32, 0, s>>>(p);
-        else tree_join_kernel<64><<<join, kJoinWarps * 32, 0, s>>>(p);
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = join;
+        cfg.blockDim = dim3(kJoinWarps * 32);
+        cfg.stream = s;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        e = shape->D == 128 ? cudaLaunchKernelEx(&cfg, tree_join_kernel<128>, p) : cudaLaunchKernelEx(&cfg, tree_join_kernel<64>, p);
     }
-    if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? BAKLAVA_OK : BAKLAVA_ERR_CUDA;
 }
