@@ -59,14 +59,18 @@ __device__ __forceinline__ float warp_sum(float x) {
 // ---------------------------------------------------------------- slab rows on the tensor cores
 constexpr int kKeys = 128;                    // slab rows to a tile
 constexpr int kRows = 128;                    // query rows to an accumulator
-constexpr int kSoftmaxWarps = 8;              // two streams of four
+// warps: two streams of four softmax warps, four that write the rows and lay out the queries (each group in the order of the
+// tensor memory's quarters), the producer, the tensor core's, the one that looks for further items, converters
+constexpr int kSoftmaxWarps = 8;
+constexpr int kRowWarps = 4;
 constexpr int kConvertWarps = 4;
+constexpr int kRowWarp0 = kSoftmaxWarps, kProducerWarp = kRowWarp0 + kRowWarps, kMmaWarp = kProducerWarp + 1, kScoutWarp = kMmaWarp + 1,
+              kConvertWarp0 = kScoutWarp + 1;
 constexpr int kItemRing = 4;
 constexpr int kMaxRedo = 8;
 constexpr int kMaxSlots = 13;
 constexpr uint32_t kTmemColumns = 512;
-constexpr uint32_t kOColumn = 256;            // S of the streams at columns 0 and 128, O at 256 (R = 2: and 384)
-constexpr uint32_t kQColumn = 384;            // R = 1: the queries
+constexpr int kMaxBuffers = 3;
 constexpr float kFinite = 3.0e38f;
 constexpr float kMaxSum = 0x1p120f;
 constexpr long long kGraceCycles = 2000000;
@@ -85,17 +89,19 @@ struct Item {
 struct Shared {
     uint4 answer;
     uint64_t full[kMaxSlots], empty[kMaxSlots], raw_full[kMaxSlots], raw_empty[kMaxSlots];
-    uint64_t s_full[2], p_ready[2], o_full[2], q_full, q_free, ref_ready, both, bar_answer, bar_item[kItemRing];
+    uint64_t s_full[kMaxBuffers], p_ready[kMaxBuffers], o_full[2], q_full[2], sums[2], q_free, o_free, ref_ready, both, bar_answer, bar_item[kItemRing];
     Item item[kItemRing], redo[kMaxRedo];
     int redo_count, redo_mark[kItemRing];
     uint32_t tmem_slot;
     int abort;
-    float ref[kRows], part[2][kRows];         // R = 1: the rows' references, the streams' sums (or maxima)
+    int finished;                             // items that are done with, counted by each row warp
+    // of two items in turn: the rows' references (R = 1: only [.][0]), the streams' sums, 4 bits: the queries' factors
+    float ref[2][2][kRows], part[2][2][kRows], factor[2][2][kRows];
 };
-constexpr int kSharedBytes = 3072;
+constexpr int kSharedBytes = 7680;
 static_assert(sizeof(Shared) <= kSharedBytes, "the tiles take the rest");
 
-// How an instance lies in shared memory: the query rows (R = 2), the ring of operand tiles, for quantised slabs the ring of
+// How an instance lies in shared memory: the query rows, the ring of operand tiles, for quantised slabs the ring of
 // tiles as they are in the slab and the rows' scales (4 bits: beside each operand tile), then Shared.
 template <int D, int R, int KV>
 struct Layout {
@@ -104,20 +110,24 @@ struct Layout {
     static constexpr int kBoxBytes = kKeys * 128;                      // 64 elements of a tile's rows
     static constexpr int kRowBytes = KV == BAKLAVA_KV_BF16 ? 2 * D : KV == BAKLAVA_KV_FP8_E4M3 ? D : D / 2;   // of the slab
     static constexpr int kRawBytes = kKeys * kRowBytes;
-    static constexpr int kQBytes = R == 2 ? R * kRows * D * 2 : 0;
+    static constexpr int kTerms = KV == BAKLAVA_KV_INT4 ? 2 : 1;       // 16-bit terms of a query element
+    static constexpr int kQTerm = R * kRows * D * 2, kQBytes = kTerms * kQTerm;
     static constexpr int kQBox = R * kRows * 128;
     static constexpr int kScaleBytes = KV == BAKLAVA_KV_INT4 ? kKeys * 8 : 0;
-    static constexpr int kSlots = kQuantised ? (R == 2 ? 3 : 4) : D == 128 ? (R == 2 ? 4 : 6) : R == 2 ? 10 : 12;
-    static constexpr int kRawSlots = !kQuantised ? 0 : KV == BAKLAVA_KV_INT4 ? 10 : R == 2 ? 4 : 6;
+    static constexpr int kSlots = kQuantised ? (R == 2 || KV == BAKLAVA_KV_INT4 ? 3 : 4) : D == 128 ? (R == 2 ? 4 : 5) : R == 2 ? 10 : 12;
+    static constexpr int kRawSlots = !kQuantised ? 0 : KV == BAKLAVA_KV_INT4 ? 6 : 3;
     static constexpr int kRing = kQBytes, kScales = kRing + kSlots * kTileBytes, kRaw = kScales + kSlots * kScaleBytes;
     static constexpr int kShared = kRaw + kRawSlots * kRawBytes;
     static constexpr int kTotal = kShared + kSharedBytes;
-    static constexpr int kThreads = (2 + kSoftmaxWarps + (kQuantised ? kConvertWarps : 0)) * 32;
-    static constexpr bool kLoadsQ = R == 2 && !kQuantised;             // the queries come by TMA
-    static constexpr int kTerms = KV == BAKLAVA_KV_INT4 ? 2 : 1;       // 16-bit terms of a query element
+    static constexpr int kThreads = (kConvertWarp0 + (kQuantised ? kConvertWarps : 0)) * 32;
+    static constexpr bool kLoadsQ = !kQuantised;                       // the queries come by TMA
+    // Tensor memory: buffers of 128 logits (the probabilities take their place), O behind them.  One accumulator leaves room for
+    // three buffers: the softmax warps find the next logits formed when they are through with a tile.
+    static constexpr int kBuffers = R == 1 ? 3 : 2;
+    static constexpr uint32_t kOColumn = kBuffers * kKeys;
     static_assert(kTotal <= 232448, "one CTA's shared memory");
-    static_assert(R == 1 || KV != BAKLAVA_KV_INT4, "queries in two terms lie in tensor memory");
-    // fp16 operands: keys of quantised slabs (codes are exact in fp16, and so are queries or their two terms), FP8 values
+    static_assert(R == 1 || KV != BAKLAVA_KV_INT4, "two rows' blocks of queries in two terms leave no room");
+    // fp16 operands: keys of quantised slabs (whose codes are exact in fp16) with their queries, FP8 values
     static constexpr uint32_t kBf16 = (1u << 7) | (1u << 10);
     static constexpr uint32_t kIdescS = tc::idesc_bf16_f32(kRows, kKeys) & ~(kQuantised ? kBf16 : 0u);
     static constexpr uint32_t kIdescPv = tc::idesc_bf16_f32_b_mn(kRows, D) & ~(KV == BAKLAVA_KV_FP8_E4M3 ? kBf16 : 0u);
@@ -181,30 +191,32 @@ struct Cta {
     uint32_t base, tmem;          // shared memory, tensor memory
     uint8_t* ptr;
 };
-// Counters that run on over the items: tiles through the rings, steps of the streams, items that had work.
+// Counters that run on over the items: tiles through the rings, steps, items that had work.
 struct Count {
-    uint32_t entry = 0, step[2] = {0, 0}, work = 0, both = 0;
+    uint32_t entry = 0, step = 0, work = 0;
 };
 enum Mode { kFast, kMaxima, kExact };
 
-// Tiles pass through the rings in the order in which the tensor core takes them.  A step is one S = Q K^T and one O += P V of
-// one stream of four softmax warps; step n belongs to stream n & 1, and S(n + 2) follows P V (n).  With two accumulators of
-// query rows (R = 2) a stream is an accumulator, and both take every tile; with one, the streams take the tiles in turn.
+// A step is one S = Q K^T and one O += P V.  Step n of an item belongs to stream n & 1 (four softmax warps); with two
+// accumulators of query rows (R = 2) a stream is an accumulator, and both take every tile, with one the streams take the tiles in
+// turn.  Steps take the buffers in turn, and S(n + buffers) follows P V (n).  Tiles pass through the rings in the order in which
+// the tensor core takes them: R = 2: K, V of each tile; R = 1: the first three K, then V, K in turn, then the last V.
 template <int R>
 __device__ __forceinline__ int tile_of(int step) { return R == 2 ? step >> 1 : step; }
 template <int R, int kMode>
-__device__ __forceinline__ uint32_t key_entry(int t) { return kMode == kMaxima ? t : R == 2 ? 2 * t : t == 0 ? 0 : 2 * t - 1; }
+__device__ __forceinline__ uint32_t key_entry(int t) { return kMode == kMaxima ? t : R == 2 ? 2 * t : t < 3 ? t : 2 * t - 2; }
 template <int R>
-__device__ __forceinline__ uint32_t value_entry(int t, int tiles) { return R == 2 || t == tiles - 1 ? 2 * t + 1 : 2 * t + 2; }
+__device__ __forceinline__ uint32_t value_entry(int t, int tiles) { return R == 2 ? 2 * t + 1 : min(tiles, t + 3) + t; }
 // the other way round: entry e of an item is the key or value tile t
 template <int R, int kMode>
 __device__ __forceinline__ bool entry_is_value(int e, int tiles, int& t) {
     if (kMode == kMaxima) { t = e; return false; }
     if (R == 2) { t = e >> 1; return e & 1; }
-    if (e == 2 * tiles - 1) { t = tiles - 1; return true; }
-    if (e == 0 || (e & 1)) { t = (e + 1) >> 1; return false; }
-    t = (e - 2) >> 1;
-    return true;
+    if (e < min(3, tiles)) { t = e; return false; }
+    const int k = e - 3;
+    if (k >= 2 * (tiles - 3)) { t = e - tiles; return true; }
+    t = (k >> 1) + (k & 1 ? 3 : 0);
+    return !(k & 1);
 }
 template <int kMode>
 __device__ __forceinline__ int entries_of(const Item& it) { return kMode == kMaxima ? it.tiles : 2 * it.tiles; }
@@ -267,9 +279,9 @@ __device__ __forceinline__ bool load_entry(const TreeParams& p, Shared& sm, cons
     return true;
 }
 template <int D, int R, int KV>
-__device__ __forceinline__ void load_queries(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, const CUtensorMap& q_map) {
+__device__ __forceinline__ void load_queries(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, uint32_t work, const CUtensorMap& q_map) {
     using L = Layout<D, R, KV>;
-    const uint32_t bar = ptx::smem_u32(&sm.q_full);
+    const uint32_t bar = ptx::smem_u32(&sm.q_full[work & 1]);
     ptx::mbar_arrive_expect_tx(bar, (uint32_t)(it.heads * p.rows_per_head * D * 2));
     for (int a = 0; a < it.heads; ++a)
 #pragma unroll
@@ -277,55 +289,47 @@ __device__ __forceinline__ void load_queries(const TreeParams& p, Shared& sm, co
             ptx::tma_load_4d(cta.base + bx * L::kQBox + a * p.rows_per_head * 128, &q_map, bx * 64, 0, it.h * p.g + it.a0 + a, it.b, bar);
 }
 template <int D, int R, int KV>
-__device__ __forceinline__ void produce(const TreeParams& p, Shared& sm, const Cta& cta, Item it, const CUtensorMap& q_map,
-                                        const CUtensorMap& k_map, const CUtensorMap& v_map) {
+__device__ __forceinline__ bool produce_item(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, Count& c, const CUtensorMap& q_map,
+                                             const CUtensorMap& k_map, const CUtensorMap& v_map) {
     using L = Layout<D, R, KV>;
+    if (L::kLoadsQ) {
+        // the queries' place is free once the last S of the item before has been formed
+        if (c.work > 0 && !ptx::mbar_wait(ptx::smem_u32(&sm.q_free), (c.work - 1) & 1)) return false;
+        load_queries<D, R, KV>(p, sm, cta, it, c.work, q_map);
+    }
+    for (int e = 0; e < 2 * it.tiles; ++e)
+        if (!load_entry<D, R, KV, kFast>(p, sm, cta, it, c.entry, e, k_map, v_map)) return false;
+    c.entry += 2 * it.tiles;
+    ++c.work;
+    return true;
+}
+// Looks for the CTA's further items and hands them to all roles; those without work are done with here.  Item j + 1 is asked
+// for when item j - 2 is done with, so that at most three are under way.
+__device__ __forceinline__ void scout(const TreeParams& p, Shared& sm) {
     const uint32_t answer = ptx::smem_u32(&sm.answer), bar_answer = ptx::smem_u32(&sm.bar_answer);
-    constexpr int kAhead = L::kQuantised ? L::kRawSlots : L::kSlots;
-    Count c;
-    bool ok = true, more = true;
     uint32_t asked = 0;
-    for (int k = 0; ok; ++k) {
-        // a block in the list of those to redo may come from the two items before this one, from it and from the next
-        const bool ask = more && *(volatile int*)&sm.redo_count + 4 <= kMaxRedo;
-        if (ask) request_block(answer, bar_answer);
-        const int total = 2 * it.tiles;
-        int e = 0;
-        if (total > 0) {
-            // never more than two items ahead of the tensor core
-            if (c.work > 1) ok = ptx::mbar_wait(ptx::smem_u32(&sm.o_full[c.work & 1]), ((c.work - 2) >> 1) & 1);
-            if (L::kLoadsQ) {
-                // the queries' place is free once the last S of the item before has been formed
-                if (ok && c.work > 0) ok = ptx::mbar_wait(ptx::smem_u32(&sm.q_free), (c.work - 1) & 1);
-                if (ok) load_queries<D, R, KV>(p, sm, cta, it, q_map);
-            }
-            for (; e < min(total, kAhead) && ok; ++e) ok = load_entry<D, R, KV, kFast>(p, sm, cta, it, c.entry, e, k_map, v_map);
-            if (!ok) break;
-        }
-        // the next item, while these are under way (those without work are done with here)
-        Item next = it;
+    bool ok = true;
+    for (int j = 0; ok; ++j) {
+        const long long t0 = clock64();
+        while (ok && *(volatile int*)&sm.finished < kRowWarps * (j - 1)) ok = clock64() - t0 < ptx::kWaitCycles && !*(volatile int*)&sm.abort;
+        if (!ok) break;
+        Item next;
         next.index = -1;
-        for (bool waiting = ask; waiting && ok;) {
+        // a CTA that has much to do again asks for nothing more: items j - 1 to j + 1 may yet be noted
+        while (ok && next.index < 0 && *(volatile int*)&sm.redo_count + 4 <= kMaxRedo) {
             uint32_t x = 0;
+            request_block(answer, bar_answer);
             ok = ptx::mbar_wait(bar_answer, asked++ & 1);
-            waiting = ok && granted_block(answer, x);
-            if (waiting) {
-                next = find_item(p, x);
-                if (next.tiles > 0) waiting = false;
-                else { next.index = -1; request_block(answer, bar_answer); }
-            }
+            if (!ok || !granted_block(answer, x)) break;
+            next = find_item(p, x);
+            if (next.tiles == 0) next.index = -1;
         }
         if (!ok) break;
-        more = next.index >= 0;
-        sm.item[k % kItemRing] = next;
-        tc::mbar_arrive(ptx::smem_u32(&sm.bar_item[k % kItemRing]));
-        for (; e < total && ok; ++e) ok = load_entry<D, R, KV, kFast>(p, sm, cta, it, c.entry, e, k_map, v_map);
-        if (!more) break;
-        c.entry += total;
-        c.work += total > 0;
-        it = next;
+        sm.item[j % kItemRing] = next;
+        tc::mbar_arrive(ptx::smem_u32(&sm.bar_item[j % kItemRing]));
+        if (next.index < 0) return;
     }
-    if (!ok) sm.abort = 1;
+    sm.abort = 1;
 }
 
 // ---------------------------------------------------------------- quantised rows into operand tiles
@@ -337,7 +341,7 @@ template <int D, int R, int KV, int kMode>
 __device__ __forceinline__ bool convert_item(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, Count& c, int warp, int lane) {
     using L = Layout<D, R, KV>;
     constexpr int kLanes = L::kRowBytes / 16, kStep = 32 / kLanes;     // lanes to a row, rows to a warp's step
-    const int w = warp - 2 - kSoftmaxWarps, piece = lane % kLanes;
+    const int w = warp - kConvertWarp0, piece = lane % kLanes;
     const int entries = entries_of<kMode>(it);
     for (int e = 0; e < entries; ++e) {
         int t;
@@ -412,67 +416,64 @@ __device__ __forceinline__ bool convert_item(const TreeParams& p, Shared& sm, co
 
 // ---------------------------------------------------------------- the tensor core's thread
 template <int D, int R, int KV>
-__device__ __forceinline__ void issue_s(const Cta& cta, int stream, uint32_t slot) {
+__device__ __forceinline__ void issue_s(const Cta& cta, int acc, uint32_t buffer, uint32_t slot) {
     using L = Layout<D, R, KV>;
+    const uint64_t dq = tc::desc_k_major_sw128(cta.base + acc * kRows * 128);
     const uint64_t dk = tc::desc_k_major_sw128(cta.base + L::kRing + slot * L::kTileBytes);
-    if (R == 1) {
 #pragma unroll
-        for (int term = 0; term < L::kTerms; ++term)
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks)
-                tc::umma_bf16_ts(cta.tmem + stream * kKeys, cta.tmem + kQColumn + term * (D / 2) + ks * 8,
-                                 dk + (((ks >> 2) * L::kBoxBytes + (ks & 3) * 32) >> 4), L::kIdescS, term + ks > 0);
-    } else {
-        const uint64_t dq = tc::desc_k_major_sw128(cta.base + stream * kRows * 128);
+    for (int term = 0; term < L::kTerms; ++term)
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
-            tc::umma_bf16(cta.tmem + stream * kKeys, dq + (((ks >> 2) * L::kQBox + (ks & 3) * 32) >> 4),
-                          dk + (((ks >> 2) * L::kBoxBytes + (ks & 3) * 32) >> 4), L::kIdescS, ks > 0);
-    }
+            tc::umma_bf16(cta.tmem + buffer * kKeys, dq + ((term * L::kQTerm + (ks >> 2) * L::kQBox + (ks & 3) * 32) >> 4),
+                          dk + (((ks >> 2) * L::kBoxBytes + (ks & 3) * 32) >> 4), L::kIdescS, term + ks > 0);
 }
 template <int D, int R, int KV>
-__device__ __forceinline__ void issue_pv(const Cta& cta, int stream, uint32_t slot, bool accumulate) {
+__device__ __forceinline__ void issue_pv(const Cta& cta, int acc, uint32_t buffer, uint32_t slot, bool accumulate) {
     using L = Layout<D, R, KV>;
     const uint64_t dv = tc::desc_mn_major_sw128(cta.base + L::kRing + slot * L::kTileBytes, L::kBoxBytes);
 #pragma unroll
     for (int ks = 0; ks < kKeys / 16; ++ks)
-        tc::umma_bf16_ts(cta.tmem + kOColumn + (R == 2 ? stream * 128 : 0), cta.tmem + stream * kKeys + ks * 8, dv + (ks * 2048 >> 4),
-                         L::kIdescPv, accumulate || ks > 0);
+        tc::umma_bf16_ts(cta.tmem + L::kOColumn + acc * 128, cta.tmem + buffer * kKeys + ks * 8, dv + (ks * 2048 >> 4), L::kIdescPv,
+                         accumulate || ks > 0);
 }
 template <int D, int R, int KV, int kMode>
 __device__ __forceinline__ bool issue_item(Shared& sm, const Cta& cta, const Item& it, Count& c) {
     using L = Layout<D, R, KV>;
+    constexpr int kB = L::kBuffers;
     const int steps = it.tiles * R;
     auto full = [&](uint32_t n) { return ptx::mbar_wait(ptx::smem_u32(&sm.full[n % L::kSlots]), n / L::kSlots & 1); };
     auto form_s = [&](int n) {
-        const uint32_t entry = c.entry + key_entry<R, kMode>(tile_of<R>(n)), slot = entry % L::kSlots;
+        const uint32_t entry = c.entry + key_entry<R, kMode>(tile_of<R>(n)), slot = entry % L::kSlots, buffer = (c.step + n) % kB;
         if (!full(entry)) return false;
         tc::fence_after_sync();
-        issue_s<D, R, KV>(cta, n & 1, slot);
-        tc::umma_commit(ptx::smem_u32(&sm.s_full[n & 1]));
+        issue_s<D, R, KV>(cta, R == 2 ? n & 1 : 0, buffer, slot);
+        tc::umma_commit(ptx::smem_u32(&sm.s_full[buffer]));
         if (R == 1 || (n & 1)) tc::umma_commit(ptx::smem_u32(&sm.empty[slot]));
-        if (L::kLoadsQ && n == steps - 1) tc::umma_commit(ptx::smem_u32(&sm.q_free));
+        if (n == steps - 1) tc::umma_commit(ptx::smem_u32(&sm.q_free));
         return true;
     };
-    if (!ptx::mbar_wait(ptx::smem_u32(&sm.q_full), c.work & 1)) return false;
-    for (int n = 0; n < min(2, steps); ++n)
+    if (!ptx::mbar_wait(ptx::smem_u32(&sm.q_full[c.work & 1]), (c.work >> 1) & 1)) return false;
+    for (int n = 0; n < min(kB, steps); ++n)
         if (!form_s(n)) return false;
     for (int n = 0; n < steps; ++n) {
-        const int stream = n & 1;
-        if (!ptx::mbar_wait(ptx::smem_u32(&sm.p_ready[stream]), c.step[stream]++ & 1)) return false;
+        const uint32_t g = c.step + n, buffer = g % kB;
+        if (!ptx::mbar_wait(ptx::smem_u32(&sm.p_ready[buffer]), g / kB & 1)) return false;
         if (kMode != kMaxima) {
             const uint32_t entry = c.entry + value_entry<R>(tile_of<R>(n), it.tiles), slot = entry % L::kSlots;
             if (!full(entry)) return false;
+            // the rows of the item before have been read from O
+            if (n == 0 && c.work > 0 && !ptx::mbar_wait(ptx::smem_u32(&sm.o_free), (c.work - 1) & 1)) return false;
             tc::fence_after_sync();
-            issue_pv<D, R, KV>(cta, stream, slot, n >= R);
-            if (R == 1 || stream == 1) tc::umma_commit(ptx::smem_u32(&sm.empty[slot]));
+            issue_pv<D, R, KV>(cta, R == 2 ? n & 1 : 0, buffer, slot, n >= R);
+            if (R == 1 || (n & 1)) tc::umma_commit(ptx::smem_u32(&sm.empty[slot]));
             if (n == steps - 1) tc::umma_commit(ptx::smem_u32(&sm.o_full[c.work & 1]));
         } else {
             tc::fence_after_sync();
         }
-        if (n + 2 < steps && !form_s(n + 2)) return false;
+        if (n + kB < steps && !form_s(n + kB)) return false;
     }
     c.entry += entries_of<kMode>(it);
+    c.step += steps;
     ++c.work;
     return true;
 }
@@ -492,36 +493,37 @@ template <int D, int R, int KV>
 __device__ __forceinline__ float query_factor(const TreeParams& p, const Item& it) {
     return KV == BAKLAVA_KV_FP8_E4M3 ? p.scale_log2 * p.c.kv_scale[((int64_t)p.layer * p.c.Hkv + it.h) * 4] : p.scale_log2;
 }
-// What of its row a thread puts into the operand: with R = 1 half of it (the streams share the row), else all.
-template <int D, int R>
-constexpr int kHeldPieces = D / 8 / (R == 1 ? 2 : 1);
-template <int D, int R>
-__device__ __forceinline__ void fetch_queries(const TreeParams& p, const Item& it, const Row& r, int stream, uint4 (&held)[kHeldPieces<D, R>]) {
-    const __nv_bfloat16* const row = p.q + it.b * p.sq.seq + (int64_t)(it.h * p.g + it.a0 + r.a) * p.sq.head + r.node * p.sq.token;
-#pragma unroll
-    for (int i = 0; i < kHeldPieces<D, R>; ++i)
-        held[i] = r.there ? *reinterpret_cast<const uint4*>(row + 8 * (i + (R == 1 ? stream * kHeldPieces<D, R> : 0))) : make_uint4(0, 0, 0, 0);
-}
-// The queries as operand: R = 1 into tensor memory, R = 2 (FP8) into shared memory.  `factor`: what an S has to be multiplied
-// with besides its key's scale, for base-2 logits.
+// A query row of a quantised slab as operand in shared memory, in fp16.  FP8: exact.  4 bits: times the channels' scales, brought to
+// 2^14 .. 2^15 by a power of two that `factor` takes back, in two terms: 22 bits of the largest (one term of 11 moves a row's
+// log-sum-exp by up to 5e-4).
 template <int D, int R, int KV>
-__device__ __forceinline__ void place_queries(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, const Row& r, int stream, int full_row,
-                                              uint32_t lane_addr, int lane, const uint4 (&held)[kHeldPieces<D, R>], float& factor) {
+__device__ __forceinline__ void place_queries(const TreeParams& p, const Cta& cta, const Item& it, const Row& r, int full_row, float& factor) {
     using L = Layout<D, R, KV>;
-    factor = query_factor<D, R, KV>(p, it);
-    float back = 1.0f;
     const float* const chan = p.c.kv_scale + ((int64_t)p.layer * p.c.Hkv + it.h) * 4 * D;      // 4 bits: the K channels' scales
+    const __nv_bfloat16* const row = p.q + it.b * p.sq.seq + (int64_t)(it.h * p.g + it.a0 + r.a) * p.sq.head + r.node * p.sq.token;
+    auto fetch = [&](int i, float (&x)[8]) {
+        const uint4 raw = r.there ? *reinterpret_cast<const uint4*>(row + 8 * i) : make_uint4(0, 0, 0, 0);
+        const uint32_t word[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&word[j]));
+            x[2 * j] = f.x; x[2 * j + 1] = f.y;
+        }
+        if (KV == BAKLAVA_KV_INT4) {
+            const float4 c0 = *reinterpret_cast<const float4*>(chan + 8 * i), c1 = *reinterpret_cast<const float4*>(chan + 8 * i + 4);
+            x[0] *= c0.x; x[1] *= c0.y; x[2] *= c0.z; x[3] *= c0.w;
+            x[4] *= c1.x; x[5] *= c1.y; x[6] *= c1.z; x[7] *= c1.w;
+        }
+    };
+    float back = 1.0f;
     if (KV == BAKLAVA_KV_INT4) {
-        // times the channels' scales, brought to 2^14 .. 2^15 by a power of two, in two fp16 terms: 22 bits of the largest
         float big = 0.0f;
-        if (r.there) {
-            const __nv_bfloat16* const row = p.q + it.b * p.sq.seq + (int64_t)(it.h * p.g + it.a0 + r.a) * p.sq.head + r.node * p.sq.token;
 #pragma unroll 4
-            for (int i = 0; i < D / 2; ++i) {
-                const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(row + 2 * i));
-                const float2 s = *reinterpret_cast<const float2*>(chan + 2 * i);
-                big = fmaxf(big, fmaxf(fabsf(x.x * s.x), fabsf(x.y * s.y)));
-            }
+        for (int i = 0; i < D / 8; ++i) {
+            float x[8];
+            fetch(i, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(x[j]));
         }
         int power;
         frexpf(big, &power);
@@ -529,50 +531,25 @@ __device__ __forceinline__ void place_queries(const TreeParams& p, Shared& sm, c
         factor = ldexpf(factor, power);
         back = ldexpf(1.0f, -power);
     }
-    __syncwarp();
+#pragma unroll 4
+    for (int i = 0; i < D / 8; ++i) {
+        float x[8];
+        fetch(i, x);
+        uint32_t w[4], low[4];
 #pragma unroll
-    for (int i = 0; i < kHeldPieces<D, R>; i += 2) {
-        uint32_t w[8], low[8];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const uint32_t raw[4] = {held[i + k].x, held[i + k].y, held[i + k].z, held[i + k].w};
-            float x[8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw[j]));
-                x[2 * j] = f.x; x[2 * j + 1] = f.y;
-            }
-            if (KV == BAKLAVA_KV_INT4) {
-                const int d0 = 8 * (i + k + stream * kHeldPieces<D, R>);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] *= chan[d0 + j] * back;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {                 // nibbles j and j + 4 of a word are a pair
-                    w[4 * k + j] = pack_f16(x[j], x[j + 4]);
-                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[4 * k + j]));
-                    low[4 * k + j] = pack_f16(x[j] - f.x, x[j + 4] - f.y);
-                }
+        for (int j = 0; j < 4; ++j) {
+            if (KV == BAKLAVA_KV_INT4) {                      // nibbles j and j + 4 of a word are a pair
+                w[j] = pack_f16(x[j] * back, x[j + 4] * back);
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+                low[j] = pack_f16(x[j] * back - f.x, x[j + 4] * back - f.y);
             } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w[4 * k + j] = KV == BAKLAVA_KV_BF16 ? raw[j] : pack_f16(x[2 * j], x[2 * j + 1]);
+                w[j] = pack_f16(x[2 * j], x[2 * j + 1]);
             }
         }
-        if (R == 1) {
-            const uint32_t column = lane_addr + kQColumn + stream * (D / 4) + i * 4;
-            store_8(column, w);
-            if (L::kTerms == 2) store_8(column + D / 2, low);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-                *reinterpret_cast<uint4*>(cta.ptr + ((i + k) >> 3) * L::kQBox + full_row * 128 + ((((i + k) & 7) ^ (full_row & 7)) << 4)) =
-                    make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
-        }
+        uint8_t* const at = cta.ptr + (i >> 3) * L::kQBox + full_row * 128 + (((i & 7) ^ (full_row & 7)) << 4);
+        *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (L::kTerms == 2) *reinterpret_cast<uint4*>(at + L::kQTerm) = make_uint4(low[0], low[1], low[2], low[3]);
     }
-    if (R == 1) tc::tmem_st_wait();
-    else tc::fence_proxy_async_smem();
-    tc::fence_before_sync();
-    __syncwarp();
-    if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.q_full));
 }
 
 // Sixteen logits -> eight columns of probabilities.  kMasked: keys first .. first + 15 of the tile, of which those at or
@@ -580,15 +557,7 @@ __device__ __forceinline__ void place_queries(const TreeParams& p, Shared& sm, c
 template <int KV, bool kMasked>
 __device__ __forceinline__ void softmax_16(uint32_t (&v)[16], uint32_t column, int first, int keys, int hole, const float4* scales,
                                            ptx::f32x2 scale2, ptx::f32x2 minus, ptx::f32x2 (&sum)[2]) {
-    if (KV == BAKLAVA_KV_INT4) {
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const float4 s = scales[(first >> 1) + c];
-            v[2 * c] = __float_as_uint(__uint_as_float(v[2 * c]) * s.x);
-            v[2 * c + 1] = __float_as_uint(__uint_as_float(v[2 * c + 1]) * s.z);
-        }
-    }
-    if (kMasked) {
+    if (kMasked && KV != BAKLAVA_KV_INT4) {
 #pragma unroll
         for (int c = 0; c < 16; ++c)
             if (first + c >= keys || first + c == hole) v[c] = 0xff800000u;
@@ -596,15 +565,24 @@ __device__ __forceinline__ void softmax_16(uint32_t (&v)[16], uint32_t column, i
     uint32_t w[8];
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-        const float2 x = ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1])), scale2, minus));
-        float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
-        sum[c & 1] = ptx::add2(sum[c & 1], ptx::pack2(p0, p1));
+        ptx::f32x2 s = ptx::pack2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1])), value2 = 0ull;
         if (KV == BAKLAVA_KV_INT4) {
-            const float4 s = scales[(first >> 1) + c];
-            p0 *= s.y;
-            p1 *= s.w;
+            const float4 of = scales[(first >> 1) + c];
+            s = ptx::mul2(s, ptx::pack2(of.x, of.z));
+            value2 = ptx::pack2(of.y, of.w);
+            if (kMasked) {
+                float2 m = ptx::unpack2(s);
+                if (first + 2 * c >= keys || first + 2 * c == hole) m.x = -INFINITY;
+                if (first + 2 * c + 1 >= keys || first + 2 * c + 1 == hole) m.y = -INFINITY;
+                s = ptx::pack2(m.x, m.y);
+            }
         }
-        w[c] = KV == BAKLAVA_KV_FP8_E4M3 ? pack_f16(p0, p1) : pack_bf16(p0, p1);
+        const float2 x = ptx::unpack2(ptx::fma2(s, scale2, minus));
+        ptx::f32x2 prob = ptx::pack2(fast_exp2(x.x), fast_exp2(x.y));
+        sum[c & 1] = ptx::add2(sum[c & 1], prob);
+        if (KV == BAKLAVA_KV_INT4) prob = ptx::mul2(prob, value2);
+        const float2 f = ptx::unpack2(prob);
+        w[c] = KV == BAKLAVA_KV_FP8_E4M3 ? pack_f16(f.x, f.y) : pack_bf16(f.x, f.y);
     }
     store_8(column, w);
 }
@@ -635,20 +613,17 @@ __device__ __forceinline__ void clear_value_row(uint8_t* tile, int row) {
     tc::fence_proxy_async_smem();
 }
 
-// One item's rows.  kMaxima: `ref` becomes the row's largest logit, raised so that the sum of that many probabilities stays
-// below one.  `before_end` is called when the last tile has been worked on.
-template <int D, int R, int KV, int kMode, typename F>
-__device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, Count& c, int warp, int lane,
-                                            float factor, float& ref, bool& again, F before_end) {
+// One item's probabilities.  kMaxima: `ref` becomes the row's largest logit, raised so that the sum of that many probabilities
+// stays below one.
+template <int D, int R, int KV, int kMode>
+__device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, Count& c, int warp, int lane, float& ref) {
     using L = Layout<D, R, KV>;
-    const int stream = (warp - 2) >> 2, quarter = warp & 3, row = 32 * quarter + lane;
+    const int stream = warp >> 2, quarter = warp & 3, row = 32 * quarter + lane, turn = c.work & 1;
     const Row r(p, it, R == 2 ? stream * kRows + row : row);
-    const int64_t at = ((int64_t)it.index * p.g + it.a0 + r.a) * p.T + r.node;
-    // (done again, a row is written only if it was marked: the others stay what they are whatever happened to this one)
-    const bool there = r.there && (kMode == kFast || p.stats[at].y == INFINITY);
-    const bool busy = __any_sync(0xffffffffu, there);                  // (a warp without rows leaves its part of P as it is)
-    const uint32_t lane_addr = cta.tmem + ((uint32_t)(32 * quarter) << 16), column = lane_addr + stream * kKeys;
+    const bool busy = __any_sync(0xffffffffu, r.there);                // (a warp without rows leaves its part of P as it is)
+    const uint32_t lane_addr = cta.tmem + ((uint32_t)(32 * quarter) << 16);
     const int steps = it.tiles * R;
+    float factor = query_factor<D, R, KV>(p, it);
     ptx::f32x2 sum[2] = {0ull, 0ull};
     float largest = -INFINITY;
     for (int n = stream; n < steps; n += 2) {
@@ -657,7 +632,12 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
         const int no_row = it.hole >= 0 ? hole : -1;
         const uint32_t entry = c.entry + value_entry<R>(t, it.tiles), slot = entry % L::kSlots;
         const float4* const scales = reinterpret_cast<const float4*>(cta.ptr + L::kScales + slot * L::kScaleBytes);
-        if (!ptx::mbar_wait(ptx::smem_u32(&sm.s_full[stream]), c.step[stream]++ & 1)) return false;
+        const uint32_t g = c.step + n, buffer = g % L::kBuffers, column = lane_addr + buffer * kKeys;
+        if (!ptx::mbar_wait(ptx::smem_u32(&sm.s_full[buffer]), g / L::kBuffers & 1)) return false;
+        if (KV == BAKLAVA_KV_INT4 && n == stream) {
+            if (!ptx::mbar_wait(ptx::smem_u32(&sm.q_full[turn]), (c.work >> 1) & 1)) return false;
+            factor = sm.factor[turn][R == 2 ? stream : 0][row];
+        }
         if (kMode != kMaxima && (KV == BAKLAVA_KV_INT4 || (!L::kQuantised && masked && (R == 1 || stream == 0))))
             if (!ptx::mbar_wait(ptx::smem_u32(&sm.full[slot]), entry / L::kSlots & 1)) return false;
         __syncwarp();
@@ -683,107 +663,130 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
                 if (row >= keys || row == no_row) clear_value_row<D, R, KV>(cta.ptr + L::kRing + slot * L::kTileBytes, row);
                 __syncwarp();
             }
-            if (busy) {
-                if (kMode == kFast && n == stream && (R == 2 || stream == 0)) {
-                    // the stabiliser need not be the maximum: the largest of the first eight rows will do
-                    uint32_t v[8];
-                    tc::tmem_ld_32x32_x8(column, v);
-                    tc::tmem_ld_wait();
-                    float top = -INFINITY;
+            if (busy && kMode == kFast && n == stream && (R == 2 || stream == 0)) {
+                // the stabiliser need not be the maximum: the largest of the first eight rows will do
+                uint32_t v[8];
+                tc::tmem_ld_32x32_x8(column, v);
+                tc::tmem_ld_wait();
+                float top = -INFINITY;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (e < keys && e != no_row) {
-                            float s = __uint_as_float(v[e]);
-                            if (KV == BAKLAVA_KV_INT4) s *= reinterpret_cast<const float*>(scales)[2 * e];
-                            top = fmaxf(top, s * factor);
-                        }
-                    ref = top == -INFINITY ? 0.0f : top;
-                }
-                if (kMode == kFast && R == 1 && n == stream) {          // stream 1 takes stream 0's
-                    if (stream == 0) {
-                        sm.ref[row] = ref;
-                        __syncwarp();
-                        if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.ref_ready));
-                    } else {
-                        if (!ptx::mbar_wait(ptx::smem_u32(&sm.ref_ready), c.work & 1)) return false;
-                        __syncwarp();
-                        ref = sm.ref[row];
+                for (int e = 0; e < 8; ++e)
+                    if (e < keys && e != no_row) {
+                        float s = __uint_as_float(v[e]);
+                        if (KV == BAKLAVA_KV_INT4) s *= reinterpret_cast<const float*>(scales)[2 * e];
+                        top = fmaxf(top, s * factor);
                     }
+                ref = top == -INFINITY ? 0.0f : top;
+            }
+            if (R == 1 && n == stream) {                                // stream 1 takes stream 0's
+                if (stream == 0) {
+                    sm.ref[turn][0][row] = ref;
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.ref_ready));
+                } else {
+                    if (!ptx::mbar_wait(ptx::smem_u32(&sm.ref_ready), c.work & 1)) return false;
+                    __syncwarp();
+                    ref = sm.ref[turn][0][row];
                 }
+            }
+            if (busy) {
                 if (masked) softmax_row<KV, true>(column, keys, no_row, scales, factor, ref, sum);
                 else softmax_row<KV, false>(column, keys, no_row, scales, factor, ref, sum);
-            } else if (kMode == kFast && R == 1 && n == 0) {
-                if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.ref_ready));
             }
         }
         tc::fence_before_sync();
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.p_ready[stream]));
+        if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.p_ready[buffer]));
     }
     c.entry += entries_of<kMode>(it);
+    c.step += steps;
     ++c.work;
-    // the softmax warps wait for one another
-    auto together = [&] {
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.both));
-        return ptx::mbar_wait(ptx::smem_u32(&sm.both), c.both++ & 1);
-    };
     if (kMode == kMaxima) {
-        if (R == 1) {
-            sm.part[stream][row] = largest;
-            if (!together()) return false;
-            largest = fmaxf(sm.part[0][row], sm.part[1][row]);
+        if (R == 1) {                                                   // the streams have seen a part of the row's keys each
+            sm.part[turn][stream][row] = largest;
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.both));
+            if (!ptx::mbar_wait(ptx::smem_u32(&sm.both), 0)) return false;
+            largest = fmaxf(sm.part[turn][0][row], sm.part[turn][1][row]);
         }
         ref = largest == -INFINITY ? 0.0f : largest + (float)(32 - __clz(it.keys));
         return true;
     }
-    before_end();
     const float2 halves = ptx::unpack2(ptx::add2(sum[0], sum[1]));
-    float l = halves.x + halves.y;
-    if (R == 1) {                                                       // the streams hold a part of every row's sum each
-        sm.part[stream][row] = l;
-        if (!together()) return false;
-        l = sm.part[0][row] + sm.part[1][row];
+    sm.part[turn][stream][row] = halves.x + halves.y;
+    if (R == 2) sm.ref[turn][stream][row] = ref;
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.sums[turn]));
+    return true;
+}
+
+// ---------------------------------------------------------------- the warps that write the rows
+// The item's queries into their places (not where they come by TMA), announced on the item's barrier.
+template <int D, int R, int KV>
+__device__ __forceinline__ void lay_out_queries(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, uint32_t work, int warp, int lane) {
+    const int row = 32 * (warp & 3) + lane;
+#pragma unroll 1
+    for (int acc = 0; acc < R; ++acc) {
+        const int full_row = acc * kRows + row;
+        float factor = query_factor<D, R, KV>(p, it);
+        place_queries<D, R, KV>(p, cta, it, Row(p, it, full_row), full_row, factor);
+        if (KV == BAKLAVA_KV_INT4) sm.factor[work & 1][acc][row] = factor;
     }
-    again = !(l <= kMaxSum);
-    if (!ptx::mbar_wait(ptx::smem_u32(&sm.o_full[(c.work - 1) & 1]), ((c.work - 1) >> 1) & 1)) return false;
+    tc::fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.q_full[work & 1]));
+}
+// The item's rows out of tensor memory.  `work`: its number among those with work.
+template <int D, int R, int KV, int kMode>
+__device__ __forceinline__ bool write_rows(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, uint32_t work, int warp, int lane, bool& again) {
+    const int quarter = warp & 3, row = 32 * quarter + lane, turn = work & 1;
+    const uint32_t lane_addr = cta.tmem + ((uint32_t)(32 * quarter) << 16);
+    if (!ptx::mbar_wait(ptx::smem_u32(&sm.sums[turn]), (work >> 1) & 1)) return false;
+    if (!ptx::mbar_wait(ptx::smem_u32(&sm.o_full[turn]), (work >> 1) & 1)) return false;
     __syncwarp();
     tc::fence_after_sync();
-    if (busy) {
-        constexpr int kColumns = R == 1 ? D / 2 : D;                    // R = 1: the streams share a row's columns
-        const int col0 = R == 1 ? stream * kColumns : 0;
-        const uint32_t o = lane_addr + kOColumn + (R == 2 ? stream * 128 : col0);
-        float* const out = p.partial + at * D + col0;
+#pragma unroll 1
+    for (int acc = 0; acc < R; ++acc) {
+        const Row r(p, it, acc * kRows + row);
+        const int64_t at = ((int64_t)it.index * p.g + it.a0 + r.a) * p.T + r.node;
+        // (done again, a row is written only if it was marked: the others stay what they are whatever happened to this one)
+        const bool there = r.there && (kMode == kFast || p.stats[at].y == INFINITY);
+        if (!__any_sync(0xffffffffu, there)) continue;
+        const float ref = sm.ref[turn][R == 1 ? 0 : acc][row];
+        const float l = R == 1 ? sm.part[turn][0][row] + sm.part[turn][1][row] : sm.part[turn][acc][row];
+        float* const out = p.partial + at * D;
         const float* const four = p.c.kv_scale + ((int64_t)p.layer * p.c.Hkv + it.h) * 4 * (KV == BAKLAVA_KV_INT4 ? D : 1);
         const float v_scale = KV == BAKLAVA_KV_FP8_E4M3 ? four[2] : 1.0f;
-#pragma unroll 1
-        for (int col = 0; col < kColumns; col += 16) {
-            uint32_t v[16];
-            load_16(o + col, v);
+        bool bad = !(l <= kMaxSum);
+        uint32_t v[2][16];
+        load_16(lane_addr + Layout<D, R, KV>::kOColumn + acc * 128, v[0]);
+#pragma unroll
+        for (int col = 0; col < D; col += 16) {
             tc::tmem_ld_wait();
+            if (col + 16 < D) load_16(lane_addr + Layout<D, R, KV>::kOColumn + acc * 128 + col + 16, v[(col >> 4) + 1 & 1]);
             float x[2][8], worst = 0.0f;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                float y = __uint_as_float(v[e]);
+                float y = __uint_as_float(v[col >> 4 & 1][e]);
                 worst = fmaf(fabsf(y), 0x1p-20f, worst);                // NaN propagates through the sum, infinities too
                 const int d = KV == BAKLAVA_KV_INT4 ? (e & 8) + ((e & 7) >> 1) + 4 * (e & 1) : e;
                 if (KV == BAKLAVA_KV_FP8_E4M3) y *= v_scale;
-                if (KV == BAKLAVA_KV_INT4) y *= four[2 * D + col0 + col + d];
+                if (KV == BAKLAVA_KV_INT4) y *= four[2 * D + col + d];
                 x[d >> 3][d & 7] = y;
             }
-            again = again || !(worst <= kFinite);
+            bad = bad || !(worst <= kFinite);
             if (there) {
                 store_sector(out + col, x[0]);
                 store_sector(out + col + 8, x[1]);
             }
         }
-        // (a row without any weight: the reference means nothing)
-        if (there && (R == 2 || stream == 0)) p.stats[at] = make_float2(l == 0.0f ? -INFINITY : ref, l);
+        // (a row without any weight: the reference means nothing; one to be done again: an infinite sum)
+        if (there) p.stats[at] = make_float2(l == 0.0f ? -INFINITY : ref, bad && kMode == kFast ? INFINITY : l);
+        again = again || (bad && there && kMode == kFast);
     }
-    again = again && there && kMode == kFast;
     tc::fence_before_sync();
-    if (R == 1 && !together()) return false;                            // (O and the sums may be written again when both have read them)
-    if (again) p.stats[at].y = INFINITY;
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.o_free));
     return true;
 }
 
@@ -793,25 +796,32 @@ __device__ __forceinline__ bool next_item(Shared& sm, int k, Item& it) {
     it = sm.item[k % kItemRing];
     return true;
 }
+// f(barrier, arrivals) for the barriers that a pass over items begins with anew; a warp's lanes share the work
 template <typename L, typename F>
-__device__ __forceinline__ void each_barrier(Shared& sm, F f) {
-    for (int s = 0; s < L::kSlots; ++s) {
-        f(sm.full[s], L::kQuantised ? kConvertWarps : 1);
-        f(sm.empty[s], 1);
+__device__ __forceinline__ void each_barrier(Shared& sm, int lane, F f) {
+    if (lane < L::kSlots) {
+        f(sm.full[lane], L::kQuantised ? kConvertWarps : 1);
+        f(sm.empty[lane], 1);
     }
-    for (int s = 0; s < L::kRawSlots; ++s) {
-        f(sm.raw_full[s], 1);
-        f(sm.raw_empty[s], kConvertWarps);
+    if (lane < L::kRawSlots) {
+        f(sm.raw_full[lane], 1);
+        f(sm.raw_empty[lane], kConvertWarps);
     }
-    for (int s = 0; s < 2; ++s) {
-        f(sm.s_full[s], 1);
-        f(sm.p_ready[s], kSoftmaxWarps / 2);
-        f(sm.o_full[s], 1);
+    if (lane < L::kBuffers) {
+        f(sm.s_full[lane], 1);
+        f(sm.p_ready[lane], kSoftmaxWarps / 2);
     }
-    f(sm.q_full, L::kLoadsQ ? 1 : kSoftmaxWarps);
-    f(sm.q_free, 1);
-    f(sm.ref_ready, kSoftmaxWarps / 2);
-    f(sm.both, kSoftmaxWarps);
+    if (lane < 2) {
+        f(sm.o_full[lane], 1);
+        f(sm.q_full[lane], L::kLoadsQ ? 1 : kRowWarps);
+        f(sm.sums[lane], kSoftmaxWarps);
+    }
+    if (lane == 2) {
+        f(sm.q_free, 1);
+        f(sm.o_free, kRowWarps);
+        f(sm.ref_ready, kSoftmaxWarps / 2);
+        f(sm.both, kSoftmaxWarps);
+    }
 }
 
 // An item again, alone: first for its rows' maxima, then with them as references.  The whole CTA; barriers are set up anew.
@@ -821,8 +831,8 @@ __device__ __noinline__ void redo_pass(const TreeParams& p, Shared& sm, const Ct
     using L = Layout<D, R, KV>;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     __syncthreads();
-    if (tid == 0) {
-        each_barrier<L>(sm, [](uint64_t& bar, int count) { ptx::mbar_init(ptx::smem_u32(&bar), count); });
+    if (warp == 0) {
+        each_barrier<L>(sm, lane, [](uint64_t& bar, int count) { ptx::mbar_init(ptx::smem_u32(&bar), count); });
         ptx::fence_mbar_init();
     }
     tc::fence_before_sync();
@@ -830,24 +840,21 @@ __device__ __noinline__ void redo_pass(const TreeParams& p, Shared& sm, const Ct
     tc::fence_after_sync();
     Count c;
     bool ok = true, again = false;
-    if (warp == 0) {
+    if (warp < kSoftmaxWarps) {
+        ok = soften_item<D, R, KV, kMode>(p, sm, cta, it, c, warp, lane, ref);
+    } else if (warp < kRowWarp0 + kRowWarps) {
+        if (!L::kLoadsQ) {
+            lay_out_queries<D, R, KV>(p, sm, cta, it, 0, warp, lane);
+        }
+        if (kMode == kExact) ok = write_rows<D, R, KV, kMode>(p, sm, cta, it, 0, warp, lane, again);
+    } else if (warp == kProducerWarp) {
         if (lane == 0) {
-            if (L::kLoadsQ) load_queries<D, R, KV>(p, sm, cta, it, q_map);
+            if (L::kLoadsQ) load_queries<D, R, KV>(p, sm, cta, it, 0, q_map);
             for (int e = 0; e < entries_of<kMode>(it) && ok; ++e) ok = load_entry<D, R, KV, kMode>(p, sm, cta, it, 0, e, k_map, v_map);
         }
-    } else if (warp == 1) {
+    } else if (warp == kMmaWarp) {
         if (lane == 0) ok = issue_item<D, R, KV, kMode>(sm, cta, it, c);
-    } else if (warp < 2 + kSoftmaxWarps) {
-        const int stream = (warp - 2) >> 2, full_row = 32 * (warp & 3) + lane + (R == 2 ? stream * kRows : 0);
-        float factor = query_factor<D, R, KV>(p, it);
-        if (!L::kLoadsQ) {
-            const Row r(p, it, full_row);
-            uint4 held[kHeldPieces<D, R>];
-            fetch_queries<D, R>(p, it, r, stream, held);
-            place_queries<D, R, KV>(p, sm, cta, it, r, stream, full_row, cta.tmem + ((uint32_t)(32 * (warp & 3)) << 16), lane, held, factor);
-        }
-        ok = soften_item<D, R, KV, kMode>(p, sm, cta, it, c, warp, lane, factor, ref, again, [] {});
-    } else {
+    } else if (warp >= kConvertWarp0) {
         ok = convert_item<D, R, KV, kMode>(p, sm, cta, it, c, warp, lane);
     }
     if (!ok) sm.abort = 1;
@@ -855,7 +862,8 @@ __device__ __noinline__ void redo_pass(const TreeParams& p, Shared& sm, const Ct
     __syncthreads();
     tc::fence_after_sync();
     if (sm.abort && tid == 0) let_copies_land();
-    if (tid == 0) each_barrier<L>(sm, [](uint64_t& bar, int) { ptx::mbar_inval(ptx::smem_u32(&bar)); });
+    __syncthreads();
+    if (warp == 0) each_barrier<L>(sm, lane, [](uint64_t& bar, int) { ptx::mbar_inval(ptx::smem_u32(&bar)); });
     __syncthreads();
 }
 
@@ -871,22 +879,25 @@ __global__ void __launch_bounds__(Layout<D, R, KV>::kThreads, 1) tree_tile_kerne
     cta.base = ptx::smem_u32(smem_raw);
     cta.ptr = smem_raw;
     launch_dependents();
-    if (tid == 0) {
-        each_barrier<L>(sm, [](uint64_t& bar, int count) { ptx::mbar_init(ptx::smem_u32(&bar), count); });
-        ptx::mbar_init(ptx::smem_u32(&sm.bar_answer), 1);
-        for (int s = 0; s < kItemRing; ++s) {
-            ptx::mbar_init(ptx::smem_u32(&sm.bar_item[s]), 1);
-            sm.redo_mark[s] = 0;
-            sm.item[s].index = -1;
+    if (warp == kScoutWarp) {
+        each_barrier<L>(sm, lane, [](uint64_t& bar, int count) { ptx::mbar_init(ptx::smem_u32(&bar), count); });
+        if (lane == 0) {
+            ptx::mbar_init(ptx::smem_u32(&sm.bar_answer), 1);
+            for (int s = 0; s < kItemRing; ++s) {
+                ptx::mbar_init(ptx::smem_u32(&sm.bar_item[s]), 1);
+                sm.redo_mark[s] = 0;
+                if (s < kItemRing - 1) sm.item[s].index = -1;
+            }
+            sm.abort = cta.base & 1023u ? 1 : 0;              // (the tiles' swizzle needs it; the base is where it is)
+            sm.redo_count = 0;
+            sm.finished = 0;
         }
-        sm.abort = cta.base & 1023u ? 1 : 0;                  // (the tiles' swizzle needs it; the base is where it is)
-        sm.redo_count = 0;
-        sm.item[kItemRing - 1] = find_item(p, blockIdx.x);
         ptx::fence_mbar_init();
-    }
-    if (warp == 1) {
+    } else if (warp == kMmaWarp) {
         tc::tmem_alloc(ptx::smem_u32(&sm.tmem_slot), kTmemColumns);
         tc::tmem_relinquish();
+    } else if (warp == kProducerWarp && lane == 0) {
+        sm.item[kItemRing - 1] = find_item(p, blockIdx.x);
     }
     tc::fence_before_sync();
     __syncthreads();
@@ -896,43 +907,51 @@ __global__ void __launch_bounds__(Layout<D, R, KV>::kThreads, 1) tree_tile_kerne
     if (!sm.abort) {
         bool ok = true;
         Count c;
-        if (warp == 0) {
-            if (lane == 0) produce<D, R, KV>(p, sm, cta, it, q_map, k_map, v_map);
-        } else if (warp == 1) {
+        if (warp < kSoftmaxWarps) {
+            float ref = 0.0f;
+            for (int k = 0; ok && it.index >= 0; ++k) {
+                if (it.tiles > 0) ok = soften_item<D, R, KV, kFast>(p, sm, cta, it, c, warp, lane, ref);
+                if (ok) ok = next_item(sm, k, it);
+            }
+        } else if (warp < kRowWarp0 + kRowWarps) {
+            uint32_t work = 0;
+            if (!L::kLoadsQ && it.tiles > 0) lay_out_queries<D, R, KV>(p, sm, cta, it, 0, warp, lane);
+            for (int k = 0; ok && it.index >= 0; ++k) {
+                // the next item's queries first: its logits are formed while this one's rows are written
+                Item next;
+                ok = next_item(sm, k, next);
+                if (!ok) break;
+                const uint32_t next_work = work + (it.tiles > 0);
+                if (!L::kLoadsQ && next.index >= 0) {
+                    if (next_work > 0) ok = ptx::mbar_wait(ptx::smem_u32(&sm.q_free), (next_work - 1) & 1);
+                    if (!ok) break;
+                    __syncwarp();
+                    lay_out_queries<D, R, KV>(p, sm, cta, next, next_work, warp, lane);
+                }
+                if (it.tiles > 0) {
+                    bool again = false;
+                    ok = write_rows<D, R, KV, kFast>(p, sm, cta, it, work, warp, lane, again);
+                    if (ok && again && atomicExch(&sm.redo_mark[k % kItemRing], k + 1) != k + 1) sm.redo[atomicAdd(&sm.redo_count, 1)] = it;
+                }
+                __syncwarp();
+                if (ok && lane == 0) atomicAdd(&sm.finished, 1);
+                work = next_work;
+                it = next;
+            }
+        } else if (warp == kProducerWarp) {
+            if (lane == 0)
+                for (int k = 0; ok && it.index >= 0; ++k) {
+                    if (it.tiles > 0) ok = produce_item<D, R, KV>(p, sm, cta, it, c, q_map, k_map, v_map);
+                    if (ok) ok = next_item(sm, k, it);
+                }
+        } else if (warp == kMmaWarp) {
             if (lane == 0)
                 for (int k = 0; ok && it.index >= 0; ++k) {
                     if (it.tiles > 0) ok = issue_item<D, R, KV, kFast>(sm, cta, it, c);
                     if (ok) ok = next_item(sm, k, it);
                 }
-        } else if (warp < 2 + kSoftmaxWarps) {
-            const int stream = (warp - 2) >> 2, full_row = 32 * (warp & 3) + lane + (R == 2 ? stream * kRows : 0);
-            const uint32_t lane_addr = cta.tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-            float ref = 0.0f, factor = 0.0f;
-            uint4 held[kHeldPieces<D, R>];
-            bool fetched = false;
-            for (int k = 0; ok && it.index >= 0; ++k) {
-                bool again = false, found = false;
-                Item next = it;
-                if (it.tiles > 0) {
-                    if (!L::kLoadsQ) {
-                        const Row r(p, it, full_row);
-                        if (!fetched) fetch_queries<D, R>(p, it, r, stream, held);
-                        place_queries<D, R, KV>(p, sm, cta, it, r, stream, full_row, lane_addr, lane, held, factor);
-                    } else {
-                        factor = query_factor<D, R, KV>(p, it);
-                    }
-                    ok = soften_item<D, R, KV, kFast>(p, sm, cta, it, c, warp, lane, factor, ref, again, [&] {
-                        // the next item's queries are asked for while this one's rows are written
-                        found = next_item(sm, k, next);
-                        __syncwarp();
-                        fetched = found && next.index >= 0;
-                        if (!L::kLoadsQ && fetched) fetch_queries<D, R>(p, next, Row(p, next, full_row), stream, held);
-                    });
-                    if (ok && again && atomicExch(&sm.redo_mark[k % kItemRing], k + 1) != k + 1) sm.redo[atomicAdd(&sm.redo_count, 1)] = it;
-                }
-                if (ok && !found) ok = next_item(sm, k, next);
-                it = next;
-            }
+        } else if (warp == kScoutWarp) {
+            if (lane == 0) scout(p, sm);
         } else {
             for (int k = 0; ok && it.index >= 0; ++k) {
                 if (it.tiles > 0) ok = convert_item<D, R, KV, kFast>(p, sm, cta, it, c, warp, lane);
@@ -947,7 +966,7 @@ __global__ void __launch_bounds__(Layout<D, R, KV>::kThreads, 1) tree_tile_kerne
     if (sm.abort) {
         if (tid == 0) let_copies_land();
     } else if (sm.redo_count > 0) {
-        if (tid == 0) each_barrier<L>(sm, [](uint64_t& bar, int) { ptx::mbar_inval(ptx::smem_u32(&bar)); });
+        if (warp == 0) each_barrier<L>(sm, lane, [](uint64_t& bar, int) { ptx::mbar_inval(ptx::smem_u32(&bar)); });
         for (int i = 0; i < sm.redo_count && !sm.abort; ++i) {
             float ref = 0.0f;
             redo_pass<D, R, KV, kMaxima>(p, sm, cta, sm.redo[i], ref, q_map, k_map, v_map);
@@ -961,7 +980,7 @@ __global__ void __launch_bounds__(Layout<D, R, KV>::kThreads, 1) tree_tile_kerne
         for (int i = 0; i < sm.redo_count; ++i) note_lost(p, sm.redo[i]);
     }
     __syncthreads();
-    if (warp == 1) tc::tmem_dealloc(cta.tmem, kTmemColumns);
+    if (warp == kMmaWarp) tc::tmem_dealloc(cta.tmem, kTmemColumns);
 }
 
 // x 2^(ref - top).  A reference is not the maximum: it may lie so far below that its sums reach 2^120, and 2^(ref - top) alone
@@ -1168,7 +1187,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_attn(
     p.layer = info->layer_begin;
     const int kv = cache->kv_dtype;
     p.rows_per_head = (T + 7) / 8 * 8;
-    // query heads that the accumulators have room for (4 bits: one accumulator, the queries' two terms take the other's place)
+    // query heads that the accumulators have room for: two, one where queries have two terms
     const int most = (kv == BAKLAVA_KV_INT4 ? 1 : 2) * kRows / p.rows_per_head;
     p.parts = (p.g + most - 1) / most;
     p.heads = (p.g + p.parts - 1) / p.parts;
