@@ -375,16 +375,38 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_plan(const ba
     tokens *= B;
     std::stable_sort(heads.begin(), heads.end(), [&](int a, int b) { return c[a] > c[b]; });
     constexpr int kKeys = 128;                               // keys to a tile
-    int64_t want = chunk_tokens;
-    if (want == 0) want = std::max<int64_t>(4 * kKeys, std::min<int64_t>(8192, tokens / n_sm));
+    auto pieces_of = [](int64_t rows, int64_t want, int64_t* len) {       // equal pieces of about `want` rows, whole tiles
+        const int64_t pieces = (rows + want - 1) / want;
+        *len = ((rows + pieces - 1) / pieces + kKeys - 1) / kKeys * kKeys;
+        return (rows + *len - 1) / *len;
+    };
+    // One block to an SM goes from item to item.  Where every item can have an SM of its own, equal chunks, the shortest with which
+    // that is so; else chunks of up to 4 096 rows first, for half of the rows, then shorter ones towards a short tail.
+    int64_t want = chunk_tokens, len;
+    bool graded = false;
+    if (want == 0) {
+        for (want = 2 * kKeys; want < 4096; want += kKeys) {
+            int64_t count = 0;
+            for (int h : heads) count += pieces_of(c[h], want, &len) * B;
+            if (count <= n_sm) break;
+        }
+        graded = want >= 2048;
+        if (graded) want = std::max<int64_t>(1024, std::min<int64_t>(4096, tokens / (2 * (int64_t)n_sm)));
+    }
     want = std::max<int64_t>(kKeys, (want + kKeys - 1) / kKeys * kKeys);
-    int64_t n_items = 0;
+    int64_t n_items = 0, done = 0;
     for (int h : heads) {
-        int64_t pieces = (c[h] + want - 1) / want;
-        const int64_t len = ((c[h] + pieces - 1) / pieces + kKeys - 1) / kKeys * kKeys;
-        pieces = (c[h] + len - 1) / len;
-        if (pieces > 32767) return BAKLAVA_ERR_UNSUPPORTED;
-        for (int b = 0; b < B; ++b)
+        for (int b = 0; b < B; ++b) {
+            int64_t now = want;
+            if (graded) {
+                if (done * 20 >= tokens * 19) now = want / 8;
+                else if (done * 5 >= tokens * 4) now = want / 4;
+                else if (done * 2 >= tokens) now = want / 2;
+                now = std::max<int64_t>(4 * kKeys, now);
+            }
+            done += c[h];
+            const int64_t pieces = pieces_of(c[h], now, &len);
+            if (pieces > 32767) return BAKLAVA_ERR_UNSUPPORTED;
             for (int64_t pc = 0; pc < pieces; ++pc, ++n_items) {
                 if (!items_out) continue;
                 if (n_items >= items_capacity) return BAKLAVA_ERR_WORKSPACE;
@@ -394,6 +416,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_plan(const ba
                 it[2] = (int32_t)len;
                 it[3] = (int32_t)(pc | (pieces << 16));
             }
+        }
     }
     if (n_items > INT32_MAX) return BAKLAVA_ERR_UNSUPPORTED;
     info->n_items = (int32_t)n_items;

@@ -7,6 +7,7 @@
 
 #include <atomic>
 #include <cmath>
+#include <cstddef>
 #include <cstdint>
 
 #include "baklava.h"
@@ -51,11 +52,6 @@ __device__ __forceinline__ void load_bf16(const __nv_bfloat16* row, int lane, fl
         x[0] = a.x; x[1] = a.y;
     }
 }
-__device__ __forceinline__ float warp_sum(float x) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
-}
 // ---------------------------------------------------------------- slab rows on the tensor cores
 constexpr int kKeys = 128;                    // slab rows to a tile
 constexpr int kRows = 128;                    // query rows to an accumulator
@@ -68,7 +64,7 @@ constexpr int kRowWarp0 = kSoftmaxWarps, kProducerWarp = kRowWarp0 + kRowWarps, 
               kConvertWarp0 = kScoutWarp + 1;
 constexpr int kItemRing = 4;
 constexpr int kMaxRedo = 8;
-constexpr int kMaxSlots = 13;
+constexpr int kMaxSlots = 12;
 constexpr uint32_t kTmemColumns = 512;
 constexpr int kMaxBuffers = 3;
 constexpr float kFinite = 3.0e38f;
@@ -96,10 +92,11 @@ struct Shared {
     int abort;
     int finished;                             // items that are done with, counted by each row warp
     // of two items in turn: the rows' references (R = 1: only [.][0]), the streams' sums, 4 bits: the queries' factors
-    float ref[2][2][kRows], part[2][2][kRows], factor[2][2][kRows];
+    float ref[2][2][kRows], part[2][2][kRows];
+    float factor[2][kRows];                   // (at the end: only where queries have factors is there room for it)
 };
-constexpr int kSharedBytes = 7680;
-static_assert(sizeof(Shared) <= kSharedBytes, "the tiles take the rest");
+constexpr int kSharedBytes = 5632;
+static_assert(offsetof(Shared, factor) <= kSharedBytes, "the tiles take the rest");
 
 // How an instance lies in shared memory: the query rows, the ring of operand tiles, for quantised slabs the ring of
 // tiles as they are in the slab and the rows' scales (4 bits: beside each operand tile), then Shared.
@@ -109,17 +106,19 @@ struct Layout {
     static constexpr int kTileBytes = kKeys * D * 2;
     static constexpr int kBoxBytes = kKeys * 128;                      // 64 elements of a tile's rows
     static constexpr int kRowBytes = KV == BAKLAVA_KV_BF16 ? 2 * D : KV == BAKLAVA_KV_FP8_E4M3 ? D : D / 2;   // of the slab
-    static constexpr int kRawBytes = kKeys * kRowBytes;
+    static constexpr int kHalf = kKeys / 2, kRawBytes = kHalf * kRowBytes;       // tiles come from quantised slabs in halves
     static constexpr int kTerms = KV == BAKLAVA_KV_INT4 ? 2 : 1;       // 16-bit terms of a query element
     static constexpr int kQTerm = R * kRows * D * 2, kQBytes = kTerms * kQTerm;
     static constexpr int kQBox = R * kRows * 128;
     static constexpr int kScaleBytes = KV == BAKLAVA_KV_INT4 ? kKeys * 8 : 0;
-    static constexpr int kSlots = kQuantised ? (R == 2 || KV == BAKLAVA_KV_INT4 ? 3 : 4) : D == 128 ? (R == 2 ? 4 : 5) : R == 2 ? 10 : 12;
-    static constexpr int kRawSlots = !kQuantised ? 0 : KV == BAKLAVA_KV_INT4 ? 6 : 3;
+    static constexpr int kSlots = kQuantised ? (KV == BAKLAVA_KV_INT4 ? 3 : 4) : D == 128 ? (R == 2 ? 4 : 5) : R == 2 ? 10 : 12;
+    static constexpr int kRawSlots = !kQuantised ? 0 : KV == BAKLAVA_KV_INT4 ? 12 : R == 2 ? 3 : 7;
     static constexpr int kRing = kQBytes, kScales = kRing + kSlots * kTileBytes, kRaw = kScales + kSlots * kScaleBytes;
     static constexpr int kShared = kRaw + kRawSlots * kRawBytes;
-    static constexpr int kTotal = kShared + kSharedBytes;
+    static constexpr int kTotal = kShared + (KV == BAKLAVA_KV_INT4 ? (int)sizeof(Shared) : kSharedBytes);
     static constexpr int kThreads = (kConvertWarp0 + (kQuantised ? kConvertWarps : 0)) * 32;
+    // (registers for more threads than there are: a block of the second kernel has room beside this one's)
+    static constexpr int kRegisterThreads = kQuantised ? kThreads : 608;
     static constexpr bool kLoadsQ = !kQuantised;                       // the queries come by TMA
     // Tensor memory: buffers of 128 logits (the probabilities take their place), O behind them.  One accumulator leaves room for
     // three buffers: the softmax warps find the next logits formed when they are through with a tile.
@@ -262,12 +261,18 @@ __device__ __forceinline__ bool load_entry(const TreeParams& p, Shared& sm, cons
     const bool value = entry_is_value<R, kMode>(e, it.tiles, t);
     const uint32_t n = base + e;
     if constexpr (L::kQuantised) {
-        const uint32_t slot = n % L::kRawSlots, bar = ptx::smem_u32(&sm.raw_full[slot]);
-        if (!ptx::mbar_wait(ptx::smem_u32(&sm.raw_empty[slot]), (n / L::kRawSlots & 1) ^ 1)) return false;
-        const uint32_t bytes = min(kKeys, it.keys - t * kKeys) * L::kRowBytes;
-        ptx::mbar_arrive_expect_tx(bar, bytes);
-        bulk_load(cta.base + L::kRaw + slot * L::kRawBytes,
-                  static_cast<const uint8_t*>(value ? p.c.v : p.c.k) + ((int64_t)it.first + t * kKeys) * L::kRowBytes, bytes, bar);
+        for (int half = 0; half < 2; ++half) {
+            const uint32_t m = 2 * n + half, slot = m % L::kRawSlots, bar = ptx::smem_u32(&sm.raw_full[slot]);
+            if (!ptx::mbar_wait(ptx::smem_u32(&sm.raw_empty[slot]), (m / L::kRawSlots & 1) ^ 1)) return false;
+            const int row0 = t * kKeys + half * L::kHalf, bytes = max(0, min(L::kHalf, it.keys - row0)) * L::kRowBytes;
+            if (bytes == 0) {
+                tc::mbar_arrive(bar);
+                continue;
+            }
+            ptx::mbar_arrive_expect_tx(bar, bytes);
+            bulk_load(cta.base + L::kRaw + slot * L::kRawBytes,
+                      static_cast<const uint8_t*>(value ? p.c.v : p.c.k) + ((int64_t)it.first + row0) * L::kRowBytes, bytes, bar);
+        }
     } else {
         const uint32_t slot = n % L::kSlots, bar = ptx::smem_u32(&sm.full[slot]), dst = cta.base + L::kRing + slot * L::kTileBytes;
         if (!ptx::mbar_wait(ptx::smem_u32(&sm.empty[slot]), (n / L::kSlots & 1) ^ 1)) return false;
@@ -346,22 +351,24 @@ __device__ __forceinline__ bool convert_item(const TreeParams& p, Shared& sm, co
     for (int e = 0; e < entries; ++e) {
         int t;
         const bool value = entry_is_value<R, kMode>(e, it.tiles, t);
-        const uint32_t n = c.entry + e, slot = n % L::kSlots, raw = n % L::kRawSlots;
+        const uint32_t n = c.entry + e, slot = n % L::kSlots;
         const int keys = it.keys - t * kKeys, no_row = it.hole >= 0 ? it.hole - t * kKeys : -1;
         float2 scale = make_float2(0.0f, 0.0f);
         const int scale_row = w * 32 + lane;
         if (KV == BAKLAVA_KV_INT4 && value && scale_row < keys && scale_row != no_row)
             scale = *reinterpret_cast<const float2*>(p.c.row_scale + 2 * ((int64_t)it.first + t * kKeys + scale_row));
-        if (!ptx::mbar_wait(ptx::smem_u32(&sm.raw_full[raw]), n / L::kRawSlots & 1)) return false;
         if (!ptx::mbar_wait(ptx::smem_u32(&sm.empty[slot]), (n / L::kSlots & 1) ^ 1)) return false;
+        uint8_t* const to = cta.ptr + L::kRing + slot * L::kTileBytes;
+        for (int half = 0; half < 2; ++half) {
+        const uint32_t m = 2 * n + half, raw = m % L::kRawSlots;
+        if (!ptx::mbar_wait(ptx::smem_u32(&sm.raw_full[raw]), m / L::kRawSlots & 1)) return false;
         __syncwarp();
         const uint8_t* const from = cta.ptr + L::kRaw + raw * L::kRawBytes;
-        uint8_t* const to = cta.ptr + L::kRing + slot * L::kTileBytes;
 #pragma unroll
-        for (int i = 0; i < 32 / kStep; ++i) {                // a warp has 32 of the tile's rows
-            const int row = w * 32 + i * kStep + lane / kLanes;
+        for (int i = 0; i < 16 / kStep; ++i) {                // a warp has sixteen of a half's rows
+            const int of_half = w * 16 + i * kStep + lane / kLanes, row = half * L::kHalf + of_half;
             const bool here = row < keys && row != no_row;
-            uint4 x = *reinterpret_cast<const uint4*>(from + row * L::kRowBytes + piece * 16);
+            uint4 x = *reinterpret_cast<const uint4*>(from + of_half * L::kRowBytes + piece * 16);
             uint8_t* const at = to + row * 128;
             auto place = [&](int chunk) { return reinterpret_cast<uint4*>(at + (chunk >> 3) * L::kBoxBytes + (((chunk & 7) ^ (row & 7)) << 4)); };
             if (KV == BAKLAVA_KV_FP8_E4M3) {
@@ -401,14 +408,14 @@ __device__ __forceinline__ bool convert_item(const TreeParams& p, Shared& sm, co
                 for (int k = 0; k < 4; ++k) *place(4 * piece + (k ^ swap)) = swap ? y[k ^ 2] : y[k];
             }
         }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.raw_empty[raw]));
+        }
         if (KV == BAKLAVA_KV_INT4 && value)
             *reinterpret_cast<float2*>(cta.ptr + L::kScales + slot * L::kScaleBytes + scale_row * 8) = scale;
         tc::fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) {
-            tc::mbar_arrive(ptx::smem_u32(&sm.full[slot]));
-            tc::mbar_arrive(ptx::smem_u32(&sm.raw_empty[raw]));
-        }
+        if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.full[slot]));
     }
     c.entry += entries;
     return true;
@@ -552,10 +559,15 @@ __device__ __forceinline__ void place_queries(const TreeParams& p, const Cta& ct
     }
 }
 
+__device__ __forceinline__ float4 load_shared(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
+    return v;
+}
 // Sixteen logits -> eight columns of probabilities.  kMasked: keys first .. first + 15 of the tile, of which those at or
 // behind `keys` and `hole` are no rows.  4 bits: `scales` are the rows' (K, V) pairs; a probability takes its value row's scale.
 template <int KV, bool kMasked>
-__device__ __forceinline__ void softmax_16(uint32_t (&v)[16], uint32_t column, int first, int keys, int hole, const float4* scales,
+__device__ __forceinline__ void softmax_16(uint32_t (&v)[16], uint32_t column, int first, int keys, int hole, uint32_t scales,
                                            ptx::f32x2 scale2, ptx::f32x2 minus, ptx::f32x2 (&sum)[2]) {
     if (kMasked && KV != BAKLAVA_KV_INT4) {
 #pragma unroll
@@ -567,7 +579,7 @@ __device__ __forceinline__ void softmax_16(uint32_t (&v)[16], uint32_t column, i
     for (int c = 0; c < 8; ++c) {
         ptx::f32x2 s = ptx::pack2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1])), value2 = 0ull;
         if (KV == BAKLAVA_KV_INT4) {
-            const float4 of = scales[(first >> 1) + c];
+            const float4 of = load_shared(scales + 8 * first + 16 * c);
             s = ptx::mul2(s, ptx::pack2(of.x, of.z));
             value2 = ptx::pack2(of.y, of.w);
             if (kMasked) {
@@ -589,7 +601,7 @@ __device__ __forceinline__ void softmax_16(uint32_t (&v)[16], uint32_t column, i
 // A row's 128 logits of a tile: sixteen are asked for while the sixteen before are worked on.  Probabilities take the place
 // of logits that have been read.
 template <int KV, bool kMasked>
-__device__ __forceinline__ void softmax_row(uint32_t column, int keys, int hole, const float4* scales, float scale, float ref, ptx::f32x2 (&sum)[2]) {
+__device__ __forceinline__ void softmax_row(uint32_t column, int keys, int hole, uint32_t scales, float scale, float ref, ptx::f32x2 (&sum)[2]) {
     const ptx::f32x2 scale2 = ptx::pack2(scale, scale), minus = ptx::pack2(-ref, -ref);
     uint32_t a[16], b[16];
     load_16(column, a);
@@ -631,12 +643,12 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
         const bool masked = keys < kKeys || (it.hole >= 0 && hole >= 0 && hole < kKeys);
         const int no_row = it.hole >= 0 ? hole : -1;
         const uint32_t entry = c.entry + value_entry<R>(t, it.tiles), slot = entry % L::kSlots;
-        const float4* const scales = reinterpret_cast<const float4*>(cta.ptr + L::kScales + slot * L::kScaleBytes);
+        const uint32_t scales = cta.base + L::kScales + slot * L::kScaleBytes;
         const uint32_t g = c.step + n, buffer = g % L::kBuffers, column = lane_addr + buffer * kKeys;
         if (!ptx::mbar_wait(ptx::smem_u32(&sm.s_full[buffer]), g / L::kBuffers & 1)) return false;
         if (KV == BAKLAVA_KV_INT4 && n == stream) {
             if (!ptx::mbar_wait(ptx::smem_u32(&sm.q_full[turn]), (c.work >> 1) & 1)) return false;
-            factor = sm.factor[turn][R == 2 ? stream : 0][row];
+            factor = sm.factor[turn][row];
         }
         if (kMode != kMaxima && (KV == BAKLAVA_KV_INT4 || (!L::kQuantised && masked && (R == 1 || stream == 0))))
             if (!ptx::mbar_wait(ptx::smem_u32(&sm.full[slot]), entry / L::kSlots & 1)) return false;
@@ -673,7 +685,7 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
                 for (int e = 0; e < 8; ++e)
                     if (e < keys && e != no_row) {
                         float s = __uint_as_float(v[e]);
-                        if (KV == BAKLAVA_KV_INT4) s *= reinterpret_cast<const float*>(scales)[2 * e];
+                        if (KV == BAKLAVA_KV_INT4) s *= e & 1 ? load_shared(scales + 16 * (e >> 1)).z : load_shared(scales + 16 * (e >> 1)).x;
                         top = fmaxf(top, s * factor);
                     }
                 ref = top == -INFINITY ? 0.0f : top;
@@ -730,7 +742,7 @@ __device__ __forceinline__ void lay_out_queries(const TreeParams& p, Shared& sm,
         const int full_row = acc * kRows + row;
         float factor = query_factor<D, R, KV>(p, it);
         place_queries<D, R, KV>(p, cta, it, Row(p, it, full_row), full_row, factor);
-        if (KV == BAKLAVA_KV_INT4) sm.factor[work & 1][acc][row] = factor;
+        if (KV == BAKLAVA_KV_INT4) sm.factor[work & 1][row] = factor;
     }
     tc::fence_proxy_async_smem();
     __syncwarp();
@@ -868,7 +880,7 @@ __device__ __noinline__ void redo_pass(const TreeParams& p, Shared& sm, const Ct
 }
 
 template <int D, int R, int KV>
-__global__ void __launch_bounds__(Layout<D, R, KV>::kThreads, 1) tree_tile_kernel(
+__global__ void __launch_bounds__(Layout<D, R, KV>::kRegisterThreads, 1) tree_tile_kernel(
         const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
         const __grid_constant__ CUtensorMap v_map) {
     using L = Layout<D, R, KV>;
@@ -989,129 +1001,195 @@ __device__ __forceinline__ float join_weight(float x, float ref, float top) {
     const float half = exp2f(0.5f * (ref - top));
     return x * half * half;
 }
-// One warp per node and query head.  First the node's ancestors, whose keys and values it reads itself: a partial like the
-// chunks'.  This part waits for nothing of the first kernel and runs beside it (blocks of 128 threads, small enough for the
-// registers that a tile kernel's block leaves).  Then the normaliser of everything, and the partials under their final weights,
-// which add up to one, so that averages of values near the end of the range do not overflow on the way.  Blocks of items that are
-// not a head's first have nothing to do.
+// One warp per node and query head, or four query heads of its group, which share the way up.  First the node's ancestors, from the tree's keys
+// and values in shared memory: logits, then a partial like the chunks'.  This part waits for nothing of the first kernel and runs
+// beside it (blocks of 128 threads, small enough for the registers that a tile kernel's block leaves).  Then the normaliser of
+// everything, and the partials under their final weights, which add up to one, so that averages of values near the end of the range do
+// not overflow on the way.  Blocks of items that are not a head's first have nothing to do.
 constexpr int kJoinWarps = 4;
-template <int D>
+__device__ __forceinline__ void warp_sums(float (&x)[1], int) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+}
+// four sums over the warp's lanes, each in every lane: lanes halve the values among them, then one value is summed per eight lanes
+__device__ __forceinline__ void warp_sums(float (&x)[4], int lane) {
+    const bool high = lane & 16, odd = lane & 8;
+    const float a = (high ? x[2] : x[0]) + __shfl_xor_sync(0xffffffffu, high ? x[0] : x[2], 16);
+    const float b = (high ? x[3] : x[1]) + __shfl_xor_sync(0xffffffffu, high ? x[1] : x[3], 16);
+    float y = (odd ? b : a) + __shfl_xor_sync(0xffffffffu, odd ? a : b, 8);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) x[h] = __shfl_sync(0xffffffffu, y, 8 * h);
+}
+// 16 bytes from global to shared memory, not waited for
+__device__ __forceinline__ void copy_16(void* to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
+}
+template <int kE>
+__device__ __forceinline__ void load_f32(const float* from, float (&x)[kE]) {
+    if (kE == 4) {
+        const float4 w = *reinterpret_cast<const float4*>(from);
+        x[0] = w.x; x[1] = w.y; x[kE - 2] = w.z; x[kE - 1] = w.w;
+    } else {
+        const float2 w = *reinterpret_cast<const float2*>(from);
+        x[0] = w.x; x[1] = w.y;
+    }
+}
+template <int D, int kHeads>
 __global__ void __launch_bounds__(kJoinWarps * 32, 5) tree_join_kernel(const __grid_constant__ TreeParams p) {
     constexpr int kE = D / 32;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
     const int4 item = p.items[blockIdx.x];
     const int pieces = item.w >> 16;
     if ((item.w & 0xffff) != 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y * kJoinWarps + warp;
-    if (row >= p.g * p.T) return;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const Unit u(p.c, p.layer, item.x);
-    const int a = row / p.T, i = row - a * p.T, y = u.h * p.g + a;
-    const int32_t* const parent = p.parent + (int64_t)u.b * p.T;
-    const int up0 = lane < p.T ? parent[lane] : -1, up1 = lane + 32 < p.T ? parent[lane + 32] : -1;
-    float q[kE], o[kE];
-    load_bf16<kE>(p.q + u.b * p.sq.seq + (int64_t)y * p.sq.head + i * p.sq.token, lane, q);
+    __nv_bfloat16* const keys = reinterpret_cast<__nv_bfloat16*>(smem_raw);
+    __nv_bfloat16* const vals = keys + p.T * D;
+    int* const parent = reinterpret_cast<int*>(vals + p.T * D);
+    for (int x = tid; x < p.T * (D / 8); x += kJoinWarps * 32) {
+        const int j = x / (D / 8), e = x % (D / 8) * 8;
+        copy_16(keys + j * D + e, p.k + u.b * p.sk.seq + (int64_t)u.h * p.sk.head + j * p.sk.token + e);
+        copy_16(vals + j * D + e, p.v + u.b * p.sv.seq + (int64_t)u.h * p.sv.head + j * p.sv.token + e);
+    }
+    if (tid < p.T) parent[tid] = p.parent[(int64_t)u.b * p.T + tid];
     const int n = nodes_of(p.n_nodes, u.b, p.T);
+    const int task = blockIdx.y * kJoinWarps + warp, sets = (p.g + kHeads - 1) / kHeads;
+    const int i = task / sets, a0 = (task - i * sets) * kHeads, heads = min(kHeads, p.g - a0);
+    float q[kHeads][kE], o[kHeads][kE];
+    if (i < p.T)
+#pragma unroll
+        for (int h = 0; h < kHeads; ++h)                      // (heads that are none: the last one's rows, not written)
+            load_bf16<kE>(p.q + u.b * p.sq.seq + (int64_t)(u.h * p.g + a0 + min(h, heads - 1)) * p.sq.head + i * p.sq.token, lane, q[h]);
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
     if (i >= n) return;
-    if (!__all_sync(0xffffffffu, (lane >= n || (up0 >= -1 && up0 < lane)) && (lane + 32 >= n || (up1 >= -1 && up1 < lane + 32)))) {
+    const bool fine = (lane >= n || (parent[lane] >= -1 && parent[lane] < lane)) &&
+                      (lane + 32 >= n || (parent[lane + 32] >= -1 && parent[lane + 32] < lane + 32));
+    if (!__all_sync(0xffffffffu, fine)) {
         if (lane == 0) atomicOr(p.c.status, BAKLAVA_STATUS_BAD_STATE);
         return;
     }
-    const __nv_bfloat16* const keys = p.k + u.b * p.sk.seq + (int64_t)u.h * p.sk.head;
-    const __nv_bfloat16* const vals = p.v + u.b * p.sv.seq + (int64_t)u.h * p.sv.head;
-    // the way up, four nodes at a time: reference six powers of two above the largest logit (64 values of any size stay in range)
-    float ref = -INFINITY, l = 0.0f;
+    // logits of the way up, log2 domain: lane d holds those of the d-th node, and of the one 32 further
+    float s[2][kHeads];
 #pragma unroll
-    for (int e = 0; e < kE; ++e) o[e] = 0.0f;
-    for (int j = i; j >= 0;) {
-        float k[4][kE], v[4][kE], s[4];
-        bool there[4];
+    for (int h = 0; h < kHeads; ++h) s[0][h] = s[1][h] = -INFINITY;
+    for (int j = i, d = 0; j >= 0; j = parent[j], ++d) {
+        float k[kE], x[kHeads];
+        load_bf16<kE>(keys + j * D, lane, k);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            there[c] = j >= 0;
-            const int at = there[c] ? j : i;                  // (behind the root: the node itself, not counted)
-            load_bf16<kE>(keys + at * p.sk.token, lane, k[c]);
-            load_bf16<kE>(vals + at * p.sv.token, lane, v[c]);
-            const int up = __shfl_sync(0xffffffffu, at < 32 ? up0 : up1, at & 31);
-            j = there[c] ? up : -1;
+        for (int h = 0; h < kHeads; ++h) {
+            x[h] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kE; ++e) x[h] = fmaf(q[h][e], k[e], x[h]);
         }
-        float top = ref;
+        warp_sums(x, lane);
+        if (lane == (d & 31))
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            s[c] = 0.0f;
+            for (int h = 0; h < kHeads; ++h) (d < 32 ? s[0][h] : s[1][h]) = x[h] * p.scale_log2;
+    }
+    // a partial of them: reference six powers of two above the largest logit (64 values of any size stay in range)
+    float ref[kHeads], l[kHeads];
 #pragma unroll
-            for (int e = 0; e < kE; ++e) s[c] = fmaf(q[e], k[c][e], s[c]);
-            s[c] = warp_sum(s[c]) * p.scale_log2;
-            if (there[c]) top = fmaxf(top, s[c] + 6.0f);
+    for (int h = 0; h < kHeads; ++h) {
+        float top = fmaxf(s[0][h], s[1][h]);
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+        ref[h] = top + 6.0f;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) s[k][h] = s[k][h] == -INFINITY ? 0.0f : exp2f(s[k][h] - ref[h]);
+        l[h] = s[0][h] + s[1][h];
+#pragma unroll
+        for (int e = 0; e < kE; ++e) o[h][e] = 0.0f;
+    }
+    warp_sums(l, lane);
+    for (int j = i, d = 0; j >= 0; j = parent[j], ++d) {
+        float v[kE];
+        load_bf16<kE>(vals + j * D, lane, v);
+#pragma unroll
+        for (int h = 0; h < kHeads; ++h) {
+            const float w = __shfl_sync(0xffffffffu, d < 32 ? s[0][h] : s[1][h], d & 31);
+#pragma unroll
+            for (int e = 0; e < kE; ++e) o[h][e] = fmaf(w, v[e], o[h][e]);
         }
-        const float was = ref == -INFINITY ? 0.0f : exp2f(ref - top);
-        l *= was;
-#pragma unroll
-        for (int e = 0; e < kE; ++e) o[e] *= was;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            if (!there[c]) continue;
-            const float w = s[c] == -INFINITY ? 0.0f : exp2f(s[c] - top);
-            l += w;
-#pragma unroll
-            for (int e = 0; e < kE; ++e) o[e] = fmaf(w, v[c][e], o[e]);
-        }
-        ref = top;
     }
     grid_dependency_wait();
-    const int64_t rows = (int64_t)p.g * p.T, first = (int64_t)blockIdx.x * rows + row;
+    const int64_t rows = (int64_t)p.g * p.T, first = (int64_t)blockIdx.x * rows + (int64_t)a0 * p.T + i;
+    // reference and sum of piece `lane` of each head; (a head of more than 32 pieces reads them again below)
+    float2 st[kHeads];
+    float top[kHeads], sum[kHeads];
     bool skipped = false;
-    float top = l > 0.0f ? ref + log2f(l) : l == 0.0f ? -INFINITY : l, sum = 0.0f;
-    const float2 mine = lane < pieces ? p.stats[first + lane * rows] : make_float2(-INFINITY, 0.0f);
-    for (int c = lane; c < pieces; c += 32) {
-        const float2 st = c < 32 ? mine : p.stats[first + c * rows];
-        skipped = skipped || st.y < 0.0f;
-        if (st.x != -INFINITY) top = fmaxf(top, st.x + log2f(st.y));
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h)
+        st[h] = lane < pieces ? p.stats[first + lane * rows + min(h, heads - 1) * p.T] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+        top[h] = l[h] > 0.0f ? ref[h] + log2f(l[h]) : l[h] == 0.0f ? -INFINITY : l[h];
+        for (int c = lane; c < pieces; c += 32) {
+            const float2 x = c < 32 ? st[h] : p.stats[first + c * rows + min(h, heads - 1) * p.T];
+            skipped = skipped || x.y < 0.0f;
+            if (x.x != -INFINITY) top[h] = fmaxf(top[h], x.x + log2f(x.y));
+        }
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], k));
+        sum[h] = 0.0f;
+        for (int c = lane; c < pieces; c += 32) {
+            const float2 x = c < 32 ? st[h] : p.stats[first + c * rows + min(h, heads - 1) * p.T];
+            if (x.x != -INFINITY) sum[h] += join_weight(x.y, x.x, top[h]);
+        }
     }
     if (__any_sync(0xffffffffu, skipped)) return;
+    warp_sums(sum, lane);
+    float inv[kHeads];
 #pragma unroll
-    for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-    for (int c = lane; c < pieces; c += 32) {
-        const float2 st = c < 32 ? mine : p.stats[first + c * rows];
-        if (st.x != -INFINITY) sum += join_weight(st.y, st.x, top);
+    for (int h = 0; h < kHeads; ++h) {
+        if (l[h] != 0.0f) sum[h] += join_weight(l[h], ref[h], top[h]);
+        inv[h] = 1.0f / sum[h];
+#pragma unroll
+        for (int e = 0; e < kE; ++e) o[h][e] = l[h] == 0.0f ? 0.0f : join_weight(o[h][e], ref[h], top[h]) * inv[h];
     }
-    sum = warp_sum(sum) + (l == 0.0f ? 0.0f : join_weight(l, ref, top));
-    const float inv = 1.0f / sum;
+    // weights as squares of their halves (see join_weight), lane c that of piece c; 0: no rows, its partial was not written
+    constexpr int kTogether = 8 / kHeads;                     // pieces whose partials are in flight together
+    const float* part[kHeads];
 #pragma unroll
-    for (int e = 0; e < kE; ++e) o[e] = l == 0.0f ? 0.0f : join_weight(o[e], ref, top) * inv;
-    for (int c0 = 0; c0 < pieces; c0 += 8) {
-        float x[8][kE], of[8];
+    for (int h = 0; h < kHeads; ++h) part[h] = p.partial + (first + min(h, heads - 1) * p.T) * D + kE * lane;
+    float half[kHeads];
+    for (int c0 = 0; c0 < pieces; c0 += kTogether) {
+        if ((c0 & 31) == 0) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int c = c0 + k;
-            of[k] = __shfl_sync(0xffffffffu, mine.x, c & 31);
-            if (c >= 32 && c < pieces) of[k] = p.stats[first + c * rows].x;
-            if (c >= pieces) of[k] = -INFINITY;
-#pragma unroll
-            for (int e = 0; e < kE; ++e) x[k][e] = 0.0f;
-            if (of[k] == -INFINITY) continue;                 // (no rows: its partial was not written)
-            const float* const part = p.partial + (first + c * rows) * D + kE * lane;
-            if (kE == 4) {
-                const float4 w = *reinterpret_cast<const float4*>(part);
-                x[k][0] = w.x; x[k][1] = w.y; x[k][kE - 2] = w.z; x[k][kE - 1] = w.w;
-            } else {
-                const float2 w = *reinterpret_cast<const float2*>(part);
-                x[k][0] = w.x; x[k][1] = w.y;
+            for (int h = 0; h < kHeads; ++h) {
+                if (c0 > 0) st[h] = c0 + lane < pieces ? p.stats[first + (c0 + lane) * rows + min(h, heads - 1) * p.T] : make_float2(-INFINITY, 0.0f);
+                half[h] = st[h].x == -INFINITY ? 0.0f : exp2f(0.5f * (st[h].x - top[h]));
             }
         }
+        float x[kTogether][kHeads][kE];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (of[k] == -INFINITY) continue;
+        for (int k = 0; k < kTogether; ++k)
 #pragma unroll
-            for (int e = 0; e < kE; ++e) o[e] += join_weight(x[k][e], of[k], top) * inv;
+            for (int h = 0; h < kHeads; ++h) load_f32<kE>(part[h] + min(c0 + k, pieces - 1) * rows * D, x[k][h]);
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k)
+#pragma unroll
+            for (int h = 0; h < kHeads; ++h) {
+                const float w = c0 + k < pieces ? __shfl_sync(0xffffffffu, half[h], (c0 + k) & 31) : 0.0f, last = w * inv[h];
+#pragma unroll
+                for (int e = 0; e < kE; ++e) o[h][e] = w == 0.0f ? o[h][e] : fmaf(x[k][h][e] * w, last, o[h][e]);
+            }
+    }
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+        if (h >= heads) break;
+        const int y = u.h * p.g + a0 + h;
+        __nv_bfloat16* const out = p.out + u.b * p.so.seq + (int64_t)y * p.so.head + i * p.so.token + kE * lane;
+        if (kE == 4) {
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(o[h][0], o[h][1]), hi = __floats2bfloat162_rn(o[h][kE - 2], o[h][kE - 1]);
+            *reinterpret_cast<uint2*>(out) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        } else {
+            *reinterpret_cast<__nv_bfloat162*>(out) = __floats2bfloat162_rn(o[h][0], o[h][1]);
         }
+        if (p.lse && lane == 0) p.lse[((int64_t)u.b * p.Hq + y) * p.T + i] = (top[h] + log2f(sum[h])) * kLn2;
     }
-    __nv_bfloat16* const out = p.out + u.b * p.so.seq + (int64_t)y * p.so.head + i * p.so.token + kE * lane;
-    if (kE == 4) {
-        const __nv_bfloat162 lo = __floats2bfloat162_rn(o[0], o[1]), hi = __floats2bfloat162_rn(o[kE - 2], o[kE - 1]);
-        *reinterpret_cast<uint2*>(out) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-    } else {
-        *reinterpret_cast<__nv_bfloat162*>(out) = __floats2bfloat162_rn(o[0], o[1]);
-    }
-    if (p.lse && lane == 0) p.lse[((int64_t)u.b * p.Hq + y) * p.T + i] = (top + log2f(sum)) * kLn2;
 }
 
 template <int D, int R, int KV>
@@ -1208,7 +1286,10 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_attn(
     else if (kv == BAKLAVA_KV_FP8_E4M3) e = two ? launch_tiles<128, 2, BAKLAVA_KV_FP8_E4M3>(p, n, qm, km, vm, s) : launch_tiles<128, 1, BAKLAVA_KV_FP8_E4M3>(p, n, qm, km, vm, s);
     else if (shape->D == 128) e = two ? launch_tiles<128, 2, BAKLAVA_KV_BF16>(p, n, qm, km, vm, s) : launch_tiles<128, 1, BAKLAVA_KV_BF16>(p, n, qm, km, vm, s);
     else e = two ? launch_tiles<64, 2, BAKLAVA_KV_BF16>(p, n, qm, km, vm, s) : launch_tiles<64, 1, BAKLAVA_KV_BF16>(p, n, qm, km, vm, s);
-    const dim3 join((unsigned)n, (unsigned)((p.g * T + kJoinWarps - 1) / kJoinWarps));
+    // few rows: a warp to each (16 nodes of 32 heads: 8 us, 17 us with four heads to a warp), many: four heads to a warp
+    const bool single = (int64_t)B * shape->Hq * T <= 8192;
+    const int tasks = T * (single ? p.g : (p.g + 3) / 4);
+    const dim3 join((unsigned)n, (unsigned)((tasks + kJoinWarps - 1) / kJoinWarps));
     if (e == cudaSuccess) {
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1216,10 +1297,12 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_attn(
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = join;
         cfg.blockDim = dim3(kJoinWarps * 32);
+        cfg.dynamicSmemBytes = T * shape->D * 4 + BAKLAVA_MAX_TREE * 4;
         cfg.stream = s;
         cfg.attrs = attr;
         cfg.numAttrs = 1;
-        e = shape->D == 128 ? cudaLaunchKernelEx(&cfg, tree_join_kernel<128>, p) : cudaLaunchKernelEx(&cfg, tree_join_kernel<64>, p);
+        if (shape->D == 128) e = single ? cudaLaunchKernelEx(&cfg, tree_join_kernel<128, 1>, p) : cudaLaunchKernelEx(&cfg, tree_join_kernel<128, 4>, p);
+        else e = single ? cudaLaunchKernelEx(&cfg, tree_join_kernel<64, 1>, p) : cudaLaunchKernelEx(&cfg, tree_join_kernel<64, 4>, p);
     }
     return e == cudaSuccess ? BAKLAVA_OK : BAKLAVA_ERR_CUDA;
 }
