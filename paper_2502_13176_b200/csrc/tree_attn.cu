@@ -91,6 +91,7 @@ struct Shared {
     uint32_t tmem_slot;
     int abort;
     int finished;                             // items that are done with, counted by each row warp
+    int loaded;                               // items whose last tile has been asked for
     // of two items in turn: the rows' references (R = 1: only [.][0]), the streams' sums, 4 bits: the queries' factors
     float ref[2][2][kRows], part[2][2][kRows];
     float factor[2][kRows];                   // (at the end: only where queries have factors is there room for it)
@@ -126,10 +127,11 @@ struct Layout {
     static constexpr uint32_t kOColumn = kBuffers * kKeys;
     static_assert(kTotal <= 232448, "one CTA's shared memory");
     static_assert(R == 1 || KV != BAKLAVA_KV_INT4, "two rows' blocks of queries in two terms leave no room");
-    // fp16 operands: keys of quantised slabs (whose codes are exact in fp16) with their queries, FP8 values
+    // Keys of quantised slabs, whose codes are exact in it, and their queries are fp16 operands.  Probabilities and values are
+    // bf16: the codes are exact there too, and a probability may be far above one (see the reference in soften_item).
     static constexpr uint32_t kBf16 = (1u << 7) | (1u << 10);
     static constexpr uint32_t kIdescS = tc::idesc_bf16_f32(kRows, kKeys) & ~(kQuantised ? kBf16 : 0u);
-    static constexpr uint32_t kIdescPv = tc::idesc_bf16_f32_b_mn(kRows, D) & ~(KV == BAKLAVA_KV_FP8_E4M3 ? kBf16 : 0u);
+    static constexpr uint32_t kIdescPv = tc::idesc_bf16_f32_b_mn(kRows, D);
 };
 
 __device__ __forceinline__ void request_block(uint32_t answer, uint32_t bar) {
@@ -151,14 +153,31 @@ __device__ __forceinline__ bool granted_block(uint32_t answer, uint32_t& x) {
         : "=r"(got), "=r"(x) : "r"(answer) : "memory");
     return got != 0;
 }
+// Slab rows are read once (by one block, where a group is not divided) and pass L2 by: what the launch writes, the partials,
+// stays there until it is read.
+__device__ __forceinline__ uint64_t l2_policy(bool once) {
+    uint64_t policy;
+    if (once) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+    else asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
+    return policy;
+}
 // untiled copy of `bytes` (a multiple of 16) to shared memory
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint64_t policy) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %4}], [%5], %6;"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(0), "r"(bar), "l"(policy) : "memory");
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t f16_pair) {       // (codes: exact)
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&f16_pair));
+    return pack_bf16(f.x, f.y);
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
@@ -260,6 +279,7 @@ __device__ __forceinline__ bool load_entry(const TreeParams& p, Shared& sm, cons
     int t;
     const bool value = entry_is_value<R, kMode>(e, it.tiles, t);
     const uint32_t n = base + e;
+    const uint64_t policy = l2_policy(p.parts == 1);
     if constexpr (L::kQuantised) {
         for (int half = 0; half < 2; ++half) {
             const uint32_t m = 2 * n + half, slot = m % L::kRawSlots, bar = ptx::smem_u32(&sm.raw_full[slot]);
@@ -271,7 +291,7 @@ __device__ __forceinline__ bool load_entry(const TreeParams& p, Shared& sm, cons
             }
             ptx::mbar_arrive_expect_tx(bar, bytes);
             bulk_load(cta.base + L::kRaw + slot * L::kRawBytes,
-                      static_cast<const uint8_t*>(value ? p.c.v : p.c.k) + ((int64_t)it.first + row0) * L::kRowBytes, bytes, bar);
+                      static_cast<const uint8_t*>(value ? p.c.v : p.c.k) + ((int64_t)it.first + row0) * L::kRowBytes, bytes, bar, policy);
         }
     } else {
         const uint32_t slot = n % L::kSlots, bar = ptx::smem_u32(&sm.full[slot]), dst = cta.base + L::kRing + slot * L::kTileBytes;
@@ -279,7 +299,7 @@ __device__ __forceinline__ bool load_entry(const TreeParams& p, Shared& sm, cons
         ptx::mbar_arrive_expect_tx(bar, L::kTileBytes);
 #pragma unroll
         for (int bx = 0; bx < D / 64; ++bx)
-            ptx::tma_load_4d(dst + bx * L::kBoxBytes, value ? &v_map : &k_map, bx * 64, it.first + t * kKeys, 0, 0, bar);
+            tile_load(dst + bx * L::kBoxBytes, value ? &v_map : &k_map, bx * 64, it.first + t * kKeys, bar, policy);
     }
     return true;
 }
@@ -309,14 +329,15 @@ __device__ __forceinline__ bool produce_item(const TreeParams& p, Shared& sm, co
     return true;
 }
 // Looks for the CTA's further items and hands them to all roles; those without work are done with here.  Item j + 1 is asked
-// for when item j - 2 is done with, so that at most three are under way.
+// for when the last tile of item j has been, not sooner (what a CTA holds no other can take: claiming two items ahead cost a
+// fifth of a launch of three items to a CTA), and when item j - 2 is done with, so that at most three are under way.
 __device__ __forceinline__ void scout(const TreeParams& p, Shared& sm) {
     const uint32_t answer = ptx::smem_u32(&sm.answer), bar_answer = ptx::smem_u32(&sm.bar_answer);
     uint32_t asked = 0;
     bool ok = true;
     for (int j = 0; ok; ++j) {
         const long long t0 = clock64();
-        while (ok && *(volatile int*)&sm.finished < kRowWarps * (j - 1)) ok = clock64() - t0 < ptx::kWaitCycles && !*(volatile int*)&sm.abort;
+        while (ok && (*(volatile int*)&sm.loaded <= j || *(volatile int*)&sm.finished < kRowWarps * (j - 1))) ok = clock64() - t0 < ptx::kWaitCycles && !*(volatile int*)&sm.abort;
         if (!ok) break;
         Item next;
         next.index = -1;
@@ -338,7 +359,7 @@ __device__ __forceinline__ void scout(const TreeParams& p, Shared& sm) {
 }
 
 // ---------------------------------------------------------------- quantised rows into operand tiles
-// A lane takes 16 bytes of a row.  FP8: 16 codes, 32 bytes of fp16.  4 bits: 32 codes, 64 bytes; a word's nibbles i and i + 4
+// A lane takes 16 bytes of a row.  FP8: 16 codes, 32 bytes of fp16 (keys) or bf16 (values).  4 bits: 32 codes, 64 bytes; a word's nibbles i and i + 4
 // make a pair, so that an operand's eight elements are dimensions 0, 4, 1, 5, 2, 6, 3, 7 of eight (queries and output rows are
 // ordered to match).  The pieces go to their places under the 128-byte swizzle, in an order that keeps eight lanes on
 // different banks.
@@ -378,6 +399,10 @@ __device__ __forceinline__ bool convert_item(const TreeParams& p, Shared& sm, co
                 fp8::f16x4_from_e4m3x4(x.y, y[0].z, y[0].w);
                 fp8::f16x4_from_e4m3x4(x.z, y[1].x, y[1].y);
                 fp8::f16x4_from_e4m3x4(x.w, y[1].z, y[1].w);
+                if (value) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) y[k] = make_uint4(bf16_pair(y[k].x), bf16_pair(y[k].y), bf16_pair(y[k].z), bf16_pair(y[k].w));
+                }
                 const int swap = piece >> 2;
                 *place(2 * piece + swap) = swap ? y[1] : y[0];
                 *place(2 * piece + 1 - swap) = swap ? y[0] : y[1];
@@ -594,7 +619,7 @@ __device__ __forceinline__ void softmax_16(uint32_t (&v)[16], uint32_t column, i
         sum[c & 1] = ptx::add2(sum[c & 1], prob);
         if (KV == BAKLAVA_KV_INT4) prob = ptx::mul2(prob, value2);
         const float2 f = ptx::unpack2(prob);
-        w[c] = KV == BAKLAVA_KV_FP8_E4M3 ? pack_f16(f.x, f.y) : pack_bf16(f.x, f.y);
+        w[c] = pack_bf16(f.x, f.y);
     }
     store_8(column, w);
 }
@@ -903,6 +928,7 @@ __global__ void __launch_bounds__(Layout<D, R, KV>::kRegisterThreads, 1) tree_ti
             sm.abort = cta.base & 1023u ? 1 : 0;              // (the tiles' swizzle needs it; the base is where it is)
             sm.redo_count = 0;
             sm.finished = 0;
+            sm.loaded = 0;
         }
         ptx::fence_mbar_init();
     } else if (warp == kMmaWarp) {
@@ -954,6 +980,7 @@ __global__ void __launch_bounds__(Layout<D, R, KV>::kRegisterThreads, 1) tree_ti
             if (lane == 0)
                 for (int k = 0; ok && it.index >= 0; ++k) {
                     if (it.tiles > 0) ok = produce_item<D, R, KV>(p, sm, cta, it, c, q_map, k_map, v_map);
+                    *(volatile int*)&sm.loaded = k + 1;
                     if (ok) ok = next_item(sm, k, it);
                 }
         } else if (warp == kMmaWarp) {
@@ -1266,7 +1293,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_attn(
     const int kv = cache->kv_dtype;
     p.rows_per_head = (T + 7) / 8 * 8;
     // query heads that the accumulators have room for: two, one where queries have two terms
-    const int most = (kv == BAKLAVA_KV_INT4 ? 1 : 2) * kRows / p.rows_per_head;
+    const int accs = kv == BAKLAVA_KV_INT4 ? 1 : kv == BAKLAVA_KV_BF16 && info->n_items <= 2 * 148 ? 1 : 2, most = accs * kRows / p.rows_per_head;
     p.parts = (p.g + most - 1) / most;
     p.heads = (p.g + p.parts - 1) / p.parts;
     p.scale_log2 = kLog2e / sqrtf((float)shape->D);
