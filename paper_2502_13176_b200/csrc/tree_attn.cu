@@ -584,9 +584,16 @@ __device__ __forceinline__ void place_queries(const TreeParams& p, const Cta& ct
     }
 }
 
+// a zero that is made here: what is computed from it is not moved in front of the waits above
+__device__ __forceinline__ uint32_t behind_waits() {
+    uint32_t zero;
+    asm volatile("mov.u32 %0, 0;" : "=r"(zero) :: "memory");
+    return zero;
+}
+// (not volatile, so that loads are issued ahead of the arithmetic that needs them; `at` comes from behind_waits())
 __device__ __forceinline__ float4 load_shared(uint32_t at) {
     float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
+    asm("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
     return v;
 }
 // Sixteen logits -> eight columns of probabilities.  kMasked: keys first .. first + 15 of the tile, of which those at or
@@ -668,7 +675,6 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
         const bool masked = keys < kKeys || (it.hole >= 0 && hole >= 0 && hole < kKeys);
         const int no_row = it.hole >= 0 ? hole : -1;
         const uint32_t entry = c.entry + value_entry<R>(t, it.tiles), slot = entry % L::kSlots;
-        const uint32_t scales = cta.base + L::kScales + slot * L::kScaleBytes;
         const uint32_t g = c.step + n, buffer = g % L::kBuffers, column = lane_addr + buffer * kKeys;
         if (!ptx::mbar_wait(ptx::smem_u32(&sm.s_full[buffer]), g / L::kBuffers & 1)) return false;
         if (KV == BAKLAVA_KV_INT4 && n == stream) {
@@ -679,6 +685,7 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
             if (!ptx::mbar_wait(ptx::smem_u32(&sm.full[slot]), entry / L::kSlots & 1)) return false;
         __syncwarp();
         tc::fence_after_sync();
+        const uint32_t scales = KV == BAKLAVA_KV_INT4 ? cta.base + L::kScales + slot * L::kScaleBytes + behind_waits() : 0u;
         if (kMode == kMaxima) {
             if (busy) {
 #pragma unroll 1

@@ -22,6 +22,19 @@ def norm_rope(shape, q, k, positions, inv_freq, q_weight=None, k_weight=None, ep
     return qo, ko
 
 
+def verify(target, draft, tokens, parent, u_accept, u_sample, n_nodes=None, distinct=False):
+    """Which drafted tokens stand (speculative sampling over a tree, from given uniform numbers).  target, draft: float32 or
+    bf16 [B, T, V] probabilities (draft None: the children were chosen, not drawn); tokens, parent: int32 [B, T]; u_accept:
+    float32 [B, T], u_sample: float32 [B]; `distinct`: siblings were drawn without replacement.  Returns device tensors (path
+    [B, T], n_path [B], next_token [B], status [1]), as `DecodeSession.commit` takes the first two."""
+    B, T, _ = target.shape
+    path, rest = torch.empty((B, T), dtype=torch.int32, device=target.device), torch.zeros((2 * B + 1,), dtype=torch.int32, device=target.device)
+    n_path, token, status = rest[:B], rest[B:2 * B], rest[2 * B:]
+    bk.baklava_tree_verify(target, draft, tokens, parent, n_nodes, u_accept, u_sample, path, n_path, token, status,
+                           bk.VERIFY_DISTINCT if distinct else 0)
+    return path, n_path, token, status
+
+
 class DecodeSession:
     def __init__(self, w, device="cuda", layers=None, chunk_tokens=0, uniform=False, alloc=None, importance=None,
                  total_tokens=None, kv_dtype=bk.KV_BF16):
@@ -133,6 +146,41 @@ class DecodeSession:
             bk.baklava_decode_attn_varlen(self.shape, self.cache, q[i:i + 1], k_new[i:i + 1], v_new[i:i + 1], t_pos,
                                           self.out[i:i + 1], self.lse[i:i + 1], fl, plan, ws)
         return self.out
+
+    def drafts(self, T, max_path=None):
+        """Room for steps with trees of up to T drafted tokens, accepted paths of up to `max_path` (T): the nodes' queries, keys
+        and values of every layer (`tree_q` [layers, B, Hq, T, D], `tree_k`, `tree_v` [layers, B, Hkv, T, D]: the model writes
+        them, e.g. through baklava_qk_norm_rope), outputs, log-sum-exps, one plan per layer, workspaces."""
+        w, nl = self.w, self.le - self.lb
+        n_sm = torch.cuda.get_device_properties(self.device).multi_processor_count
+        bf = dict(dtype=torch.bfloat16, device=self.device)
+        self.tree_T, self.max_path = T, T if max_path is None else max_path
+        self.tree_q, self.tree_out = (torch.zeros((nl, w.B, w.Hq, T, w.D), **bf) for _ in range(2))
+        self.tree_k, self.tree_v = (torch.zeros((nl, w.B, w.Hkv, T, w.D), **bf) for _ in range(2))
+        self.tree_lse = torch.zeros((nl, w.B, w.Hq, T), dtype=torch.float32, device=self.device)
+        self.tree_plans = [bk.baklava_tree_plan(self.shape, self.cap, w.B, l, T, n_sm=n_sm, kv_dtype=self.kv_dtype).to(self.device)
+                           for l in range(self.lb, self.le)]
+        # (the layers follow one another on the stream and share a workspace)
+        self.tree_ws = torch.empty((max(int(p.info.ws_bytes) for p in self.tree_plans),), dtype=torch.uint8, device=self.device)
+        self.commit_ws = bk.tree_commit_workspace(self.shape, self.plan, self.max_path, self.device)
+
+    def tree_layer(self, l, parent, n_nodes=None):
+        """Attention of the drafted tree over layer l's slabs and over the nodes' ancestors; returns [B, Hq, T, D].  parent:
+        device int32 [B, T]; n_nodes: device int32 [B] or None."""
+        if not self.lb <= l < self.le:
+            raise ValueError("layer %d of %d .. %d" % (l, self.lb, self.le - 1))
+        i = l - self.lb
+        bk.baklava_tree_attn(self.shape, self.cache, self.tree_q[i], self.tree_k[i], self.tree_v[i], parent, n_nodes, self.tree_out[i],
+                             self.tree_lse[i], self.tree_plans[i], self.tree_ws)
+        return self.tree_out[i]
+
+    def commit(self, path, n_path, t_pos, flags=0):
+        """The accepted path (as `verify` returned it) into all layers' slabs: scores, append, eviction.  t_pos: device int32 [B],
+        the position of each path's first token; returns the next step's."""
+        t_next = torch.empty_like(t_pos)
+        bk.baklava_tree_commit(self.shape, self.cache, self.tree_q, self.tree_k, self.tree_v, self.tree_lse, path, n_path, self.max_path,
+                               t_pos, t_next, flags, self.plan, self.commit_ws)
+        return t_next
 
     def retained_kv_bytes(self):
         """Bytes of K and V in valid rows of the session's layers: what one step must read."""
