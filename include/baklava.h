@@ -491,6 +491,14 @@ int baklava_tree_commit(const baklava_shape* shape, const baklava_cache* cache, 
                         const baklava_plan_info* info, void* ws, size_t ws_bytes, void* stream);
 size_t baklava_tree_commit_workspace_size(const baklava_shape* shape, const baklava_plan_info* info, int32_t max_path);
 
+/* The three calls above from one array of 64-bit words, their arguments in order, pointers as integers and each
+ * baklava_strides as its three numbers: for bindings that pay for every argument of a foreign call (ctypes: 2 of the 15 us that
+ * a verification takes on the host).  `words` has to be their exact number; the result is the call's own. */
+#define BAKLAVA_CALL_TREE_ATTN     0    /* 27 words */
+#define BAKLAVA_CALL_TREE_VERIFY   1    /* 19 words */
+#define BAKLAVA_CALL_TREE_COMMIT   2    /* 18 words */
+int baklava_tree_call(int32_t call, const int64_t* args, int32_t words);
+
 /* ------------------------------------------------------------------ prompt scores (seed of step 3)
  * The accumulated attention a prompt leaves on its own tokens, for ONE layer: with the causal
  * attention matrix A_h = softmax(Q_h K^T / sqrt(D)) of Eq. 1,

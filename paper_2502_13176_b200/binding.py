@@ -8,6 +8,7 @@ first call raises: there is no other path.
 import ctypes
 import functools
 import os
+import struct
 from ctypes import POINTER, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 
 import numpy as np
@@ -116,6 +117,7 @@ def lib():
             c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_uint32, c_void_p, POINTER(PlanInfo), c_void_p, c_size_t, c_void_p]
         L.baklava_tree_commit_workspace_size.restype = c_size_t
         L.baklava_tree_commit_workspace_size.argtypes = [POINTER(Shape), POINTER(PlanInfo), c_int32]
+        L.baklava_tree_call.argtypes = [c_int32, c_char_p, c_int32]
         L.baklava_output_error.argtypes = [c_void_p, c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
         L.baklava_output_error_workspace_size.restype = c_size_t
         L.baklava_output_error_workspace_size.argtypes = [c_int64]
@@ -348,6 +350,8 @@ def baklava_prefill_scores(shape, q, k, prompt_len, B, T, score, ws, stream=None
 
 
 def _device():
+    if torch.cuda._initialized:                      # (the two calls below take a microsecond)
+        return torch._C._cuda_getDevice()
     return torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else -2   # -2: none
 
 
@@ -378,11 +382,11 @@ def _dense(t, what, dev, dtype, shape):
     """Pointer of a contiguous tensor, NULL for None."""
     if t is None:
         return None
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: expected a contiguous %s tensor %s, got %s %s" % (what, dtype, shape, t.dtype, tuple(t.shape)))
-    if t.get_device() != dev:
-        _elsewhere(t, what, dev)
-    return t.data_ptr()
+    _elsewhere(t, what, dev)
 
 
 def baklava_qk_norm_rope(shape, q, k, positions, inv_freq, q_weight, k_weight, eps, q_out, k_out, flags=0, stream=None):
@@ -445,10 +449,33 @@ def baklava_tree_plan(shape, cap, B, layer, T, chunk_tokens=0, n_sm=148, kv_dtyp
     return Plan(items, info)
 
 
+_address = ctypes.addressof
+_words = {n: struct.Struct("%dq" % n).pack for n in (18, 19, 27)}
+_CALL_ATTN, _CALL_VERIFY, _CALL_COMMIT = 0, 1, 2
+_I32, _F32 = torch.int32, torch.float32
+
+
+def _tree_call(call, what, *args):
+    n = len(args)
+    rc = lib().baklava_tree_call(call, _words[n](*args), n)
+    if rc != OK:
+        raise BaklavaError(rc, what)
+
+
+def _row_words(t, what, dev, shape):
+    """Pointer and strides of a bf16 tensor [seqs, heads, tokens, D] (any view whose last dimension is contiguous)."""
+    st = t.stride()
+    if t.dtype is _BF16 and t.shape == shape and st[3] == 1 and t.get_device() == dev:
+        return t.data_ptr(), st[0], st[1], st[2]
+    _rows(t, what, dev, shape)
+    return t.data_ptr(), st[0], st[1], st[2]
+
+
 def _planned(plan, dev):
-    if plan.items_dev is None or plan.items_dev.get_device() != dev:
+    items = plan.items_dev
+    if items is None or items.get_device() != dev:
         raise ValueError("the plan's items are not on the current device (Plan.to)")
-    return plan.items_dev.data_ptr()
+    return items.data_ptr(), _address(plan.info)
 
 
 def _workspace(ws, dev):
@@ -464,53 +491,52 @@ def _cache_here(cache, B, dev):
         raise ValueError("the cache holds %d sequences, the tensors %d" % (cache.B, B))
     if cache.k_slab.get_device() != dev:
         _elsewhere(cache.k_slab, "the cache", dev)
+    return _address(cache.struct)
 
 
 def baklava_tree_attn(shape, cache, q, k, v, parent, n_nodes, out, lse, plan, ws, stream=None):
     """q, out: bf16 [B, Hq, T, D], k, v: bf16 [B, Hkv, T, D], any views with contiguous rows; parent: int32 [B, T]; n_nodes:
     int32 [B] or None; lse: float32 [B, Hq, T] or None; plan: baklava_tree_plan's for the layer."""
-    B, _, T, _ = q.shape
+    B, Hq, T, _ = q.shape
     D = shape.D
     dev = _device()
     queries, keys = (B, shape.Hq, T, D), (B, shape.Hkv, T, D)
-    _cache_here(cache, B, dev)
-    _check(lib().baklava_tree_attn(shape, ctypes.byref(cache.struct), *_rows(q, "q", dev, queries), *_rows(k, "k", dev, keys),
-                                   *_rows(v, "v", dev, keys), _dense(parent, "parent", dev, torch.int32, (B, T)),
-                                   _dense(n_nodes, "n_nodes", dev, torch.int32, (B,)), T, *_rows(out, "out", dev, queries),
-                                   _dense(lse, "lse", dev, torch.float32, queries[:3]), _planned(plan, dev),
-                                   ctypes.byref(plan.info), *_workspace(ws, dev), _stream(stream, dev)), "baklava_tree_attn")
+    _tree_call(_CALL_ATTN, "baklava_tree_attn", _address(shape), _cache_here(cache, B, dev), *_row_words(q, "q", dev, queries),
+               *_row_words(k, "k", dev, keys), *_row_words(v, "v", dev, keys), _dense(parent, "parent", dev, _I32, (B, T)),
+               _dense(n_nodes, "n_nodes", dev, _I32, (B,)) or 0, T, *_row_words(out, "out", dev, queries),
+               _dense(lse, "lse", dev, _F32, (B, Hq, T)) or 0, *_planned(plan, dev), *_workspace(ws, dev), _stream(stream, dev))
 
 
 def _probabilities(t, what, dev, shape, dtype):
     """Pointer and row stride of probabilities [B, T, V]: rows contiguous, all the same distance apart."""
-    B, T, _ = shape
+    B, T, V = shape
     st = t.stride()
     row = st[1] if T > 1 else st[0]
-    if t.dtype is not dtype or t.shape != shape or st[2] != 1 and shape[2] > 1 or B > 1 and T > 1 and st[0] != T * st[1]:
+    if t.dtype is not dtype or t.shape != shape or st[2] != 1 and V > 1 or B > 1 and T > 1 and st[0] != T * st[1]:
         raise ValueError("%s: expected %s [%d, %d, %d] with contiguous rows at one distance, got %s %s with strides %s"
-                         % ((what, dtype) + tuple(shape) + (t.dtype, tuple(t.shape), st)))
+                         % (what, dtype, B, T, V, t.dtype, tuple(t.shape), st))
     if t.get_device() != dev:
         _elsewhere(t, what, dev)
-    return t.data_ptr(), max(row, shape[2])
+    return t.data_ptr(), row if row > V else V
 
 
 def baklava_tree_verify(target, draft, tokens, parent, n_nodes, u_accept, u_sample, path, n_path, next_token, status, flags=0,
                         stream=None):
     """target: float32 or bf16 [B, T, V]; draft: the same or None; tokens, parent, path: int32 [B, T]; n_nodes, n_path,
     next_token: int32 [B] (n_nodes may be None); u_accept: float32 [B, T]; u_sample: float32 [B]; status: int32 [1]."""
-    B, T, V = target.shape
+    probs, kind = target.shape, target.dtype
+    B, T, V = probs
     dev = _device()
-    if target.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError("target: expected float32 or bfloat16, got %s" % target.dtype)
-    i32, f32 = torch.int32, torch.float32
-    _check(lib().baklava_tree_verify(*_probabilities(target, "target", dev, target.shape, target.dtype),
-                                     *((None, 0) if draft is None else _probabilities(draft, "draft", dev, target.shape, target.dtype)),
-                                     PROB_F32 if target.dtype is f32 else PROB_BF16, _dense(tokens, "tokens", dev, i32, (B, T)),
-                                     _dense(parent, "parent", dev, i32, (B, T)), _dense(n_nodes, "n_nodes", dev, i32, (B,)), B, T, V,
-                                     _dense(u_accept, "u_accept", dev, f32, (B, T)), _dense(u_sample, "u_sample", dev, f32, (B,)),
-                                     flags, _dense(path, "path", dev, i32, (B, T)), _dense(n_path, "n_path", dev, i32, (B,)),
-                                     _dense(next_token, "next_token", dev, i32, (B,)), _dense(status, "status", dev, i32, (1,)),
-                                     _stream(stream, dev)), "baklava_tree_verify")
+    if kind is not _F32 and kind is not _BF16:
+        raise ValueError("target: expected float32 or bfloat16, got %s" % kind)
+    per_node, per_seq = (B, T), (B,)
+    _tree_call(_CALL_VERIFY, "baklava_tree_verify", *_probabilities(target, "target", dev, probs, kind),
+               *((0, 0) if draft is None else _probabilities(draft, "draft", dev, probs, kind)), PROB_F32 if kind is _F32 else PROB_BF16,
+               _dense(tokens, "tokens", dev, _I32, per_node), _dense(parent, "parent", dev, _I32, per_node),
+               _dense(n_nodes, "n_nodes", dev, _I32, per_seq) or 0, B, T, V, _dense(u_accept, "u_accept", dev, _F32, per_node),
+               _dense(u_sample, "u_sample", dev, _F32, per_seq), flags, _dense(path, "path", dev, _I32, per_node),
+               _dense(n_path, "n_path", dev, _I32, per_seq), _dense(next_token, "next_token", dev, _I32, per_seq),
+               _dense(status, "status", dev, _I32, (1,)), _stream(stream, dev))
 
 
 def tree_commit_workspace(shape, plan, max_path, device="cuda"):
@@ -523,18 +549,15 @@ def baklava_tree_commit(shape, cache, q, k, v, lse, path, n_path, max_path, t_po
     may be None with FLAG_NO_SCORE); path: int32 [B, T]; n_path, t_pos, t_next: int32 [B] (t_next may be None); plan: one of
     baklava_decode_plan for the layers; ws: tree_commit_workspace."""
     n, B, _, T, _ = k.shape
-    dev, i32 = _device(), torch.int32
-    if n != plan.info.layer_end - plan.info.layer_begin:
-        raise ValueError("k has %d layers, the plan %d" % (n, plan.info.layer_end - plan.info.layer_begin))
-    _cache_here(cache, B, dev)
-    keys = (n, B, shape.Hkv, T, shape.D)
-    _check(lib().baklava_tree_commit(shape, ctypes.byref(cache.struct), _dense(q, "q", dev, _BF16, (n, B, shape.Hq, T, shape.D)),
-                                     _dense(k, "k", dev, _BF16, keys), _dense(v, "v", dev, _BF16, keys),
-                                     _dense(lse, "lse", dev, torch.float32, (n, B, shape.Hq, T)), T,
-                                     _dense(path, "path", dev, i32, (B, T)), _dense(n_path, "n_path", dev, i32, (B,)), max_path,
-                                     _dense(t_pos, "t_pos", dev, i32, (B,)), _dense(t_next, "t_next", dev, i32, (B,)), flags,
-                                     _planned(plan, dev), ctypes.byref(plan.info), *_workspace(ws, dev), _stream(stream, dev)),
-           "baklava_tree_commit")
+    dev, info = _device(), plan.info
+    if n != info.layer_end - info.layer_begin:
+        raise ValueError("k has %d layers, the plan %d" % (n, info.layer_end - info.layer_begin))
+    Hq, keys = shape.Hq, (n, B, shape.Hkv, T, shape.D)
+    _tree_call(_CALL_COMMIT, "baklava_tree_commit", _address(shape), _cache_here(cache, B, dev),
+               _dense(q, "q", dev, _BF16, (n, B, Hq, T, shape.D)) or 0, _dense(k, "k", dev, _BF16, keys), _dense(v, "v", dev, _BF16, keys),
+               _dense(lse, "lse", dev, _F32, (n, B, Hq, T)) or 0, T, _dense(path, "path", dev, _I32, (B, T)),
+               _dense(n_path, "n_path", dev, _I32, (B,)), max_path, _dense(t_pos, "t_pos", dev, _I32, (B,)),
+               _dense(t_next, "t_next", dev, _I32, (B,)) or 0, flags, *_planned(plan, dev), *_workspace(ws, dev), _stream(stream, dev))
 
 
 def baklava_output_error(out, ref, loss, ws, stream=None):

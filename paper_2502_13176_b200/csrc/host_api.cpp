@@ -432,6 +432,92 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_plan(const ba
     return BAKLAVA_ERR_WORKSPACE;
 }
 
+// ---------------------------------------------------------------- the drafted-token calls from one array
+extern "C" __attribute__((visibility("default"))) int baklava_tree_call(int32_t call, const int64_t* args, int32_t words) {
+    if (!args) return BAKLAVA_ERR_INVALID_ARG;
+    const int64_t* at = args;
+    bool fits = true;
+    auto ptr = [&] { return reinterpret_cast<void*>(static_cast<uintptr_t>(*at++)); };
+    auto i32 = [&] {
+        const int64_t x = *at++;
+        fits = fits && x >= INT32_MIN && x <= (int64_t)UINT32_MAX;
+        return (int32_t)x;
+    };
+    auto strides = [&] {
+        baklava_strides s = {at[0], at[1], at[2]};
+        at += 3;
+        return s;
+    };
+    if (call == BAKLAVA_CALL_TREE_ATTN && words == 27) {
+        const auto* shape = static_cast<const baklava_shape*>(ptr());
+        const auto* cache = static_cast<const baklava_cache*>(ptr());
+        const void* q = ptr();
+        const baklava_strides qs = strides();
+        const void* k = ptr();
+        const baklava_strides ks = strides();
+        const void* v = ptr();
+        const baklava_strides vs = strides();
+        const auto* parent = static_cast<const int32_t*>(ptr());
+        const auto* n_nodes = static_cast<const int32_t*>(ptr());
+        const int32_t T = i32();
+        void* out = ptr();
+        const baklava_strides os = strides();
+        auto* lse = static_cast<float*>(ptr());
+        const auto* items = static_cast<const int32_t*>(ptr());
+        const auto* info = static_cast<const baklava_plan_info*>(ptr());
+        void* ws = ptr();
+        const size_t ws_bytes = (size_t)*at++;
+        void* stream = ptr();
+        return fits ? baklava_tree_attn(shape, cache, q, &qs, k, &ks, v, &vs, parent, n_nodes, T, out, &os, lse, items, info, ws, ws_bytes, stream)
+                    : BAKLAVA_ERR_INVALID_ARG;
+    }
+    if (call == BAKLAVA_CALL_TREE_VERIFY && words == 19) {
+        const void* target = ptr();
+        const int64_t target_stride = *at++;
+        const void* draft = ptr();
+        const int64_t draft_stride = *at++;
+        const int32_t dtype = i32();
+        const auto* tokens = static_cast<const int32_t*>(ptr());
+        const auto* parent = static_cast<const int32_t*>(ptr());
+        const auto* n_nodes = static_cast<const int32_t*>(ptr());
+        const int32_t B = i32(), T = i32(), V = i32();
+        const auto* ua = static_cast<const float*>(ptr());
+        const auto* us = static_cast<const float*>(ptr());
+        const uint32_t flags = (uint32_t)i32();
+        auto* path = static_cast<int32_t*>(ptr());
+        auto* n_path = static_cast<int32_t*>(ptr());
+        auto* token = static_cast<int32_t*>(ptr());
+        auto* status = static_cast<uint32_t*>(ptr());
+        void* stream = ptr();
+        return fits ? baklava_tree_verify(target, target_stride, draft, draft_stride, dtype, tokens, parent, n_nodes, B, T, V, ua, us, flags, path,
+                                          n_path, token, status, stream)
+                    : BAKLAVA_ERR_INVALID_ARG;
+    }
+    if (call == BAKLAVA_CALL_TREE_COMMIT && words == 18) {
+        const auto* shape = static_cast<const baklava_shape*>(ptr());
+        const auto* cache = static_cast<const baklava_cache*>(ptr());
+        const void* q = ptr();
+        const void* k = ptr();
+        const void* v = ptr();
+        const auto* lse = static_cast<const float*>(ptr());
+        const int32_t T = i32();
+        const auto* path = static_cast<const int32_t*>(ptr());
+        const auto* n_path = static_cast<const int32_t*>(ptr());
+        const int32_t max_path = i32();
+        const auto* t_pos = static_cast<const int32_t*>(ptr());
+        auto* t_next = static_cast<int32_t*>(ptr());
+        const uint32_t flags = (uint32_t)i32();
+        const auto* items = static_cast<const int32_t*>(ptr());
+        const auto* info = static_cast<const baklava_plan_info*>(ptr());
+        void* ws = ptr();
+        const size_t ws_bytes = (size_t)*at++;
+        void* stream = ptr();
+        return fits ? baklava_tree_commit(shape, cache, q, k, v, lse, T, path, n_path, max_path, t_pos, t_next, flags, items, info, ws, ws_bytes, stream)
+                    : BAKLAVA_ERR_INVALID_ARG;
+    }
+    return BAKLAVA_ERR_INVALID_ARG;
+}
+
 // ---------------------------------------------------------------- Algorithm 3: which configuration wins
 extern "C" __attribute__((visibility("default"))) int baklava_search_pick(const double* avg_loss, int32_t n,
                                                                           int32_t* best) {

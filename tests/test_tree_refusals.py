@@ -94,6 +94,23 @@ def test_commit_refuses(kw, code):
     assert commit(**kw) == code
 
 
+@pytest.mark.parametrize("call,words,other", [(0, 27, 28), (1, 19, 20), (2, 18, 17), (3, 18, 18), (-1, 27, 27)])
+def test_calls_from_an_array(call, words, other):
+    """A wrong number of words or call is refused, numbers beyond 32 bits too; with the right ones the call's own refusal comes."""
+    f = bk.lib().baklava_tree_call
+    pack = lambda *x: np.array(x, dtype=np.int64).tobytes()                                   # noqa: E731
+    assert f(call, pack(*[0] * other), other) == INVALID and f(call, None, words) == INVALID
+    if call == 1:
+        good = [P, 100, P, 100, 0, P, P, 0, 2, 4, 100, P, P, 0, P, P, P, P, 0]
+        assert f(1, pack(*good[:9], 65, *good[10:]), 19) == UNSUPPORTED and f(1, pack(*good[:9], 1 << 32, *good[10:]), 19) == INVALID
+    if call == 0:
+        sh, c = bk.make_shape(1, 4, 2, 80), cache()
+        assert f(0, pack(ctypes.addressof(sh), ctypes.addressof(c), *[0] * 25), 27) == SHAPE
+    if call == 2:
+        sh, c = bk.make_shape(1, 4, 2, 80), cache()
+        assert f(2, pack(ctypes.addressof(sh), ctypes.addressof(c), *[0] * 16), 18) == SHAPE
+
+
 def test_workspace_of_nothing():
     sh, info = bk.make_shape(1, 4, 2, 64), bk.PlanInfo(n_items=4, chunk_tokens=128)
     size = lambda i, m: bk.lib().baklava_tree_commit_workspace_size(ctypes.byref(sh), i, m)   # noqa: E731
