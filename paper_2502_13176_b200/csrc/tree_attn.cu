@@ -85,7 +85,7 @@ struct Item {
 struct Shared {
     uint4 answer;
     uint64_t full[kMaxSlots], empty[kMaxSlots], raw_full[kMaxSlots], raw_empty[kMaxSlots];
-    uint64_t s_full[kMaxBuffers], p_ready[kMaxBuffers], o_full[2], q_full[2], sums[2], q_free, o_free, ref_ready, both, bar_answer, bar_item[kItemRing];
+    uint64_t s_full[kMaxBuffers], p_ready[kMaxBuffers], o_full[2], q_full[2], sums[2], scales_full[4], ref_ready[2], q_free, o_free, both, bar_answer, bar_item[kItemRing];
     Item item[kItemRing], redo[kMaxRedo];
     int redo_count, redo_mark[kItemRing];
     uint32_t tmem_slot;
@@ -126,6 +126,10 @@ struct Layout {
     static constexpr int kBuffers = R == 1 ? 3 : 2;
     static constexpr uint32_t kOColumn = kBuffers * kKeys;
     static_assert(kTotal <= 232448, "one CTA's shared memory");
+    // A softmax warp waits for a value tile that it has to clear as soon as it has the tile's logits.  A barrier's phase can be waited
+    // for only when the one before it is over: the tile in the same place before must have landed by then.  With five places it
+    // is the same tile's keys or older (R = 2: four, the value tile two before).  4 bits: the scales have barriers of their own.
+    static_assert(kQuantised || kSlots >= (R == 1 ? 5 : 4), "see above");
     static_assert(R == 1 || KV != BAKLAVA_KV_INT4, "two rows' blocks of queries in two terms leave no room");
     // Keys of quantised slabs, whose codes are exact in it, and their queries are fp16 operands.  Probabilities and values are
     // bf16: the codes are exact there too, and a probability may be far above one (see the reference in soften_item).
@@ -381,68 +385,72 @@ __device__ __forceinline__ bool convert_item(const TreeParams& p, Shared& sm, co
         if (!ptx::mbar_wait(ptx::smem_u32(&sm.empty[slot]), (n / L::kSlots & 1) ^ 1)) return false;
         uint8_t* const to = cta.ptr + L::kRing + slot * L::kTileBytes;
         for (int half = 0; half < 2; ++half) {
-        const uint32_t m = 2 * n + half, raw = m % L::kRawSlots;
-        if (!ptx::mbar_wait(ptx::smem_u32(&sm.raw_full[raw]), m / L::kRawSlots & 1)) return false;
-        __syncwarp();
-        const uint8_t* const from = cta.ptr + L::kRaw + raw * L::kRawBytes;
+            const uint32_t m = 2 * n + half, raw = m % L::kRawSlots;
+            if (!ptx::mbar_wait(ptx::smem_u32(&sm.raw_full[raw]), m / L::kRawSlots & 1)) return false;
+            __syncwarp();
+            const uint8_t* const from = cta.ptr + L::kRaw + raw * L::kRawBytes;
 #pragma unroll
-        for (int i = 0; i < 16 / kStep; ++i) {                // a warp has sixteen of a half's rows
-            const int of_half = w * 16 + i * kStep + lane / kLanes, row = half * L::kHalf + of_half;
-            const bool here = row < keys && row != no_row;
-            uint4 x = *reinterpret_cast<const uint4*>(from + of_half * L::kRowBytes + piece * 16);
-            uint8_t* const at = to + row * 128;
-            auto place = [&](int chunk) { return reinterpret_cast<uint4*>(at + (chunk >> 3) * L::kBoxBytes + (((chunk & 7) ^ (row & 7)) << 4)); };
-            if (KV == BAKLAVA_KV_FP8_E4M3) {
-                if (!here) x = make_uint4(0, 0, 0, 0);
-                uint4 y[2];
-                fp8::f16x4_from_e4m3x4(x.x, y[0].x, y[0].y);
-                fp8::f16x4_from_e4m3x4(x.y, y[0].z, y[0].w);
-                fp8::f16x4_from_e4m3x4(x.z, y[1].x, y[1].y);
-                fp8::f16x4_from_e4m3x4(x.w, y[1].z, y[1].w);
-                if (value) {
+            for (int i = 0; i < 16 / kStep; ++i) {                // a warp has sixteen of a half's rows
+                const int of_half = w * 16 + i * kStep + lane / kLanes, row = half * L::kHalf + of_half;
+                const bool here = row < keys && row != no_row;
+                uint4 x = *reinterpret_cast<const uint4*>(from + of_half * L::kRowBytes + piece * 16);
+                uint8_t* const at = to + row * 128;
+                auto place = [&](int chunk) { return reinterpret_cast<uint4*>(at + (chunk >> 3) * L::kBoxBytes + (((chunk & 7) ^ (row & 7)) << 4)); };
+                if (KV == BAKLAVA_KV_FP8_E4M3) {
+                    if (!here) x = make_uint4(0, 0, 0, 0);
+                    uint4 y[2];
+                    fp8::f16x4_from_e4m3x4(x.x, y[0].x, y[0].y);
+                    fp8::f16x4_from_e4m3x4(x.y, y[0].z, y[0].w);
+                    fp8::f16x4_from_e4m3x4(x.z, y[1].x, y[1].y);
+                    fp8::f16x4_from_e4m3x4(x.w, y[1].z, y[1].w);
+                    if (value) {
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) y[k] = make_uint4(bf16_pair(y[k].x), bf16_pair(y[k].y), bf16_pair(y[k].z), bf16_pair(y[k].w));
-                }
-                const int swap = piece >> 2;
-                *place(2 * piece + swap) = swap ? y[1] : y[0];
-                *place(2 * piece + 1 - swap) = swap ? y[0] : y[1];
-            } else {
-                if (!here) x = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
-                const uint32_t word[4] = {x.x, x.y, x.z, x.w};
-                uint4 y[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    uint32_t z[4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const uint32_t nib = (word[k] >> (4 * q)) & 0x000f000fu;
-                        if (value) {                          // bf16: 128 + code, less 136
-                            const uint32_t m = nib | 0x43004300u;
-                            const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&m), __float2bfloat162_rn(136.0f));
-                            z[q] = *reinterpret_cast<const uint32_t*>(&v);
-                        } else {                              // fp16: 1024 + code, less 1032
-                            const uint32_t m = nib | 0x64006400u;
-                            const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&m), __half2half2(__ushort_as_half(0x6408)));
-                            z[q] = *reinterpret_cast<const uint32_t*>(&v);
-                        }
+                        for (int k = 0; k < 2; ++k) y[k] = make_uint4(bf16_pair(y[k].x), bf16_pair(y[k].y), bf16_pair(y[k].z), bf16_pair(y[k].w));
                     }
-                    y[k] = make_uint4(z[0], z[1], z[2], z[3]);
-                }
-                const int swap = piece & 2;
+                    const int swap = piece >> 2;
+                    *place(2 * piece + swap) = swap ? y[1] : y[0];
+                    *place(2 * piece + 1 - swap) = swap ? y[0] : y[1];
+                } else {
+                    if (!here) x = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
+                    const uint32_t word[4] = {x.x, x.y, x.z, x.w};
+                    uint4 y[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) *place(4 * piece + (k ^ swap)) = swap ? y[k ^ 2] : y[k];
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t z[4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const uint32_t nib = (word[k] >> (4 * q)) & 0x000f000fu;
+                            if (value) {                          // bf16: 128 + code, less 136
+                                const uint32_t m = nib | 0x43004300u;
+                                const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&m), __float2bfloat162_rn(136.0f));
+                                z[q] = *reinterpret_cast<const uint32_t*>(&v);
+                            } else {                              // fp16: 1024 + code, less 1032
+                                const uint32_t m = nib | 0x64006400u;
+                                const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&m), __half2half2(__ushort_as_half(0x6408)));
+                                z[q] = *reinterpret_cast<const uint32_t*>(&v);
+                            }
+                        }
+                        y[k] = make_uint4(z[0], z[1], z[2], z[3]);
+                    }
+                    const int swap = piece & 2;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) *place(4 * piece + (k ^ swap)) = swap ? y[k ^ 2] : y[k];
+                }
             }
-        }
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.raw_empty[raw]));
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.raw_empty[raw]));
         }
         if (KV == BAKLAVA_KV_INT4 && value)
             *reinterpret_cast<float2*>(cta.ptr + L::kScales + slot * L::kScaleBytes + scale_row * 8) = scale;
         tc::fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.full[slot]));
+        if (lane == 0) {
+            tc::mbar_arrive(ptx::smem_u32(&sm.full[slot]));
+            if (KV == BAKLAVA_KV_INT4 && value) tc::mbar_arrive(ptx::smem_u32(&sm.scales_full[(c.step + t) & 3]));
+        }
     }
     c.entry += entries;
+    c.step += it.tiles;                                       // (4 bits: a step for a tile)
     return true;
 }
 
@@ -670,6 +678,13 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
     float factor = query_factor<D, R, KV>(p, it);
     ptx::f32x2 sum[2] = {0ull, 0ull};
     float largest = -INFINITY;
+    // R = 1: stream 1 takes stream 0's references.  It waits for them in items that have no step for it too: a phase of a barrier
+    // can be waited for only when the one before it is over, and this keeps it from running ahead through items of one tile.
+    if (R == 1 && stream == 1 && kMode != kMaxima) {
+        if (!ptx::mbar_wait(ptx::smem_u32(&sm.ref_ready[turn]), (c.work >> 1) & 1)) return false;
+        __syncwarp();
+        ref = sm.ref[turn][0][row];
+    }
     for (int n = stream; n < steps; n += 2) {
         const int t = tile_of<R>(n), keys = it.keys - t * kKeys, hole = it.hole - t * kKeys;
         const bool masked = keys < kKeys || (it.hole >= 0 && hole >= 0 && hole < kKeys);
@@ -681,7 +696,9 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
             if (!ptx::mbar_wait(ptx::smem_u32(&sm.q_full[turn]), (c.work >> 1) & 1)) return false;
             factor = sm.factor[turn][row];
         }
-        if (kMode != kMaxima && (KV == BAKLAVA_KV_INT4 || (!L::kQuantised && masked && (R == 1 || stream == 0))))
+        if (kMode != kMaxima && KV == BAKLAVA_KV_INT4)
+            if (!ptx::mbar_wait(ptx::smem_u32(&sm.scales_full[g & 3]), g >> 2 & 1)) return false;
+        if (kMode != kMaxima && !L::kQuantised && masked && (R == 1 || stream == 0))
             if (!ptx::mbar_wait(ptx::smem_u32(&sm.full[slot]), entry / L::kSlots & 1)) return false;
         __syncwarp();
         tc::fence_after_sync();
@@ -722,16 +739,10 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
                     }
                 ref = top == -INFINITY ? 0.0f : top;
             }
-            if (R == 1 && n == stream) {                                // stream 1 takes stream 0's
-                if (stream == 0) {
-                    sm.ref[turn][0][row] = ref;
-                    __syncwarp();
-                    if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.ref_ready));
-                } else {
-                    if (!ptx::mbar_wait(ptx::smem_u32(&sm.ref_ready), c.work & 1)) return false;
-                    __syncwarp();
-                    ref = sm.ref[turn][0][row];
-                }
+            if (R == 1 && n == 0) {                                     // stream 1 takes these
+                sm.ref[turn][0][row] = ref;
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.ref_ready[turn]));
             }
             if (busy) {
                 if (masked) softmax_row<KV, true>(column, keys, no_row, scales, factor, ref, sum);
@@ -851,6 +862,7 @@ __device__ __forceinline__ void each_barrier(Shared& sm, int lane, F f) {
         f(sm.raw_full[lane], 1);
         f(sm.raw_empty[lane], kConvertWarps);
     }
+    if (L::kScaleBytes > 0 && lane < 4) f(sm.scales_full[lane], kConvertWarps);
     if (lane < L::kBuffers) {
         f(sm.s_full[lane], 1);
         f(sm.p_ready[lane], kSoftmaxWarps / 2);
@@ -859,11 +871,11 @@ __device__ __forceinline__ void each_barrier(Shared& sm, int lane, F f) {
         f(sm.o_full[lane], 1);
         f(sm.q_full[lane], L::kLoadsQ ? 1 : kRowWarps);
         f(sm.sums[lane], kSoftmaxWarps);
+        f(sm.ref_ready[lane], kSoftmaxWarps / 2);
     }
     if (lane == 2) {
         f(sm.q_free, 1);
         f(sm.o_free, kRowWarps);
-        f(sm.ref_ready, kSoftmaxWarps / 2);
         f(sm.both, kSoftmaxWarps);
     }
 }

@@ -238,3 +238,62 @@ def test_repeated_replayed_and_side_by_side():
     torch.cuda.synchronize()
     again, _ = run(c, q2, k, v, parent, None)
     assert torch.equal(outs[2], again)
+
+
+@pytest.mark.parametrize("kv,T,D", [("bf16", 8, 128), ("bf16", 64, 128), ("bf16", 16, 64), ("fp8", 8, 128), ("fp8", 64, 128), ("int4", 8, 128), ("int4", 40, 128)])
+def test_long_heads_side_by_side(kv, T, D):
+    """A device full of long items, where loads are late: the same bits every time and for other inputs in between, right where
+    looked at."""
+    rng = np.random.default_rng(16)
+    sh = bk.make_shape(1, 32, 8, D)
+    B = 6
+    caps = [[9008, 2000, 5008, 7008, 12000, 10000, 16000, 3008]]
+    held = np.array(caps)[None] - 1 - rng.integers(0, 900, (B, 1, 8))
+    c = Held(sh, caps, B, kv, held, np.minimum(held, rng.integers(0, 16000, held.shape)), seed=7, poison=kv != "bf16")
+    q, k, v, parent = inputs(rng, sh, B, T)
+    ref, rz = run(c, q, k, v, parent, None)
+    for i in range(6):
+        out, z = run(c, q, k, v, parent, None)
+        assert torch.equal(out, ref) and torch.equal(z, rz), i
+    for b, h in ((0, 0), (5, 6), (3, 1)):
+        rows = c.rows(b, 0, h)
+        K, V = c.values(0, rows, 0, h), c.values(1, rows, 0, h)
+        y = slice(4 * h, 4 * h + 4)
+        q64, k64, v64, par = (x[b].double().cpu().numpy() for x in (q, k, v, parent))
+        want, wz = ot.tree_attention(q64[y], k64[h], v64[h], par.astype(int), K, V)
+        for i in (0, T // 2, T - 1):
+            w = ot.way(par.astype(int), i)
+            keys, vals = np.concatenate([K, k64[h, w]]), np.concatenate([V, v64[h, w]])
+            bo, bz = bounds(q64[y, i], keys, vals, want[:, i], wz[:, i])
+            assert (np.abs(rz[b, y, i].double().cpu().numpy() - wz[:, i]) <= bz).all()
+            assert (np.abs(ref[b, y, i].double().cpu().numpy() - want[:, i]) <= bo).all()
+
+
+@pytest.mark.parametrize("kv,T,D", [("bf16", 8, 128), ("bf16", 64, 128), ("bf16", 16, 64), ("fp8", 16, 128), ("fp8", 64, 128), ("int4", 16, 128), ("int4", 48, 128)])
+def test_many_short_heads(kv, T, D):
+    """Several items to a block, most of them of one tile, some of more, some of none: the same bits every time, and right
+    where looked at."""
+    rng = np.random.default_rng(17)
+    sh = bk.make_shape(1, 32, 8, D)
+    B = 64
+    caps = [[16, 112, 128, 304, 64, 16, 1008, 144]]
+    held = np.array(caps)[None] - 1 - rng.integers(0, 15, (B, 1, 8))
+    held[rng.random(held.shape) < 0.1] = 0
+    c = Held(sh, caps, B, kv, held, np.minimum(held, rng.integers(0, 100, held.shape)), seed=8, poison=kv != "bf16")
+    q, k, v, parent = inputs(rng, sh, B, T)
+    ref, rz = run(c, q, k, v, parent, None)
+    for i in range(6):
+        out, z = run(c, q, k, v, parent, None)
+        assert torch.equal(out, ref) and torch.equal(z, rz), i
+    for b in (0, 31, 63):
+        for h in range(8):
+            rows = c.rows(b, 0, h)
+            K, V = c.values(0, rows, 0, h), c.values(1, rows, 0, h)
+            y = slice(4 * h, 4 * h + 4)
+            q64, k64, v64, par = (x[b].double().cpu().numpy() for x in (q, k, v, parent))
+            want, wz = ot.tree_attention(q64[y], k64[h], v64[h], par.astype(int), K, V)
+            for i in (0, T - 1):
+                w = ot.way(par.astype(int), i)
+                bo, bz = bounds(q64[y, i], np.concatenate([K, k64[h, w]]), np.concatenate([V, v64[h, w]]), want[:, i], wz[:, i])
+                assert (np.abs(rz[b, y, i].double().cpu().numpy() - wz[:, i]) <= bz).all()
+                assert (np.abs(ref[b, y, i].double().cpu().numpy() - want[:, i]) <= bo).all()
