@@ -187,17 +187,6 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ void load_16(uint32_t taddr, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void store_8(uint32_t taddr, const uint32_t (&r)[8]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
-}
 // eight fp32 of a row: one sector
 __device__ __forceinline__ void store_sector(float* to, const float (&x)[8]) {
     asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -636,7 +625,7 @@ __device__ __forceinline__ void softmax_16(uint32_t (&v)[16], uint32_t column, i
         const float2 f = ptx::unpack2(prob);
         w[c] = pack_bf16(f.x, f.y);
     }
-    store_8(column, w);
+    tc::tmem_st_32x32_x8(column, w);
 }
 // A row's 128 logits of a tile: sixteen are asked for while the sixteen before are worked on.  Probabilities take the place
 // of logits that have been read.
@@ -644,14 +633,14 @@ template <int KV, bool kMasked>
 __device__ __forceinline__ void softmax_row(uint32_t column, int keys, int hole, uint32_t scales, float scale, float ref, ptx::f32x2 (&sum)[2]) {
     const ptx::f32x2 scale2 = ptx::pack2(scale, scale), minus = ptx::pack2(-ref, -ref);
     uint32_t a[16], b[16];
-    load_16(column, a);
+    tc::tmem_ld_32x32_x16(column, a);
 #pragma unroll
     for (int c = 0; c < kKeys; c += 32) {
         tc::tmem_ld_wait();
-        load_16(column + c + 16, b);
+        tc::tmem_ld_32x32_x16(column + c + 16, b);
         softmax_16<KV, kMasked>(a, column + c / 2, c, keys, hole, scales, scale2, minus, sum);
         tc::tmem_ld_wait();
-        if (c + 32 < kKeys) load_16(column + c + 32, a);
+        if (c + 32 < kKeys) tc::tmem_ld_32x32_x16(column + c + 32, a);
         softmax_16<KV, kMasked>(b, column + c / 2 + 8, c + 16, keys, hole, scales, scale2, minus, sum);
     }
     tc::tmem_st_wait();
@@ -708,7 +697,7 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
 #pragma unroll 1
                 for (int k = 0; k < kKeys; k += 16) {
                     uint32_t v[16];
-                    load_16(column + k, v);
+                    tc::tmem_ld_32x32_x16(column + k, v);
                     tc::tmem_ld_wait();
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
@@ -814,11 +803,11 @@ __device__ __forceinline__ bool write_rows(const TreeParams& p, Shared& sm, cons
         const float v_scale = KV == BAKLAVA_KV_FP8_E4M3 ? four[2] : 1.0f;
         bool bad = !(l <= kMaxSum);
         uint32_t v[2][16];
-        load_16(lane_addr + Layout<D, R, KV>::kOColumn + acc * 128, v[0]);
+        tc::tmem_ld_32x32_x16(lane_addr + Layout<D, R, KV>::kOColumn + acc * 128, v[0]);
 #pragma unroll
         for (int col = 0; col < D; col += 16) {
             tc::tmem_ld_wait();
-            if (col + 16 < D) load_16(lane_addr + Layout<D, R, KV>::kOColumn + acc * 128 + col + 16, v[(col >> 4) + 1 & 1]);
+            if (col + 16 < D) tc::tmem_ld_32x32_x16(lane_addr + Layout<D, R, KV>::kOColumn + acc * 128 + col + 16, v[(col >> 4) + 1 & 1]);
             float x[2][8], worst = 0.0f;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
