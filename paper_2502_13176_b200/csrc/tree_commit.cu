@@ -95,8 +95,8 @@ constexpr int kColumnPad = 64;                // bytes between the columns' rows
 constexpr int kMaxColumns = 256;              // columns in shared memory at a time (long paths of large groups take several rounds)
 
 // The first `leave` of a warp's rows in the order in which rows leave, ascending, in shared memory.  Few rows get in once the
-// list is full: a key is looked at only if it is below the last one.  (A bound shared by the block's lists let fewer in and cost as much as
-// it saved.)
+// list is full: a key is looked at only if it is below the last one.  (Sorting a step's rows and merging them in cost a pass over 2.5 M
+// bf16 rows 27 us more than it does, a bound shared by the block's lists 15.)
 struct LeaveList {
     unsigned long long keys[96];
     int slots[96];
@@ -380,8 +380,8 @@ __global__ void __launch_bounds__(kThreads, 2) path_scores_kernel(const __grid_c
 // memory as the fp16 operand A (codes are exact there), 128 rows to four warps, and the tensor core multiplies them with the path's queries
 // in shared memory; then a thread has all of its row's logits of 64 columns in its own lane and adds up their shares without a
 // word to its neighbours.  An SM has four such groups of warps, which run on their own: while one converts, another's products are
-// formed.  They are of four blocks where the queries leave room for that (what a block does once is then a smaller part of its
-// time: 16 sequences, 63 columns of 4 bits GROUPS1 us, GROUPS2 in two blocks), else of two or of one.
+// formed.  They are of two blocks where the queries leave room for that, else of one (40 nodes of groups of seven over 2 M rows of 4 bits:
+// 822 us, with one block of two groups 1036).
 template <int KV>
 struct Coded {
     static constexpr int D = 128, kRowBytes = KV == BAKLAVA_KV_FP8_E4M3 ? D : D / 2, kPieces = kRowBytes / 16;
@@ -877,10 +877,8 @@ cudaError_t launch_coded(const CommitParams& p, int n_items, cudaStream_t s) {
 }
 template <int KV>
 cudaError_t launch_scores_coded(const CommitParams& p, int n_items, cudaStream_t s) {
-    constexpr int kSm = 227 * 1024 - 4 * 1024;                // of an SM, less what the system takes of it for each block
-    const int columns = coded_columns(p);
-    if (4 * coded_shared<KV, 1>(columns) <= kSm) return launch_coded<KV, 1>(p, n_items, s);
-    if (2 * coded_shared<KV, 2>(columns) <= kSm) return launch_coded<KV, 2>(p, n_items, s);
+    // (an SM's shared memory, less what the system takes of it for each block)
+    if (2 * coded_shared<KV, 2>(coded_columns(p)) <= 225 * 1024) return launch_coded<KV, 2>(p, n_items, s);
     return launch_coded<KV, 4>(p, n_items, s);
 }
 
