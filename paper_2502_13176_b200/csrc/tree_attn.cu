@@ -59,7 +59,7 @@ constexpr int kRows = 128;                    // query rows to an accumulator
 // tensor memory's quarters), the producer, the tensor core's, the one that looks for further items, converters
 constexpr int kSoftmaxWarps = 8;
 constexpr int kRowWarps = 4;
-constexpr int kConvertWarps = 4;
+constexpr int kConvertWarps = 4;              // that convert a tile together
 constexpr int kRowWarp0 = kSoftmaxWarps, kProducerWarp = kRowWarp0 + kRowWarps, kMmaWarp = kProducerWarp + 1, kScoutWarp = kMmaWarp + 1,
               kConvertWarp0 = kScoutWarp + 1;
 constexpr int kItemRing = 4;
@@ -100,7 +100,8 @@ constexpr int kSharedBytes = 5632;
 static_assert(offsetof(Shared, factor) <= kSharedBytes, "the tiles take the rest");
 
 // How an instance lies in shared memory: the query rows, the ring of operand tiles, for quantised slabs the ring of
-// tiles as they are in the slab and the rows' scales (4 bits: beside each operand tile), then Shared.
+// tiles as they are in the slab and the rows' scales (4 bits: of four tiles; those of tile n + 4 come in when its keys are converted,
+// for which V(n), and so the logits of n, must have been done with), then Shared.
 template <int D, int R, int KV>
 struct Layout {
     static constexpr bool kQuantised = KV != BAKLAVA_KV_BF16;
@@ -114,10 +115,14 @@ struct Layout {
     static constexpr int kScaleBytes = KV == BAKLAVA_KV_INT4 ? kKeys * 8 : 0;
     static constexpr int kSlots = kQuantised ? (KV == BAKLAVA_KV_INT4 ? 3 : 4) : D == 128 ? (R == 2 ? 4 : 5) : R == 2 ? 10 : 12;
     static constexpr int kRawSlots = !kQuantised ? 0 : KV == BAKLAVA_KV_INT4 ? 12 : R == 2 ? 3 : 7;
-    static constexpr int kRing = kQBytes, kScales = kRing + kSlots * kTileBytes, kRaw = kScales + kSlots * kScaleBytes;
+    static constexpr int kRing = kQBytes, kScales = kRing + kSlots * kTileBytes, kRaw = kScales + 4 * kScaleBytes;
     static constexpr int kShared = kRaw + kRawSlots * kRawBytes;
     static constexpr int kTotal = kShared + (KV == BAKLAVA_KV_INT4 ? (int)sizeof(Shared) : kSharedBytes);
-    static constexpr int kThreads = (kConvertWarp0 + (kQuantised ? kConvertWarps : 0)) * 32;
+    // 4 bits: two teams of converting warps, which take the tiles in turn (one team: 239 us for a batch of 16 long sequences, TEAMS with two;
+    // FP8 rows are less work, and more threads have fewer registers each)
+    static constexpr int kTeams = KV == BAKLAVA_KV_INT4 ? 2 : 1;
+    static_assert(kTeams == 1 || kRawSlots % 4 == 0, "a place of the ring is one team's: it waits for all of the place's phases");
+    static constexpr int kThreads = (kConvertWarp0 + (kQuantised ? kTeams * kConvertWarps : 0)) * 32;
     // (registers for more threads than there are: a block of the second kernel has room beside this one's)
     static constexpr int kRegisterThreads = kQuantised ? kThreads : 608;
     static constexpr bool kLoadsQ = !kQuantised;                       // the queries come by TMA
@@ -360,16 +365,17 @@ template <int D, int R, int KV, int kMode>
 __device__ __forceinline__ bool convert_item(const TreeParams& p, Shared& sm, const Cta& cta, const Item& it, Count& c, int warp, int lane) {
     using L = Layout<D, R, KV>;
     constexpr int kLanes = L::kRowBytes / 16, kStep = 32 / kLanes;     // lanes to a row, rows to a warp's step
-    const int w = warp - kConvertWarp0, piece = lane % kLanes;
+    const int team = (warp - kConvertWarp0) / kConvertWarps, w = (warp - kConvertWarp0) % kConvertWarps, piece = lane % kLanes;
     const int entries = entries_of<kMode>(it);
     for (int e = 0; e < entries; ++e) {
         int t;
         const bool value = entry_is_value<R, kMode>(e, it.tiles, t);
         const uint32_t n = c.entry + e, slot = n % L::kSlots;
+        if (n % L::kTeams != team) continue;
         const int keys = it.keys - t * kKeys, no_row = it.hole >= 0 ? it.hole - t * kKeys : -1;
         float2 scale = make_float2(0.0f, 0.0f);
         const int scale_row = w * 32 + lane;
-        if (KV == BAKLAVA_KV_INT4 && value && scale_row < keys && scale_row != no_row)
+        if (KV == BAKLAVA_KV_INT4 && !value && scale_row < keys && scale_row != no_row)
             scale = *reinterpret_cast<const float2*>(p.c.row_scale + 2 * ((int64_t)it.first + t * kKeys + scale_row));
         if (!ptx::mbar_wait(ptx::smem_u32(&sm.empty[slot]), (n / L::kSlots & 1) ^ 1)) return false;
         uint8_t* const to = cta.ptr + L::kRing + slot * L::kTileBytes;
@@ -429,13 +435,13 @@ __device__ __forceinline__ bool convert_item(const TreeParams& p, Shared& sm, co
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(ptx::smem_u32(&sm.raw_empty[raw]));
         }
-        if (KV == BAKLAVA_KV_INT4 && value)
-            *reinterpret_cast<float2*>(cta.ptr + L::kScales + slot * L::kScaleBytes + scale_row * 8) = scale;
+        if (KV == BAKLAVA_KV_INT4 && !value)                  // both of a row's scales: the softmax warps need them with the logits
+            *reinterpret_cast<float2*>(cta.ptr + L::kScales + ((c.step + t) & 3) * L::kScaleBytes + scale_row * 8) = scale;
         tc::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
             tc::mbar_arrive(ptx::smem_u32(&sm.full[slot]));
-            if (KV == BAKLAVA_KV_INT4 && value) tc::mbar_arrive(ptx::smem_u32(&sm.scales_full[(c.step + t) & 3]));
+            if (KV == BAKLAVA_KV_INT4 && !value) tc::mbar_arrive(ptx::smem_u32(&sm.scales_full[(c.step + t) & 3]));
         }
     }
     c.entry += entries;
@@ -691,7 +697,7 @@ __device__ __forceinline__ bool soften_item(const TreeParams& p, Shared& sm, con
             if (!ptx::mbar_wait(ptx::smem_u32(&sm.full[slot]), entry / L::kSlots & 1)) return false;
         __syncwarp();
         tc::fence_after_sync();
-        const uint32_t scales = KV == BAKLAVA_KV_INT4 ? cta.base + L::kScales + slot * L::kScaleBytes + behind_waits() : 0u;
+        const uint32_t scales = KV == BAKLAVA_KV_INT4 ? cta.base + L::kScales + (g & 3) * L::kScaleBytes + behind_waits() : 0u;
         if (kMode == kMaxima) {
             if (busy) {
 #pragma unroll 1
