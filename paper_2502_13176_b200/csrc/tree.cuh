@@ -73,15 +73,6 @@ struct Head {
 __device__ __forceinline__ int nodes_of(const int32_t* n_nodes, int b, int T) {
     return n_nodes ? min(max(n_nodes[b], 0), T) : T;
 }
-// Whether the tree's parents can be (a whole warp; n <= 64).
-__device__ __forceinline__ bool tree_ok(const int32_t* parent, int n, int lane) {
-    bool ok = true;
-    for (int i = lane; i < n; i += 32) {
-        const int p = parent[i];
-        ok = ok && p >= -1 && p < i;
-    }
-    return __all_sync(0xffffffffu, ok);
-}
 
 }  // namespace tree
 

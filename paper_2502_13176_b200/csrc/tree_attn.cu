@@ -118,7 +118,7 @@ struct Layout {
     static constexpr int kRing = kQBytes, kScales = kRing + kSlots * kTileBytes, kRaw = kScales + 4 * kScaleBytes;
     static constexpr int kShared = kRaw + kRawSlots * kRawBytes;
     static constexpr int kTotal = kShared + (KV == BAKLAVA_KV_INT4 ? (int)sizeof(Shared) : kSharedBytes);
-    // 4 bits: two teams of converting warps, which take the tiles in turn (one team: 239 us for a batch of 16 long sequences, TEAMS with two;
+    // 4 bits: two teams of converting warps, which take the tiles in turn (a batch of 16 long sequences: 220 us with one team of eight warps, 215;
     // FP8 rows are less work, and more threads have fewer registers each)
     static constexpr int kTeams = KV == BAKLAVA_KV_INT4 ? 2 : 1;
     static_assert(kTeams == 1 || kRawSlots % 4 == 0, "a place of the ring is one team's: it waits for all of the place's phases");
@@ -207,6 +207,14 @@ struct Cta {
     uint32_t base, tmem;          // shared memory, tensor memory
     uint8_t* ptr;
 };
+// A place in a ring and the phase of its barriers.
+template <int kPlaces>
+struct Cursor {
+    uint32_t at = 0, phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++at == kPlaces) { at = 0; phase ^= 1u; }
+    }
+};
 // Counters that run on over the items: tiles through the rings, steps, items that had work.
 struct Count {
     uint32_t entry = 0, step = 0, work = 0;
@@ -219,8 +227,6 @@ enum Mode { kFast, kMaxima, kExact };
 // the tensor core takes them: R = 2: K, V of each tile; R = 1: the first three K, then V, K in turn, then the last V.
 template <int R>
 __device__ __forceinline__ int tile_of(int step) { return R == 2 ? step >> 1 : step; }
-template <int R, int kMode>
-__device__ __forceinline__ uint32_t key_entry(int t) { return kMode == kMaxima ? t : R == 2 ? 2 * t : t < 3 ? t : 2 * t - 2; }
 template <int R>
 __device__ __forceinline__ uint32_t value_entry(int t, int tiles) { return R == 2 ? 2 * t + 1 : min(tiles, t + 3) + t; }
 // the other way round: entry e of an item is the key or value tile t
@@ -450,6 +456,9 @@ __device__ __forceinline__ bool convert_item(const TreeParams& p, Shared& sm, co
 }
 
 // ---------------------------------------------------------------- the tensor core's thread
+// It is busy for most of a step (some 75 cycles for each product, and what lies between them), so it counts places instead of dividing, and
+// only descriptors' low words change (64 nodes over FP8 rows 293 -> 290 us).
+__device__ __forceinline__ uint64_t with_low(uint64_t desc, uint32_t more) { return (desc & 0xffffffff00000000ull) | (uint32_t)((uint32_t)desc + more); }
 template <int D, int R, int KV>
 __device__ __forceinline__ void issue_s(const Cta& cta, int acc, uint32_t buffer, uint32_t slot) {
     using L = Layout<D, R, KV>;
@@ -459,8 +468,8 @@ __device__ __forceinline__ void issue_s(const Cta& cta, int acc, uint32_t buffer
     for (int term = 0; term < L::kTerms; ++term)
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
-            tc::umma_bf16(cta.tmem + buffer * kKeys, dq + ((term * L::kQTerm + (ks >> 2) * L::kQBox + (ks & 3) * 32) >> 4),
-                          dk + (((ks >> 2) * L::kBoxBytes + (ks & 3) * 32) >> 4), L::kIdescS, term + ks > 0);
+            tc::umma_bf16(cta.tmem + buffer * kKeys, with_low(dq, (term * L::kQTerm + (ks >> 2) * L::kQBox + (ks & 3) * 32) >> 4),
+                          with_low(dk, ((ks >> 2) * L::kBoxBytes + (ks & 3) * 32) >> 4), L::kIdescS, term + ks > 0);
 }
 template <int D, int R, int KV>
 __device__ __forceinline__ void issue_pv(const Cta& cta, int acc, uint32_t buffer, uint32_t slot, bool accumulate) {
@@ -468,22 +477,38 @@ __device__ __forceinline__ void issue_pv(const Cta& cta, int acc, uint32_t buffe
     const uint64_t dv = tc::desc_mn_major_sw128(cta.base + L::kRing + slot * L::kTileBytes, L::kBoxBytes);
 #pragma unroll
     for (int ks = 0; ks < kKeys / 16; ++ks)
-        tc::umma_bf16_ts(cta.tmem + L::kOColumn + acc * 128, cta.tmem + buffer * kKeys + ks * 8, dv + (ks * 2048 >> 4), L::kIdescPv,
+        tc::umma_bf16_ts(cta.tmem + L::kOColumn + acc * 128, cta.tmem + buffer * kKeys + ks * 8, with_low(dv, ks * 2048 >> 4), L::kIdescPv,
                          accumulate || ks > 0);
 }
+template <int D, int R, int KV>
+struct Issue {                                                // (runs on over the items, as Count does)
+    Cursor<Layout<D, R, KV>::kSlots> ring;
+    Cursor<Layout<D, R, KV>::kBuffers> buffer;
+    uint32_t work = 0;
+};
 template <int D, int R, int KV, int kMode>
-__device__ __forceinline__ bool issue_item(Shared& sm, const Cta& cta, const Item& it, Count& c) {
+__device__ __forceinline__ bool issue_item(Shared& sm, const Cta& cta, const Item& it, Issue<D, R, KV>& c) {
     using L = Layout<D, R, KV>;
     constexpr int kB = L::kBuffers;
     const int steps = it.tiles * R;
-    auto full = [&](uint32_t n) { return ptx::mbar_wait(ptx::smem_u32(&sm.full[n % L::kSlots]), n / L::kSlots & 1); };
+    const uint32_t full = ptx::smem_u32(&sm.full[0]), empty = ptx::smem_u32(&sm.empty[0]), s_full = ptx::smem_u32(&sm.s_full[0]),
+                   p_ready = ptx::smem_u32(&sm.p_ready[0]);
+    // R = 1: one cursor, the tiles come in the order of their use; R = 2: keys and values in turn
+    auto key = c.ring, value_of_two = c.ring;
+    auto& value = R == 1 ? key : value_of_two;
+    if (R == 2) value.next();
+    auto ahead = c.buffer;
     auto form_s = [&](int n) {
-        const uint32_t entry = c.entry + key_entry<R, kMode>(tile_of<R>(n)), slot = entry % L::kSlots, buffer = (c.step + n) % kB;
-        if (!full(entry)) return false;
+        if (!ptx::mbar_wait(full + 8 * key.at, key.phase)) return false;
         tc::fence_after_sync();
-        issue_s<D, R, KV>(cta, R == 2 ? n & 1 : 0, buffer, slot);
-        tc::umma_commit(ptx::smem_u32(&sm.s_full[buffer]));
-        if (R == 1 || (n & 1)) tc::umma_commit(ptx::smem_u32(&sm.empty[slot]));
+        issue_s<D, R, KV>(cta, R == 2 ? n & 1 : 0, ahead.at, key.at);
+        tc::umma_commit(s_full + 8 * ahead.at);
+        ahead.next();
+        if (R == 1 || (n & 1)) {
+            tc::umma_commit(empty + 8 * key.at);
+            key.next();
+            if (R == 2 && kMode != kMaxima) key.next();
+        }
         if (n == steps - 1) tc::umma_commit(ptx::smem_u32(&sm.q_free));
         return true;
     };
@@ -491,24 +516,26 @@ __device__ __forceinline__ bool issue_item(Shared& sm, const Cta& cta, const Ite
     for (int n = 0; n < min(kB, steps); ++n)
         if (!form_s(n)) return false;
     for (int n = 0; n < steps; ++n) {
-        const uint32_t g = c.step + n, buffer = g % kB;
-        if (!ptx::mbar_wait(ptx::smem_u32(&sm.p_ready[buffer]), g / kB & 1)) return false;
+        if (!ptx::mbar_wait(p_ready + 8 * c.buffer.at, c.buffer.phase)) return false;
         if (kMode != kMaxima) {
-            const uint32_t entry = c.entry + value_entry<R>(tile_of<R>(n), it.tiles), slot = entry % L::kSlots;
-            if (!full(entry)) return false;
+            if (!ptx::mbar_wait(full + 8 * value.at, value.phase)) return false;
             // the rows of the item before have been read from O
             if (n == 0 && c.work > 0 && !ptx::mbar_wait(ptx::smem_u32(&sm.o_free), (c.work - 1) & 1)) return false;
             tc::fence_after_sync();
-            issue_pv<D, R, KV>(cta, R == 2 ? n & 1 : 0, buffer, slot, n >= R);
-            if (R == 1 || (n & 1)) tc::umma_commit(ptx::smem_u32(&sm.empty[slot]));
+            issue_pv<D, R, KV>(cta, R == 2 ? n & 1 : 0, c.buffer.at, value.at, n >= R);
+            if (R == 1 || (n & 1)) {
+                tc::umma_commit(empty + 8 * value.at);
+                value.next();
+                if (R == 2) value.next();
+            }
             if (n == steps - 1) tc::umma_commit(ptx::smem_u32(&sm.o_full[c.work & 1]));
         } else {
             tc::fence_after_sync();
         }
+        c.buffer.next();
         if (n + kB < steps && !form_s(n + kB)) return false;
     }
-    c.entry += entries_of<kMode>(it);
-    c.step += steps;
+    c.ring = key;
     ++c.work;
     return true;
 }
@@ -904,7 +931,8 @@ __device__ __noinline__ void redo_pass(const TreeParams& p, Shared& sm, const Ct
             for (int e = 0; e < entries_of<kMode>(it) && ok; ++e) ok = load_entry<D, R, KV, kMode>(p, sm, cta, it, 0, e, k_map, v_map);
         }
     } else if (warp == kMmaWarp) {
-        if (lane == 0) ok = issue_item<D, R, KV, kMode>(sm, cta, it, c);
+        Issue<D, R, KV> issue;
+        if (lane == 0) ok = issue_item<D, R, KV, kMode>(sm, cta, it, issue);
     } else if (warp >= kConvertWarp0) {
         ok = convert_item<D, R, KV, kMode>(p, sm, cta, it, c, warp, lane);
     }
@@ -998,9 +1026,10 @@ __global__ void __launch_bounds__(Layout<D, R, KV>::kRegisterThreads, 1) tree_ti
                     if (ok) ok = next_item(sm, k, it);
                 }
         } else if (warp == kMmaWarp) {
+            Issue<D, R, KV> issue;
             if (lane == 0)
                 for (int k = 0; ok && it.index >= 0; ++k) {
-                    if (it.tiles > 0) ok = issue_item<D, R, KV, kFast>(sm, cta, it, c);
+                    if (it.tiles > 0) ok = issue_item<D, R, KV, kFast>(sm, cta, it, issue);
                     if (ok) ok = next_item(sm, k, it);
                 }
         } else if (warp == kScoutWarp) {
