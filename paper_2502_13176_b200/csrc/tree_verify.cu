@@ -7,6 +7,11 @@
 // one multiply-add for a token however many were refused; only tokens that have been tried themselves (which leave q, or are
 // its point masses) have values of their own, in a short list.  Sums are fp64: the drawn token is decided by comparing with
 // them, and 32 bits would decide otherwise once in forty draws from 128 000 tokens.
+//
+// A cluster of up to eight blocks to a sequence, which share the vocabulary and add up through one another's shared memory.  Bound by
+// what a walk reads after one another: a pass for each refusal whose mass is asked for, and the draw's share searched from coarse to fine.
+// One chain of five over 32 000 tokens 7.0 us on the device; 16 trees of 32 over 128 000 tokens 26 us, of which the bytes that a walk
+// must read (16 MB) are 2.5; 256 trees of 12 over 152 064 bf16 tokens 61 us (78 MB: 12).
 #include <atomic>
 #include <cmath>
 #include <cstdint>

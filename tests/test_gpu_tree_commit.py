@@ -225,3 +225,83 @@ def test_a_capacity_without_room_for_the_sinks():
     q, k, v = nodes_of(rng, sh, 1, 2)
     commit(c, q, k, v, torch.zeros((1, 1, 2, 2)), np.array([[0, 1]], dtype=np.int32), np.array([2], dtype=np.int32), 2, [20])
     assert int(c.cache.status.item()) == bk.STATUS_BAD_STATE and int(c.cache.len[0, 0, 0]) == 15
+
+
+@pytest.mark.parametrize("kv", ["fp8", "int4"])
+@pytest.mark.parametrize("chunk", [64, 128, 320, 1024])
+def test_rows_of_codes_in_any_chunks(kv, chunk):
+    """Heads and chunks that end inside a group of 128 rows, on it, one before and one behind; holes at both ends; one to many columns."""
+    rng = np.random.default_rng(chunk)
+    sh = bk.make_shape(1, 14, 2, 128, n_sink=2, recent_num=1, recent_den=4)
+    B, T = 9, 40
+    c = Held(sh, [[1104, 400]], B, kv, [[[n, m]] for n, m in ((1, 2), (127, 15), (128, 16), (129, 17), (255, 127), (256, 128), (1023, 257), (1025, 385),
+                                                             (1103, 399))],
+             [[[n, m]] for n, m in ((0, 0), (0, 15), (127, 3), (128, 17), (255, 0), (1, 127), (1023, 256), (77, 384), (1102, 399))], seed=chunk)
+    q, k, v = nodes_of(rng, sh, B, T)
+    path, n = paths_of(rng, B, T, T, "chain")
+    n[:] = [1, 2, 3, 5, 9, 10, 0, 37, 40]                     # 7 to 280 columns
+    lse = lse_of(c, q, k, path, n)
+    commit(c, q, k, v, lse, path, n, T, [40000] * B, chunk=chunk)
+    check(c, q, k, v, lse, path, n, [40000] * B)
+    assert int(c.cache.status.item()) == 0
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "int4"])
+def test_beside_other_calls_and_replayed(kv):
+    """Bit for bit what the calls leave alone: while attention of a tree and another commit run on other streams, and from a graph."""
+    rng = np.random.default_rng(12)
+    sh = bk.make_shape(2, 8, 2, 128, n_sink=3)
+    B, T = 6, 12
+    caps = [[3008, 400], [800, 5008]]
+    held = np.array(caps)[None] - 1 - rng.integers(0, 300, (B, 2, 2))
+    holes = np.minimum(held, rng.integers(0, 400, held.shape))
+    q, k, v = nodes_of(rng, sh, B, T)
+    path, n = paths_of(rng, B, T, 7, "chain")
+    i32 = lambda x: torch.as_tensor(np.asarray(x), dtype=torch.int32).cuda()                  # noqa: E731
+
+    class Call:
+        def __init__(self):
+            self.c = Held(sh, caps, B, kv, held, holes, seed=5)
+            self.plan = bk.baklava_decode_plan(sh, self.c.cap, B, 0, 2, self.c.stride, kv_dtype=FORMATS[kv]).to("cuda")
+            self.ws = bk.tree_commit_workspace(sh, self.plan, 7)
+            self.at = [i32([30000] * B), i32([0] * B)]
+            self.dev = [x.cuda() for x in (q, k, v, torch.full((2, B, 8, T), 9.0))] + [i32(path), i32(n)]
+            torch.cuda.synchronize()
+
+        def __call__(self):
+            bk.baklava_tree_commit(sh, self.c.cache, *self.dev, 7, *self.at, 0, self.plan, self.ws)
+            self.at.reverse()
+
+        def state(self):
+            torch.cuda.synchronize()
+            c = self.c.cache
+            return [x.clone().view(torch.uint8) for x in (c.k_slab, c.v_slab, c.pos, c.score, c.len, c.free_slot)]
+
+    alone, two, three = Call(), Call(), Call()
+    for _ in range(4):
+        alone()
+    want = alone.state()
+    other = Held(sh, caps, B, kv, held, holes, seed=6)
+    tree_plan = bk.baklava_tree_plan(sh, other.cap, B, 1, T, kv_dtype=FORMATS[kv]).to("cuda")
+    tree_ws = bk.decode_workspace(tree_plan)
+    parent = i32(np.tile(np.arange(-1, T - 1), (B, 1)))
+    out, lse = torch.empty((B, 8, T, 128), dtype=torch.bfloat16, device="cuda"), torch.empty((B, 8, T), device="cuda")
+    layer = [x[1].contiguous().cuda() for x in (q, k, v)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        three()
+        three()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for i in range(4):
+        with torch.cuda.stream(streams[0]):
+            two()
+        with torch.cuda.stream(streams[1]):
+            bk.baklava_tree_attn(sh, other.cache, *layer, parent, None, out, lse, tree_plan, tree_ws)
+        if i % 2 == 0:
+            with torch.cuda.stream(streams[2]):
+                graph.replay()
+    for call in (two, three):
+        for x, y in zip(call.state(), want):
+            assert torch.equal(x, y)
+        assert int(call.c.cache.status.item()) == 0
