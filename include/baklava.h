@@ -484,7 +484,10 @@ int baklava_tree_verify(const void* target, int64_t target_stride, const void* d
  *   t_next       device int32 [B] or NULL: t_pos + n_path, the next step's t_pos (not the same array); a sequence that sits
  *                out or is skipped keeps its t_pos
  *   items, info  a plan of baklava_decode_plan for the layer range (the one that the session's decode step has)
- *   ws           device workspace >= baklava_tree_commit_workspace_size(); need not be cleared */
+ *   ws           device workspace >= baklava_tree_commit_workspace_size(); need not be cleared; not shared by calls that
+ *                overlap in time
+ * Errors: BAD_STATE heads and sequences are skipped; a lost wait (FP8 and 4-bit slabs) sets TIMEOUT and leaves rows without their
+ * part of the scores. */
 int baklava_tree_commit(const baklava_shape* shape, const baklava_cache* cache, const void* q, const void* k, const void* v,
                         const float* lse, int32_t T, const int32_t* path, const int32_t* n_path, int32_t max_path,
                         const int32_t* t_pos, int32_t* t_next, uint32_t flags, const int32_t* items,

@@ -33,7 +33,7 @@ using namespace tree;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kJoinThreads = 128, kFreshThreads = 128;
+constexpr int kJoinThreads = 128, kFreshThreads = 128, kOldestThreads = 128;
 constexpr int kMaxTree = BAKLAVA_MAX_TREE;
 constexpr int kMaxEntries = 512;              // of a head's lists that are ranked in one go
 
@@ -156,8 +156,10 @@ __device__ __forceinline__ void write_list(const CommitParams& p, const LeaveLis
     }
 }
 
-// Positions only: the oldest rows of an item.
-__global__ void __launch_bounds__(kThreads) oldest_rows_kernel(const __grid_constant__ CommitParams p) {
+// Positions only: the oldest rows of an item.  (Blocks of four warps: 2 000 chunks are there at once.  One sequence, 32 layers: WINDOW128 us,
+// with eight warps 13.5.)
+__global__ void __launch_bounds__(kOldestThreads) oldest_rows_kernel(const __grid_constant__ CommitParams p) {
+    constexpr int kThreads = kOldestThreads, kWarps = kThreads / 32, kAhead = 8;
     __shared__ LeaveList lists[kWarps];
     const int4 item = p.items[blockIdx.x];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -169,15 +171,15 @@ __global__ void __launch_bounds__(kThreads) oldest_rows_kernel(const __grid_cons
     const int hi = min(item.y + item.z, hd.slots);
     start_list(lists[warp], lane);
     unsigned long long last = ~0ull;
-    for (int j0 = item.y + warp * 32; j0 < hi; j0 += 4 * kThreads) {
-        int pos[4];
+    for (int j0 = item.y + warp * 32; j0 < hi; j0 += kAhead * kThreads) {
+        int pos[kAhead];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kAhead; ++i) {
             const int j = j0 + i * kThreads + lane;
             pos[i] = j < hi && j != hd.hole ? p.c.pos[hd.first + j] : -1;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < kAhead; ++i)
             enlist(lists[warp], pos[i] >= p.n_sink && pos[i] <= job.newest ? leave_key(false, 0.0f, pos[i]) : ~0ull,
                    j0 + i * kThreads + lane, job.leave, last, lane);
     }
@@ -955,7 +957,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_commit(
         if (shape->D == 128) e = launch(fresh_scores_kernel<128>, (unsigned)units, kFreshThreads, pairs + max_path * 256, true, s, p);
         else e = launch(fresh_scores_kernel<64>, (unsigned)units, kFreshThreads, pairs + max_path * 128, true, s, p);
     } else if (p.evict) {
-        e = launch(oldest_rows_kernel, (unsigned)n, kThreads, 0, false, s, p);
+        e = launch(oldest_rows_kernel, (unsigned)n, kOldestThreads, 0, false, s, p);
     }
     if (e != cudaSuccess) return BAKLAVA_ERR_CUDA;
     const bool behind = p.scored || p.evict;
