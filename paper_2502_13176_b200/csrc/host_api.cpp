@@ -4,8 +4,10 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <functional>
 #include <new>
 #include <numeric>
+#include <queue>
 #include <vector>
 
 #include "baklava.h"
@@ -366,47 +368,74 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_plan(const ba
     const int32_t* const c = cap + (size_t)layer * Hkv;
     std::vector<int> heads(Hkv);
     std::iota(heads.begin(), heads.end(), 0);
-    int64_t tokens = 0;
     for (int h : heads) {
         if (c[h] <= 0 || c[h] % shape->page != 0) return BAKLAVA_ERR_INVALID_ARG;
         if (c[h] > INT32_MAX - 256) return BAKLAVA_ERR_UNSUPPORTED;
-        tokens += c[h];
     }
-    tokens *= B;
-    std::stable_sort(heads.begin(), heads.end(), [&](int a, int b) { return c[a] > c[b]; });
     constexpr int kKeys = 128;                               // keys to a tile
     auto pieces_of = [](int64_t rows, int64_t want, int64_t* len) {       // equal pieces of about `want` rows, whole tiles
         const int64_t pieces = (rows + want - 1) / want;
         *len = ((rows + pieces - 1) / pieces + kKeys - 1) / kKeys * kKeys;
         return (rows + *len - 1) / *len;
     };
+    // Heads in the order of their pieces' length: blocks start in that order, and short ones at the end make a short tail.
+    auto order_by_pieces = [&](int64_t want, int64_t* count) {
+        int64_t len;
+        *count = 0;
+        for (int h : heads) *count += pieces_of(c[h], want, &len) * B;
+        std::stable_sort(heads.begin(), heads.end(), [&](int a, int b) {
+            int64_t la, lb;
+            pieces_of(c[a], want, &la);
+            pieces_of(c[b], want, &lb);
+            return la > lb;
+        });
+    };
     // One block to an SM goes from item to item.  Where every item can have an SM of its own, equal chunks, the shortest with which
-    // that is so; else chunks of up to 4 096 rows first, for half of the rows, then shorter ones towards a short tail.
-    int64_t want = chunk_tokens, len;
-    bool graded = false;
+    // that is so.  Else the chunks under which the last SM is through first, with what an item costs besides its rows (384 rows'
+    // time: its first tiles, its last rows) and its partials, which are written and read once more (2 g T / SMs rows' time).  16 sequences,
+    // 8 heads of 2 288 to 16 544 rows, 64 nodes over FP8 rows: 288 us with chunks of 4 096 for half of the rows, then shorter ones,
+    // 257 with these (8 nodes over 4 bits 213, 196; 32 sequences, 16 nodes, bf16 241, 228).
+    int64_t want = chunk_tokens, count = 0, len;
     if (want == 0) {
         for (want = 2 * kKeys; want < 4096; want += kKeys) {
-            int64_t count = 0;
+            count = 0;
             for (int h : heads) count += pieces_of(c[h], want, &len) * B;
             if (count <= n_sm) break;
         }
-        graded = want >= 2048;
-        if (graded) want = std::max<int64_t>(1024, std::min<int64_t>(4096, tokens / (2 * (int64_t)n_sm)));
+        if (want >= 2048) {
+            constexpr int64_t kItemRows = 384;
+            const double partial_rows = 2.0 * (shape->Hq / Hkv) * T / n_sm;
+            const int64_t longest = *std::max_element(c, c + Hkv), most = std::max<int64_t>(8ll * n_sm, (int64_t)B * Hkv);
+            double least = 0.0;
+            int64_t best = 0;
+            for (int64_t w = 4 * kKeys; w < longest + kKeys || best == 0; w += std::max<int64_t>(kKeys, w / 32 / kKeys * kKeys)) {
+                order_by_pieces(w, &count);
+                if (count > most && w < longest) continue;
+                std::priority_queue<int64_t, std::vector<int64_t>, std::greater<int64_t>> sm;
+                for (int i = 0; i < n_sm; ++i) sm.push(0);
+                int64_t last = 0;
+                for (int h : heads) {
+                    const int64_t pieces = pieces_of(c[h], w, &len);
+                    for (int64_t n = 0; n < pieces * B; ++n) {
+                        const int64_t through = sm.top() + std::min(len, c[h] - n % pieces * len) + kItemRows;
+                        sm.pop();
+                        sm.push(through);
+                        last = std::max(last, through);
+                    }
+                }
+                const double cost = (double)last + partial_rows * (double)count;
+                if (best == 0 || cost < least) { best = w; least = cost; }
+            }
+            want = best;
+        }
     }
     want = std::max<int64_t>(kKeys, (want + kKeys - 1) / kKeys * kKeys);
-    int64_t n_items = 0, done = 0;
+    order_by_pieces(want, &count);
+    int64_t n_items = 0;
     for (int h : heads) {
+        const int64_t pieces = pieces_of(c[h], want, &len);
+        if (pieces > 32767) return BAKLAVA_ERR_UNSUPPORTED;
         for (int b = 0; b < B; ++b) {
-            int64_t now = want;
-            if (graded) {
-                if (done * 20 >= tokens * 19) now = want / 8;
-                else if (done * 5 >= tokens * 4) now = want / 4;
-                else if (done * 2 >= tokens) now = want / 2;
-                now = std::max<int64_t>(4 * kKeys, now);
-            }
-            done += c[h];
-            const int64_t pieces = pieces_of(c[h], now, &len);
-            if (pieces > 32767) return BAKLAVA_ERR_UNSUPPORTED;
             for (int64_t pc = 0; pc < pieces; ++pc, ++n_items) {
                 if (!items_out) continue;
                 if (n_items >= items_capacity) return BAKLAVA_ERR_WORKSPACE;

@@ -16,9 +16,9 @@
 // heads) forms the ancestors' part from the nodes' own keys and values, beside the first kernel, then waits for it and joins the partials.
 //
 // What bounds it (per layer; B200, 6.54 TB/s, 1.63 PFLOP/s): bf16 slabs the bytes once there are enough of them: 32 sequences, 8 heads
-// of 9 824 rows, 16 nodes of 32 heads: 241 us for 1.30 GB, 213 of them in the first kernel (6.1 TB/s).  A single sequence of that shape is
+// of 9 824 rows, 16 nodes of 32 heads: 228 us for 1.30 GB (5.7 TB/s with start, tail and join).  A single sequence of that shape is
 // 40 MB, 6.2 us of bytes, and takes 23: a block's way to its first tile, its last rows, the join.  Codes: the work between the bytes
-// and the product.  64 nodes over 16 sequences of FP8 rows 290 us (101 us of products at the peak rate), 8 nodes over 4-bit rows 215 us
+// and the product.  64 nodes over 16 sequences of FP8 rows 257 us (101 us of products at the peak rate), 8 nodes over 4-bit rows 196 us
 // (26.5 us of bytes): two softmax streams of one busy warp each, 5 200 cycles for 128 rows, and conversion beside them.
 #include <cuda_fp16.h>
 
