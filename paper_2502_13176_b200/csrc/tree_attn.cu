@@ -1352,8 +1352,10 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_attn(
     p.layer = info->layer_begin;
     const int kv = cache->kv_dtype;
     p.rows_per_head = (T + 7) / 8 * 8;
-    // query heads that the accumulators have room for: two, one where queries have two terms
-    const int accs = kv == BAKLAVA_KV_INT4 ? 1 : kv == BAKLAVA_KV_BF16 && info->n_items <= 2 * 148 ? 1 : 2, most = accs * kRows / p.rows_per_head;
+    // Query heads that the accumulators have room for: two, one where queries have two terms.  One also where a chunk has an SM for itself: a
+    // group is then divided among two blocks, which between them fill the SMs that are idle (16 ragged sequences, g = 7, 27 nodes: 39 us,
+    // 47 with two), while in longer launches the second reading of the slab costs more (16 long sequences, 40 nodes: 221 us, 208 with two).
+    const int accs = kv == BAKLAVA_KV_INT4 ? 1 : kv == BAKLAVA_KV_BF16 && info->n_items <= 148 ? 1 : 2, most = accs * kRows / p.rows_per_head;
     p.parts = (p.g + most - 1) / most;
     p.heads = (p.g + p.parts - 1) / p.parts;
     p.scale_log2 = kLog2e / sqrtf((float)shape->D);
