@@ -442,8 +442,10 @@ int baklava_tree_plan(const baklava_shape* shape, const int32_t* cap, int32_t B,
  * When no child is left the next token is drawn from r: the lowest v with r(0) + .. + r(v) > u_sample[b] * (sum of r).
  * q is the distribution that n's children were drawn from: draft[b, n]; with BAKLAVA_VERIFY_DISTINCT (siblings drawn without
  * replacement) a refused token leaves it, q(v) <- 0 and q <- q / (1 - what has left); with draft = NULL (children chosen, not
- * drawn) q is 1 at x and 0 elsewhere.  Everything is computed in fp64 from the given values; the accepted tokens and the
- * next one are then distributed as the target's own (speculative sampling).
+ * drawn) q is 1 at x and 0 elsewhere.  What refusals leave of r is known to 2^-52 of target[b, n]'s values: where they leave less
+ * than that (siblings that are not distinct, or that use up their distribution), rounding decides whether anything is left.
+ * Everything is computed in fp64 from the given values; the accepted tokens and the next one are then distributed as the
+ * target's own (speculative sampling).
  *   target, draft     device, [B, T] rows of V probabilities >= 0, rows target_stride (draft_stride) >= V elements apart,
  *                     fp32 or bf16 (prob_dtype); what is not above 0 (NaN) counts as 0
  *   tokens, parent    device int32 [B, T]; n_nodes device int32 [B] or NULL

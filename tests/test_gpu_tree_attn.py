@@ -240,8 +240,9 @@ def test_repeated_replayed_and_side_by_side():
     assert torch.equal(outs[2], again)
 
 
-@pytest.mark.parametrize("kv,T,D", [("bf16", 8, 128), ("bf16", 64, 128), ("bf16", 16, 64), ("fp8", 8, 128), ("fp8", 64, 128), ("int4", 8, 128), ("int4", 40, 128)])
-def test_long_heads_side_by_side(kv, T, D):
+@pytest.mark.parametrize("kv,T,D,chunk", [("bf16", 8, 128, 0), ("bf16", 64, 128, 0), ("bf16", 64, 128, 1024), ("bf16", 16, 64, 0), ("bf16", 64, 64, 1536),
+                                          ("fp8", 8, 128, 0), ("fp8", 64, 128, 0), ("int4", 8, 128, 0), ("int4", 40, 128, 0), ("int4", 40, 128, 640)])
+def test_long_heads_side_by_side(kv, T, D, chunk):
     """A device full of long items, where loads are late: the same bits every time and for other inputs in between, right where
     looked at."""
     rng = np.random.default_rng(16)
@@ -251,9 +252,9 @@ def test_long_heads_side_by_side(kv, T, D):
     held = np.array(caps)[None] - 1 - rng.integers(0, 900, (B, 1, 8))
     c = Held(sh, caps, B, kv, held, np.minimum(held, rng.integers(0, 16000, held.shape)), seed=7, poison=kv != "bf16")
     q, k, v, parent = inputs(rng, sh, B, T)
-    ref, rz = run(c, q, k, v, parent, None)
+    ref, rz = run(c, q, k, v, parent, None, chunk=chunk)
     for i in range(6):
-        out, z = run(c, q, k, v, parent, None)
+        out, z = run(c, q, k, v, parent, None, chunk=chunk)
         assert torch.equal(out, ref) and torch.equal(z, rz), i
     for b, h in ((0, 0), (5, 6), (3, 1)):
         rows = c.rows(b, 0, h)
@@ -269,7 +270,8 @@ def test_long_heads_side_by_side(kv, T, D):
             assert (np.abs(ref[b, y, i].double().cpu().numpy() - want[:, i]) <= bo).all()
 
 
-@pytest.mark.parametrize("kv,T,D", [("bf16", 8, 128), ("bf16", 64, 128), ("bf16", 16, 64), ("fp8", 16, 128), ("fp8", 64, 128), ("int4", 16, 128), ("int4", 48, 128)])
+@pytest.mark.parametrize("kv,T,D", [("bf16", 8, 128), ("bf16", 64, 128), ("bf16", 16, 64), ("bf16", 47, 64), ("fp8", 16, 128), ("fp8", 64, 128),
+                                    ("int4", 16, 128), ("int4", 48, 128)])
 def test_many_short_heads(kv, T, D):
     """Several items to a block, most of them of one tile, some of more, some of none: the same bits every time, and right
     where looked at."""

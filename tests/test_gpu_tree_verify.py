@@ -144,3 +144,34 @@ def test_repeated_and_replayed():
     torch.cuda.synchronize()
     for x, r in zip(outs, ref):
         np.testing.assert_array_equal(x.cpu().numpy(), r)
+
+
+@pytest.mark.parametrize("V", [1, 2, 7, 40])
+def test_the_same_token_twice_among_distinct_siblings(V):
+    """What should not be there: a token that has left already has nothing of q any more, and nothing of what is left of the target.
+
+    Once all of q has left but for one token, r and q / left are both one there, and every further refusal takes all but a rounding of r.
+    What is left is formed as p - K q, to 2^-52 of p: equality can be asked for while it is above 2^-30 of p, as then 22 bits of
+    it are right and the comparisons of this test's random numbers (24 bits) are decided by less than one in a million of them."""
+    t, d, tok, par, _, ua, us, _ = case(20 + V, 40, 16, V, "drawn", tree="star", like=1.5)
+    path, count, token, status = verify(t, d, tok, par, None, ua, us, bk.VERIFY_DISTINCT)
+    t64, d64 = t.double().cpu().numpy(), d.double().cpu().numpy()
+    sure = 0
+    for b in range(40):
+        want, nxt = ot.verify(t64[b], d64[b], tok[b], par[b], 16, np.float32(ua[b]), np.float32(us[b]), True)
+        got = path[b, :count[b]].tolist(), int(token[b])
+        assert got[0][0] == 0 and all(par[b, c] == p for p, c in zip(got[0], got[0][1:])) and 0 <= got[1] < V
+        mass = least = 1.0
+        r, gone = t64[b, 0], np.zeros(V, dtype=bool)
+        for c in range(1, want[1] if len(want) > 1 else 16):  # the refused children of the root
+            if par[b, c] == 0:
+                left = 1 - d64[b, 0][gone].sum()
+                rest = np.maximum(r - np.where(gone, 0, d64[b, 0] / left), 0) if left > 0 else r
+                gone[tok[b, c]] = True
+                mass *= rest.sum()
+                least = min(least, mass)
+                r = rest / rest.sum() if rest.sum() > 0 else t64[b, 0]
+        if least > 2.0 ** -30:
+            sure += 1
+            assert got == (want, nxt), b
+    assert status == 0 and (V < 7 or sure > 10), sure
