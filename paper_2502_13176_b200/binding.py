@@ -508,16 +508,17 @@ def baklava_tree_attn(shape, cache, q, k, v, parent, n_nodes, out, lse, plan, ws
 
 
 def _probabilities(t, what, dev, shape, dtype):
-    """Pointer and row stride of probabilities [B, T, V]: rows contiguous, all the same distance apart."""
+    """Pointer and row stride of probabilities [B, T, V]: rows contiguous, all the same distance apart, at least a row (rows that
+    repeat, as expand() makes them, or overlap are none that a stride could reach)."""
     B, T, V = shape
     st = t.stride()
-    row = st[1] if T > 1 else st[0]
-    if t.dtype is not dtype or t.shape != shape or st[2] != 1 and V > 1 or B > 1 and T > 1 and st[0] != T * st[1]:
-        raise ValueError("%s: expected %s [%d, %d, %d] with contiguous rows at one distance, got %s %s with strides %s"
+    row = st[1] if T > 1 else st[0] if B > 1 else V           # (the stride of a single row means nothing)
+    if t.dtype is not dtype or t.shape != shape or st[2] != 1 and V > 1 or B > 1 and T > 1 and st[0] != T * st[1] or row < V:
+        raise ValueError("%s: expected %s [%d, %d, %d] with contiguous rows at one distance of at least a row, got %s %s with strides %s"
                          % (what, dtype, B, T, V, t.dtype, tuple(t.shape), st))
     if t.get_device() != dev:
         _elsewhere(t, what, dev)
-    return t.data_ptr(), row if row > V else V
+    return t.data_ptr(), row
 
 
 def baklava_tree_verify(target, draft, tokens, parent, n_nodes, u_accept, u_sample, path, n_path, next_token, status, flags=0,
