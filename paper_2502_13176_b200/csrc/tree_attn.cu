@@ -1129,7 +1129,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32, 5) tree_join_kernel(const __g
     extern __shared__ __align__(16) uint8_t smem_raw[];
     const int4 item = p.items[blockIdx.x];
     const int pieces = item.w >> 16;
-    if ((item.w & 0xffff) != 0) return;
+    if ((item.w & 0xffff) != 0) return;                       // (never the plan's first item)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const Unit u(p.c, p.layer, item.x);
     __nv_bfloat16* const keys = reinterpret_cast<__nv_bfloat16*>(smem_raw);
@@ -1151,11 +1151,14 @@ __global__ void __launch_bounds__(kJoinWarps * 32, 5) tree_join_kernel(const __g
             load_bf16<kE>(p.q + u.b * p.sq.seq + (int64_t)(u.h * p.g + a0 + min(h, heads - 1)) * p.sq.head + i * p.sq.token, lane, q[h]);
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    if (i >= n) return;
     const bool fine = (lane >= n || (parent[lane] >= -1 && parent[lane] < lane)) &&
                       (lane + 32 >= n || (parent[lane + 32] >= -1 && parent[lane + 32] < lane + 32));
-    if (!__all_sync(0xffffffffu, fine)) {
-        if (lane == 0) atomicOr(p.c.status, BAKLAVA_STATUS_BAD_STATE);
+    const bool tree = __all_sync(0xffffffffu, fine);
+    if (i >= n || !tree) {
+        if (i < n && lane == 0) atomicOr(p.c.status, BAKLAVA_STATUS_BAD_STATE);
+        // (Where no sequence has a row to be written, nothing else would keep this grid from completing before the first kernel does, and
+        // what follows on the stream would begin beside that.  One item's blocks do for all: the others leave their places.)
+        if (blockIdx.x == 0) grid_dependency_wait();
         return;
     }
     // logits of the way up, log2 domain: lane d holds those of the d-th node, and of the one 32 further
