@@ -862,10 +862,10 @@ __device__ __forceinline__ bool write_rows(const TreeParams& p, Shared& sm, cons
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 float y = __uint_as_float(v[col >> 4 & 1][e]);
-                worst = fmaf(fabsf(y), 0x1p-20f, worst);                // NaN propagates through the sum, infinities too
                 const int d = KV == BAKLAVA_KV_INT4 ? (e & 8) + ((e & 7) >> 1) + 4 * (e & 1) : e;
                 if (KV == BAKLAVA_KV_FP8_E4M3) y *= v_scale;
                 if (KV == BAKLAVA_KV_INT4) y *= four[2 * D + col + d];
+                worst = fmaf(fabsf(y), 0x1p-20f, worst);                // as it is written; NaN propagates through the sum, infinities too
                 x[d >> 3][d & 7] = y;
             }
             bad = bad || !(worst <= kFinite);
