@@ -430,7 +430,7 @@ int baklava_tree_attn(const baklava_shape* shape, const baklava_cache* cache,
                       const int32_t* items, const baklava_plan_info* info, void* ws, size_t ws_bytes, void* stream);
 
 /* The work list of baklava_tree_attn for one layer (host; arguments and use as baklava_decode_plan's; a plan serves
- * trees of up to T nodes). */
+ * trees of up to T nodes; chunks have at most 2^19 rows, whatever chunk_tokens says). */
 int baklava_tree_plan(const baklava_shape* shape, const int32_t* cap, int32_t B, int32_t layer, int32_t T,
                       int32_t chunk_tokens, int32_t n_sm, int32_t kv_dtype, int32_t* items_out, int64_t items_capacity,
                       baklava_plan_info* info);

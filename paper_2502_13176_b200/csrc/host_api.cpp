@@ -373,6 +373,9 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_plan(const ba
         if (c[h] > INT32_MAX - 256) return BAKLAVA_ERR_UNSUPPORTED;
     }
     constexpr int kKeys = 128;                               // keys to a tile
+    // Rows of a chunk at most.  Some of a block's warps wait from its chunk's first tile to its last, and a wait is given up after
+    // 10^8 cycles; a row takes 25 (bf16) to 60 (FP8, two accumulators) when the device is full, so that this leaves three times as much.
+    constexpr int64_t kMostRows = 1 << 19;
     auto pieces_of = [](int64_t rows, int64_t want, int64_t* len) {       // equal pieces of about `want` rows, whole tiles
         const int64_t pieces = (rows + want - 1) / want;
         *len = ((rows + pieces - 1) / pieces + kKeys - 1) / kKeys * kKeys;
@@ -405,7 +408,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_plan(const ba
         if (want >= 2048) {
             constexpr int64_t kItemRows = 384;
             const double partial_rows = 2.0 * (shape->Hq / Hkv) * T / n_sm;
-            const int64_t longest = *std::max_element(c, c + Hkv), most = std::max<int64_t>(8ll * n_sm, (int64_t)B * Hkv);
+            const int64_t longest = std::min<int64_t>(kMostRows, *std::max_element(c, c + Hkv)), most = std::max<int64_t>(8ll * n_sm, (int64_t)B * Hkv);
             double least = 0.0;
             int64_t best = 0;
             for (int64_t w = 4 * kKeys; w < longest + kKeys || best == 0; w += std::max<int64_t>(kKeys, w / 32 / kKeys * kKeys)) {
@@ -429,7 +432,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_plan(const ba
             want = best;
         }
     }
-    want = std::max<int64_t>(kKeys, (want + kKeys - 1) / kKeys * kKeys);
+    want = std::min(kMostRows, std::max<int64_t>(kKeys, (want + kKeys - 1) / kKeys * kKeys));
     order_by_pieces(want, &count);
     int64_t n_items = 0;
     for (int h : heads) {
