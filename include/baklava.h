@@ -484,7 +484,8 @@ int baklava_tree_verify(const void* target, int64_t target_stride, const void* d
  *                0 .. T - 1: the sequence is skipped with BAD_STATE)
  *   t_pos        device int32 [B], above every position in the cache
  *   t_next       device int32 [B] or NULL: t_pos + n_path, the next step's t_pos (not the same array); a sequence that sits
- *                out or is skipped keeps its t_pos
+ *                out or is skipped keeps its t_pos (one with some heads in a bad state goes on: the others have taken
+ *                the path)
  *   items, info  a plan of baklava_decode_plan for the layer range (the one that the session's decode step has)
  *   ws           device workspace >= baklava_tree_commit_workspace_size(); need not be cleared; not shared by calls that
  *                overlap in time

@@ -61,18 +61,19 @@ struct Job {
     int a, t0;                      // joining rows, position of the first
     int leave;                      // rows that leave
     int newest;                     // rows at positions up to this may leave
-    bool idle, bad, overflow;
+    bool idle, wrong, bad, overflow;         // wrong: of the whole sequence; bad: wrong, or the head's own state cannot be
     __device__ __forceinline__ Job(const CommitParams& p, const Unit& u, const Head& hd) {
         a = p.n_path[u.b];
         t0 = p.t_pos[u.b];
         idle = t0 < 0 || a == 0;
-        bad = !idle && (hd.bad || a < 0 || a > p.max_path || t0 > INT32_MAX - kMaxTree);
-        if (!idle && !bad) {
+        wrong = !idle && (a < 0 || a > p.max_path || t0 > INT32_MAX - kMaxTree);
+        if (!idle && !wrong) {
             const int32_t* const path = p.path + (int64_t)u.b * p.T;
             bool off = false;
             for (int i = threadIdx.x & 31; i < a; i += 32) off = off || path[i] < 0 || path[i] >= p.T;
-            bad = __any_sync(0xffffffffu, off);
+            wrong = __any_sync(0xffffffffu, off);
         }
+        bad = !idle && (wrong || hd.bad);
         leave = p.evict ? max(0, hd.n + a - (hd.C - 1)) : 0;
         overflow = !p.evict && hd.n + a > hd.C;
         const long long window = max(0ll, (long long)(hd.C - 1 - p.n_sink) * p.recent_num / p.recent_den);
@@ -648,7 +649,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_rows_kernel(const __grid_co
     const Head hd(p.c, u);
     const Job job(p, u, hd);
     grid_dependency_wait();                                   // (the first kernel reads a head's state, this one changes it)
-    if (p.t_next && u.li == 0 && u.h == 0 && tid == 0) p.t_next[u.b] = job.idle || job.bad ? p.t_pos[u.b] : job.t0 + job.a;
+    // (by the sequence alone: where this head is in a bad state the others have taken the path)
+    if (p.t_next && u.li == 0 && u.h == 0 && tid == 0) p.t_next[u.b] = job.idle || job.wrong ? p.t_pos[u.b] : job.t0 + job.a;
     if (job.idle) return;
     if (job.bad || job.overflow) {
         if (tid == 0) atomicOr(p.c.status, job.bad ? BAKLAVA_STATUS_BAD_STATE : BAKLAVA_STATUS_OVERFLOW);
