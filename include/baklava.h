@@ -74,6 +74,8 @@ extern "C" {
 #define BAKLAVA_FLAG_NO_EVICT      4u   /* never evict; a cache that fills up stays full              */
 #define BAKLAVA_FLAG_OVERLAP_PREV   8u   /* this call may start while the work in front of it on the   */
                                         /*   stream is still finishing (see baklava_decode_attn)      */
+#define BAKLAVA_FLAG_ROW_QUOTIENT  16u   /* baklava_tree_commit: 4-bit rows join with the scale max |y| / 7 that the   */
+                                        /*   other calls write                                          */
 #define BAKLAVA_FLAG_TEST_STALL  256u   /* test aid, never set it in production: the first chunk of   */
                                         /*   every head is fed its first 64 rows only, so               */
                                         /*   that the bounded wait for the next ones runs out and the   */
@@ -471,7 +473,9 @@ int baklava_tree_verify(const void* target, int64_t target_stride, const void* d
  *   3. if it then holds more than cap - 1 rows, it is cut to cap - 1 by the retention policy as baklava_evict does it (sinks
  *      and the last W positions stay, of the rest the lowest scores go, among equal ones the latest; W as for the decode
  *      step, positions counted from t_pos[b] + a - 1)                                                     (Eq. 5-6)
- * 4-bit rows join with the scale max |y| * fl32(1 / 7), which may differ by one rounding from the other calls' quotient.
+ * With ROW_QUOTIENT 4-bit rows join as every other call writes them, so that a token's bits do not depend on whether it was
+ * drafted or decoded; without it their scale is max |y| * fl32(1 / 7), which may differ from that by one rounding (a code near a
+ * tie then too).  Rows of both kinds are valid and may lie in one slab.
  * Rows that stay keep their slots.  The joining rows that stay take the free slots in ascending order; the next free
  * slot becomes free_slot.  Freed slots keep what they held.  Flags as for the decode step: NO_SCORE leaves scores as they are
  * (joining rows have 0) and implies NO_EVICT except under sinks + window, where the oldest rows go; NO_EVICT: a path that does

@@ -17,6 +17,7 @@ import torch
 OK = 0
 FLAG_NO_APPEND, FLAG_NO_SCORE, FLAG_NO_EVICT = 1, 2, 4
 FLAG_OVERLAP_PREV = 8
+FLAG_ROW_QUOTIENT = 16
 FLAG_TEST_STALL = 256
 SCOPE_LAYER, SCOPE_MODEL = 0, 1
 STATUS_OVERFLOW, STATUS_BAD_STATE, STATUS_TIMEOUT = 1, 2, 4

@@ -1,7 +1,7 @@
 // 4-bit rows for quantised K/V slabs (device side).  With y = x * (1 / channel scale) in fp32 (the reciprocal is the
 // caller's), a row's scale is s = max |y| / 7 and an element's code u = clamp(rint(y / s), -7, 7) + 8 in 1 .. 15 (8 in a
 // row of zeros); it stands for (u - 8) * s * channel scale.  Both quotients are IEEE divisions, so every
-// implementation that divides in fp32 gets the same codes bit for bit.  A byte holds an even channel in its low half
+// implementation that divides in fp32 gets the same codes bit for bit (baklava_tree_commit does with BAKLAVA_FLAG_ROW_QUOTIENT).  A byte holds an even channel in its low half
 // and the next one in its high half.
 #pragma once
 #include <cuda_bf16.h>

@@ -53,6 +53,7 @@ struct CommitParams {
     float* fresh;                   // [n_units][max_path]: the joining rows' scores
     int32_t T, g, D, Hq, layer_begin, max_path, n_sink, recent_num, recent_den;
     int32_t scored, evict;          // scores are kept; rows may leave
+    int32_t quotient;               // 4-bit rows join with the quotient as their scale
     float scale_log2;
 };
 
@@ -818,10 +819,10 @@ __global__ void __launch_bounds__(kJoinThreads) join_rows_kernel(const __grid_co
             } else {
                 float y[4];
                 int4q::scaled4(raw, *reinterpret_cast<const float4*>(p.c.kv_scale + ((int64_t)u.head * 4 + 2 * which + 1) * 128 + 4 * lane), y);
-                // The scale by the reciprocal of 7, which is what array libraries make of a division by a constant: rows that
-                // were quantised by such code and rows that join here agree bit for bit (from the other calls' quotient it is
-                // one rounding away).
-                const float s = __fmul_rn(__uint_as_float(__reduce_max_sync(0xffffffffu, int4q::largest_bits(y))), 1.0f / 7.0f);
+                // The format's scale, or the one by the reciprocal of 7, one rounding away from it at most, which is what array
+                // libraries make of a division by a constant.
+                const uint32_t top_bits = __reduce_max_sync(0xffffffffu, int4q::largest_bits(y));
+                const float s = p.quotient ? int4q::row_scale(top_bits) : __fmul_rn(__uint_as_float(top_bits), 1.0f / 7.0f);
                 *reinterpret_cast<uint16_t*>(slab + row * 64 + 2 * lane) = (uint16_t)int4q::codes4(y, s);
                 if (lane == 0) p.c.row_scale[2 * row + which] = s;
             }
@@ -907,7 +908,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_commit(
     if (rc) return rc;
     if (!cache || !k || !v || !path || !n_path || !t_pos || !items || !info || !ws || T <= 0 || max_path <= 0 || max_path > T)
         return BAKLAVA_ERR_INVALID_ARG;
-    if (flags & ~(BAKLAVA_FLAG_NO_SCORE | BAKLAVA_FLAG_NO_EVICT)) return BAKLAVA_ERR_INVALID_ARG;
+    if (flags & ~(BAKLAVA_FLAG_NO_SCORE | BAKLAVA_FLAG_NO_EVICT | BAKLAVA_FLAG_ROW_QUOTIENT)) return BAKLAVA_ERR_INVALID_ARG;
     const bool scored = !(flags & BAKLAVA_FLAG_NO_SCORE);
     if (scored && (!q || !lse)) return BAKLAVA_ERR_INVALID_ARG;
     if (t_next == t_pos) return BAKLAVA_ERR_INVALID_ARG;
@@ -945,6 +946,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_commit(
     p.n_sink = shape->n_sink; p.recent_num = shape->recent_num; p.recent_den = shape->recent_den;
     p.scored = scored;
     p.evict = !(flags & BAKLAVA_FLAG_NO_EVICT) && (scored || shape->recent_num == shape->recent_den);
+    p.quotient = flags & BAKLAVA_FLAG_ROW_QUOTIENT ? 1 : 0;
     p.scale_log2 = kLog2e / sqrtf((float)shape->D);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t e = cudaSuccess;

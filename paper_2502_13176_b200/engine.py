@@ -176,10 +176,10 @@ class DecodeSession:
 
     def commit(self, path, n_path, t_pos, flags=0):
         """The accepted path (as `verify` returned it) into all layers' slabs: scores, append, eviction.  t_pos: device int32 [B],
-        the position of each path's first token; returns the next step's."""
+        the position of each path's first token; returns the next step's.  4-bit rows have the bits that a decode step gives them."""
         t_next = torch.empty_like(t_pos)
         bk.baklava_tree_commit(self.shape, self.cache, self.tree_q, self.tree_k, self.tree_v, self.tree_lse, path, n_path, self.max_path,
-                               t_pos, t_next, flags, self.plan, self.commit_ws)
+                               t_pos, t_next, flags | bk.FLAG_ROW_QUOTIENT, self.plan, self.commit_ws)
         return t_next
 
     def retained_kv_bytes(self):
