@@ -61,7 +61,7 @@ class DecodeSession:
         nl = self.le - self.lb
         self.out = torch.zeros((nl, w.B, w.Hq, w.D), dtype=torch.bfloat16, device=self.device)
         self.lse = torch.zeros((nl, w.B, w.Hq), dtype=torch.float32, device=self.device)
-        self.t = 0
+        self.t = 0                                   # position of the next `step`; None after a `commit`: the device has it, per sequence
         self.prompt_error = None
 
     def prefill_synthetic(self, prompt_len=None, data=None):
@@ -108,8 +108,11 @@ class DecodeSession:
         return out
 
     def step(self, q, k_new, v_new, flags=0):
-        """One decode step for the session's layer range; returns the output tensor (device, bf16)."""
-        bk.baklava_decode_attn(self.shape, self.cache, q, k_new, v_new, self.t, self.out, self.lse, flags,
+        """One decode step for the session's layer range, all sequences at position `t`; returns the output tensor (device, bf16).
+        After a `commit` the positions are what that returned: the next step is `step_varlen`'s (or `t` is set anew)."""
+        if self.t is None and not flags & bk.FLAG_NO_APPEND:
+            raise RuntimeError("a commit has moved the sequences on: step_varlen with the positions that it returned")
+        bk.baklava_decode_attn(self.shape, self.cache, q, k_new, v_new, self.t or 0, self.out, self.lse, flags,
                                self.plan, self.ws)
         if not (flags & bk.FLAG_NO_APPEND):
             self.t += 1
@@ -176,10 +179,11 @@ class DecodeSession:
 
     def commit(self, path, n_path, t_pos, flags=0):
         """The accepted path (as `verify` returned it) into all layers' slabs: scores, append, eviction.  t_pos: device int32 [B],
-        the position of each path's first token; returns the next step's.  4-bit rows have the bits that a decode step gives them."""
+        the position of each path's first token; returns the next step's (of `tree_layer` and `commit` or of `step_varlen`).  4-bit rows have the bits that a decode step gives them."""
         t_next = torch.empty_like(t_pos)
         bk.baklava_tree_commit(self.shape, self.cache, self.tree_q, self.tree_k, self.tree_v, self.tree_lse, path, n_path, self.max_path,
                                t_pos, t_next, flags | bk.FLAG_ROW_QUOTIENT, self.plan, self.commit_ws)
+        self.t = None
         return t_next
 
     def retained_kv_bytes(self):
