@@ -363,7 +363,7 @@ extern "C" __attribute__((visibility("default"))) int baklava_tree_plan(const ba
     if (!cap || !info || B <= 0 || T <= 0 || layer < 0 || layer >= shape->L) return BAKLAVA_ERR_INVALID_ARG;
     if (chunk_tokens < 0 || (chunk_tokens == 0 && n_sm <= 0)) return BAKLAVA_ERR_INVALID_ARG;
     if (kv_dtype != BAKLAVA_KV_BF16 && kv_dtype != BAKLAVA_KV_FP8_E4M3 && kv_dtype != BAKLAVA_KV_INT4) return BAKLAVA_ERR_INVALID_ARG;
-    if (T > BAKLAVA_MAX_TREE) return BAKLAVA_ERR_UNSUPPORTED;
+    if (T > BAKLAVA_MAX_TREE || B > 65535) return BAKLAVA_ERR_UNSUPPORTED;        // (what the call refuses)
     const int Hkv = shape->Hkv;
     const int32_t* const c = cap + (size_t)layer * Hkv;
     std::vector<int> heads(Hkv);

@@ -13,6 +13,18 @@ def _built():
     bkbuild.build()
 
 
+@pytest.mark.parametrize("B", [65536, 1 << 20, 2147483647])
+def test_more_sequences_than_a_call_takes(B):
+    """Refused as the call refuses them, before a list of billions of chunks is gone through."""
+    with pytest.raises(bk.BaklavaError) as e:
+        bk.baklava_tree_plan(bk.make_shape(1, 4, 1, 128), [[16]], B, 0, 8)
+    assert e.value.code == -7
+
+
+def test_as_many_as_it_takes():
+    assert len(bk.baklava_tree_plan(bk.make_shape(1, 4, 1, 128), [[16]], 65535, 0, 8).items) == 65535
+
+
 @pytest.mark.parametrize("kv", [bk.KV_BF16, bk.KV_INT4])
 @pytest.mark.parametrize("B,caps,chunk", [(148, [[1 << 22]], 0), (1, [[1 << 24, 4096]], 1 << 30), (1, [[1 << 24, 4096]], 0), (300, [[600000, 16]], 0),
                                           (2, [[LONGEST, LONGEST + 16]], 1 << 30), (1, [[2147483376, 16]], 2147483647), (1, [[2147483376, 16]], 0)])
