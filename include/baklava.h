@@ -121,7 +121,7 @@ typedef struct baklava_shape {
  * reciprocals are passed alongside so that every implementation multiplies by the same number.
  * baklava_decode_attn(_varlen) and baklava_evict(_varlen) quantise the rows they write (k_new / v_new,
  * the dense prompt) and read the slabs accordingly; queries stay bf16 (they must be finite in fp16:
- * |q| < 65504).  Only D = 128.  Everything else (positions, scores, policy) is unchanged.
+ * |q| < 65504, and what is below 2^-17 of them counts to 2^-25).  Only D = 128.  Everything else (positions, scores, policy) is unchanged.
  *
  * With kv_dtype = BAKLAVA_KV_INT4 a row is D / 2 bytes of 4-bit codes (an even channel in the low half of its byte)
  * and one fp32 scale of its own for K and one for V, beside caller-chosen fp32 scales per channel of each (l, h) (keys
@@ -414,8 +414,9 @@ int baklava_evict_varlen(const baklava_shape* shape, const baklava_cache* cache,
  *   out[b, h, i] = sum_j softmax_j(q_i . k_j / sqrt(D)) v_j  over the valid rows j of the slab (Eq. 7) and over node i
  * and its ancestors in the tree, whose keys and values are k and v; lse is the natural-log normaliser.  The cache is not
  * changed.  A node's result depends on nothing else: not on other branches, freed slots or rows behind the last one,
- * whatever they hold (NaN and infinities among them).  Sums are held in fp32; probabilities are rounded to 16 bits for the
- * product with V.  Quantised slabs as described above; k and v of the nodes are taken as they are.
+ * whatever they hold (NaN and infinities among them).  Sums are held in fp32; probabilities are rounded to bf16, 2^-8 of each,
+ * for the product with V (over quantised slabs too, where the decode step has them in fp16).  Quantised slabs as described
+ * above; k and v of the nodes are taken as they are (the decode step attends to its new row as the slab has it).
  *   q, out       device bf16 [B, Hq, T, D] under their strides (not overlapping)
  *   k, v         device bf16 [B, Hkv, T, D] under their strides
  *   parent       device int32 [B, T], T <= BAKLAVA_MAX_TREE

@@ -16,9 +16,10 @@
 // heads) forms the ancestors' part from the nodes' own keys and values, beside the first kernel, then waits for it and joins the partials.
 //
 // What bounds it (per layer; B200, 6.54 TB/s, 1.63 PFLOP/s): bf16 slabs the bytes once there are enough of them: 32 sequences, 8 heads
-// of 9 824 rows, 16 nodes of 32 heads: 228 us for 1.30 GB (5.7 TB/s with start, tail and join).  A single sequence of that shape is
-// 40 MB, 6.2 us of bytes, and takes 23: a block's way to its first tile, its last rows, the join.  Codes: the work between the bytes
-// and the product.  64 nodes over 16 sequences of FP8 rows 257 us (101 us of products at the peak rate), 8 nodes over 4-bit rows 196 us
+// of 9 824 rows, 16 nodes of 32 heads: 226 us for 1.30 GB (5.7 TB/s with start, tail and join) in a short run, 251 (5.2) for half a second and
+// longer, under the power cap.  A single sequence of that shape is 40 MB, 6.2 us of bytes, and takes 23: a block's way to its first
+// tile, its last rows, the join.  Codes: the work between the bytes and the product.  64 nodes over 16 sequences of FP8 rows 257 us
+// (101 us of products at the peak rate; the same in a long run), 8 nodes over 4-bit rows 193 us
 // (26.5 us of bytes): two softmax streams of one busy warp each, 5 200 cycles for 128 rows, and conversion beside them.
 #include <cuda_fp16.h>
 
@@ -572,7 +573,8 @@ template <int D, int R, int KV>
 __device__ __forceinline__ float query_factor(const TreeParams& p, const Item& it) {
     return KV == BAKLAVA_KV_FP8_E4M3 ? p.scale_log2 * p.c.kv_scale[((int64_t)p.layer * p.c.Hkv + it.h) * 4] : p.scale_log2;
 }
-// A query row of a quantised slab as operand in shared memory, in fp16.  FP8: exact.  4 bits: times the channels' scales, brought to
+// A query row of a quantised slab as operand in shared memory, in fp16.  FP8: as it is, which is exact from 2^-17 up (a
+// bf16 number has eight bits) and to 2^-25 below; the decode step has the same.  4 bits: times the channels' scales, brought to
 // 2^14 .. 2^15 by a power of two that `factor` takes back, in two terms: 22 bits of the largest (one term of 11 moves a row's
 // log-sum-exp by up to 5e-4).
 template <int D, int R, int KV>

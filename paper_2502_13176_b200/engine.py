@@ -179,7 +179,8 @@ class DecodeSession:
 
     def commit(self, path, n_path, t_pos, flags=0):
         """The accepted path (as `verify` returned it) into all layers' slabs: scores, append, eviction.  t_pos: device int32 [B],
-        the position of each path's first token; returns the next step's (of `tree_layer` and `commit` or of `step_varlen`).  4-bit rows have the bits that a decode step gives them."""
+        the position of each path's first token; returns the next step's (of `tree_layer` and `commit`, or of `step_varlen`).  4-bit
+        rows have the bits that a decode step gives them."""
         t_next = torch.empty_like(t_pos)
         bk.baklava_tree_commit(self.shape, self.cache, self.tree_q, self.tree_k, self.tree_v, self.tree_lse, path, n_path, self.max_path,
                                t_pos, t_next, flags | bk.FLAG_ROW_QUOTIENT, self.plan, self.commit_ws)
